@@ -559,6 +559,88 @@ mc_status mc_decode_attn_static(const mc_config* cfg, const mc_batch* batch, con
                                 int32_t layer_sel, const void* q, const void* k_new, const void* v_new,
                                 float sm_scale, void* out, float* lse, void* stream);
 
+/* ---- One uncompressed layer --------------------------------------------------------------------------------
+ * MiniCache merges the layers from S = L/2 upwards (Sec. 4.1); the layers below S keep ordinary caches.  The calls
+ * below attend such a layer during decode and keep its length bounded: mc_layer_attn (single-query attention, the
+ * step's rows appended in the same call), mc_layer_observe (the attention weight that a prompt's last queries give
+ * to every cached token) and mc_layer_evict (the rows with the least accumulated weight go).  (The paper has no
+ * counterpart: it leaves those layers to the serving engine.)  A layer that is evicted from has lengths of its own:
+ * give it a mc_batch of its own (its own seq_lens; a block table may be shared as long as the pages it names are
+ * this layer's slots). */
+
+/* One layer's cache.
+ * k_pool, v_pool  [n_pages][n_kv_heads][page_size][128] of cfg->dtype (the layer pools of mc_layer_kv)
+ * positions       [n_pages][n_kv_heads][page_size] int32: position of every cached row, or NULL: a row's token index
+ *                 is its position.  mc_layer_evict needs it (it fills holes with later rows, head by head, so that
+ *                 rows end up in another order in every head).  256-byte aligned.
+ * weights         [n_pages][n_kv_heads][page_size] fp32: accumulated attention weight of every cached row, or NULL
+ * status          [MC_STATUS_WORDS] int32, cleared by the caller; flags accumulate (MC_STATUS_FLAGS; the other words
+ *                 are not used) */
+typedef struct mc_layer_cache {
+  void* k_pool;
+  void* v_pool;
+  int32_t* positions;
+  float* weights;
+  int32_t* status;
+} mc_layer_cache;
+
+/* What a score is and which tokens a query sees.  For a query at position P and a cached row at position p:
+ *   s = sm_scale * q.k;   if softcap > 0: s = softcap * tanh(s / softcap);
+ *   if alibi_slopes: s -= alibi_slopes[query head] * (P - p)
+ *   seen  iff  p <= P  and  ( p < prefix_len[b]  or  ( p >= doc_start[b] and (window == 0 or P - p < window) ) )
+ * (a window behind a few prefix tokens; a packed document; a shared prefix that every document sees).  A row that
+ * is not seen has no influence whatever it holds.
+ * alibi_slopes  device [n_q_heads] fp32 or NULL
+ * doc_start     device [batch] int32 or NULL (0)
+ * prefix_len    device [batch] int32 or NULL (0)
+ * q_pos         device [batch] int32 or NULL.  mc_layer_attn: the query's position; NULL: seq_lens[b] with a new row,
+ *               seq_lens[b] - 1 without (the positions of a cache that was never evicted from).
+ *               mc_layer_observe: the position of the last query; NULL: seq_lens[b] - 1.  Below -1 counts as -1.
+ * softcap       0: none.  window: 0: none. */
+typedef struct mc_score_opts {
+  const float* alibi_slopes;
+  const int32_t* doc_start;
+  const int32_t* prefix_len;
+  const int32_t* q_pos;
+  float sm_scale;
+  float softcap;
+  int32_t window;
+  int32_t reserved;
+} mc_score_opts;
+
+/* Flags of mc_layer_attn / mc_layer_observe. */
+#define MC_LAYER_APPEND 1     /* write the new K and V rows (and, to a positions pool, q_pos) to slot seq_lens[b] */
+#define MC_LAYER_ACCUMULATE 2 /* add to layer->weights */
+
+/* Operations of mc_layer_workspace_bytes and the meaning of its `arg`: the flags the call will be made with
+ * (MC_OP_LAYER_ATTN), the number of observed queries (MC_OP_LAYER_OBSERVE), 0 (MC_OP_LAYER_EVICT). */
+enum { MC_OP_LAYER_ATTN = 2, MC_OP_LAYER_OBSERVE = 3, MC_OP_LAYER_EVICT = 4 };
+
+/* Scratch bytes a mc_layer_* call needs (a multiple of 256).  Pure host arithmetic; batch->block_table and seq_lens
+ * are not looked at.  Contents are irrelevant on entry and must stay untouched until the call has run. */
+mc_status mc_layer_workspace_bytes(const mc_config* cfg, const mc_batch* batch, int32_t op, int32_t arg, size_t* bytes);
+
+/* Single-query attention of every sequence over one layer's cache.
+ * q            [batch][n_q_heads][128]
+ * k_new, v_new [batch][n_kv_heads][128] rows of the step's new token, attended as token seq_lens[b] (its position is
+ *              q_pos with a positions pool, its index without one); both NULL to attend the cache alone
+ * flags        MC_LAYER_APPEND: the new rows are also written to the cache (the block table must hold their page;
+ *              seq_lens is not modified).  MC_LAYER_ACCUMULATE: weights of every seen row += the sum over its kv
+ *              head's query heads of the softmax probability; the appended row's weight is set to its own (without
+ *              this flag, to 0); a new row that is not appended leaves none.
+ * out          [batch][n_q_heads][128] cfg->dtype;  lse [batch][n_q_heads] fp32 natural log, or NULL
+ * workspace    mc_layer_workspace_bytes(MC_OP_LAYER_ATTN, flags) bytes, 256-byte aligned
+ * A query that sees nothing yields zeros and lse = -inf, and adds no weight.  Scores and sums are held in fp32; the
+ * probabilities are rounded once to cfg->dtype before they meet the values.  cfg->cache_bits must be 0 or 16; batch
+ * at most 512. */
+mc_status mc_layer_attn(const mc_config* cfg, const mc_batch* batch, const mc_layer_cache* layer, const mc_score_opts* opts,
+                        const void* q, const void* k_new, const void* v_new, int32_t flags, void* out, float* lse,
+                        void* workspace, size_t workspace_bytes, void* stream);
+
+/* Copies the layer's status words to `out_words[MC_STATUS_WORDS]` after synchronising `stream`; returns as
+ * mc_read_status does. */
+mc_status mc_layer_read_status(const mc_layer_cache* layer, void* stream, int32_t* out_words);
+
 /* Self-test of the error path of the bounded waits (the paper has no counterpart): enqueues a
  * one-warp kernel that waits, with the same bounded wait the streaming kernels use and a limit of
  * `poll_limit` polls, on a barrier that nothing completes.  The wait gives up, sets

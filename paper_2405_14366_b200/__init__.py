@@ -7,6 +7,8 @@ from .binding import (  # noqa: F401
     McConfig,
     PairCache,
     Batch,
+    LayerCache,
+    ScoreOpts,
     lib,
     MC_LAYER_LM1,
     MC_LAYER_L,
@@ -14,5 +16,10 @@ from .binding import (  # noqa: F401
     MC_RETAIN_DISTINCT,
     MC_RETAIN_LITERAL,
     MC_RETAIN_TOPK,
+    MC_LAYER_APPEND,
+    MC_LAYER_ACCUMULATE,
+    MC_OP_LAYER_ATTN,
+    MC_OP_LAYER_OBSERVE,
+    MC_OP_LAYER_EVICT,
     McError,
 )

@@ -16,6 +16,8 @@ MC_F16, MC_BF16 = 0, 1
 MC_RETAIN_DISTINCT, MC_RETAIN_LITERAL, MC_RETAIN_TOPK = 0, 1, 2
 MC_LAYER_LM1, MC_LAYER_L, MC_LAYER_BOTH = 0, 1, 2
 MC_OP_MERGE, MC_OP_DECODE_ATTN = 0, 1
+MC_OP_LAYER_ATTN, MC_OP_LAYER_OBSERVE, MC_OP_LAYER_EVICT = 2, 3, 4
+MC_LAYER_APPEND, MC_LAYER_ACCUMULATE = 1, 2
 MC_STATUS_WORDS = 4
 MC_STATUS_FLAGS, MC_STATUS_RETAINED_TOTAL, MC_STATUS_NEAR_THRESHOLD = 0, 1, 2
 MC_FLAG_RETAIN_OVERFLOW, MC_FLAG_WAIT_TIMEOUT, MC_FLAG_BAD_METADATA, MC_FLAG_BOUNDS = 1, 2, 4, 8
@@ -66,6 +68,16 @@ class _PairCache(C.Structure):
                 ("status", C.c_void_p), ("res_k", C.c_void_p), ("res_v", C.c_void_p)]
 
 
+class _LayerCache(C.Structure):
+    _fields_ = [("k_pool", C.c_void_p), ("v_pool", C.c_void_p), ("positions", C.c_void_p), ("weights", C.c_void_p),
+                ("status", C.c_void_p)]
+
+
+class _ScoreOpts(C.Structure):
+    _fields_ = [("alibi_slopes", C.c_void_p), ("doc_start", C.c_void_p), ("prefix_len", C.c_void_p), ("q_pos", C.c_void_p),
+                ("sm_scale", C.c_float), ("softcap", C.c_float), ("window", C.c_int32), ("reserved", C.c_int32)]
+
+
 class _PairSizes(C.Structure):
     _fields_ = [("tile_bytes", C.c_size_t), ("e_bytes", C.c_size_t), ("dist_bytes", C.c_size_t),
                 ("ret_count_bytes", C.c_size_t), ("ret_offset_bytes", C.c_size_t), ("ret_index_bytes", C.c_size_t),
@@ -82,7 +94,8 @@ class _Stats(C.Structure):
 
 EXPORTS = ("mc_decode_drain_host", "mc_decode_stage_host", "mc_decode_attn_append", "mc_prefill_merge_pair", "mc_admit_sequences", "mc_build_flags", "mc_merge_pairs", "mc_pair_bytes", "mc_get_stats", "mc_version", "mc_status_str", "mc_last_cuda_error", "mc_workspace_bytes", "mc_merge_pair",
            "mc_append_pair", "mc_restore", "mc_decode_attn", "mc_read_status", "mc_merge_pair_host",
-           "mc_decode_attn_host", "mc_decode_io_bytes", "mc_decode_attn_static", "mc_merge_pair_q4", "mc_selftest_wait_timeout")
+           "mc_decode_attn_host", "mc_decode_io_bytes", "mc_decode_attn_static", "mc_merge_pair_q4", "mc_selftest_wait_timeout",
+           "mc_layer_workspace_bytes", "mc_layer_attn", "mc_layer_read_status")
 
 
 def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
@@ -277,6 +290,57 @@ class PairCache:
         return sum(t.numel() * t.element_size() for t in ts)
 
 
+def _typed(name: str, t: Optional[torch.Tensor], dtype) -> Optional[int]:
+    assert t is None or (t.dtype == dtype and t.is_contiguous()), f"{name}: a contiguous {dtype} tensor is wanted"
+    return _ptr(t)
+
+
+@dataclasses.dataclass
+class LayerCache:
+    """One uncompressed layer's paged cache (caller-owned tensors, see mc_layer_cache): k_pool / v_pool
+    [n_pages][n_kv_heads][page_size][128] in the storage type, positions int32 / weights float32
+    [n_pages][n_kv_heads][page_size] or None, status int32 [MC_STATUS_WORDS] (zeros; made here if not given)."""
+    cfg: McConfig
+    k_pool: torch.Tensor
+    v_pool: torch.Tensor
+    positions: Optional[torch.Tensor] = None
+    weights: Optional[torch.Tensor] = None
+    status: Optional[torch.Tensor] = None
+
+    def __post_init__(self):
+        if self.status is None:
+            self.status = torch.zeros(MC_STATUS_WORDS, dtype=torch.int32, device=self.k_pool.device)
+
+    def c(self, n_pages: int) -> _LayerCache:
+        dt, rows = self.cfg.torch_dtype, n_pages * self.cfg.n_kv_heads * self.cfg.page_size
+        for t, n in ((self.k_pool, 128 * rows), (self.v_pool, 128 * rows), (self.positions, rows), (self.weights, rows),
+                     (self.status, MC_STATUS_WORDS)):
+            assert t is None or t.numel() >= n, "a pool holds fewer than n_pages pages"
+        return _LayerCache(_typed("k_pool", self.k_pool, dt), _typed("v_pool", self.v_pool, dt),
+                           _typed("positions", self.positions, torch.int32), _typed("weights", self.weights, torch.float32),
+                           _typed("status", self.status, torch.int32))
+
+
+@dataclasses.dataclass
+class ScoreOpts:
+    """How a score is formed and which tokens a query sees (see mc_score_opts).  Tensors live on the device:
+    alibi_slopes float32 [n_q_heads]; doc_start, prefix_len, q_pos int32 [batch]."""
+    sm_scale: float
+    softcap: float = 0.0
+    alibi_slopes: Optional[torch.Tensor] = None
+    window: int = 0
+    doc_start: Optional[torch.Tensor] = None
+    prefix_len: Optional[torch.Tensor] = None
+    q_pos: Optional[torch.Tensor] = None
+
+    def c(self, cfg: McConfig, batch: int) -> _ScoreOpts:
+        for t, n in ((self.alibi_slopes, cfg.n_q_heads), (self.doc_start, batch), (self.prefix_len, batch), (self.q_pos, batch)):
+            assert t is None or t.numel() >= n, "a score option holds too few entries"
+        return _ScoreOpts(_typed("alibi_slopes", self.alibi_slopes, torch.float32), _typed("doc_start", self.doc_start, torch.int32),
+                          _typed("prefix_len", self.prefix_len, torch.int32), _typed("q_pos", self.q_pos, torch.int32),
+                          float(self.sm_scale), float(self.softcap), int(self.window), 0)
+
+
 class MiniCacheLib:
     """Loads libminicache.so and exposes its entry points under their C names."""
 
@@ -331,6 +395,11 @@ class MiniCacheLib:
         L.mc_merge_pair_q4.argtypes = [P(_Config), P(_Batch), P(_LayerQ4), P(_LayerQ4), P(_PairCache), C.c_int32, V,
                                        C.c_size_t, V]
         L.mc_merge_pair_q4.restype = C.c_int32
+        L.mc_layer_workspace_bytes.argtypes = [P(_Config), P(_Batch), C.c_int32, C.c_int32, P(C.c_size_t)]
+        L.mc_layer_attn.argtypes = [P(_Config), P(_Batch), P(_LayerCache), P(_ScoreOpts), V, V, V, C.c_int32, V, V, V, C.c_size_t, V]
+        L.mc_layer_read_status.argtypes = [P(_LayerCache), V, P(C.c_int32)]
+        for f in ("mc_layer_workspace_bytes", "mc_layer_attn", "mc_layer_read_status"):
+            getattr(L, f).restype = C.c_int32
         L.mc_selftest_wait_timeout.argtypes = [P(_PairCache), C.c_int32, V]
         L.mc_selftest_wait_timeout.restype = C.c_int32
         for f in ("mc_workspace_bytes", "mc_merge_pair", "mc_append_pair", "mc_restore", "mc_decode_attn",
@@ -536,6 +605,37 @@ class MiniCacheLib:
         if code == 5:
             raise McError(code, "MC_ERR_CAPACITY", self._lib.mc_last_cuda_error().decode())
         self._check(code)
+
+    # -- one uncompressed layer -------------------------------------------------------------------
+    def mc_layer_workspace_bytes(self, cfg: McConfig, batch: Batch, op: int, arg: int = 0) -> int:
+        """arg: the call's flags (MC_OP_LAYER_ATTN), the number of observed queries (MC_OP_LAYER_OBSERVE), 0 (MC_OP_LAYER_EVICT)."""
+        out = C.c_size_t(0)
+        c, b = cfg.c(), batch.c()
+        self._check(self._lib.mc_layer_workspace_bytes(C.byref(c), C.byref(b), int(op), int(arg), C.byref(out)))
+        return out.value
+
+    def mc_layer_attn(self, cfg: McConfig, batch: Batch, layer: LayerCache, opts: ScoreOpts, q, k_new, v_new, flags: int, out, lse,
+                      workspace: torch.Tensor, stream=None):
+        """q, out [batch][n_q_heads][128], k_new / v_new [batch][n_kv_heads][128] or None; flags: MC_LAYER_APPEND |
+        MC_LAYER_ACCUMULATE; lse [batch][n_q_heads] float32 or None."""
+        c, b = cfg.c(), batch.c()
+        n, dt = b.batch, cfg.torch_dtype
+        for t, heads in ((q, cfg.n_q_heads), (out, cfg.n_q_heads), (k_new, cfg.n_kv_heads), (v_new, cfg.n_kv_heads)):
+            assert t is None or t.numel() == n * heads * 128, "rows of 128 channels per sequence and head are wanted"
+        assert lse is None or lse.numel() == n * cfg.n_q_heads
+        l, o = layer.c(b.n_pages), opts.c(cfg, n)
+        self._check(self._lib.mc_layer_attn(C.byref(c), C.byref(b), C.byref(l), C.byref(o), _typed("q", q, dt),
+                                            _typed("k_new", k_new, dt), _typed("v_new", v_new, dt), int(flags),
+                                            _typed("out", out, dt), _typed("lse", lse, torch.float32), _ptr(workspace),
+                                            workspace.numel() * workspace.element_size(), _stream(stream)))
+
+    def mc_layer_read_status(self, layer: LayerCache, stream=None, check: bool = True):
+        words = (C.c_int32 * MC_STATUS_WORDS)()
+        l = layer.c(0)
+        code = self._lib.mc_layer_read_status(C.byref(l), _stream(stream), words)
+        if check:
+            self._check(code)
+        return list(words), code
 
     def mc_selftest_wait_timeout(self, pair: PairCache, poll_limit: int = 20000, stream=None):
         pc = pair.c()

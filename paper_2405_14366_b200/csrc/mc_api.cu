@@ -10,6 +10,7 @@
 #include "mc_common.cuh"
 #include "mc_items.cuh"
 #include "mc_kernels.h"
+#include "mc_layer.h"
 #include "mc_append.cuh"
 #include "mc_q4.cuh"
 
@@ -696,6 +697,74 @@ mc_status mc_decode_drain_host(const mc_config* cfg, const mc_batch* batch, int3
   MC_CUDA_CHECK(cudaMemcpyAsync(out_host, out_dev, rows * kRowBytes, cudaMemcpyDeviceToHost, (cudaStream_t)stream));
   if (lse_host) MC_CUDA_CHECK(cudaMemcpyAsync(lse_host, lse_dev, rows * sizeof(float), cudaMemcpyDeviceToHost, (cudaStream_t)stream));
   return MC_OK;
+}
+
+// ---- one uncompressed layer ------------------------------------------------------------------------
+// What every mc_layer_* call checks about its configuration, batch and cache.
+static mc_status check_layer(const mc_config* cfg, const mc_batch* batch, const mc_layer_cache* layer) {
+  mc_status st = check_config(cfg);
+  if (st != MC_OK) return st;
+  st = check_batch(cfg, batch);
+  if (st != MC_OK) return st;
+  if (cfg->cache_bits == 4) return MC_ERR_UNSUPPORTED;
+  if (batch->batch > kMaxLayerBatch) return MC_ERR_SHAPE;
+  if (batch->batch > 0 && batch->n_pages == 0) return MC_ERR_INVALID_ARG;  // (a bad page id reads page 0: there has to be one)
+  if (!layer || !layer->k_pool || !layer->v_pool || !layer->status) return MC_ERR_INVALID_ARG;
+  if (!aligned256(layer->k_pool) || !aligned256(layer->v_pool) || !aligned256(layer->positions) || !aligned256(layer->weights))
+    return MC_ERR_ALIGN;
+  if (((uintptr_t)layer->status) & 3u) return MC_ERR_ALIGN;
+  return MC_OK;
+}
+
+static mc_status check_score_opts(const mc_score_opts* o) {
+  if (o == nullptr || o->window < 0 || !(o->softcap >= 0.f) || o->softcap > 3.0e38f || !(o->sm_scale == o->sm_scale) ||
+      o->sm_scale > 3.0e38f || o->sm_scale < -3.0e38f)
+    return MC_ERR_INVALID_ARG;
+  const uintptr_t al = (uintptr_t)o->alibi_slopes | (uintptr_t)o->doc_start | (uintptr_t)o->prefix_len | (uintptr_t)o->q_pos;
+  return (al & 3u) ? MC_ERR_ALIGN : MC_OK;
+}
+
+mc_status mc_layer_workspace_bytes(const mc_config* cfg, const mc_batch* batch, int32_t op, int32_t arg, size_t* bytes) {
+  mc_status st = check_config(cfg);
+  if (st != MC_OK) return st;
+  if (batch == nullptr || bytes == nullptr) return MC_ERR_INVALID_ARG;
+  if (batch->batch < 0 || batch->max_seq_len < 0) return MC_ERR_INVALID_ARG;
+  switch (op) {
+    case MC_OP_LAYER_ATTN:
+      if (arg & ~(MC_LAYER_APPEND | MC_LAYER_ACCUMULATE)) return MC_ERR_INVALID_ARG;
+      *bytes = layer_attn_workspace_bytes(cfg, batch, arg) + 256;
+      return MC_OK;
+    default:
+      return MC_ERR_INVALID_ARG;
+  }
+}
+
+mc_status mc_layer_attn(const mc_config* cfg, const mc_batch* batch, const mc_layer_cache* layer, const mc_score_opts* opts,
+                        const void* q, const void* k_new, const void* v_new, int32_t flags, void* out, float* lse, void* workspace,
+                        size_t workspace_bytes, void* stream) {
+  ApiRange range_("mc_layer_attn");
+  mc_status st = check_layer(cfg, batch, layer);
+  if (st != MC_OK) return st;
+  st = check_score_opts(opts);
+  if (st != MC_OK) return st;
+  if (!q || !out || (k_new == nullptr) != (v_new == nullptr)) return MC_ERR_INVALID_ARG;
+  if (flags & ~(MC_LAYER_APPEND | MC_LAYER_ACCUMULATE)) return MC_ERR_INVALID_ARG;
+  if ((flags & MC_LAYER_APPEND) && !k_new) return MC_ERR_INVALID_ARG;
+  if ((flags & MC_LAYER_ACCUMULATE) && !layer->weights) return MC_ERR_INVALID_ARG;
+  if (((uintptr_t)q | (uintptr_t)out | (uintptr_t)k_new | (uintptr_t)v_new) & 15u) return MC_ERR_ALIGN;
+  if (((uintptr_t)lse) & 3u) return MC_ERR_ALIGN;
+  if (workspace == nullptr || !aligned256(workspace)) return workspace ? MC_ERR_ALIGN : MC_ERR_INVALID_ARG;
+  if (workspace_bytes < layer_attn_workspace_bytes(cfg, batch, flags)) return MC_ERR_CAPACITY;
+  return launch_layer_attn(cfg, batch, make_geom(cfg, batch), layer, opts, q, k_new, v_new, flags, out, lse, workspace,
+                           (cudaStream_t)stream);
+}
+
+mc_status mc_layer_read_status(const mc_layer_cache* layer, void* stream, int32_t* out_words) {
+  if (layer == nullptr || layer->status == nullptr || out_words == nullptr) return MC_ERR_INVALID_ARG;
+  MC_CUDA_CHECK(cudaMemcpyAsync(out_words, layer->status, MC_STATUS_WORDS * sizeof(int32_t), cudaMemcpyDeviceToHost,
+                                (cudaStream_t)stream));
+  MC_CUDA_CHECK(cudaStreamSynchronize((cudaStream_t)stream));
+  return out_words[MC_STATUS_FLAGS] != 0 ? MC_ERR_DEVICE_STATUS : MC_OK;
 }
 
 mc_status mc_selftest_wait_timeout(const mc_pair_cache* pair, int32_t poll_limit, void* stream) {

@@ -1,0 +1,14 @@
+// Internal launch interface of the operators of an uncompressed layer's cache (mc_layer_*).
+#pragma once
+#include "mc_common.cuh"
+
+namespace mc {
+
+constexpr int kMaxLayerBatch = 512;  // sequences whose unit prefix lives in shared memory
+
+size_t layer_attn_workspace_bytes(const mc_config* cfg, const mc_batch* bt, int flags);
+mc_status launch_layer_attn(const mc_config* cfg, const mc_batch* bt, const Geom& g, const mc_layer_cache* layer,
+                            const mc_score_opts* opts, const void* q, const void* k_new, const void* v_new, int flags, void* out,
+                            float* lse, void* workspace, cudaStream_t stream);
+
+}  // namespace mc

@@ -1,0 +1,792 @@
+// Single-query decode attention over one uncompressed layer's paged cache: the layers below MiniCache's start layer
+// S (Sec. 4.1 merges S .. L-1 only; the others keep their K and V as they are).
+//
+//   s_i = cap tanh(sm q.k_i / cap) - slope_h (q_pos - p_i)      (cap, slope: optional)
+//   out = sum_i softmax(s)_i v_i  over the tokens that the query sees (causal, window, document, prefix)
+//
+// One pass over the cache with a running maximum and sum.  The token axis is cut into units of 128 tokens (only units
+// that hold a visible token are counted); the grid is T teams of S CTAs, a team takes an equal share of the units of
+// the batch, its member j takes them for the kv heads j, j + S, ...: the split of mc_attn.cu, for the same reason
+// (equal shares whatever the lengths are, neighbouring tiles of a page streamed at about the same time).
+// A warp owns 16-token slices of its CTA's units and is a pipeline of its own: it streams their K and V rows through
+// its ring of stages with tiled bulk copies (128-byte swizzle; its lane 0 issues them, an mbarrier per stage counts
+// the bytes) and consumes them itself, so nothing but the end of a piece -- the units of one (sequence, kv head) in
+// the team's share -- makes the four warps wait for one another.  Scores never leave registers: D = K q^T
+// (16 tokens x 8 query rows) becomes the B operand of V^T P by two 8x8 transposes (movmatrix).
+// Where a slice's rows come from is worked out a lane per slice, 32 slices at a time and one window ahead: a
+// dependent load takes microseconds while the copies saturate the memory system.
+#include <algorithm>
+
+#include "mc_layer.cuh"
+#include "mc_layer.h"
+#include "mc_kernels.h"
+#include "mc_mma.cuh"
+#include "mc_pipe.cuh"
+#include "mc_tc.cuh"
+
+namespace mc {
+
+constexpr int kLaUnit = 128;   // tokens per unit of work
+constexpr int kLaSlice = 16;   // tokens per stage: one k step of the V contraction, never more than a page
+constexpr int kLaWarps = 4;
+constexpr int kLaThreads = kLaWarps * 32;
+constexpr int kLaStages = 3;
+constexpr int kLaStageBytes = 2 * kLaSlice * kRowBytes;  // K rows, V rows: 8 KB
+constexpr int kLaRows = 8;                               // query rows per kv head: the 8-wide N tile
+constexpr int kLaSlab = 132;                             // floats per row of a partial output in shared memory
+constexpr int kLaCtasPerSm = 2;
+constexpr int kLaBoxBytes = kLaSlice * 128;              // one copy: 16 rows x 64 channels
+
+struct LayerAttnParams {
+  Geom g;
+  ScoreRule rule;
+  char* k_pool;
+  char* v_pool;
+  int32_t* positions;
+  float* weights;
+  int32_t* status;
+  const char* q;
+  const char* k_new;
+  const char* v_new;
+  float* part_o;   // [piece][nq rows of a head]...: [(team + sequence)][n_q_heads][128]
+  float* part_ml;  // [(team + sequence)][n_q_heads][2]
+  float* scores;   // [unit][n_kv_heads][128][nq], null unless weights are gathered
+  int nq, n_q_heads;
+  int team_size, n_teams;
+  int flags;
+};
+
+// A sequence as the call sees it: its view, and the units that hold a visible token: the first `ua`, then those from
+// `ub0` on, `u` in all.  (A cache with positions may hold them in any order: every unit counts.)
+struct Seq {
+  View view;
+  int n, n_tot;  // cached tokens; with the step's new one
+  int a, lo, hi; // visible indices [0, a) and [lo, hi) (no positions pool)
+  int ua, ub0, u;
+  bool bad;
+};
+__device__ __forceinline__ Seq seq_of(const LayerAttnParams& p, int b) {
+  Seq s;
+  const int raw = p.g.seq_lens[b];
+  s.bad = raw < 0 || raw > p.g.max_seq_len;
+  s.n = min(max(raw, 0), p.g.max_seq_len);
+  s.n_tot = s.n + (p.k_new != nullptr ? 1 : 0);
+  s.view = view_at(p.rule, b, max(p.rule.q_pos ? p.rule.q_pos[b] : s.n_tot - 1, -1));
+  s.a = s.lo = 0;
+  s.hi = s.n_tot;
+  s.ua = (s.n_tot + kLaUnit - 1) / kLaUnit;
+  s.ub0 = s.ua;
+  s.u = s.ua;
+  if (p.positions == nullptr) {
+    const int end = min(s.n_tot - 1, s.view.q_pos) + 1;  // one past the last index the query may see
+    s.a = max(min(end, s.view.prefix), 0);
+    s.lo = max(s.view.lo_pos, s.a);
+    s.hi = end;
+    s.ua = (s.a + kLaUnit - 1) / kLaUnit;
+    s.ub0 = s.ua;
+    int ub1 = s.ua;
+    if (s.hi > s.lo) {
+      s.ub0 = max(s.lo / kLaUnit, s.ua);
+      ub1 = max((s.hi + kLaUnit - 1) / kLaUnit, s.ub0);
+    }
+    if (p.flags & MC_LAYER_APPEND) {  // the unit of the appended row counts whether the query sees it or not
+      const int un = s.n / kLaUnit;
+      if (ub1 <= s.ub0) s.ub0 = ub1 = max(un, s.ua);
+      if (ub1 <= un) ub1 = un + 1;
+    }
+    s.u = s.ua + (ub1 - s.ub0);
+  }
+  return s;
+}
+
+// Exclusive prefix of the sequences' unit counts in shared memory: pre[batch] = all units.  Every thread calls it.
+__device__ __forceinline__ void unit_prefix(const LayerAttnParams& p, int* pre, int n_threads, int& bad) {
+  const int tid = threadIdx.x, lane = tid & 31;
+  for (int b = tid; b < p.g.batch; b += n_threads) {
+    const Seq s = seq_of(p, b);
+    bad |= s.bad ? 1 : 0;
+    pre[b + 1] = s.u;
+  }
+  __syncthreads();
+  if (tid < 32) {
+    const int per = (p.g.batch + 31) / 32;
+    const int b0 = min(lane * per, p.g.batch), b1 = min(b0 + per, p.g.batch);
+    int sum = 0;
+    for (int b = b0; b < b1; ++b) sum += pre[b + 1];
+    int incl = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int v = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += v;
+    }
+    int acc = incl - sum;
+    for (int b = b0; b < b1; ++b) {
+      acc += pre[b + 1];
+      pre[b + 1] = acc;
+    }
+    if (lane == 0) pre[0] = 0;
+  }
+  __syncthreads();
+}
+
+__device__ __forceinline__ int seq_of_unit(const int* pre, int batch, int x) {
+  int lo = 0, hi = batch - 1;  // last b with pre[b] <= x
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (pre[mid] <= x) lo = mid; else hi = mid - 1;
+  }
+  return lo;
+}
+
+// Teams that get any units: no team's share is empty, so a sequence's pieces are consecutive teams.
+__device__ __forceinline__ int live_teams(const LayerAttnParams& p, int n_units) { return min(p.n_teams, max(n_units, 1)); }
+
+// One slice as a lane of the window knows it.
+struct Slice {
+  int head, b, t0;  // kv head, sequence, first token
+  int x;            // unit (global)
+  int page;         // raw page id (looked at one window later)
+  int flags;
+};
+enum { kSlTokens = 1, kSlLoad = 2, kSlFirst = 4, kSlLast = 8, kSlBadSlot = 16 };
+
+template <int DT>
+__device__ __forceinline__ uint32_t transpose8(uint32_t v) {
+  uint32_t r;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+  return r;
+}
+
+template <int DT>
+__global__ void __launch_bounds__(kLaThreads, kLaCtasPerSm)
+layer_attn_split_kernel(const __grid_constant__ LayerAttnParams p, const __grid_constant__ CUtensorMap map_k,
+                        const __grid_constant__ CUtensorMap map_v) {
+  // (lengths, block table, score options and queries are the caller's: read before the wait, as in mc_attn.cu)
+  grid_dep_launch();
+  extern __shared__ unsigned char smem_raw[];
+  unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  float* slab = reinterpret_cast<float*>(smem + kLaWarps * kLaStages * kLaStageBytes);  // [2][kLaRows][kLaSlab]
+  float* ml_s = slab + 2 * kLaRows * kLaSlab;                                           // [2][kLaRows][2]
+  int* pos_s = reinterpret_cast<int*>(ml_s + 2 * kLaRows * 2);                          // [warps][stages][16]
+  uint64_t* bars = reinterpret_cast<uint64_t*>(pos_s + kLaWarps * kLaStages * kLaSlice);  // [warps][stages]
+  int* pre_s = reinterpret_cast<int*>(bars + kLaWarps * kLaStages);                     // [batch + 1]
+  volatile int* s_abort = pre_s + p.g.batch + 1;
+
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int row = lane >> 2, t4 = lane & 3, colp = 2 * t4;
+  const int mi = lane >> 3, mr = lane & 7;
+  const int H = p.g.n_kv_heads, nq = p.nq, shift = p.g.page_shift;
+  const uint32_t bar0 = smem_u32(bars + warp * kLaStages);
+  const uint32_t st0 = smem_u32(smem) + warp * kLaStages * kLaStageBytes;
+  const uint32_t pos0 = smem_u32(pos_s + warp * kLaStages * kLaSlice);
+
+  if (tid == 0) {
+    for (int s = 0; s < kLaWarps * kLaStages; ++s) mbar_init(smem_u32(bars + s), 1);
+    *s_abort = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  int bad = 0;
+  unit_prefix(p, pre_s, kLaThreads, bad);  // (ends with a barrier)
+  const int n_units = pre_s[p.g.batch];
+  const int teams = live_teams(p, n_units);
+  const int team = blockIdx.x / p.team_size, member = blockIdx.x % p.team_size;
+  int x_begin = 0, x_end = 0;
+  if (team < teams) {
+    x_begin = (int)((long long)n_units * team / teams);
+    x_end = (int)((long long)n_units * (team + 1) / teams);
+  }
+  const int nx = x_end - x_begin;
+  const int n_heads = member < H ? (H - member + p.team_size - 1) / p.team_size : 0;
+  const int n_slices = 2 * nx * n_heads;  // of each warp
+
+  // slice i of this warp: head by head, unit by unit, the slices `warp` and `warp + 4` of a unit
+  auto load_slice = [&](int i) {
+    Slice s;
+    s.head = s.b = s.t0 = s.x = s.page = s.flags = 0;
+    if (i >= n_slices) return s;
+    const int hd = i / (2 * nx), rem = i - hd * 2 * nx;
+    s.head = member + hd * p.team_size;
+    s.x = x_begin + (rem >> 1);
+    s.b = seq_of_unit(pre_s, p.g.batch, s.x);
+    const Seq q = seq_of(p, s.b);
+    const int k = s.x - pre_s[s.b];
+    s.t0 = (k < q.ua ? k : q.ub0 + k - q.ua) * kLaUnit + (warp + 4 * (rem & 1)) * kLaSlice;
+    if (s.t0 < q.n_tot) s.flags |= kSlTokens;
+    if (s.t0 < q.n) s.flags |= kSlLoad;
+    if (!(rem & 1) && (s.x == x_begin || k == 0)) s.flags |= kSlFirst;
+    if ((rem & 1) && (s.x + 1 == x_end || k + 1 == q.u)) s.flags |= kSlLast;
+    if ((s.flags & kSlLoad) || ((s.flags & kSlTokens) && (p.flags & MC_LAYER_APPEND))) {
+      const int slot = s.t0 >> shift;
+      if (slot < p.g.max_pages_per_seq) s.page = p.g.block_table[(size_t)s.b * p.g.max_pages_per_seq + slot];
+      else s.flags |= kSlBadSlot;
+    }
+    return s;
+  };
+  Slice win = load_slice(lane), nxt = load_slice(32 + lane);
+
+  auto load_q = [&](int b, int head, uint32_t (&q0)[8], uint32_t (&q2)[8]) {
+    // B fragment: query row `row`, channels 16 ks + 2 t4 + {0, 1} and + {8, 9}
+    const uint32_t* src = reinterpret_cast<const uint32_t*>(p.q) + ((size_t)b * p.n_q_heads + head * nq + row) * (kHeadDim / 2) + t4;
+#pragma unroll
+    for (int ks = 0; ks < 8; ++ks) {
+      q0[ks] = row < nq ? src[8 * ks] : 0u;
+      q2[ks] = row < nq ? src[8 * ks + 4] : 0u;
+    }
+  };
+  uint32_t q0[8], q2[8];
+  {
+    const int b = __shfl_sync(0xffffffffu, win.b, 0), h = __shfl_sync(0xffffffffu, win.head, 0);
+    if (n_slices > 0) load_q(b, h, q0, q2);
+  }
+
+  grid_dep_wait();
+  if (bad) atomicOr(p.status, MC_FLAG_BAD_METADATA);
+
+  // row (of the pools' rows) where a slice begins; a page id outside the pools reads page 0 and is flagged
+  auto slice_row = [&](int page, int head, int t0) {
+    if (!page_ok(p.g, page)) page = 0;
+    return (page * H + head) * p.g.page_size + (t0 & (p.g.page_size - 1));
+  };
+  auto issue = [&](int i) {  // slice i into its stage
+    if (i >= n_slices) return;
+    const int src = i & 31;
+    // (i lies in the current window or, at its end, in the next one)
+    const bool ahead = i >= 32 && (i & 31) < kLaStages - 1;
+    const int fl = __shfl_sync(0xffffffffu, ahead ? nxt.flags : win.flags, src);
+    const int page = __shfl_sync(0xffffffffu, ahead ? nxt.page : win.page, src);
+    const int head = __shfl_sync(0xffffffffu, ahead ? nxt.head : win.head, src);
+    const int t0 = __shfl_sync(0xffffffffu, ahead ? nxt.t0 : win.t0, src);
+    const int s = i % kLaStages;
+    if (!(fl & kSlLoad) || *s_abort) return;
+    if (lane == 0) {
+      if ((fl & kSlBadSlot) || !page_ok(p.g, page)) atomicOr(p.status, MC_FLAG_BAD_METADATA);
+      const int y = slice_row(page, head, t0);
+      const uint32_t bar = bar0 + 8 * s, dst = st0 + s * kLaStageBytes;
+      mbar_expect_tx(bar, (uint32_t)(kLaStageBytes + (p.positions ? kLaSlice * 4 : 0)));
+      tma_load_2d(dst, &map_k, 0, y, bar);
+      tma_load_2d(dst + kLaBoxBytes, &map_k, 64, y, bar);
+      tma_load_2d(dst + 2 * kLaBoxBytes, &map_v, 0, y, bar);
+      tma_load_2d(dst + 3 * kLaBoxBytes, &map_v, 64, y, bar);
+      if (p.positions) bulk_load(pos0 + s * kLaSlice * 4, p.positions + y, kLaSlice * 4, bar);
+    }
+  };
+  for (int i = 0; i < kLaStages - 1; ++i) issue(i);
+
+  float acc[8][4];
+  float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;  // query rows colp, colp + 1
+  float sl0 = 0.f, sl1 = 0.f;
+  Seq sq = {};
+  uint32_t phase = 0;  // bit s: parity of stage s's next completion
+
+  for (int i = 0; i < n_slices; ++i) {
+    const int src = i & 31;
+    if (src == 0 && i > 0) {
+      win = nxt;
+      nxt = load_slice((i & ~31) + 32 + lane);
+    }
+    // the stage of the slice before this one is free: its warp has read it
+    __syncwarp();
+    issue(i + kLaStages - 1);
+    const int fl = __shfl_sync(0xffffffffu, win.flags, src);
+    const int b = __shfl_sync(0xffffffffu, win.b, src);
+    const int head = __shfl_sync(0xffffffffu, win.head, src);
+    const int t0 = __shfl_sync(0xffffffffu, win.t0, src);
+    const int s = i % kLaStages;
+    if (fl & kSlFirst) {
+      m0 = m1 = -INFINITY;
+      l0 = l1 = 0.f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) acc[j][k] = 0.f;
+      sq = seq_of(p, b);
+      if (p.rule.slopes) {
+        sl0 = colp < nq ? p.rule.slopes[head * nq + colp] * kLog2e : 0.f;
+        sl1 = colp + 1 < nq ? p.rule.slopes[head * nq + colp + 1] * kLog2e : 0.f;
+      }
+    }
+    if (fl & kSlTokens) {
+      const uint32_t sb = st0 + s * kLaStageBytes;
+      const bool has_new = p.k_new != nullptr && sq.n >= t0 && sq.n < t0 + kLaSlice;  // (warp-uniform)
+      uint4 rown = make_uint4(0u, 0u, 0u, 0u);
+      if (has_new) {  // lanes 0..15: the new K row's chunks, 16..31: the V row's
+        const char* src_row = (lane < 16 ? p.k_new : p.v_new) + ((size_t)b * H + head) * kRowBytes;
+        rown = *reinterpret_cast<const uint4*>(src_row + (lane & 15) * 16);
+      }
+      if (fl & kSlLoad) {
+        mbar_wait(bar0 + 8 * s, (phase >> s) & 1, s_abort, p.status);  // (on a time-out the CTA only runs to its end)
+        phase ^= 1u << s;
+      }
+      bool wrote = false;
+      if (has_new) {
+        // the step's row takes its place in the stage (its slot of the page holds nothing yet) and, on request, in the cache
+        const int r = sq.n - t0, c = lane & 15;
+        const uint32_t a = sb + (lane < 16 ? 0 : 2 * kLaBoxBytes) + (c >> 3) * kLaBoxBytes + r * 128 + (((c & 7) ^ (r & 7)) << 4);
+        asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(a), "r"(rown.x), "r"(rown.y), "r"(rown.z), "r"(rown.w) : "memory");
+        wrote = true;
+        if (p.positions && lane == 0) pos_s[(warp * kLaStages + s) * kLaSlice + r] = sq.view.q_pos;
+        if (p.flags & MC_LAYER_APPEND) {
+          const int page = __shfl_sync(0xffffffffu, win.page, src);
+          if (!(fl & kSlBadSlot) && page_ok(p.g, page)) {
+            const size_t at = (size_t)slice_row(page, head, t0) + r;
+            *reinterpret_cast<uint4*>((lane < 16 ? p.k_pool : p.v_pool) + at * kRowBytes + c * 16) = rown;
+            if (p.positions && lane == 0) p.positions[at] = sq.view.q_pos;
+            if (p.weights && !(p.flags & MC_LAYER_ACCUMULATE) && lane == 0) p.weights[at] = 0.f;
+          } else if (lane == 0) {
+            atomicOr(p.status, MC_FLAG_BAD_METADATA);
+          }
+        }
+        __syncwarp();
+      }
+      // ---- scores: D[token][query row], even and odd k steps summed apart
+      float d0[4] = {0.f, 0.f, 0.f, 0.f}, d1[4] = {0.f, 0.f, 0.f, 0.f};
+      {
+        const int tr = (mi & 1) * 8 + mr;
+        uint32_t ra[8][4];
+#pragma unroll
+        for (int ks = 0; ks < 8; ++ks) {
+          const int c = 2 * ks + (mi >> 1);
+          ldsm_x4(sb + (c >> 3) * kLaBoxBytes + tr * 128 + (((c & 7) ^ mr) << 4), ra[ks][0], ra[ks][1], ra[ks][2], ra[ks][3]);
+        }
+#pragma unroll
+        for (int ks = 0; ks < 8; ks += 2) {
+          mma_rows<DT>(d0, ra[ks][0], ra[ks][1], ra[ks][2], ra[ks][3], q0[ks], q2[ks]);
+          mma_rows<DT>(d1, ra[ks + 1][0], ra[ks + 1][1], ra[ks + 1][2], ra[ks + 1][3], q0[ks + 1], q2[ks + 1]);
+        }
+      }
+      float sc[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) sc[k] = score_of(p.rule, d0[k] + d1[k]);
+      // ---- distance bias and masks (tokens t0 + row and + 8)
+      uint32_t hidden = 0;  // bit r: token t0 + r is not seen (the same in every lane)
+      {
+        int p0 = t0 + row, p8 = p0 + 8;
+        bool v0 = true, v8 = true, whole;
+        if (p.positions) {
+          const int* ps = pos_s + (warp * kLaStages + s) * kLaSlice;
+          v0 = p0 < sq.n_tot;
+          v8 = p8 < sq.n_tot;
+          p0 = ps[row];
+          p8 = ps[row + 8];
+          v0 = v0 && sq.view.sees(p0);
+          v8 = v8 && sq.view.sees(p8);
+          whole = __all_sync(0xffffffffu, v0 && v8);
+        } else {
+          whole = (t0 + kLaSlice <= sq.a) || (t0 >= sq.lo && t0 + kLaSlice <= sq.hi);
+          if (!whole) {
+            v0 = p0 < sq.a || (p0 >= sq.lo && p0 < sq.hi);
+            v8 = p8 < sq.a || (p8 >= sq.lo && p8 < sq.hi);
+          }
+        }
+        if (p.rule.slopes) {
+          const float e0 = (float)(sq.view.q_pos - p0), e8 = (float)(sq.view.q_pos - p8);
+          sc[0] = fmaf(-sl0, e0, sc[0]);
+          sc[1] = fmaf(-sl1, e0, sc[1]);
+          sc[2] = fmaf(-sl0, e8, sc[2]);
+          sc[3] = fmaf(-sl1, e8, sc[3]);
+        }
+        if (!whole) {
+          if (!v0) sc[0] = sc[1] = -INFINITY;
+          if (!v8) sc[2] = sc[3] = -INFINITY;
+          const uint32_t h0 = __ballot_sync(0xffffffffu, !v0), h8 = __ballot_sync(0xffffffffu, !v8);
+#pragma unroll
+          for (int r = 0; r < 8; ++r) hidden |= ((h0 >> (4 * r)) & 1u) << r | ((h8 >> (4 * r)) & 1u) << (r + 8);
+        }
+      }
+      if (p.scores != nullptr) {
+        const int x = __shfl_sync(0xffffffffu, win.x, src);
+        float* o = p.scores + (((size_t)x * H + head) * kLaUnit + (t0 & (kLaUnit - 1)) + row) * nq + colp;
+        if (nq == 1) {
+          if (t4 == 0) {
+            o[0] = sc[0];
+            o[8] = sc[2];
+          }
+        } else if (colp < nq) {
+          *reinterpret_cast<float2*>(o) = make_float2(sc[0], sc[1]);
+          *reinterpret_cast<float2*>(o + 8 * nq) = make_float2(sc[2], sc[3]);
+        }
+      }
+      if (hidden != 0xffffu) {
+        // ---- running maximum and sum
+        float n0 = fmaxf(sc[0], sc[2]), n1 = fmaxf(sc[1], sc[3]);
+#pragma unroll
+        for (int o = 4; o < 32; o <<= 1) {
+          n0 = fmaxf(n0, __shfl_xor_sync(0xffffffffu, n0, o));
+          n1 = fmaxf(n1, __shfl_xor_sync(0xffffffffu, n1, o));
+        }
+        if (__any_sync(0xffffffffu, n0 > m0 || n1 > m1)) {
+          n0 = fmaxf(n0, m0);
+          n1 = fmaxf(n1, m1);
+          const float f0 = n0 == m0 ? 1.f : exp2f(m0 - n0), f1 = n1 == m1 ? 1.f : exp2f(m1 - n1);
+          m0 = n0;
+          m1 = n1;
+          l0 *= f0;
+          l1 *= f1;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            acc[j][0] *= f0;
+            acc[j][1] *= f1;
+            acc[j][2] *= f0;
+            acc[j][3] *= f1;
+          }
+        }
+        // (a row that has seen nothing yet has maximum -inf: its probabilities are 2^-inf, not NaN)
+        const float b0 = m0 == -INFINITY ? 0.f : m0, b1 = m1 == -INFINITY ? 0.f : m1;
+        const float e0 = exp2f(sc[0] - b0), e1 = exp2f(sc[1] - b1), e2 = exp2f(sc[2] - b0), e3 = exp2f(sc[3] - b1);
+        l0 += e0 + e2;
+        l1 += e1 + e3;
+        // P as the B operand: rounded once to the storage type (half a step of a number <= 1, as a V element carries)
+        const uint32_t pb0 = transpose8<DT>(Elem<DT>::pack(e0, e1)), pb1 = transpose8<DT>(Elem<DT>::pack(e2, e3));
+        if (hidden) {  // rows that are not seen may hold anything, infinities and NaN too: 0 * x has to stay 0
+          for (int k = lane; k < kLaSlice * 16; k += 32) {
+            const int r = k >> 4, c = k & 15;
+            if ((hidden >> r) & 1u)
+              asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(sb + 2 * kLaBoxBytes + (c >> 3) * kLaBoxBytes + r * 128 +
+                                                                         ((c & 7) << 4)),
+                           "r"(0u)
+                           : "memory");
+          }
+          wrote = true;
+          __syncwarp();
+        }
+        // ---- V^T P: D[channel][query row]
+        const int tr = (mi >> 1) * 8 + mr;
+        uint32_t ra[8][4];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int c = 2 * j + (mi & 1);
+          ldsm_x4_t(sb + 2 * kLaBoxBytes + (c >> 3) * kLaBoxBytes + tr * 128 + (((c & 7) ^ mr) << 4), ra[j][0], ra[j][1], ra[j][2],
+                    ra[j][3]);
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) mma_rows<DT>(acc[j], ra[j][0], ra[j][1], ra[j][2], ra[j][3], pb0, pb1);
+      }
+      if (wrote) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    if (fl & kSlLast) {
+      // the next piece's queries travel while the four warps' partial results meet
+      if (i + 1 < n_slices) {
+        const bool nw = src == 31;
+        const int bn = __shfl_sync(0xffffffffu, nw ? nxt.b : win.b, (i + 1) & 31);
+        const int hn = __shfl_sync(0xffffffffu, nw ? nxt.head : win.head, (i + 1) & 31);
+        load_q(bn, hn, q0, q2);
+      }
+#pragma unroll
+      for (int o = 4; o < 32; o <<= 1) {
+        l0 += __shfl_xor_sync(0xffffffffu, l0, o);
+        l1 += __shfl_xor_sync(0xffffffffu, l1, o);
+      }
+      // warps 2, 3 into 0, 1; then 1 into 0
+      __syncthreads();
+#pragma unroll
+      for (int step = 2; step > 0; step >>= 1) {
+        if (warp >= step && warp < 2 * step) {
+          float* o = slab + (warp - step) * kLaRows * kLaSlab;
+          float* mlo = ml_s + (warp - step) * kLaRows * 2;
+          if (colp < nq) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              o[colp * kLaSlab + 16 * j + row] = acc[j][0];
+              o[colp * kLaSlab + 16 * j + row + 8] = acc[j][2];
+            }
+            if (row == 0) {
+              mlo[2 * colp] = m0;
+              mlo[2 * colp + 1] = l0;
+            }
+          }
+          if (colp + 1 < nq) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              o[(colp + 1) * kLaSlab + 16 * j + row] = acc[j][1];
+              o[(colp + 1) * kLaSlab + 16 * j + row + 8] = acc[j][3];
+            }
+            if (row == 0) {
+              mlo[2 * colp + 2] = m1;
+              mlo[2 * colp + 3] = l1;
+            }
+          }
+        }
+        __syncthreads();
+        if (warp < step) {
+          const float* o = slab + warp * kLaRows * kLaSlab;
+          const float* mlo = ml_s + warp * kLaRows * 2;
+          auto join = [&](float& m, float& l, int r, float& fa, float& fb) {
+            const float mb = mlo[2 * r], lb = mlo[2 * r + 1];
+            const float M = fmaxf(m, mb);
+            fa = l == 0.f ? 0.f : exp2f(m - M);
+            fb = lb == 0.f ? 0.f : exp2f(mb - M);
+            m = M;
+            l = l * fa + lb * fb;
+          };
+          float fa = 0.f, fb = 0.f;
+          if (colp < nq) {
+            join(m0, l0, colp, fa, fb);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              acc[j][0] = acc[j][0] * fa + o[colp * kLaSlab + 16 * j + row] * fb;
+              acc[j][2] = acc[j][2] * fa + o[colp * kLaSlab + 16 * j + row + 8] * fb;
+            }
+          }
+          if (colp + 1 < nq) {
+            join(m1, l1, colp + 1, fa, fb);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              acc[j][1] = acc[j][1] * fa + o[(colp + 1) * kLaSlab + 16 * j + row] * fb;
+              acc[j][3] = acc[j][3] * fa + o[(colp + 1) * kLaSlab + 16 * j + row + 8] * fb;
+            }
+          }
+        }
+        if (step == 2) __syncthreads();
+      }
+      if (warp == 0) {
+        const size_t prow = (size_t)(team + b) * p.n_q_heads + head * nq;
+        if (colp < nq) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            p.part_o[(prow + colp) * kHeadDim + 16 * j + row] = acc[j][0];
+            p.part_o[(prow + colp) * kHeadDim + 16 * j + row + 8] = acc[j][2];
+          }
+          if (row == 0) *reinterpret_cast<float2*>(p.part_ml + 2 * (prow + colp)) = make_float2(m0, l0);
+        }
+        if (colp + 1 < nq) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            p.part_o[(prow + colp + 1) * kHeadDim + 16 * j + row] = acc[j][1];
+            p.part_o[(prow + colp + 1) * kHeadDim + 16 * j + row + 8] = acc[j][3];
+          }
+          if (row == 0) *reinterpret_cast<float2*>(p.part_ml + 2 * (prow + colp + 1)) = make_float2(m1, l1);
+        }
+      }
+    }
+  }
+  if (*s_abort) {  // let copies in flight land before the CTA's memory is released
+    for (int k = 0; k < 2000; ++k) __nanosleep(1000);
+  }
+}
+
+// Joins a sequence's pieces (consecutive teams): out = sum_j 2^(m_j - M) o_j / sum_j 2^(m_j - M) l_j.  Blocks
+// [0, combine_x): R query heads each (8: a warp per output row; 1: the eight warps share one row's pieces).  Blocks
+// behind them (calls that gather weights): w_i += sum over the head group of 2^(s_i - lse) for eight units of one kv
+// head, from the scores the split kernel left; they work the log-sum-exps out themselves, so one launch does both.
+constexpr int kLcThreads = 256;
+constexpr int kLcWarps = kLcThreads / 32;
+constexpr int kLcUnits = 8;  // units per weight block
+
+template <int DT, int R>
+__global__ void __launch_bounds__(kLcThreads) layer_attn_combine_kernel(const __grid_constant__ LayerAttnParams p, unsigned short* out,
+                                                                        float* lse, int combine_x) {
+  grid_dep_launch();
+  __shared__ int pre_s[kMaxLayerBatch + 1];
+  __shared__ float4 acc_s[kLcWarps][32];
+  __shared__ float red_s[kLcWarps];
+  __shared__ float lse_s[kLaRows];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int b = blockIdx.y;
+  int bad = 0;
+  unit_prefix(p, pre_s, kLcThreads, bad);
+  const long long U = pre_s[p.g.batch];
+  const int T = live_teams(p, (int)U);
+  const int x0 = pre_s[b], u = pre_s[b + 1] - x0;
+  // the team of unit x is the last c with floor(U c / T) <= x
+  const int c0 = u > 0 ? (int)(((long long)(x0 + 1) * T - 1) / U) : 0;
+  const int c1 = u > 0 ? (int)(((long long)(x0 + u) * T - 1) / U) : -1;
+  if ((int)blockIdx.x >= combine_x) {
+    const int per_head = ((int)gridDim.x - combine_x) / p.g.n_kv_heads;
+    const int j = (int)blockIdx.x - combine_x, head = j / per_head, k0 = (j % per_head) * kLcUnits;
+    if (k0 >= u) return;
+    const Seq sq = seq_of(p, b);
+    grid_dep_wait();
+    for (int r = warp; r < p.nq; r += kLcWarps) {
+      float m = -INFINITY, l = 0.f;
+      for (int c = c0 + lane; c <= c1; c += 32) {
+        const float2 v = *reinterpret_cast<const float2*>(p.part_ml + 2 * ((size_t)(c + b) * p.n_q_heads + head * p.nq + r));
+        const float M = fmaxf(m, v.x);
+        l = (l == 0.f ? 0.f : l * exp2f(m - M)) + (v.y == 0.f ? 0.f : v.y * exp2f(v.x - M));
+        m = M;
+      }
+#pragma unroll
+      for (int o = 16; o; o >>= 1) {
+        const float m2 = __shfl_xor_sync(0xffffffffu, m, o), l2 = __shfl_xor_sync(0xffffffffu, l, o);
+        const float M = fmaxf(m, m2);
+        l = (l == 0.f ? 0.f : l * exp2f(m - M)) + (l2 == 0.f ? 0.f : l2 * exp2f(m2 - M));
+        m = M;
+      }
+      if (lane == 0) lse_s[r] = l == 0.f ? INFINITY : m + log2f(l);  // (a row that saw nothing gives nothing)
+    }
+    __syncthreads();
+    const int k1 = min(k0 + kLcUnits, u);
+    for (int i = tid; i < (k1 - k0) * kLaUnit; i += kLcThreads) {
+      const int k = k0 + i / kLaUnit, in = i % kLaUnit;
+      const int t = (k < sq.ua ? k : sq.ub0 + k - sq.ua) * kLaUnit + in;
+      const bool fresh = t == sq.n;  // the appended row: its weight begins here
+      if (t >= sq.n_tot || (fresh && !(p.flags & MC_LAYER_APPEND))) continue;
+      const float* s = p.scores + (((size_t)(x0 + k) * p.g.n_kv_heads + head) * kLaUnit + in) * p.nq;
+      float w = 0.f;
+      for (int r = 0; r < p.nq; ++r) w += exp2f(s[r] - lse_s[r]);
+      const int slot = t >> p.g.page_shift;
+      if (slot >= p.g.max_pages_per_seq) continue;  // (flagged by the split kernel)
+      const int page = p.g.block_table[(size_t)b * p.g.max_pages_per_seq + slot];
+      if (!page_ok(p.g, page)) continue;
+      float* dst = p.weights + ((size_t)page * p.g.n_kv_heads + head) * p.g.page_size + (t & (p.g.page_size - 1));
+      *dst = fresh ? w : *dst + w;
+    }
+    return;
+  }
+  constexpr int GP = kLcWarps / R;  // warps per output row
+  const int grp = warp % GP;
+  const int hq = blockIdx.x * R + warp / GP;
+  const bool active = hq < p.n_q_heads;
+  grid_dep_wait();
+  float M = -INFINITY, L = 0.f;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (active) {
+    for (int c = c0 + grp; c <= c1; c += 4 * GP) {  // four pieces in flight
+      float2 ml[4];
+      float4 v[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        ml[k] = make_float2(-INFINITY, 0.f);
+        v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (c + k * GP <= c1) {
+          const size_t prow = (size_t)(c + k * GP + b) * p.n_q_heads + hq;
+          ml[k] = *reinterpret_cast<const float2*>(p.part_ml + 2 * prow);
+          v[k] = *reinterpret_cast<const float4*>(p.part_o + prow * kHeadDim + 4 * lane);
+        }
+      }
+      float M2 = M;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) M2 = fmaxf(M2, ml[k].x);
+      const float f = L == 0.f ? 0.f : exp2f(M - M2);
+      M = M2;
+      L *= f;
+      o.x *= f;
+      o.y *= f;
+      o.z *= f;
+      o.w *= f;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float w = ml[k].y == 0.f ? 0.f : exp2f(ml[k].x - M);
+        L = fmaf(w, ml[k].y, L);
+        o.x = fmaf(w, v[k].x, o.x);
+        o.y = fmaf(w, v[k].y, o.y);
+        o.z = fmaf(w, v[k].z, o.z);
+        o.w = fmaf(w, v[k].w, o.w);
+      }
+    }
+  }
+  if (GP > 1) {
+    __shared__ float max_s[kLcWarps];
+    acc_s[warp][lane] = o;
+    if (lane == 0) {
+      red_s[warp] = L;
+      max_s[warp] = M;
+    }
+    __syncthreads();
+    if (grp != 0 || !active) return;
+    float Ma = M;
+    for (int g = 1; g < GP; ++g) Ma = fmaxf(Ma, max_s[warp + g]);
+    const float f = L == 0.f ? 0.f : exp2f(M - Ma);
+    L *= f;
+    o.x *= f;
+    o.y *= f;
+    o.z *= f;
+    o.w *= f;
+    for (int g = 1; g < GP; ++g) {
+      const float lg = red_s[warp + g], fg = lg == 0.f ? 0.f : exp2f(max_s[warp + g] - Ma);
+      const float4 t = acc_s[warp + g][lane];
+      L = fmaf(fg, lg, L);
+      o.x = fmaf(fg, t.x, o.x);
+      o.y = fmaf(fg, t.y, o.y);
+      o.z = fmaf(fg, t.z, o.z);
+      o.w = fmaf(fg, t.w, o.w);
+    }
+    M = Ma;
+  } else if (!active) {
+    return;
+  }
+  const float inv = L == 0.f ? 0.f : 1.f / L;  // (a query that sees nothing: zeros, log-sum-exp -inf)
+  const size_t orow = (size_t)b * p.n_q_heads + hq;
+  uint2 packed;
+  packed.x = Elem<DT>::pack(o.x * inv, o.y * inv);
+  packed.y = Elem<DT>::pack(o.z * inv, o.w * inv);
+  *reinterpret_cast<uint2*>(out + orow * kHeadDim + lane * 4) = packed;
+  if (lse != nullptr && lane == 0) lse[orow] = L == 0.f ? -INFINITY : (M + log2f(L)) * kLn2;
+}
+
+// ---- host side ------------------------------------------------------------------------------------
+struct LayerAttnPlan {
+  int team_size, n_teams;
+  long long max_units;  // of the batch
+  int seq_units;        // of the longest sequence
+  size_t o_bytes, ml_bytes, score_bytes;
+};
+// n_sm: multiprocessors of the device; the workspace is sized for kLaMaxCtas / kLaCtasPerSm of them, so that its size
+// needs no device.
+constexpr int kLaMaxCtas = 512;
+static LayerAttnPlan layer_attn_plan(const mc_config* cfg, const mc_batch* bt, int flags, int n_sm) {
+  LayerAttnPlan pl;
+  const int slots = std::min(n_sm * kLaCtasPerSm, kLaMaxCtas);
+  const int per_cta = (cfg->n_kv_heads + std::min(slots, 32) - 1) / std::min(slots, 32);
+  pl.team_size = (cfg->n_kv_heads + per_cta - 1) / per_cta;
+  pl.seq_units = bt->max_seq_len / kLaUnit + 1;  // (with the step's new token)
+  pl.max_units = (long long)bt->batch * pl.seq_units;
+  pl.n_teams = (int)std::max<long long>(1, std::min<long long>(slots / pl.team_size, pl.max_units));
+  const size_t prow = (size_t)(pl.n_teams + bt->batch) * cfg->n_q_heads;
+  pl.o_bytes = align_up(prow * kHeadDim * 4, 256);
+  pl.ml_bytes = align_up(prow * 2 * 4, 256);
+  pl.score_bytes = (flags & MC_LAYER_ACCUMULATE) ? align_up((size_t)pl.max_units * kLaUnit * cfg->n_q_heads * 4, 256) : 0;
+  return pl;
+}
+size_t layer_attn_workspace_bytes(const mc_config* cfg, const mc_batch* bt, int flags) {
+  const LayerAttnPlan pl = layer_attn_plan(cfg, bt, flags, kLaMaxCtas / kLaCtasPerSm);
+  return pl.o_bytes + pl.ml_bytes + pl.score_bytes;
+}
+
+mc_status launch_layer_attn(const mc_config* cfg, const mc_batch* bt, const Geom& g, const mc_layer_cache* layer,
+                            const mc_score_opts* opts, const void* q, const void* k_new, const void* v_new, int flags, void* out,
+                            float* lse, void* workspace, cudaStream_t stream) {
+  if (bt->batch == 0) return MC_OK;
+  int n_sm = 0;
+  if (mc_status st = sm_count(&n_sm)) return st;
+  const LayerAttnPlan pl = layer_attn_plan(cfg, bt, flags, n_sm);
+  CUtensorMap map_k, map_v;
+  const uint64_t rows = (uint64_t)std::max<int64_t>(bt->n_pages, 1) * cfg->n_kv_heads * cfg->page_size;
+  if (mc_status st = make_map(&map_k, cfg->dtype, layer->k_pool, rows, kHeadDim, kLaSlice)) return st;
+  if (mc_status st = make_map(&map_v, cfg->dtype, layer->v_pool, rows, kHeadDim, kLaSlice)) return st;
+  LayerAttnParams ap;
+  ap.g = g;
+  ap.rule = make_score_rule(opts);
+  ap.k_pool = (char*)layer->k_pool;
+  ap.v_pool = (char*)layer->v_pool;
+  ap.positions = layer->positions;
+  ap.weights = layer->weights;
+  ap.status = layer->status;
+  ap.q = (const char*)q;
+  ap.k_new = (const char*)k_new;
+  ap.v_new = (const char*)v_new;
+  ap.part_o = (float*)workspace;
+  ap.part_ml = (float*)((char*)workspace + pl.o_bytes);
+  ap.scores = (flags & MC_LAYER_ACCUMULATE) ? (float*)((char*)workspace + pl.o_bytes + pl.ml_bytes) : nullptr;
+  ap.nq = cfg->n_q_heads / cfg->n_kv_heads;
+  ap.n_q_heads = cfg->n_q_heads;
+  ap.team_size = pl.team_size;
+  ap.n_teams = pl.n_teams;
+  ap.flags = flags;
+  const size_t smem = 1024 + (size_t)kLaWarps * kLaStages * kLaStageBytes + 2 * kLaRows * (kLaSlab + 2) * 4 +
+                      kLaWarps * kLaStages * (kLaSlice * 4 + 8) + (size_t)(bt->batch + 2) * 4;
+  auto* split = cfg->dtype == MC_F16 ? layer_attn_split_kernel<MC_F16> : layer_attn_split_kernel<MC_BF16>;
+  MC_CUDA_CHECK(cudaFuncSetAttribute(split, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+  MC_CUDA_CHECK(launch_pdl(split, dim3(pl.n_teams * pl.team_size), dim3(kLaThreads), smem, stream, ap, map_k, map_v));
+  // many output rows: a warp per row; few: a block per row
+  const bool warp_rows = (long long)bt->batch * cfg->n_q_heads >= 1024;
+  const int combine_x = warp_rows ? (cfg->n_q_heads + kLcWarps - 1) / kLcWarps : cfg->n_q_heads;
+  const int weight_x = (flags & MC_LAYER_ACCUMULATE) ? cfg->n_kv_heads * ((pl.seq_units + kLcUnits - 1) / kLcUnits) : 0;
+  auto* combine = cfg->dtype == MC_F16 ? (warp_rows ? layer_attn_combine_kernel<MC_F16, kLcWarps> : layer_attn_combine_kernel<MC_F16, 1>)
+                                       : (warp_rows ? layer_attn_combine_kernel<MC_BF16, kLcWarps> : layer_attn_combine_kernel<MC_BF16, 1>);
+  MC_CUDA_CHECK(launch_pdl(combine, dim3(combine_x + weight_x, bt->batch), dim3(kLcThreads), 0, stream, ap, (unsigned short*)out, lse,
+                           combine_x));
+  MC_CUDA_CHECK(cudaGetLastError());
+  return MC_OK;
+}
+
+}  // namespace mc
