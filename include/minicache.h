@@ -637,6 +637,18 @@ mc_status mc_layer_attn(const mc_config* cfg, const mc_batch* batch, const mc_la
                         const void* q, const void* k_new, const void* v_new, int32_t flags, void* out, float* lse,
                         void* workspace, size_t workspace_bytes, void* stream);
 
+/* The attention weight that the last n_obs queries of every sequence give to the cached tokens: what the tokens of a
+ * prompt are ranked by (mc_layer_evict) before the first decode step.
+ * q          [batch][n_obs][n_q_heads][128]: query j stands at position q_pos - (n_obs - 1) + j (q_pos: see
+ *            mc_score_opts); one at a negative position is ignored (a prompt shorter than n_obs)
+ * weights of every cached row = (MC_LAYER_ACCUMULATE: +=) the sum, over the queries and over the query heads of its kv
+ *            head, of the softmax probability; every token of every sequence is written.  Positions and q_pos below
+ *            2^31 - 1.
+ * n_obs * n_q_heads / n_kv_heads at most 256 (MC_ERR_SHAPE).  flags: 0 or MC_LAYER_ACCUMULATE.
+ * workspace  mc_layer_workspace_bytes(MC_OP_LAYER_OBSERVE, n_obs) bytes, 256-byte aligned */
+mc_status mc_layer_observe(const mc_config* cfg, const mc_batch* batch, const mc_layer_cache* layer, const mc_score_opts* opts,
+                           const void* q, int32_t n_obs, int32_t flags, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Copies the layer's status words to `out_words[MC_STATUS_WORDS]` after synchronising `stream`; returns as
  * mc_read_status does. */
 mc_status mc_layer_read_status(const mc_layer_cache* layer, void* stream, int32_t* out_words);

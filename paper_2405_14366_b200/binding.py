@@ -95,7 +95,7 @@ class _Stats(C.Structure):
 EXPORTS = ("mc_decode_drain_host", "mc_decode_stage_host", "mc_decode_attn_append", "mc_prefill_merge_pair", "mc_admit_sequences", "mc_build_flags", "mc_merge_pairs", "mc_pair_bytes", "mc_get_stats", "mc_version", "mc_status_str", "mc_last_cuda_error", "mc_workspace_bytes", "mc_merge_pair",
            "mc_append_pair", "mc_restore", "mc_decode_attn", "mc_read_status", "mc_merge_pair_host",
            "mc_decode_attn_host", "mc_decode_io_bytes", "mc_decode_attn_static", "mc_merge_pair_q4", "mc_selftest_wait_timeout",
-           "mc_layer_workspace_bytes", "mc_layer_attn", "mc_layer_read_status")
+           "mc_layer_workspace_bytes", "mc_layer_attn", "mc_layer_observe", "mc_layer_read_status")
 
 
 def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
@@ -397,8 +397,9 @@ class MiniCacheLib:
         L.mc_merge_pair_q4.restype = C.c_int32
         L.mc_layer_workspace_bytes.argtypes = [P(_Config), P(_Batch), C.c_int32, C.c_int32, P(C.c_size_t)]
         L.mc_layer_attn.argtypes = [P(_Config), P(_Batch), P(_LayerCache), P(_ScoreOpts), V, V, V, C.c_int32, V, V, V, C.c_size_t, V]
+        L.mc_layer_observe.argtypes = [P(_Config), P(_Batch), P(_LayerCache), P(_ScoreOpts), V, C.c_int32, C.c_int32, V, C.c_size_t, V]
         L.mc_layer_read_status.argtypes = [P(_LayerCache), V, P(C.c_int32)]
-        for f in ("mc_layer_workspace_bytes", "mc_layer_attn", "mc_layer_read_status"):
+        for f in ("mc_layer_workspace_bytes", "mc_layer_attn", "mc_layer_observe", "mc_layer_read_status"):
             getattr(L, f).restype = C.c_int32
         L.mc_selftest_wait_timeout.argtypes = [P(_PairCache), C.c_int32, V]
         L.mc_selftest_wait_timeout.restype = C.c_int32
@@ -628,6 +629,17 @@ class MiniCacheLib:
                                             _typed("k_new", k_new, dt), _typed("v_new", v_new, dt), int(flags),
                                             _typed("out", out, dt), _typed("lse", lse, torch.float32), _ptr(workspace),
                                             workspace.numel() * workspace.element_size(), _stream(stream)))
+
+    def mc_layer_observe(self, cfg: McConfig, batch: Batch, layer: LayerCache, opts: ScoreOpts, q, flags: int, workspace: torch.Tensor,
+                         stream=None):
+        """q [batch][n_obs][n_q_heads][128]: the last n_obs queries of every sequence; flags: 0 (weights are written) or
+        MC_LAYER_ACCUMULATE (added to)."""
+        c, b = cfg.c(), batch.c()
+        assert q.dim() == 4 and tuple(q.shape) == (b.batch, q.shape[1], cfg.n_q_heads, 128), "q: [batch][n_obs][n_q_heads][128]"
+        l, o = layer.c(b.n_pages), opts.c(cfg, b.batch)
+        self._check(self._lib.mc_layer_observe(C.byref(c), C.byref(b), C.byref(l), C.byref(o), _typed("q", q, cfg.torch_dtype),
+                                               int(q.shape[1]), int(flags), _ptr(workspace),
+                                               workspace.numel() * workspace.element_size(), _stream(stream)))
 
     def mc_layer_read_status(self, layer: LayerCache, stream=None, check: bool = True):
         words = (C.c_int32 * MC_STATUS_WORDS)()

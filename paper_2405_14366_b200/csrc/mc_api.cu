@@ -734,6 +734,11 @@ mc_status mc_layer_workspace_bytes(const mc_config* cfg, const mc_batch* batch, 
       if (arg & ~(MC_LAYER_APPEND | MC_LAYER_ACCUMULATE)) return MC_ERR_INVALID_ARG;
       *bytes = layer_attn_workspace_bytes(cfg, batch, arg) + 256;
       return MC_OK;
+    case MC_OP_LAYER_OBSERVE:
+      if (arg <= 0) return MC_ERR_INVALID_ARG;
+      if ((int64_t)arg * (cfg->n_q_heads / cfg->n_kv_heads) > kMaxObserveRows) return MC_ERR_SHAPE;
+      *bytes = layer_observe_workspace_bytes(cfg, batch, arg);
+      return MC_OK;
     default:
       return MC_ERR_INVALID_ARG;
   }
@@ -757,6 +762,21 @@ mc_status mc_layer_attn(const mc_config* cfg, const mc_batch* batch, const mc_la
   if (workspace_bytes < layer_attn_workspace_bytes(cfg, batch, flags)) return MC_ERR_CAPACITY;
   return launch_layer_attn(cfg, batch, make_geom(cfg, batch), layer, opts, q, k_new, v_new, flags, out, lse, workspace,
                            (cudaStream_t)stream);
+}
+
+mc_status mc_layer_observe(const mc_config* cfg, const mc_batch* batch, const mc_layer_cache* layer, const mc_score_opts* opts,
+                           const void* q, int32_t n_obs, int32_t flags, void* workspace, size_t workspace_bytes, void* stream) {
+  ApiRange range_("mc_layer_observe");
+  mc_status st = check_layer(cfg, batch, layer);
+  if (st != MC_OK) return st;
+  st = check_score_opts(opts);
+  if (st != MC_OK) return st;
+  if (!q || !layer->weights || n_obs <= 0 || (flags & ~MC_LAYER_ACCUMULATE)) return MC_ERR_INVALID_ARG;
+  if ((int64_t)n_obs * (cfg->n_q_heads / cfg->n_kv_heads) > kMaxObserveRows) return MC_ERR_SHAPE;
+  if (((uintptr_t)q) & 15u) return MC_ERR_ALIGN;
+  if (workspace == nullptr || !aligned256(workspace)) return workspace ? MC_ERR_ALIGN : MC_ERR_INVALID_ARG;
+  if (workspace_bytes < layer_observe_workspace_bytes(cfg, batch, n_obs)) return MC_ERR_CAPACITY;
+  return launch_layer_observe(cfg, batch, make_geom(cfg, batch), layer, opts, q, n_obs, flags, workspace, (cudaStream_t)stream);
 }
 
 mc_status mc_layer_read_status(const mc_layer_cache* layer, void* stream, int32_t* out_words) {

@@ -11,4 +11,9 @@ mc_status launch_layer_attn(const mc_config* cfg, const mc_batch* bt, const Geom
                             const mc_score_opts* opts, const void* q, const void* k_new, const void* v_new, int flags, void* out,
                             float* lse, void* workspace, cudaStream_t stream);
 
+constexpr int kMaxObserveRows = 256;  // observed queries x query heads per kv head
+size_t layer_observe_workspace_bytes(const mc_config* cfg, const mc_batch* bt, int n_obs);
+mc_status launch_layer_observe(const mc_config* cfg, const mc_batch* bt, const Geom& g, const mc_layer_cache* layer,
+                               const mc_score_opts* opts, const void* q, int n_obs, int flags, void* workspace, cudaStream_t stream);
+
 }  // namespace mc

@@ -9,6 +9,8 @@ namespace mc {
 
 // A [rows][cols] 16-bit row-major matrix, copied in boxes of box_rows rows x 64 columns with the 128-byte swizzle.
 mc_status make_map(CUtensorMap* map, int dtype, const void* base, uint64_t rows, uint64_t cols, int box_rows);
+// The same for [planes][rows][cols], boxes of box_planes x box_rows rows.
+mc_status make_map3(CUtensorMap* map, int dtype, const void* base, uint64_t planes, uint64_t rows, uint64_t cols, int box_planes, int box_rows);
 
 __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
   asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),

@@ -71,6 +71,25 @@ def test_layer_attn_refusals(lib):
     assert L.mc_layer_read_status(None, None, None) == 1
 
 
+def test_layer_observe_refusals(lib):
+    L = lib._lib
+
+    def obs(c=None, b=None, l=None, o=None, q=0x100000, n_obs=32, flags=0, ws=0x500000, n=1 << 30):
+        c, b, l, o = c or cfg(), b or batch(), l or layer(), o or opts()
+        return L.mc_layer_observe(C.byref(c), C.byref(b), C.byref(l), C.byref(o), q, n_obs, flags, ws, n, None)
+    for kw, code in CFG:
+        assert obs(c=cfg(**kw)) == code, kw
+    for kw, code in BATCH:
+        assert obs(b=batch(**kw)) == code, kw
+    for kw, code in LAYER + [(dict(w=0), 1)]:
+        assert obs(l=layer(**kw)) == code, kw
+    for kw, code in OPTS:
+        assert obs(o=opts(**kw)) == code, kw
+    assert obs(q=0) == 1 and obs(n_obs=0) == 1 and obs(n_obs=-3) == 1 and obs(flags=1) == 1 and obs(flags=4) == 1
+    assert obs(n_obs=65) == 2 and obs(c=cfg(n_kv_heads=32), n_obs=257) == 2 and obs(n_obs=1 << 30) == 2
+    assert obs(q=0x100008) == 4 and obs(ws=0) == 1 and obs(ws=0x500080) == 4 and obs(n=16) == 5
+
+
 def test_workspace_bytes(lib):
     out = C.c_size_t(0)
     L, c = lib._lib, cfg()
@@ -86,6 +105,7 @@ def test_workspace_bytes(lib):
     assert need(batch(max_len=128), 2, 3) - need(batch(max_len=128), 2, 1) == 2 * 256 * 32 * 4  # the step's token has a unit of its own
     assert need(batch(), 2, 4) == -1 and need(batch(), 9, 0) == -1 and need(batch(), 0, 0) == -1
     assert need(batch(), 2, 0, cfg(page_size=8)) == -2
+    assert need(batch(), 3, 0) == -1 and need(batch(), 3, 65) == -2 and need(batch(), 3, 64) > need(batch(), 3, 32) > 0
     assert L.mc_layer_workspace_bytes(C.byref(c), None, 2, 0, C.byref(out)) == 1
     assert L.mc_layer_workspace_bytes(C.byref(c), C.byref(batch()), 2, 0, None) == 1
 
