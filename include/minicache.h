@@ -649,6 +649,29 @@ mc_status mc_layer_attn(const mc_config* cfg, const mc_batch* batch, const mc_la
 mc_status mc_layer_observe(const mc_config* cfg, const mc_batch* batch, const mc_layer_cache* layer, const mc_score_opts* opts,
                            const void* q, int32_t n_obs, int32_t flags, void* workspace, size_t workspace_bytes, void* stream);
 
+/* What mc_layer_evict keeps.
+ * budget    rows that stay per (sequence, kv head); at least 1, at least n_sink + n_recent
+ * n_sink    rows at positions below it stay;  n_recent: rows at positions above q_pos - n_recent stay
+ * q_pos     device [batch] int32: position of the newest cached token; NULL: seq_lens[b] - 1 (never evicted from) */
+typedef struct mc_evict_opts {
+  const int32_t* q_pos;
+  int32_t budget;
+  int32_t n_sink;
+  int32_t n_recent;
+  int32_t reserved;
+} mc_evict_opts;
+
+/* Evicts from every sequence with more than `budget` cached tokens all rows but `budget` of each kv head: the guarded
+ * ones (see mc_evict_opts), then those with the largest weight; ties go to the lower token index, a NaN ranks below
+ * every number.  Rows that stay and sit in the first `budget` slots are not touched; the k-th (in index order) that
+ * sits behind them is copied, with its position and weight, to the k-th slot before `budget` whose row is evicted.
+ * Slots from `budget` on keep what they held.  layer->positions and layer->weights are needed.
+ * new_lens   device [batch] int32: min(seq_lens[b], budget); must not overlap seq_lens (the caller copies it there, or
+ *            passes it as the seq_lens of later calls)
+ * workspace  mc_layer_workspace_bytes(MC_OP_LAYER_EVICT, 0) bytes, 256-byte aligned */
+mc_status mc_layer_evict(const mc_config* cfg, const mc_batch* batch, const mc_layer_cache* layer, const mc_evict_opts* opts,
+                         int32_t* new_lens, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Copies the layer's status words to `out_words[MC_STATUS_WORDS]` after synchronising `stream`; returns as
  * mc_read_status does. */
 mc_status mc_layer_read_status(const mc_layer_cache* layer, void* stream, int32_t* out_words);

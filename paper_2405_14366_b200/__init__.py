@@ -9,6 +9,7 @@ from .binding import (  # noqa: F401
     Batch,
     LayerCache,
     ScoreOpts,
+    EvictOpts,
     lib,
     MC_LAYER_LM1,
     MC_LAYER_L,

@@ -78,6 +78,10 @@ class _ScoreOpts(C.Structure):
                 ("sm_scale", C.c_float), ("softcap", C.c_float), ("window", C.c_int32), ("reserved", C.c_int32)]
 
 
+class _EvictOpts(C.Structure):
+    _fields_ = [("q_pos", C.c_void_p), ("budget", C.c_int32), ("n_sink", C.c_int32), ("n_recent", C.c_int32), ("reserved", C.c_int32)]
+
+
 class _PairSizes(C.Structure):
     _fields_ = [("tile_bytes", C.c_size_t), ("e_bytes", C.c_size_t), ("dist_bytes", C.c_size_t),
                 ("ret_count_bytes", C.c_size_t), ("ret_offset_bytes", C.c_size_t), ("ret_index_bytes", C.c_size_t),
@@ -95,7 +99,7 @@ class _Stats(C.Structure):
 EXPORTS = ("mc_decode_drain_host", "mc_decode_stage_host", "mc_decode_attn_append", "mc_prefill_merge_pair", "mc_admit_sequences", "mc_build_flags", "mc_merge_pairs", "mc_pair_bytes", "mc_get_stats", "mc_version", "mc_status_str", "mc_last_cuda_error", "mc_workspace_bytes", "mc_merge_pair",
            "mc_append_pair", "mc_restore", "mc_decode_attn", "mc_read_status", "mc_merge_pair_host",
            "mc_decode_attn_host", "mc_decode_io_bytes", "mc_decode_attn_static", "mc_merge_pair_q4", "mc_selftest_wait_timeout",
-           "mc_layer_workspace_bytes", "mc_layer_attn", "mc_layer_observe", "mc_layer_read_status")
+           "mc_layer_workspace_bytes", "mc_layer_attn", "mc_layer_observe", "mc_layer_evict", "mc_layer_read_status")
 
 
 def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
@@ -341,6 +345,19 @@ class ScoreOpts:
                           float(self.sm_scale), float(self.softcap), int(self.window), 0)
 
 
+@dataclasses.dataclass
+class EvictOpts:
+    """What mc_layer_evict keeps (see mc_evict_opts); q_pos: device int32 [batch] or None."""
+    budget: int
+    n_sink: int = 0
+    n_recent: int = 0
+    q_pos: Optional[torch.Tensor] = None
+
+    def c(self, batch: int) -> _EvictOpts:
+        assert self.q_pos is None or self.q_pos.numel() >= batch, "q_pos holds too few entries"
+        return _EvictOpts(_typed("q_pos", self.q_pos, torch.int32), int(self.budget), int(self.n_sink), int(self.n_recent), 0)
+
+
 class MiniCacheLib:
     """Loads libminicache.so and exposes its entry points under their C names."""
 
@@ -398,8 +415,9 @@ class MiniCacheLib:
         L.mc_layer_workspace_bytes.argtypes = [P(_Config), P(_Batch), C.c_int32, C.c_int32, P(C.c_size_t)]
         L.mc_layer_attn.argtypes = [P(_Config), P(_Batch), P(_LayerCache), P(_ScoreOpts), V, V, V, C.c_int32, V, V, V, C.c_size_t, V]
         L.mc_layer_observe.argtypes = [P(_Config), P(_Batch), P(_LayerCache), P(_ScoreOpts), V, C.c_int32, C.c_int32, V, C.c_size_t, V]
+        L.mc_layer_evict.argtypes = [P(_Config), P(_Batch), P(_LayerCache), P(_EvictOpts), V, V, C.c_size_t, V]
         L.mc_layer_read_status.argtypes = [P(_LayerCache), V, P(C.c_int32)]
-        for f in ("mc_layer_workspace_bytes", "mc_layer_attn", "mc_layer_observe", "mc_layer_read_status"):
+        for f in ("mc_layer_workspace_bytes", "mc_layer_attn", "mc_layer_observe", "mc_layer_evict", "mc_layer_read_status"):
             getattr(L, f).restype = C.c_int32
         L.mc_selftest_wait_timeout.argtypes = [P(_PairCache), C.c_int32, V]
         L.mc_selftest_wait_timeout.restype = C.c_int32
@@ -640,6 +658,15 @@ class MiniCacheLib:
         self._check(self._lib.mc_layer_observe(C.byref(c), C.byref(b), C.byref(l), C.byref(o), _typed("q", q, cfg.torch_dtype),
                                                int(q.shape[1]), int(flags), _ptr(workspace),
                                                workspace.numel() * workspace.element_size(), _stream(stream)))
+
+    def mc_layer_evict(self, cfg: McConfig, batch: Batch, layer: LayerCache, opts: EvictOpts, new_lens: torch.Tensor,
+                       workspace: torch.Tensor, stream=None):
+        """new_lens int32 [batch] receives min(seq_lens, budget); it must not share memory with batch.seq_lens."""
+        c, b = cfg.c(), batch.c()
+        assert new_lens.numel() == b.batch
+        l, o = layer.c(b.n_pages), opts.c(b.batch)
+        self._check(self._lib.mc_layer_evict(C.byref(c), C.byref(b), C.byref(l), C.byref(o), _typed("new_lens", new_lens, torch.int32),
+                                             _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream)))
 
     def mc_layer_read_status(self, layer: LayerCache, stream=None, check: bool = True):
         words = (C.c_int32 * MC_STATUS_WORDS)()

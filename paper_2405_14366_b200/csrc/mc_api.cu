@@ -739,6 +739,10 @@ mc_status mc_layer_workspace_bytes(const mc_config* cfg, const mc_batch* batch, 
       if ((int64_t)arg * (cfg->n_q_heads / cfg->n_kv_heads) > kMaxObserveRows) return MC_ERR_SHAPE;
       *bytes = layer_observe_workspace_bytes(cfg, batch, arg);
       return MC_OK;
+    case MC_OP_LAYER_EVICT:
+      if (arg != 0) return MC_ERR_INVALID_ARG;
+      *bytes = layer_evict_workspace_bytes(cfg, batch) + 256;
+      return MC_OK;
     default:
       return MC_ERR_INVALID_ARG;
   }
@@ -777,6 +781,22 @@ mc_status mc_layer_observe(const mc_config* cfg, const mc_batch* batch, const mc
   if (workspace == nullptr || !aligned256(workspace)) return workspace ? MC_ERR_ALIGN : MC_ERR_INVALID_ARG;
   if (workspace_bytes < layer_observe_workspace_bytes(cfg, batch, n_obs)) return MC_ERR_CAPACITY;
   return launch_layer_observe(cfg, batch, make_geom(cfg, batch), layer, opts, q, n_obs, flags, workspace, (cudaStream_t)stream);
+}
+
+mc_status mc_layer_evict(const mc_config* cfg, const mc_batch* batch, const mc_layer_cache* layer, const mc_evict_opts* opts,
+                         int32_t* new_lens, void* workspace, size_t workspace_bytes, void* stream) {
+  ApiRange range_("mc_layer_evict");
+  mc_status st = check_layer(cfg, batch, layer);
+  if (st != MC_OK) return st;
+  if (!layer->positions || !layer->weights || !opts || !new_lens) return MC_ERR_INVALID_ARG;
+  if (opts->budget < 1 || opts->n_sink < 0 || opts->n_recent < 0 || (int64_t)opts->n_sink + opts->n_recent > opts->budget)
+    return MC_ERR_INVALID_ARG;
+  if (((uintptr_t)opts->q_pos | (uintptr_t)new_lens) & 3u) return MC_ERR_ALIGN;
+  // every CTA reads its sequence's length, one of them writes the new one
+  if (new_lens < batch->seq_lens + batch->batch && batch->seq_lens < new_lens + batch->batch) return MC_ERR_INVALID_ARG;
+  if (workspace == nullptr || !aligned256(workspace)) return workspace ? MC_ERR_ALIGN : MC_ERR_INVALID_ARG;
+  if (workspace_bytes < layer_evict_workspace_bytes(cfg, batch)) return MC_ERR_CAPACITY;
+  return launch_layer_evict(cfg, batch, make_geom(cfg, batch), layer, opts, new_lens, workspace, (cudaStream_t)stream);
 }
 
 mc_status mc_layer_read_status(const mc_layer_cache* layer, void* stream, int32_t* out_words) {

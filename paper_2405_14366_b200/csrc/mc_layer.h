@@ -16,4 +16,8 @@ size_t layer_observe_workspace_bytes(const mc_config* cfg, const mc_batch* bt, i
 mc_status launch_layer_observe(const mc_config* cfg, const mc_batch* bt, const Geom& g, const mc_layer_cache* layer,
                                const mc_score_opts* opts, const void* q, int n_obs, int flags, void* workspace, cudaStream_t stream);
 
+size_t layer_evict_workspace_bytes(const mc_config* cfg, const mc_batch* bt);
+mc_status launch_layer_evict(const mc_config* cfg, const mc_batch* bt, const Geom& g, const mc_layer_cache* layer,
+                             const mc_evict_opts* opts, int32_t* new_lens, void* workspace, cudaStream_t stream);
+
 }  // namespace mc

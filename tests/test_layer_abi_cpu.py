@@ -90,6 +90,26 @@ def test_layer_observe_refusals(lib):
     assert obs(q=0x100008) == 4 and obs(ws=0) == 1 and obs(ws=0x500080) == 4 and obs(n=16) == 5
 
 
+def test_layer_evict_refusals(lib):
+    L = lib._lib
+
+    def ev(c=None, b=None, l=None, o=(0, 100, 4, 10), nl=0x600000, ws=0x500000, n=1 << 30):
+        c, b, l, o = c or cfg(), b or batch(), l or layer(), B._EvictOpts(*o, 0)
+        return L.mc_layer_evict(C.byref(c), C.byref(b), C.byref(l), C.byref(o), nl, ws, n, None)
+    for kw, code in CFG:
+        assert ev(c=cfg(**kw)) == code, kw
+    for kw, code in BATCH:
+        assert ev(b=batch(**kw)) == code, kw
+    for kw, code in LAYER + [(dict(w=0), 1), (dict(pos=0), 1)]:
+        assert ev(l=layer(**kw)) == code, kw
+    for o, code in (((0, 0, 0, 0), 1), ((0, -5, 0, 0), 1), ((0, 10, -1, 0), 1), ((0, 10, 0, -1), 1), ((0, 10, 6, 5), 1),
+                    ((0, 2 ** 31 - 1, 2 ** 31 - 1, 2 ** 31 - 1), 1), ((2, 10, 1, 1), 4)):
+        assert ev(o=o) == code, o
+    assert ev(nl=0) == 1 and ev(nl=0x600002) == 4
+    assert ev(nl=0x2000) == 1 and ev(nl=0x2004) == 1 and ev(nl=0x1ffc) == 1  # over the lengths it reads
+    assert ev(ws=0) == 1 and ev(ws=0x500080) == 4 and ev(n=16) == 5
+
+
 def test_workspace_bytes(lib):
     out = C.c_size_t(0)
     L, c = lib._lib, cfg()
@@ -105,6 +125,7 @@ def test_workspace_bytes(lib):
     assert need(batch(max_len=128), 2, 3) - need(batch(max_len=128), 2, 1) == 2 * 256 * 32 * 4  # the step's token has a unit of its own
     assert need(batch(), 2, 4) == -1 and need(batch(), 9, 0) == -1 and need(batch(), 0, 0) == -1
     assert need(batch(), 2, 0, cfg(page_size=8)) == -2
+    assert need(batch(), 4, 0) >= 2 * 8 * 64 * 4 and need(batch(), 4, 1) == -1
     assert need(batch(), 3, 0) == -1 and need(batch(), 3, 65) == -2 and need(batch(), 3, 64) > need(batch(), 3, 32) > 0
     assert L.mc_layer_workspace_bytes(C.byref(c), None, 2, 0, C.byref(out)) == 1
     assert L.mc_layer_workspace_bytes(C.byref(c), C.byref(batch()), 2, 0, None) == 1
