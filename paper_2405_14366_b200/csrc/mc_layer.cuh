@@ -8,7 +8,7 @@ constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLn2 = 0.69314718055994530942f;
 
 // The score rule of a call (mc_score_opts) in the form the kernels use; scores are kept as log2(e) times their value,
-// so that a probability is one exp2f.
+// so that a probability is one instruction.
 struct ScoreRule {
   const float* slopes;       // [n_q_heads] or null
   const int32_t* doc_start;  // [batch] or null
@@ -47,6 +47,68 @@ __device__ __forceinline__ float tanh_score(float x) {
   }
   const float t = 1.f - __fdividef(2.f, 1.f + exp2f(fminf(y, 64.f) * (2.f * kLog2e)));
   return x != x ? x : copysignf(t, x);  // (fminf would turn a NaN into a number)
+}
+// 2^x to 2 ulp, one instruction: probabilities below 2^-126 are zero (exp2f's scaling of denormals costs as much again).
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// Two binary32 numbers in one 64-bit register: sm_100's packed arithmetic does both in one issue slot.
+__device__ __forceinline__ uint64_t pack2(float x, float y) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
+  return r;
+}
+__device__ __forceinline__ void unpack2(uint64_t v, float& x, float& y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(v)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+// tanh of two numbers in [-1, 1]: x P(x^2), P of degree 6 fitted to tanh(x) / x on [0, 1] by reweighted least squares
+// (5e-8 relative before rounding): no special-function unit, which the exponentials need.
+__device__ __forceinline__ uint64_t tanh2_small(uint64_t x) {
+  const uint64_t z = mul2(x, x);
+  uint64_t q = pack2(1.0410172275e-03f, 1.0410172275e-03f);
+  q = fma2(q, z, pack2(-6.2033628195e-03f, -6.2033628195e-03f));
+  q = fma2(q, z, pack2(2.0289962009e-02f, 2.0289962009e-02f));
+  q = fma2(q, z, pack2(-5.3457019959e-02f, -5.3457019959e-02f));
+  q = fma2(q, z, pack2(1.3325203849e-01f, 1.3325203849e-01f));
+  q = fma2(q, z, pack2(-3.3332839133e-01f, -3.3332839133e-01f));
+  q = fma2(q, z, pack2(9.9999995024e-01f, 9.9999995024e-01f));
+  return mul2(x, q);
+}
+// The same in [-1/2, 1/2], degree 4.
+__device__ __forceinline__ uint64_t tanh2_tiny(uint64_t x) {
+  const uint64_t z = mul2(x, x);
+  uint64_t q = pack2(1.7134999450e-02f, 1.7134999450e-02f);
+  q = fma2(q, z, pack2(-5.2986071693e-02f, -5.2986071693e-02f));
+  q = fma2(q, z, pack2(1.3324779261e-01f, 1.3324779261e-01f));
+  q = fma2(q, z, pack2(-3.3333069391e-01f, -3.3333069391e-01f));
+  q = fma2(q, z, pack2(9.9999998687e-01f, 9.9999998687e-01f));
+  return mul2(x, q);
+}
+// The largest of three numbers, and of one and two magnitudes (sm_100's three-input forms).
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+__device__ __forceinline__ float max3_abs(float a, float b, float c) {
+  float r;
+  asm("max.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
 }
 // q . k -> score (log2 units), the cap included, the distance bias not.
 __device__ __forceinline__ float score_of(const ScoreRule& r, float dot) {

@@ -417,7 +417,7 @@ layer_attn_split_kernel(const __grid_constant__ LayerAttnParams p, const __grid_
         if (__any_sync(0xffffffffu, n0 > m0 || n1 > m1)) {
           n0 = fmaxf(n0, m0);
           n1 = fmaxf(n1, m1);
-          const float f0 = n0 == m0 ? 1.f : exp2f(m0 - n0), f1 = n1 == m1 ? 1.f : exp2f(m1 - n1);
+          const float f0 = n0 == m0 ? 1.f : ex2(m0 - n0), f1 = n1 == m1 ? 1.f : ex2(m1 - n1);
           m0 = n0;
           m1 = n1;
           l0 *= f0;
@@ -432,7 +432,7 @@ layer_attn_split_kernel(const __grid_constant__ LayerAttnParams p, const __grid_
         }
         // (a row that has seen nothing yet has maximum -inf: its probabilities are 2^-inf, not NaN)
         const float b0 = m0 == -INFINITY ? 0.f : m0, b1 = m1 == -INFINITY ? 0.f : m1;
-        const float e0 = exp2f(sc[0] - b0), e1 = exp2f(sc[1] - b1), e2 = exp2f(sc[2] - b0), e3 = exp2f(sc[3] - b1);
+        const float e0 = ex2(sc[0] - b0), e1 = ex2(sc[1] - b1), e2 = ex2(sc[2] - b0), e3 = ex2(sc[3] - b1);
         l0 += e0 + e2;
         l1 += e1 + e3;
         // P as the B operand: rounded once to the storage type (half a step of a number <= 1, as a V element carries)
@@ -513,8 +513,8 @@ layer_attn_split_kernel(const __grid_constant__ LayerAttnParams p, const __grid_
           auto join = [&](float& m, float& l, int r, float& fa, float& fb) {
             const float mb = mlo[2 * r], lb = mlo[2 * r + 1];
             const float M = fmaxf(m, mb);
-            fa = l == 0.f ? 0.f : exp2f(m - M);
-            fb = lb == 0.f ? 0.f : exp2f(mb - M);
+            fa = l == 0.f ? 0.f : ex2(m - M);
+            fb = lb == 0.f ? 0.f : ex2(mb - M);
             m = M;
             l = l * fa + lb * fb;
           };
@@ -601,14 +601,14 @@ __global__ void __launch_bounds__(kLcThreads) layer_attn_combine_kernel(const __
       for (int c = c0 + lane; c <= c1; c += 32) {
         const float2 v = *reinterpret_cast<const float2*>(p.part_ml + 2 * ((size_t)(c + b) * p.n_q_heads + head * p.nq + r));
         const float M = fmaxf(m, v.x);
-        l = (l == 0.f ? 0.f : l * exp2f(m - M)) + (v.y == 0.f ? 0.f : v.y * exp2f(v.x - M));
+        l = (l == 0.f ? 0.f : l * ex2(m - M)) + (v.y == 0.f ? 0.f : v.y * ex2(v.x - M));
         m = M;
       }
 #pragma unroll
       for (int o = 16; o; o >>= 1) {
         const float m2 = __shfl_xor_sync(0xffffffffu, m, o), l2 = __shfl_xor_sync(0xffffffffu, l, o);
         const float M = fmaxf(m, m2);
-        l = (l == 0.f ? 0.f : l * exp2f(m - M)) + (l2 == 0.f ? 0.f : l2 * exp2f(m2 - M));
+        l = (l == 0.f ? 0.f : l * ex2(m - M)) + (l2 == 0.f ? 0.f : l2 * ex2(m2 - M));
         m = M;
       }
       if (lane == 0) lse_s[r] = l == 0.f ? INFINITY : m + log2f(l);  // (a row that saw nothing gives nothing)
@@ -622,7 +622,7 @@ __global__ void __launch_bounds__(kLcThreads) layer_attn_combine_kernel(const __
       if (t >= sq.n_tot || (fresh && !(p.flags & MC_LAYER_APPEND))) continue;
       const float* s = p.scores + (((size_t)(x0 + k) * p.g.n_kv_heads + head) * kLaUnit + in) * p.nq;
       float w = 0.f;
-      for (int r = 0; r < p.nq; ++r) w += exp2f(s[r] - lse_s[r]);
+      for (int r = 0; r < p.nq; ++r) w += ex2(s[r] - lse_s[r]);
       const int slot = t >> p.g.page_shift;
       if (slot >= p.g.max_pages_per_seq) continue;  // (flagged by the split kernel)
       const int page = p.g.block_table[(size_t)b * p.g.max_pages_per_seq + slot];
@@ -656,7 +656,7 @@ __global__ void __launch_bounds__(kLcThreads) layer_attn_combine_kernel(const __
       float M2 = M;
 #pragma unroll
       for (int k = 0; k < 4; ++k) M2 = fmaxf(M2, ml[k].x);
-      const float f = L == 0.f ? 0.f : exp2f(M - M2);
+      const float f = L == 0.f ? 0.f : ex2(M - M2);
       M = M2;
       L *= f;
       o.x *= f;
@@ -665,7 +665,7 @@ __global__ void __launch_bounds__(kLcThreads) layer_attn_combine_kernel(const __
       o.w *= f;
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const float w = ml[k].y == 0.f ? 0.f : exp2f(ml[k].x - M);
+        const float w = ml[k].y == 0.f ? 0.f : ex2(ml[k].x - M);
         L = fmaf(w, ml[k].y, L);
         o.x = fmaf(w, v[k].x, o.x);
         o.y = fmaf(w, v[k].y, o.y);
@@ -685,14 +685,14 @@ __global__ void __launch_bounds__(kLcThreads) layer_attn_combine_kernel(const __
     if (grp != 0 || !active) return;
     float Ma = M;
     for (int g = 1; g < GP; ++g) Ma = fmaxf(Ma, max_s[warp + g]);
-    const float f = L == 0.f ? 0.f : exp2f(M - Ma);
+    const float f = L == 0.f ? 0.f : ex2(M - Ma);
     L *= f;
     o.x *= f;
     o.y *= f;
     o.z *= f;
     o.w *= f;
     for (int g = 1; g < GP; ++g) {
-      const float lg = red_s[warp + g], fg = lg == 0.f ? 0.f : exp2f(max_s[warp + g] - Ma);
+      const float lg = red_s[warp + g], fg = lg == 0.f ? 0.f : ex2(max_s[warp + g] - Ma);
       const float4 t = acc_s[warp + g][lane];
       L = fmaf(fg, lg, L);
       o.x = fmaf(fg, t.x, o.x);

@@ -14,9 +14,11 @@
 // backwards: the keys read last are the ones still in L2.
 //
 // One persistent CTA per SM; the tiles of all (sequence, kv head) segments are shared out equally.  Warp 0 streams K
-// tiles (a tiled copy per page and 64-channel half) and the segments' Q; warp 1 issues tcgen05.mma into two
-// tensor-memory buffers; two groups of four warps take the tiles in turn, each from its own buffer.  The exponentials
-// bound it: 2 R per token, 16 a clock and SM.  Every wait is bounded; tensor memory is released on every path.
+// tiles (a tiled copy per page and 64-channel half) and the segments' Q; warp 1 issues tcgen05.mma into a tensor-memory
+// buffer per group of four warps: up to 128 rows the four groups take the tiles in turn, beyond that two groups share a
+// tile, one for each 128 rows.  (Two groups instead of four: the latencies of 9 cycles per instruction showed.)  The
+// exponentials bound it: 2 R per token, 16 a clock and SM.  Every wait is bounded; tensor memory is released on every
+// path.
 #include <algorithm>
 
 #include "mc_layer.cuh"
@@ -30,8 +32,8 @@ namespace mc {
 constexpr int kObTile = 128;                             // tokens per tile
 constexpr int kObHalf = kObTile * 128;                   // bytes of a tile's 64-channel half
 constexpr int kObTileBytes = 2 * kObHalf;                // 32 KB
-constexpr int kObMaxRows = 256;
-constexpr int kObThreads = 320;                          // producer, tensor-core issue, two groups of four warps
+constexpr int kObGroups = 4;                             // groups of four warps that take scores out of tensor memory
+constexpr int kObThreads = 64 + kObGroups * 128;         // producer, tensor-core issue, the groups
 constexpr int kObQBufs = 2;
 constexpr int kObMaxStages = 4;
 constexpr int kObNoToken = 0x7fffffff;                   // position of a tile's rows behind the sequence: never seen
@@ -43,13 +45,14 @@ struct ObserveParams {
   const int32_t* positions;
   float* weights;
   int32_t* status;
-  float* part_ml;  // [(CTA + segment)][2 groups][rows][2]
+  float* part_ml;  // [(CTA + segment)][rows][slots][2]
   int n_obs, nq, n_q_heads;
   int rows;      // n_obs * nq
   int nt;        // row tiles of 128: 1 or 2
+  int slots;     // groups that share a row tile: 4 / nt
   int rp, rep;   // rows of a copy (32, 64 or 128), copies in a row tile
   int jt;        // queries per Q copy
-  int stages;    // K ring
+  int stage_shift;  // K ring: 4 or 2 stages
   int add;       // pass 2 adds to the weights (else it writes them)
   int zero;      // pass 1 clears the weights first
   int n_ctas;
@@ -108,8 +111,37 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map
                : "memory");
 }
 __device__ __forceinline__ void group_sync(int grp) { asm volatile("bar.sync %0, 128;" ::"r"(1 + grp) : "memory"); }
+__device__ __forceinline__ void pair_sync(int pair) { asm volatile("bar.sync %0, 256;" ::"r"(1 + kObGroups + pair) : "memory"); }
 
-template <int DT, int PASS>
+// 16 accumulators -> tanh(sm q.k / cap) (CAP) or q.k unchanged; the score is `factor` times that.
+template <bool CAP>
+__device__ __forceinline__ void capped16(const ScoreRule& r, const uint32_t (&raw)[16], float (&t)[16]) {
+  if (!CAP) {
+#pragma unroll
+    for (int k = 0; k < 16; ++k) t[k] = __uint_as_float(raw[k]);
+    return;
+  }
+  const uint64_t inv = pack2(r.cap_inv, r.cap_inv);
+  float big = 0.f;
+#pragma unroll
+  for (int k = 0; k < 16; k += 2) {
+    unpack2(mul2(pack2(__uint_as_float(raw[k]), __uint_as_float(raw[k + 1])), inv), t[k], t[k + 1]);
+    big = max3_abs(big, t[k], t[k + 1]);
+  }
+  // (a NaN is dropped by the maximum and stays one in every branch)
+  if (__all_sync(0xffffffffu, big <= 0.5f)) {
+#pragma unroll
+    for (int k = 0; k < 16; k += 2) unpack2(tanh2_tiny(pack2(t[k], t[k + 1])), t[k], t[k + 1]);
+  } else if (__all_sync(0xffffffffu, big <= 1.f)) {
+#pragma unroll
+    for (int k = 0; k < 16; k += 2) unpack2(tanh2_small(pack2(t[k], t[k + 1])), t[k], t[k + 1]);
+  } else {
+#pragma unroll
+    for (int k = 0; k < 16; ++k) t[k] = tanh_score(t[k]);
+  }
+}
+
+template <int DT, int PASS, bool CAP>
 __global__ void __launch_bounds__(kObThreads, 1)
 layer_observe_kernel(const __grid_constant__ ObserveParams p, const __grid_constant__ CUtensorMap map_k,
                      const __grid_constant__ CUtensorMap map_q) {
@@ -118,18 +150,19 @@ layer_observe_kernel(const __grid_constant__ ObserveParams p, const __grid_const
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   // barriers: K full / empty per stage, Q full / empty per buffer, accumulator full / empty per group
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + kObSmem);
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * kObMaxStages + 4 + 4);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * kObMaxStages + 4 + 2 * kObGroups);
   volatile int* s_abort = reinterpret_cast<volatile int*>(tmem_slot + 1);
-  float* row_s = reinterpret_cast<float*>(tmem_slot + 2);     // [2 groups][256][2]: pass 1 (m, l) of the lanes; pass 2 lse, slope
-  int* pos_s = reinterpret_cast<int*>(row_s + 2 * kObMaxRows * 2);  // [2 groups][128]
-  int* pre_s = pos_s + 2 * kObTile;                           // [batch + 1]
+  float* row_s = reinterpret_cast<float*>(tmem_slot + 4);             // [groups][128][2]: pass 1 (m, l) of the lanes; pass 2 -lse, slope
+  int* view_s = reinterpret_cast<int*>(row_s + kObGroups * kObTile * 2);  // [groups][2][128]: pass 2: position, lowest position seen
+  int* pos_s = view_s + kObGroups * kObTile * 2;                      // [groups][128]: pass 1: positions; pass 2: weights on their way
+  int* pre_s = pos_s + kObGroups * kObTile;                           // [batch + 1]
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int H = p.g.n_kv_heads, ps = p.g.page_size, shift = p.g.page_shift;
   const uint32_t full0 = smem_u32(bars), empty0 = full0 + 8 * kObMaxStages, qfull0 = empty0 + 8 * kObMaxStages, qempty0 = qfull0 + 16;
-  const uint32_t tfull0 = qempty0 + 16, tempty0 = tfull0 + 16;
+  const uint32_t tfull0 = qempty0 + 16, tempty0 = tfull0 + 8 * kObGroups;
   const int q_bytes = p.nt * kObTileBytes, q_half = p.nt * kObHalf;
   const uint32_t sq0 = smem_u32(smem), sk0 = sq0 + kObQBufs * q_bytes;
-  const uint32_t tmem_cols = 2u * kObTile * p.nt;
+  constexpr uint32_t tmem_cols = kObGroups * kObTile;
 
   int bad = 0;
   for (int b = tid; b < p.g.batch; b += kObThreads) {
@@ -145,6 +178,8 @@ layer_observe_kernel(const __grid_constant__ ObserveParams p, const __grid_const
     for (int s = 0; s < 2; ++s) {
       mbar_init(qfull0 + 8 * s, 1);
       mbar_init(qempty0 + 8 * s, 1);
+    }
+    for (int s = 0; s < kObGroups; ++s) {
       mbar_init(tfull0 + 8 * s, 1);
       mbar_init(tempty0 + 8 * s, 4);
     }
@@ -184,6 +219,7 @@ layer_observe_kernel(const __grid_constant__ ObserveParams p, const __grid_const
     n_x = (int)(U * (cta + 1) / T) - x_begin;
   }
   constexpr int DIR = PASS == 1 ? 1 : -1;
+  const int s_mask = (1 << p.stage_shift) - 1;
   const int x_first = PASS == 1 ? x_begin : x_begin + n_x - 1;
   grid_dep_wait();
   if (bad) atomicOr(p.status, MC_FLAG_BAD_METADATA);
@@ -208,25 +244,38 @@ layer_observe_kernel(const __grid_constant__ ObserveParams p, const __grid_const
 
   if (warp == 0) {
     // ===================== producer =====================
+    // Rows of the pools where the pages of the next tiles begin, a lane per page, one window of 32 pages ahead: a load
+    // per tile would pace the stream by its latency .
+    const int ppt = kObTile >> shift, lane_tile = lane >> (7 - shift), lane_page = lane & (ppt - 1);
+    const int win_tiles = 32 >> (7 - shift);  // pages per tile: ppt; tiles per window
+    auto load_window = [&](int i0, int& head, bool& has) {
+      const int i = i0 + lane_tile;
+      head = 0;
+      has = false;
+      if (i >= n_x) return 0;
+      ObCursor d;
+      d.seek(pre_s, p.g.batch, H, x_first + DIR * i);
+      const ObSeq q = ob_seq(p, d.b);
+      const int t = (d.k < q.ua ? d.k : q.ub0 + d.k - q.ua) * kObTile + (lane_page << shift);
+      head = d.g;
+      has = t < q.n;
+      return has ? p.g.block_table[(size_t)d.b * p.g.max_pages_per_seq + (t >> shift)] : 0;
+    };
+    int head, head_n;
+    bool has, has_n;
+    int page = load_window(0, head, has), page_n = load_window(win_tiles, head_n, has_n);
     ObCursor c;
     if (n_x > 0) c.seek(pre_s, p.g.batch, H, x_first);
     bool first = true, ok = true;
     int seg = 0;
-    ObSeq sq = {};
-    int sq_b = -1;
-    bool has = false;  // this lane has a page of the tile
-    // page id of this lane's page of the current tile, one tile ahead (a tile has at most 8 pages)
-    auto tile_page = [&](const ObCursor& d) {
-      if (d.b != sq_b) {
-        sq = ob_seq(p, d.b);
-        sq_b = d.b;
-      }
-      const int t = (d.k < sq.ua ? d.k : sq.ub0 + d.k - sq.ua) * kObTile + (lane << shift);
-      has = lane < (kObTile >> shift) && t < sq.n;
-      return has ? p.g.block_table[(size_t)d.b * p.g.max_pages_per_seq + (t >> shift)] : 0;
-    };
-    int page = n_x > 0 ? tile_page(c) : 0;
     for (int i = 0; i < n_x && ok; ++i) {
+      const int in_win = i & (win_tiles - 1);
+      if (in_win == 0 && i > 0) {
+        page = page_n;
+        head = head_n;
+        has = has_n;
+        page_n = load_window(i + win_tiles, head_n, has_n);
+      }
       if (first) {
         const int qb = seg & 1;
         if (seg >= 2) ok = __all_sync(0xffffffffu, mbar_wait(qempty0 + 8 * qb, ((seg >> 1) - 1) & 1, s_abort, p.status));
@@ -241,33 +290,29 @@ layer_observe_kernel(const __grid_constant__ ObserveParams p, const __grid_const
         }
         __syncwarp();
       }
-      const int s = i % p.stages;
-      if (i >= p.stages) ok = __all_sync(0xffffffffu, mbar_wait(empty0 + 8 * s, ((i / p.stages) - 1) & 1, s_abort, p.status));
+      const int s = i & s_mask, lap = i >> p.stage_shift;
+      if (lap > 0) ok = __all_sync(0xffffffffu, mbar_wait(empty0 + 8 * s, (lap - 1) & 1, s_abort, p.status));
       if (!ok) break;
-      const int here = page;
-      const bool copies = has;
-      const ObCursor now = c;
-      first = last_of_seg(c, i);
-      if (first) ++seg;
-      if (i + 1 < n_x) {
-        advance(c, x_first + DIR * (i + 1));
-        page = tile_page(c);
-      }
       const uint32_t bar = full0 + 8 * s, dst = sk0 + s * kObTileBytes;
+      const bool copies = has && lane_tile == in_win;
       const int n_copy = __popc(__ballot_sync(0xffffffffu, copies));
       if (lane == 0) mbar_expect_tx(bar, (uint32_t)(n_copy * 2 * ps * 128));
       __syncwarp();
       if (copies) {
-        int pg = here;
+        int pg = page;
         if (!page_ok(p.g, pg)) {  // never an address: page 0 is read in its place and the call flagged
           atomicOr(p.status, MC_FLAG_BAD_METADATA);
           pg = 0;
         }
-        const int y = (pg * H + now.g) * ps;
-        tma_load_2d(dst + lane * ps * 128, &map_k, 0, y, bar);
-        tma_load_2d(dst + kObHalf + lane * ps * 128, &map_k, 64, y, bar);
+        const int y = (pg * H + head) * ps;
+        const uint32_t to = dst + lane_page * ps * 128;
+        tma_load_2d(to, &map_k, 0, y, bar);
+        tma_load_2d(to + kObHalf, &map_k, 64, y, bar);
       }
       __syncwarp();
+      first = last_of_seg(c, i);
+      if (first) ++seg;
+      if (i + 1 < n_x) advance(c, x_first + DIR * (i + 1));
     }
   } else if (warp == 1) {
     // ===================== tensor-core issue =====================
@@ -275,25 +320,39 @@ layer_observe_kernel(const __grid_constant__ ObserveParams p, const __grid_const
       ObCursor c;
       if (n_x > 0) c.seek(pre_s, p.g.batch, H, x_first);
       int seg = 0;
-      bool first = true;
-      const int n_cols = PASS == 1 ? kObTile : (p.rows + 15) / 16 * 16;
-      const uint32_t idesc = umma_idesc<DT, 8>() - (1u << 17) + ((uint32_t)(n_cols >> 3) << 17);
-      for (int i = 0; i < n_x; ++i) {
-        const int s = i % p.stages, buf = i & 1, qb = seg & 1;
+      bool first = true, ok = true;
+      // One thread paces the tensor cores, so its loop is short: a descriptor's low word is an address in 16-byte
+      // units (and the fixed bits), its high word never changes; k step 4 starts the second 64-channel half.
+      const uint64_t d0 = smem_desc_k128(0);
+      const uint32_t d_hi = (uint32_t)(d0 >> 32), d_lo = (uint32_t)d0, q_step = (uint32_t)(q_half >> 4);
+      uint32_t idesc[2];
+#pragma unroll
+      for (int tt = 0; tt < 2; ++tt) {
+        const int n_cols = PASS == 1 ? kObTile : (max(min(p.rows - tt * kObTile, kObTile), 1) + 15) / 16 * 16;
+        idesc[tt] = umma_idesc<DT, 8>() - (1u << 17) + ((uint32_t)(n_cols >> 3) << 17);
+      }
+      for (int i = 0; i < n_x && ok; ++i) {
+        const int s = i & s_mask, qb = seg & 1;
         if (first && !mbar_wait(qfull0 + 8 * qb, (seg >> 1) & 1, s_abort, p.status)) break;
-        if (i >= 2 && !mbar_wait(tempty0 + 8 * buf, ((i >> 1) - 1) & 1, s_abort, p.status)) break;
-        if (!mbar_wait(full0 + 8 * s, (i / p.stages) & 1, s_abort, p.status)) break;
-        tc_fence_after();
-        const uint32_t d = tmem_d + buf * kObTile * p.nt;
-        const uint32_t qa = sq0 + qb * q_bytes, ka = sk0 + s * kObTileBytes;
-        for (int tt = 0; tt < (PASS == 1 ? p.nt : 1); ++tt) {
+        if (!mbar_wait(full0 + 8 * s, (i >> p.stage_shift) & 1, s_abort, p.status)) break;
+        const uint32_t q_lo = d_lo + ((sq0 + qb * q_bytes) >> 4), k_lo = d_lo + ((sk0 + s * kObTileBytes) >> 4);
+#pragma unroll
+        for (int tt = 0; tt < 2; ++tt) {
+          if (tt >= p.nt) break;
+          const int grp = p.nt == 1 ? i & 3 : 2 * (i & 1) + tt, turn = p.nt == 1 ? i >> 2 : i >> 1;
+          if (turn >= 1) ok = mbar_wait(tempty0 + 8 * grp, (turn - 1) & 1, s_abort, p.status);
+          if (!ok) break;
+          tc_fence_after();
+          const uint32_t d = tmem_d + grp * kObTile;
 #pragma unroll
           for (int k = 0; k < kHeadDim / 16; ++k) {
-            const uint64_t dq = smem_desc_k128(qa + (k >> 2) * q_half + tt * kObHalf) + (uint64_t)(2 * (k & 3));
-            const uint64_t dk = smem_desc_k128(ka + (k >> 2) * kObHalf) + (uint64_t)(2 * (k & 3));
-            if (PASS == 1) umma_f16(d + tt * kObTile, dq, dk, idesc, k > 0 ? 1u : 0u);
-            else umma_f16(d, dk, dq, idesc, k > 0 ? 1u : 0u);
+            const uint32_t ql = q_lo + (k >= 4 ? q_step : 0u) + (uint32_t)(tt * (kObHalf >> 4) + 2 * (k & 3));
+            const uint32_t kl = k_lo + (uint32_t)((k >> 2) * (kObHalf >> 4) + 2 * (k & 3));
+            const uint64_t dq = ((uint64_t)d_hi << 32) | ql, dk = ((uint64_t)d_hi << 32) | kl;
+            if (PASS == 1) umma_f16(d, dq, dk, idesc[tt], k > 0 ? 1u : 0u);
+            else umma_f16(d, dk, dq, idesc[tt], k > 0 ? 1u : 0u);
           }
+          umma_commit(tfull0 + 8 * grp);
         }
         umma_commit(empty0 + 8 * s);
         first = last_of_seg(c, i);
@@ -301,67 +360,75 @@ layer_observe_kernel(const __grid_constant__ ObserveParams p, const __grid_const
           umma_commit(qempty0 + 8 * qb);
           ++seg;
         }
-        umma_commit(tfull0 + 8 * buf);
         if (i + 1 < n_x) advance(c, x_first + DIR * (i + 1));
       }
     }
   } else {
     // ===================== scores =====================
+    // group: with one row tile it takes every fourth tile, with two row tiles every second one, the rows of tile `tt`
     const int grp = (warp - 2) >> 2, quad = warp & 3, gl = quad * 32 + lane;  // gl: this thread's tensor-memory lane
-    const uint32_t tbuf = tmem_d + grp * kObTile * p.nt + ((uint32_t)(quad * 32) << 16);
-    float* row_g = row_s + grp * kObMaxRows * 2;
+    const int tt = p.nt == 1 ? 0 : grp & 1, g_mask = 4 / p.nt - 1, mine = p.nt == 1 ? grp : grp >> 1;
+    const int row0 = tt * kObTile, n_rows = min(p.rows - row0, kObTile);
+    const uint32_t tbuf = tmem_d + grp * kObTile + ((uint32_t)(quad * 32) << 16);
+    float* row_g = row_s + grp * kObTile * 2;
+    int* row_q = view_s + grp * kObTile * 2;
     int* pos_g = pos_s + grp * kObTile;
-    const bool no_max = p.rule.cap_log2 > 0.f && p.rule.cap_log2 <= 100.f && p.rule.slopes == nullptr;
+    const bool no_max = CAP && p.rule.cap_log2 <= 100.f && p.rule.slopes == nullptr;
+    const float factor = CAP ? p.rule.cap_log2 : p.rule.scale_log2;
+    const uint64_t factor2 = pack2(factor, factor);
     ObCursor c;
     if (n_x > 0) c.seek(pre_s, p.g.batch, H, x_first);
     bool first = true;
     ObSeq sq = {};
-    float m[2], l[2], slope[2];  // pass 1: this lane's row of each row tile
-    View vw[2];
-    bool live[2];
-    const int copy = gl / p.rp, c_lo = copy * (kObTile / p.rep), c_n = kObTile / p.rep;  // pass 1: this copy's columns
+    View v0 = {}, v1 = {}, vw = {};  // of the first and last query; pass 1: of this lane's row
+    float m = 0.f, l = 0.f, slope = 0.f;
+    // pass 1: this lane's row, and the columns its copy takes
+    const int copy = gl / p.rp, c_n = kObTile / p.rep, c_lo = copy * c_n, r_own = gl % p.rp;
+    const bool live = r_own < n_rows, warp_live = (quad * 32) % p.rp < n_rows;
+    int turn = 0;  // tiles this group has taken
     for (int i = 0; i < n_x; ++i) {  // (also after a wait that ran out: the group's barriers stay matched)
       if (first) {
         sq = ob_seq(p, c.b);
+        v0 = view_at(p.rule, c.b, max(sq.last - p.n_obs + 1, -1));
+        v1 = view_at(p.rule, c.b, sq.last);
         if (PASS == 1) {
-#pragma unroll
-          for (int tt = 0; tt < 2; ++tt) {
-            const int r = tt * kObTile + gl % p.rp;
-            m[tt] = no_max ? 0.f : -INFINITY;
-            l[tt] = 0.f;
-            live[tt] = tt < p.nt && copy < p.rep && r < p.rows;
-            vw[tt] = view_at(p.rule, c.b, max(sq.last - p.n_obs + 1 + (live[tt] ? r / p.nq : 0), -1));
-            slope[tt] = live[tt] && p.rule.slopes ? p.rule.slopes[c.g * p.nq + r % p.nq] * kLog2e : 0.f;
-          }
+          m = no_max ? 0.f : -INFINITY;
+          l = 0.f;
+          const int r = row0 + (live ? r_own : 0);
+          vw = view_at(p.rule, c.b, max(sq.last - p.n_obs + 1 + r / p.nq, -1));
+          slope = p.rule.slopes ? p.rule.slopes[c.g * p.nq + r % p.nq] * kLog2e : 0.f;
         } else {
-          // log-sum-exp of every row, from the partial sums of the CTAs that share the segment
+          // -log-sum-exp of every row, from the partial sums of the CTAs that share the segment
           const long long x0 = pre_s[c.b] + (long long)c.g * c.u;
           const int c0 = (int)(((x0 + 1) * T - 1) / U), c1 = (int)(((x0 + c.u) * T - 1) / U);
           group_sync(grp);  // everybody has done with the segment before
-          for (int r = gl; r < p.rows; r += kObTile) {
+          if (gl < n_rows) {
+            const int r = row0 + gl;
             float mm = -INFINITY, ll = 0.f;
             for (int cc = c0; cc <= c1; ++cc) {
-              const float4 v = *reinterpret_cast<const float4*>(p.part_ml + ((size_t)(cc + c.b * H + c.g) * p.rows + r) * 4);
-              const float M = fmaxf(mm, fmaxf(v.x, v.z));
-              ll = (ll == 0.f ? 0.f : ll * exp2f(mm - M)) + (v.y == 0.f ? 0.f : v.y * exp2f(v.x - M)) +
-                   (v.w == 0.f ? 0.f : v.w * exp2f(v.z - M));
-              mm = M;
+              const float2* q = reinterpret_cast<const float2*>(p.part_ml) + ((size_t)(cc + c.b * H + c.g) * p.rows + r) * p.slots;
+              for (int k = 0; k < p.slots; ++k) {
+                const float2 v = q[k];
+                const float M = fmaxf(mm, v.x);
+                ll = (ll == 0.f ? 0.f : ll * ex2(mm - M)) + (v.y == 0.f ? 0.f : v.y * ex2(v.x - M));
+                mm = M;
+              }
             }
-            row_g[r] = ll == 0.f ? INFINITY : mm + log2f(ll);  // (a row that saw nothing gives nothing)
-            row_g[kObMaxRows + r] = p.rule.slopes ? p.rule.slopes[c.g * p.nq + r % p.nq] * kLog2e : 0.f;
+            row_g[gl] = ll == 0.f ? -INFINITY : -(mm + log2f(ll));  // (a row that saw nothing gives nothing)
+            row_g[kObTile + gl] = p.rule.slopes ? p.rule.slopes[c.g * p.nq + r % p.nq] * kLog2e : 0.f;
+            const View v = view_at(p.rule, c.b, max(sq.last - p.n_obs + 1 + r / p.nq, -1));
+            row_q[gl] = v.q_pos;
+            row_q[kObTile + gl] = v.lo_pos;
           }
           group_sync(grp);
         }
       }
       first = last_of_seg(c, i);
-      if ((i & 1) == grp) {
+      if ((i & g_mask) == mine) {
         const int t0 = (c.k < sq.ua ? c.k : sq.ub0 + c.k - sq.ua) * kObTile;
         // a tile that every query sees whole needs no masks
-        const int qp0 = max(sq.last - p.n_obs + 1, -1);
-        const View v0 = view_at(p.rule, c.b, qp0), v1 = view_at(p.rule, c.b, sq.last);
-        const bool whole = p.positions == nullptr && t0 + kObTile <= sq.n && t0 + kObTile - 1 <= qp0 &&
-                           (t0 + kObTile <= v0.prefix || t0 >= v1.lo_pos);
-        const bool easy = whole && p.rule.slopes == nullptr;
+        const bool easy = p.positions == nullptr && p.rule.slopes == nullptr && t0 + kObTile <= sq.n && t0 + kObTile - 1 <= v0.q_pos &&
+                          (t0 + kObTile <= v0.prefix || t0 >= v1.lo_pos);
         // this thread's token: position, and in pass 2 where its weight goes
         const int t = t0 + gl;
         int pos = t < sq.n ? t : kObNoToken;
@@ -380,107 +447,142 @@ layer_observe_kernel(const __grid_constant__ ObserveParams p, const __grid_const
           group_sync(grp);
         }
         float w_old = 0.f;
-        if (PASS == 2 && p.add && dst) w_old = *dst;
-        const bool good = __all_sync(0xffffffffu, mbar_wait(tfull0 + 8 * grp, (i >> 1) & 1, s_abort, p.status));
+        if (PASS == 2 && p.add && dst && tt == 0) w_old = *dst;
+        const bool good = __all_sync(0xffffffffu, mbar_wait(tfull0 + 8 * grp, turn & 1, s_abort, p.status));
+        ++turn;
         tc_fence_after();
-        if (!good) {
-        } else if (PASS == 1) {
+        float w = 0.f;
+        if (good && PASS == 1 && warp_live) {
+          uint64_t lr = pack2(l, 0.f);
+          auto take = [&](uint32_t (&raw)[16], int c0) {  // 16 columns from c0 on
+            float s[16];
+            capped16<CAP>(p.rule, raw, s);
+            float f = factor;  // what is left to multiply by
+            if (!easy) {
+              f = 1.f;
 #pragma unroll
-          for (int tt = 0; tt < 2; ++tt) {
-            if (tt * kObTile + (quad * 32) % p.rp >= p.rows) continue;  // (no lane of this warp has a row)
-            float mr = m[tt], lr = l[tt];
-            for (int c0 = 0; c0 < c_n; c0 += 32) {
-              uint32_t raw[32];
-              tmem_ld32(tbuf + tt * kObTile + c_lo + c0, raw);
-              float s[32];
-#pragma unroll
-              for (int k = 0; k < 32; ++k) s[k] = score_of(p.rule, __uint_as_float(raw[k]));
-              if (!easy) {
-#pragma unroll
-                for (int k = 0; k < 32; ++k) {
-                  const int pk = pos_g[c_lo + c0 + k];
-                  s[k] = vw[tt].sees(pk) ? fmaf(-slope[tt], (float)(vw[tt].q_pos - pk), s[k]) : -INFINITY;
-                }
+              for (int k = 0; k < 16; ++k) {
+                const int pk = pos_g[c0 + k];
+                s[k] = vw.sees(pk) ? fmaf(-slope, (float)(vw.q_pos - pk), s[k] * factor) : -INFINITY;
               }
-              if (!no_max) {
-                float mx = s[0];
-#pragma unroll
-                for (int k = 1; k < 32; ++k) mx = fmaxf(mx, s[k]);
-                if (mx > mr) {
-                  lr *= exp2f(mr - mx);  // (l = 0 while m = -inf)
-                  mr = mx;
-                }
-              }
-              const float mb = mr == -INFINITY ? 0.f : mr;
-              float sum0 = 0.f, sum1 = 0.f;
-#pragma unroll
-              for (int k = 0; k < 32; k += 2) {
-                sum0 += exp2f(s[k] - mb);
-                sum1 += exp2f(s[k + 1] - mb);
-              }
-              lr += sum0 + sum1;
             }
-            m[tt] = mr;
-            l[tt] = lr;
-          }
-        } else {
-          float w0 = 0.f, w1 = 0.f;
-          for (int r0 = 0; r0 < p.rows; r0 += 32) {
-            uint32_t raw[32];
-            tmem_ld32(tbuf + r0, raw);
-            const int nr = min(32, p.rows - r0);
-            if (easy && nr == 32) {
+            if (!no_max) {
+              float mx = s[0];
+              if (f >= 0.f) {
 #pragma unroll
-              for (int k = 0; k < 32; k += 2) {
-                w0 += exp2f(score_of(p.rule, __uint_as_float(raw[k])) - row_g[r0 + k]);
-                w1 += exp2f(score_of(p.rule, __uint_as_float(raw[k + 1])) - row_g[r0 + k + 1]);
+                for (int k = 1; k < 15; k += 2) mx = max3(mx, s[k], s[k + 1]);
+                mx = fmaxf(mx, s[15]);
+              } else {
+#pragma unroll
+                for (int k = 1; k < 16; ++k) mx = fminf(mx, s[k]);
+              }
+              mx *= f;
+              if (mx > m) {
+                const float g = ex2(m - mx);  // (l = 0 while m = -inf)
+                lr = mul2(lr, pack2(g, g));
+                m = mx;
+              }
+            }
+            const float mb = m == -INFINITY ? 0.f : m;
+            const uint64_t f2 = pack2(f, f), n2 = pack2(-mb, -mb);
+            uint64_t sum0 = 0, sum1 = 0;
+#pragma unroll
+            for (int k = 0; k < 16; k += 4) {
+              float e0, e1, e2, e3;
+              unpack2(fma2(pack2(s[k], s[k + 1]), f2, n2), e0, e1);
+              unpack2(fma2(pack2(s[k + 2], s[k + 3]), f2, n2), e2, e3);
+              sum0 = add2(sum0, pack2(ex2(e0), ex2(e1)));
+              sum1 = add2(sum1, pack2(ex2(e2), ex2(e3)));
+            }
+            lr = add2(lr, add2(sum0, sum1));
+          };
+          // the next 16 columns travel while these are worked on (c_n is 32, 64 or 128)
+          uint32_t ra[16], rb[16];
+          tmem_ld16_async(tbuf + c_lo, ra);
+#pragma unroll 1
+          for (int ch = c_lo; ch < c_lo + c_n; ch += 32) {
+            tmem_wait16(ra);
+            tmem_ld16_async(tbuf + ch + 16, rb);
+            take(ra, ch);
+            tmem_wait16(rb);
+            if (ch + 32 < c_lo + c_n) tmem_ld16_async(tbuf + ch + 32, ra);
+            take(rb, ch + 16);
+          }
+          float la, lb;
+          unpack2(lr, la, lb);
+          l = la + lb;
+        } else if (good && PASS == 2) {
+          uint64_t wa = 0, wb = 0;
+          auto take = [&](uint32_t (&raw)[16], int r0) {  // 16 rows from r0 on
+            float s[16];
+            capped16<CAP>(p.rule, raw, s);
+            if (easy && r0 + 16 <= n_rows) {
+              const ulonglong2* z2 = reinterpret_cast<const ulonglong2*>(row_g + r0);
+#pragma unroll
+              for (int k = 0; k < 16; k += 4) {
+                const ulonglong2 z = z2[k / 4];
+                float e0, e1, e2, e3;
+                unpack2(fma2(pack2(s[k], s[k + 1]), factor2, z.x), e0, e1);
+                unpack2(fma2(pack2(s[k + 2], s[k + 3]), factor2, z.y), e2, e3);
+                wa = add2(wa, pack2(ex2(e0), ex2(e1)));
+                wb = add2(wb, pack2(ex2(e2), ex2(e3)));
               }
             } else {
 #pragma unroll
-              for (int k = 0; k < 32; ++k) {
-                if (k < nr) {
-                  const int r = r0 + k;
-                  float s = score_of(p.rule, __uint_as_float(raw[k]));
-                  bool sees = true;
-                  if (!easy) {
-                    const int qp = max(qp0, sq.last - p.n_obs + 1 + r / p.nq);
-                    const int lo = p.rule.window > 0 ? max(p.rule.doc_start ? p.rule.doc_start[c.b] : 0, qp - p.rule.window + 1) : v0.lo_pos;
-                    sees = pos <= qp && (pos < v0.prefix || pos >= lo);
-                    s = fmaf(-row_g[kObMaxRows + r], (float)(qp - pos), s);
-                  }
-                  if (sees) w0 += exp2f(s - row_g[r]);
+              for (int k = 0; k < 16; ++k) {
+                const int r = r0 + k;
+                if (r < n_rows) {
+                  const View v = {row_q[r], v0.prefix, row_q[kObTile + r]};
+                  const float e = fmaf(-row_g[kObTile + r], (float)(v.q_pos - pos), fmaf(s[k], factor, row_g[r]));
+                  if (v.sees(pos)) w += ex2(e);
                 }
               }
             }
+          };
+          uint32_t ra[16], rb[16];
+          tmem_ld16_async(tbuf, ra);
+#pragma unroll 1
+          for (int r0 = 0; r0 < n_rows; r0 += 32) {
+            tmem_wait16(ra);
+            if (r0 + 16 < n_rows) tmem_ld16_async(tbuf + r0 + 16, rb);
+            take(ra, r0);
+            tmem_wait16(rb);
+            if (r0 + 32 < n_rows) tmem_ld16_async(tbuf + r0 + 32, ra);
+            if (r0 + 16 < n_rows) take(rb, r0 + 16);
           }
-          if (dst) *dst = w_old + (w0 + w1);
+          float a0, a1, b0, b1;
+          unpack2(wa, a0, a1);
+          unpack2(wb, b0, b1);
+          w += (a0 + a1) + (b0 + b1);
         }
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(tempty0 + 8 * grp);
+        if (PASS == 2) {
+          if (p.nt == 2) {  // the two row tiles' sums meet in the first one's group
+            if (tt == 1) pos_g[gl] = __float_as_int(w);
+            pair_sync(grp >> 1);
+            if (tt == 0) w += __int_as_float(pos_g[kObTile + gl]);
+            pair_sync(grp >> 1);
+          }
+          if (dst && tt == 0) *dst = w_old + w;
+        }
       }
       if (PASS == 1 && first) {
         // the copies of a row meet; one partial result per (CTA, segment, group)
-#pragma unroll
-        for (int tt = 0; tt < 2; ++tt) {
-          if (tt >= p.nt) continue;
-          group_sync(grp);
-          row_g[2 * gl] = l[tt] == 0.f ? -INFINITY : m[tt];
-          row_g[2 * gl + 1] = live[tt] ? l[tt] : 0.f;
-          group_sync(grp);
-          const int r = tt * kObTile + gl;
-          if (gl < p.rp && r < p.rows) {
-            float mm = -INFINITY, ll = 0.f;
-            for (int k = 0; k < p.rep; ++k) {
-              const float mk = row_g[2 * (k * p.rp + gl)], lk = row_g[2 * (k * p.rp + gl) + 1];
-              const float M = fmaxf(mm, mk);
-              ll = (ll == 0.f ? 0.f : ll * exp2f(mm - M)) + (lk == 0.f ? 0.f : lk * exp2f(mk - M));
-              mm = M;
-            }
-            float* o = p.part_ml + (((size_t)(cta + c.b * H + c.g) * p.rows + r) * 2 + grp) * 2;
-            o[0] = mm;
-            o[1] = ll;
+        group_sync(grp);
+        row_g[2 * gl] = l == 0.f ? -INFINITY : m;
+        row_g[2 * gl + 1] = live ? l : 0.f;
+        group_sync(grp);
+        if (gl < p.rp && gl < n_rows) {
+          float mm = -INFINITY, ll = 0.f;
+          for (int k = 0; k < p.rep; ++k) {
+            const float mk = row_g[2 * (k * p.rp + gl)], lk = row_g[2 * (k * p.rp + gl) + 1];
+            const float M = fmaxf(mm, mk);
+            ll = (ll == 0.f ? 0.f : ll * ex2(mm - M)) + (lk == 0.f ? 0.f : lk * ex2(mk - M));
+            mm = M;
           }
+          reinterpret_cast<float2*>(p.part_ml)[((size_t)(cta + c.b * H + c.g) * p.rows + row0 + gl) * p.slots + mine] = make_float2(mm, ll);
         }
       }
       if (i + 1 < n_x) advance(c, x_first + DIR * (i + 1));
@@ -498,7 +600,7 @@ layer_observe_kernel(const __grid_constant__ ObserveParams p, const __grid_const
 constexpr int kObMaxCtas = 256;
 size_t layer_observe_workspace_bytes(const mc_config* cfg, const mc_batch* bt, int n_obs) {
   const size_t rows = (size_t)n_obs * (cfg->n_q_heads / cfg->n_kv_heads);
-  return align_up(((size_t)kObMaxCtas + (size_t)bt->batch * cfg->n_kv_heads) * rows * 4 * sizeof(float), 256);
+  return align_up(((size_t)kObMaxCtas + (size_t)bt->batch * cfg->n_kv_heads) * rows * kObGroups * 2 * sizeof(float), 256);
 }
 
 mc_status launch_layer_observe(const mc_config* cfg, const mc_batch* bt, const Geom& g, const mc_layer_cache* layer,
@@ -518,10 +620,11 @@ mc_status launch_layer_observe(const mc_config* cfg, const mc_batch* bt, const G
   op.n_q_heads = cfg->n_q_heads;
   op.rows = n_obs * op.nq;
   op.nt = op.rows > kObTile ? 2 : 1;
+  op.slots = kObGroups / op.nt;
   op.rp = op.rows > 64 ? 128 : (op.rows > 32 ? 64 : 32);
   op.rep = kObTile / op.rp;
   op.jt = std::min(n_obs, kObTile / op.nq);
-  op.stages = op.nt == 1 ? kObMaxStages : 2;
+  op.stage_shift = op.nt == 1 ? 2 : 1;
   const bool hidden_tiles = opts->window > 0 || opts->doc_start != nullptr || opts->q_pos != nullptr;
   op.zero = !(flags & MC_LAYER_ACCUMULATE) && hidden_tiles;
   op.add = (flags & MC_LAYER_ACCUMULATE) || hidden_tiles;
@@ -531,10 +634,15 @@ mc_status launch_layer_observe(const mc_config* cfg, const mc_batch* bt, const G
   const uint64_t rows = (uint64_t)bt->n_pages * cfg->n_kv_heads * cfg->page_size;
   if (mc_status st = make_map(&map_k, cfg->dtype, layer->k_pool, rows, kHeadDim, cfg->page_size)) return st;
   if (mc_status st = make_map3(&map_q, cfg->dtype, q, (uint64_t)bt->batch * n_obs, cfg->n_q_heads, kHeadDim, op.jt, op.nq)) return st;
-  const size_t smem = 1024 + kObSmem + (2 * kObMaxStages + 8) * 8 + 8 + 2 * kObMaxRows * 2 * 4 + 2 * kObTile * 4 + (size_t)(bt->batch + 1) * 4;
+  const size_t smem = 1024 + kObSmem + (2 * kObMaxStages + 4 + 2 * kObGroups) * 8 + 16 + kObGroups * kObTile * (2 * 8 + 4) + (size_t)(bt->batch + 1) * 4;
+  using Kernel = void (*)(const ObserveParams, const CUtensorMap, const CUtensorMap);
+  static const Kernel kernels[2][2][2] = {
+      {{layer_observe_kernel<MC_F16, 1, false>, layer_observe_kernel<MC_F16, 1, true>},
+       {layer_observe_kernel<MC_F16, 2, false>, layer_observe_kernel<MC_F16, 2, true>}},
+      {{layer_observe_kernel<MC_BF16, 1, false>, layer_observe_kernel<MC_BF16, 1, true>},
+       {layer_observe_kernel<MC_BF16, 2, false>, layer_observe_kernel<MC_BF16, 2, true>}}};
   for (int pass = 1; pass <= 2; ++pass) {
-    auto* kern = cfg->dtype == MC_F16 ? (pass == 1 ? layer_observe_kernel<MC_F16, 1> : layer_observe_kernel<MC_F16, 2>)
-                                      : (pass == 1 ? layer_observe_kernel<MC_BF16, 1> : layer_observe_kernel<MC_BF16, 2>);
+    const Kernel kern = kernels[cfg->dtype == MC_F16 ? 0 : 1][pass - 1][opts->softcap > 0.f ? 1 : 0];
     MC_CUDA_CHECK(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
     MC_CUDA_CHECK(launch_pdl(kern, dim3(op.n_ctas), dim3(kObThreads), smem, stream, op, map_k, map_q));
   }
