@@ -7,6 +7,12 @@ namespace mc {
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLn2 = 0.69314718055994530942f;
 
+// tanh(x) = x P(x^2) by reweighted least squares on tanh(x) / x: degree 4 on [-1/2, 1/2] (1.3e-8 relative), degree 6 on
+// [-1, 1] (5e-8).
+constexpr float kTanhTiny[5] = {9.9999998687e-01f, -3.3333069391e-01f, 1.3324779261e-01f, -5.2986071693e-02f, 1.7134999450e-02f};
+constexpr float kTanhSmall[7] = {9.9999995024e-01f, -3.3332839133e-01f, 1.3325203849e-01f, -5.3457019959e-02f,
+                                 2.0289962009e-02f, -6.2033628195e-03f, 1.0410172275e-03f};
+
 // The score rule of a call (mc_score_opts) in the form the kernels use; scores are kept as log2(e) times their value,
 // so that a probability is one instruction.
 struct ScoreRule {
@@ -75,29 +81,6 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
   uint64_t r;
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
   return r;
-}
-// tanh of two numbers in [-1, 1]: x P(x^2), P of degree 6 fitted to tanh(x) / x on [0, 1] by reweighted least squares
-// (5e-8 relative before rounding): no special-function unit, which the exponentials need.
-__device__ __forceinline__ uint64_t tanh2_small(uint64_t x) {
-  const uint64_t z = mul2(x, x);
-  uint64_t q = pack2(1.0410172275e-03f, 1.0410172275e-03f);
-  q = fma2(q, z, pack2(-6.2033628195e-03f, -6.2033628195e-03f));
-  q = fma2(q, z, pack2(2.0289962009e-02f, 2.0289962009e-02f));
-  q = fma2(q, z, pack2(-5.3457019959e-02f, -5.3457019959e-02f));
-  q = fma2(q, z, pack2(1.3325203849e-01f, 1.3325203849e-01f));
-  q = fma2(q, z, pack2(-3.3332839133e-01f, -3.3332839133e-01f));
-  q = fma2(q, z, pack2(9.9999995024e-01f, 9.9999995024e-01f));
-  return mul2(x, q);
-}
-// The same in [-1/2, 1/2], degree 4.
-__device__ __forceinline__ uint64_t tanh2_tiny(uint64_t x) {
-  const uint64_t z = mul2(x, x);
-  uint64_t q = pack2(1.7134999450e-02f, 1.7134999450e-02f);
-  q = fma2(q, z, pack2(-5.2986071693e-02f, -5.2986071693e-02f));
-  q = fma2(q, z, pack2(1.3324779261e-01f, 1.3324779261e-01f));
-  q = fma2(q, z, pack2(-3.3333069391e-01f, -3.3333069391e-01f));
-  q = fma2(q, z, pack2(9.9999998687e-01f, 9.9999998687e-01f));
-  return mul2(x, q);
 }
 // The largest of three numbers, and of one and two magnitudes (sm_100's three-input forms).
 __device__ __forceinline__ float max3(float a, float b, float c) {

@@ -14,11 +14,13 @@
 // backwards: the keys read last are the ones still in L2.
 //
 // One persistent CTA per SM; the tiles of all (sequence, kv head) segments are shared out equally.  Warp 0 streams K
-// tiles (a tiled copy per page and 64-channel half) and the segments' Q; warp 1 issues tcgen05.mma into a tensor-memory
-// buffer per group of four warps: up to 128 rows the four groups take the tiles in turn, beyond that two groups share a
-// tile, one for each 128 rows.  (Two groups instead of four: the latencies of 9 cycles per instruction showed.)  The
-// exponentials bound it: 2 R per token, 16 a clock and SM.  Every wait is bounded; tensor memory is released on every
-// path.
+// tiles (a tiled copy per page and 64-channel half) and the segments' Q; warp 1 issues tcgen05.mma, four groups of four
+// warps take the scores out.  A unit is 64 columns of a tile's scores (pass 1: 64 tokens, pass 2: 64 rows); the units of
+// a tile go to 1, 2 or 4 groups, and every group has two tensor-memory buffers, so that its next unit is multiplied
+// while it works on this one.  Bounds: the keys' bytes, twice, and the 2 R exponentials per token (16 a clock and SM),
+// with the cap's polynomial on the FMA pipe next to them.  Every wait is bounded; tensor memory is released on every path.
+#include <math.h>
+
 #include <algorithm>
 
 #include "mc_layer.cuh"
@@ -33,6 +35,11 @@ constexpr int kObTile = 128;                             // tokens per tile
 constexpr int kObHalf = kObTile * 128;                   // bytes of a tile's 64-channel half
 constexpr int kObTileBytes = 2 * kObHalf;                // 32 KB
 constexpr int kObGroups = 4;                             // groups of four warps that take scores out of tensor memory
+constexpr int kObUnit = 128;                             // columns a group takes at a time: a tensor-memory buffer
+constexpr int kObGroupBufs = 512 / (kObGroups * kObUnit);
+constexpr int kObBufs = kObGroupBufs * kObGroups;
+constexpr int kObHalves = kObTile / kObUnit;             // pass 1: units per tile and row tile
+constexpr int kObChunk = 16;                             // columns in registers at a time (a row copy's share at least)
 constexpr int kObThreads = 64 + kObGroups * 128;         // producer, tensor-core issue, the groups
 constexpr int kObQBufs = 2;
 constexpr int kObMaxStages = 4;
@@ -49,13 +56,18 @@ struct ObserveParams {
   int n_obs, nq, n_q_heads;
   int rows;      // n_obs * nq
   int nt;        // row tiles of 128: 1 or 2
-  int slots;     // groups that share a row tile: 4 / nt
+  int slots;     // groups that share a row tile in pass 1: 4 / nt
+  int v1, v2;    // units per tile in pass 1 and pass 2: 1, 2 or 4
   int rp, rep;   // rows of a copy (32, 64 or 128), copies in a row tile
   int jt;        // queries per Q copy
   int stage_shift;  // K ring: 4 or 2 stages
   int add;       // pass 2 adds to the weights (else it writes them)
   int zero;      // pass 1 clears the weights first
   int n_ctas;
+  // Capped scores as d Q(d^2) straight from d = q.k: the polynomials of tanh with sm / cap and cap log2(e) folded into
+  // their coefficients, and the |d| up to which each of them holds.
+  float tiny[5], small[7];
+  float tiny_max, small_max;
 };
 
 // A sequence as the call sees it: tiles that hold a token some query sees (the first `ua`, then those from `ub0`).
@@ -112,33 +124,59 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map
 }
 __device__ __forceinline__ void group_sync(int grp) { asm volatile("bar.sync %0, 128;" ::"r"(1 + grp) : "memory"); }
 __device__ __forceinline__ void pair_sync(int pair) { asm volatile("bar.sync %0, 256;" ::"r"(1 + kObGroups + pair) : "memory"); }
+__device__ __forceinline__ void groups_sync() { asm volatile("bar.sync %0, 512;" ::"n"(3 + kObGroups) : "memory"); }
 
-// 16 accumulators -> tanh(sm q.k / cap) (CAP) or q.k unchanged; the score is `factor` times that.
+__device__ __forceinline__ void tmem_load(uint32_t addr, uint32_t (&r)[32]) { tmem_ld32(addr, r); }
+__device__ __forceinline__ void tmem_load(uint32_t addr, uint32_t (&r)[16]) {
+  tmem_ld16_async(addr, r);
+  tmem_wait16(r);
+}
+// Accumulators d -> factors t with score = d t (log2 units), two per 64-bit register: the scale, or the folded polynomial
+// of the cap (d may be replaced: beyond the polynomials' range the score itself goes there, with factor 1).
 template <bool CAP>
-__device__ __forceinline__ void capped16(const ScoreRule& r, const uint32_t (&raw)[16], float (&t)[16]) {
+__device__ __forceinline__ void factors(const ObserveParams& p, uint32_t (&raw)[kObChunk], uint64_t (&t)[kObChunk / 2]) {
   if (!CAP) {
 #pragma unroll
-    for (int k = 0; k < 16; ++k) t[k] = __uint_as_float(raw[k]);
+    for (int k = 0; k < kObChunk / 2; ++k) t[k] = pack2(p.rule.scale_log2, p.rule.scale_log2);
     return;
   }
-  const uint64_t inv = pack2(r.cap_inv, r.cap_inv);
   float big = 0.f;
 #pragma unroll
-  for (int k = 0; k < 16; k += 2) {
-    unpack2(mul2(pack2(__uint_as_float(raw[k]), __uint_as_float(raw[k + 1])), inv), t[k], t[k + 1]);
-    big = max3_abs(big, t[k], t[k + 1]);
-  }
+  for (int k = 0; k < kObChunk; k += 2) big = max3_abs(big, __uint_as_float(raw[k]), __uint_as_float(raw[k + 1]));
   // (a NaN is dropped by the maximum and stays one in every branch)
-  if (__all_sync(0xffffffffu, big <= 0.5f)) {
+  if (__all_sync(0xffffffffu, big <= p.tiny_max)) {
 #pragma unroll
-    for (int k = 0; k < 16; k += 2) unpack2(tanh2_tiny(pack2(t[k], t[k + 1])), t[k], t[k + 1]);
-  } else if (__all_sync(0xffffffffu, big <= 1.f)) {
+    for (int k = 0; k < kObChunk / 2; ++k) {
+      const uint64_t d = pack2(__uint_as_float(raw[2 * k]), __uint_as_float(raw[2 * k + 1])), z = mul2(d, d);
+      uint64_t q = pack2(p.tiny[4], p.tiny[4]);
 #pragma unroll
-    for (int k = 0; k < 16; k += 2) unpack2(tanh2_small(pack2(t[k], t[k + 1])), t[k], t[k + 1]);
+      for (int j = 3; j >= 0; --j) q = fma2(q, z, pack2(p.tiny[j], p.tiny[j]));
+      t[k] = q;
+    }
+  } else if (__all_sync(0xffffffffu, big <= p.small_max)) {
+#pragma unroll
+    for (int k = 0; k < kObChunk / 2; ++k) {
+      const uint64_t d = pack2(__uint_as_float(raw[2 * k]), __uint_as_float(raw[2 * k + 1])), z = mul2(d, d);
+      uint64_t q = pack2(p.small[6], p.small[6]);
+#pragma unroll
+      for (int j = 5; j >= 0; --j) q = fma2(q, z, pack2(p.small[j], p.small[j]));
+      t[k] = q;
+    }
   } else {
 #pragma unroll
-    for (int k = 0; k < 16; ++k) t[k] = tanh_score(t[k]);
+    for (int k = 0; k < kObChunk / 2; ++k) {
+      t[k] = pack2(1.f, 1.f);
+      raw[2 * k] = __float_as_uint(score_of(p.rule, __uint_as_float(raw[2 * k])));
+      raw[2 * k + 1] = __float_as_uint(score_of(p.rule, __uint_as_float(raw[2 * k + 1])));
+    }
   }
+}
+// 2^x of two numbers.  (Taking three pairs in eight by a polynomial on the FMA pipe instead of the special-function unit
+// lost 10 % on 256 uncapped rows: the warps wait for latencies, not for that unit.)
+__device__ __forceinline__ uint64_t ex2_both(uint64_t x) {
+  float a, b;
+  unpack2(x, a, b);
+  return pack2(ex2(a), ex2(b));
 }
 
 template <int DT, int PASS, bool CAP>
@@ -150,19 +188,19 @@ layer_observe_kernel(const __grid_constant__ ObserveParams p, const __grid_const
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   // barriers: K full / empty per stage, Q full / empty per buffer, accumulator full / empty per group
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + kObSmem);
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * kObMaxStages + 4 + 2 * kObGroups);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * kObMaxStages + 4 + 2 * kObBufs);
   volatile int* s_abort = reinterpret_cast<volatile int*>(tmem_slot + 1);
   float* row_s = reinterpret_cast<float*>(tmem_slot + 4);             // [groups][128][2]: pass 1 (m, l) of the lanes; pass 2 -lse, slope
   int* view_s = reinterpret_cast<int*>(row_s + kObGroups * kObTile * 2);  // [groups][2][128]: pass 2: position, lowest position seen
-  int* pos_s = view_s + kObGroups * kObTile * 2;                      // [groups][128]: pass 1: positions; pass 2: weights on their way
-  int* pre_s = pos_s + kObGroups * kObTile;                           // [batch + 1]
+  int* pos_s = view_s + kObGroups * kObTile * 2;                      // pass 1: [groups][128] positions; pass 2: [2 turns][groups][128] partial weights
+  int* pre_s = pos_s + 2 * kObGroups * kObTile;                           // [batch + 1]
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int H = p.g.n_kv_heads, ps = p.g.page_size, shift = p.g.page_shift;
   const uint32_t full0 = smem_u32(bars), empty0 = full0 + 8 * kObMaxStages, qfull0 = empty0 + 8 * kObMaxStages, qempty0 = qfull0 + 16;
-  const uint32_t tfull0 = qempty0 + 16, tempty0 = tfull0 + 8 * kObGroups;
+  const uint32_t tfull0 = qempty0 + 16, tempty0 = tfull0 + 8 * kObBufs;
   const int q_bytes = p.nt * kObTileBytes, q_half = p.nt * kObHalf;
   const uint32_t sq0 = smem_u32(smem), sk0 = sq0 + kObQBufs * q_bytes;
-  constexpr uint32_t tmem_cols = kObGroups * kObTile;
+  constexpr uint32_t tmem_cols = kObBufs * kObUnit;
 
   int bad = 0;
   for (int b = tid; b < p.g.batch; b += kObThreads) {
@@ -179,7 +217,7 @@ layer_observe_kernel(const __grid_constant__ ObserveParams p, const __grid_const
       mbar_init(qfull0 + 8 * s, 1);
       mbar_init(qempty0 + 8 * s, 1);
     }
-    for (int s = 0; s < kObGroups; ++s) {
+    for (int s = 0; s < kObBufs; ++s) {
       mbar_init(tfull0 + 8 * s, 1);
       mbar_init(tempty0 + 8 * s, 4);
     }
@@ -278,7 +316,7 @@ layer_observe_kernel(const __grid_constant__ ObserveParams p, const __grid_const
       }
       if (first) {
         const int qb = seg & 1;
-        if (seg >= 2) ok = __all_sync(0xffffffffu, mbar_wait(qempty0 + 8 * qb, ((seg >> 1) - 1) & 1, s_abort, p.status));
+        if (seg >= 2) ok = __all_sync(0xffffffffu, mbar_wait_lean(qempty0 + 8 * qb, ((seg >> 1) - 1) & 1, s_abort, p.status));
         if (!ok) break;
         if (lane == 0) {
           const uint32_t bar = qfull0 + 8 * qb, dst = sq0 + qb * q_bytes;
@@ -291,7 +329,7 @@ layer_observe_kernel(const __grid_constant__ ObserveParams p, const __grid_const
         __syncwarp();
       }
       const int s = i & s_mask, lap = i >> p.stage_shift;
-      if (lap > 0) ok = __all_sync(0xffffffffu, mbar_wait(empty0 + 8 * s, (lap - 1) & 1, s_abort, p.status));
+      if (lap > 0) ok = __all_sync(0xffffffffu, mbar_wait_lean(empty0 + 8 * s, (lap - 1) & 1, s_abort, p.status));
       if (!ok) break;
       const uint32_t bar = full0 + 8 * s, dst = sk0 + s * kObTileBytes;
       const bool copies = has && lane_tile == in_win;
@@ -325,34 +363,36 @@ layer_observe_kernel(const __grid_constant__ ObserveParams p, const __grid_const
       // units (and the fixed bits), its high word never changes; k step 4 starts the second 64-channel half.
       const uint64_t d0 = smem_desc_k128(0);
       const uint32_t d_hi = (uint32_t)(d0 >> 32), d_lo = (uint32_t)d0, q_step = (uint32_t)(q_half >> 4);
-      uint32_t idesc[2];
-#pragma unroll
-      for (int tt = 0; tt < 2; ++tt) {
-        const int n_cols = PASS == 1 ? kObTile : (max(min(p.rows - tt * kObTile, kObTile), 1) + 15) / 16 * 16;
-        idesc[tt] = umma_idesc<DT, 8>() - (1u << 17) + ((uint32_t)(n_cols >> 3) << 17);
-      }
+      const int V = PASS == 1 ? p.v1 : p.v2, v_shift = V == 1 ? 0 : (V == 2 ? 1 : 2);
+      const uint32_t idesc_full = umma_idesc<DT, kObUnit>();
       for (int i = 0; i < n_x && ok; ++i) {
         const int s = i & s_mask, qb = seg & 1;
-        if (first && !mbar_wait(qfull0 + 8 * qb, (seg >> 1) & 1, s_abort, p.status)) break;
-        if (!mbar_wait(full0 + 8 * s, (i >> p.stage_shift) & 1, s_abort, p.status)) break;
+        if (first && !mbar_wait_lean(qfull0 + 8 * qb, (seg >> 1) & 1, s_abort, p.status)) break;
+        if (!mbar_wait_lean(full0 + 8 * s, (i >> p.stage_shift) & 1, s_abort, p.status)) break;
         const uint32_t q_lo = d_lo + ((sq0 + qb * q_bytes) >> 4), k_lo = d_lo + ((sk0 + s * kObTileBytes) >> 4);
-#pragma unroll
-        for (int tt = 0; tt < 2; ++tt) {
-          if (tt >= p.nt) break;
-          const int grp = p.nt == 1 ? i & 3 : 2 * (i & 1) + tt, turn = p.nt == 1 ? i >> 2 : i >> 1;
-          if (turn >= 1) ok = mbar_wait(tempty0 + 8 * grp, (turn - 1) & 1, s_abort, p.status);
+        const int turn = i >> (2 - v_shift), lap = turn / kObGroupBufs;
+        for (int v = 0; v < V; ++v) {
+          const int buf = kObGroupBufs * (((i << v_shift) + v) & 3) + turn % kObGroupBufs;
+          if (lap >= 1) ok = mbar_wait_lean(tempty0 + 8 * buf, (lap - 1) & 1, s_abort, p.status);
           if (!ok) break;
           tc_fence_after();
-          const uint32_t d = tmem_d + grp * kObTile;
+          const uint32_t d = tmem_d + buf * kObUnit;
+          // pass 1: a row tile against a unit of tokens; pass 2: the tile's tokens against a unit of rows
+          const uint32_t qv = q_lo + (uint32_t)((PASS == 1 ? v / kObHalves * kObTile : v * kObUnit) * 8);
+          const uint32_t kv = k_lo + (uint32_t)((PASS == 1 ? v % kObHalves * kObUnit : 0) * 8);
+          const int left = p.rows - v * kObUnit;
+          const uint32_t idesc = PASS == 1 || left >= kObUnit
+                                     ? idesc_full
+                                     : umma_idesc<DT, 8>() - (1u << 17) + ((uint32_t)((max(left, 1) + 15) / 16 * 2) << 17);
 #pragma unroll
           for (int k = 0; k < kHeadDim / 16; ++k) {
-            const uint32_t ql = q_lo + (k >= 4 ? q_step : 0u) + (uint32_t)(tt * (kObHalf >> 4) + 2 * (k & 3));
-            const uint32_t kl = k_lo + (uint32_t)((k >> 2) * (kObHalf >> 4) + 2 * (k & 3));
+            const uint32_t ql = qv + (k >= 4 ? q_step : 0u) + (uint32_t)(2 * (k & 3));
+            const uint32_t kl = kv + (uint32_t)((k >> 2) * (kObHalf >> 4) + 2 * (k & 3));
             const uint64_t dq = ((uint64_t)d_hi << 32) | ql, dk = ((uint64_t)d_hi << 32) | kl;
-            if (PASS == 1) umma_f16(d, dq, dk, idesc[tt], k > 0 ? 1u : 0u);
-            else umma_f16(d, dk, dq, idesc[tt], k > 0 ? 1u : 0u);
+            if (PASS == 1) umma_f16(d, dq, dk, idesc, k > 0 ? 1u : 0u);
+            else umma_f16(d, dk, dq, idesc, k > 0 ? 1u : 0u);
           }
-          umma_commit(tfull0 + 8 * grp);
+          umma_commit(tfull0 + 8 * buf);
         }
         umma_commit(empty0 + 8 * s);
         first = last_of_seg(c, i);
@@ -365,228 +405,242 @@ layer_observe_kernel(const __grid_constant__ ObserveParams p, const __grid_const
     }
   } else {
     // ===================== scores =====================
-    // group: with one row tile it takes every fourth tile, with two row tiles every second one, the rows of tile `tt`
+    // the group takes unit v of the tiles mine, mine + stride, ...
     const int grp = (warp - 2) >> 2, quad = warp & 3, gl = quad * 32 + lane;  // gl: this thread's tensor-memory lane
-    const int tt = p.nt == 1 ? 0 : grp & 1, g_mask = 4 / p.nt - 1, mine = p.nt == 1 ? grp : grp >> 1;
-    const int row0 = tt * kObTile, n_rows = min(p.rows - row0, kObTile);
-    const uint32_t tbuf = tmem_d + grp * kObTile + ((uint32_t)(quad * 32) << 16);
+    const int V = PASS == 1 ? p.v1 : p.v2, stride = 4 / V, mine = grp / V, v = grp % V;
+    const int row0 = PASS == 1 ? v / kObHalves * kObTile : v * kObUnit;  // its rows
+    const int n_rows = min(p.rows - row0, PASS == 1 ? kObTile : kObUnit);  // (may be none in pass 2)
+    const int tok0 = PASS == 1 ? v % kObHalves * kObUnit : 0;             // pass 1: where its tokens begin in the tile
+    const uint32_t tbuf0 = tmem_d + kObGroupBufs * grp * kObUnit + ((uint32_t)(quad * 32) << 16);
+    const uint32_t my_full = tfull0 + 8 * kObGroupBufs * grp, my_empty = tempty0 + 8 * kObGroupBufs * grp;
     float* row_g = row_s + grp * kObTile * 2;
     int* row_q = view_s + grp * kObTile * 2;
     int* pos_g = pos_s + grp * kObTile;
     const bool no_max = CAP && p.rule.cap_log2 <= 100.f && p.rule.slopes == nullptr;
-    const float factor = CAP ? p.rule.cap_log2 : p.rule.scale_log2;
-    const uint64_t factor2 = pack2(factor, factor);
-    ObCursor c;
-    if (n_x > 0) c.seek(pre_s, p.g.batch, H, x_first);
-    bool first = true;
-    ObSeq sq = {};
-    View v0 = {}, v1 = {}, vw = {};  // of the first and last query; pass 1: of this lane's row
-    float m = 0.f, l = 0.f, slope = 0.f;
     // pass 1: this lane's row, and the columns its copy takes
-    const int copy = gl / p.rp, c_n = kObTile / p.rep, c_lo = copy * c_n, r_own = gl % p.rp;
+    const int copy = gl / p.rp, c_n = kObUnit / p.rep, c_lo = copy * c_n, r_own = gl % p.rp;
     const bool live = r_own < n_rows, warp_live = (quad * 32) % p.rp < n_rows;
-    int turn = 0;  // tiles this group has taken
-    for (int i = 0; i < n_x; ++i) {  // (also after a wait that ran out: the group's barriers stay matched)
-      if (first) {
-        sq = ob_seq(p, c.b);
-        v0 = view_at(p.rule, c.b, max(sq.last - p.n_obs + 1, -1));
-        v1 = view_at(p.rule, c.b, sq.last);
-        if (PASS == 1) {
-          m = no_max ? 0.f : -INFINITY;
-          l = 0.f;
-          const int r = row0 + (live ? r_own : 0);
-          vw = view_at(p.rule, c.b, max(sq.last - p.n_obs + 1 + r / p.nq, -1));
-          slope = p.rule.slopes ? p.rule.slopes[c.g * p.nq + r % p.nq] * kLog2e : 0.f;
-        } else {
-          // -log-sum-exp of every row, from the partial sums of the CTAs that share the segment
-          const long long x0 = pre_s[c.b] + (long long)c.g * c.u;
-          const int c0 = (int)(((x0 + 1) * T - 1) / U), c1 = (int)(((x0 + c.u) * T - 1) / U);
-          group_sync(grp);  // everybody has done with the segment before
-          if (gl < n_rows) {
-            const int r = row0 + gl;
-            float mm = -INFINITY, ll = 0.f;
-            for (int cc = c0; cc <= c1; ++cc) {
-              const float2* q = reinterpret_cast<const float2*>(p.part_ml) + ((size_t)(cc + c.b * H + c.g) * p.rows + r) * p.slots;
-              for (int k = 0; k < p.slots; ++k) {
-                const float2 v = q[k];
-                const float M = fmaxf(mm, v.x);
-                ll = (ll == 0.f ? 0.f : ll * ex2(mm - M)) + (v.y == 0.f ? 0.f : v.y * ex2(v.x - M));
-                mm = M;
-              }
+    View v0 = {}, vw = {};  // of the first query; pass 1: of this lane's row
+    float m = 0.f, l = 0.f, slope = 0.f;
+    int n = 0, skip = 0, ua = 0, easy_hi = 0, easy_pre = 0, easy_lo = 0;  // of the segment
+    const int32_t* table = p.g.block_table;
+    ObCursor c = {-1, 0, 0, 0};
+
+    auto begin_segment = [&]() {
+      const ObSeq sq = ob_seq(p, c.b);
+      n = sq.n;
+      ua = sq.ua;
+      skip = sq.ub0 - sq.ua;
+      table = p.g.block_table + (size_t)c.b * p.g.max_pages_per_seq;
+      v0 = view_at(p.rule, c.b, max(sq.last - p.n_obs + 1, -1));
+      const View v1 = view_at(p.rule, c.b, sq.last);
+      // a tile that every query sees whole needs no masks: t0 <= easy_hi and (t0 <= easy_pre or t0 >= easy_lo)
+      easy_hi = p.positions || p.rule.slopes ? -1 : min(n, v0.q_pos + 1) - kObTile;
+      easy_pre = v0.prefix - kObTile;
+      easy_lo = v1.lo_pos;
+      if (PASS == 1) {
+        m = no_max ? 0.f : -INFINITY;
+        l = 0.f;
+        const int r = row0 + (live ? r_own : 0);
+        vw = view_at(p.rule, c.b, max(sq.last - p.n_obs + 1 + r / p.nq, -1));
+        slope = p.rule.slopes ? p.rule.slopes[c.g * p.nq + r % p.nq] * kLog2e : 0.f;
+      } else {
+        // -log-sum-exp of every row, from the partial sums of the CTAs (and their groups) that share the segment
+        const long long x0 = pre_s[c.b] + (long long)c.g * c.u;
+        const int c0 = (int)(((x0 + 1) * T - 1) / U), c1 = (int)(((x0 + c.u) * T - 1) / U);
+        group_sync(grp);  // everybody has done with the segment before
+        if (gl < n_rows) {
+          const int r = row0 + gl;
+          float mm = -INFINITY, ll = 0.f;
+          for (int cc = c0; cc <= c1; ++cc) {
+            // tiles [i0, i1) of that CTA lie in the segment; a group has a part if one of them is its own
+            const long long xb = U * cc / T, xe = U * (cc + 1) / T;
+            const int i0 = (int)(max(x0, xb) - xb), i1 = (int)(min(x0 + c.u, xe) - xb);
+            const float2* q = reinterpret_cast<const float2*>(p.part_ml) + ((size_t)(cc + c.b * H + c.g) * p.rows + r) * p.slots;
+            const int s1 = 4 / p.v1;  // pass 1: tiles from one of a group's units to its next
+            for (int k = 0; k < p.slots; ++k) {
+              const int first1 = (p.nt == 1 ? k / p.v1 : (kObHalves == 2 ? 0 : k)) - i0;
+              if (i0 + (first1 & (s1 - 1)) >= i1) continue;
+              const float2 v = q[k];
+              const float M = fmaxf(mm, v.x);
+              ll = (ll == 0.f ? 0.f : ll * ex2(mm - M)) + (v.y == 0.f ? 0.f : v.y * ex2(v.x - M));
+              mm = M;
             }
-            row_g[gl] = ll == 0.f ? -INFINITY : -(mm + log2f(ll));  // (a row that saw nothing gives nothing)
-            row_g[kObTile + gl] = p.rule.slopes ? p.rule.slopes[c.g * p.nq + r % p.nq] * kLog2e : 0.f;
-            const View v = view_at(p.rule, c.b, max(sq.last - p.n_obs + 1 + r / p.nq, -1));
-            row_q[gl] = v.q_pos;
-            row_q[kObTile + gl] = v.lo_pos;
           }
-          group_sync(grp);
+          row_g[gl] = ll == 0.f ? -INFINITY : -(mm + log2f(ll));  // (a row that saw nothing gives nothing)
+          row_g[kObTile + gl] = p.rule.slopes ? p.rule.slopes[c.g * p.nq + r % p.nq] * kLog2e : 0.f;
+          const View v = view_at(p.rule, c.b, max(sq.last - p.n_obs + 1 + r / p.nq, -1));
+          row_q[gl] = v.q_pos;
+          row_q[kObTile + gl] = v.lo_pos;
+        }
+        group_sync(grp);
+      }
+    };
+    auto end_segment = [&]() {  // pass 1: the copies of a row meet; one partial result per (CTA, segment, group)
+      group_sync(grp);
+      row_g[2 * gl] = l == 0.f ? -INFINITY : m;
+      row_g[2 * gl + 1] = live ? l : 0.f;
+      group_sync(grp);
+      if (gl < p.rp && gl < n_rows) {
+        float mm = -INFINITY, ll = 0.f;
+        for (int k = 0; k < p.rep; ++k) {
+          const float mk = row_g[2 * (k * p.rp + gl)], lk = row_g[2 * (k * p.rp + gl) + 1];
+          const float M = fmaxf(mm, mk);
+          ll = (ll == 0.f ? 0.f : ll * ex2(mm - M)) + (lk == 0.f ? 0.f : lk * ex2(mk - M));
+          mm = M;
+        }
+        reinterpret_cast<float2*>(p.part_ml)[((size_t)(cta + c.b * H + c.g) * p.rows + row0 + gl) * p.slots + (p.nt == 1 ? grp : (kObHalves == 2 ? grp & 1 : grp >> 1))] = make_float2(mm, ll);
+      }
+    };
+
+    uint32_t turn = 0;  // tiles this group has taken
+    for (int i = mine; i < n_x; i += stride, ++turn) {  // (to the end also after a wait that ran out: the barriers stay matched)
+      if (c.b >= 0) c.k += DIR * stride;
+      if ((unsigned)c.k >= (unsigned)c.u) {
+        if (PASS == 1 && c.b >= 0) end_segment();
+        c.seek(pre_s, p.g.batch, H, x_first + DIR * i);
+        begin_segment();
+      }
+      const int t0 = (c.k < ua ? c.k : c.k + skip) * kObTile;
+      const bool easy = t0 <= easy_hi && (t0 <= easy_pre || t0 >= easy_lo);
+      // this thread's token: position, and in pass 2 where its weight goes
+      const int t = t0 + gl;
+      int pos = t < n ? t : kObNoToken;
+      float* dst = nullptr;
+      float w_old = 0.f;
+      if ((PASS == 2 || !easy) && t < n) {
+        const int page = table[t >> shift];
+        if (page_ok(p.g, page)) {
+          const int at = (page * H + c.g) * ps + (t & (ps - 1));
+          if (PASS == 2) {
+            dst = p.weights + at;
+            if (p.add && v == 0) w_old = *dst;
+          }
+          if (p.positions) pos = p.positions[at];
         }
       }
-      first = last_of_seg(c, i);
-      if ((i & g_mask) == mine) {
-        const int t0 = (c.k < sq.ua ? c.k : sq.ub0 + c.k - sq.ua) * kObTile;
-        // a tile that every query sees whole needs no masks
-        const bool easy = p.positions == nullptr && p.rule.slopes == nullptr && t0 + kObTile <= sq.n && t0 + kObTile - 1 <= v0.q_pos &&
-                          (t0 + kObTile <= v0.prefix || t0 >= v1.lo_pos);
-        // this thread's token: position, and in pass 2 where its weight goes
-        const int t = t0 + gl;
-        int pos = t < sq.n ? t : kObNoToken;
-        float* dst = nullptr;
-        if (t < sq.n && (PASS == 2 || p.positions)) {
-          const int page = p.g.block_table[(size_t)c.b * p.g.max_pages_per_seq + (t >> shift)];
-          const size_t at = ((size_t)page * H + c.g) * ps + (t & (ps - 1));
-          if (page_ok(p.g, page)) {
-            dst = p.weights + at;
-            if (p.positions) pos = p.positions[at];
-          }
-        }
-        if (PASS == 1 && !easy) {
-          group_sync(grp);
-          pos_g[gl] = pos;
-          group_sync(grp);
-        }
-        float w_old = 0.f;
-        if (PASS == 2 && p.add && dst && tt == 0) w_old = *dst;
-        const bool good = __all_sync(0xffffffffu, mbar_wait(tfull0 + 8 * grp, turn & 1, s_abort, p.status));
-        ++turn;
-        tc_fence_after();
-        float w = 0.f;
-        if (good && PASS == 1 && warp_live) {
-          uint64_t lr = pack2(l, 0.f);
-          auto take = [&](uint32_t (&raw)[16], int c0) {  // 16 columns from c0 on
-            float s[16];
-            capped16<CAP>(p.rule, raw, s);
-            float f = factor;  // what is left to multiply by
-            if (!easy) {
-              f = 1.f;
+      if (PASS == 1 && !easy) {
+        group_sync(grp);
+        pos_g[gl] = pos;
+        group_sync(grp);
+      }
+      const uint32_t b_off = turn % kObGroupBufs;
+      const uint32_t tbuf = tbuf0 + b_off * kObUnit;
+      const bool good = __all_sync(0xffffffffu, mbar_wait_lean(my_full + 8 * b_off, (turn / kObGroupBufs) & 1, s_abort, p.status));
+      tc_fence_after();
+      float w = 0.f;
+      if (good && PASS == 1 && warp_live) {
+        uint64_t lr = pack2(l, 0.f);
+#pragma unroll 1
+        for (int ch = c_lo; ch < c_lo + c_n; ch += kObChunk) {
+          uint32_t raw[kObChunk];
+          tmem_load(tbuf + ch, raw);
+          uint64_t f[kObChunk / 2];
+          factors<CAP>(p, raw, f);
+          if (!easy) {  // distance bias and masks: the scores themselves, factor 1
 #pragma unroll
-              for (int k = 0; k < 16; ++k) {
-                const int pk = pos_g[c0 + k];
-                s[k] = vw.sees(pk) ? fmaf(-slope, (float)(vw.q_pos - pk), s[k] * factor) : -INFINITY;
-              }
+            for (int k = 0; k < kObChunk; ++k) {
+              const int pk = pos_g[tok0 + ch + k];
+              float fa, fb;
+              unpack2(f[k / 2], fa, fb);
+              const float s = __uint_as_float(raw[k]) * ((k & 1) ? fb : fa);
+              raw[k] = __float_as_uint(vw.sees(pk) ? fmaf(-slope, (float)(vw.q_pos - pk), s) : -INFINITY);
+              if (k & 1) f[k / 2] = pack2(1.f, 1.f);
             }
-            if (!no_max) {
-              float mx = s[0];
-              if (f >= 0.f) {
+          }
+          if (!no_max) {
+            float mx;
+            if (CAP) {
+              float s[kObChunk];
 #pragma unroll
-                for (int k = 1; k < 15; k += 2) mx = max3(mx, s[k], s[k + 1]);
-                mx = fmaxf(mx, s[15]);
+              for (int k = 0; k < kObChunk; k += 2)
+                unpack2(mul2(pack2(__uint_as_float(raw[k]), __uint_as_float(raw[k + 1])), f[k / 2]), s[k], s[k + 1]);
+              mx = s[0];
+#pragma unroll
+              for (int k = 1; k < kObChunk; ++k) mx = fmaxf(mx, s[k]);
+            } else {
+              const float scale = easy ? p.rule.scale_log2 : 1.f;
+              mx = __uint_as_float(raw[0]);
+              if (scale >= 0.f) {
+#pragma unroll
+                for (int k = 1; k < kObChunk - 1; k += 2) mx = max3(mx, __uint_as_float(raw[k]), __uint_as_float(raw[k + 1]));
+                mx = fmaxf(mx, __uint_as_float(raw[kObChunk - 1]));
               } else {
 #pragma unroll
-                for (int k = 1; k < 16; ++k) mx = fminf(mx, s[k]);
+                for (int k = 1; k < kObChunk; ++k) mx = fminf(mx, __uint_as_float(raw[k]));
               }
-              mx *= f;
-              if (mx > m) {
-                const float g = ex2(m - mx);  // (l = 0 while m = -inf)
-                lr = mul2(lr, pack2(g, g));
-                m = mx;
-              }
+              mx *= scale;
             }
-            const float mb = m == -INFINITY ? 0.f : m;
-            const uint64_t f2 = pack2(f, f), n2 = pack2(-mb, -mb);
-            uint64_t sum0 = 0, sum1 = 0;
+            if (mx > m) {
+              const float g = ex2(m - mx);  // (l = 0 while m = -inf)
+              lr = mul2(lr, pack2(g, g));
+              m = mx;
+            }
+          }
+          const float mb = m == -INFINITY ? 0.f : m;
+          const uint64_t n2 = pack2(-mb, -mb);
+          uint64_t sum0 = 0, sum1 = 0;
 #pragma unroll
-            for (int k = 0; k < 16; k += 4) {
-              float e0, e1, e2, e3;
-              unpack2(fma2(pack2(s[k], s[k + 1]), f2, n2), e0, e1);
-              unpack2(fma2(pack2(s[k + 2], s[k + 3]), f2, n2), e2, e3);
-              sum0 = add2(sum0, pack2(ex2(e0), ex2(e1)));
-              sum1 = add2(sum1, pack2(ex2(e2), ex2(e3)));
-            }
-            lr = add2(lr, add2(sum0, sum1));
-          };
-          // the next 16 columns travel while these are worked on (c_n is 32, 64 or 128)
-          uint32_t ra[16], rb[16];
-          tmem_ld16_async(tbuf + c_lo, ra);
+          for (int k = 0; k < kObChunk; k += 4) {
+            sum0 = add2(sum0, ex2_both(fma2(pack2(__uint_as_float(raw[k]), __uint_as_float(raw[k + 1])), f[k / 2], n2)));
+            sum1 = add2(sum1, ex2_both(fma2(pack2(__uint_as_float(raw[k + 2]), __uint_as_float(raw[k + 3])), f[k / 2 + 1], n2)));
+          }
+          lr = add2(lr, add2(sum0, sum1));
+        }
+        float la, lb;
+        unpack2(lr, la, lb);
+        l = la + lb;
+      } else if (good && PASS == 2) {
+        uint64_t wa = 0, wb = 0;
 #pragma unroll 1
-          for (int ch = c_lo; ch < c_lo + c_n; ch += 32) {
-            tmem_wait16(ra);
-            tmem_ld16_async(tbuf + ch + 16, rb);
-            take(ra, ch);
-            tmem_wait16(rb);
-            if (ch + 32 < c_lo + c_n) tmem_ld16_async(tbuf + ch + 32, ra);
-            take(rb, ch + 16);
-          }
-          float la, lb;
-          unpack2(lr, la, lb);
-          l = la + lb;
-        } else if (good && PASS == 2) {
-          uint64_t wa = 0, wb = 0;
-          auto take = [&](uint32_t (&raw)[16], int r0) {  // 16 rows from r0 on
-            float s[16];
-            capped16<CAP>(p.rule, raw, s);
-            if (easy && r0 + 16 <= n_rows) {
-              const ulonglong2* z2 = reinterpret_cast<const ulonglong2*>(row_g + r0);
+        for (int r0 = 0; r0 < n_rows; r0 += kObChunk) {
+          uint32_t raw[kObChunk];
+          tmem_load(tbuf + r0, raw);
+          uint64_t f[kObChunk / 2];
+          factors<CAP>(p, raw, f);
+          if (easy && r0 + kObChunk <= n_rows) {
+            const ulonglong2* z2 = reinterpret_cast<const ulonglong2*>(row_g + r0);
 #pragma unroll
-              for (int k = 0; k < 16; k += 4) {
-                const ulonglong2 z = z2[k / 4];
-                float e0, e1, e2, e3;
-                unpack2(fma2(pack2(s[k], s[k + 1]), factor2, z.x), e0, e1);
-                unpack2(fma2(pack2(s[k + 2], s[k + 3]), factor2, z.y), e2, e3);
-                wa = add2(wa, pack2(ex2(e0), ex2(e1)));
-                wb = add2(wb, pack2(ex2(e2), ex2(e3)));
-              }
-            } else {
+            for (int k = 0; k < kObChunk; k += 4) {
+              const ulonglong2 z = z2[k / 4];
+              wa = add2(wa, ex2_both(fma2(pack2(__uint_as_float(raw[k]), __uint_as_float(raw[k + 1])), f[k / 2], z.x)));
+              wb = add2(wb, ex2_both(fma2(pack2(__uint_as_float(raw[k + 2]), __uint_as_float(raw[k + 3])), f[k / 2 + 1], z.y)));
+            }
+          } else {
 #pragma unroll
-              for (int k = 0; k < 16; ++k) {
-                const int r = r0 + k;
-                if (r < n_rows) {
-                  const View v = {row_q[r], v0.prefix, row_q[kObTile + r]};
-                  const float e = fmaf(-row_g[kObTile + r], (float)(v.q_pos - pos), fmaf(s[k], factor, row_g[r]));
-                  if (v.sees(pos)) w += ex2(e);
-                }
+            for (int k = 0; k < kObChunk; ++k) {
+              const int r = r0 + k;
+              if (r < n_rows) {
+                float fa, fb;
+                unpack2(f[k / 2], fa, fb);
+                const View v = {row_q[r], v0.prefix, row_q[kObTile + r]};
+                const float e = fmaf(-row_g[kObTile + r], (float)(v.q_pos - pos), fmaf(__uint_as_float(raw[k]), (k & 1) ? fb : fa, row_g[r]));
+                if (v.sees(pos)) w += ex2(e);
               }
             }
-          };
-          uint32_t ra[16], rb[16];
-          tmem_ld16_async(tbuf, ra);
-#pragma unroll 1
-          for (int r0 = 0; r0 < n_rows; r0 += 32) {
-            tmem_wait16(ra);
-            if (r0 + 16 < n_rows) tmem_ld16_async(tbuf + r0 + 16, rb);
-            take(ra, r0);
-            tmem_wait16(rb);
-            if (r0 + 32 < n_rows) tmem_ld16_async(tbuf + r0 + 32, ra);
-            if (r0 + 16 < n_rows) take(rb, r0 + 16);
           }
-          float a0, a1, b0, b1;
-          unpack2(wa, a0, a1);
-          unpack2(wb, b0, b1);
-          w += (a0 + a1) + (b0 + b1);
         }
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(tempty0 + 8 * grp);
-        if (PASS == 2) {
-          if (p.nt == 2) {  // the two row tiles' sums meet in the first one's group
-            if (tt == 1) pos_g[gl] = __float_as_int(w);
-            pair_sync(grp >> 1);
-            if (tt == 0) w += __int_as_float(pos_g[kObTile + gl]);
-            pair_sync(grp >> 1);
-          }
-          if (dst && tt == 0) *dst = w_old + w;
-        }
+        float a0, a1, b0, b1;
+        unpack2(wa, a0, a1);
+        unpack2(wb, b0, b1);
+        w += (a0 + a1) + (b0 + b1);
       }
-      if (PASS == 1 && first) {
-        // the copies of a row meet; one partial result per (CTA, segment, group)
-        group_sync(grp);
-        row_g[2 * gl] = l == 0.f ? -INFINITY : m;
-        row_g[2 * gl + 1] = live ? l : 0.f;
-        group_sync(grp);
-        if (gl < p.rp && gl < n_rows) {
-          float mm = -INFINITY, ll = 0.f;
-          for (int k = 0; k < p.rep; ++k) {
-            const float mk = row_g[2 * (k * p.rp + gl)], lk = row_g[2 * (k * p.rp + gl) + 1];
-            const float M = fmaxf(mm, mk);
-            ll = (ll == 0.f ? 0.f : ll * ex2(mm - M)) + (lk == 0.f ? 0.f : lk * ex2(mk - M));
-            mm = M;
-          }
-          reinterpret_cast<float2*>(p.part_ml)[((size_t)(cta + c.b * H + c.g) * p.rows + row0 + gl) * p.slots + mine] = make_float2(mm, ll);
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(my_empty + 8 * b_off);
+      if (PASS == 2) {
+        if (V > 1) {  // a token's partial weights meet; the next turn's barrier lies between these reads and the slots' reuse
+          float* part = reinterpret_cast<float*>(pos_s) + ((turn & 1) * kObGroups + grp - v) * kObTile + gl;
+          if (v > 0) part[v * kObTile] = w;
+          if (V == 2) pair_sync(grp >> 1);
+          else groups_sync();
+          if (v == 0)
+            for (int k = 1; k < V; ++k) w += part[k * kObTile];
         }
+        if (dst && v == 0) *dst = w_old + w;
       }
-      if (i + 1 < n_x) advance(c, x_first + DIR * (i + 1));
     }
+    if (PASS == 1 && c.b >= 0) end_segment();
   }
   tc_fence_before();
   __syncthreads();
@@ -621,6 +675,8 @@ mc_status launch_layer_observe(const mc_config* cfg, const mc_batch* bt, const G
   op.rows = n_obs * op.nq;
   op.nt = op.rows > kObTile ? 2 : 1;
   op.slots = kObGroups / op.nt;
+  op.v1 = kObHalves * op.nt;
+  op.v2 = op.rows <= kObUnit ? 1 : (op.rows <= 2 * kObUnit ? 2 : 4);
   op.rp = op.rows > 64 ? 128 : (op.rows > 32 ? 64 : 32);
   op.rep = kObTile / op.rp;
   op.jt = std::min(n_obs, kObTile / op.nq);
@@ -630,11 +686,23 @@ mc_status launch_layer_observe(const mc_config* cfg, const mc_batch* bt, const G
   op.add = (flags & MC_LAYER_ACCUMULATE) || hidden_tiles;
   const long long max_tiles = (long long)bt->batch * cfg->n_kv_heads * ((bt->max_seq_len + kObTile - 1) / kObTile);
   op.n_ctas = (int)std::max<long long>(1, std::min<long long>(std::min(n_sm, kObMaxCtas), max_tiles));
+  if (opts->softcap > 0.f) {
+    const double inv = (double)opts->sm_scale / opts->softcap, top = (double)opts->softcap * kLog2e;
+    double scale = inv * top;  // of coefficient j: inv^(2 j + 1) * cap * log2(e)
+    for (int j = 0; j < 7; ++j, scale *= inv * inv) {
+      if (j < 5) op.tiny[j] = (float)(kTanhTiny[j] * scale);
+      op.small[j] = (float)(kTanhSmall[j] * scale);
+    }
+    // (a polynomial whose coefficients leave binary32's normal range is not used)
+    const auto fits = [](float c) { return fabsf(c) > 1e-37f && fabsf(c) < 1e30f; };
+    op.tiny_max = fits(op.tiny[0]) && fits(op.tiny[4]) ? (float)(0.5 / fabs(inv)) : -1.f;
+    op.small_max = fits(op.small[0]) && fits(op.small[6]) ? (float)(1.0 / fabs(inv)) : -1.f;
+  }
   CUtensorMap map_k, map_q;
   const uint64_t rows = (uint64_t)bt->n_pages * cfg->n_kv_heads * cfg->page_size;
   if (mc_status st = make_map(&map_k, cfg->dtype, layer->k_pool, rows, kHeadDim, cfg->page_size)) return st;
   if (mc_status st = make_map3(&map_q, cfg->dtype, q, (uint64_t)bt->batch * n_obs, cfg->n_q_heads, kHeadDim, op.jt, op.nq)) return st;
-  const size_t smem = 1024 + kObSmem + (2 * kObMaxStages + 4 + 2 * kObGroups) * 8 + 16 + kObGroups * kObTile * (2 * 8 + 4) + (size_t)(bt->batch + 1) * 4;
+  const size_t smem = 1024 + kObSmem + (2 * kObMaxStages + 4 + 2 * kObBufs) * 8 + 16 + kObGroups * kObTile * (2 * 8 + 8) + (size_t)(bt->batch + 1) * 4;
   using Kernel = void (*)(const ObserveParams, const CUtensorMap, const CUtensorMap);
   static const Kernel kernels[2][2][2] = {
       {{layer_observe_kernel<MC_F16, 1, false>, layer_observe_kernel<MC_F16, 1, true>},

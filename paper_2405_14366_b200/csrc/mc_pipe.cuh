@@ -47,4 +47,16 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
   return false;
 }
 
+// The same in few instructions, for kernels whose waiting warps share the schedulers with working ones: a try already
+// suspends the warp for a while (an explicit time hint made it poll three times as often).
+__device__ __forceinline__ bool mbar_wait_lean(uint32_t bar, uint32_t parity, volatile int* s_abort, int32_t* status) {
+  for (uint32_t it = 0; it < kWaitLimit; ++it) {
+    if (mbar_try_wait(bar, parity)) return true;
+    if ((it & 255) == 255 && *s_abort) return false;
+  }
+  *s_abort = 1;
+  atomicOr(status, MC_FLAG_WAIT_TIMEOUT);
+  return false;
+}
+
 }  // namespace mc
