@@ -4,11 +4,13 @@
 // row that stays behind them moves into the k-th slot that fell free before them.  So one decode step that evicts one
 // token moves one row, and nothing is read that is also written: sources lie at or behind `budget`, targets before it.
 //
-// A cluster of CTAs per segment: every CTA keeps the ordered 32-bit keys of its share of the tokens in shared memory,
-// the budget-th largest key is found digit by digit (11 + 11 + 10 bits: a histogram per CTA, summed over the
-// cluster through distributed shared memory), then holes and movers are listed in index order (a warp per run of
-// tokens, counts scanned over the cluster) and the cluster's warps copy the rows.  Bytes: 8 per token for the
-// keys, 2 x 512 per moved row; short caches are bound by the chain of barriers (about a microsecond per digit).
+// A cluster of CTAs per segment (one CTA where the segments alone fill the GPU): every CTA keeps the ordered 32-bit keys
+// of its share of the tokens in shared memory, the budget-th largest key is found digit by digit (11 + 11 + 10 bits:
+// a histogram per CTA, its non-empty bins added to every CTA's total through distributed shared memory), then holes and
+// movers are listed in index order (a warp per run of tokens, counts scanned over the cluster) and the cluster's warps
+// copy the rows.  The steady state of a bounded cache, one token too many, needs no digits: the smallest key goes.
+// Bytes: 8 per token for the keys, 2 x 512 per moved row; short caches are bound by the chain of dependent loads and
+// barriers.
 #include <cooperative_groups.h>
 
 #include <algorithm>
@@ -48,33 +50,42 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
   return (u & 0x80000000u) ? ~u : u | 0x80000000u;
 }
 
-// Exclusive sum over the block of one int per warp (lane 0's), for every warp, and the total.
-__device__ __forceinline__ int warp_prefix(int v, int* s, int warp, int lane, int& total) {
+// Exclusive sums over the block of two ints per warp, and the totals.
+struct Two {
+  int a, b;
+};
+__device__ __forceinline__ Two warp_prefix(Two v, Two* s, int warp, int lane, Two& total) {
   __syncthreads();
   if (lane == 0) s[warp] = v;
   __syncthreads();
-  int before = 0, all = 0;
+  Two before = {0, 0}, all = {0, 0};
 #pragma unroll
   for (int k = 0; k < kEvWarps; ++k) {
-    const int x = s[k];
-    if (k < warp) before += x;
-    all += x;
+    const Two x = s[k];
+    if (k < warp) {
+      before.a += x.a;
+      before.b += x.b;
+    }
+    all.a += x.a;
+    all.b += x.b;
   }
   total = all;
   return before;
 }
 
-__global__ void __launch_bounds__(kEvThreads) layer_evict_kernel(const __grid_constant__ EvictParams p) {
+__global__ void __launch_bounds__(kEvThreads, 2) layer_evict_kernel(const __grid_constant__ EvictParams p) {
   // (no early start of the kernel behind: it may take new_lens for its lengths, which are read before the wait)
   cg::cluster_group cl = cg::this_cluster();
   const int C = (int)cl.num_blocks(), rank = (int)cl.block_rank();
-  extern __shared__ uint32_t smem_u[];
-  uint32_t* hist = smem_u;                            // [3][kEvBins]
-  uint32_t* keys = hist + 3 * kEvBins;                // [smem_keys]
-  uint32_t* mask = keys + p.smem_keys;                // [(smem_keys + 31) / 32 + 1]: who stays, a bit per token
-  __shared__ int warp_s[kEvWarps];
-  __shared__ int pub[4];                              // read by the cluster: ties, holes, movers of this CTA
-  __shared__ int found[2];                            // digit, how many keys lie above it
+  extern __shared__ __align__(16) uint32_t smem_u[];
+  uint32_t* total = smem_u;                           // [3][kEvBins]: the cluster's histograms
+  uint32_t* local = total + 3 * kEvBins;              // [kEvBins]: this CTA's, digit by digit (clusters only)
+  uint32_t* keys = local + kEvBins;                   // [smem_keys]
+  uint32_t* mask = keys + p.smem_keys;                // [smem_keys / 32 + 1]: who stays, a bit per token
+  __shared__ Two warp_s[kEvWarps];
+  __shared__ uint64_t best_s[kEvWarps];
+  __shared__ Two pub[kEvMaxCluster], pub_tie[kEvMaxCluster];  // written by the cluster: (holes, movers) and ties of every CTA
+  __shared__ int found[4];                            // digit, keys above it, keys equal (cluster), keys equal (this CTA)
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int H = p.g.n_kv_heads, ps = p.g.page_size, shift = p.g.page_shift;
   const int seg = blockIdx.x / C, b = seg / H, head = seg - b * H;
@@ -92,68 +103,124 @@ __global__ void __launch_bounds__(kEvThreads) layer_evict_kernel(const __grid_co
   const int i0 = min(n, rank * per), cnt = min(n, i0 + per) - i0;  // this CTA's tokens
   const int32_t* table = p.g.block_table + (size_t)b * p.g.max_pages_per_seq;
   const bool held = per <= p.smem_keys;
+  const int shrink = n - p.budget;
 
-  auto slot_of = [&](int t) -> long long {  // slot of the [page][head][row] pools; -1: not a page
+  auto slot_of = [&](int t) -> int {  // slot of the [page][head][row] pools; -1: not a page
     const int page = table[t >> shift];
     if (!page_ok(p.g, page)) return -1;
-    return ((long long)page * H + head) * ps + (t & (ps - 1));
+    return (page * H + head) * ps + (t & (ps - 1));
   };
-  auto load_key = [&](int i) -> uint32_t {
-    const long long at = slot_of(i0 + i);
-    if (at < 0) {
-      atomicOr(p.status, MC_FLAG_BAD_METADATA);
-      return 0u;
-    }
-    const int pos = p.positions[at];
-    const float w = p.weights[at];
+  auto key_of = [&](int at, int pos, float w) -> uint32_t {
+    if (at < 0) return 0u;
     return (pos < p.n_sink || pos > recent) ? 0xffffffffu : weight_key(w);
   };
+  auto load_key = [&](int i) -> uint32_t {
+    const int at = slot_of(i0 + i);
+    return at < 0 ? 0u : key_of(at, p.positions[at], p.weights[at]);
+  };
   auto key_at = [&](int i) -> uint32_t { return held ? keys[i] : load_key(i); };
+  // visits every key of the CTA's share once, four loads in flight
+  auto for_keys = [&](auto&& visit) {
+    int bad = 0;
+    for (int i = tid; i < cnt; i += 4 * kEvThreads) {
+      int at[4], pos[4];
+      float w[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) at[k] = i + k * kEvThreads < cnt ? slot_of(i0 + i + k * kEvThreads) : -2;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        pos[k] = at[k] >= 0 ? p.positions[at[k]] : 0;
+        w[k] = at[k] >= 0 ? p.weights[at[k]] : 0.f;
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        bad |= at[k] == -1 ? 1 : 0;
+        if (at[k] > -2) visit(i + k * kEvThreads, key_of(at[k], pos[k], w[k]));
+      }
+    }
+    if (bad) atomicOr(p.status, MC_FLAG_BAD_METADATA);
+  };
+  auto copy_row = [&](int from, int to) {  // by a warp: lanes 0..15 K, 16..31 V
+    char* pool = lane < 16 ? p.k_pool : p.v_pool;
+    const uint4 v = ld_stream16(pool + (size_t)from * kRowBytes + (lane & 15) * 16);
+    st_stream16(pool + (size_t)to * kRowBytes + (lane & 15) * 16, v);
+  };
 
-  for (int i = tid; i < 3 * kEvBins; i += kEvThreads) hist[i] = 0;
-  __syncthreads();
+  if (shrink == 1 && C == 1) {
+    // ---- one token too many: the smallest key, the last index among equals, goes; the last token takes its slot
+    uint64_t best = ~0ull;  // (key, n - index): ties go to the lower index, so the higher one is evicted
+    for_keys([&](int i, uint32_t k) { best = min(best, ((uint64_t)k << 32) | (uint32_t)(n - 1 - i)); });
+#pragma unroll
+    for (int o = 16; o; o >>= 1) best = min(best, __shfl_xor_sync(0xffffffffu, best, o));
+    if (lane == 0) best_s[warp] = best;
+    __syncthreads();
+    if (warp != 0) return;
+    best = best_s[lane & (kEvWarps - 1)];
+#pragma unroll
+    for (int o = 16; o; o >>= 1) best = min(best, __shfl_xor_sync(0xffffffffu, best, o));
+    const int gone = n - 1 - (int)(uint32_t)best;
+    if (gone == p.budget) return;  // the last token itself
+    const int from = slot_of(p.budget), to = slot_of(gone);
+    if (from < 0 || to < 0) return;
+    copy_row(from, to);
+    if (lane == 0) {
+      p.weights[to] = p.weights[from];
+      p.positions[to] = p.positions[from];
+    }
+    return;
+  }
+
+  for (int i = tid; i < kEvBins; i += kEvThreads) reinterpret_cast<uint4*>(total)[i] = make_uint4(0u, 0u, 0u, 0u);  // 3 totals, local
+  if (C > 1) cl.sync();  // nobody adds to a total before it is cleared
+  else __syncthreads();
   // ---- the budget-th largest key ------------------------------------------------------------------
   uint32_t prefix = 0;       // digits found so far
   int want = p.budget;       // rank of the key among those that share the prefix
 #pragma unroll
   for (int d = 0; d < 3; ++d) {
     const int sh = d == 0 ? 21 : (d == 1 ? 10 : 0), bits = d == 2 ? 10 : 11;
-    uint32_t* h = hist + d * kEvBins;
-    for (int i = tid; i < cnt; i += kEvThreads) {
-      uint32_t k;
-      if (d == 0 || !held) {
-        k = load_key(i);
-        if (d == 0 && held) keys[i] = k;
-      } else {
-        k = keys[i];
-      }
-      if (d == 0 || (k >> (sh + bits)) == prefix) atomicAdd(&h[(k >> sh) & ((1u << bits) - 1)], 1u);
-    }
-    cl.sync();
-    // every CTA sums the cluster's histograms for itself: a thread takes four digits, the largest first
-    int c4[4], sum = 0;
+    uint32_t* tot = total + d * kEvBins;
+    uint32_t* h = C > 1 ? local : tot;
+    auto count = [&](int i, uint32_t k) {
+      if (d == 0 && held) keys[i] = k;
+      if (d == 0 || (k >> ((sh + bits) & 31)) == prefix) atomicAdd(&h[(k >> sh) & ((1u << bits) - 1)], 1u);
+    };
+    if (d == 0 || !held) for_keys(count);
+    else
+      for (int i = tid; i < cnt; i += kEvThreads) count(i, keys[i]);
+    __syncthreads();
+    // a thread takes four digits, the largest first
+    const int quad = kEvThreads - 1 - tid;
+    uint4 mine = reinterpret_cast<const uint4*>(h)[quad];
+    if (C > 1) {
+      reinterpret_cast<uint4*>(h)[quad] = make_uint4(0u, 0u, 0u, 0u);
+      const uint32_t v[4] = {mine.x, mine.y, mine.z, mine.w};
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const int bin = kEvBins - 1 - (4 * tid + k);
-      int v = 0;
-      for (int r = 0; r < C; ++r) v += (int)cl.map_shared_rank(h, r)[bin];
-      c4[k] = v;
-      sum += v;
+      for (int k = 0; k < 4; ++k)
+        if (v[k])
+          for (int r = 0; r < C; ++r) atomicAdd(cl.map_shared_rank(tot, r) + 4 * quad + k, v[k]);
+      cl.sync();
     }
+    const uint4 all = C > 1 ? reinterpret_cast<const uint4*>(tot)[quad] : mine;
+    const int c4[4] = {(int)all.w, (int)all.z, (int)all.y, (int)all.x};
+    const int m4[4] = {(int)mine.w, (int)mine.z, (int)mine.y, (int)mine.x};
+    const int sum = c4[0] + c4[1] + c4[2] + c4[3];
     int incl = sum;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const int v = __shfl_up_sync(0xffffffffu, incl, o);
       if (lane >= o) incl += v;
     }
-    int total;
-    const int before = warp_prefix(__shfl_sync(0xffffffffu, incl, 31), warp_s, warp, lane, total);
-    int above = before + incl - sum;
+    Two all_sum;
+    const Two before = warp_prefix({__shfl_sync(0xffffffffu, incl, 31), 0}, warp_s, warp, lane, all_sum);
+    int above = before.a + incl - sum;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       if (above < want && want <= above + c4[k]) {
-        found[0] = kEvBins - 1 - (4 * tid + k);
+        found[0] = 4 * quad + 3 - k;
         found[1] = above;
+        found[2] = c4[k];
+        found[3] = m4[k];
       }
       above += c4[k];
     }
@@ -165,16 +232,21 @@ __global__ void __launch_bounds__(kEvThreads) layer_evict_kernel(const __grid_co
   const uint32_t thr = prefix;
   const int words = (cnt + 31) / 32, wper = (words + kEvWarps - 1) / kEvWarps;
   const int w0 = min(words, warp * wper), w1 = min(words, w0 + wper);
-  int ties = 0;
-  for (int w = w0; w < w1; ++w) {
-    const int i = 32 * w + lane;
-    ties += __popc(__ballot_sync(0xffffffffu, i < cnt && key_at(i) == thr));
+  int tie = -0x40000000;  // ties before this warp's run; (all of them stay: no need to count)
+  if (want < found[2]) {
+    int ties = 0;
+    for (int w = w0; w < w1; ++w) {
+      const int i = 32 * w + lane;
+      ties += __popc(__ballot_sync(0xffffffffu, i < cnt && key_at(i) == thr));
+    }
+    Two sum;
+    tie = warp_prefix({ties, 0}, warp_s, warp, lane, sum).a;
+    if (C > 1) {
+      if (tid < C) cl.map_shared_rank(pub_tie, tid)[rank].a = sum.a;
+      cl.sync();
+      for (int r = 0; r < rank; ++r) tie += pub_tie[r].a;
+    }
   }
-  int total_ties;
-  int tie = warp_prefix(ties, warp_s, warp, lane, total_ties);
-  if (tid == 0) pub[0] = total_ties;
-  cl.sync();
-  for (int r = 0; r < rank; ++r) tie += *cl.map_shared_rank(&pub[0], r);
   // ---- who stays; holes before the budget, movers behind it ------------------------------------------
   auto stay_word = [&](int w, int& t) -> uint32_t {
     const int i = 32 * w + lane;
@@ -184,7 +256,8 @@ __global__ void __launch_bounds__(kEvThreads) layer_evict_kernel(const __grid_co
     t += __popc(eq);
     return __ballot_sync(0xffffffffu, stay);
   };
-  int holes = 0, movers = 0, tie_w = tie;
+  Two mine = {0, 0};  // holes, movers
+  int tie_w = tie;
   for (int w = w0; w < w1; ++w) {
     const uint32_t s = stay_word(w, tie_w);
     if (held && lane == 0) mask[w] = s;
@@ -192,26 +265,24 @@ __global__ void __launch_bounds__(kEvThreads) layer_evict_kernel(const __grid_co
     const uint32_t low = rel >= 32 ? 0xffffffffu : (rel <= 0 ? 0u : (1u << rel) - 1u);
     const int valid = cnt - 32 * w;
     const uint32_t here = valid >= 32 ? 0xffffffffu : (1u << valid) - 1u;
-    holes += __popc(~s & low & here);
-    movers += __popc(s & ~low);
+    mine.a += __popc(~s & low & here);
+    mine.b += __popc(s & ~low);
   }
-  int total_h, total_m;
-  int at_h = warp_prefix(holes, warp_s, warp, lane, total_h);
-  int at_m = warp_prefix(movers, warp_s, warp, lane, total_m);
-  if (tid == 0) {
-    pub[1] = total_h;
-    pub[2] = total_m;
-  }
-  cl.sync();
-  int n_moves = 0;
-  for (int r = 0; r < C; ++r) {
-    const int* q = cl.map_shared_rank(&pub[0], r);
-    const int m = q[2];
-    if (r < rank) {
-      at_h += q[1];
-      at_m += m;
+  Two sum;
+  Two at = warp_prefix(mine, warp_s, warp, lane, sum);
+  int n_moves = sum.b;
+  if (C > 1) {
+    if (tid < C) cl.map_shared_rank(pub, tid)[rank] = sum;
+    cl.sync();
+    n_moves = 0;
+    for (int r = 0; r < C; ++r) {
+      const Two q = pub[r];
+      if (r < rank) {
+        at.a += q.a;
+        at.b += q.b;
+      }
+      n_moves += q.b;
     }
-    n_moves += m;
   }
   int32_t* hole_l = p.lists + (size_t)seg * 2 * p.list_stride;
   int32_t* move_l = hole_l + p.list_stride;
@@ -221,19 +292,21 @@ __global__ void __launch_bounds__(kEvThreads) layer_evict_kernel(const __grid_co
     const bool stay = (s >> lane) & 1u;
     const bool hole = i < cnt && t < p.budget && !stay, mover = stay && t >= p.budget;
     const uint32_t hb = __ballot_sync(0xffffffffu, hole), mb = __ballot_sync(0xffffffffu, mover), lt = (1u << lane) - 1u;
-    if (hole) hole_l[at_h + __popc(hb & lt)] = t;
-    if (mover) move_l[at_m + __popc(mb & lt)] = t;
-    at_h += __popc(hb);
-    at_m += __popc(mb);
+    if (hole) hole_l[at.a + __popc(hb & lt)] = t;
+    if (mover) move_l[at.b + __popc(mb & lt)] = t;
+    at.a += __popc(hb);
+    at.b += __popc(mb);
   }
-  cl.sync();  // the lists are complete (and nobody reads another CTA's shared memory from here on)
-  // ---- the rows: a lane works a move's slots out, then the warp copies it (lanes 0..15 K, 16..31 V) -------
+  if (C > 1) cl.sync();  // the lists are complete (and nobody touches another CTA's shared memory from here on)
+  else __syncthreads();
+  // ---- the rows: a lane works a move's slots out, then the warp copies it ------------------------------
   const int n_warps = C * kEvWarps, gw = rank * kEvWarps + warp;
   const int share = min(32, max(1, (n_moves + n_warps - 1) / n_warps));
   char* pool = lane < 16 ? p.k_pool : p.v_pool;
+  constexpr int kDeep = 8;  // rows in flight per warp
   for (int m0 = gw * share; m0 < n_moves; m0 += n_warps * share) {
     const int m = m0 + lane;
-    long long src = -1, dst = -1;
+    int src = -1, dst = -1;
     if (lane < share && m < n_moves) {
       src = slot_of(__ldcg(move_l + m));
       dst = slot_of(__ldcg(hole_l + m));
@@ -243,19 +316,19 @@ __global__ void __launch_bounds__(kEvThreads) layer_evict_kernel(const __grid_co
       }
     }
     const int live = min(share, n_moves - m0);
-    for (int k0 = 0; k0 < live; k0 += 4) {  // four rows in flight
-      uint4 v[4];
-      long long to[4];
+    for (int k0 = 0; k0 < live; k0 += kDeep) {
+      uint4 v[kDeep];
+      int to[kDeep];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const long long from = __shfl_sync(0xffffffffu, src, (k0 + k) & 31);
+      for (int k = 0; k < kDeep; ++k) {
+        const int from = __shfl_sync(0xffffffffu, src, (k0 + k) & 31);
         to[k] = __shfl_sync(0xffffffffu, dst, (k0 + k) & 31);
         if (k0 + k >= live || from < 0) to[k] = -1;
-        if (to[k] >= 0) v[k] = ld_stream16(pool + from * kRowBytes + (lane & 15) * 16);
+        if (to[k] >= 0) v[k] = ld_stream16(pool + (size_t)from * kRowBytes + (lane & 15) * 16);
       }
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
-        if (to[k] >= 0) st_stream16(pool + to[k] * kRowBytes + (lane & 15) * 16, v[k]);
+      for (int k = 0; k < kDeep; ++k)
+        if (to[k] >= 0) st_stream16(pool + (size_t)to[k] * kRowBytes + (lane & 15) * 16, v[k]);
     }
   }
 }
@@ -283,11 +356,17 @@ mc_status launch_layer_evict(const mc_config* cfg, const mc_batch* bt, const Geo
   ep.budget = opts->budget;
   ep.n_sink = opts->n_sink;
   ep.n_recent = opts->n_recent;
-  int cluster = 1;  // about 2048 tokens per CTA
-  while (cluster < kEvMaxCluster && bt->max_seq_len > 2048 * cluster) cluster *= 2;
+  int n_sm = 0;
+  if (mc_status st = sm_count(&n_sm)) return st;
+  // CTAs per segment: as many as the GPU takes at once (two per SM), if a CTA still has 1024 tokens.  (More of them run
+  // in two waves: 256 segments of 4096 tokens took 90 us with two CTAs each, 4MB_US with one.)
+  int cluster = 1;
+  while (cluster < kEvMaxCluster && (long long)bt->batch * cfg->n_kv_heads * cluster * 2 <= 2 * n_sm &&
+         bt->max_seq_len > 1024 * cluster)
+    cluster *= 2;
   const int per = (bt->max_seq_len + cluster - 1) / cluster;
   ep.smem_keys = std::min((per + 31) / 32 * 32, kEvSmemKeys);
-  const size_t smem = (size_t)(3 * kEvBins + ep.smem_keys + ep.smem_keys / 32 + 1) * 4;
+  const size_t smem = (size_t)(4 * kEvBins + ep.smem_keys + ep.smem_keys / 32 + 1) * 4;
   MC_CUDA_CHECK(cudaFuncSetAttribute(layer_evict_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
   cudaLaunchConfig_t cfgl = {};
   cfgl.gridDim = dim3((unsigned)(bt->batch * cfg->n_kv_heads * cluster));
