@@ -7,6 +7,7 @@ from __future__ import annotations
 
 import ctypes as C
 import dataclasses
+import operator
 import os
 from typing import Optional
 
@@ -299,6 +300,26 @@ def _typed(name: str, t: Optional[torch.Tensor], dtype) -> Optional[int]:
     return _ptr(t)
 
 
+def _checked(owner, tensors, sizes) -> bool:
+    """Whether `owner`'s tensors have to be checked (again): not if they are the same objects as at its last call."""
+    last = getattr(owner, "_seen", None)
+    return last is None or last[1] != sizes or not all(map(operator.is_, last[0], tensors))
+
+
+_CFG = {}
+
+
+def _cfg_c(cfg: "McConfig") -> _Config:
+    """cfg.c(), remembered by the fields' values: the mc_layer_* calls are made once per layer and decode step."""
+    key = tuple(cfg.__dict__.values())
+    c = _CFG.get(key)
+    if c is None:
+        if len(_CFG) > 256:
+            _CFG.clear()
+        c = _CFG[key] = cfg.c()
+    return c
+
+
 @dataclasses.dataclass
 class LayerCache:
     """One uncompressed layer's paged cache (caller-owned tensors, see mc_layer_cache): k_pool / v_pool
@@ -316,13 +337,16 @@ class LayerCache:
             self.status = torch.zeros(MC_STATUS_WORDS, dtype=torch.int32, device=self.k_pool.device)
 
     def c(self, n_pages: int) -> _LayerCache:
-        dt, rows = self.cfg.torch_dtype, n_pages * self.cfg.n_kv_heads * self.cfg.page_size
-        for t, n in ((self.k_pool, 128 * rows), (self.v_pool, 128 * rows), (self.positions, rows), (self.weights, rows),
-                     (self.status, MC_STATUS_WORDS)):
-            assert t is None or t.numel() >= n, "a pool holds fewer than n_pages pages"
-        return _LayerCache(_typed("k_pool", self.k_pool, dt), _typed("v_pool", self.v_pool, dt),
-                           _typed("positions", self.positions, torch.int32), _typed("weights", self.weights, torch.float32),
-                           _typed("status", self.status, torch.int32))
+        k, v, pos, w, st = seen = (self.k_pool, self.v_pool, self.positions, self.weights, self.status)
+        if _checked(self, seen, n_pages):
+            dt, rows = self.cfg.torch_dtype, n_pages * self.cfg.n_kv_heads * self.cfg.page_size
+            for name, t, want, n in (("k_pool", k, dt, 128 * rows), ("v_pool", v, dt, 128 * rows), ("positions", pos, torch.int32, rows),
+                                     ("weights", w, torch.float32, rows), ("status", st, torch.int32, MC_STATUS_WORDS)):
+                _typed(name, t, want)
+                assert t is None or t.numel() >= n, f"{name} holds fewer than n_pages pages"
+            self._seen = (seen, n_pages)
+        return _LayerCache(k.data_ptr(), v.data_ptr(), None if pos is None else pos.data_ptr(), None if w is None else w.data_ptr(),
+                           st.data_ptr())
 
 
 @dataclasses.dataclass
@@ -338,11 +362,16 @@ class ScoreOpts:
     q_pos: Optional[torch.Tensor] = None
 
     def c(self, cfg: McConfig, batch: int) -> _ScoreOpts:
-        for t, n in ((self.alibi_slopes, cfg.n_q_heads), (self.doc_start, batch), (self.prefix_len, batch), (self.q_pos, batch)):
-            assert t is None or t.numel() >= n, "a score option holds too few entries"
-        return _ScoreOpts(_typed("alibi_slopes", self.alibi_slopes, torch.float32), _typed("doc_start", self.doc_start, torch.int32),
-                          _typed("prefix_len", self.prefix_len, torch.int32), _typed("q_pos", self.q_pos, torch.int32),
-                          float(self.sm_scale), float(self.softcap), int(self.window), 0)
+        a, d, p, q = seen = (self.alibi_slopes, self.doc_start, self.prefix_len, self.q_pos)
+        sizes = (cfg.n_q_heads, batch)
+        if _checked(self, seen, sizes):
+            for name, t, want, n in (("alibi_slopes", a, torch.float32, cfg.n_q_heads), ("doc_start", d, torch.int32, batch),
+                                     ("prefix_len", p, torch.int32, batch), ("q_pos", q, torch.int32, batch)):
+                _typed(name, t, want)
+                assert t is None or t.numel() >= n, f"{name} holds too few entries"
+            self._seen = (seen, sizes)
+        return _ScoreOpts(None if a is None else a.data_ptr(), None if d is None else d.data_ptr(), None if p is None else p.data_ptr(),
+                          None if q is None else q.data_ptr(), self.sm_scale, self.softcap, self.window, 0)
 
 
 @dataclasses.dataclass
@@ -637,22 +666,26 @@ class MiniCacheLib:
                       workspace: torch.Tensor, stream=None):
         """q, out [batch][n_q_heads][128], k_new / v_new [batch][n_kv_heads][128] or None; flags: MC_LAYER_APPEND |
         MC_LAYER_ACCUMULATE; lse [batch][n_q_heads] float32 or None."""
-        c, b = cfg.c(), batch.c()
-        n, dt = b.batch, cfg.torch_dtype
-        for t, heads in ((q, cfg.n_q_heads), (out, cfg.n_q_heads), (k_new, cfg.n_kv_heads), (v_new, cfg.n_kv_heads)):
-            assert t is None or t.numel() == n * heads * 128, "rows of 128 channels per sequence and head are wanted"
-        assert lse is None or lse.numel() == n * cfg.n_q_heads
+        c, b = _cfg_c(cfg), batch.c()
+        n, dt = b.batch, q.dtype
+        rows_q, rows_kv = n * cfg.n_q_heads * 128, n * cfg.n_kv_heads * 128
+        assert dt is cfg.torch_dtype, "q: the storage type is wanted"
+        for t, rows in ((q, rows_q), (out, rows_q), (k_new, rows_kv), (v_new, rows_kv)):
+            assert t is None or (t.dtype is dt and t.numel() == rows and t.is_contiguous()), \
+                "contiguous rows of 128 channels per sequence and head are wanted"
+        assert lse is None or (lse.dtype is torch.float32 and lse.numel() == n * cfg.n_q_heads and lse.is_contiguous()), "lse: float32 [batch][n_q_heads]"
         l, o = layer.c(b.n_pages), opts.c(cfg, n)
-        self._check(self._lib.mc_layer_attn(C.byref(c), C.byref(b), C.byref(l), C.byref(o), _typed("q", q, dt),
-                                            _typed("k_new", k_new, dt), _typed("v_new", v_new, dt), int(flags),
-                                            _typed("out", out, dt), _typed("lse", lse, torch.float32), _ptr(workspace),
-                                            workspace.numel() * workspace.element_size(), _stream(stream)))
+        code = self._lib.mc_layer_attn(c, b, l, o, q.data_ptr(), None if k_new is None else k_new.data_ptr(),
+                                       None if v_new is None else v_new.data_ptr(), flags, out.data_ptr(),
+                                       None if lse is None else lse.data_ptr(), workspace.data_ptr(), workspace.nbytes, _stream(stream))
+        if code:
+            self._check(code)
 
     def mc_layer_observe(self, cfg: McConfig, batch: Batch, layer: LayerCache, opts: ScoreOpts, q, flags: int, workspace: torch.Tensor,
                          stream=None):
         """q [batch][n_obs][n_q_heads][128]: the last n_obs queries of every sequence; flags: 0 (weights are written) or
         MC_LAYER_ACCUMULATE (added to)."""
-        c, b = cfg.c(), batch.c()
+        c, b = _cfg_c(cfg), batch.c()
         assert q.dim() == 4 and tuple(q.shape) == (b.batch, q.shape[1], cfg.n_q_heads, 128), "q: [batch][n_obs][n_q_heads][128]"
         l, o = layer.c(b.n_pages), opts.c(cfg, b.batch)
         self._check(self._lib.mc_layer_observe(C.byref(c), C.byref(b), C.byref(l), C.byref(o), _typed("q", q, cfg.torch_dtype),
@@ -662,7 +695,7 @@ class MiniCacheLib:
     def mc_layer_evict(self, cfg: McConfig, batch: Batch, layer: LayerCache, opts: EvictOpts, new_lens: torch.Tensor,
                        workspace: torch.Tensor, stream=None):
         """new_lens int32 [batch] receives min(seq_lens, budget); it must not share memory with batch.seq_lens."""
-        c, b = cfg.c(), batch.c()
+        c, b = _cfg_c(cfg), batch.c()
         assert new_lens.numel() == b.batch
         l, o = layer.c(b.n_pages), opts.c(b.batch)
         self._check(self._lib.mc_layer_evict(C.byref(c), C.byref(b), C.byref(l), C.byref(o), _typed("new_lens", new_lens, torch.int32),

@@ -211,8 +211,11 @@ layer_attn_split_kernel(const __grid_constant__ LayerAttnParams p, const __grid_
     const Seq q = seq_of(p, s.b);
     const int k = s.x - pre_s[s.b];
     s.t0 = (k < q.ua ? k : q.ub0 + k - q.ua) * kLaUnit + (warp + 4 * (rem & 1)) * kLaSlice;
-    if (s.t0 < q.n_tot) s.flags |= kSlTokens;
-    if (s.t0 < q.n) s.flags |= kSlLoad;
+    // (without a positions pool a slice that holds no visible token, nor the row to append, is left out)
+    const bool wanted = p.positions != nullptr || s.t0 < q.a || (s.t0 + kLaSlice > q.lo && s.t0 < q.hi) ||
+                        ((p.flags & MC_LAYER_APPEND) && q.n >= s.t0 && q.n < s.t0 + kLaSlice);
+    if (wanted && s.t0 < q.n_tot) s.flags |= kSlTokens;
+    if (wanted && s.t0 < q.n) s.flags |= kSlLoad;
     if (!(rem & 1) && (s.x == x_begin || k == 0)) s.flags |= kSlFirst;
     if ((rem & 1) && (s.x + 1 == x_end || k + 1 == q.u)) s.flags |= kSlLast;
     if ((s.flags & kSlLoad) || ((s.flags & kSlTokens) && (p.flags & MC_LAYER_APPEND))) {
@@ -595,7 +598,47 @@ __global__ void __launch_bounds__(kLcThreads) layer_attn_combine_kernel(const __
     const int j = (int)blockIdx.x - combine_x, head = j / per_head, k0 = (j % per_head) * kLcUnits;
     if (k0 >= u) return;
     const Seq sq = seq_of(p, b);
+    const int k1 = min(k0 + kLcUnits, u);
+    // A thread owns four tokens.  Where their weights live follows from the caller's tables (before the wait); scores,
+    // old weights and the partial sums are then requested together.
+    constexpr int kOwn = kLcUnits * kLaUnit / kLcThreads;
+    int at[kOwn], from[kOwn];
+    bool fresh[kOwn];
+#pragma unroll
+    for (int j = 0; j < kOwn; ++j) {
+      const int i = tid + j * kLcThreads, k = k0 + i / kLaUnit, in = i % kLaUnit;
+      const int t = (k < sq.ua ? k : sq.ub0 + k - sq.ua) * kLaUnit + in, slot = t >> p.g.page_shift;
+      fresh[j] = t == sq.n;  // the appended row: its weight begins here
+      at[j] = -1;
+      from[j] = -1;
+      if (k >= k1 || t >= sq.n_tot || slot >= p.g.max_pages_per_seq || (fresh[j] && !(p.flags & MC_LAYER_APPEND))) continue;
+      const bool seen = p.positions != nullptr || t < sq.a || (t >= sq.lo && t < sq.hi);
+      if (!seen && !fresh[j]) continue;  // (no score was written)
+      const int page = p.g.block_table[(size_t)b * p.g.max_pages_per_seq + slot];
+      if (!page_ok(p.g, page)) continue;  // (flagged by the split kernel)
+      at[j] = (page * p.g.n_kv_heads + head) * p.g.page_size + (t & (p.g.page_size - 1));
+      if (seen) from[j] = ((x0 + k) * p.g.n_kv_heads + head) * kLaUnit + in;
+    }
     grid_dep_wait();
+    float s[kOwn][kLaRows], w[kOwn];
+#pragma unroll
+    for (int j = 0; j < kOwn; ++j) {
+      w[j] = at[j] >= 0 && !fresh[j] ? p.weights[at[j]] : 0.f;
+      const float* src = p.scores + (size_t)max(from[j], 0) * p.nq;
+#pragma unroll
+      for (int r = 0; r < kLaRows; r += 4) {
+        if ((p.nq & 3) == 0) {
+          const float4 v = from[j] >= 0 && r < p.nq ? *reinterpret_cast<const float4*>(src + r) : make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+          s[j][r] = v.x;
+          s[j][r + 1] = v.y;
+          s[j][r + 2] = v.z;
+          s[j][r + 3] = v.w;
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[j][r + e] = from[j] >= 0 && r + e < p.nq ? src[r + e] : -INFINITY;
+        }
+      }
+    }
     for (int r = warp; r < p.nq; r += kLcWarps) {
       float m = -INFINITY, l = 0.f;
       for (int c = c0 + lane; c <= c1; c += 32) {
@@ -614,21 +657,14 @@ __global__ void __launch_bounds__(kLcThreads) layer_attn_combine_kernel(const __
       if (lane == 0) lse_s[r] = l == 0.f ? INFINITY : m + log2f(l);  // (a row that saw nothing gives nothing)
     }
     __syncthreads();
-    const int k1 = min(k0 + kLcUnits, u);
-    for (int i = tid; i < (k1 - k0) * kLaUnit; i += kLcThreads) {
-      const int k = k0 + i / kLaUnit, in = i % kLaUnit;
-      const int t = (k < sq.ua ? k : sq.ub0 + k - sq.ua) * kLaUnit + in;
-      const bool fresh = t == sq.n;  // the appended row: its weight begins here
-      if (t >= sq.n_tot || (fresh && !(p.flags & MC_LAYER_APPEND))) continue;
-      const float* s = p.scores + (((size_t)(x0 + k) * p.g.n_kv_heads + head) * kLaUnit + in) * p.nq;
-      float w = 0.f;
-      for (int r = 0; r < p.nq; ++r) w += ex2(s[r] - lse_s[r]);
-      const int slot = t >> p.g.page_shift;
-      if (slot >= p.g.max_pages_per_seq) continue;  // (flagged by the split kernel)
-      const int page = p.g.block_table[(size_t)b * p.g.max_pages_per_seq + slot];
-      if (!page_ok(p.g, page)) continue;
-      float* dst = p.weights + ((size_t)page * p.g.n_kv_heads + head) * p.g.page_size + (t & (p.g.page_size - 1));
-      *dst = fresh ? w : *dst + w;
+#pragma unroll
+    for (int j = 0; j < kOwn; ++j) {
+      if (at[j] < 0) continue;
+      float sum = 0.f;
+#pragma unroll
+      for (int r = 0; r < kLaRows; ++r)
+        if (r < p.nq) sum += ex2(s[j][r] - lse_s[r]);
+      p.weights[at[j]] = w[j] + sum;
     }
     return;
   }
