@@ -9,9 +9,18 @@ constexpr float kLn2 = 0.69314718055994530942f;
 
 // tanh(x) = x P(x^2) by reweighted least squares on tanh(x) / x: degree 4 on [-1/2, 1/2] (1.3e-8 relative), degree 6 on
 // [-1, 1] (5e-8).
-constexpr float kTanhTiny[5] = {9.9999998687e-01f, -3.3333069391e-01f, 1.3324779261e-01f, -5.2986071693e-02f, 1.7134999450e-02f};
-constexpr float kTanhSmall[7] = {9.9999995024e-01f, -3.3332839133e-01f, 1.3325203849e-01f, -5.3457019959e-02f,
-                                 2.0289962009e-02f, -6.2033628195e-03f, 1.0410172275e-03f};
+__host__ __device__ constexpr float tanh_tiny(int j) {
+  return j == 0 ? 9.9999998687e-01f : j == 1 ? -3.3333069391e-01f : j == 2 ? 1.3324779261e-01f : j == 3 ? -5.2986071693e-02f : 1.7134999450e-02f;
+}
+__host__ __device__ constexpr float tanh_small(int j) {
+  return j == 0   ? 9.9999995024e-01f
+         : j == 1 ? -3.3332839133e-01f
+         : j == 2 ? 1.3325203849e-01f
+         : j == 3 ? -5.3457019959e-02f
+         : j == 4 ? 2.0289962009e-02f
+         : j == 5 ? -6.2033628195e-03f
+                  : 1.0410172275e-03f;
+}
 
 // The score rule of a call (mc_score_opts) in the form the kernels use; scores are kept as log2(e) times their value,
 // so that a probability is one instruction.
@@ -82,6 +91,37 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
   return r;
 }
+// q . k -> score (log2 units), the cap included, the distance bias not.
+__device__ __forceinline__ float score_of(const ScoreRule& r, float dot) {
+  return r.cap_log2 > 0.f ? r.cap_log2 * tanh_score(dot * r.cap_inv) : dot * r.scale_log2;
+}
+
+// Four scores of a warp's lanes.  With a cap: x P(x^2) two at a time while every |x| of the warp is at most 1 (scores up
+// to the cap itself before it), else the exact form.
+__device__ __forceinline__ void scores_of(const ScoreRule& r, float (&s)[4]) {
+  if (!(r.cap_log2 > 0.f)) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) s[k] *= r.scale_log2;
+    return;
+  }
+  float big = 0.f;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) big = fmaxf(big, fabsf(s[k] * r.cap_inv));
+  if (__all_sync(0xffffffffu, big <= 1.f)) {
+    const uint64_t inv = pack2(r.cap_inv, r.cap_inv), cap = pack2(r.cap_log2, r.cap_log2);
+#pragma unroll
+    for (int k = 0; k < 4; k += 2) {
+      const uint64_t x = mul2(pack2(s[k], s[k + 1]), inv), z = mul2(x, x);
+      uint64_t q = pack2(tanh_small(6), tanh_small(6));
+#pragma unroll
+      for (int j = 5; j >= 0; --j) q = fma2(q, z, pack2(tanh_small(j), tanh_small(j)));
+      unpack2(mul2(mul2(x, q), cap), s[k], s[k + 1]);
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) s[k] = score_of(r, s[k]);
+  }
+}
 // The largest of three numbers, and of one and two magnitudes (sm_100's three-input forms).
 __device__ __forceinline__ float max3(float a, float b, float c) {
   float r;
@@ -93,11 +133,6 @@ __device__ __forceinline__ float max3_abs(float a, float b, float c) {
   asm("max.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
 }
-// q . k -> score (log2 units), the cap included, the distance bias not.
-__device__ __forceinline__ float score_of(const ScoreRule& r, float dot) {
-  return r.cap_log2 > 0.f ? r.cap_log2 * tanh_score(dot * r.cap_inv) : dot * r.scale_log2;
-}
-
 // What one query sees: positions p with p <= q_pos and (p < prefix or p >= lo_pos).
 struct View {
   int q_pos, prefix, lo_pos;

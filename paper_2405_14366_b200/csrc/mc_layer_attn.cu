@@ -4,15 +4,17 @@
 //   s_i = cap tanh(sm q.k_i / cap) - slope_h (q_pos - p_i)      (cap, slope: optional)
 //   out = sum_i softmax(s)_i v_i  over the tokens that the query sees (causal, window, document, prefix)
 //
-// One pass over the cache with a running maximum and sum.  The token axis is cut into units of 128 tokens (only units
+// One pass over the cache with a running maximum and sum.  The token axis is cut into units of 64 tokens (only units
 // that hold a visible token are counted); the grid is T teams of S CTAs, a team takes an equal share of the units of
 // the batch, its member j takes them for the kv heads j, j + S, ...: the split of mc_attn.cu, for the same reason
 // (equal shares whatever the lengths are, neighbouring tiles of a page streamed at about the same time).
-// A warp owns 16-token slices of its CTA's units and is a pipeline of its own: it streams their K and V rows through
-// its ring of stages with tiled bulk copies (128-byte swizzle; its lane 0 issues them, an mbarrier per stage counts
-// the bytes) and consumes them itself, so nothing but the end of a piece -- the units of one (sequence, kv head) in
-// the team's share -- makes the four warps wait for one another.  Scores never leave registers: D = K q^T
-// (16 tokens x 8 query rows) becomes the B operand of V^T P by two 8x8 transposes (movmatrix).
+// A warp owns a 16-token slice of each of its CTA's units and is a pipeline of its own: it streams the slices' K and V
+// rows through its ring of stages with tiled bulk copies (128-byte swizzle; its lane 0 issues them, an mbarrier per
+// stage counts the bytes), consumes them itself and writes a partial result of its own for every piece -- the units of
+// one (sequence, kv head) in the team's share --, so that no warp ever waits for another.  Scores never leave
+// registers: D = K q^T (16 tokens x 8 query rows) becomes the B operand of V^T P by two 8x8 transposes (movmatrix).
+// Two stages of 8 KB per warp, 128 KB per SM: a third stage was SLOWER (7b batch 83 -> 88 us, 16 x 8192 grouped 87 ->
+// 93): more requests outstanding than the memory serves well.
 // Where a slice's rows come from is worked out a lane per slice, 32 slices at a time and one window ahead: a
 // dependent load takes microseconds while the copies saturate the memory system.
 #include <algorithm>
@@ -26,14 +28,13 @@
 
 namespace mc {
 
-constexpr int kLaUnit = 128;   // tokens per unit of work
+constexpr int kLaUnit = 64;    // tokens per unit of work: a slice per warp
 constexpr int kLaSlice = 16;   // tokens per stage: one k step of the V contraction, never more than a page
 constexpr int kLaWarps = 4;
 constexpr int kLaThreads = kLaWarps * 32;
-constexpr int kLaStages = 3;
+constexpr int kLaStages = 2;
 constexpr int kLaStageBytes = 2 * kLaSlice * kRowBytes;  // K rows, V rows: 8 KB
 constexpr int kLaRows = 8;                               // query rows per kv head: the 8-wide N tile
-constexpr int kLaSlab = 132;                             // floats per row of a partial output in shared memory
 constexpr int kLaCtasPerSm = 2;
 constexpr int kLaBoxBytes = kLaSlice * 128;              // one copy: 16 rows x 64 channels
 
@@ -48,9 +49,9 @@ struct LayerAttnParams {
   const char* q;
   const char* k_new;
   const char* v_new;
-  float* part_o;   // [piece][nq rows of a head]...: [(team + sequence)][n_q_heads][128]
-  float* part_ml;  // [(team + sequence)][n_q_heads][2]
-  float* scores;   // [unit][n_kv_heads][128][nq], null unless weights are gathered
+  float* part_o;   // [(team + sequence)][warp][n_q_heads][128]
+  float* part_ml;  // [(team + sequence)][warp][n_q_heads][2]
+  float* scores;   // [unit][n_kv_heads][kLaUnit][nq], null unless weights are gathered
   int nq, n_q_heads;
   int team_size, n_teams;
   int flags;
@@ -143,12 +144,13 @@ __device__ __forceinline__ int live_teams(const LayerAttnParams& p, int n_units)
 
 // One slice as a lane of the window knows it.
 struct Slice {
-  int head, b, t0;  // kv head, sequence, first token
-  int x;            // unit (global)
-  int page;         // raw page id (looked at one window later)
-  int flags;
+  int meta;  // flags | sequence << 5 | kv head << 14
+  int t0;    // first token
+  int x;     // unit (global)
+  int page;  // raw page id (looked at only when the slice's turn is near)
 };
 enum { kSlTokens = 1, kSlLoad = 2, kSlFirst = 4, kSlLast = 8, kSlBadSlot = 16 };
+static_assert(kMaxLayerBatch <= 512, "nine bits");
 
 template <int DT>
 __device__ __forceinline__ uint32_t transpose8(uint32_t v) {
@@ -165,9 +167,7 @@ layer_attn_split_kernel(const __grid_constant__ LayerAttnParams p, const __grid_
   grid_dep_launch();
   extern __shared__ unsigned char smem_raw[];
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  float* slab = reinterpret_cast<float*>(smem + kLaWarps * kLaStages * kLaStageBytes);  // [2][kLaRows][kLaSlab]
-  float* ml_s = slab + 2 * kLaRows * kLaSlab;                                           // [2][kLaRows][2]
-  int* pos_s = reinterpret_cast<int*>(ml_s + 2 * kLaRows * 2);                          // [warps][stages][16]
+  int* pos_s = reinterpret_cast<int*>(smem + kLaWarps * kLaStages * kLaStageBytes);     // [warps][stages][16]
   uint64_t* bars = reinterpret_cast<uint64_t*>(pos_s + kLaWarps * kLaStages * kLaSlice);  // [warps][stages]
   int* pre_s = reinterpret_cast<int*>(bars + kLaWarps * kLaStages);                     // [batch + 1]
   volatile int* s_abort = pre_s + p.g.batch + 1;
@@ -180,6 +180,10 @@ layer_attn_split_kernel(const __grid_constant__ LayerAttnParams p, const __grid_
   const uint32_t st0 = smem_u32(smem) + warp * kLaStages * kLaStageBytes;
   const uint32_t pos0 = smem_u32(pos_s + warp * kLaStages * kLaSlice);
 
+  if (tid == 32) {
+    prefetch_map(&map_k);
+    prefetch_map(&map_v);
+  }
   if (tid == 0) {
     for (int s = 0; s < kLaWarps * kLaStages; ++s) mbar_init(smem_u32(bars + s), 1);
     *s_abort = 0;
@@ -197,34 +201,48 @@ layer_attn_split_kernel(const __grid_constant__ LayerAttnParams p, const __grid_
   }
   const int nx = x_end - x_begin;
   const int n_heads = member < H ? (H - member + p.team_size - 1) / p.team_size : 0;
-  const int n_slices = 2 * nx * n_heads;  // of each warp
+  const int n_slices = nx * n_heads;  // of each warp
 
-  // slice i of this warp: head by head, unit by unit, the slices `warp` and `warp + 4` of a unit
+  // slice i of this warp: head by head, unit by unit
   auto load_slice = [&](int i) {
     Slice s;
-    s.head = s.b = s.t0 = s.x = s.page = s.flags = 0;
+    s.meta = s.t0 = s.x = s.page = 0;
     if (i >= n_slices) return s;
-    const int hd = i / (2 * nx), rem = i - hd * 2 * nx;
-    s.head = member + hd * p.team_size;
-    s.x = x_begin + (rem >> 1);
-    s.b = seq_of_unit(pre_s, p.g.batch, s.x);
-    const Seq q = seq_of(p, s.b);
-    const int k = s.x - pre_s[s.b];
-    s.t0 = (k < q.ua ? k : q.ub0 + k - q.ua) * kLaUnit + (warp + 4 * (rem & 1)) * kLaSlice;
+    const int hd = n_heads == 1 ? 0 : i / nx, rem = i - hd * nx;
+    const int head = member + hd * p.team_size;
+    s.x = x_begin + rem;
+    const int b = seq_of_unit(pre_s, p.g.batch, s.x);
+    const Seq q = seq_of(p, b);
+    const int k = s.x - pre_s[b];
+    s.t0 = (k < q.ua ? k : q.ub0 + k - q.ua) * kLaUnit + warp * kLaSlice;
     // (without a positions pool a slice that holds no visible token, nor the row to append, is left out)
     const bool wanted = p.positions != nullptr || s.t0 < q.a || (s.t0 + kLaSlice > q.lo && s.t0 < q.hi) ||
                         ((p.flags & MC_LAYER_APPEND) && q.n >= s.t0 && q.n < s.t0 + kLaSlice);
-    if (wanted && s.t0 < q.n_tot) s.flags |= kSlTokens;
-    if (wanted && s.t0 < q.n) s.flags |= kSlLoad;
-    if (!(rem & 1) && (s.x == x_begin || k == 0)) s.flags |= kSlFirst;
-    if ((rem & 1) && (s.x + 1 == x_end || k + 1 == q.u)) s.flags |= kSlLast;
-    if ((s.flags & kSlLoad) || ((s.flags & kSlTokens) && (p.flags & MC_LAYER_APPEND))) {
+    int fl = 0;
+    if (wanted && s.t0 < q.n_tot) fl |= kSlTokens;
+    if (wanted && s.t0 < q.n) fl |= kSlLoad;
+    if (s.x == x_begin || k == 0) fl |= kSlFirst;
+    if (s.x + 1 == x_end || k + 1 == q.u) fl |= kSlLast;
+    if ((fl & kSlLoad) || ((fl & kSlTokens) && (p.flags & MC_LAYER_APPEND))) {
       const int slot = s.t0 >> shift;
-      if (slot < p.g.max_pages_per_seq) s.page = p.g.block_table[(size_t)s.b * p.g.max_pages_per_seq + slot];
-      else s.flags |= kSlBadSlot;
+      if (slot < p.g.max_pages_per_seq) s.page = p.g.block_table[(size_t)b * p.g.max_pages_per_seq + slot];
+      else fl |= kSlBadSlot;
     }
+    s.meta = fl | b << 5 | head << 14;
     return s;
   };
+  // row (of the pools' rows) where a slice begins, -1 if nothing is to be copied; a page id outside the pools reads
+  // page 0 and is flagged
+  auto slice_row = [&](int page, int head, int t0) {
+    if (!page_ok(p.g, page)) page = 0;
+    return (page * H + head) * p.g.page_size + (t0 & (p.g.page_size - 1));
+  };
+  auto row_of = [&](const Slice& s) {
+    if (!(s.meta & kSlLoad)) return -1;
+    if ((s.meta & kSlBadSlot) || !page_ok(p.g, s.page)) atomicOr(p.status, MC_FLAG_BAD_METADATA);
+    return slice_row(s.page, s.meta >> 14, s.t0);
+  };
+  // (both windows before the stream begins: the lengths that load_slice looks at would take microseconds behind it)
   Slice win = load_slice(lane), nxt = load_slice(32 + lane);
 
   auto load_q = [&](int b, int head, uint32_t (&q0)[8], uint32_t (&q2)[8]) {
@@ -238,33 +256,23 @@ layer_attn_split_kernel(const __grid_constant__ LayerAttnParams p, const __grid_
   };
   uint32_t q0[8], q2[8];
   {
-    const int b = __shfl_sync(0xffffffffu, win.b, 0), h = __shfl_sync(0xffffffffu, win.head, 0);
-    if (n_slices > 0) load_q(b, h, q0, q2);
+    const int meta = __shfl_sync(0xffffffffu, win.meta, 0);
+    if (n_slices > 0) load_q((meta >> 5) & 511, meta >> 14, q0, q2);
   }
 
   grid_dep_wait();
   if (bad) atomicOr(p.status, MC_FLAG_BAD_METADATA);
 
-  // row (of the pools' rows) where a slice begins; a page id outside the pools reads page 0 and is flagged
-  auto slice_row = [&](int page, int head, int t0) {
-    if (!page_ok(p.g, page)) page = 0;
-    return (page * H + head) * p.g.page_size + (t0 & (p.g.page_size - 1));
-  };
-  auto issue = [&](int i) {  // slice i into its stage
+  int win_row = row_of(win), nxt_row = -1;
+  auto issue = [&](int i) {  // slice i into its stage (four lanes issuing a box each were slower than one lane issuing four)
     if (i >= n_slices) return;
-    const int src = i & 31;
     // (i lies in the current window or, at its end, in the next one)
-    const bool ahead = i >= 32 && (i & 31) < kLaStages - 1;
-    const int fl = __shfl_sync(0xffffffffu, ahead ? nxt.flags : win.flags, src);
-    const int page = __shfl_sync(0xffffffffu, ahead ? nxt.page : win.page, src);
-    const int head = __shfl_sync(0xffffffffu, ahead ? nxt.head : win.head, src);
-    const int t0 = __shfl_sync(0xffffffffu, ahead ? nxt.t0 : win.t0, src);
+    const int y = __shfl_sync(0xffffffffu, i >= 32 && (i & 31) < kLaStages - 1 ? nxt_row : win_row, i & 31);
+    if (y < 0 || *s_abort) return;
     const int s = i % kLaStages;
-    if (!(fl & kSlLoad) || *s_abort) return;
+    const uint32_t bar = bar0 + 8 * s;
     if (lane == 0) {
-      if ((fl & kSlBadSlot) || !page_ok(p.g, page)) atomicOr(p.status, MC_FLAG_BAD_METADATA);
-      const int y = slice_row(page, head, t0);
-      const uint32_t bar = bar0 + 8 * s, dst = st0 + s * kLaStageBytes;
+      const uint32_t dst = st0 + s * kLaStageBytes;
       mbar_expect_tx(bar, (uint32_t)(kLaStageBytes + (p.positions ? kLaSlice * 4 : 0)));
       tma_load_2d(dst, &map_k, 0, y, bar);
       tma_load_2d(dst + kLaBoxBytes, &map_k, 64, y, bar);
@@ -285,14 +293,15 @@ layer_attn_split_kernel(const __grid_constant__ LayerAttnParams p, const __grid_
     const int src = i & 31;
     if (src == 0 && i > 0) {
       win = nxt;
+      win_row = nxt_row;
       nxt = load_slice((i & ~31) + 32 + lane);
     }
+    if (src == 32 - kLaStages) nxt_row = row_of(nxt);  // (its loads are long done)
     // the stage of the slice before this one is free: its warp has read it
     __syncwarp();
     issue(i + kLaStages - 1);
-    const int fl = __shfl_sync(0xffffffffu, win.flags, src);
-    const int b = __shfl_sync(0xffffffffu, win.b, src);
-    const int head = __shfl_sync(0xffffffffu, win.head, src);
+    const int fl = __shfl_sync(0xffffffffu, win.meta, src);  // (flags in the low bits)
+    const int b = (fl >> 5) & 511, head = fl >> 14;
     const int t0 = __shfl_sync(0xffffffffu, win.t0, src);
     const int s = i % kLaStages;
     if (fl & kSlFirst) {
@@ -303,6 +312,18 @@ layer_attn_split_kernel(const __grid_constant__ LayerAttnParams p, const __grid_
 #pragma unroll
         for (int k = 0; k < 4; ++k) acc[j][k] = 0.f;
       sq = seq_of(p, b);
+      // what this piece will read late and the next piece first goes to L1 meanwhile (a demand load takes microseconds
+      // behind the stream): the step's new rows, the next piece's queries
+      if (p.k_new && lane < 4) {
+        const char* r = ((lane & 2) ? p.v_new : p.k_new) + ((size_t)b * H + head) * kRowBytes + (lane & 1) * 128;
+        asm volatile("prefetch.global.L1 [%0];" ::"l"(r));
+      }
+      const uint32_t later = __ballot_sync(0xffffffffu, (win.meta & kSlFirst) != 0) & ~((2u << src) - 1u);
+      if (later) {
+        const int mn = __shfl_sync(0xffffffffu, win.meta, __ffs(later) - 1);
+        if (lane < 2 * nq)
+          asm volatile("prefetch.global.L1 [%0];" ::"l"(p.q + (((size_t)((mn >> 5) & 511) * p.n_q_heads + (mn >> 14) * nq) * kRowBytes) + lane * 128));
+      }
       if (p.rule.slopes) {
         sl0 = colp < nq ? p.rule.slopes[head * nq + colp] * kLog2e : 0.f;
         sl1 = colp + 1 < nq ? p.rule.slopes[head * nq + colp + 1] * kLog2e : 0.f;
@@ -341,8 +362,8 @@ layer_attn_split_kernel(const __grid_constant__ LayerAttnParams p, const __grid_
         }
         __syncwarp();
       }
-      // ---- scores: D[token][query row], even and odd k steps summed apart
-      float d0[4] = {0.f, 0.f, 0.f, 0.f}, d1[4] = {0.f, 0.f, 0.f, 0.f};
+      // ---- scores: D[token][query row], k steps in four chains
+      float d[4][4] = {};  // four chains of k steps
       {
         const int tr = (mi & 1) * 8 + mr;
         uint32_t ra[8][4];
@@ -352,14 +373,12 @@ layer_attn_split_kernel(const __grid_constant__ LayerAttnParams p, const __grid_
           ldsm_x4(sb + (c >> 3) * kLaBoxBytes + tr * 128 + (((c & 7) ^ mr) << 4), ra[ks][0], ra[ks][1], ra[ks][2], ra[ks][3]);
         }
 #pragma unroll
-        for (int ks = 0; ks < 8; ks += 2) {
-          mma_rows<DT>(d0, ra[ks][0], ra[ks][1], ra[ks][2], ra[ks][3], q0[ks], q2[ks]);
-          mma_rows<DT>(d1, ra[ks + 1][0], ra[ks + 1][1], ra[ks + 1][2], ra[ks + 1][3], q0[ks + 1], q2[ks + 1]);
-        }
+        for (int ks = 0; ks < 8; ++ks) mma_rows<DT>(d[ks & 3], ra[ks][0], ra[ks][1], ra[ks][2], ra[ks][3], q0[ks], q2[ks]);
       }
       float sc[4];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) sc[k] = score_of(p.rule, d0[k] + d1[k]);
+      for (int k = 0; k < 4; ++k) sc[k] = (d[0][k] + d[1][k]) + (d[2][k] + d[3][k]);
+      scores_of(p.rule, sc);
       // ---- distance bias and masks (tokens t0 + row and + 8)
       uint32_t hidden = 0;  // bit r: token t0 + r is not seen (the same in every lane)
       {
@@ -410,14 +429,14 @@ layer_attn_split_kernel(const __grid_constant__ LayerAttnParams p, const __grid_
         }
       }
       if (hidden != 0xffffu) {
-        // ---- running maximum and sum
+        // ---- running maximum and sum (the lanes compare notes only when one of them holds a larger score)
         float n0 = fmaxf(sc[0], sc[2]), n1 = fmaxf(sc[1], sc[3]);
-#pragma unroll
-        for (int o = 4; o < 32; o <<= 1) {
-          n0 = fmaxf(n0, __shfl_xor_sync(0xffffffffu, n0, o));
-          n1 = fmaxf(n1, __shfl_xor_sync(0xffffffffu, n1, o));
-        }
         if (__any_sync(0xffffffffu, n0 > m0 || n1 > m1)) {
+#pragma unroll
+          for (int o = 4; o < 32; o <<= 1) {
+            n0 = fmaxf(n0, __shfl_xor_sync(0xffffffffu, n0, o));
+            n1 = fmaxf(n1, __shfl_xor_sync(0xffffffffu, n1, o));
+          }
           n0 = fmaxf(n0, m0);
           n1 = fmaxf(n1, m1);
           const float f0 = n0 == m0 ? 1.f : ex2(m0 - n0), f1 = n1 == m1 ? 1.f : ex2(m1 - n1);
@@ -467,98 +486,32 @@ layer_attn_split_kernel(const __grid_constant__ LayerAttnParams p, const __grid_
       if (wrote) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
     if (fl & kSlLast) {
-      // the next piece's queries travel while the four warps' partial results meet
       if (i + 1 < n_slices) {
         const bool nw = src == 31;
-        const int bn = __shfl_sync(0xffffffffu, nw ? nxt.b : win.b, (i + 1) & 31);
-        const int hn = __shfl_sync(0xffffffffu, nw ? nxt.head : win.head, (i + 1) & 31);
-        load_q(bn, hn, q0, q2);
+        const int mn = __shfl_sync(0xffffffffu, nw ? nxt.meta : win.meta, (i + 1) & 31);
+        load_q((mn >> 5) & 511, mn >> 14, q0, q2);
       }
 #pragma unroll
       for (int o = 4; o < 32; o <<= 1) {
         l0 += __shfl_xor_sync(0xffffffffu, l0, o);
         l1 += __shfl_xor_sync(0xffffffffu, l1, o);
       }
-      // warps 2, 3 into 0, 1; then 1 into 0
-      __syncthreads();
+      const size_t prow = ((size_t)(team + b) * kLaWarps + warp) * p.n_q_heads + head * nq;
+      if (colp < nq) {
 #pragma unroll
-      for (int step = 2; step > 0; step >>= 1) {
-        if (warp >= step && warp < 2 * step) {
-          float* o = slab + (warp - step) * kLaRows * kLaSlab;
-          float* mlo = ml_s + (warp - step) * kLaRows * 2;
-          if (colp < nq) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-              o[colp * kLaSlab + 16 * j + row] = acc[j][0];
-              o[colp * kLaSlab + 16 * j + row + 8] = acc[j][2];
-            }
-            if (row == 0) {
-              mlo[2 * colp] = m0;
-              mlo[2 * colp + 1] = l0;
-            }
-          }
-          if (colp + 1 < nq) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-              o[(colp + 1) * kLaSlab + 16 * j + row] = acc[j][1];
-              o[(colp + 1) * kLaSlab + 16 * j + row + 8] = acc[j][3];
-            }
-            if (row == 0) {
-              mlo[2 * colp + 2] = m1;
-              mlo[2 * colp + 3] = l1;
-            }
-          }
+        for (int j = 0; j < 8; ++j) {
+          p.part_o[(prow + colp) * kHeadDim + 16 * j + row] = acc[j][0];
+          p.part_o[(prow + colp) * kHeadDim + 16 * j + row + 8] = acc[j][2];
         }
-        __syncthreads();
-        if (warp < step) {
-          const float* o = slab + warp * kLaRows * kLaSlab;
-          const float* mlo = ml_s + warp * kLaRows * 2;
-          auto join = [&](float& m, float& l, int r, float& fa, float& fb) {
-            const float mb = mlo[2 * r], lb = mlo[2 * r + 1];
-            const float M = fmaxf(m, mb);
-            fa = l == 0.f ? 0.f : ex2(m - M);
-            fb = lb == 0.f ? 0.f : ex2(mb - M);
-            m = M;
-            l = l * fa + lb * fb;
-          };
-          float fa = 0.f, fb = 0.f;
-          if (colp < nq) {
-            join(m0, l0, colp, fa, fb);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-              acc[j][0] = acc[j][0] * fa + o[colp * kLaSlab + 16 * j + row] * fb;
-              acc[j][2] = acc[j][2] * fa + o[colp * kLaSlab + 16 * j + row + 8] * fb;
-            }
-          }
-          if (colp + 1 < nq) {
-            join(m1, l1, colp + 1, fa, fb);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-              acc[j][1] = acc[j][1] * fa + o[(colp + 1) * kLaSlab + 16 * j + row] * fb;
-              acc[j][3] = acc[j][3] * fa + o[(colp + 1) * kLaSlab + 16 * j + row + 8] * fb;
-            }
-          }
-        }
-        if (step == 2) __syncthreads();
+        if (row == 0) *reinterpret_cast<float2*>(p.part_ml + 2 * (prow + colp)) = make_float2(m0, l0);
       }
-      if (warp == 0) {
-        const size_t prow = (size_t)(team + b) * p.n_q_heads + head * nq;
-        if (colp < nq) {
+      if (colp + 1 < nq) {
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            p.part_o[(prow + colp) * kHeadDim + 16 * j + row] = acc[j][0];
-            p.part_o[(prow + colp) * kHeadDim + 16 * j + row + 8] = acc[j][2];
-          }
-          if (row == 0) *reinterpret_cast<float2*>(p.part_ml + 2 * (prow + colp)) = make_float2(m0, l0);
+        for (int j = 0; j < 8; ++j) {
+          p.part_o[(prow + colp + 1) * kHeadDim + 16 * j + row] = acc[j][1];
+          p.part_o[(prow + colp + 1) * kHeadDim + 16 * j + row + 8] = acc[j][3];
         }
-        if (colp + 1 < nq) {
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            p.part_o[(prow + colp + 1) * kHeadDim + 16 * j + row] = acc[j][1];
-            p.part_o[(prow + colp + 1) * kHeadDim + 16 * j + row + 8] = acc[j][3];
-          }
-          if (row == 0) *reinterpret_cast<float2*>(p.part_ml + 2 * (prow + colp + 1)) = make_float2(m1, l1);
-        }
+        if (row == 0) *reinterpret_cast<float2*>(p.part_ml + 2 * (prow + colp + 1)) = make_float2(m1, l1);
       }
     }
   }
@@ -569,11 +522,11 @@ layer_attn_split_kernel(const __grid_constant__ LayerAttnParams p, const __grid_
 
 // Joins a sequence's pieces (consecutive teams): out = sum_j 2^(m_j - M) o_j / sum_j 2^(m_j - M) l_j.  Blocks
 // [0, combine_x): R query heads each (8: a warp per output row; 1: the eight warps share one row's pieces).  Blocks
-// behind them (calls that gather weights): w_i += sum over the head group of 2^(s_i - lse) for eight units of one kv
+// behind them (calls that gather weights): w_i += sum over the head group of 2^(s_i - lse) for 1024 tokens of one kv
 // head, from the scores the split kernel left; they work the log-sum-exps out themselves, so one launch does both.
 constexpr int kLcThreads = 256;
 constexpr int kLcWarps = kLcThreads / 32;
-constexpr int kLcUnits = 8;  // units per weight block
+constexpr int kLcUnits = 16;  // units per weight block: 1024 tokens
 
 template <int DT, int R>
 __global__ void __launch_bounds__(kLcThreads) layer_attn_combine_kernel(const __grid_constant__ LayerAttnParams p, unsigned short* out,
@@ -641,8 +594,8 @@ __global__ void __launch_bounds__(kLcThreads) layer_attn_combine_kernel(const __
     }
     for (int r = warp; r < p.nq; r += kLcWarps) {
       float m = -INFINITY, l = 0.f;
-      for (int c = c0 + lane; c <= c1; c += 32) {
-        const float2 v = *reinterpret_cast<const float2*>(p.part_ml + 2 * ((size_t)(c + b) * p.n_q_heads + head * p.nq + r));
+      for (int c = c0 * kLaWarps + lane; c < (c1 + 1) * kLaWarps; c += 32) {
+        const float2 v = *reinterpret_cast<const float2*>(p.part_ml + 2 * ((size_t)(c + b * kLaWarps) * p.n_q_heads + head * p.nq + r));
         const float M = fmaxf(m, v.x);
         l = (l == 0.f ? 0.f : l * ex2(m - M)) + (v.y == 0.f ? 0.f : v.y * ex2(v.x - M));
         m = M;
@@ -676,15 +629,16 @@ __global__ void __launch_bounds__(kLcThreads) layer_attn_combine_kernel(const __
   float M = -INFINITY, L = 0.f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
   if (active) {
-    for (int c = c0 + grp; c <= c1; c += 4 * GP) {  // four pieces in flight
+    const int c_end = (c1 + 1) * kLaWarps;  // (a piece has a part of each of its CTA's warps)
+    for (int c = c0 * kLaWarps + grp; c < c_end; c += 4 * GP) {  // four parts in flight
       float2 ml[4];
       float4 v[4];
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         ml[k] = make_float2(-INFINITY, 0.f);
         v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (c + k * GP <= c1) {
-          const size_t prow = (size_t)(c + k * GP + b) * p.n_q_heads + hq;
+        if (c + k * GP < c_end) {
+          const size_t prow = (size_t)(c + k * GP + b * kLaWarps) * p.n_q_heads + hq;
           ml[k] = *reinterpret_cast<const float2*>(p.part_ml + 2 * prow);
           v[k] = *reinterpret_cast<const float4*>(p.part_o + prow * kHeadDim + 4 * lane);
         }
@@ -767,7 +721,7 @@ static LayerAttnPlan layer_attn_plan(const mc_config* cfg, const mc_batch* bt, i
   pl.seq_units = bt->max_seq_len / kLaUnit + 1;  // (with the step's new token)
   pl.max_units = (long long)bt->batch * pl.seq_units;
   pl.n_teams = (int)std::max<long long>(1, std::min<long long>(slots / pl.team_size, pl.max_units));
-  const size_t prow = (size_t)(pl.n_teams + bt->batch) * cfg->n_q_heads;
+  const size_t prow = (size_t)(pl.n_teams + bt->batch) * kLaWarps * cfg->n_q_heads;
   pl.o_bytes = align_up(prow * kHeadDim * 4, 256);
   pl.ml_bytes = align_up(prow * 2 * 4, 256);
   pl.score_bytes = (flags & MC_LAYER_ACCUMULATE) ? align_up((size_t)pl.max_units * kLaUnit * cfg->n_q_heads * 4, 256) : 0;
@@ -808,8 +762,10 @@ mc_status launch_layer_attn(const mc_config* cfg, const mc_batch* bt, const Geom
   ap.team_size = pl.team_size;
   ap.n_teams = pl.n_teams;
   ap.flags = flags;
-  const size_t smem = 1024 + (size_t)kLaWarps * kLaStages * kLaStageBytes + 2 * kLaRows * (kLaSlab + 2) * 4 +
-                      kLaWarps * kLaStages * (kLaSlice * 4 + 8) + (size_t)(bt->batch + 2) * 4;
+  // (asked for so much that two CTAs fill an SM: with room for a third, an early start behind another kernel packs some
+  // SMs with three and leaves others with one -- 83 -> 86 us on 8 x 4096)
+  const size_t smem = std::max<size_t>(80 * 1024, 1024 + (size_t)kLaWarps * kLaStages * (kLaStageBytes + kLaSlice * 4 + 8) +
+                                                      (size_t)(bt->batch + 2) * 4);
   auto* split = cfg->dtype == MC_F16 ? layer_attn_split_kernel<MC_F16> : layer_attn_split_kernel<MC_BF16>;
   MC_CUDA_CHECK(cudaFuncSetAttribute(split, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
   MC_CUDA_CHECK(launch_pdl(split, dim3(pl.n_teams * pl.team_size), dim3(kLaThreads), smem, stream, ap, map_k, map_v));

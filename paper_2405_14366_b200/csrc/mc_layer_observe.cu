@@ -690,8 +690,8 @@ mc_status launch_layer_observe(const mc_config* cfg, const mc_batch* bt, const G
     const double inv = (double)opts->sm_scale / opts->softcap, top = (double)opts->softcap * kLog2e;
     double scale = inv * top;  // of coefficient j: inv^(2 j + 1) * cap * log2(e)
     for (int j = 0; j < 7; ++j, scale *= inv * inv) {
-      if (j < 5) op.tiny[j] = (float)(kTanhTiny[j] * scale);
-      op.small[j] = (float)(kTanhSmall[j] * scale);
+      if (j < 5) op.tiny[j] = (float)(tanh_tiny(j) * scale);
+      op.small[j] = (float)(tanh_small(j) * scale);
     }
     // (a polynomial whose coefficients leave binary32's normal range is not used)
     const auto fits = [](float c) { return fabsf(c) > 1e-37f && fabsf(c) < 1e30f; };

@@ -119,10 +119,9 @@ def test_workspace_bytes(lib):
         return out.value if code == 0 else -code
     plain = need(batch(), 2, 1)
     assert plain > 0 and plain % 256 == 0
-    # gathering weights keeps the scores: 4 bytes per (token, query head), whole units of 128 tokens
-    assert need(batch(), 2, 3) - plain == 2 * 128 * 32 * 4
-    assert need(batch(max_len=127), 2, 3) - need(batch(max_len=127), 2, 1) == 2 * 128 * 32 * 4
-    assert need(batch(max_len=128), 2, 3) - need(batch(max_len=128), 2, 1) == 2 * 256 * 32 * 4  # the step's token has a unit of its own
+    # gathering weights keeps the scores: 4 bytes per (token, query head), whole units of 64 tokens
+    for n, held in ((63, 64), (64, 128), (127, 128), (128, 192)):  # (the step's token counts)
+        assert need(batch(max_len=n, mpps=9), 2, 3) - need(batch(max_len=n, mpps=9), 2, 1) == 2 * held * 32 * 4
     assert need(batch(), 2, 4) == -1 and need(batch(), 9, 0) == -1 and need(batch(), 0, 0) == -1
     assert need(batch(), 2, 0, cfg(page_size=8)) == -2
     assert need(batch(), 4, 0) >= 2 * 8 * 64 * 4 and need(batch(), 4, 1) == -1
