@@ -34,7 +34,6 @@ constexpr int kLaWarps = 4;
 constexpr int kLaThreads = kLaWarps * 32;
 constexpr int kLaStages = 2;
 constexpr int kLaStageBytes = 2 * kLaSlice * kRowBytes;  // K rows, V rows: 8 KB
-constexpr int kLaRows = 8;                               // query rows per kv head: the 8-wide N tile
 constexpr int kLaCtasPerSm = 2;
 constexpr int kLaBoxBytes = kLaSlice * 128;              // one copy: 16 rows x 64 channels
 
@@ -51,7 +50,9 @@ struct LayerAttnParams {
   const char* v_new;
   float* part_o;   // [(team + sequence)][warp][n_q_heads][128]
   float* part_ml;  // [(team + sequence)][warp][n_q_heads][2]
-  float* scores;   // [unit][n_kv_heads][kLaUnit][nq], null unless weights are gathered
+  float* scores;   // [sequence][unit of the sequence][n_kv_heads][kLaUnit][nq], null unless weights are gathered
+  float* lse2;     // [batch][n_q_heads] log-sum-exps in log2 units for the weights' kernel
+  int seq_units;   // units of the longest sequence
   int nq, n_q_heads;
   int team_size, n_teams;
   int flags;
@@ -101,12 +102,14 @@ __device__ __forceinline__ Seq seq_of(const LayerAttnParams& p, int b) {
 }
 
 // Exclusive prefix of the sequences' unit counts in shared memory: pre[batch] = all units.  Every thread calls it.
-__device__ __forceinline__ void unit_prefix(const LayerAttnParams& p, int* pre, int n_threads, int& bad) {
+// `keep` (may be null): the sequences themselves.
+__device__ __forceinline__ void unit_prefix(const LayerAttnParams& p, int* pre, int n_threads, int& bad, Seq* keep = nullptr) {
   const int tid = threadIdx.x, lane = tid & 31;
   for (int b = tid; b < p.g.batch; b += n_threads) {
     const Seq s = seq_of(p, b);
     bad |= s.bad ? 1 : 0;
     pre[b + 1] = s.u;
+    if (keep != nullptr) keep[b] = s;
   }
   __syncthreads();
   if (tid < 32) {
@@ -146,7 +149,7 @@ __device__ __forceinline__ int live_teams(const LayerAttnParams& p, int n_units)
 struct Slice {
   int meta;  // flags | sequence << 5 | kv head << 14
   int t0;    // first token
-  int x;     // unit (global)
+  int x;     // unit: sequence * seq_units + unit of the sequence
   int page;  // raw page id (looked at only when the slice's turn is near)
 };
 enum { kSlTokens = 1, kSlLoad = 2, kSlFirst = 4, kSlLast = 8, kSlBadSlot = 16 };
@@ -169,7 +172,8 @@ layer_attn_split_kernel(const __grid_constant__ LayerAttnParams p, const __grid_
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   int* pos_s = reinterpret_cast<int*>(smem + kLaWarps * kLaStages * kLaStageBytes);     // [warps][stages][16]
   uint64_t* bars = reinterpret_cast<uint64_t*>(pos_s + kLaWarps * kLaStages * kLaSlice);  // [warps][stages]
-  int* pre_s = reinterpret_cast<int*>(bars + kLaWarps * kLaStages);                     // [batch + 1]
+  Seq* seq_s = reinterpret_cast<Seq*>(bars + kLaWarps * kLaStages);                     // [batch]
+  int* pre_s = reinterpret_cast<int*>(seq_s + p.g.batch);                               // [batch + 1]
   volatile int* s_abort = pre_s + p.g.batch + 1;
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -190,7 +194,7 @@ layer_attn_split_kernel(const __grid_constant__ LayerAttnParams p, const __grid_
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   int bad = 0;
-  unit_prefix(p, pre_s, kLaThreads, bad);  // (ends with a barrier)
+  unit_prefix(p, pre_s, kLaThreads, bad, seq_s);  // (ends with a barrier)
   const int n_units = pre_s[p.g.batch];
   const int teams = live_teams(p, n_units);
   const int team = blockIdx.x / p.team_size, member = blockIdx.x % p.team_size;
@@ -210,10 +214,11 @@ layer_attn_split_kernel(const __grid_constant__ LayerAttnParams p, const __grid_
     if (i >= n_slices) return s;
     const int hd = n_heads == 1 ? 0 : i / nx, rem = i - hd * nx;
     const int head = member + hd * p.team_size;
-    s.x = x_begin + rem;
-    const int b = seq_of_unit(pre_s, p.g.batch, s.x);
-    const Seq q = seq_of(p, b);
-    const int k = s.x - pre_s[b];
+    const int x = x_begin + rem;
+    const int b = seq_of_unit(pre_s, p.g.batch, x);
+    const Seq& q = seq_s[b];
+    const int k = x - pre_s[b];
+    s.x = b * p.seq_units + k;
     s.t0 = (k < q.ua ? k : q.ub0 + k - q.ua) * kLaUnit + warp * kLaSlice;
     // (without a positions pool a slice that holds no visible token, nor the row to append, is left out)
     const bool wanted = p.positions != nullptr || s.t0 < q.a || (s.t0 + kLaSlice > q.lo && s.t0 < q.hi) ||
@@ -221,8 +226,8 @@ layer_attn_split_kernel(const __grid_constant__ LayerAttnParams p, const __grid_
     int fl = 0;
     if (wanted && s.t0 < q.n_tot) fl |= kSlTokens;
     if (wanted && s.t0 < q.n) fl |= kSlLoad;
-    if (s.x == x_begin || k == 0) fl |= kSlFirst;
-    if (s.x + 1 == x_end || k + 1 == q.u) fl |= kSlLast;
+    if (x == x_begin || k == 0) fl |= kSlFirst;
+    if (x + 1 == x_end || k + 1 == q.u) fl |= kSlLast;
     if ((fl & kSlLoad) || ((fl & kSlTokens) && (p.flags & MC_LAYER_APPEND))) {
       const int slot = s.t0 >> shift;
       if (slot < p.g.max_pages_per_seq) s.page = p.g.block_table[(size_t)b * p.g.max_pages_per_seq + slot];
@@ -242,7 +247,6 @@ layer_attn_split_kernel(const __grid_constant__ LayerAttnParams p, const __grid_
     if ((s.meta & kSlBadSlot) || !page_ok(p.g, s.page)) atomicOr(p.status, MC_FLAG_BAD_METADATA);
     return slice_row(s.page, s.meta >> 14, s.t0);
   };
-  // (both windows before the stream begins: the lengths that load_slice looks at would take microseconds behind it)
   Slice win = load_slice(lane), nxt = load_slice(32 + lane);
 
   auto load_q = [&](int b, int head, uint32_t (&q0)[8], uint32_t (&q2)[8]) {
@@ -311,7 +315,7 @@ layer_attn_split_kernel(const __grid_constant__ LayerAttnParams p, const __grid_
       for (int j = 0; j < 8; ++j)
 #pragma unroll
         for (int k = 0; k < 4; ++k) acc[j][k] = 0.f;
-      sq = seq_of(p, b);
+      sq = seq_s[b];
       // what this piece will read late and the next piece first goes to L1 meanwhile (a demand load takes microseconds
       // behind the stream): the step's new rows, the next piece's queries
       if (p.k_new && lane < 4) {
@@ -520,22 +524,19 @@ layer_attn_split_kernel(const __grid_constant__ LayerAttnParams p, const __grid_
   }
 }
 
-// Joins a sequence's pieces (consecutive teams): out = sum_j 2^(m_j - M) o_j / sum_j 2^(m_j - M) l_j.  Blocks
-// [0, combine_x): R query heads each (8: a warp per output row; 1: the eight warps share one row's pieces).  Blocks
-// behind them (calls that gather weights): w_i += sum over the head group of 2^(s_i - lse) for 1024 tokens of one kv
-// head, from the scores the split kernel left; they work the log-sum-exps out themselves, so one launch does both.
+// Joins a sequence's pieces (consecutive teams, a part per warp of their CTAs):
+// out = sum_j 2^(m_j - M) o_j / sum_j 2^(m_j - M) l_j.  A block has R query heads, 8 / R warps each: about three parts per
+// warp, so that a warp's loads travel together.
 constexpr int kLcThreads = 256;
 constexpr int kLcWarps = kLcThreads / 32;
-constexpr int kLcUnits = 16;  // units per weight block: 1024 tokens
 
 template <int DT, int R>
 __global__ void __launch_bounds__(kLcThreads) layer_attn_combine_kernel(const __grid_constant__ LayerAttnParams p, unsigned short* out,
-                                                                        float* lse, int combine_x) {
+                                                                        float* lse) {
   grid_dep_launch();
   __shared__ int pre_s[kMaxLayerBatch + 1];
   __shared__ float4 acc_s[kLcWarps][32];
   __shared__ float red_s[kLcWarps];
-  __shared__ float lse_s[kLaRows];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int b = blockIdx.y;
   int bad = 0;
@@ -546,81 +547,6 @@ __global__ void __launch_bounds__(kLcThreads) layer_attn_combine_kernel(const __
   // the team of unit x is the last c with floor(U c / T) <= x
   const int c0 = u > 0 ? (int)(((long long)(x0 + 1) * T - 1) / U) : 0;
   const int c1 = u > 0 ? (int)(((long long)(x0 + u) * T - 1) / U) : -1;
-  if ((int)blockIdx.x >= combine_x) {
-    const int per_head = ((int)gridDim.x - combine_x) / p.g.n_kv_heads;
-    const int j = (int)blockIdx.x - combine_x, head = j / per_head, k0 = (j % per_head) * kLcUnits;
-    if (k0 >= u) return;
-    const Seq sq = seq_of(p, b);
-    const int k1 = min(k0 + kLcUnits, u);
-    // A thread owns four tokens.  Where their weights live follows from the caller's tables (before the wait); scores,
-    // old weights and the partial sums are then requested together.
-    constexpr int kOwn = kLcUnits * kLaUnit / kLcThreads;
-    int at[kOwn], from[kOwn];
-    bool fresh[kOwn];
-#pragma unroll
-    for (int j = 0; j < kOwn; ++j) {
-      const int i = tid + j * kLcThreads, k = k0 + i / kLaUnit, in = i % kLaUnit;
-      const int t = (k < sq.ua ? k : sq.ub0 + k - sq.ua) * kLaUnit + in, slot = t >> p.g.page_shift;
-      fresh[j] = t == sq.n;  // the appended row: its weight begins here
-      at[j] = -1;
-      from[j] = -1;
-      if (k >= k1 || t >= sq.n_tot || slot >= p.g.max_pages_per_seq || (fresh[j] && !(p.flags & MC_LAYER_APPEND))) continue;
-      const bool seen = p.positions != nullptr || t < sq.a || (t >= sq.lo && t < sq.hi);
-      if (!seen && !fresh[j]) continue;  // (no score was written)
-      const int page = p.g.block_table[(size_t)b * p.g.max_pages_per_seq + slot];
-      if (!page_ok(p.g, page)) continue;  // (flagged by the split kernel)
-      at[j] = (page * p.g.n_kv_heads + head) * p.g.page_size + (t & (p.g.page_size - 1));
-      if (seen) from[j] = ((x0 + k) * p.g.n_kv_heads + head) * kLaUnit + in;
-    }
-    grid_dep_wait();
-    float s[kOwn][kLaRows], w[kOwn];
-#pragma unroll
-    for (int j = 0; j < kOwn; ++j) {
-      w[j] = at[j] >= 0 && !fresh[j] ? p.weights[at[j]] : 0.f;
-      const float* src = p.scores + (size_t)max(from[j], 0) * p.nq;
-#pragma unroll
-      for (int r = 0; r < kLaRows; r += 4) {
-        if ((p.nq & 3) == 0) {
-          const float4 v = from[j] >= 0 && r < p.nq ? *reinterpret_cast<const float4*>(src + r) : make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
-          s[j][r] = v.x;
-          s[j][r + 1] = v.y;
-          s[j][r + 2] = v.z;
-          s[j][r + 3] = v.w;
-        } else {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) s[j][r + e] = from[j] >= 0 && r + e < p.nq ? src[r + e] : -INFINITY;
-        }
-      }
-    }
-    for (int r = warp; r < p.nq; r += kLcWarps) {
-      float m = -INFINITY, l = 0.f;
-      for (int c = c0 * kLaWarps + lane; c < (c1 + 1) * kLaWarps; c += 32) {
-        const float2 v = *reinterpret_cast<const float2*>(p.part_ml + 2 * ((size_t)(c + b * kLaWarps) * p.n_q_heads + head * p.nq + r));
-        const float M = fmaxf(m, v.x);
-        l = (l == 0.f ? 0.f : l * ex2(m - M)) + (v.y == 0.f ? 0.f : v.y * ex2(v.x - M));
-        m = M;
-      }
-#pragma unroll
-      for (int o = 16; o; o >>= 1) {
-        const float m2 = __shfl_xor_sync(0xffffffffu, m, o), l2 = __shfl_xor_sync(0xffffffffu, l, o);
-        const float M = fmaxf(m, m2);
-        l = (l == 0.f ? 0.f : l * ex2(m - M)) + (l2 == 0.f ? 0.f : l2 * ex2(m2 - M));
-        m = M;
-      }
-      if (lane == 0) lse_s[r] = l == 0.f ? INFINITY : m + log2f(l);  // (a row that saw nothing gives nothing)
-    }
-    __syncthreads();
-#pragma unroll
-    for (int j = 0; j < kOwn; ++j) {
-      if (at[j] < 0) continue;
-      float sum = 0.f;
-#pragma unroll
-      for (int r = 0; r < kLaRows; ++r)
-        if (r < p.nq) sum += ex2(s[j][r] - lse_s[r]);
-      p.weights[at[j]] = w[j] + sum;
-    }
-    return;
-  }
   constexpr int GP = kLcWarps / R;  // warps per output row
   const int grp = warp % GP;
   const int hq = blockIdx.x * R + warp / GP;
@@ -700,7 +626,73 @@ __global__ void __launch_bounds__(kLcThreads) layer_attn_combine_kernel(const __
   packed.x = Elem<DT>::pack(o.x * inv, o.y * inv);
   packed.y = Elem<DT>::pack(o.z * inv, o.w * inv);
   *reinterpret_cast<uint2*>(out + orow * kHeadDim + lane * 4) = packed;
-  if (lse != nullptr && lane == 0) lse[orow] = L == 0.f ? -INFINITY : (M + log2f(L)) * kLn2;
+  if (lane == 0) {
+    const float z = L == 0.f ? -INFINITY : M + log2f(L);
+    if (lse != nullptr) lse[orow] = z * kLn2;
+    if (p.scores != nullptr) p.lse2[orow] = L == 0.f ? INFINITY : z;  // (a row that saw nothing gives no weight)
+  }
+}
+
+// w_i += sum over the head group of 2^(s_i - lse), from the scores the split kernel left: a block has 1024 tokens of one
+// kv head, a thread four of them.  Where their weights live follows from the caller's tables (before the wait); scores,
+// old weights and log-sum-exps are then requested together.  (Inside the combine kernel, each block joining the partial
+// sums for itself, this took 19 us on 4 x 32768 tokens.)
+constexpr int kLwTokens = 1024;
+
+template <int NQ>
+__global__ void __launch_bounds__(kLcThreads) layer_attn_weights_kernel(const __grid_constant__ LayerAttnParams p, int chunks) {
+  grid_dep_launch();
+  const int tid = threadIdx.x, b = blockIdx.y, head = blockIdx.x / chunks, k0 = (blockIdx.x % chunks) * (kLwTokens / kLaUnit);
+  const Seq sq = seq_of(p, b);
+  constexpr int kOwn = kLwTokens / kLcThreads;
+  int at[kOwn];
+  long long from[kOwn];  // (past 32 bits in a long batch)
+  bool fresh[kOwn];
+#pragma unroll
+  for (int j = 0; j < kOwn; ++j) {
+    const int i = tid + j * kLcThreads, k = k0 + i / kLaUnit, in = i % kLaUnit;
+    const int t = (k < sq.ua ? k : sq.ub0 + k - sq.ua) * kLaUnit + in, slot = t >> p.g.page_shift;
+    fresh[j] = t == sq.n;  // the appended row: its weight begins here
+    at[j] = -1;
+    from[j] = -1;
+    if (k >= sq.u || t >= sq.n_tot || slot >= p.g.max_pages_per_seq || (fresh[j] && !(p.flags & MC_LAYER_APPEND))) continue;
+    const bool seen = p.positions != nullptr || t < sq.a || (t >= sq.lo && t < sq.hi);
+    if (!seen && !fresh[j]) continue;  // (no score was written)
+    const int page = p.g.block_table[(size_t)b * p.g.max_pages_per_seq + slot];
+    if (!page_ok(p.g, page)) continue;  // (flagged by the split kernel)
+    at[j] = (page * p.g.n_kv_heads + head) * p.g.page_size + (t & (p.g.page_size - 1));
+    if (seen) from[j] = ((long long)(b * p.seq_units + k) * p.g.n_kv_heads + head) * kLaUnit + in;
+  }
+  grid_dep_wait();
+  float s[kOwn][NQ], w[kOwn], z[NQ];
+#pragma unroll
+  for (int r = 0; r < NQ; ++r) z[r] = p.lse2[(size_t)b * p.n_q_heads + head * NQ + r];
+#pragma unroll
+  for (int j = 0; j < kOwn; ++j) {
+    w[j] = at[j] >= 0 && !fresh[j] ? p.weights[at[j]] : 0.f;
+    const float* src = p.scores + (size_t)max(from[j], 0LL) * NQ;
+    if (NQ % 4 == 0) {
+#pragma unroll
+      for (int r = 0; r < NQ; r += 4) {
+        const float4 v = from[j] >= 0 ? *reinterpret_cast<const float4*>(src + r) : make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+        s[j][r] = v.x;
+        s[j][(r + 1) % NQ] = v.y;
+        s[j][(r + 2) % NQ] = v.z;
+        s[j][(r + 3) % NQ] = v.w;
+      }
+    } else {
+#pragma unroll
+      for (int r = 0; r < NQ; ++r) s[j][r] = from[j] >= 0 ? src[r] : -INFINITY;
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < kOwn; ++j) {
+    if (at[j] < 0) continue;
+    float sum = 0.f;
+#pragma unroll
+    for (int r = 0; r < NQ; ++r) sum += ex2(s[j][r] - z[r]);
+    p.weights[at[j]] = w[j] + sum;
+  }
 }
 
 // ---- host side ------------------------------------------------------------------------------------
@@ -708,7 +700,7 @@ struct LayerAttnPlan {
   int team_size, n_teams;
   long long max_units;  // of the batch
   int seq_units;        // of the longest sequence
-  size_t o_bytes, ml_bytes, score_bytes;
+  size_t o_bytes, ml_bytes, score_bytes, lse_bytes;
 };
 // n_sm: multiprocessors of the device; the workspace is sized for kLaMaxCtas / kLaCtasPerSm of them, so that its size
 // needs no device.
@@ -725,11 +717,12 @@ static LayerAttnPlan layer_attn_plan(const mc_config* cfg, const mc_batch* bt, i
   pl.o_bytes = align_up(prow * kHeadDim * 4, 256);
   pl.ml_bytes = align_up(prow * 2 * 4, 256);
   pl.score_bytes = (flags & MC_LAYER_ACCUMULATE) ? align_up((size_t)pl.max_units * kLaUnit * cfg->n_q_heads * 4, 256) : 0;
+  pl.lse_bytes = (flags & MC_LAYER_ACCUMULATE) ? align_up((size_t)bt->batch * cfg->n_q_heads * 4, 256) : 0;
   return pl;
 }
 size_t layer_attn_workspace_bytes(const mc_config* cfg, const mc_batch* bt, int flags) {
   const LayerAttnPlan pl = layer_attn_plan(cfg, bt, flags, kLaMaxCtas / kLaCtasPerSm);
-  return pl.o_bytes + pl.ml_bytes + pl.score_bytes;
+  return pl.o_bytes + pl.ml_bytes + pl.score_bytes + pl.lse_bytes;
 }
 
 mc_status launch_layer_attn(const mc_config* cfg, const mc_batch* bt, const Geom& g, const mc_layer_cache* layer,
@@ -757,6 +750,8 @@ mc_status launch_layer_attn(const mc_config* cfg, const mc_batch* bt, const Geom
   ap.part_o = (float*)workspace;
   ap.part_ml = (float*)((char*)workspace + pl.o_bytes);
   ap.scores = (flags & MC_LAYER_ACCUMULATE) ? (float*)((char*)workspace + pl.o_bytes + pl.ml_bytes) : nullptr;
+  ap.lse2 = (float*)((char*)workspace + pl.o_bytes + pl.ml_bytes + pl.score_bytes);
+  ap.seq_units = pl.seq_units;
   ap.nq = cfg->n_q_heads / cfg->n_kv_heads;
   ap.n_q_heads = cfg->n_q_heads;
   ap.team_size = pl.team_size;
@@ -765,18 +760,31 @@ mc_status launch_layer_attn(const mc_config* cfg, const mc_batch* bt, const Geom
   // (asked for so much that two CTAs fill an SM: with room for a third, an early start behind another kernel packs some
   // SMs with three and leaves others with one -- 83 -> 86 us on 8 x 4096)
   const size_t smem = std::max<size_t>(80 * 1024, 1024 + (size_t)kLaWarps * kLaStages * (kLaStageBytes + kLaSlice * 4 + 8) +
-                                                      (size_t)(bt->batch + 2) * 4);
+                                                      (size_t)(bt->batch + 2) * (4 + sizeof(Seq)));
   auto* split = cfg->dtype == MC_F16 ? layer_attn_split_kernel<MC_F16> : layer_attn_split_kernel<MC_BF16>;
   MC_CUDA_CHECK(cudaFuncSetAttribute(split, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
   MC_CUDA_CHECK(launch_pdl(split, dim3(pl.n_teams * pl.team_size), dim3(kLaThreads), smem, stream, ap, map_k, map_v));
-  // many output rows: a warp per row; few: a block per row
-  const bool warp_rows = (long long)bt->batch * cfg->n_q_heads >= 1024;
-  const int combine_x = warp_rows ? (cfg->n_q_heads + kLcWarps - 1) / kLcWarps : cfg->n_q_heads;
-  const int weight_x = (flags & MC_LAYER_ACCUMULATE) ? cfg->n_kv_heads * ((pl.seq_units + kLcUnits - 1) / kLcUnits) : 0;
-  auto* combine = cfg->dtype == MC_F16 ? (warp_rows ? layer_attn_combine_kernel<MC_F16, kLcWarps> : layer_attn_combine_kernel<MC_F16, 1>)
-                                       : (warp_rows ? layer_attn_combine_kernel<MC_BF16, kLcWarps> : layer_attn_combine_kernel<MC_BF16, 1>);
-  MC_CUDA_CHECK(launch_pdl(combine, dim3(combine_x + weight_x, bt->batch), dim3(kLcThreads), 0, stream, ap, (unsigned short*)out, lse,
-                           combine_x));
+  // warps per output row: about three parts each
+  const long long parts = (long long)kLaWarps * (pl.n_teams / bt->batch + 1);
+  int per_block = kLcWarps;  // rows
+  while (per_block > 1 && parts > 3 * (kLcWarps / per_block)) per_block /= 2;
+  using Combine = void (*)(const LayerAttnParams, unsigned short*, float*);
+  static const Combine combines[2][4] = {
+      {layer_attn_combine_kernel<MC_F16, 1>, layer_attn_combine_kernel<MC_F16, 2>, layer_attn_combine_kernel<MC_F16, 4>,
+       layer_attn_combine_kernel<MC_F16, 8>},
+      {layer_attn_combine_kernel<MC_BF16, 1>, layer_attn_combine_kernel<MC_BF16, 2>, layer_attn_combine_kernel<MC_BF16, 4>,
+       layer_attn_combine_kernel<MC_BF16, 8>}};
+  const Combine combine = combines[cfg->dtype == MC_F16 ? 0 : 1][per_block == 1 ? 0 : per_block == 2 ? 1 : per_block == 4 ? 2 : 3];
+  MC_CUDA_CHECK(launch_pdl(combine, dim3((cfg->n_q_heads + per_block - 1) / per_block, bt->batch), dim3(kLcThreads), 0, stream, ap,
+                           (unsigned short*)out, lse));
+  if (flags & MC_LAYER_ACCUMULATE) {
+    const int chunks = (pl.seq_units * kLaUnit + kLwTokens - 1) / kLwTokens;
+    auto* weights = ap.nq == 1   ? layer_attn_weights_kernel<1>
+                    : ap.nq == 2 ? layer_attn_weights_kernel<2>
+                    : ap.nq == 4 ? layer_attn_weights_kernel<4>
+                                 : layer_attn_weights_kernel<8>;
+    MC_CUDA_CHECK(launch_pdl(weights, dim3(cfg->n_kv_heads * chunks, bt->batch), dim3(kLcThreads), 0, stream, ap, chunks));
+  }
   MC_CUDA_CHECK(cudaGetLastError());
   return MC_OK;
 }

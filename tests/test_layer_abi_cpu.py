@@ -121,7 +121,7 @@ def test_workspace_bytes(lib):
     assert plain > 0 and plain % 256 == 0
     # gathering weights keeps the scores: 4 bytes per (token, query head), whole units of 64 tokens
     for n, held in ((63, 64), (64, 128), (127, 128), (128, 192)):  # (the step's token counts)
-        assert need(batch(max_len=n, mpps=9), 2, 3) - need(batch(max_len=n, mpps=9), 2, 1) == 2 * held * 32 * 4
+        assert need(batch(max_len=n, mpps=9), 2, 3) - need(batch(max_len=n, mpps=9), 2, 1) == (2 * held + 2) * 32 * 4  # (and the rows' log-sum-exps)
     assert need(batch(), 2, 4) == -1 and need(batch(), 9, 0) == -1 and need(batch(), 0, 0) == -1
     assert need(batch(), 2, 0, cfg(page_size=8)) == -2
     assert need(batch(), 4, 0) >= 2 * 8 * 64 * 4 and need(batch(), 4, 1) == -1
