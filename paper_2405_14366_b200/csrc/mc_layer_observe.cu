@@ -273,6 +273,16 @@ layer_observe_kernel(const __grid_constant__ ObserveParams p, const __grid_const
     }
   }
 
+  if (PASS == 1 && n_x > 0) {
+    // a group without a tile in one of the CTA's segments leaves no part of it: cleared here (consecutive parts)
+    ObCursor a, z;
+    a.seek(pre_s, p.g.batch, H, x_begin);
+    z.seek(pre_s, p.g.batch, H, x_begin + n_x - 1);
+    const size_t per = (size_t)p.rows * p.slots * 2, lo = (size_t)(cta + a.b * H + a.g) * per, hi = (size_t)(cta + z.b * H + z.g + 1) * per;
+    for (size_t i = lo + tid; i < hi; i += kObThreads) p.part_ml[i] = 0.f;
+    __syncthreads();
+  }
+
   // the step from tile to tile; `seg` tells that the next tile begins another segment
   auto advance = [&](ObCursor& c, int x) {
     c.k += DIR;
@@ -452,20 +462,29 @@ layer_observe_kernel(const __grid_constant__ ObserveParams p, const __grid_const
         if (gl < n_rows) {
           const int r = row0 + gl;
           float mm = -INFINITY, ll = 0.f;
-          for (int cc = c0; cc <= c1; ++cc) {
-            // tiles [i0, i1) of that CTA lie in the segment; a group has a part if one of them is its own
-            const long long xb = U * cc / T, xe = U * (cc + 1) / T;
-            const int i0 = (int)(max(x0, xb) - xb), i1 = (int)(min(x0 + c.u, xe) - xb);
-            const float2* q = reinterpret_cast<const float2*>(p.part_ml) + ((size_t)(cc + c.b * H + c.g) * p.rows + r) * p.slots;
-            const int s1 = 4 / p.v1;  // pass 1: tiles from one of a group's units to its next
-            for (int k = 0; k < p.slots; ++k) {
-              const int first1 = (p.nt == 1 ? k / p.v1 : (kObHalves == 2 ? 0 : k)) - i0;
-              if (i0 + (first1 & (s1 - 1)) >= i1) continue;
-              const float2 v = q[k];
-              const float M = fmaxf(mm, v.x);
-              ll = (ll == 0.f ? 0.f : ll * ex2(mm - M)) + (v.y == 0.f ? 0.f : v.y * ex2(v.x - M));
-              mm = M;
+          auto take = [&](float m2, float l2) {
+            if (l2 == 0.f) return;
+            const float M = fmaxf(mm, m2);
+            ll = (ll == 0.f ? 0.f : ll * ex2(mm - M)) + l2 * ex2(m2 - M);
+            mm = M;
+          };
+          for (int cc = c0; cc <= c1; cc += 4) {  // the parts of four CTAs in flight
+            float4 q[4][2];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              q[e][0] = q[e][1] = make_float4(0.f, 0.f, 0.f, 0.f);
+              if (cc + e > c1) continue;
+              const float4* s4 = reinterpret_cast<const float4*>(p.part_ml + ((size_t)(cc + e + c.b * H + c.g) * p.rows + r) * p.slots * 2);
+              q[e][0] = s4[0];
+              if (p.slots == 4) q[e][1] = s4[1];
             }
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+              for (int k = 0; k < 2; ++k) {
+                take(q[e][k].x, q[e][k].y);
+                take(q[e][k].z, q[e][k].w);
+              }
           }
           row_g[gl] = ll == 0.f ? -INFINITY : -(mm + log2f(ll));  // (a row that saw nothing gives nothing)
           row_g[kObTile + gl] = p.rule.slopes ? p.rule.slopes[c.g * p.nq + r % p.nq] * kLog2e : 0.f;
@@ -503,22 +522,13 @@ layer_observe_kernel(const __grid_constant__ ObserveParams p, const __grid_const
       }
       const int t0 = (c.k < ua ? c.k : c.k + skip) * kObTile;
       const bool easy = t0 <= easy_hi && (t0 <= easy_pre || t0 >= easy_lo);
-      // this thread's token: position, and in pass 2 where its weight goes
+      // this thread's token: its page is asked for now; what follows from it, its position and (pass 2) where its weight
+      // goes, is looked at only when needed: the load takes microseconds behind the stream of keys
       const int t = t0 + gl;
       int pos = t < n ? t : kObNoToken;
-      float* dst = nullptr;
-      float w_old = 0.f;
-      if ((PASS == 2 || !easy) && t < n) {
-        const int page = table[t >> shift];
-        if (page_ok(p.g, page)) {
-          const int at = (page * H + c.g) * ps + (t & (ps - 1));
-          if (PASS == 2) {
-            dst = p.weights + at;
-            if (p.add && v == 0) w_old = *dst;
-          }
-          if (p.positions) pos = p.positions[at];
-        }
-      }
+      const int page = (PASS == 2 || !easy) && t < n ? table[t >> shift] : -1;
+      const int at = (page * H + c.g) * ps + (t & (ps - 1));
+      if (p.positions && page_ok(p.g, page)) pos = p.positions[at];
       if (PASS == 1 && !easy) {
         group_sync(grp);
         pos_g[gl] = pos;
@@ -637,7 +647,7 @@ layer_observe_kernel(const __grid_constant__ ObserveParams p, const __grid_const
           if (v == 0)
             for (int k = 1; k < V; ++k) w += part[k * kObTile];
         }
-        if (dst && v == 0) *dst = w_old + w;
+        if (v == 0 && page_ok(p.g, page)) p.weights[at] = (p.add ? p.weights[at] : 0.f) + w;
       }
     }
     if (PASS == 1 && c.b >= 0) end_segment();
