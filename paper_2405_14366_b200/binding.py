@@ -686,20 +686,23 @@ class MiniCacheLib:
         """q [batch][n_obs][n_q_heads][128]: the last n_obs queries of every sequence; flags: 0 (weights are written) or
         MC_LAYER_ACCUMULATE (added to)."""
         c, b = _cfg_c(cfg), batch.c()
-        assert q.dim() == 4 and tuple(q.shape) == (b.batch, q.shape[1], cfg.n_q_heads, 128), "q: [batch][n_obs][n_q_heads][128]"
+        shape = q.shape
+        assert len(shape) == 4 and shape[0] == b.batch and shape[2] == cfg.n_q_heads and shape[3] == 128, "q: [batch][n_obs][n_q_heads][128]"
+        assert q.dtype is cfg.torch_dtype and q.is_contiguous(), "q: contiguous rows of the storage type are wanted"
         l, o = layer.c(b.n_pages), opts.c(cfg, b.batch)
-        self._check(self._lib.mc_layer_observe(C.byref(c), C.byref(b), C.byref(l), C.byref(o), _typed("q", q, cfg.torch_dtype),
-                                               int(q.shape[1]), int(flags), _ptr(workspace),
-                                               workspace.numel() * workspace.element_size(), _stream(stream)))
+        code = self._lib.mc_layer_observe(c, b, l, o, q.data_ptr(), shape[1], flags, workspace.data_ptr(), workspace.nbytes, _stream(stream))
+        if code:
+            self._check(code)
 
     def mc_layer_evict(self, cfg: McConfig, batch: Batch, layer: LayerCache, opts: EvictOpts, new_lens: torch.Tensor,
                        workspace: torch.Tensor, stream=None):
         """new_lens int32 [batch] receives min(seq_lens, budget); it must not share memory with batch.seq_lens."""
         c, b = _cfg_c(cfg), batch.c()
-        assert new_lens.numel() == b.batch
+        assert new_lens.dtype is torch.int32 and new_lens.numel() == b.batch and new_lens.is_contiguous(), "new_lens: int32 [batch]"
         l, o = layer.c(b.n_pages), opts.c(b.batch)
-        self._check(self._lib.mc_layer_evict(C.byref(c), C.byref(b), C.byref(l), C.byref(o), _typed("new_lens", new_lens, torch.int32),
-                                             _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream)))
+        code = self._lib.mc_layer_evict(c, b, l, o, new_lens.data_ptr(), workspace.data_ptr(), workspace.nbytes, _stream(stream))
+        if code:
+            self._check(code)
 
     def mc_layer_read_status(self, layer: LayerCache, stream=None, check: bool = True):
         words = (C.c_int32 * MC_STATUS_WORDS)()

@@ -13,8 +13,9 @@
 // R rows (4 R bytes per token) are more to store and fetch than the key row (256 bytes).  Pass 2 walks its tiles
 // backwards: the keys read last are the ones still in L2.
 //
-// One persistent CTA per SM; the tiles of all (sequence, kv head) segments are shared out equally.  Warp 0 streams K
-// tiles (a tiled copy per page and 64-channel half) and the segments' Q; warp 1 issues tcgen05.mma, four groups of four
+// One persistent CTA per SM; the tiles of all (sequence, kv head) segments are shared out equally.  The last two warps
+// stream K tiles (a tiled copy per page and 64-channel half; a warp issues one in about 120 cycles, sixteen per tile of
+// 16-token pages, so that one warp alone paced the stream at 4.6 TB/s), warp 0 the segments' Q; warp 1 issues tcgen05.mma, four groups of four
 // warps take the scores out.  A unit is 64 columns of a tile's scores (pass 1: 64 tokens, pass 2: 64 rows); the units of
 // a tile go to 1, 2 or 4 groups, and every group has two tensor-memory buffers, so that its next unit is multiplied
 // while it works on this one.  Bounds: the keys' bytes, twice, and the 2 R exponentials per token (16 a clock and SM),
@@ -40,7 +41,8 @@ constexpr int kObGroupBufs = 512 / (kObGroups * kObUnit);
 constexpr int kObBufs = kObGroupBufs * kObGroups;
 constexpr int kObHalves = kObTile / kObUnit;             // pass 1: units per tile and row tile
 constexpr int kObChunk = 16;                             // columns in registers at a time (a row copy's share at least)
-constexpr int kObThreads = 64 + kObGroups * 128;         // producer, tensor-core issue, the groups
+constexpr int kObProducers = 2;                          // warps that copy K tiles, in turn
+constexpr int kObThreads = 64 + kObGroups * 128 + 32 * kObProducers;  // Q copies, tensor-core issue, the groups, K copies
 constexpr int kObQBufs = 2;
 constexpr int kObMaxStages = 4;
 constexpr int kObNoToken = 0x7fffffff;                   // position of a tile's rows behind the sequence: never seen
@@ -291,13 +293,37 @@ layer_observe_kernel(const __grid_constant__ ObserveParams p, const __grid_const
   auto last_of_seg = [&](const ObCursor& c, int i) { return i + 1 == n_x || (DIR > 0 ? c.k + 1 == c.u : c.k == 0); };
 
   if (warp == 0) {
-    // ===================== producer =====================
+    // ===================== Q of the segments =====================
+    ObCursor c;
+    if (n_x > 0) c.seek(pre_s, p.g.batch, H, x_first);
+    int seg = 0;
+    for (int i = 0; i < n_x;) {
+      const int qb = seg & 1;
+      bool ok = true;
+      if (seg >= 2) ok = __all_sync(0xffffffffu, mbar_wait_lean(qempty0 + 8 * qb, ((seg >> 1) - 1) & 1, s_abort, p.status));
+      if (!ok) break;
+      if (lane == 0) {
+        const uint32_t bar = qfull0 + 8 * qb, dst = sq0 + qb * q_bytes;
+        mbar_expect_tx(bar, (uint32_t)(2 * p.nt * p.rep * p.jt * p.nq * 128));
+        for (int tt = 0; tt < p.nt; ++tt)
+          for (int r = 0; r < p.rep; ++r)
+            for (int h = 0; h < 2; ++h)
+              tma_load_3d(dst + h * q_half + (tt * kObTile + r * p.rp) * 128, &map_q, 64 * h, c.g * p.nq, c.b * p.n_obs + tt * p.jt, bar);
+      }
+      __syncwarp();
+      ++seg;
+      i += DIR > 0 ? c.u - c.k : c.k + 1;  // the first tile of the next segment
+      if (i < n_x) c.seek(pre_s, p.g.batch, H, x_first + DIR * i);
+    }
+  } else if (warp >= 2 + 4 * kObGroups) {
+    // ===================== K tiles =====================
+    const int prod = warp - 2 - 4 * kObGroups;  // takes the tiles prod, prod + 2, ...
     // Rows of the pools where the pages of the next tiles begin, a lane per page, one window of 32 pages ahead: a load
-    // per tile would pace the stream by its latency .
+    // per tile would pace the stream by its latency.
     const int ppt = kObTile >> shift, lane_tile = lane >> (7 - shift), lane_page = lane & (ppt - 1);
     const int win_tiles = 32 >> (7 - shift);  // pages per tile: ppt; tiles per window
-    auto load_window = [&](int i0, int& head, bool& has) {
-      const int i = i0 + lane_tile;
+    auto load_window = [&](int k0, int& head, bool& has) {
+      const int i = (k0 + lane_tile) * kObProducers + prod;
       head = 0;
       has = false;
       if (i >= n_x) return 0;
@@ -312,33 +338,16 @@ layer_observe_kernel(const __grid_constant__ ObserveParams p, const __grid_const
     int head, head_n;
     bool has, has_n;
     int page = load_window(0, head, has), page_n = load_window(win_tiles, head_n, has_n);
-    ObCursor c;
-    if (n_x > 0) c.seek(pre_s, p.g.batch, H, x_first);
-    bool first = true, ok = true;
-    int seg = 0;
-    for (int i = 0; i < n_x && ok; ++i) {
-      const int in_win = i & (win_tiles - 1);
-      if (in_win == 0 && i > 0) {
+    for (int k = 0, i = prod; i < n_x; ++k, i += kObProducers) {
+      const int in_win = k & (win_tiles - 1);
+      if (in_win == 0 && k > 0) {
         page = page_n;
         head = head_n;
         has = has_n;
-        page_n = load_window(i + win_tiles, head_n, has_n);
-      }
-      if (first) {
-        const int qb = seg & 1;
-        if (seg >= 2) ok = __all_sync(0xffffffffu, mbar_wait_lean(qempty0 + 8 * qb, ((seg >> 1) - 1) & 1, s_abort, p.status));
-        if (!ok) break;
-        if (lane == 0) {
-          const uint32_t bar = qfull0 + 8 * qb, dst = sq0 + qb * q_bytes;
-          mbar_expect_tx(bar, (uint32_t)(2 * p.nt * p.rep * p.jt * p.nq * 128));
-          for (int tt = 0; tt < p.nt; ++tt)
-            for (int r = 0; r < p.rep; ++r)
-              for (int h = 0; h < 2; ++h)
-                tma_load_3d(dst + h * q_half + (tt * kObTile + r * p.rp) * 128, &map_q, 64 * h, c.g * p.nq, c.b * p.n_obs + tt * p.jt, bar);
-        }
-        __syncwarp();
+        page_n = load_window(k + win_tiles, head_n, has_n);
       }
       const int s = i & s_mask, lap = i >> p.stage_shift;
+      bool ok = true;
       if (lap > 0) ok = __all_sync(0xffffffffu, mbar_wait_lean(empty0 + 8 * s, (lap - 1) & 1, s_abort, p.status));
       if (!ok) break;
       const uint32_t bar = full0 + 8 * s, dst = sk0 + s * kObTileBytes;
@@ -358,9 +367,6 @@ layer_observe_kernel(const __grid_constant__ ObserveParams p, const __grid_const
         tma_load_2d(to + kObHalf, &map_k, 64, y, bar);
       }
       __syncwarp();
-      first = last_of_seg(c, i);
-      if (first) ++seg;
-      if (i + 1 < n_x) advance(c, x_first + DIR * (i + 1));
     }
   } else if (warp == 1) {
     // ===================== tensor-core issue =====================
