@@ -611,11 +611,14 @@ layer_observe_kernel(const __grid_constant__ ObserveParams p, const __grid_const
 #pragma unroll 1
         for (int r0 = 0; r0 < n_rows; r0 += kObChunk) {
           uint32_t raw[kObChunk];
-          tmem_load(tbuf + r0, raw);
+          tmem_ld16_async(tbuf + r0, raw);
+          ulonglong2 z2[kObChunk / 4];  // -log-sum-exps, on their way together with the scores
+#pragma unroll
+          for (int k = 0; k < kObChunk / 4; ++k) z2[k] = reinterpret_cast<const ulonglong2*>(row_g + r0)[k];
+          tmem_wait16(raw);
           uint64_t f[kObChunk / 2];
           factors<CAP>(p, raw, f);
           if (easy && r0 + kObChunk <= n_rows) {
-            const ulonglong2* z2 = reinterpret_cast<const ulonglong2*>(row_g + r0);
 #pragma unroll
             for (int k = 0; k < kObChunk; k += 4) {
               const ulonglong2 z = z2[k / 4];
