@@ -13,13 +13,13 @@
 // R rows (4 R bytes per token) are more to store and fetch than the key row (256 bytes).  Pass 2 walks its tiles
 // backwards: the keys read last are the ones still in L2.
 //
-// One persistent CTA per SM; the tiles of all (sequence, kv head) segments are shared out equally.  The last two warps
-// stream K tiles (a tiled copy per page and 64-channel half; a warp issues one in about 120 cycles, sixteen per tile of
-// 16-token pages, so that one warp alone paced the stream at 4.6 TB/s), warp 0 the segments' Q; warp 1 issues tcgen05.mma, four groups of four
-// warps take the scores out.  A unit is 64 columns of a tile's scores (pass 1: 64 tokens, pass 2: 64 rows); the units of
-// a tile go to 1, 2 or 4 groups, and every group has two tensor-memory buffers, so that its next unit is multiplied
-// while it works on this one.  Bounds: the keys' bytes, twice, and the 2 R exponentials per token (16 a clock and SM),
-// with the cap's polynomial on the FMA pipe next to them.  Every wait is bounded; tensor memory is released on every path.
+// One persistent CTA per SM; the tiles of all (sequence, kv head) segments are shared out equally.  The last warp streams
+// K tiles (a tiled copy per page and 64-channel half), warp 0 the segments' Q; four groups of four warps take the scores
+// out of tensor memory, each from a buffer of 128 columns of its own: up to 128 rows they take the tiles in turn, beyond
+// that two of them share a tile, one per 128 rows.  Two threads issue tcgen05.mma, each for two groups: with one, a
+// group that was late kept the others waiting for their next product.  Bounds: the keys' bytes, twice, and the 2 R
+// exponentials per token (16 a clock and SM), with the cap's polynomial on the FMA pipe next to them; in fact the groups
+// wait for latencies most of the time.  Every wait is bounded; tensor memory is released on every path.
 #include <math.h>
 
 #include <algorithm>
@@ -36,13 +36,8 @@ constexpr int kObTile = 128;                             // tokens per tile
 constexpr int kObHalf = kObTile * 128;                   // bytes of a tile's 64-channel half
 constexpr int kObTileBytes = 2 * kObHalf;                // 32 KB
 constexpr int kObGroups = 4;                             // groups of four warps that take scores out of tensor memory
-constexpr int kObUnit = 128;                             // columns a group takes at a time: a tensor-memory buffer
-constexpr int kObGroupBufs = 512 / (kObGroups * kObUnit);
-constexpr int kObBufs = kObGroupBufs * kObGroups;
-constexpr int kObHalves = kObTile / kObUnit;             // pass 1: units per tile and row tile
-constexpr int kObChunk = 16;                             // columns in registers at a time (a row copy's share at least)
-constexpr int kObProducers = 2;                          // warps that copy K tiles, in turn
-constexpr int kObThreads = 64 + kObGroups * 128 + 32 * kObProducers;  // Q copies, tensor-core issue, the groups, K copies
+constexpr int kObChunk = 16;                             // columns in registers at a time
+constexpr int kObThreads = 128 + kObGroups * 128;        // Q copies, tensor-core issue, the groups, tensor-core issue, K copies
 constexpr int kObQBufs = 2;
 constexpr int kObMaxStages = 4;
 constexpr int kObNoToken = 0x7fffffff;                   // position of a tile's rows behind the sequence: never seen
@@ -59,7 +54,6 @@ struct ObserveParams {
   int rows;      // n_obs * nq
   int nt;        // row tiles of 128: 1 or 2
   int slots;     // groups that share a row tile in pass 1: 4 / nt
-  int v1, v2;    // units per tile in pass 1 and pass 2: 1, 2 or 4
   int rp, rep;   // rows of a copy (32, 64 or 128), copies in a row tile
   int jt;        // queries per Q copy
   int stage_shift;  // K ring: 4 or 2 stages
@@ -126,7 +120,6 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map
 }
 __device__ __forceinline__ void group_sync(int grp) { asm volatile("bar.sync %0, 128;" ::"r"(1 + grp) : "memory"); }
 __device__ __forceinline__ void pair_sync(int pair) { asm volatile("bar.sync %0, 256;" ::"r"(1 + kObGroups + pair) : "memory"); }
-__device__ __forceinline__ void groups_sync() { asm volatile("bar.sync %0, 512;" ::"n"(3 + kObGroups) : "memory"); }
 
 __device__ __forceinline__ void tmem_load(uint32_t addr, uint32_t (&r)[32]) { tmem_ld32(addr, r); }
 __device__ __forceinline__ void tmem_load(uint32_t addr, uint32_t (&r)[16]) {
@@ -190,7 +183,7 @@ layer_observe_kernel(const __grid_constant__ ObserveParams p, const __grid_const
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   // barriers: K full / empty per stage, Q full / empty per buffer, accumulator full / empty per group
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + kObSmem);
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * kObMaxStages + 4 + 2 * kObBufs);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * kObMaxStages + 4 + 2 * kObGroups);
   volatile int* s_abort = reinterpret_cast<volatile int*>(tmem_slot + 1);
   float* row_s = reinterpret_cast<float*>(tmem_slot + 4);             // [groups][128][2]: pass 1 (m, l) of the lanes; pass 2 -lse, slope
   int* view_s = reinterpret_cast<int*>(row_s + kObGroups * kObTile * 2);  // [groups][2][128]: pass 2: position, lowest position seen
@@ -199,10 +192,10 @@ layer_observe_kernel(const __grid_constant__ ObserveParams p, const __grid_const
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int H = p.g.n_kv_heads, ps = p.g.page_size, shift = p.g.page_shift;
   const uint32_t full0 = smem_u32(bars), empty0 = full0 + 8 * kObMaxStages, qfull0 = empty0 + 8 * kObMaxStages, qempty0 = qfull0 + 16;
-  const uint32_t tfull0 = qempty0 + 16, tempty0 = tfull0 + 8 * kObBufs;
+  const uint32_t tfull0 = qempty0 + 16, tempty0 = tfull0 + 8 * kObGroups;
   const int q_bytes = p.nt * kObTileBytes, q_half = p.nt * kObHalf;
   const uint32_t sq0 = smem_u32(smem), sk0 = sq0 + kObQBufs * q_bytes;
-  constexpr uint32_t tmem_cols = kObBufs * kObUnit;
+  constexpr uint32_t tmem_cols = kObGroups * kObTile;
 
   int bad = 0;
   for (int b = tid; b < p.g.batch; b += kObThreads) {
@@ -213,13 +206,13 @@ layer_observe_kernel(const __grid_constant__ ObserveParams p, const __grid_const
   if (tid == 0) {
     for (int s = 0; s < kObMaxStages; ++s) {
       mbar_init(full0 + 8 * s, 1);
-      mbar_init(empty0 + 8 * s, 1);
+      mbar_init(empty0 + 8 * s, p.nt);  // both issuing threads read a tile that has two row tiles
     }
     for (int s = 0; s < 2; ++s) {
       mbar_init(qfull0 + 8 * s, 1);
-      mbar_init(qempty0 + 8 * s, 1);
+      mbar_init(qempty0 + 8 * s, 2);
     }
-    for (int s = 0; s < kObBufs; ++s) {
+    for (int s = 0; s < kObGroups; ++s) {
       mbar_init(tfull0 + 8 * s, 1);
       mbar_init(tempty0 + 8 * s, 4);
     }
@@ -315,15 +308,14 @@ layer_observe_kernel(const __grid_constant__ ObserveParams p, const __grid_const
       i += DIR > 0 ? c.u - c.k : c.k + 1;  // the first tile of the next segment
       if (i < n_x) c.seek(pre_s, p.g.batch, H, x_first + DIR * i);
     }
-  } else if (warp >= 2 + 4 * kObGroups) {
+  } else if (warp == 3 + 4 * kObGroups) {
     // ===================== K tiles =====================
-    const int prod = warp - 2 - 4 * kObGroups;  // takes the tiles prod, prod + 2, ...
     // Rows of the pools where the pages of the next tiles begin, a lane per page, one window of 32 pages ahead: a load
     // per tile would pace the stream by its latency.
     const int ppt = kObTile >> shift, lane_tile = lane >> (7 - shift), lane_page = lane & (ppt - 1);
     const int win_tiles = 32 >> (7 - shift);  // pages per tile: ppt; tiles per window
     auto load_window = [&](int k0, int& head, bool& has) {
-      const int i = (k0 + lane_tile) * kObProducers + prod;
+      const int i = k0 + lane_tile;
       head = 0;
       has = false;
       if (i >= n_x) return 0;
@@ -338,13 +330,13 @@ layer_observe_kernel(const __grid_constant__ ObserveParams p, const __grid_const
     int head, head_n;
     bool has, has_n;
     int page = load_window(0, head, has), page_n = load_window(win_tiles, head_n, has_n);
-    for (int k = 0, i = prod; i < n_x; ++k, i += kObProducers) {
-      const int in_win = k & (win_tiles - 1);
-      if (in_win == 0 && k > 0) {
+    for (int i = 0; i < n_x; ++i) {
+      const int in_win = i & (win_tiles - 1);
+      if (in_win == 0 && i > 0) {
         page = page_n;
         head = head_n;
         has = has_n;
-        page_n = load_window(k + win_tiles, head_n, has_n);
+        page_n = load_window(i + win_tiles, head_n, has_n);
       }
       const int s = i & s_mask, lap = i >> p.stage_shift;
       bool ok = true;
@@ -368,52 +360,45 @@ layer_observe_kernel(const __grid_constant__ ObserveParams p, const __grid_const
       }
       __syncwarp();
     }
-  } else if (warp == 1) {
-    // ===================== tensor-core issue =====================
+  } else if (warp == 1 || warp == 2 + 4 * kObGroups) {
+    // ===================== tensor-core issue: thread 0 for groups 0 and 2, thread 1 for groups 1 and 3 =====================
+    const int issuer = warp == 1 ? 0 : 1;
     if (lane == 0) {
       ObCursor c;
       if (n_x > 0) c.seek(pre_s, p.g.batch, H, x_first);
       int seg = 0;
-      bool first = true, ok = true;
-      // One thread paces the tensor cores, so its loop is short: a descriptor's low word is an address in 16-byte
-      // units (and the fixed bits), its high word never changes; k step 4 starts the second 64-channel half.
+      bool first = true;
+      // A descriptor's low word is an address in 16-byte units (and fixed bits), its high word never changes; k step 4
+      // starts the second 64-channel half.
       const uint64_t d0 = smem_desc_k128(0);
       const uint32_t d_hi = (uint32_t)(d0 >> 32), d_lo = (uint32_t)d0, q_step = (uint32_t)(q_half >> 4);
-      const int V = PASS == 1 ? p.v1 : p.v2, v_shift = V == 1 ? 0 : (V == 2 ? 1 : 2);
-      const uint32_t idesc_full = umma_idesc<DT, kObUnit>();
-      for (int i = 0; i < n_x && ok; ++i) {
+      const int tt = p.nt == 1 ? 0 : issuer;  // this thread's row tile
+      const int n_cols = PASS == 1 ? kObTile : (min(p.rows - tt * kObTile, kObTile) + 15) / 16 * 16;
+      const uint32_t idesc = umma_idesc<DT, 8>() - (1u << 17) + ((uint32_t)(n_cols >> 3) << 17);
+      for (int i = 0; i < n_x; ++i) {
         const int s = i & s_mask, qb = seg & 1;
         if (first && !mbar_wait_lean(qfull0 + 8 * qb, (seg >> 1) & 1, s_abort, p.status)) break;
-        if (!mbar_wait_lean(full0 + 8 * s, (i >> p.stage_shift) & 1, s_abort, p.status)) break;
-        const uint32_t q_lo = d_lo + ((sq0 + qb * q_bytes) >> 4), k_lo = d_lo + ((sk0 + s * kObTileBytes) >> 4);
-        const int turn = i >> (2 - v_shift), lap = turn / kObGroupBufs;
-        for (int v = 0; v < V; ++v) {
-          const int buf = kObGroupBufs * (((i << v_shift) + v) & 3) + turn % kObGroupBufs;
-          if (lap >= 1) ok = mbar_wait_lean(tempty0 + 8 * buf, (lap - 1) & 1, s_abort, p.status);
-          if (!ok) break;
+        if (p.nt == 2 || (i & 1) == issuer) {
+          if (!mbar_wait_lean(full0 + 8 * s, (i >> p.stage_shift) & 1, s_abort, p.status)) break;
+          const int grp = p.nt == 1 ? i & 3 : 2 * (i & 1) + tt, turn = p.nt == 1 ? i >> 2 : i >> 1;
+          if (turn >= 1 && !mbar_wait_lean(tempty0 + 8 * grp, (turn - 1) & 1, s_abort, p.status)) break;
           tc_fence_after();
-          const uint32_t d = tmem_d + buf * kObUnit;
-          // pass 1: a row tile against a unit of tokens; pass 2: the tile's tokens against a unit of rows
-          const uint32_t qv = q_lo + (uint32_t)((PASS == 1 ? v / kObHalves * kObTile : v * kObUnit) * 8);
-          const uint32_t kv = k_lo + (uint32_t)((PASS == 1 ? v % kObHalves * kObUnit : 0) * 8);
-          const int left = p.rows - v * kObUnit;
-          const uint32_t idesc = PASS == 1 || left >= kObUnit
-                                     ? idesc_full
-                                     : umma_idesc<DT, 8>() - (1u << 17) + ((uint32_t)((max(left, 1) + 15) / 16 * 2) << 17);
+          const uint32_t q_lo = d_lo + ((sq0 + qb * q_bytes) >> 4) + (uint32_t)(tt * (kObHalf >> 4));
+          const uint32_t k_lo = d_lo + ((sk0 + s * kObTileBytes) >> 4), d = tmem_d + grp * kObTile;
 #pragma unroll
           for (int k = 0; k < kHeadDim / 16; ++k) {
-            const uint32_t ql = qv + (k >= 4 ? q_step : 0u) + (uint32_t)(2 * (k & 3));
-            const uint32_t kl = kv + (uint32_t)((k >> 2) * (kObHalf >> 4) + 2 * (k & 3));
+            const uint32_t ql = q_lo + (k >= 4 ? q_step : 0u) + (uint32_t)(2 * (k & 3));
+            const uint32_t kl = k_lo + (uint32_t)((k >> 2) * (kObHalf >> 4) + 2 * (k & 3));
             const uint64_t dq = ((uint64_t)d_hi << 32) | ql, dk = ((uint64_t)d_hi << 32) | kl;
             if (PASS == 1) umma_f16(d, dq, dk, idesc, k > 0 ? 1u : 0u);
             else umma_f16(d, dk, dq, idesc, k > 0 ? 1u : 0u);
           }
-          umma_commit(tfull0 + 8 * buf);
+          umma_commit(tfull0 + 8 * grp);
+          umma_commit(empty0 + 8 * s);
         }
-        umma_commit(empty0 + 8 * s);
         first = last_of_seg(c, i);
         if (first) {
-          umma_commit(qempty0 + 8 * qb);
+          umma_commit(qempty0 + 8 * qb);  // (arrives at once if this thread had no tile of the segment)
           ++seg;
         }
         if (i + 1 < n_x) advance(c, x_first + DIR * (i + 1));
@@ -421,20 +406,18 @@ layer_observe_kernel(const __grid_constant__ ObserveParams p, const __grid_const
     }
   } else {
     // ===================== scores =====================
-    // the group takes unit v of the tiles mine, mine + stride, ...
+    // with one row tile the group takes every fourth tile, with two every second one, the rows of tile `tt`
     const int grp = (warp - 2) >> 2, quad = warp & 3, gl = quad * 32 + lane;  // gl: this thread's tensor-memory lane
-    const int V = PASS == 1 ? p.v1 : p.v2, stride = 4 / V, mine = grp / V, v = grp % V;
-    const int row0 = PASS == 1 ? v / kObHalves * kObTile : v * kObUnit;  // its rows
-    const int n_rows = min(p.rows - row0, PASS == 1 ? kObTile : kObUnit);  // (may be none in pass 2)
-    const int tok0 = PASS == 1 ? v % kObHalves * kObUnit : 0;             // pass 1: where its tokens begin in the tile
-    const uint32_t tbuf0 = tmem_d + kObGroupBufs * grp * kObUnit + ((uint32_t)(quad * 32) << 16);
-    const uint32_t my_full = tfull0 + 8 * kObGroupBufs * grp, my_empty = tempty0 + 8 * kObGroupBufs * grp;
+    const int tt = p.nt == 1 ? 0 : grp & 1, stride = 4 / p.nt, mine = p.nt == 1 ? grp : grp >> 1;
+    const int row0 = tt * kObTile, n_rows = min(p.rows - row0, kObTile);
+    const uint32_t tbuf = tmem_d + grp * kObTile + ((uint32_t)(quad * 32) << 16);
+    const uint32_t my_full = tfull0 + 8 * grp, my_empty = tempty0 + 8 * grp;
     float* row_g = row_s + grp * kObTile * 2;
     int* row_q = view_s + grp * kObTile * 2;
     int* pos_g = pos_s + grp * kObTile;
     const bool no_max = CAP && p.rule.cap_log2 <= 100.f && p.rule.slopes == nullptr;
     // pass 1: this lane's row, and the columns its copy takes
-    const int copy = gl / p.rp, c_n = kObUnit / p.rep, c_lo = copy * c_n, r_own = gl % p.rp;
+    const int copy = gl / p.rp, c_n = kObTile / p.rep, c_lo = copy * c_n, r_own = gl % p.rp;
     const bool live = r_own < n_rows, warp_live = (quad * 32) % p.rp < n_rows;
     View v0 = {}, vw = {};  // of the first query; pass 1: of this lane's row
     float m = 0.f, l = 0.f, slope = 0.f;
@@ -514,7 +497,7 @@ layer_observe_kernel(const __grid_constant__ ObserveParams p, const __grid_const
           ll = (ll == 0.f ? 0.f : ll * ex2(mm - M)) + (lk == 0.f ? 0.f : lk * ex2(mk - M));
           mm = M;
         }
-        reinterpret_cast<float2*>(p.part_ml)[((size_t)(cta + c.b * H + c.g) * p.rows + row0 + gl) * p.slots + (p.nt == 1 ? grp : (kObHalves == 2 ? grp & 1 : grp >> 1))] = make_float2(mm, ll);
+        reinterpret_cast<float2*>(p.part_ml)[((size_t)(cta + c.b * H + c.g) * p.rows + row0 + gl) * p.slots + mine] = make_float2(mm, ll);
       }
     };
 
@@ -540,9 +523,7 @@ layer_observe_kernel(const __grid_constant__ ObserveParams p, const __grid_const
         pos_g[gl] = pos;
         group_sync(grp);
       }
-      const uint32_t b_off = turn % kObGroupBufs;
-      const uint32_t tbuf = tbuf0 + b_off * kObUnit;
-      const bool good = __all_sync(0xffffffffu, mbar_wait_lean(my_full + 8 * b_off, (turn / kObGroupBufs) & 1, s_abort, p.status));
+      const bool good = __all_sync(0xffffffffu, mbar_wait_lean(my_full, turn & 1, s_abort, p.status));
       tc_fence_after();
       float w = 0.f;
       if (good && PASS == 1 && warp_live) {
@@ -556,7 +537,7 @@ layer_observe_kernel(const __grid_constant__ ObserveParams p, const __grid_const
           if (!easy) {  // distance bias and masks: the scores themselves, factor 1
 #pragma unroll
             for (int k = 0; k < kObChunk; ++k) {
-              const int pk = pos_g[tok0 + ch + k];
+              const int pk = pos_g[ch + k];
               float fa, fb;
               unpack2(f[k / 2], fa, fb);
               const float s = __uint_as_float(raw[k]) * ((k & 1) ? fb : fa);
@@ -646,17 +627,15 @@ layer_observe_kernel(const __grid_constant__ ObserveParams p, const __grid_const
       }
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(my_empty + 8 * b_off);
+      if (lane == 0) mbar_arrive(my_empty);
       if (PASS == 2) {
-        if (V > 1) {  // a token's partial weights meet; the next turn's barrier lies between these reads and the slots' reuse
-          float* part = reinterpret_cast<float*>(pos_s) + ((turn & 1) * kObGroups + grp - v) * kObTile + gl;
-          if (v > 0) part[v * kObTile] = w;
-          if (V == 2) pair_sync(grp >> 1);
-          else groups_sync();
-          if (v == 0)
-            for (int k = 1; k < V; ++k) w += part[k * kObTile];
+        if (p.nt == 2) {  // a token's partial weights meet; the next turn's barrier lies between this read and the slot's reuse
+          float* part = reinterpret_cast<float*>(pos_s) + ((turn & 1) * kObGroups + grp - tt) * kObTile + gl;
+          if (tt == 1) *part = w;
+          pair_sync(grp >> 1);
+          if (tt == 0) w += *part;
         }
-        if (v == 0 && page_ok(p.g, page)) p.weights[at] = (p.add ? p.weights[at] : 0.f) + w;
+        if (tt == 0 && page_ok(p.g, page)) p.weights[at] = (p.add ? p.weights[at] : 0.f) + w;
       }
     }
     if (PASS == 1 && c.b >= 0) end_segment();
@@ -694,8 +673,6 @@ mc_status launch_layer_observe(const mc_config* cfg, const mc_batch* bt, const G
   op.rows = n_obs * op.nq;
   op.nt = op.rows > kObTile ? 2 : 1;
   op.slots = kObGroups / op.nt;
-  op.v1 = kObHalves * op.nt;
-  op.v2 = op.rows <= kObUnit ? 1 : (op.rows <= 2 * kObUnit ? 2 : 4);
   op.rp = op.rows > 64 ? 128 : (op.rows > 32 ? 64 : 32);
   op.rep = kObTile / op.rp;
   op.jt = std::min(n_obs, kObTile / op.nq);
@@ -721,7 +698,7 @@ mc_status launch_layer_observe(const mc_config* cfg, const mc_batch* bt, const G
   const uint64_t rows = (uint64_t)bt->n_pages * cfg->n_kv_heads * cfg->page_size;
   if (mc_status st = make_map(&map_k, cfg->dtype, layer->k_pool, rows, kHeadDim, cfg->page_size)) return st;
   if (mc_status st = make_map3(&map_q, cfg->dtype, q, (uint64_t)bt->batch * n_obs, cfg->n_q_heads, kHeadDim, op.jt, op.nq)) return st;
-  const size_t smem = 1024 + kObSmem + (2 * kObMaxStages + 4 + 2 * kObBufs) * 8 + 16 + kObGroups * kObTile * (2 * 8 + 8) + (size_t)(bt->batch + 1) * 4;
+  const size_t smem = 1024 + kObSmem + (2 * kObMaxStages + 4 + 2 * kObGroups) * 8 + 16 + kObGroups * kObTile * (2 * 8 + 8) + (size_t)(bt->batch + 1) * 4;
   using Kernel = void (*)(const ObserveParams, const CUtensorMap, const CUtensorMap);
   static const Kernel kernels[2][2][2] = {
       {{layer_observe_kernel<MC_F16, 1, false>, layer_observe_kernel<MC_F16, 1, true>},
