@@ -564,9 +564,15 @@ mc_status mc_decode_attn_static(const mc_config* cfg, const mc_batch* batch, con
  * below attend such a layer during decode and keep its length bounded: mc_layer_attn (single-query attention, the
  * step's rows appended in the same call), mc_layer_observe (the attention weight that a prompt's last queries give
  * to every cached token) and mc_layer_evict (the rows with the least accumulated weight go).  (The paper has no
- * counterpart: it leaves those layers to the serving engine.)  A layer that is evicted from has lengths of its own:
- * give it a mc_batch of its own (its own seq_lens; a block table may be shared as long as the pages it names are
- * this layer's slots). */
+ * counterpart: it leaves those layers to the serving engine.)
+ * - A layer that is evicted from has lengths of its own: give it a mc_batch of its own (its own seq_lens; a block table
+ *   may be shared as long as the pages it names are this layer's slots).  max_seq_len sizes grids and scratch memory:
+ *   keep it near the longest length that can occur.
+ * - Calls that write a layer's cache (everything but mc_layer_attn without flags) are ordered by the caller, on one
+ *   stream or with events; a page that such a call writes to belongs to one sequence.
+ * - block_table, seq_lens, q and the score options may be read before the kernel ahead in the stream has completed (see
+ *   the conventions at the top).  mc_layer_evict's new_lens may be passed on as the seq_lens of the next call: the
+ *   eviction lets nothing start early. */
 
 /* One layer's cache.
  * k_pool, v_pool  [n_pages][n_kv_heads][page_size][128] of cfg->dtype (the layer pools of mc_layer_kv)

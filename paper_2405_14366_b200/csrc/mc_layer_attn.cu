@@ -640,58 +640,63 @@ __global__ void __launch_bounds__(kLcThreads) layer_attn_combine_kernel(const __
 constexpr int kLwTokens = 1024;
 
 template <int NQ>
-__global__ void __launch_bounds__(kLcThreads) layer_attn_weights_kernel(const __grid_constant__ LayerAttnParams p, int chunks) {
+__global__ void __launch_bounds__(kLcThreads) layer_attn_weights_kernel(const __grid_constant__ LayerAttnParams p, int blocks) {
   grid_dep_launch();
-  const int tid = threadIdx.x, b = blockIdx.y, head = blockIdx.x / chunks, k0 = (blockIdx.x % chunks) * (kLwTokens / kLaUnit);
+  const int tid = threadIdx.x, b = blockIdx.y, head = blockIdx.x / blocks;
   const Seq sq = seq_of(p, b);
-  constexpr int kOwn = kLwTokens / kLcThreads;
-  int at[kOwn];
-  long long from[kOwn];  // (past 32 bits in a long batch)
-  bool fresh[kOwn];
+  constexpr int kOwn = kLwTokens / kLcThreads, kStep = kLwTokens / kLaUnit;
+  // (the grid is sized for the GPU, not for the longest length a sequence might have: a block takes every `blocks`-th chunk)
+  bool waited = false;
+  for (int k0 = (blockIdx.x % blocks) * kStep; k0 < sq.u; k0 += blocks * kStep) {
+    int at[kOwn];
+    long long from[kOwn];  // (past 32 bits in a long batch)
+    bool fresh[kOwn];
 #pragma unroll
-  for (int j = 0; j < kOwn; ++j) {
-    const int i = tid + j * kLcThreads, k = k0 + i / kLaUnit, in = i % kLaUnit;
-    const int t = (k < sq.ua ? k : sq.ub0 + k - sq.ua) * kLaUnit + in, slot = t >> p.g.page_shift;
-    fresh[j] = t == sq.n;  // the appended row: its weight begins here
-    at[j] = -1;
-    from[j] = -1;
-    if (k >= sq.u || t >= sq.n_tot || slot >= p.g.max_pages_per_seq || (fresh[j] && !(p.flags & MC_LAYER_APPEND))) continue;
-    const bool seen = p.positions != nullptr || t < sq.a || (t >= sq.lo && t < sq.hi);
-    if (!seen && !fresh[j]) continue;  // (no score was written)
-    const int page = p.g.block_table[(size_t)b * p.g.max_pages_per_seq + slot];
-    if (!page_ok(p.g, page)) continue;  // (flagged by the split kernel)
-    at[j] = (page * p.g.n_kv_heads + head) * p.g.page_size + (t & (p.g.page_size - 1));
-    if (seen) from[j] = ((long long)(b * p.seq_units + k) * p.g.n_kv_heads + head) * kLaUnit + in;
-  }
-  grid_dep_wait();
-  float s[kOwn][NQ], w[kOwn], z[NQ];
-#pragma unroll
-  for (int r = 0; r < NQ; ++r) z[r] = p.lse2[(size_t)b * p.n_q_heads + head * NQ + r];
-#pragma unroll
-  for (int j = 0; j < kOwn; ++j) {
-    w[j] = at[j] >= 0 && !fresh[j] ? p.weights[at[j]] : 0.f;
-    const float* src = p.scores + (size_t)max(from[j], 0LL) * NQ;
-    if (NQ % 4 == 0) {
-#pragma unroll
-      for (int r = 0; r < NQ; r += 4) {
-        const float4 v = from[j] >= 0 ? *reinterpret_cast<const float4*>(src + r) : make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
-        s[j][r] = v.x;
-        s[j][(r + 1) % NQ] = v.y;
-        s[j][(r + 2) % NQ] = v.z;
-        s[j][(r + 3) % NQ] = v.w;
-      }
-    } else {
-#pragma unroll
-      for (int r = 0; r < NQ; ++r) s[j][r] = from[j] >= 0 ? src[r] : -INFINITY;
+    for (int j = 0; j < kOwn; ++j) {
+      const int i = tid + j * kLcThreads, k = k0 + i / kLaUnit, in = i % kLaUnit;
+      const int t = (k < sq.ua ? k : sq.ub0 + k - sq.ua) * kLaUnit + in, slot = t >> p.g.page_shift;
+      fresh[j] = t == sq.n;  // the appended row: its weight begins here
+      at[j] = -1;
+      from[j] = -1;
+      if (k >= sq.u || t >= sq.n_tot || slot >= p.g.max_pages_per_seq || (fresh[j] && !(p.flags & MC_LAYER_APPEND))) continue;
+      const bool seen = p.positions != nullptr || t < sq.a || (t >= sq.lo && t < sq.hi);
+      if (!seen && !fresh[j]) continue;  // (no score was written)
+      const int page = p.g.block_table[(size_t)b * p.g.max_pages_per_seq + slot];
+      if (!page_ok(p.g, page)) continue;  // (flagged by the split kernel)
+      at[j] = (page * p.g.n_kv_heads + head) * p.g.page_size + (t & (p.g.page_size - 1));
+      if (seen) from[j] = ((long long)(b * p.seq_units + k) * p.g.n_kv_heads + head) * kLaUnit + in;
     }
-  }
+    if (!waited) grid_dep_wait();
+    waited = true;
+    float s[kOwn][NQ], w[kOwn], z[NQ];
 #pragma unroll
-  for (int j = 0; j < kOwn; ++j) {
-    if (at[j] < 0) continue;
-    float sum = 0.f;
+    for (int r = 0; r < NQ; ++r) z[r] = p.lse2[(size_t)b * p.n_q_heads + head * NQ + r];
 #pragma unroll
-    for (int r = 0; r < NQ; ++r) sum += ex2(s[j][r] - z[r]);
-    p.weights[at[j]] = w[j] + sum;
+    for (int j = 0; j < kOwn; ++j) {
+      w[j] = at[j] >= 0 && !fresh[j] ? p.weights[at[j]] : 0.f;
+      const float* src = p.scores + (size_t)max(from[j], 0LL) * NQ;
+      if (NQ % 4 == 0) {
+#pragma unroll
+        for (int r = 0; r < NQ; r += 4) {
+          const float4 v = from[j] >= 0 ? *reinterpret_cast<const float4*>(src + r) : make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+          s[j][r] = v.x;
+          s[j][(r + 1) % NQ] = v.y;
+          s[j][(r + 2) % NQ] = v.z;
+          s[j][(r + 3) % NQ] = v.w;
+        }
+      } else {
+#pragma unroll
+        for (int r = 0; r < NQ; ++r) s[j][r] = from[j] >= 0 ? src[r] : -INFINITY;
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < kOwn; ++j) {
+      if (at[j] < 0) continue;
+      float sum = 0.f;
+#pragma unroll
+      for (int r = 0; r < NQ; ++r) sum += ex2(s[j][r] - z[r]);
+      p.weights[at[j]] = w[j] + sum;
+    }
   }
 }
 
@@ -778,12 +783,13 @@ mc_status launch_layer_attn(const mc_config* cfg, const mc_batch* bt, const Geom
   MC_CUDA_CHECK(launch_pdl(combine, dim3((cfg->n_q_heads + per_block - 1) / per_block, bt->batch), dim3(kLcThreads), 0, stream, ap,
                            (unsigned short*)out, lse));
   if (flags & MC_LAYER_ACCUMULATE) {
-    const int chunks = (pl.seq_units * kLaUnit + kLwTokens - 1) / kLwTokens;
+    const int chunks = (pl.seq_units * kLaUnit + kLwTokens - 1) / kLwTokens, segs = bt->batch * cfg->n_kv_heads;
+    const int blocks = std::min(chunks, (8 * n_sm + segs - 1) / segs);  // per (sequence, kv head)
     auto* weights = ap.nq == 1   ? layer_attn_weights_kernel<1>
                     : ap.nq == 2 ? layer_attn_weights_kernel<2>
                     : ap.nq == 4 ? layer_attn_weights_kernel<4>
                                  : layer_attn_weights_kernel<8>;
-    MC_CUDA_CHECK(launch_pdl(weights, dim3(cfg->n_kv_heads * chunks, bt->batch), dim3(kLcThreads), 0, stream, ap, chunks));
+    MC_CUDA_CHECK(launch_pdl(weights, dim3(cfg->n_kv_heads * blocks, bt->batch), dim3(kLcThreads), 0, stream, ap, blocks));
   }
   MC_CUDA_CHECK(cudaGetLastError());
   return MC_OK;

@@ -131,6 +131,8 @@ def test_long_and_many(L):
     run(L, [70 + 13 * i for i in range(64)], H=2, Hq=2, ps=16, append=True)
     run(L, [3] * 512, H=1, Hq=2, ps=16, append=True, acc=True)
     run(L, [10, 40], H=2, Hq=2, ps=16, max_len=100000)  # a bound far above the lengths
+    run(L, [10, 40, 3000], H=2, Hq=2, ps=16, max_len=100000, acc=True, append=True)
+    run(L, [2600] * 80, H=8, Hq=8, ps=64, dtype="bf16", acc=True, append=True, alibi=True)  # weight blocks with several chunks
 
 
 def test_results_do_not_depend_on_the_call_before(L):
