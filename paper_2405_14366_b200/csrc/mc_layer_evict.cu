@@ -360,7 +360,7 @@ mc_status launch_layer_evict(const mc_config* cfg, const mc_batch* bt, const Geo
   int n_sm = 0;
   if (mc_status st = sm_count(&n_sm)) return st;
   // CTAs per segment: as many as the GPU takes at once (two per SM), if a CTA still has 1024 tokens.  (More of them run
-  // in two waves: 256 segments of 4096 tokens took 90 us with two CTAs each, 4MB_US with one.)
+  // in two waves: 256 segments of 4096 tokens took 90 us with two CTAs each, 67 with one.)
   int cluster = 1;
   while (cluster < kEvMaxCluster && (long long)bt->batch * cfg->n_kv_heads * cluster * 2 <= 2 * n_sm &&
          bt->max_seq_len > 1024 * cluster)
