@@ -570,9 +570,11 @@ mc_status mc_decode_attn_static(const mc_config* cfg, const mc_batch* batch, con
  *   keep it near the longest length that can occur.
  * - Calls that write a layer's cache (everything but mc_layer_attn without flags) are ordered by the caller, on one
  *   stream or with events; a page that such a call writes to belongs to one sequence.
- * - block_table, seq_lens, q and the score options may be read before the kernel ahead in the stream has completed (see
- *   the conventions at the top).  mc_layer_evict's new_lens may be passed on as the seq_lens of the next call: the
- *   eviction lets nothing start early. */
+ * - block_table, seq_lens and the score options may be read before the kernel ahead in the stream has completed (see the
+ *   conventions at the top); q, k_new and v_new are not, so that one call's out may be the next one's q.
+ *   mc_layer_evict's new_lens may be passed on as the seq_lens of the next mc_layer_* call: the eviction lets nothing
+ *   start early.
+ * - batch at most 512, max_seq_len at most 2^30, batch * n_kv_heads * (max_seq_len / 64 + 2) below 2^31 (MC_ERR_SHAPE). */
 
 /* One layer's cache.
  * k_pool, v_pool  [n_pages][n_kv_heads][page_size][128] of cfg->dtype (the layer pools of mc_layer_kv)
@@ -602,7 +604,7 @@ typedef struct mc_layer_cache {
  * q_pos         device [batch] int32 or NULL.  mc_layer_attn: the query's position; NULL: seq_lens[b] with a new row,
  *               seq_lens[b] - 1 without (the positions of a cache that was never evicted from).
  *               mc_layer_observe: the position of the last query; NULL: seq_lens[b] - 1.  Below -1 counts as -1.
- * softcap       0: none.  window: 0: none. */
+ * softcap       0: none.  window: 0: none.  sm_scale, softcap and their quotient at most 2e38 in magnitude. */
 typedef struct mc_score_opts {
   const float* alibi_slopes;
   const int32_t* doc_start;
@@ -637,8 +639,7 @@ mc_status mc_layer_workspace_bytes(const mc_config* cfg, const mc_batch* batch, 
  * out          [batch][n_q_heads][128] cfg->dtype;  lse [batch][n_q_heads] fp32 natural log, or NULL
  * workspace    mc_layer_workspace_bytes(MC_OP_LAYER_ATTN, flags) bytes, 256-byte aligned
  * A query that sees nothing yields zeros and lse = -inf, and adds no weight.  Scores and sums are held in fp32; the
- * probabilities are rounded once to cfg->dtype before they meet the values.  cfg->cache_bits must be 0 or 16; batch
- * at most 512. */
+ * probabilities are rounded once to cfg->dtype before they meet the values.  cfg->cache_bits must be 0 or 16. */
 mc_status mc_layer_attn(const mc_config* cfg, const mc_batch* batch, const mc_layer_cache* layer, const mc_score_opts* opts,
                         const void* q, const void* k_new, const void* v_new, int32_t flags, void* out, float* lse,
                         void* workspace, size_t workspace_bytes, void* stream);
@@ -672,8 +673,8 @@ typedef struct mc_evict_opts {
  * every number.  Rows that stay and sit in the first `budget` slots are not touched; the k-th (in index order) that
  * sits behind them is copied, with its position and weight, to the k-th slot before `budget` whose row is evicted.
  * Slots from `budget` on keep what they held.  layer->positions and layer->weights are needed.
- * new_lens   device [batch] int32: min(seq_lens[b], budget); must not overlap seq_lens (the caller copies it there, or
- *            passes it as the seq_lens of later calls)
+ * new_lens   device [batch] int32: min(seq_lens[b], budget); must not overlap seq_lens or q_pos (the caller copies it to
+ *            seq_lens, or passes it as the seq_lens of later calls)
  * workspace  mc_layer_workspace_bytes(MC_OP_LAYER_EVICT, 0) bytes, 256-byte aligned */
 mc_status mc_layer_evict(const mc_config* cfg, const mc_batch* batch, const mc_layer_cache* layer, const mc_evict_opts* opts,
                          int32_t* new_lens, void* workspace, size_t workspace_bytes, void* stream);

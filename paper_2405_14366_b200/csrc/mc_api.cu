@@ -1,4 +1,5 @@
 // C-ABI entry points: argument validation and dispatch to the kernel launchers.
+#include <math.h>
 #include <stdio.h>
 #include <string.h>
 
@@ -700,6 +701,10 @@ mc_status mc_decode_drain_host(const mc_config* cfg, const mc_batch* batch, int3
 }
 
 // ---- one uncompressed layer ------------------------------------------------------------------------
+// Token indices and numbers of 64-token units, of all sequences and kv heads, are 32-bit.
+static bool too_long(const mc_config* cfg, const mc_batch* batch) {
+  return batch->max_seq_len > (1 << 30) || (int64_t)batch->batch * cfg->n_kv_heads * (batch->max_seq_len / 64 + 2) > 0x7fffffffLL;
+}
 // What every mc_layer_* call checks about its configuration, batch and cache.
 static mc_status check_layer(const mc_config* cfg, const mc_batch* batch, const mc_layer_cache* layer) {
   mc_status st = check_config(cfg);
@@ -708,6 +713,7 @@ static mc_status check_layer(const mc_config* cfg, const mc_batch* batch, const 
   if (st != MC_OK) return st;
   if (cfg->cache_bits == 4) return MC_ERR_UNSUPPORTED;
   if (batch->batch > kMaxLayerBatch) return MC_ERR_SHAPE;
+  if (too_long(cfg, batch)) return MC_ERR_SHAPE;
   if (batch->batch > 0 && batch->n_pages == 0) return MC_ERR_INVALID_ARG;  // (a bad page id reads page 0: there has to be one)
   if (!layer || !layer->k_pool || !layer->v_pool || !layer->status) return MC_ERR_INVALID_ARG;
   if (!aligned256(layer->k_pool) || !aligned256(layer->v_pool) || !aligned256(layer->positions) || !aligned256(layer->weights))
@@ -717,9 +723,10 @@ static mc_status check_layer(const mc_config* cfg, const mc_batch* batch, const 
 }
 
 static mc_status check_score_opts(const mc_score_opts* o) {
-  if (o == nullptr || o->window < 0 || !(o->softcap >= 0.f) || o->softcap > 3.0e38f || !(o->sm_scale == o->sm_scale) ||
-      o->sm_scale > 3.0e38f || o->sm_scale < -3.0e38f)
+  // (what the kernels make of them, sm_scale log2(e), softcap log2(e) and sm_scale / softcap, has to be a number too)
+  if (o == nullptr || o->window < 0 || !(o->softcap >= 0.f && o->softcap <= 2.0e38f) || !(fabsf(o->sm_scale) <= 2.0e38f))
     return MC_ERR_INVALID_ARG;
+  if (o->softcap > 0.f && !(fabsf(o->sm_scale / o->softcap) <= 2.0e38f)) return MC_ERR_INVALID_ARG;
   const uintptr_t al = (uintptr_t)o->alibi_slopes | (uintptr_t)o->doc_start | (uintptr_t)o->prefix_len | (uintptr_t)o->q_pos;
   return (al & 3u) ? MC_ERR_ALIGN : MC_OK;
 }
@@ -729,6 +736,7 @@ mc_status mc_layer_workspace_bytes(const mc_config* cfg, const mc_batch* batch, 
   if (st != MC_OK) return st;
   if (batch == nullptr || bytes == nullptr) return MC_ERR_INVALID_ARG;
   if (batch->batch < 0 || batch->max_seq_len < 0) return MC_ERR_INVALID_ARG;
+  if (batch->batch > kMaxLayerBatch || too_long(cfg, batch)) return MC_ERR_SHAPE;
   switch (op) {
     case MC_OP_LAYER_ATTN:
       if (arg & ~(MC_LAYER_APPEND | MC_LAYER_ACCUMULATE)) return MC_ERR_INVALID_ARG;
@@ -792,8 +800,9 @@ mc_status mc_layer_evict(const mc_config* cfg, const mc_batch* batch, const mc_l
   if (opts->budget < 1 || opts->n_sink < 0 || opts->n_recent < 0 || (int64_t)opts->n_sink + opts->n_recent > opts->budget)
     return MC_ERR_INVALID_ARG;
   if (((uintptr_t)opts->q_pos | (uintptr_t)new_lens) & 3u) return MC_ERR_ALIGN;
-  // every CTA reads its sequence's length, one of them writes the new one
-  if (new_lens < batch->seq_lens + batch->batch && batch->seq_lens < new_lens + batch->batch) return MC_ERR_INVALID_ARG;
+  // every CTA reads its sequence's length and position, one of them writes the new length
+  for (const int32_t* in : {batch->seq_lens, opts->q_pos})
+    if (in != nullptr && new_lens < in + batch->batch && in < new_lens + batch->batch) return MC_ERR_INVALID_ARG;
   if (workspace == nullptr || !aligned256(workspace)) return workspace ? MC_ERR_ALIGN : MC_ERR_INVALID_ARG;
   if (workspace_bytes < layer_evict_workspace_bytes(cfg, batch)) return MC_ERR_CAPACITY;
   return launch_layer_evict(cfg, batch, make_geom(cfg, batch), layer, opts, new_lens, workspace, (cudaStream_t)stream);

@@ -110,6 +110,26 @@ def test_layer_evict_refusals(lib):
     assert ev(ws=0) == 1 and ev(ws=0x500080) == 4 and ev(n=16) == 5
 
 
+def test_refusals_of_sizes_and_scales_past_the_arithmetic(lib):
+    """Lengths whose 32-bit token and unit numbers would wrap, scales whose product or quotient is no number, a result
+    over an input."""
+    L, out = lib._lib, C.c_size_t(0)
+    long = [dict(max_len=2 ** 31 - 1, mpps=2 ** 27), dict(max_len=2 ** 30 + 1, mpps=2 ** 27, batch=1),
+            dict(batch=512, max_len=2 ** 27, mpps=2 ** 24)]
+    for kw in long:
+        b, l, e = batch(**kw), layer(), B._EvictOpts(0, 100, 4, 10, 0)
+        assert attn(lib, b=b, n=1 << 60) == 2, kw
+        assert L.mc_layer_observe(C.byref(cfg()), C.byref(b), C.byref(l), C.byref(opts()), 0x100000, 32, 0, 0x500000, 1 << 60, None) == 2, kw
+        assert L.mc_layer_evict(C.byref(cfg()), C.byref(b), C.byref(l), C.byref(e), 0x600000, 0x500000, 1 << 60, None) == 2, kw
+        for op, arg in ((2, 0), (2, 3), (3, 32), (4, 0)):
+            assert L.mc_layer_workspace_bytes(C.byref(cfg()), C.byref(b), op, arg, C.byref(out)) == 2, kw
+    for kw in (dict(sm=1.0, cap=1e-40), dict(cap=2.9e38), dict(sm=2.9e38), dict(sm=-2.9e38), dict(sm=1e20, cap=1e-20)):
+        assert attn(lib, o=opts(**kw)) == 1, kw
+    for q_pos in (0x600000, 0x600004, 0x5ffffc):  # new_lens over the positions it reads
+        o = B._EvictOpts(q_pos, 100, 4, 10, 0)
+        assert L.mc_layer_evict(C.byref(cfg()), C.byref(batch()), C.byref(layer()), C.byref(o), 0x600000, 0x500000, 1 << 30, None) == 1
+
+
 def test_workspace_bytes(lib):
     out = C.c_size_t(0)
     L, c = lib._lib, cfg()
