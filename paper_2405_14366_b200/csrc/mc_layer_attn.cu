@@ -69,7 +69,7 @@ struct Seq {
 };
 __device__ __forceinline__ Seq seq_of(const LayerAttnParams& p, int b) {
   Seq s;
-  const int raw = p.g.seq_lens[b];
+  const int raw = __ldcg(p.g.seq_lens + b);  // (from L2: an eviction ahead in the stream may just have written it)
   s.bad = raw < 0 || raw > p.g.max_seq_len;
   s.n = min(max(raw, 0), p.g.max_seq_len);
   s.n_tot = s.n + (p.k_new != nullptr ? 1 : 0);
@@ -166,7 +166,7 @@ template <int DT>
 __global__ void __launch_bounds__(kLaThreads, kLaCtasPerSm)
 layer_attn_split_kernel(const __grid_constant__ LayerAttnParams p, const __grid_constant__ CUtensorMap map_k,
                         const __grid_constant__ CUtensorMap map_v) {
-  // (lengths, block table, score options and queries are the caller's: read before the wait, as in mc_attn.cu)
+  // (lengths, block table and score options are the caller's: read before the wait, as in mc_attn.cu)
   grid_dep_launch();
   extern __shared__ unsigned char smem_raw[];
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -258,12 +258,6 @@ layer_attn_split_kernel(const __grid_constant__ LayerAttnParams p, const __grid_
       q2[ks] = row < nq ? src[8 * ks + 4] : 0u;
     }
   };
-  uint32_t q0[8], q2[8];
-  {
-    const int meta = __shfl_sync(0xffffffffu, win.meta, 0);
-    if (n_slices > 0) load_q((meta >> 5) & 511, meta >> 14, q0, q2);
-  }
-
   grid_dep_wait();
   if (bad) atomicOr(p.status, MC_FLAG_BAD_METADATA);
 
@@ -286,6 +280,12 @@ layer_attn_split_kernel(const __grid_constant__ LayerAttnParams p, const __grid_
     }
   };
   for (int i = 0; i < kLaStages - 1; ++i) issue(i);
+  // (behind the wait: the queries may be what the kernel ahead wrote, another layer's output for instance)
+  uint32_t q0[8], q2[8];
+  {
+    const int meta = __shfl_sync(0xffffffffu, win.meta, 0);
+    if (n_slices > 0) load_q((meta >> 5) & 511, meta >> 14, q0, q2);
+  }
 
   float acc[8][4];
   float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;  // query rows colp, colp + 1
@@ -694,10 +694,11 @@ __global__ void __launch_bounds__(kLcThreads) layer_attn_weights_kernel(const __
       if (at[j] < 0) continue;
       float sum = 0.f;
 #pragma unroll
-      for (int r = 0; r < NQ; ++r) sum += ex2(s[j][r] - z[r]);
+      for (int r = 0; r < NQ; ++r) sum += s[j][r] == -INFINITY ? 0.f : ex2(s[j][r] - z[r]);  // (a row not seen: nothing, whatever z)
       p.weights[at[j]] = w[j] + sum;
     }
   }
+  if (!waited) grid_dep_wait();  // (a grid that ended without it would let the kernel behind overtake those ahead)
 }
 
 // ---- host side ------------------------------------------------------------------------------------

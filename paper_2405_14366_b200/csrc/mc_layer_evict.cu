@@ -90,13 +90,24 @@ __global__ void __launch_bounds__(kEvThreads, 2) layer_evict_kernel(const __grid
   const int H = p.g.n_kv_heads, ps = p.g.page_size, shift = p.g.page_shift;
   const int seg = blockIdx.x / C, b = seg / H, head = seg - b * H;
   grid_dep_wait();
-  const int raw = p.g.seq_lens[b];
+  const int raw = __ldcg(p.g.seq_lens + b);
   const int n = min(max(raw, 0), p.g.max_seq_len);
-  if (head == 0 && rank == 0 && tid == 0) {
+  const bool scribe = head == 0 && rank == 0 && tid == kEvThreads - 1;
+  int was = 0;
+  if (scribe) {
     if (raw != n) atomicOr(p.status, MC_FLAG_BAD_METADATA);
-    p.new_lens[b] = min(n, p.budget);
+    was = atomicExch(p.new_lens + b, min(n, p.budget));
   }
-  if (n <= p.budget) return;  // (the whole cluster)
+  // The new length is in L2 before this grid ends, since the kernel behind may read it before its wait: an exchange has
+  // happened when what was there before is back, and this waits for that.  (5.9 us on 8 x 32 segments of 1025 tokens; a
+  // store, and a fence here, 6.0; the fence right behind the store 6.4.)
+  auto settle = [&]() {
+    if (was == 0x7fffffff) __nanosleep(0);
+  };
+  if (n <= p.budget) {  // (the whole cluster)
+    settle();
+    return;
+  }
   const int last = max(p.q_pos ? p.q_pos[b] : n - 1, -1);
   const int recent = last - p.n_recent;  // positions above it are guarded
   const int per = (n + C - 1) / C;
@@ -154,7 +165,10 @@ __global__ void __launch_bounds__(kEvThreads, 2) layer_evict_kernel(const __grid
     for (int o = 16; o; o >>= 1) best = min(best, __shfl_xor_sync(0xffffffffu, best, o));
     if (lane == 0) best_s[warp] = best;
     __syncthreads();
-    if (warp != 0) return;
+    if (warp != 0) {
+      settle();
+      return;
+    }
     best = best_s[lane & (kEvWarps - 1)];
 #pragma unroll
     for (int o = 16; o; o >>= 1) best = min(best, __shfl_xor_sync(0xffffffffu, best, o));
@@ -332,6 +346,7 @@ __global__ void __launch_bounds__(kEvThreads, 2) layer_evict_kernel(const __grid
         if (to[k] >= 0) st_stream16(pool + (size_t)to[k] * kRowBytes + (lane & 15) * 16, v[k]);
     }
   }
+  settle();
 }
 
 // ---- host side ------------------------------------------------------------------------------------

@@ -74,7 +74,7 @@ struct ObSeq {
 };
 __device__ __forceinline__ ObSeq ob_seq(const ObserveParams& p, int b) {
   ObSeq s;
-  const int raw = p.g.seq_lens[b];
+  const int raw = __ldcg(p.g.seq_lens + b);  // (from L2: an eviction ahead in the stream may just have written it)
   s.bad = raw < 0 || raw > p.g.max_seq_len;
   s.n = min(max(raw, 0), p.g.max_seq_len);
   s.last = min(max(p.rule.q_pos ? p.rule.q_pos[b] : s.n - 1, -1), kObNoToken - 1);

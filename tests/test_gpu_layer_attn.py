@@ -173,6 +173,68 @@ def test_another_stream_and_a_captured_graph(L):
             assert ((o2[b, 4 * h:4 * h + 4].cpu().double() - p @ v2.double()).abs() <= tol).all()
 
 
+def test_one_call_s_output_as_the_next_one_s_query(L):
+    """Calls chained without a kernel between them give what the same calls give with the device idle between them."""
+    c = L.Cache([700, 40, 1500], 4, 16, 16, "bf16", seed=8)
+    mc, lib = c.mc, c.mc.lib()
+    q = c.queries(3, 16).cuda()
+    outs = []
+    for wait in (True, False):
+        a, b, ws = q.clone(), torch.zeros_like(q), c.workspace(mc.MC_OP_LAYER_ATTN, 0)
+        torch.cuda.synchronize()
+        for _ in range(12):
+            lib.mc_layer_attn(c.cfg, c.batch, c.layer, mc.ScoreOpts(300.0), a, None, None, 0, b, None, ws)
+            if wait:
+                torch.cuda.synchronize()
+            a, b = b, a
+        torch.cuda.synchronize()
+        outs.append(a.clone())
+    assert torch.equal(outs[0], outs[1]) and torch.isfinite(outs[0].float()).all()
+
+
+def test_a_query_of_nan_leaves_the_weights_of_rows_it_does_not_see(L):
+    c = L.Cache([300, 90], 2, 8, 16, "bf16", seed=9, marks=True, weights=True)
+    mc, lib = c.mc, c.mc.lib()
+    pos = torch.tensor(c.q_next, dtype=torch.int32, device="cuda")
+    q = c.queries(2, 8).cuda()
+    q[0, 1] = float("nan")  # of kv head 0
+    out, before = torch.empty_like(q), c.d["w"].clone()
+    window = 100
+    lib.mc_layer_attn(c.cfg, c.batch, c.layer, mc.ScoreOpts(SM, window=window, q_pos=pos), q, None, None, mc.MC_LAYER_ACCUMULATE, out, None,
+                      c.workspace(mc.MC_OP_LAYER_ATTN, mc.MC_LAYER_ACCUMULATE))
+    torch.cuda.synchronize()
+    after, other = c.gathered("w", 0), c.gathered("w", 1)
+    c.d["w"] = before
+    was = c.gathered("w", 0)
+    seen = L.seen(c.dense_pos[0], c.q_next[0], window=window)
+    assert seen.any() and not seen.all()
+    assert torch.equal(after[~seen], was[~seen])
+    assert after[:, 0][seen[:, 0]].isnan().all() and torch.isfinite(after[:, 1]).all()
+    assert out[0, 1].isnan().all() and torch.isfinite(out[0, 4:].float()).all() and torch.isfinite(out[1].float()).all()
+    assert torch.isfinite(other).all()
+
+
+def test_calls_around_one_whose_sequences_are_all_empty(L):
+    """A call with nothing to do between two others, all on one workspace and without a pause: results as with pauses."""
+    c = L.Cache([20000, 9000], 4, 16, 64, "bf16", seed=10, weights=True)
+    mc, lib = c.mc, c.mc.lib()
+    q = c.queries(2, 16).cuda()
+    none = mc.Batch(c.d["table"], torch.zeros_like(c.d_lens), c.max_len, c.n_pages)
+    start, got = c.d["w"].clone(), []
+    for wait in (True, False):
+        c.d["w"].copy_(start)
+        ws, outs = c.workspace(mc.MC_OP_LAYER_ATTN, mc.MC_LAYER_ACCUMULATE), [torch.full_like(q, 7.0) for _ in range(9)]
+        torch.cuda.synchronize()
+        for i, o in enumerate(outs):
+            lib.mc_layer_attn(c.cfg, none if i % 3 else c.batch, c.layer, mc.ScoreOpts(SM), q, None, None, mc.MC_LAYER_ACCUMULATE, o, None, ws)
+            if wait:
+                torch.cuda.synchronize()
+        torch.cuda.synchronize()
+        got.append((torch.stack(outs), c.d["w"].clone()))
+    assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
+    assert not got[0][0][1].any() and got[0][0][0].any()
+
+
 def test_bad_pages_and_lengths_are_flagged(L):
     c = L.Cache([100, 50], 2, 4, 16, "f16", poison=False)
     mc, lib = c.mc, c.mc.lib()

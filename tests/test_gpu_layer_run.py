@@ -243,3 +243,46 @@ def test_rows_past_four_gigabytes(L):
         assert torch.equal(kept_k[:, h], kd[kept_pos[:, h], h])
         order = sorted(range(n), key=lambda i: (i <= n - 1 - 8, -got[i, h].item(), i))[:100]
         assert set(kept_pos[:, h].tolist()) == set(order)
+
+
+@pytest.mark.parametrize("graph", [False, True])
+def test_new_lengths_passed_straight_on(L, graph):
+    """The eviction's new lengths as the lengths of the next calls, two buffers in turn, without a kernel between: the same
+    bits as with the device idle after every call."""
+    lens, budget, steps = [700, 90, 1300], 64, 6
+    got = []
+    for wait in (True, False):
+        c = L.Cache(lens, 4, 16, 16, "bf16", seed=21, marks=True, weights=True, poison=False)
+        mc, lib = c.mc, c.mc.lib()
+        pos = torch.tensor(c.q_next, dtype=torch.int32, device="cuda")
+        bufs = [c.d_lens.clone(), torch.zeros_like(c.d_lens)]
+        batches = [mc.Batch(c.d["table"], x, c.max_len, c.n_pages) for x in bufs]
+        ws = torch.zeros(max(lib.mc_layer_workspace_bytes(c.cfg, c.batch, op, arg)
+                             for op, arg in ((mc.MC_OP_LAYER_ATTN, 2), (mc.MC_OP_LAYER_OBSERVE, 8), (mc.MC_OP_LAYER_EVICT, 0))),
+                         dtype=torch.uint8, device="cuda")
+        q, q_obs = c.queries(3, 16).cuda(), c.queries(3, 8, 16).cuda()
+        outs = [torch.zeros_like(q) for _ in range(steps)]
+        score, less = mc.ScoreOpts(SM, q_pos=pos), [mc.EvictOpts(budget * (steps - i), 2, 8, pos) for i in range(steps)]
+
+        def run(pause):
+            for i in range(steps):
+                now, then = batches[i % 2], batches[1 - i % 2]
+                lib.mc_layer_evict(c.cfg, now, c.layer, less[i], bufs[1 - i % 2], ws)
+                pause()
+                lib.mc_layer_attn(c.cfg, then, c.layer, score, q, None, None, mc.MC_LAYER_ACCUMULATE, outs[i], None, ws)
+                pause()
+                lib.mc_layer_observe(c.cfg, then, c.layer, score, q_obs, mc.MC_LAYER_ACCUMULATE, ws)
+                pause()
+        torch.cuda.synchronize()
+        if wait or not graph:
+            run(torch.cuda.synchronize if wait else lambda: None)
+        else:
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g):
+                run(lambda: None)
+            g.replay()
+        torch.cuda.synchronize()
+        assert bufs[0].tolist() == [budget] * 3
+        got.append((torch.stack(outs), c.gathered("w", 0, budget), c.gathered("pos", 2, budget)))
+        assert lib.mc_layer_read_status(c.layer, check=False)[1] == 0
+    assert all(torch.equal(a, b) for a, b in zip(*got)) and torch.isfinite(got[0][0].float()).all()
