@@ -7,7 +7,6 @@ from __future__ import annotations
 
 import ctypes as C
 import dataclasses
-import operator
 import os
 from typing import Optional
 
@@ -155,6 +154,15 @@ class Batch:
         mp = self.block_table.shape[1] if self.block_table.dim() == 2 else 0
         return _Batch(_ptr(self.block_table), _ptr(self.seq_lens), b, mp, int(self.max_seq_len), 0, int(self.n_pages))
 
+    def layer_c(self) -> _Batch:
+        """c() for the mc_layer_* calls: a row of the block table for every sequence."""
+        bt, sl = self.block_table, self.seq_lens
+        shape, n = bt.shape, sl.numel()
+        assert len(shape) == 2 and shape[0] >= n, "block_table [batch][max_pages_per_seq] and seq_lens [batch] are wanted"
+        return _Batch(_held("block_table", bt, torch.int32, 0), _held("seq_lens", sl, torch.int32, 0), n, shape[1], self.max_seq_len, 0,
+                      self.n_pages)
+
+
 
 class PairCache:
     """Caller-owned device buffers of one compressed layer pair (allocated with torch)."""
@@ -295,15 +303,22 @@ class PairCache:
         return sum(t.numel() * t.element_size() for t in ts)
 
 
-def _typed(name: str, t: Optional[torch.Tensor], dtype) -> Optional[int]:
-    assert t is None or (t.dtype == dtype and t.is_contiguous()), f"{name}: a contiguous {dtype} tensor is wanted"
-    return _ptr(t)
+def _held(name: str, t: Optional[torch.Tensor], dtype, n: int) -> Optional[int]:
+    """Address of a contiguous tensor of at least n elements, or None."""
+    if t is None:
+        return None
+    assert t.dtype is dtype and t.is_contiguous(), f"{name}: a contiguous {dtype} tensor is wanted"
+    assert t.numel() >= n, f"{name}: at least {n} entries are wanted"
+    return t.data_ptr()
 
 
-def _checked(owner, tensors, sizes) -> bool:
-    """Whether `owner`'s tensors have to be checked (again): not if they are the same objects as at its last call."""
-    last = getattr(owner, "_seen", None)
-    return last is None or last[1] != sizes or not all(map(operator.is_, last[0], tensors))
+def _layer_stream(stream, tensors) -> Optional[int]:
+    """The stream of a mc_layer_* call, all of whose tensors have to be on the device that is current."""
+    devs = {t.get_device() for t in tensors if t is not None}
+    dev = devs.pop()
+    assert not devs and dev >= 0 and dev == torch.cuda.current_device(), "all tensors have to be on the current CUDA device"
+    # (the stream's handle itself: building a Stream object costs 1 us of a 10 us call)
+    return (torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream) or None
 
 
 _CFG = {}
@@ -336,17 +351,16 @@ class LayerCache:
         if self.status is None:
             self.status = torch.zeros(MC_STATUS_WORDS, dtype=torch.int32, device=self.k_pool.device)
 
-    def c(self, n_pages: int) -> _LayerCache:
-        k, v, pos, w, st = seen = (self.k_pool, self.v_pool, self.positions, self.weights, self.status)
-        if _checked(self, seen, n_pages):
-            dt, rows = self.cfg.torch_dtype, n_pages * self.cfg.n_kv_heads * self.cfg.page_size
-            for name, t, want, n in (("k_pool", k, dt, 128 * rows), ("v_pool", v, dt, 128 * rows), ("positions", pos, torch.int32, rows),
-                                     ("weights", w, torch.float32, rows), ("status", st, torch.int32, MC_STATUS_WORDS)):
-                _typed(name, t, want)
-                assert t is None or t.numel() >= n, f"{name} holds fewer than n_pages pages"
-            self._seen = (seen, n_pages)
-        return _LayerCache(k.data_ptr(), v.data_ptr(), None if pos is None else pos.data_ptr(), None if w is None else w.data_ptr(),
-                           st.data_ptr())
+    def tensors(self):
+        return self.k_pool, self.v_pool, self.positions, self.weights, self.status
+
+    def c(self, n_pages: int, cfg: Optional[McConfig] = None) -> _LayerCache:
+        """cfg: the call's configuration (default: the cache's own), which the pools have to hold n_pages pages of."""
+        cfg = cfg or self.cfg
+        dt, rows = cfg.torch_dtype, n_pages * cfg.n_kv_heads * cfg.page_size
+        return _LayerCache(_held("k_pool", self.k_pool, dt, 128 * rows), _held("v_pool", self.v_pool, dt, 128 * rows),
+                           _held("positions", self.positions, torch.int32, rows), _held("weights", self.weights, torch.float32, rows),
+                           _held("status", self.status, torch.int32, MC_STATUS_WORDS))
 
 
 @dataclasses.dataclass
@@ -361,17 +375,13 @@ class ScoreOpts:
     prefix_len: Optional[torch.Tensor] = None
     q_pos: Optional[torch.Tensor] = None
 
+    def tensors(self):
+        return self.alibi_slopes, self.doc_start, self.prefix_len, self.q_pos
+
     def c(self, cfg: McConfig, batch: int) -> _ScoreOpts:
-        a, d, p, q = seen = (self.alibi_slopes, self.doc_start, self.prefix_len, self.q_pos)
-        sizes = (cfg.n_q_heads, batch)
-        if _checked(self, seen, sizes):
-            for name, t, want, n in (("alibi_slopes", a, torch.float32, cfg.n_q_heads), ("doc_start", d, torch.int32, batch),
-                                     ("prefix_len", p, torch.int32, batch), ("q_pos", q, torch.int32, batch)):
-                _typed(name, t, want)
-                assert t is None or t.numel() >= n, f"{name} holds too few entries"
-            self._seen = (seen, sizes)
-        return _ScoreOpts(None if a is None else a.data_ptr(), None if d is None else d.data_ptr(), None if p is None else p.data_ptr(),
-                          None if q is None else q.data_ptr(), self.sm_scale, self.softcap, self.window, 0)
+        return _ScoreOpts(_held("alibi_slopes", self.alibi_slopes, torch.float32, cfg.n_q_heads),
+                          _held("doc_start", self.doc_start, torch.int32, batch), _held("prefix_len", self.prefix_len, torch.int32, batch),
+                          _held("q_pos", self.q_pos, torch.int32, batch), self.sm_scale, self.softcap, self.window, 0)
 
 
 @dataclasses.dataclass
@@ -383,8 +393,7 @@ class EvictOpts:
     q_pos: Optional[torch.Tensor] = None
 
     def c(self, batch: int) -> _EvictOpts:
-        assert self.q_pos is None or self.q_pos.numel() >= batch, "q_pos holds too few entries"
-        return _EvictOpts(_typed("q_pos", self.q_pos, torch.int32), int(self.budget), int(self.n_sink), int(self.n_recent), 0)
+        return _EvictOpts(_held("q_pos", self.q_pos, torch.int32, batch), int(self.budget), int(self.n_sink), int(self.n_recent), 0)
 
 
 class MiniCacheLib:
@@ -665,8 +674,9 @@ class MiniCacheLib:
     def mc_layer_attn(self, cfg: McConfig, batch: Batch, layer: LayerCache, opts: ScoreOpts, q, k_new, v_new, flags: int, out, lse,
                       workspace: torch.Tensor, stream=None):
         """q, out [batch][n_q_heads][128], k_new / v_new [batch][n_kv_heads][128] or None; flags: MC_LAYER_APPEND |
-        MC_LAYER_ACCUMULATE; lse [batch][n_q_heads] float32 or None."""
-        c, b = _cfg_c(cfg), batch.c()
+        MC_LAYER_ACCUMULATE; lse [batch][n_q_heads] float32 or None.  Every tensor of a mc_layer_* call has to be on the
+        device that is current (AssertionError)."""
+        c, b = _cfg_c(cfg), batch.layer_c()
         n, dt = b.batch, q.dtype
         rows_q, rows_kv = n * cfg.n_q_heads * 128, n * cfg.n_kv_heads * 128
         assert dt is cfg.torch_dtype, "q: the storage type is wanted"
@@ -674,10 +684,11 @@ class MiniCacheLib:
             assert t is None or (t.dtype is dt and t.numel() == rows and t.is_contiguous()), \
                 "contiguous rows of 128 channels per sequence and head are wanted"
         assert lse is None or (lse.dtype is torch.float32 and lse.numel() == n * cfg.n_q_heads and lse.is_contiguous()), "lse: float32 [batch][n_q_heads]"
-        l, o = layer.c(b.n_pages), opts.c(cfg, n)
+        l, o = layer.c(b.n_pages, cfg), opts.c(cfg, n)
+        at = _layer_stream(stream, (q, out, k_new, v_new, lse, workspace, batch.block_table, batch.seq_lens, *layer.tensors(), *opts.tensors()))
         code = self._lib.mc_layer_attn(c, b, l, o, q.data_ptr(), None if k_new is None else k_new.data_ptr(),
                                        None if v_new is None else v_new.data_ptr(), flags, out.data_ptr(),
-                                       None if lse is None else lse.data_ptr(), workspace.data_ptr(), workspace.nbytes, _stream(stream))
+                                       None if lse is None else lse.data_ptr(), workspace.data_ptr(), workspace.nbytes, at)
         if code:
             self._check(code)
 
@@ -685,22 +696,24 @@ class MiniCacheLib:
                          stream=None):
         """q [batch][n_obs][n_q_heads][128]: the last n_obs queries of every sequence; flags: 0 (weights are written) or
         MC_LAYER_ACCUMULATE (added to)."""
-        c, b = _cfg_c(cfg), batch.c()
+        c, b = _cfg_c(cfg), batch.layer_c()
         shape = q.shape
         assert len(shape) == 4 and shape[0] == b.batch and shape[2] == cfg.n_q_heads and shape[3] == 128, "q: [batch][n_obs][n_q_heads][128]"
         assert q.dtype is cfg.torch_dtype and q.is_contiguous(), "q: contiguous rows of the storage type are wanted"
-        l, o = layer.c(b.n_pages), opts.c(cfg, b.batch)
-        code = self._lib.mc_layer_observe(c, b, l, o, q.data_ptr(), shape[1], flags, workspace.data_ptr(), workspace.nbytes, _stream(stream))
+        l, o = layer.c(b.n_pages, cfg), opts.c(cfg, b.batch)
+        at = _layer_stream(stream, (q, workspace, batch.block_table, batch.seq_lens, *layer.tensors(), *opts.tensors()))
+        code = self._lib.mc_layer_observe(c, b, l, o, q.data_ptr(), shape[1], flags, workspace.data_ptr(), workspace.nbytes, at)
         if code:
             self._check(code)
 
     def mc_layer_evict(self, cfg: McConfig, batch: Batch, layer: LayerCache, opts: EvictOpts, new_lens: torch.Tensor,
                        workspace: torch.Tensor, stream=None):
-        """new_lens int32 [batch] receives min(seq_lens, budget); it must not share memory with batch.seq_lens."""
-        c, b = _cfg_c(cfg), batch.c()
+        """new_lens int32 [batch] receives min(seq_lens, budget); it must not share memory with batch.seq_lens or opts.q_pos."""
+        c, b = _cfg_c(cfg), batch.layer_c()
         assert new_lens.dtype is torch.int32 and new_lens.numel() == b.batch and new_lens.is_contiguous(), "new_lens: int32 [batch]"
-        l, o = layer.c(b.n_pages), opts.c(b.batch)
-        code = self._lib.mc_layer_evict(c, b, l, o, new_lens.data_ptr(), workspace.data_ptr(), workspace.nbytes, _stream(stream))
+        l, o = layer.c(b.n_pages, cfg), opts.c(b.batch)
+        at = _layer_stream(stream, (new_lens, workspace, batch.block_table, batch.seq_lens, *layer.tensors(), opts.q_pos))
+        code = self._lib.mc_layer_evict(c, b, l, o, new_lens.data_ptr(), workspace.data_ptr(), workspace.nbytes, at)
         if code:
             self._check(code)
 

@@ -162,3 +162,39 @@ def test_binding_refuses_tensors_of_another_type_or_size():
     for bad in (dict(alibi_slopes=torch.zeros(3)), dict(doc_start=torch.zeros(2)), dict(q_pos=torch.zeros(1, dtype=torch.int32))):
         with pytest.raises(AssertionError):
             mc.ScoreOpts(0.1, **bad).c(c, 2)
+
+
+def test_binding_checks_every_call_anew(lib):
+    """Against the call's own configuration, and again when a tensor it has seen has become smaller."""
+    small, wide = mc.McConfig(2, 4, 16, "f16"), mc.McConfig(4, 8, 16, "f16")
+    k = torch.zeros(3, 2, 16, 128, dtype=torch.float16)
+    layer = mc.LayerCache(small, k, k.clone(), status=torch.zeros(B.MC_STATUS_WORDS, dtype=torch.int32))
+    layer.c(3)
+    layer.c(3, small)
+    with pytest.raises(AssertionError):
+        layer.c(3, wide)
+    k.resize_(2, 2, 16, 128)
+    with pytest.raises(AssertionError):
+        layer.c(3)
+    pos = torch.zeros(2, dtype=torch.int32)
+    o = mc.ScoreOpts(0.1, q_pos=pos)
+    o.c(small, 2)
+    pos.resize_(1)
+    with pytest.raises(AssertionError):
+        o.c(small, 2)
+
+
+def test_binding_refuses_host_tensors_and_short_block_tables(lib):
+    c = mc.McConfig(2, 4, 16, "f16")
+    k = torch.zeros(3, 2, 16, 128, dtype=torch.float16)
+    layer = mc.LayerCache(c, k, k.clone(), torch.zeros(3, 2, 16, dtype=torch.int32), torch.zeros(3, 2, 16), torch.zeros(B.MC_STATUS_WORDS, dtype=torch.int32))
+    lens, ws = torch.tensor([5, 7], dtype=torch.int32), torch.zeros(1 << 20, dtype=torch.uint8)
+    q, new = torch.zeros(2, 4, 128, dtype=torch.float16), torch.zeros(2, dtype=torch.int32)
+    ok, short = (mc.Batch(torch.zeros(n, 1, dtype=torch.int32), lens, 16, 3) for n in (2, 1))
+    for batch in (ok, short):
+        with pytest.raises(AssertionError, match="CUDA device" if batch is ok else "block_table"):
+            lib.mc_layer_attn(c, batch, layer, mc.ScoreOpts(0.1), q, None, None, 0, q.clone(), None, ws)
+        with pytest.raises(AssertionError, match="CUDA device" if batch is ok else "block_table"):
+            lib.mc_layer_observe(c, batch, layer, mc.ScoreOpts(0.1), q[:, None], 0, ws)
+        with pytest.raises(AssertionError, match="CUDA device" if batch is ok else "block_table"):
+            lib.mc_layer_evict(c, batch, layer, mc.EvictOpts(4), new, ws)
