@@ -262,26 +262,46 @@ __global__ void __launch_bounds__(kEvThreads, 2) layer_evict_kernel(const __grid
     }
   }
   // ---- who stays; holes before the budget, movers behind it ------------------------------------------
+  const bool all_ties = want >= found[2];
   auto stay_word = [&](int w, int& t) -> uint32_t {
     const int i = 32 * w + lane;
     const uint32_t k = i < cnt ? key_at(i) : 0u;
+    if (all_ties) return __ballot_sync(0xffffffffu, i < cnt && k >= thr);
     const uint32_t eq = __ballot_sync(0xffffffffu, i < cnt && k == thr);
     const bool stay = i < cnt && (k > thr || (k == thr && t + __popc(eq & ((1u << lane) - 1u)) < want));
     t += __popc(eq);
     return __ballot_sync(0xffffffffu, stay);
   };
+  // 32 words of the run, a lane each: what follows from a word is worked out for 32 of them at once
+  auto stay_words = [&](int wb, int& t) -> uint32_t {
+    uint32_t own = 0;
+    const int live = min(32, w1 - wb);
+#pragma unroll 4
+    for (int j = 0; j < live; ++j) {
+      const uint32_t s = stay_word(wb + j, t);
+      if (lane == j) own = s;
+    }
+    return own;
+  };
+  auto split_word = [&](int w, uint32_t s, uint32_t& holes, uint32_t& movers) {
+    const int rel = p.budget - (i0 + 32 * w), valid = w < w1 ? cnt - 32 * w : 0;  // tokens of the word before the budget; in all
+    const uint32_t low = rel >= 32 ? 0xffffffffu : (rel <= 0 ? 0u : (1u << rel) - 1u);
+    const uint32_t here = valid >= 32 ? 0xffffffffu : (valid <= 0 ? 0u : (1u << valid) - 1u);
+    holes = ~s & low & here;
+    movers = s & ~low & here;
+  };
   Two mine = {0, 0};  // holes, movers
   int tie_w = tie;
-  for (int w = w0; w < w1; ++w) {
-    const uint32_t s = stay_word(w, tie_w);
-    if (held && lane == 0) mask[w] = s;
-    const int rel = p.budget - (i0 + 32 * w);  // tokens of this word before the budget
-    const uint32_t low = rel >= 32 ? 0xffffffffu : (rel <= 0 ? 0u : (1u << rel) - 1u);
-    const int valid = cnt - 32 * w;
-    const uint32_t here = valid >= 32 ? 0xffffffffu : (1u << valid) - 1u;
-    mine.a += __popc(~s & low & here);
-    mine.b += __popc(s & ~low);
+  for (int wb = w0; wb < w1; wb += 32) {
+    const uint32_t s = stay_words(wb, tie_w);
+    if (held && wb + lane < w1) mask[wb + lane] = s;
+    uint32_t holes, movers;
+    split_word(wb + lane, s, holes, movers);
+    mine.a += __popc(holes);
+    mine.b += __popc(movers);
   }
+  mine.a = __reduce_add_sync(0xffffffffu, mine.a);
+  mine.b = __reduce_add_sync(0xffffffffu, mine.b);
   Two sum;
   Two at = warp_prefix(mine, warp_s, warp, lane, sum);
   int n_moves = sum.b;
@@ -300,16 +320,28 @@ __global__ void __launch_bounds__(kEvThreads, 2) layer_evict_kernel(const __grid
   }
   int32_t* hole_l = p.lists + (size_t)seg * 2 * p.list_stride;
   int32_t* move_l = hole_l + p.list_stride;
-  for (int w = w0; w < w1; ++w) {
-    const uint32_t s = held ? mask[w] : stay_word(w, tie);
-    const int i = 32 * w + lane, t = i0 + i;
-    const bool stay = (s >> lane) & 1u;
-    const bool hole = i < cnt && t < p.budget && !stay, mover = stay && t >= p.budget;
-    const uint32_t hb = __ballot_sync(0xffffffffu, hole), mb = __ballot_sync(0xffffffffu, mover), lt = (1u << lane) - 1u;
-    if (hole) hole_l[at.a + __popc(hb & lt)] = t;
-    if (mover) move_l[at.b + __popc(mb & lt)] = t;
-    at.a += __popc(hb);
-    at.b += __popc(mb);
+  for (int wb = w0; wb < w1; wb += 32) {
+    const uint32_t s = !held ? stay_words(wb, tie) : (wb + lane < w1 ? mask[wb + lane] : 0u);
+    uint32_t holes, movers;
+    split_word(wb + lane, s, holes, movers);
+    const int both = __popc(holes) | __popc(movers) << 16;  // (sums of 32 words: at most 1024 each)
+    int incl = both;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int v = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += v;
+    }
+    const uint32_t lt = (1u << lane) - 1u;
+    const int live = min(32, w1 - wb), t0 = i0 + 32 * wb + lane;
+    for (int j = 0; j < live; ++j) {
+      const uint32_t hb = __shfl_sync(0xffffffffu, holes, j), mb = __shfl_sync(0xffffffffu, movers, j);
+      const int ahead = __shfl_sync(0xffffffffu, incl - both, j);
+      if ((hb >> lane) & 1u) hole_l[at.a + (ahead & 0xffff) + __popc(hb & lt)] = t0 + 32 * j;
+      if ((mb >> lane) & 1u) move_l[at.b + (ahead >> 16) + __popc(mb & lt)] = t0 + 32 * j;
+    }
+    const int sums = __shfl_sync(0xffffffffu, incl, 31);
+    at.a += sums & 0xffff;
+    at.b += sums >> 16;
   }
   if (C > 1) cl.sync();  // the lists are complete (and nobody touches another CTA's shared memory from here on)
   else __syncthreads();
