@@ -52,6 +52,7 @@ struct ObserveParams {
   float* part_ml;  // [(CTA + segment)][rows][slots][2]
   int n_obs, nq, n_q_heads;
   int rows;      // n_obs * nq
+  int nq_shift;  // nq = 1, 2, 4 or 8
   int nt;        // row tiles of 128: 1 or 2
   int slots;     // groups that share a row tile in pass 1: 4 / nt
   int rp, rep;   // rows of a copy (32, 64 or 128), copies in a row tile
@@ -66,22 +67,29 @@ struct ObserveParams {
   float tiny_max, small_max;
 };
 
-// A sequence as the call sees it: tiles that hold a token some query sees (the first `ua`, then those from `ub0`).
+// A sequence as the call sees it: tiles that hold a token some query sees (the first `ua`, then those from `ub0`).  Every
+// CTA keeps them in shared memory: a demand load takes microseconds behind the stream of keys.
 struct ObSeq {
   int n, last;
   int ua, ub0, u;
-  bool bad;
+  int prefix, doc;
 };
-__device__ __forceinline__ ObSeq ob_seq(const ObserveParams& p, int b) {
+__device__ __forceinline__ View ob_view(const ObserveParams& p, const ObSeq& s, int q_pos) {
+  return View{q_pos, s.prefix, p.rule.window > 0 ? max(s.doc, q_pos - p.rule.window + 1) : s.doc};
+}
+__device__ __forceinline__ ObSeq ob_seq(const ObserveParams& p, int b, int& bad) {
   ObSeq s;
   const int raw = __ldcg(p.g.seq_lens + b);  // (from L2: an eviction ahead in the stream may just have written it)
-  s.bad = raw < 0 || raw > p.g.max_seq_len;
+  const int at = p.rule.q_pos ? p.rule.q_pos[b] : 0;
+  s.prefix = p.rule.prefix_len ? p.rule.prefix_len[b] : 0;
+  s.doc = p.rule.doc_start ? p.rule.doc_start[b] : 0;
+  bad |= raw < 0 || raw > p.g.max_seq_len ? 1 : 0;
   s.n = min(max(raw, 0), p.g.max_seq_len);
-  s.last = min(max(p.rule.q_pos ? p.rule.q_pos[b] : s.n - 1, -1), kObNoToken - 1);
+  s.last = min(max(p.rule.q_pos ? at : s.n - 1, -1), kObNoToken - 1);
   s.ua = (s.n + kObTile - 1) / kObTile;
   s.ub0 = s.u = s.ua;
   if (p.positions == nullptr) {
-    const View first = view_at(p.rule, b, max(s.last - p.n_obs + 1, -1));  // the query that looks back furthest
+    const View first = ob_view(p, s, max(s.last - p.n_obs + 1, -1));  // the query that looks back furthest
     const int end = min(s.n - 1, s.last) + 1;
     const int a = max(min(end, first.prefix), 0), lo = max(first.lo_pos, a);
     s.ua = (a + kObTile - 1) / kObTile;
@@ -189,6 +197,7 @@ layer_observe_kernel(const __grid_constant__ ObserveParams p, const __grid_const
   int* view_s = reinterpret_cast<int*>(row_s + kObGroups * kObTile * 2);  // [groups][2][128]: pass 2: position, lowest position seen
   int* pos_s = view_s + kObGroups * kObTile * 2;                      // pass 1: [groups][128] positions; pass 2: [2 turns][groups][128] partial weights
   int* pre_s = pos_s + 2 * kObGroups * kObTile;                           // [batch + 1]
+  ObSeq* seq_s = reinterpret_cast<ObSeq*>(pre_s + p.g.batch + 1);     // [batch]
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int H = p.g.n_kv_heads, ps = p.g.page_size, shift = p.g.page_shift;
   const uint32_t full0 = smem_u32(bars), empty0 = full0 + 8 * kObMaxStages, qfull0 = empty0 + 8 * kObMaxStages, qempty0 = qfull0 + 16;
@@ -197,10 +206,14 @@ layer_observe_kernel(const __grid_constant__ ObserveParams p, const __grid_const
   const uint32_t sq0 = smem_u32(smem), sk0 = sq0 + kObQBufs * q_bytes;
   constexpr uint32_t tmem_cols = kObGroups * kObTile;
 
+  if (tid == kObThreads - 1) {
+    prefetch_map(&map_k);
+    prefetch_map(&map_q);
+  }
   int bad = 0;
   for (int b = tid; b < p.g.batch; b += kObThreads) {
-    const ObSeq s = ob_seq(p, b);
-    bad |= s.bad ? 1 : 0;
+    const ObSeq s = ob_seq(p, b, bad);
+    seq_s[b] = s;
     pre_s[b + 1] = s.u * H;
   }
   if (tid == 0) {
@@ -248,34 +261,48 @@ layer_observe_kernel(const __grid_constant__ ObserveParams p, const __grid_const
   const int cta = blockIdx.x;
   int x_begin = 0, n_x = 0;
   if (cta < T) {
-    x_begin = (int)(U * cta / T);
-    n_x = (int)(U * (cta + 1) / T) - x_begin;
+    const bool small = U * T <= 0xffffffffLL;  // (64-bit division is a hundred instructions)
+    x_begin = small ? (int)((uint32_t)U * (uint32_t)cta / (uint32_t)T) : (int)(U * cta / T);
+    n_x = (small ? (int)((uint32_t)U * (uint32_t)(cta + 1) / (uint32_t)T) : (int)(U * (cta + 1) / T)) - x_begin;
   }
   constexpr int DIR = PASS == 1 ? 1 : -1;
   const int s_mask = (1 << p.stage_shift) - 1;
   const int x_first = PASS == 1 ? x_begin : x_begin + n_x - 1;
+  // Rows of the pools where the pages of the next tiles begin, a lane per page, one window of 32 pages ahead: a load
+  // per tile would pace the stream by its latency.
+  const int ppt = kObTile >> shift, lane_tile = lane >> (7 - shift), lane_page = lane & (ppt - 1);
+  const int win_tiles = 32 >> (7 - shift);  // pages per tile: ppt; tiles per window
+  auto load_window = [&](int k0, int& head, bool& has) {
+    const int i = k0 + lane_tile;
+    head = 0;
+    has = false;
+    if (i >= n_x) return 0;
+    ObCursor d;
+    d.seek(pre_s, p.g.batch, H, x_first + DIR * i);
+    const ObSeq& q = seq_s[d.b];
+    const int t = (d.k < q.ua ? d.k : q.ub0 + d.k - q.ua) * kObTile + (lane_page << shift);
+    head = d.g;
+    has = t < q.n;
+    return has ? p.g.block_table[(size_t)d.b * p.g.max_pages_per_seq + (t >> shift)] : 0;
+  };
+  int head = 0, head_n = 0, page = 0, page_n = 0;
+  bool has = false, has_n = false;
+  if (warp == 3 + 4 * kObGroups) {  // (the block table is the caller's: read before the wait)
+    page = load_window(0, head, has);
+    page_n = load_window(win_tiles, head_n, has_n);
+  }
   grid_dep_wait();
   if (bad) atomicOr(p.status, MC_FLAG_BAD_METADATA);
 
   if (PASS == 1 && p.zero) {  // tokens that no query sees keep no weight: all are cleared, pass 2 adds
     for (int s = cta; s < p.g.batch * H; s += gridDim.x) {
       const int b = s / H, g = s - b * H;
-      const int n = min(max(p.g.seq_lens[b], 0), p.g.max_seq_len);
+      const int n = seq_s[b].n;
       for (int t = tid; t < n; t += kObThreads) {
         const int page = p.g.block_table[(size_t)b * p.g.max_pages_per_seq + (t >> shift)];
         if (page_ok(p.g, page)) p.weights[((size_t)page * H + g) * ps + (t & (ps - 1))] = 0.f;
       }
     }
-  }
-
-  if (PASS == 1 && n_x > 0) {
-    // a group without a tile in one of the CTA's segments leaves no part of it: cleared here (consecutive parts)
-    ObCursor a, z;
-    a.seek(pre_s, p.g.batch, H, x_begin);
-    z.seek(pre_s, p.g.batch, H, x_begin + n_x - 1);
-    const size_t per = (size_t)p.rows * p.slots * 2, lo = (size_t)(cta + a.b * H + a.g) * per, hi = (size_t)(cta + z.b * H + z.g + 1) * per;
-    for (size_t i = lo + tid; i < hi; i += kObThreads) p.part_ml[i] = 0.f;
-    __syncthreads();
   }
 
   // the step from tile to tile; `seg` tells that the next tile begins another segment
@@ -310,26 +337,6 @@ layer_observe_kernel(const __grid_constant__ ObserveParams p, const __grid_const
     }
   } else if (warp == 3 + 4 * kObGroups) {
     // ===================== K tiles =====================
-    // Rows of the pools where the pages of the next tiles begin, a lane per page, one window of 32 pages ahead: a load
-    // per tile would pace the stream by its latency.
-    const int ppt = kObTile >> shift, lane_tile = lane >> (7 - shift), lane_page = lane & (ppt - 1);
-    const int win_tiles = 32 >> (7 - shift);  // pages per tile: ppt; tiles per window
-    auto load_window = [&](int k0, int& head, bool& has) {
-      const int i = k0 + lane_tile;
-      head = 0;
-      has = false;
-      if (i >= n_x) return 0;
-      ObCursor d;
-      d.seek(pre_s, p.g.batch, H, x_first + DIR * i);
-      const ObSeq q = ob_seq(p, d.b);
-      const int t = (d.k < q.ua ? d.k : q.ub0 + d.k - q.ua) * kObTile + (lane_page << shift);
-      head = d.g;
-      has = t < q.n;
-      return has ? p.g.block_table[(size_t)d.b * p.g.max_pages_per_seq + (t >> shift)] : 0;
-    };
-    int head, head_n;
-    bool has, has_n;
-    int page = load_window(0, head, has), page_n = load_window(win_tiles, head_n, has_n);
     for (int i = 0; i < n_x; ++i) {
       const int in_win = i & (win_tiles - 1);
       if (in_win == 0 && i > 0) {
@@ -417,8 +424,8 @@ layer_observe_kernel(const __grid_constant__ ObserveParams p, const __grid_const
     int* pos_g = pos_s + grp * kObTile;
     const bool no_max = CAP && p.rule.cap_log2 <= 100.f && p.rule.slopes == nullptr;
     // pass 1: this lane's row, and the columns its copy takes
-    const int copy = gl / p.rp, c_n = kObTile / p.rep, c_lo = copy * c_n, r_own = gl % p.rp;
-    const bool live = r_own < n_rows, warp_live = (quad * 32) % p.rp < n_rows;
+    const int c_n = p.rp, c_lo = gl & ~(p.rp - 1), r_own = gl & (p.rp - 1);  // (copies of rp rows, 128 / rp of them: rp columns each)
+    const bool live = r_own < n_rows, warp_live = ((quad * 32) & (p.rp - 1)) < n_rows;
     View v0 = {}, vw = {};  // of the first query; pass 1: of this lane's row
     float m = 0.f, l = 0.f, slope = 0.f;
     int n = 0, skip = 0, ua = 0, easy_hi = 0, easy_pre = 0, easy_lo = 0;  // of the segment
@@ -426,13 +433,13 @@ layer_observe_kernel(const __grid_constant__ ObserveParams p, const __grid_const
     ObCursor c = {-1, 0, 0, 0};
 
     auto begin_segment = [&]() {
-      const ObSeq sq = ob_seq(p, c.b);
+      const ObSeq& sq = seq_s[c.b];
       n = sq.n;
       ua = sq.ua;
       skip = sq.ub0 - sq.ua;
       table = p.g.block_table + (size_t)c.b * p.g.max_pages_per_seq;
-      v0 = view_at(p.rule, c.b, max(sq.last - p.n_obs + 1, -1));
-      const View v1 = view_at(p.rule, c.b, sq.last);
+      v0 = ob_view(p, sq, max(sq.last - p.n_obs + 1, -1));
+      const View v1 = ob_view(p, sq, sq.last);
       // a tile that every query sees whole needs no masks: t0 <= easy_hi and (t0 <= easy_pre or t0 >= easy_lo)
       easy_hi = p.positions || p.rule.slopes ? -1 : min(n, v0.q_pos + 1) - kObTile;
       easy_pre = v0.prefix - kObTile;
@@ -441,22 +448,18 @@ layer_observe_kernel(const __grid_constant__ ObserveParams p, const __grid_const
         m = no_max ? 0.f : -INFINITY;
         l = 0.f;
         const int r = row0 + (live ? r_own : 0);
-        vw = view_at(p.rule, c.b, max(sq.last - p.n_obs + 1 + r / p.nq, -1));
-        slope = p.rule.slopes ? p.rule.slopes[c.g * p.nq + r % p.nq] * kLog2e : 0.f;
+        vw = ob_view(p, sq, max(sq.last - p.n_obs + 1 + (r >> p.nq_shift), -1));
+        slope = p.rule.slopes ? p.rule.slopes[c.g * p.nq + (r & (p.nq - 1))] * kLog2e : 0.f;
       } else {
         // -log-sum-exp of every row, from the partial sums of the CTAs (and their groups) that share the segment
         const long long x0 = pre_s[c.b] + (long long)c.g * c.u;
-        const int c0 = (int)(((x0 + 1) * T - 1) / U), c1 = (int)(((x0 + c.u) * T - 1) / U);
+        const long long y0 = (x0 + 1) * T - 1, y1 = (x0 + c.u) * T - 1;
+        const int c0 = y1 < 0xffffffffLL ? (int)((uint32_t)y0 / (uint32_t)U) : (int)(y0 / U);
+        const int c1 = y1 < 0xffffffffLL ? (int)((uint32_t)y1 / (uint32_t)U) : (int)(y1 / U);
         group_sync(grp);  // everybody has done with the segment before
         if (gl < n_rows) {
           const int r = row0 + gl;
           float mm = -INFINITY, ll = 0.f;
-          auto take = [&](float m2, float l2) {
-            if (l2 == 0.f) return;
-            const float M = fmaxf(mm, m2);
-            ll = (ll == 0.f ? 0.f : ll * ex2(mm - M)) + l2 * ex2(m2 - M);
-            mm = M;
-          };
           for (int cc = c0; cc <= c1; cc += 4) {  // the parts of four CTAs in flight
             float4 q[4][2];
 #pragma unroll
@@ -467,24 +470,45 @@ layer_observe_kernel(const __grid_constant__ ObserveParams p, const __grid_const
               q[e][0] = s4[0];
               if (p.slots == 4) q[e][1] = s4[1];
             }
+            float M = mm;  // (a part without a token has sum 0 and counts for nothing)
 #pragma unroll
             for (int e = 0; e < 4; ++e)
 #pragma unroll
               for (int k = 0; k < 2; ++k) {
-                take(q[e][k].x, q[e][k].y);
-                take(q[e][k].z, q[e][k].w);
+                if (q[e][k].y == 0.f) q[e][k].x = -INFINITY;
+                if (q[e][k].w == 0.f) q[e][k].z = -INFINITY;
+                M = fmaxf(M, fmaxf(q[e][k].x, q[e][k].z));
+              }
+            ll = ll == 0.f ? 0.f : ll * ex2(mm - M);
+            mm = M;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+              for (int k = 0; k < 2; ++k) {
+                if (q[e][k].y != 0.f) ll = fmaf(q[e][k].y, ex2(q[e][k].x - M), ll);
+                if (q[e][k].w != 0.f) ll = fmaf(q[e][k].w, ex2(q[e][k].z - M), ll);
               }
           }
           row_g[gl] = ll == 0.f ? -INFINITY : -(mm + log2f(ll));  // (a row that saw nothing gives nothing)
-          row_g[kObTile + gl] = p.rule.slopes ? p.rule.slopes[c.g * p.nq + r % p.nq] * kLog2e : 0.f;
-          const View v = view_at(p.rule, c.b, max(sq.last - p.n_obs + 1 + r / p.nq, -1));
+          row_g[kObTile + gl] = p.rule.slopes ? p.rule.slopes[c.g * p.nq + (r & (p.nq - 1))] * kLog2e : 0.f;
+          const View v = ob_view(p, sq, max(sq.last - p.n_obs + 1 + (r >> p.nq_shift), -1));
           row_q[gl] = v.q_pos;
           row_q[kObTile + gl] = v.lo_pos;
         }
         group_sync(grp);
       }
     };
+    // Pass 1: a segment of the CTA in which this group had no tile has an empty part of it.  (`filled`: the next segment
+    // without a part.  Clearing the CTA's parts beforehand took 5000 cycles before the first copy of keys.)
+    int filled = 0;
+    auto fill_to = [&](int seg) {
+      for (; filled < seg; ++filled)
+        if (gl < n_rows)
+          reinterpret_cast<float2*>(p.part_ml)[((size_t)(cta + filled) * p.rows + row0 + gl) * p.slots + mine] = make_float2(0.f, 0.f);
+    };
     auto end_segment = [&]() {  // pass 1: the copies of a row meet; one partial result per (CTA, segment, group)
+      fill_to(c.b * H + c.g);
+      ++filled;
       group_sync(grp);
       row_g[2 * gl] = l == 0.f ? -INFINITY : m;
       row_g[2 * gl + 1] = live ? l : 0.f;
@@ -501,6 +525,11 @@ layer_observe_kernel(const __grid_constant__ ObserveParams p, const __grid_const
       }
     };
 
+    if (PASS == 1 && n_x > 0) {
+      ObCursor a;
+      a.seek(pre_s, p.g.batch, H, x_begin);
+      filled = a.b * H + a.g;
+    }
     uint32_t turn = 0;  // tiles this group has taken
     for (int i = mine; i < n_x; i += stride, ++turn) {  // (to the end also after a wait that ran out: the barriers stay matched)
       if (c.b >= 0) c.k += DIR * stride;
@@ -526,12 +555,20 @@ layer_observe_kernel(const __grid_constant__ ObserveParams p, const __grid_const
       const bool good = __all_sync(0xffffffffu, mbar_wait_lean(my_full, turn & 1, s_abort, p.status));
       tc_fence_after();
       float w = 0.f;
+      bool released = false;
+      auto release = [&]() {  // the buffer, as soon as its last columns are in registers
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(my_empty);
+        released = true;
+      };
       if (good && PASS == 1 && warp_live) {
         uint64_t lr = pack2(l, 0.f);
 #pragma unroll 1
         for (int ch = c_lo; ch < c_lo + c_n; ch += kObChunk) {
           uint32_t raw[kObChunk];
           tmem_load(tbuf + ch, raw);
+          if (ch + kObChunk == c_lo + c_n) release();
           uint64_t f[kObChunk / 2];
           factors<CAP>(p, raw, f);
           if (!easy) {  // distance bias and masks: the scores themselves, factor 1
@@ -597,6 +634,7 @@ layer_observe_kernel(const __grid_constant__ ObserveParams p, const __grid_const
 #pragma unroll
           for (int k = 0; k < kObChunk / 4; ++k) z2[k] = reinterpret_cast<const ulonglong2*>(row_g + r0)[k];
           tmem_wait16(raw);
+          if (r0 + kObChunk >= n_rows) release();
           uint64_t f[kObChunk / 2];
           factors<CAP>(p, raw, f);
           if (easy && r0 + kObChunk <= n_rows) {
@@ -625,9 +663,7 @@ layer_observe_kernel(const __grid_constant__ ObserveParams p, const __grid_const
         unpack2(wb, b0, b1);
         w += (a0 + a1) + (b0 + b1);
       }
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(my_empty);
+      if (!released) release();
       if (PASS == 2) {
         if (p.nt == 2) {  // a token's partial weights meet; the next turn's barrier lies between this read and the slot's reuse
           float* part = reinterpret_cast<float*>(pos_s) + ((turn & 1) * kObGroups + grp - tt) * kObTile + gl;
@@ -638,7 +674,12 @@ layer_observe_kernel(const __grid_constant__ ObserveParams p, const __grid_const
         if (tt == 0 && page_ok(p.g, page)) p.weights[at] = (p.add ? p.weights[at] : 0.f) + w;
       }
     }
-    if (PASS == 1 && c.b >= 0) end_segment();
+    if (PASS == 1 && n_x > 0) {
+      if (c.b >= 0) end_segment();
+      ObCursor z;
+      z.seek(pre_s, p.g.batch, H, x_begin + n_x - 1);
+      fill_to(z.b * H + z.g + 1);
+    }
   }
   tc_fence_before();
   __syncthreads();
@@ -671,6 +712,7 @@ mc_status launch_layer_observe(const mc_config* cfg, const mc_batch* bt, const G
   op.nq = cfg->n_q_heads / cfg->n_kv_heads;
   op.n_q_heads = cfg->n_q_heads;
   op.rows = n_obs * op.nq;
+  op.nq_shift = op.nq == 1 ? 0 : op.nq == 2 ? 1 : op.nq == 4 ? 2 : 3;
   op.nt = op.rows > kObTile ? 2 : 1;
   op.slots = kObGroups / op.nt;
   op.rp = op.rows > 64 ? 128 : (op.rows > 32 ? 64 : 32);
@@ -698,7 +740,8 @@ mc_status launch_layer_observe(const mc_config* cfg, const mc_batch* bt, const G
   const uint64_t rows = (uint64_t)bt->n_pages * cfg->n_kv_heads * cfg->page_size;
   if (mc_status st = make_map(&map_k, cfg->dtype, layer->k_pool, rows, kHeadDim, cfg->page_size)) return st;
   if (mc_status st = make_map3(&map_q, cfg->dtype, q, (uint64_t)bt->batch * n_obs, cfg->n_q_heads, kHeadDim, op.jt, op.nq)) return st;
-  const size_t smem = 1024 + kObSmem + (2 * kObMaxStages + 4 + 2 * kObGroups) * 8 + 16 + kObGroups * kObTile * (2 * 8 + 8) + (size_t)(bt->batch + 1) * 4;
+  const size_t smem = 1024 + kObSmem + (2 * kObMaxStages + 4 + 2 * kObGroups) * 8 + 16 + kObGroups * kObTile * (2 * 8 + 8) + (size_t)(bt->batch + 1) * 4 +
+                      (size_t)bt->batch * sizeof(ObSeq);
   using Kernel = void (*)(const ObserveParams, const CUtensorMap, const CUtensorMap);
   static const Kernel kernels[2][2][2] = {
       {{layer_observe_kernel<MC_F16, 1, false>, layer_observe_kernel<MC_F16, 1, true>},
