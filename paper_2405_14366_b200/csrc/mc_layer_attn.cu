@@ -15,6 +15,7 @@
 // registers: D = K q^T (16 tokens x 8 query rows) becomes the B operand of V^T P by two 8x8 transposes (movmatrix).
 // Two stages of 8 KB per warp, 128 KB per SM: a third stage was SLOWER (7b batch 83 -> 88 us, 16 x 8192 grouped 87 ->
 // 93): more requests outstanding than the memory serves well.
+// Short sequences are not split: a CTA takes one whole and joins its warps' results itself (launch_layer_attn).
 // Where a slice's rows come from is worked out a lane per slice, 32 slices at a time and one window ahead: a
 // dependent load takes microseconds while the copies saturate the memory system.
 #include <algorithm>
@@ -56,6 +57,9 @@ struct LayerAttnParams {
   int nq, n_q_heads;
   int team_size, n_teams;
   int flags;
+  int direct;  // 0, or where in shared memory the warps of a CTA join their results: a team has one sequence, all of it
+  unsigned short* out;
+  float* lse;
 };
 
 // A sequence as the call sees it: its view, and the units that hold a visible token: the first `ua`, then those from
@@ -175,6 +179,8 @@ layer_attn_split_kernel(const __grid_constant__ LayerAttnParams p, const __grid_
   Seq* seq_s = reinterpret_cast<Seq*>(bars + kLaWarps * kLaStages);                     // [batch]
   int* pre_s = reinterpret_cast<int*>(seq_s + p.g.batch);                               // [batch + 1]
   volatile int* s_abort = pre_s + p.g.batch + 1;
+  float* join_o = reinterpret_cast<float*>(smem + p.direct);  // (direct) [warps][query rows][128]
+  float* join_ml = join_o + kLaWarps * p.nq * kHeadDim;        // [warps][query rows][2]
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int row = lane >> 2, t4 = lane & 3, colp = 2 * t4;
@@ -199,7 +205,10 @@ layer_attn_split_kernel(const __grid_constant__ LayerAttnParams p, const __grid_
   const int teams = live_teams(p, n_units);
   const int team = blockIdx.x / p.team_size, member = blockIdx.x % p.team_size;
   int x_begin = 0, x_end = 0;
-  if (team < teams) {
+  if (p.direct) {
+    x_begin = pre_s[team];
+    x_end = pre_s[team + 1];
+  } else if (team < teams) {
     x_begin = (int)((long long)n_units * team / teams);
     x_end = (int)((long long)n_units * (team + 1) / teams);
   }
@@ -285,6 +294,17 @@ layer_attn_split_kernel(const __grid_constant__ LayerAttnParams p, const __grid_
   {
     const int meta = __shfl_sync(0xffffffffu, win.meta, 0);
     if (n_slices > 0) load_q((meta >> 5) & 511, meta >> 14, q0, q2);
+  }
+
+  if (p.direct && nx == 0) {  // no token at all
+    for (int hd = 0; hd < n_heads; ++hd) {
+      const size_t orow = (size_t)team * p.n_q_heads + (member + hd * p.team_size) * nq;
+      for (int i = tid; i < nq * 16; i += kLaThreads) reinterpret_cast<uint4*>(p.out + orow * kHeadDim)[i] = make_uint4(0u, 0u, 0u, 0u);
+      if (tid < nq) {
+        if (p.lse != nullptr) p.lse[orow + tid] = -INFINITY;
+        if (p.scores != nullptr) p.lse2[orow + tid] = INFINITY;
+      }
+    }
   }
 
   float acc[8][4];
@@ -501,21 +521,56 @@ layer_attn_split_kernel(const __grid_constant__ LayerAttnParams p, const __grid_
         l1 += __shfl_xor_sync(0xffffffffu, l1, o);
       }
       const size_t prow = ((size_t)(team + b) * kLaWarps + warp) * p.n_q_heads + head * nq;
+      float* to = p.direct ? join_o + warp * nq * kHeadDim : p.part_o + prow * kHeadDim;
+      float* to_ml = p.direct ? join_ml + warp * nq * 2 : p.part_ml + 2 * prow;
       if (colp < nq) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          p.part_o[(prow + colp) * kHeadDim + 16 * j + row] = acc[j][0];
-          p.part_o[(prow + colp) * kHeadDim + 16 * j + row + 8] = acc[j][2];
+          to[colp * kHeadDim + 16 * j + row] = acc[j][0];
+          to[colp * kHeadDim + 16 * j + row + 8] = acc[j][2];
         }
-        if (row == 0) *reinterpret_cast<float2*>(p.part_ml + 2 * (prow + colp)) = make_float2(m0, l0);
+        if (row == 0) *reinterpret_cast<float2*>(to_ml + 2 * colp) = make_float2(m0, l0);
       }
       if (colp + 1 < nq) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          p.part_o[(prow + colp + 1) * kHeadDim + 16 * j + row] = acc[j][1];
-          p.part_o[(prow + colp + 1) * kHeadDim + 16 * j + row + 8] = acc[j][3];
+          to[(colp + 1) * kHeadDim + 16 * j + row] = acc[j][1];
+          to[(colp + 1) * kHeadDim + 16 * j + row + 8] = acc[j][3];
         }
-        if (row == 0) *reinterpret_cast<float2*>(p.part_ml + 2 * (prow + colp + 1)) = make_float2(m1, l1);
+        if (row == 0) *reinterpret_cast<float2*>(to_ml + 2 * (colp + 1)) = make_float2(m1, l1);
+      }
+      if (p.direct) {  // the four warps' results, joined as the combine kernel does it
+        __syncthreads();
+        for (int k = tid; k < nq * 32; k += kLaThreads) {
+          const int r = k >> 5, c4 = (k & 31) * 4;
+          float M = -INFINITY, L = 0.f;
+          float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+          for (int w = 0; w < kLaWarps; ++w) M = fmaxf(M, join_ml[(w * nq + r) * 2]);
+#pragma unroll
+          for (int w = 0; w < kLaWarps; ++w) {
+            const float2 ml = *reinterpret_cast<const float2*>(join_ml + (w * nq + r) * 2);
+            const float4 v = *reinterpret_cast<const float4*>(join_o + (w * nq + r) * kHeadDim + c4);
+            const float f = ml.y == 0.f ? 0.f : ex2(ml.x - M);
+            L = fmaf(f, ml.y, L);
+            o.x = fmaf(f, v.x, o.x);
+            o.y = fmaf(f, v.y, o.y);
+            o.z = fmaf(f, v.z, o.z);
+            o.w = fmaf(f, v.w, o.w);
+          }
+          const float inv = L == 0.f ? 0.f : 1.f / L;
+          const size_t orow = (size_t)b * p.n_q_heads + head * nq + r;
+          uint2 packed;
+          packed.x = Elem<DT>::pack(o.x * inv, o.y * inv);
+          packed.y = Elem<DT>::pack(o.z * inv, o.w * inv);
+          *reinterpret_cast<uint2*>(p.out + orow * kHeadDim + c4) = packed;
+          if (c4 == 0) {
+            const float z = L == 0.f ? -INFINITY : M + log2f(L);
+            if (p.lse != nullptr) p.lse[orow] = z * kLn2;
+            if (p.scores != nullptr) p.lse2[orow] = L == 0.f ? INFINITY : z;
+          }
+        }
+        __syncthreads();  // (before the next head's results take the same place)
       }
     }
   }
@@ -761,28 +816,39 @@ mc_status launch_layer_attn(const mc_config* cfg, const mc_batch* bt, const Geom
   ap.nq = cfg->n_q_heads / cfg->n_kv_heads;
   ap.n_q_heads = cfg->n_q_heads;
   ap.team_size = pl.team_size;
-  ap.n_teams = pl.n_teams;
   ap.flags = flags;
+  ap.out = (unsigned short*)out;
+  ap.lse = lse;
+  // Short sequences, one CTA (team member) for all of each: it writes the output itself and there is no second launch.
+  // That costs 2.2 us and 1.1 us per unit of the longest sequence, the split 3.9 us and 1.1 us per unit of a CTA's equal
+  // share (32 heads: one sequence of 33 tokens 3.3 against 4.9 us, of 127 4.6 against 5.2, of 255 6.8 against 4.9; nine of
+  // 255 8.3 against 10.1).  At most four units, as the lengths behind the bound may differ.
+  const long long slots = n_sm * kLaCtasPerSm, ctas = (long long)bt->batch * pl.team_size;
+  const bool direct = ctas <= slots && pl.seq_units <= 4 && 2 * (pl.seq_units * slots - std::max(slots, ctas * pl.seq_units)) <= 3 * slots;
+  ap.n_teams = direct ? bt->batch : pl.n_teams;
   // (asked for so much that two CTAs fill an SM: with room for a third, an early start behind another kernel packs some
   // SMs with three and leaves others with one -- 83 -> 86 us on 8 x 4096)
-  const size_t smem = std::max<size_t>(80 * 1024, 1024 + (size_t)kLaWarps * kLaStages * (kLaStageBytes + kLaSlice * 4 + 8) +
-                                                      (size_t)(bt->batch + 2) * (4 + sizeof(Seq)));
+  const size_t used = align_up((size_t)kLaWarps * kLaStages * (kLaStageBytes + kLaSlice * 4 + 8) + (size_t)(bt->batch + 2) * (4 + sizeof(Seq)), 16);
+  ap.direct = direct ? (int)used : 0;
+  const size_t smem = std::max<size_t>(80 * 1024, 1024 + used + (direct ? (size_t)kLaWarps * ap.nq * (kHeadDim + 2) * 4 : 0));
   auto* split = cfg->dtype == MC_F16 ? layer_attn_split_kernel<MC_F16> : layer_attn_split_kernel<MC_BF16>;
   MC_CUDA_CHECK(cudaFuncSetAttribute(split, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-  MC_CUDA_CHECK(launch_pdl(split, dim3(pl.n_teams * pl.team_size), dim3(kLaThreads), smem, stream, ap, map_k, map_v));
-  // warps per output row: about three parts each
-  const long long parts = (long long)kLaWarps * (pl.n_teams / bt->batch + 1);
-  int per_block = kLcWarps;  // rows
-  while (per_block > 1 && parts > 3 * (kLcWarps / per_block)) per_block /= 2;
-  using Combine = void (*)(const LayerAttnParams, unsigned short*, float*);
-  static const Combine combines[2][4] = {
-      {layer_attn_combine_kernel<MC_F16, 1>, layer_attn_combine_kernel<MC_F16, 2>, layer_attn_combine_kernel<MC_F16, 4>,
-       layer_attn_combine_kernel<MC_F16, 8>},
-      {layer_attn_combine_kernel<MC_BF16, 1>, layer_attn_combine_kernel<MC_BF16, 2>, layer_attn_combine_kernel<MC_BF16, 4>,
-       layer_attn_combine_kernel<MC_BF16, 8>}};
-  const Combine combine = combines[cfg->dtype == MC_F16 ? 0 : 1][per_block == 1 ? 0 : per_block == 2 ? 1 : per_block == 4 ? 2 : 3];
-  MC_CUDA_CHECK(launch_pdl(combine, dim3((cfg->n_q_heads + per_block - 1) / per_block, bt->batch), dim3(kLcThreads), 0, stream, ap,
-                           (unsigned short*)out, lse));
+  MC_CUDA_CHECK(launch_pdl(split, dim3(ap.n_teams * pl.team_size), dim3(kLaThreads), smem, stream, ap, map_k, map_v));
+  if (!direct) {
+    // warps per output row: about three parts each
+    const long long parts = (long long)kLaWarps * (pl.n_teams / bt->batch + 1);
+    int per_block = kLcWarps;  // rows
+    while (per_block > 1 && parts > 3 * (kLcWarps / per_block)) per_block /= 2;
+    using Combine = void (*)(const LayerAttnParams, unsigned short*, float*);
+    static const Combine combines[2][4] = {
+        {layer_attn_combine_kernel<MC_F16, 1>, layer_attn_combine_kernel<MC_F16, 2>, layer_attn_combine_kernel<MC_F16, 4>,
+         layer_attn_combine_kernel<MC_F16, 8>},
+        {layer_attn_combine_kernel<MC_BF16, 1>, layer_attn_combine_kernel<MC_BF16, 2>, layer_attn_combine_kernel<MC_BF16, 4>,
+         layer_attn_combine_kernel<MC_BF16, 8>}};
+    const Combine combine = combines[cfg->dtype == MC_F16 ? 0 : 1][per_block == 1 ? 0 : per_block == 2 ? 1 : per_block == 4 ? 2 : 3];
+    MC_CUDA_CHECK(launch_pdl(combine, dim3((cfg->n_q_heads + per_block - 1) / per_block, bt->batch), dim3(kLcThreads), 0, stream, ap,
+                             (unsigned short*)out, lse));
+  }
   if (flags & MC_LAYER_ACCUMULATE) {
     const int chunks = (pl.seq_units * kLaUnit + kLwTokens - 1) / kLwTokens, segs = bt->batch * cfg->n_kv_heads;
     const int blocks = std::min(chunks, (8 * n_sm + segs - 1) / segs);  // per (sequence, kv head)

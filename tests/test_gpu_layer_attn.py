@@ -126,6 +126,23 @@ def test_cap_and_bias(L, cap, alibi):
     run(L, [900, 65, 2], H=4, Hq=4, ps=16, dtype="bf16", alibi=alibi, marks=True, sm=-0.2)
 
 
+@pytest.mark.parametrize("H,Hq,ps", [(1, 1, 16), (32, 32, 16), (40, 80, 32), (64, 64, 16), (8, 64, 64), (3, 12, 16)])
+@pytest.mark.parametrize("marks", [False, True])
+def test_short_sequences(L, H, Hq, ps, marks):
+    """Up to a few hundred tokens: whole sequences per CTA, several kv heads per CTA, nothing to see, each kind of mask."""
+    run(L, [33], H=H, Hq=Hq, ps=ps, append=True, acc=True, marks=marks)
+    run(L, [0, 1, 62, 0, 63], H=H, Hq=Hq, ps=ps, dtype="bf16", append=True, acc=True, marks=marks, alibi=True)
+    run(L, [0, 17, 62, 63, 64], H=H, Hq=Hq, ps=ps, new=False, acc=True, marks=marks, cap=5.0)
+    run(L, [64, 127, 5], H=H, Hq=Hq, ps=ps, marks=marks, window=20, prefixes=[3, 0, 9], docs=[0, 10 ** 6, 2], append=True)
+    run(L, [130, 191, 0], H=H, Hq=Hq, ps=ps, dtype="bf16", new=False, marks=marks, window=64, prefixes=[70, 0, 0], docs=[100, 10 ** 6, 0])
+
+
+def test_short_sequences_that_fill_the_gpu(L):
+    for n in (60, 120, 180, 255):
+        run(L, [max(n - 7 * i, 0) for i in range(9)], H=32, Hq=32, ps=16, append=True, acc=True)
+    run(L, [255, 0, 3, 200, 64, 129] * 6, H=8, Hq=32, ps=32, dtype="bf16", marks=True, append=True, acc=True, alibi=True)
+
+
 def test_long_and_many(L):
     run(L, [20000], H=2, Hq=8, ps=64, dtype="bf16", alibi=True, marks=True, acc=True, append=True)
     run(L, [70 + 13 * i for i in range(64)], H=2, Hq=2, ps=16, append=True)
