@@ -20,6 +20,7 @@
 // group that was late kept the others waiting for their next product.  Bounds: the keys' bytes, twice, and the 2 R
 // exponentials per token (16 a clock and SM), with the cap's polynomial on the FMA pipe next to them; in fact the groups
 // wait for latencies most of the time.  Every wait is bounded; tensor memory is released on every path.
+#include <cooperative_groups.h>
 #include <math.h>
 
 #include <algorithm>
@@ -31,6 +32,7 @@
 #include "mc_tc.cuh"
 
 namespace mc {
+namespace cg = cooperative_groups;
 
 constexpr int kObTile = 128;                             // tokens per tile
 constexpr int kObHalf = kObTile * 128;                   // bytes of a tile's 64-channel half
@@ -180,6 +182,96 @@ __device__ __forceinline__ uint64_t ex2_both(uint64_t x) {
   float a, b;
   unpack2(x, a, b);
   return pack2(ex2(a), ex2(b));
+}
+
+// Pass 1: 16 columns (tokens at `pos`, looked at unless the tile is seen whole) of this thread's query row.
+template <bool CAP>
+__device__ __forceinline__ void add_columns(const ObserveParams& p, uint32_t (&raw)[kObChunk], bool easy, const int* pos, const View& vw,
+                                            float slope, bool no_max, float& m, uint64_t& lr) {
+  uint64_t f[kObChunk / 2];
+  factors<CAP>(p, raw, f);
+  if (!easy) {  // distance bias and masks: the scores themselves, factor 1
+#pragma unroll
+    for (int k = 0; k < kObChunk; ++k) {
+      const int pk = pos[k];
+      float fa, fb;
+      unpack2(f[k / 2], fa, fb);
+      const float s = __uint_as_float(raw[k]) * ((k & 1) ? fb : fa);
+      raw[k] = __float_as_uint(vw.sees(pk) ? fmaf(-slope, (float)(vw.q_pos - pk), s) : -INFINITY);
+      if (k & 1) f[k / 2] = pack2(1.f, 1.f);
+    }
+  }
+  if (!no_max) {
+    float mx;
+    if (CAP) {
+      float s[kObChunk];
+#pragma unroll
+      for (int k = 0; k < kObChunk; k += 2)
+        unpack2(mul2(pack2(__uint_as_float(raw[k]), __uint_as_float(raw[k + 1])), f[k / 2]), s[k], s[k + 1]);
+      mx = s[0];
+#pragma unroll
+      for (int k = 1; k < kObChunk; ++k) mx = fmaxf(mx, s[k]);
+    } else {
+      const float scale = easy ? p.rule.scale_log2 : 1.f;
+      mx = __uint_as_float(raw[0]);
+      if (scale >= 0.f) {
+#pragma unroll
+        for (int k = 1; k < kObChunk - 1; k += 2) mx = max3(mx, __uint_as_float(raw[k]), __uint_as_float(raw[k + 1]));
+        mx = fmaxf(mx, __uint_as_float(raw[kObChunk - 1]));
+      } else {
+#pragma unroll
+        for (int k = 1; k < kObChunk; ++k) mx = fminf(mx, __uint_as_float(raw[k]));
+      }
+      mx *= scale;
+    }
+    if (mx > m) {
+      const float g = ex2(m - mx);  // (l = 0 while m = -inf)
+      lr = mul2(lr, pack2(g, g));
+      m = mx;
+    }
+  }
+  const float mb = m == -INFINITY ? 0.f : m;
+  const uint64_t n2 = pack2(-mb, -mb);
+  uint64_t sum0 = 0, sum1 = 0;
+#pragma unroll
+  for (int k = 0; k < kObChunk; k += 4) {
+    sum0 = add2(sum0, ex2_both(fma2(pack2(__uint_as_float(raw[k]), __uint_as_float(raw[k + 1])), f[k / 2], n2)));
+    sum1 = add2(sum1, ex2_both(fma2(pack2(__uint_as_float(raw[k + 2]), __uint_as_float(raw[k + 3])), f[k / 2 + 1], n2)));
+  }
+  lr = add2(lr, add2(sum0, sum1));
+}
+// Pass 2: 16 query rows of this thread's token at `pos`, whose -log-sum-exps z2 holds.
+struct ObRows {
+  const float* neg_lse;
+  const float* slope;
+  const int* q_pos;
+  const int* lo_pos;
+  int live, prefix;
+};
+template <bool CAP>
+__device__ __forceinline__ void add_rows(const ObserveParams& p, uint32_t (&raw)[kObChunk], const ulonglong2 (&z2)[kObChunk / 4], bool easy,
+                                         const ObRows& rows, int pos, uint64_t& wa, uint64_t& wb, float& w) {
+  uint64_t f[kObChunk / 2];
+  factors<CAP>(p, raw, f);
+  if (easy && rows.live == kObChunk) {
+#pragma unroll
+    for (int k = 0; k < kObChunk; k += 4) {
+      const ulonglong2 z = z2[k / 4];
+      wa = add2(wa, ex2_both(fma2(pack2(__uint_as_float(raw[k]), __uint_as_float(raw[k + 1])), f[k / 2], z.x)));
+      wb = add2(wb, ex2_both(fma2(pack2(__uint_as_float(raw[k + 2]), __uint_as_float(raw[k + 3])), f[k / 2 + 1], z.y)));
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < kObChunk; ++k) {
+      if (k < rows.live) {
+        float fa, fb;
+        unpack2(f[k / 2], fa, fb);
+        const View v = {rows.q_pos[k], rows.prefix, rows.lo_pos[k]};
+        const float e = fmaf(-rows.slope[k], (float)(v.q_pos - pos), fmaf(__uint_as_float(raw[k]), (k & 1) ? fb : fa, rows.neg_lse[k]));
+        if (v.sees(pos)) w += ex2(e);
+      }
+    }
+  }
 }
 
 template <int DT, int PASS, bool CAP>
@@ -569,57 +661,7 @@ layer_observe_kernel(const __grid_constant__ ObserveParams p, const __grid_const
           uint32_t raw[kObChunk];
           tmem_load(tbuf + ch, raw);
           if (ch + kObChunk == c_lo + c_n) release();
-          uint64_t f[kObChunk / 2];
-          factors<CAP>(p, raw, f);
-          if (!easy) {  // distance bias and masks: the scores themselves, factor 1
-#pragma unroll
-            for (int k = 0; k < kObChunk; ++k) {
-              const int pk = pos_g[ch + k];
-              float fa, fb;
-              unpack2(f[k / 2], fa, fb);
-              const float s = __uint_as_float(raw[k]) * ((k & 1) ? fb : fa);
-              raw[k] = __float_as_uint(vw.sees(pk) ? fmaf(-slope, (float)(vw.q_pos - pk), s) : -INFINITY);
-              if (k & 1) f[k / 2] = pack2(1.f, 1.f);
-            }
-          }
-          if (!no_max) {
-            float mx;
-            if (CAP) {
-              float s[kObChunk];
-#pragma unroll
-              for (int k = 0; k < kObChunk; k += 2)
-                unpack2(mul2(pack2(__uint_as_float(raw[k]), __uint_as_float(raw[k + 1])), f[k / 2]), s[k], s[k + 1]);
-              mx = s[0];
-#pragma unroll
-              for (int k = 1; k < kObChunk; ++k) mx = fmaxf(mx, s[k]);
-            } else {
-              const float scale = easy ? p.rule.scale_log2 : 1.f;
-              mx = __uint_as_float(raw[0]);
-              if (scale >= 0.f) {
-#pragma unroll
-                for (int k = 1; k < kObChunk - 1; k += 2) mx = max3(mx, __uint_as_float(raw[k]), __uint_as_float(raw[k + 1]));
-                mx = fmaxf(mx, __uint_as_float(raw[kObChunk - 1]));
-              } else {
-#pragma unroll
-                for (int k = 1; k < kObChunk; ++k) mx = fminf(mx, __uint_as_float(raw[k]));
-              }
-              mx *= scale;
-            }
-            if (mx > m) {
-              const float g = ex2(m - mx);  // (l = 0 while m = -inf)
-              lr = mul2(lr, pack2(g, g));
-              m = mx;
-            }
-          }
-          const float mb = m == -INFINITY ? 0.f : m;
-          const uint64_t n2 = pack2(-mb, -mb);
-          uint64_t sum0 = 0, sum1 = 0;
-#pragma unroll
-          for (int k = 0; k < kObChunk; k += 4) {
-            sum0 = add2(sum0, ex2_both(fma2(pack2(__uint_as_float(raw[k]), __uint_as_float(raw[k + 1])), f[k / 2], n2)));
-            sum1 = add2(sum1, ex2_both(fma2(pack2(__uint_as_float(raw[k + 2]), __uint_as_float(raw[k + 3])), f[k / 2 + 1], n2)));
-          }
-          lr = add2(lr, add2(sum0, sum1));
+          add_columns<CAP>(p, raw, easy, pos_g + ch, vw, slope, no_max, m, lr);
         }
         float la, lb;
         unpack2(lr, la, lb);
@@ -635,28 +677,8 @@ layer_observe_kernel(const __grid_constant__ ObserveParams p, const __grid_const
           for (int k = 0; k < kObChunk / 4; ++k) z2[k] = reinterpret_cast<const ulonglong2*>(row_g + r0)[k];
           tmem_wait16(raw);
           if (r0 + kObChunk >= n_rows) release();
-          uint64_t f[kObChunk / 2];
-          factors<CAP>(p, raw, f);
-          if (easy && r0 + kObChunk <= n_rows) {
-#pragma unroll
-            for (int k = 0; k < kObChunk; k += 4) {
-              const ulonglong2 z = z2[k / 4];
-              wa = add2(wa, ex2_both(fma2(pack2(__uint_as_float(raw[k]), __uint_as_float(raw[k + 1])), f[k / 2], z.x)));
-              wb = add2(wb, ex2_both(fma2(pack2(__uint_as_float(raw[k + 2]), __uint_as_float(raw[k + 3])), f[k / 2 + 1], z.y)));
-            }
-          } else {
-#pragma unroll
-            for (int k = 0; k < kObChunk; ++k) {
-              const int r = r0 + k;
-              if (r < n_rows) {
-                float fa, fb;
-                unpack2(f[k / 2], fa, fb);
-                const View v = {row_q[r], v0.prefix, row_q[kObTile + r]};
-                const float e = fmaf(-row_g[kObTile + r], (float)(v.q_pos - pos), fmaf(__uint_as_float(raw[k]), (k & 1) ? fb : fa, row_g[r]));
-                if (v.sees(pos)) w += ex2(e);
-              }
-            }
-          }
+          const ObRows rows = {row_g + r0, row_g + kObTile + r0, row_q + r0, row_q + kObTile + r0, min(n_rows - r0, kObChunk), v0.prefix};
+          add_rows<CAP>(p, raw, z2, easy, rows, pos, wa, wb, w);
         }
         float a0, a1, b0, b1;
         unpack2(wa, a0, a1);
@@ -683,6 +705,227 @@ layer_observe_kernel(const __grid_constant__ ObserveParams p, const __grid_const
   }
   tc_fence_before();
   __syncthreads();
+  if (*s_abort) {  // let copies in flight land before the CTA's memory is released
+    for (int k = 0; k < 2000; ++k) __nanosleep(1000);
+  }
+  if (warp == 1) tmem_dealloc(tmem_d, tmem_cols);
+}
+
+// ---- short prompts: both passes in one launch -------------------------------------------------------
+// A cluster per (sequence, kv head), a CTA per 128 tokens.  Both products of a CTA's tile are issued at once (they need
+// nothing from each other: 256 accumulator columns per 128 rows) and the keys are read once; the row sums of the CTAs meet
+// through distributed shared memory between the two halves of the arithmetic.  Tiles are not left out here: one that no
+// query sees gets its weights, zeros, from the CTA that has it.
+constexpr int kOsMaxCluster = 8;
+constexpr int kOsThreads = kObGroups * 128;
+constexpr int kOsRows = 2 * kObTile;
+constexpr int kOsArrays = kOsMaxCluster * kOsRows * 8 + kOsRows * 16 + kObGroups * kObTile * 8 + kObTile * 4 + kObGroups * kObTile * 4;
+
+template <int DT, bool CAP>
+__global__ void __launch_bounds__(kOsThreads, 1)
+layer_observe_short_kernel(const __grid_constant__ ObserveParams p, const __grid_constant__ CUtensorMap map_k,
+                           const __grid_constant__ CUtensorMap map_q) {
+  cg::cluster_group cl = cg::this_cluster();
+  const int C = (int)cl.num_blocks(), rank = (int)cl.block_rank();
+  extern __shared__ unsigned char smem_raw[];
+  unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  float2* all_s = reinterpret_cast<float2*>(smem + (1 + p.nt) * kObTileBytes);  // [CTA of the cluster][rows] (m, l), written by the cluster
+  float* neg_lse = reinterpret_cast<float*>(all_s + kOsMaxCluster * kOsRows);   // [rows], then slopes, positions, lowest positions seen
+  float* slope_s = neg_lse + kOsRows;
+  int* qpos_s = reinterpret_cast<int*>(slope_s + kOsRows);
+  int* lo_s = qpos_s + kOsRows;
+  float2* part_s = reinterpret_cast<float2*>(lo_s + kOsRows);  // [groups][128] (m, l) of the lanes
+  int* pos_s = reinterpret_cast<int*>(part_s + kObGroups * kObTile);  // [128]
+  float* w_s = reinterpret_cast<float*>(pos_s + kObTile);             // [groups][128]
+  __shared__ uint64_t bars[3];  // operands, products of pass 1, of pass 2
+  __shared__ uint32_t tmem_slot;
+  __shared__ volatile int abort_s;
+  volatile int* s_abort = &abort_s;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int H = p.g.n_kv_heads, ps = p.g.page_size, shift = p.g.page_shift;
+  const int seg = blockIdx.x / C, b = seg / H, head = seg - b * H;
+  const uint32_t full = smem_u32(bars), done1 = full + 8, done2 = full + 16;
+  const uint32_t sk = smem_u32(smem), sq = sk + kObTileBytes;
+  const int q_half = p.nt * kObHalf;
+  const uint32_t tmem_cols = p.nt * 2 * kObTile;
+
+  if (tid == 0) {
+    prefetch_map(&map_k);
+    prefetch_map(&map_q);
+    for (int k = 0; k < 3; ++k) mbar_init(full + 8 * k, 1);
+    abort_s = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) tmem_alloc(smem_u32(&tmem_slot), tmem_cols);
+  int bad = 0;
+  const ObSeq s = ob_seq(p, b, bad);
+  const int t0 = rank * kObTile, n = s.n;
+  const bool live = t0 < n;  // (the whole CTA)
+  const int32_t* table = p.g.block_table + (size_t)b * p.g.max_pages_per_seq;
+  // warp 0: the tile's pages, a lane each; every thread of the first group: its token's
+  const bool has = warp == 0 && lane < (kObTile >> shift) && t0 + (lane << shift) < n;
+  const int copy_page = has ? table[(t0 >> shift) + lane] : 0;
+  const int page = tid < kObTile && t0 + tid < n ? table[(t0 + tid) >> shift] : -1;
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_d = tmem_slot;
+  cl.barrier_arrive();
+  grid_dep_launch();  // (not before the tensor memory is ours: a kernel behind that took it first would wait for this one)
+  grid_dep_wait();
+  if (bad && rank == 0 && head == 0 && tid == 0) atomicOr(p.status, MC_FLAG_BAD_METADATA);
+
+  if (live && warp == 0) {
+    const int n_copy = __popc(__ballot_sync(0xffffffffu, has));
+    if (lane == 0) mbar_expect_tx(full, (uint32_t)(n_copy * 2 * ps * 128 + 2 * p.nt * p.rep * p.jt * p.nq * 128));
+    __syncwarp();
+    if (has) {
+      int pg = copy_page;
+      if (!page_ok(p.g, pg)) {  // never an address: page 0 is read in its place and the call flagged
+        atomicOr(p.status, MC_FLAG_BAD_METADATA);
+        pg = 0;
+      }
+      const int y = (pg * H + head) * ps;
+      const uint32_t to = sk + lane * ps * 128;
+      tma_load_2d(to, &map_k, 0, y, full);
+      tma_load_2d(to + kObHalf, &map_k, 64, y, full);
+    }
+    if (lane < 2 * p.nt * p.rep) {
+      const int h = lane & 1, r = (lane >> 1) % p.rep, tt = (lane >> 1) / p.rep;
+      tma_load_3d(sq + h * q_half + (tt * kObTile + r * p.rp) * 128, &map_q, 64 * h, head * p.nq, b * p.n_obs + tt * p.jt, full);
+    }
+    __syncwarp();
+    if (lane == 0 && mbar_wait_lean(full, 0, s_abort, p.status)) {
+      tc_fence_after();
+      const uint64_t d0 = smem_desc_k128(0);
+#pragma unroll
+      for (int pass = 1; pass <= 2; ++pass) {
+        for (int tt = 0; tt < p.nt; ++tt) {
+          const int n_cols = pass == 1 ? kObTile : (min(p.rows - tt * kObTile, kObTile) + 15) / 16 * 16;
+          const uint32_t idesc = umma_idesc<DT, 8>() - (1u << 17) + ((uint32_t)(n_cols >> 3) << 17);
+          const uint32_t d = tmem_d + ((pass - 1) * p.nt + tt) * kObTile;
+#pragma unroll
+          for (int k = 0; k < kHeadDim / 16; ++k) {
+            const uint64_t dq = d0 + (uint64_t)((sq + tt * kObHalf + (k >> 2) * q_half) >> 4) + (uint64_t)(2 * (k & 3));
+            const uint64_t dk = d0 + (uint64_t)((sk + (k >> 2) * kObHalf) >> 4) + (uint64_t)(2 * (k & 3));
+            if (pass == 1) umma_f16(d, dq, dk, idesc, k > 0 ? 1u : 0u);
+            else umma_f16(d, dk, dq, idesc, k > 0 ? 1u : 0u);
+          }
+        }
+        umma_commit(pass == 1 ? done1 : done2);
+      }
+    }
+    __syncwarp();
+  }
+
+  // with one row tile the four groups share its columns (pass 1) and rows (pass 2), with two a pair of groups has each
+  const int grp = warp >> 2, quad = warp & 3, gl = quad * 32 + lane;
+  const int tt = p.nt == 1 ? 0 : grp & 1, share = p.nt == 1 ? grp : grp >> 1, shares = kObGroups / p.nt;
+  const int row0 = tt * kObTile, n_rows = min(p.rows - row0, kObTile);
+  const uint32_t tbuf = tmem_d + ((uint32_t)(quad * 32) << 16);
+  const bool no_max = CAP && p.rule.cap_log2 <= 100.f && p.rule.slopes == nullptr;
+  const View v0 = ob_view(p, s, max(s.last - p.n_obs + 1, -1)), v1 = ob_view(p, s, s.last);
+  const bool easy = !p.positions && !p.rule.slopes && t0 + kObTile <= min(n, v0.q_pos + 1) && (t0 + kObTile <= v0.prefix || t0 >= v1.lo_pos);
+  const int at = (page * H + head) * ps + ((t0 + tid) & (ps - 1));  // (of the first group's tokens)
+  if (tid < kObTile) {
+    int pos = t0 + tid < n ? t0 + tid : kObNoToken;
+    if (p.positions && page_ok(p.g, page)) pos = p.positions[at];
+    pos_s[tid] = pos;
+  }
+  if (tid < p.rows) {  // what pass 2 has to know of a row
+    const View v = ob_view(p, s, max(s.last - p.n_obs + 1 + (tid >> p.nq_shift), -1));
+    qpos_s[tid] = v.q_pos;
+    lo_s[tid] = v.lo_pos;
+    slope_s[tid] = p.rule.slopes ? p.rule.slopes[head * p.nq + (tid & (p.nq - 1))] * kLog2e : 0.f;
+  }
+  __syncthreads();
+
+  // ---- pass 1: the lane's query row, a share of the columns that its copy takes
+  float m = no_max ? 0.f : -INFINITY, l = 0.f;
+  bool good = true;
+  if (live) {
+    good = __all_sync(0xffffffffu, mbar_wait_lean(done1, 0, s_abort, p.status));
+    tc_fence_after();
+    const int c_lo = gl & ~(p.rp - 1), r_own = gl & (p.rp - 1);
+    if (good && ((quad * 32) & (p.rp - 1)) < n_rows) {
+      const int r = row0 + min(r_own, n_rows - 1);
+      const View vw = {qpos_s[r], s.prefix, lo_s[r]};
+      uint64_t lr = 0;
+#pragma unroll 1
+      for (int ch = c_lo + share * kObChunk; ch < c_lo + p.rp; ch += shares * kObChunk) {
+        uint32_t raw[kObChunk];
+        tmem_load(tbuf + tt * kObTile + ch, raw);
+        add_columns<CAP>(p, raw, easy, pos_s + ch, vw, slope_s[r], no_max, m, lr);
+      }
+      float la, lb;
+      unpack2(lr, la, lb);
+      l = la + lb;
+    }
+  }
+  part_s[grp * kObTile + gl] = make_float2(l == 0.f ? -INFINITY : m, l);
+  __syncthreads();
+  // ---- a row's parts: of the CTA's groups and copies, then of the cluster's CTAs
+  cl.barrier_wait();  // (every CTA of the cluster runs: its shared memory may be written)
+  if (tid < p.rows) {
+    const int row_tile = tid / kObTile, r = tid % kObTile;
+    float mm = -INFINITY, ll = 0.f;
+    for (int k = 0; k < shares * p.rep; ++k) {
+      const int g = p.nt == 1 ? k / p.rep : 2 * (k / p.rep) + row_tile;
+      const float2 e = part_s[g * kObTile + (k % p.rep) * p.rp + r];
+      if (e.y == 0.f) continue;
+      const float M = fmaxf(mm, e.x);
+      ll = (ll == 0.f ? 0.f : ll * ex2(mm - M)) + e.y * ex2(e.x - M);
+      mm = M;
+    }
+    for (int c = 0; c < C; ++c) *cl.map_shared_rank(all_s + rank * kOsRows + tid, c) = make_float2(mm, ll);
+  }
+  cl.sync();
+  if (tid < p.rows) {
+    float mm = -INFINITY, ll = 0.f;
+    for (int c = 0; c < C; ++c) {
+      const float2 e = all_s[c * kOsRows + tid];
+      if (e.y != 0.f) mm = fmaxf(mm, e.x);
+    }
+    for (int c = 0; c < C; ++c) {
+      const float2 e = all_s[c * kOsRows + tid];
+      if (e.y != 0.f) ll = fmaf(e.y, ex2(e.x - mm), ll);
+    }
+    neg_lse[tid] = ll == 0.f ? -INFINITY : -(mm + log2f(ll));  // (a row that saw nothing gives nothing)
+  }
+  __syncthreads();
+  // ---- pass 2: the lane's token, a share of the rows
+  float w = 0.f;
+  if (live) {
+    good = __all_sync(0xffffffffu, mbar_wait_lean(done2, 0, s_abort, p.status)) && good;
+    tc_fence_after();
+    if (good) {
+      const int pos = pos_s[gl];
+      uint64_t wa = 0, wb = 0;
+#pragma unroll 1
+      for (int r0 = share * kObChunk; r0 < n_rows; r0 += shares * kObChunk) {
+        uint32_t raw[kObChunk];
+        tmem_load(tbuf + (p.nt + tt) * kObTile + r0, raw);
+        ulonglong2 z2[kObChunk / 4];
+#pragma unroll
+        for (int k = 0; k < kObChunk / 4; ++k) z2[k] = reinterpret_cast<const ulonglong2*>(neg_lse + row0 + r0)[k];
+        const ObRows rows = {neg_lse + row0 + r0, slope_s + row0 + r0, qpos_s + row0 + r0, lo_s + row0 + r0, min(n_rows - r0, kObChunk), s.prefix};
+        add_rows<CAP>(p, raw, z2, easy, rows, pos, wa, wb, w);
+      }
+      float a0, a1, b0, b1;
+      unpack2(wa, a0, a1);
+      unpack2(wb, b0, b1);
+      w += (a0 + a1) + (b0 + b1);
+    }
+  }
+  w_s[grp * kObTile + gl] = w;
+  tc_fence_before();
+  __syncthreads();
+  if (tid < kObTile && page_ok(p.g, page)) {
+    float sum = 0.f;
+#pragma unroll
+    for (int g = 0; g < kObGroups; ++g) sum += w_s[g * kObTile + tid];
+    p.weights[at] = (p.add ? p.weights[at] : 0.f) + sum;
+  }
   if (*s_abort) {  // let copies in flight land before the CTA's memory is released
     for (int k = 0; k < 2000; ++k) __nanosleep(1000);
   }
@@ -740,6 +983,34 @@ mc_status launch_layer_observe(const mc_config* cfg, const mc_batch* bt, const G
   const uint64_t rows = (uint64_t)bt->n_pages * cfg->n_kv_heads * cfg->page_size;
   if (mc_status st = make_map(&map_k, cfg->dtype, layer->k_pool, rows, kHeadDim, cfg->page_size)) return st;
   if (mc_status st = make_map3(&map_q, cfg->dtype, q, (uint64_t)bt->batch * n_obs, cfg->n_q_heads, kHeadDim, op.jt, op.nq)) return st;
+  const int tiles = (bt->max_seq_len + kObTile - 1) / kObTile;
+  if (tiles >= 1 && tiles <= kOsMaxCluster && (long long)bt->batch * cfg->n_kv_heads * tiles <= n_sm) {
+    op.add = (flags & MC_LAYER_ACCUMULATE) ? 1 : 0;
+    using Short = void (*)(const ObserveParams, const CUtensorMap, const CUtensorMap);
+    static const Short shorts[2][2] = {{layer_observe_short_kernel<MC_F16, false>, layer_observe_short_kernel<MC_F16, true>},
+                                       {layer_observe_short_kernel<MC_BF16, false>, layer_observe_short_kernel<MC_BF16, true>}};
+    const Short kern = shorts[cfg->dtype == MC_F16 ? 0 : 1][opts->softcap > 0.f ? 1 : 0];
+    // (more than half an SM's shared memory: two CTAs on one SM might wait for each other's tensor memory)
+    const size_t need = std::max<size_t>(1024 + (size_t)(1 + op.nt) * kObTileBytes + kOsArrays, 120 * 1024);
+    MC_CUDA_CHECK(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)need));
+    cudaLaunchConfig_t lc = {};
+    lc.gridDim = dim3((unsigned)(bt->batch * cfg->n_kv_heads * tiles));
+    lc.blockDim = dim3(kOsThreads);
+    lc.dynamicSmemBytes = need;
+    lc.stream = stream;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = tiles;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
+    lc.attrs = attr;
+    lc.numAttrs = 2;
+    MC_CUDA_CHECK(cudaLaunchKernelEx(&lc, kern, op, map_k, map_q));
+    MC_CUDA_CHECK(cudaGetLastError());
+    return MC_OK;
+  }
   const size_t smem = 1024 + kObSmem + (2 * kObMaxStages + 4 + 2 * kObGroups) * 8 + 16 + kObGroups * kObTile * (2 * 8 + 8) + (size_t)(bt->batch + 1) * 4 +
                       (size_t)bt->batch * sizeof(ObSeq);
   using Kernel = void (*)(const ObserveParams, const CUtensorMap, const CUtensorMap);
