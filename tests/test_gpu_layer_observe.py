@@ -102,6 +102,39 @@ def test_cap_and_bias(L, cap, alibi):
     run(L, [900, 65, 2], 64, H=2, Hq=8, ps=16, dtype="bf16", cap=cap, alibi=alibi, sm=-0.2)
 
 
+@pytest.mark.parametrize("marks", [False, True])
+@pytest.mark.parametrize("acc", [False, True])
+@pytest.mark.parametrize("window,prefix,doc", [(1, 0, 0), (7, 4, 0), (130, 0, 50), (64, 200, 0), (0, 17, 333), (0, 0, 10 ** 6),
+                                               (5, 3, 10 ** 6), (2 ** 31 - 1, 0, 0), (300, 2 ** 31 - 1, 9)])
+def test_masks_next_to_a_longer_prompt(L, window, prefix, doc, marks, acc):
+    """More than 1024 tokens in one of the sequences: the two launches."""
+    run(L, [700, 129, 1, 0, 1100], 20, H=2, Hq=8, ps=16, window=window, prefixes=[prefix] * 5, docs=[doc, doc // 2, 0, doc, 5], marks=marks,
+        acc=acc, dtype="bf16")
+    run(L, [1030, 129, 1, 0, 512], 40, H=2, Hq=8, ps=32, window=window, prefixes=[prefix] * 5, marks=marks, acc=acc)
+
+
+@pytest.mark.parametrize("cap", [0.0, 0.5, 50.0, 90.0])
+@pytest.mark.parametrize("alibi", [False, True])
+def test_cap_bias_and_positions_next_to_a_longer_prompt(L, cap, alibi):
+    run(L, [1300, 65, 2], 16, H=2, Hq=8, ps=32, cap=cap, alibi=alibi, acc=True)
+    run(L, [1300, 65, 2], 33, H=4, Hq=4, ps=16, dtype="bf16", cap=cap, alibi=alibi, marks=True, sm=3.0, scale=0.1)
+    run(L, [65, 1300, 2], 64, H=2, Hq=8, ps=16, dtype="bf16", cap=cap, alibi=alibi, sm=-0.2)
+    run(L, [1300, 200, 129], 20, H=2, Hq=8, ps=16, q_pos=[300, 10 ** 6, -1], cap=cap, alibi=alibi, window=90)
+
+
+@pytest.mark.parametrize("tiles", range(1, 9))
+def test_every_size_of_a_short_prompt(L, tiles):
+    """One to eight tiles of 128 tokens, whole, begun and just begun; rows of each layout."""
+    n = 128 * tiles
+    for H, Hq, J in ((2, 2, 32), (2, 8, 16), (1, 8, 12), (2, 8, 40)):
+        run(L, [n, n - 1, n - 127, max(n - 300, 0)], J, H=H, Hq=Hq, ps=64, dtype="bf16", acc=tiles % 2 == 0, marks=tiles % 3 == 0)
+
+
+def test_short_prompts_in_two_waves(L):
+    run(L, [512, 300, 1, 0, 511, 129, 400, 256], 32, H=8, Hq=32, ps=16, dtype="bf16", cap=30.0)
+    run(L, [1024, 0, 1000], 64, H=8, Hq=32, ps=16, alibi=True)
+
+
 def test_long_many_and_repeatable(L):
     run(L, [20001], 64, H=2, Hq=8, ps=64, dtype="bf16")
     run(L, [70 + 13 * i for i in range(64)], 32, H=2, Hq=2, ps=16)
