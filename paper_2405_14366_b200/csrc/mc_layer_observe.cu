@@ -713,16 +713,19 @@ layer_observe_kernel(const __grid_constant__ ObserveParams p, const __grid_const
 }
 
 // ---- short prompts: both passes in one launch -------------------------------------------------------
-// A cluster per (sequence, kv head), a CTA per 128 tokens.  Both products of a CTA's tile are issued at once (they need
-// nothing from each other: 256 accumulator columns per 128 rows) and the keys are read once; the row sums of the CTAs meet
-// through distributed shared memory between the two halves of the arithmetic.  Tiles are not left out here: one that no
-// query sees gets its weights, zeros, from the CTA that has it.
+// A cluster per (sequence, kv head); a CTA has one, two or four tiles of 128 tokens and reads their keys once.  Tensor
+// memory holds four products of 128 rows: with room for both, pass 2's are issued at once (they need nothing from pass 1),
+// else as soon as pass 1 is through with its own.  The four groups share out (tile, row tile) units, and a unit's columns
+// or rows where there are fewer units than groups; the row sums of the CTAs meet through distributed shared memory between
+// the two halves of the arithmetic.  Tiles are not left out here: one that no query sees gets its weights, zeros, from the
+// CTA that has it.
 constexpr int kOsMaxCluster = 8;
 constexpr int kOsThreads = kObGroups * 128;
 constexpr int kOsRows = 2 * kObTile;
-constexpr int kOsArrays = kOsMaxCluster * kOsRows * 8 + kOsRows * 16 + kObGroups * kObTile * 8 + kObTile * 4 + kObGroups * kObTile * 4;
+constexpr int kOsMaxTiles = 4;  // of a CTA; times row tiles: at most 4 as well
+constexpr int kOsArrays = kOsMaxCluster * kOsRows * 8 + kOsRows * 16 + kObGroups * kObTile * 8 + kOsMaxTiles * kObTile * 4 + kObGroups * kObTile * 4;
 
-template <int DT, bool CAP>
+template <int DT, bool CAP, int T>
 __global__ void __launch_bounds__(kOsThreads, 1)
 layer_observe_short_kernel(const __grid_constant__ ObserveParams p, const __grid_constant__ CUtensorMap map_k,
                            const __grid_constant__ CUtensorMap map_q) {
@@ -730,14 +733,14 @@ layer_observe_short_kernel(const __grid_constant__ ObserveParams p, const __grid
   const int C = (int)cl.num_blocks(), rank = (int)cl.block_rank();
   extern __shared__ unsigned char smem_raw[];
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  float2* all_s = reinterpret_cast<float2*>(smem + (1 + p.nt) * kObTileBytes);  // [CTA of the cluster][rows] (m, l), written by the cluster
+  float2* all_s = reinterpret_cast<float2*>(smem + (T + p.nt) * kObTileBytes);  // [CTA of the cluster][rows] (m, l), written by the cluster
   float* neg_lse = reinterpret_cast<float*>(all_s + kOsMaxCluster * kOsRows);   // [rows], then slopes, positions, lowest positions seen
   float* slope_s = neg_lse + kOsRows;
   int* qpos_s = reinterpret_cast<int*>(slope_s + kOsRows);
   int* lo_s = qpos_s + kOsRows;
   float2* part_s = reinterpret_cast<float2*>(lo_s + kOsRows);  // [groups][128] (m, l) of the lanes
-  int* pos_s = reinterpret_cast<int*>(part_s + kObGroups * kObTile);  // [128]
-  float* w_s = reinterpret_cast<float*>(pos_s + kObTile);             // [groups][128]
+  int* pos_s = reinterpret_cast<int*>(part_s + kObGroups * kObTile);  // [tiles][128]
+  float* w_s = reinterpret_cast<float*>(pos_s + T * kObTile);         // [groups][128]
   __shared__ uint64_t bars[3];  // operands, products of pass 1, of pass 2
   __shared__ uint32_t tmem_slot;
   __shared__ volatile int abort_s;
@@ -746,9 +749,11 @@ layer_observe_short_kernel(const __grid_constant__ ObserveParams p, const __grid
   const int H = p.g.n_kv_heads, ps = p.g.page_size, shift = p.g.page_shift;
   const int seg = blockIdx.x / C, b = seg / H, head = seg - b * H;
   const uint32_t full = smem_u32(bars), done1 = full + 8, done2 = full + 16;
-  const uint32_t sk = smem_u32(smem), sq = sk + kObTileBytes;
+  const uint32_t sk = smem_u32(smem), sq = sk + T * kObTileBytes;
   const int q_half = p.nt * kObHalf;
-  const uint32_t tmem_cols = p.nt * 2 * kObTile;
+  const int two = p.nt - 1, units = T << two;  // (1, 2 or 4)
+  const bool both = T == 1 || units <= 2;
+  const uint32_t tmem_cols = units == 1 ? 2 * kObTile : 4 * kObTile;
 
   if (tid == 0) {
     prefetch_map(&map_k);
@@ -760,13 +765,13 @@ layer_observe_short_kernel(const __grid_constant__ ObserveParams p, const __grid
   if (warp == 1) tmem_alloc(smem_u32(&tmem_slot), tmem_cols);
   int bad = 0;
   const ObSeq s = ob_seq(p, b, bad);
-  const int t0 = rank * kObTile, n = s.n;
-  const bool live = t0 < n;  // (the whole CTA)
+  const int t0 = rank * T * kObTile, n = s.n;
+  const int live = min(T, max(n - t0 + kObTile - 1, 0) / kObTile);  // tiles with a token
   const int32_t* table = p.g.block_table + (size_t)b * p.g.max_pages_per_seq;
-  // warp 0: the tile's pages, a lane each; every thread of the first group: its token's
-  const bool has = warp == 0 && lane < (kObTile >> shift) && t0 + (lane << shift) < n;
+  // warp 0: the tiles' pages, a lane each (32 at most); a thread per token: its token's
+  const bool has = warp == 0 && lane < T * (kObTile >> shift) && t0 + (lane << shift) < n;
   const int copy_page = has ? table[(t0 >> shift) + lane] : 0;
-  const int page = tid < kObTile && t0 + tid < n ? table[(t0 + tid) >> shift] : -1;
+  const int page = tid < T * kObTile && t0 + tid < n ? table[(t0 + tid) >> shift] : -1;
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -776,6 +781,25 @@ layer_observe_short_kernel(const __grid_constant__ ObserveParams p, const __grid
   grid_dep_wait();
   if (bad && rank == 0 && head == 0 && tid == 0) atomicOr(p.status, MC_FLAG_BAD_METADATA);
 
+  // (one thread)
+  auto products = [&](int pass, uint32_t done) {
+    const uint64_t d0 = smem_desc_k128(0);
+    for (int j = 0; j < (T == 1 ? 1 : live); ++j) {
+      for (int tt = 0; tt < p.nt; ++tt) {
+        const int n_cols = pass == 1 ? kObTile : (min(p.rows - tt * kObTile, kObTile) + 15) / 16 * 16;
+        const uint32_t idesc = umma_idesc<DT, 8>() - (1u << 17) + ((uint32_t)(n_cols >> 3) << 17);
+        const uint32_t d = tmem_d + ((j << two) + tt + (pass == 2 && both ? units : 0)) * kObTile;
+#pragma unroll
+        for (int k = 0; k < kHeadDim / 16; ++k) {
+          const uint64_t dq = d0 + (uint64_t)((sq + tt * kObHalf + (k >> 2) * q_half) >> 4) + (uint64_t)(2 * (k & 3));
+          const uint64_t dk = d0 + (uint64_t)((sk + j * kObTileBytes + (k >> 2) * kObHalf) >> 4) + (uint64_t)(2 * (k & 3));
+          if (pass == 1) umma_f16(d, dq, dk, idesc, k > 0 ? 1u : 0u);
+          else umma_f16(d, dk, dq, idesc, k > 0 ? 1u : 0u);
+        }
+      }
+    }
+    umma_commit(done);
+  };
   if (live && warp == 0) {
     const int n_copy = __popc(__ballot_sync(0xffffffffu, has));
     if (lane == 0) mbar_expect_tx(full, (uint32_t)(n_copy * 2 * ps * 128 + 2 * p.nt * p.rep * p.jt * p.nq * 128));
@@ -787,7 +811,8 @@ layer_observe_short_kernel(const __grid_constant__ ObserveParams p, const __grid
         pg = 0;
       }
       const int y = (pg * H + head) * ps;
-      const uint32_t to = sk + lane * ps * 128;
+      const int j = (lane << shift) / kObTile;
+      const uint32_t to = sk + j * kObTileBytes + ((lane << shift) - j * kObTile) * 128;
       tma_load_2d(to, &map_k, 0, y, full);
       tma_load_2d(to + kObHalf, &map_k, 64, y, full);
     }
@@ -798,37 +823,23 @@ layer_observe_short_kernel(const __grid_constant__ ObserveParams p, const __grid
     __syncwarp();
     if (lane == 0 && mbar_wait_lean(full, 0, s_abort, p.status)) {
       tc_fence_after();
-      const uint64_t d0 = smem_desc_k128(0);
 #pragma unroll
-      for (int pass = 1; pass <= 2; ++pass) {
-        for (int tt = 0; tt < p.nt; ++tt) {
-          const int n_cols = pass == 1 ? kObTile : (min(p.rows - tt * kObTile, kObTile) + 15) / 16 * 16;
-          const uint32_t idesc = umma_idesc<DT, 8>() - (1u << 17) + ((uint32_t)(n_cols >> 3) << 17);
-          const uint32_t d = tmem_d + ((pass - 1) * p.nt + tt) * kObTile;
-#pragma unroll
-          for (int k = 0; k < kHeadDim / 16; ++k) {
-            const uint64_t dq = d0 + (uint64_t)((sq + tt * kObHalf + (k >> 2) * q_half) >> 4) + (uint64_t)(2 * (k & 3));
-            const uint64_t dk = d0 + (uint64_t)((sk + (k >> 2) * kObHalf) >> 4) + (uint64_t)(2 * (k & 3));
-            if (pass == 1) umma_f16(d, dq, dk, idesc, k > 0 ? 1u : 0u);
-            else umma_f16(d, dk, dq, idesc, k > 0 ? 1u : 0u);
-          }
-        }
-        umma_commit(pass == 1 ? done1 : done2);
-      }
+      for (int pass = 1; pass <= 2; ++pass)
+        if (pass == 1 || both) products(pass, pass == 1 ? done1 : done2);
     }
     __syncwarp();
   }
 
-  // with one row tile the four groups share its columns (pass 1) and rows (pass 2), with two a pair of groups has each
+  // a group's unit: tile j, row tile tt; `shares` groups have the same
   const int grp = warp >> 2, quad = warp & 3, gl = quad * 32 + lane;
-  const int tt = p.nt == 1 ? 0 : grp & 1, share = p.nt == 1 ? grp : grp >> 1, shares = kObGroups / p.nt;
-  const int row0 = tt * kObTile, n_rows = min(p.rows - row0, kObTile);
+  const int unit = grp & (units - 1), j = unit >> two, tt = unit & two, shares = (kObGroups / T) >> two, share = grp / T >> two;
+  const int row0 = tt * kObTile, n_rows = min(p.rows - row0, kObTile), tj = t0 + j * kObTile;
   const uint32_t tbuf = tmem_d + ((uint32_t)(quad * 32) << 16);
   const bool no_max = CAP && p.rule.cap_log2 <= 100.f && p.rule.slopes == nullptr;
   const View v0 = ob_view(p, s, max(s.last - p.n_obs + 1, -1)), v1 = ob_view(p, s, s.last);
-  const bool easy = !p.positions && !p.rule.slopes && t0 + kObTile <= min(n, v0.q_pos + 1) && (t0 + kObTile <= v0.prefix || t0 >= v1.lo_pos);
-  const int at = (page * H + head) * ps + ((t0 + tid) & (ps - 1));  // (of the first group's tokens)
-  if (tid < kObTile) {
+  const bool easy = !p.positions && !p.rule.slopes && tj + kObTile <= min(n, v0.q_pos + 1) && (tj + kObTile <= v0.prefix || tj >= v1.lo_pos);
+  const int at = (page * H + head) * ps + ((t0 + tid) & (ps - 1));  // where the weight of token t0 + tid lives
+  if (tid < T * kObTile) {
     int pos = t0 + tid < n ? t0 + tid : kObNoToken;
     if (p.positions && page_ok(p.g, page)) pos = p.positions[at];
     pos_s[tid] = pos;
@@ -844,7 +855,7 @@ layer_observe_short_kernel(const __grid_constant__ ObserveParams p, const __grid
   // ---- pass 1: the lane's query row, a share of the columns that its copy takes
   float m = no_max ? 0.f : -INFINITY, l = 0.f;
   bool good = true;
-  if (live) {
+  if (j < live) {
     good = __all_sync(0xffffffffu, mbar_wait_lean(done1, 0, s_abort, p.status));
     tc_fence_after();
     const int c_lo = gl & ~(p.rp - 1), r_own = gl & (p.rp - 1);
@@ -855,8 +866,8 @@ layer_observe_short_kernel(const __grid_constant__ ObserveParams p, const __grid
 #pragma unroll 1
       for (int ch = c_lo + share * kObChunk; ch < c_lo + p.rp; ch += shares * kObChunk) {
         uint32_t raw[kObChunk];
-        tmem_load(tbuf + tt * kObTile + ch, raw);
-        add_columns<CAP>(p, raw, easy, pos_s + ch, vw, slope_s[r], no_max, m, lr);
+        tmem_load(tbuf + unit * kObTile + ch, raw);
+        add_columns<CAP>(p, raw, easy, pos_s + j * kObTile + ch, vw, slope_s[r], no_max, m, lr);
       }
       float la, lb;
       unpack2(lr, la, lb);
@@ -864,13 +875,19 @@ layer_observe_short_kernel(const __grid_constant__ ObserveParams p, const __grid
     }
   }
   part_s[grp * kObTile + gl] = make_float2(l == 0.f ? -INFINITY : m, l);
+  if (!both) tc_fence_before();
   __syncthreads();
+  if (!both && live && tid == 0 && good) {
+    tc_fence_after();
+    products(2, done2);
+  }
+  __syncwarp();
   // ---- a row's parts: of the CTA's groups and copies, then of the cluster's CTAs
   cl.barrier_wait();  // (every CTA of the cluster runs: its shared memory may be written)
   if (tid < p.rows) {
     const int row_tile = tid / kObTile, r = tid % kObTile;
     float mm = -INFINITY, ll = 0.f;
-    for (int k = 0; k < shares * p.rep; ++k) {
+    for (int k = 0; k < (kObGroups >> two) * p.rep; ++k) {
       const int g = p.nt == 1 ? k / p.rep : 2 * (k / p.rep) + row_tile;
       const float2 e = part_s[g * kObTile + (k % p.rep) * p.rp + r];
       if (e.y == 0.f) continue;
@@ -896,16 +913,16 @@ layer_observe_short_kernel(const __grid_constant__ ObserveParams p, const __grid
   __syncthreads();
   // ---- pass 2: the lane's token, a share of the rows
   float w = 0.f;
-  if (live) {
+  if (j < live) {
     good = __all_sync(0xffffffffu, mbar_wait_lean(done2, 0, s_abort, p.status)) && good;
     tc_fence_after();
     if (good) {
-      const int pos = pos_s[gl];
+      const int pos = pos_s[j * kObTile + gl];
       uint64_t wa = 0, wb = 0;
 #pragma unroll 1
       for (int r0 = share * kObChunk; r0 < n_rows; r0 += shares * kObChunk) {
         uint32_t raw[kObChunk];
-        tmem_load(tbuf + (p.nt + tt) * kObTile + r0, raw);
+        tmem_load(tbuf + (unit + (both ? units : 0)) * kObTile + r0, raw);
         ulonglong2 z2[kObChunk / 4];
 #pragma unroll
         for (int k = 0; k < kObChunk / 4; ++k) z2[k] = reinterpret_cast<const ulonglong2*>(neg_lse + row0 + r0)[k];
@@ -921,10 +938,12 @@ layer_observe_short_kernel(const __grid_constant__ ObserveParams p, const __grid
   w_s[grp * kObTile + gl] = w;
   tc_fence_before();
   __syncthreads();
-  if (tid < kObTile && page_ok(p.g, page)) {
+  if (tid < T * kObTile && page_ok(p.g, page)) {
+    const int jt = tid / kObTile;
     float sum = 0.f;
 #pragma unroll
-    for (int g = 0; g < kObGroups; ++g) sum += w_s[g * kObTile + tid];
+    for (int g = 0; g < kObGroups; ++g)
+      if ((g & (units - 1)) >> two == jt) sum += w_s[g * kObTile + (tid & (kObTile - 1))];
     p.weights[at] = (p.add ? p.weights[at] : 0.f) + sum;
   }
   if (*s_abort) {  // let copies in flight land before the CTA's memory is released
@@ -938,6 +957,21 @@ constexpr int kObMaxCtas = 256;
 size_t layer_observe_workspace_bytes(const mc_config* cfg, const mc_batch* bt, int n_obs) {
   const size_t rows = (size_t)n_obs * (cfg->n_q_heads / cfg->n_kv_heads);
   return align_up(((size_t)kObMaxCtas + (size_t)bt->batch * cfg->n_kv_heads) * rows * kObGroups * 2 * sizeof(float), 256);
+}
+
+// Tiles per CTA of the one-launch kernel, 0: the two launches.  The fewest with which its clusters run in one wave, a CTA
+// per SM.  (Larger clusters fill the GPU's partitions less well: 16 of eight CTAs, and 24 of six, took two waves.)  One
+// wave always won: 8 kv heads under 32, 32 queries, 512 tokens 9.7 us against 22.4 (one prompt), 15.3 against 26.8 (eight,
+// two tiles each), 24.3 against 29.4 (sixteen, four tiles each); 4096 tokens 23.5 against 29.7; 32 heads, 32 queries, 512
+// tokens 8.7 against 14.6 (one prompt), 11.3 against 15.7 (two), 15.1 against 17.8 (four); 64 queries of 8 / 32 heads, 1024
+// tokens 15.2 against 24.9 (one prompt), 23.9 against 29.8 (four).
+static int short_tiles(int tiles, long long segs, int nt, int n_sm) {
+  for (int per = 1; per * nt <= kOsMaxTiles; per *= 2) {
+    const int cluster = (tiles + per - 1) / per;
+    const int room = cluster <= 2 ? n_sm : cluster <= 4 ? n_sm - n_sm / 8 : n_sm - n_sm / 4;
+    if (tiles >= 1 && cluster <= kOsMaxCluster && segs * cluster <= room) return per;
+  }
+  return 0;
 }
 
 mc_status launch_layer_observe(const mc_config* cfg, const mc_batch* bt, const Geom& g, const mc_layer_cache* layer,
@@ -984,24 +1018,22 @@ mc_status launch_layer_observe(const mc_config* cfg, const mc_batch* bt, const G
   const uint64_t rows = (uint64_t)bt->n_pages * cfg->n_kv_heads * cfg->page_size;
   if (mc_status st = make_map(&map_k, cfg->dtype, layer->k_pool, rows, kHeadDim, cfg->page_size)) return st;
   if (mc_status st = make_map3(&map_q, cfg->dtype, q, (uint64_t)bt->batch * n_obs, cfg->n_q_heads, kHeadDim, op.jt, op.nq)) return st;
-  // Short prompts in one launch, as long as its CTAs (one per SM) run in one wave, or in two where the rows are so many
-  // that the persistent kernel, a tile per group of warps, has too few tiles to go round: 8 kv heads under 32, 32
-  // queries, 512 tokens: 9.6 against 22.4 us for one prompt, 20.8 against 26.9 for eight (256 CTAs), 40 against 29 for
-  // sixteen; 64 queries, 1024 tokens: 26.0 against 29.9 with 192 CTAs, 37 against 30 with 256; 32 rows (32 heads, 512
-  // tokens): 8.6 against 14.6 with 128 CTAs, 16.9 against 15.7 with 256.
   const int tiles = (bt->max_seq_len + kObTile - 1) / kObTile;
-  const int room = op.rows <= 64 ? n_sm : op.nt == 1 ? 2 * n_sm : n_sm + n_sm / 2;
-  if (tiles >= 1 && tiles <= kOsMaxCluster && (long long)bt->batch * cfg->n_kv_heads * tiles <= room) {
+  const int per = short_tiles(tiles, (long long)bt->batch * cfg->n_kv_heads, op.nt, n_sm), cluster = per ? (tiles + per - 1) / per : 0;
+  if (per) {
     op.add = (flags & MC_LAYER_ACCUMULATE) ? 1 : 0;
     using Short = void (*)(const ObserveParams, const CUtensorMap, const CUtensorMap);
-    static const Short shorts[2][2] = {{layer_observe_short_kernel<MC_F16, false>, layer_observe_short_kernel<MC_F16, true>},
-                                       {layer_observe_short_kernel<MC_BF16, false>, layer_observe_short_kernel<MC_BF16, true>}};
-    const Short kern = shorts[cfg->dtype == MC_F16 ? 0 : 1][opts->softcap > 0.f ? 1 : 0];
+    static const Short shorts[2][2][3] = {
+        {{layer_observe_short_kernel<MC_F16, false, 1>, layer_observe_short_kernel<MC_F16, false, 2>, layer_observe_short_kernel<MC_F16, false, 4>},
+         {layer_observe_short_kernel<MC_F16, true, 1>, layer_observe_short_kernel<MC_F16, true, 2>, layer_observe_short_kernel<MC_F16, true, 4>}},
+        {{layer_observe_short_kernel<MC_BF16, false, 1>, layer_observe_short_kernel<MC_BF16, false, 2>, layer_observe_short_kernel<MC_BF16, false, 4>},
+         {layer_observe_short_kernel<MC_BF16, true, 1>, layer_observe_short_kernel<MC_BF16, true, 2>, layer_observe_short_kernel<MC_BF16, true, 4>}}};
+    const Short kern = shorts[cfg->dtype == MC_F16 ? 0 : 1][opts->softcap > 0.f ? 1 : 0][per >> 1];
     // (more than half an SM's shared memory: two CTAs on one SM might wait for each other's tensor memory)
-    const size_t need = std::max<size_t>(1024 + (size_t)(1 + op.nt) * kObTileBytes + kOsArrays, 120 * 1024);
+    const size_t need = std::max<size_t>(1024 + (size_t)(per + op.nt) * kObTileBytes + kOsArrays, 120 * 1024);
     MC_CUDA_CHECK(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)need));
     cudaLaunchConfig_t lc = {};
-    lc.gridDim = dim3((unsigned)(bt->batch * cfg->n_kv_heads * tiles));
+    lc.gridDim = dim3((unsigned)(bt->batch * cfg->n_kv_heads * cluster));
     lc.blockDim = dim3(kOsThreads);
     lc.dynamicSmemBytes = need;
     lc.stream = stream;
@@ -1009,7 +1041,7 @@ mc_status launch_layer_observe(const mc_config* cfg, const mc_batch* bt, const G
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = tiles;
+    attr[1].val.clusterDim.x = cluster;
     attr[1].val.clusterDim.y = 1;
     attr[1].val.clusterDim.z = 1;
     lc.attrs = attr;

@@ -122,6 +122,26 @@ def test_cap_bias_and_positions_next_to_a_longer_prompt(L, cap, alibi):
     run(L, [1300, 200, 129], 20, H=2, Hq=8, ps=16, q_pos=[300, 10 ** 6, -1], cap=cap, alibi=alibi, window=90)
 
 
+@pytest.mark.parametrize("longest", [4200, 2300])
+@pytest.mark.parametrize("window,prefix,doc", [(1, 0, 0), (7, 4, 0), (130, 0, 50), (64, 200, 0), (0, 17, 333), (0, 0, 10 ** 6),
+                                               (300, 2 ** 31 - 1, 9)])
+def test_masks_next_to_a_long_prompt(L, window, prefix, doc, longest):
+    """Past what one launch holds (4096 tokens; 2048 where there are more than 128 rows)."""
+    J = 20 if longest > 4096 else 40
+    for acc, marks in ((False, False), (True, False), (False, True)):
+        run(L, [700, 129, 1, 0, longest], J, H=2, Hq=8, ps=16, window=window, prefixes=[prefix] * 5, docs=[doc, doc // 2, 0, doc, 5],
+            marks=marks, acc=acc, dtype="bf16", cap=20.0 if acc else 0.0, alibi=marks)
+
+
+@pytest.mark.parametrize("J", [8, 32, 50])
+def test_two_and_four_tiles_per_cta(L, J):
+    for lens in ([2000, 1025, 0, 3], [1030, 129], [2048], [4000, 2049, 127, 0], [4096, 100]):
+        run(L, lens, J, H=2, Hq=8, ps=64, dtype="bf16", acc=True, cap=30.0 if J == 8 else 0.0)
+        run(L, lens[::-1], J, H=1, Hq=2, ps=16, window=700, prefixes=[5] * len(lens), marks=J == 32)
+    run(L, [512, 300, 0, 511], J, H=32, Hq=32, ps=16)
+    run(L, [512, 257], J, H=32, Hq=32, ps=32, alibi=True)
+
+
 @pytest.mark.parametrize("tiles", range(1, 9))
 def test_every_size_of_a_short_prompt(L, tiles):
     """One to eight tiles of 128 tokens, whole, begun and just begun; rows of each layout."""
