@@ -10,7 +10,8 @@
 // movers are listed in index order (a warp per run of tokens, counts scanned over the cluster) and the cluster's warps
 // copy the rows.  The steady state of a bounded cache, one token too many, needs no digits: the smallest key goes.
 // Bytes: 8 per token for the keys, 2 x 512 per moved row; short caches are bound by the chain of dependent loads and
-// barriers.
+// barriers.  Measured: 58 us on 8 x 32 segments of 4096 tokens down to 1000 (202 MB of rows at 5.6 TB/s in 36 us, the
+// selection before it 12 us), 49 us on 4 x 8 of 32768 down to 4096 (115 MB in 20 us).
 #include <cooperative_groups.h>
 
 #include <algorithm>

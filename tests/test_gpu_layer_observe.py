@@ -176,3 +176,17 @@ def test_bad_pages_are_flagged(L):
     assert code == 8 and words[0] == 4
     for page in (int(c.table[0, 2]), int(c.table[1, 0])):
         assert torch.equal(c.d["w"][page], w0[page])  # nothing is written to a page that the table does not name
+
+
+def test_bad_pages_of_a_long_prompt_are_flagged(L):
+    c = L.Cache([4300, 50], 2, 4, 16, "f16", weights=True, poison=False)
+    mc, lib = c.mc, c.mc.lib()
+    q, ws = c.queries(2, 8, 4).cuda(), c.workspace(mc.MC_OP_LAYER_OBSERVE, 8)
+    w0 = c.d["w"].clone()
+    c.d["table"][0, 200] = 10 ** 6
+    c.d["table"][1, 0] = -2
+    lib.mc_layer_observe(c.cfg, c.batch, c.layer, mc.ScoreOpts(SM), q, 0, ws)
+    words, code = lib.mc_layer_read_status(c.layer, check=False)
+    assert code == 8 and words[0] == 4
+    for page in (int(c.table[0, 200]), int(c.table[1, 0])):
+        assert torch.equal(c.d["w"][page], w0[page])
