@@ -112,6 +112,9 @@ def _stream(stream) -> Optional[int]:
     return stream.cuda_stream or None
 
 
+_TORCH_DTYPES = {"f16": torch.float16, "bf16": torch.bfloat16}
+
+
 @dataclasses.dataclass
 class McConfig:
     n_kv_heads: int
@@ -136,7 +139,7 @@ class McConfig:
 
     @property
     def torch_dtype(self):
-        return {"f16": torch.float16, "bf16": torch.bfloat16}[self.dtype]
+        return _TORCH_DTYPES[self.dtype]
 
 
 @dataclasses.dataclass
@@ -154,13 +157,14 @@ class Batch:
         mp = self.block_table.shape[1] if self.block_table.dim() == 2 else 0
         return _Batch(_ptr(self.block_table), _ptr(self.seq_lens), b, mp, int(self.max_seq_len), 0, int(self.n_pages))
 
-    def layer_c(self) -> _Batch:
-        """c() for the mc_layer_* calls: a row of the block table for every sequence."""
+    def layer_c(self, dev: Optional[int] = None) -> _Batch:
+        """c() for the mc_layer_* calls: a row of the block table for every sequence, both tensors on device dev."""
         bt, sl = self.block_table, self.seq_lens
-        shape, n = bt.shape, sl.numel()
-        assert len(shape) == 2 and shape[0] >= n, "block_table [batch][max_pages_per_seq] and seq_lens [batch] are wanted"
-        return _Batch(_held("block_table", bt, torch.int32, 0), _held("seq_lens", sl, torch.int32, 0), n, shape[1], self.max_seq_len, 0,
-                      self.n_pages)
+        n, pages = sl.numel(), bt.size(1) if bt.dim() == 2 else -1
+        if not (pages >= 0 and bt.size(0) >= n and _good(bt, torch.int32, 0, dev) and _good(sl, torch.int32, 0, dev)):
+            _refuse(dev, block_table=(bt, torch.int32, 0), seq_lens=(sl, torch.int32, 0))
+            raise AssertionError("block_table [batch][max_pages_per_seq] and seq_lens [batch] are wanted")
+        return _Batch(bt.data_ptr(), sl.data_ptr(), n, pages, int(self.max_seq_len), 0, int(self.n_pages))
 
 
 
@@ -303,20 +307,23 @@ class PairCache:
         return sum(t.numel() * t.element_size() for t in ts)
 
 
-def _held(name: str, t: Optional[torch.Tensor], dtype, n: int) -> Optional[int]:
-    """Address of a contiguous tensor of at least n elements, or None."""
-    if t is None:
-        return None
-    assert t.dtype is dtype and t.is_contiguous(), f"{name}: a contiguous {dtype} tensor is wanted"
-    assert t.numel() >= n, f"{name}: at least {n} entries are wanted"
-    return t.data_ptr()
+# The mc_layer_* calls are made once per layer and decode step, where a microsecond counts: their tensors are checked in
+# plain expressions, at every call, and _refuse finds out what was wrong.
+def _good(t: Optional[torch.Tensor], dtype, n: int, dev: Optional[int]) -> bool:
+    return t is None or (t.dtype is dtype and t.numel() >= n and t.is_contiguous() and (dev is None or t.get_device() == dev))
 
 
-def _layer_stream(stream, tensors) -> Optional[int]:
-    """The stream of a mc_layer_* call, all of whose tensors have to be on the device that is current."""
-    devs = {t.get_device() for t in tensors if t is not None}
-    dev = devs.pop()
-    assert not devs and dev >= 0 and dev == torch.cuda.current_device(), "all tensors have to be on the current CUDA device"
+def _refuse(dev: Optional[int], **tensors) -> None:
+    """tensors: name=(tensor, type, entries); raises AssertionError for the first that is not as wanted."""
+    for name, (t, dtype, n) in tensors.items():
+        assert t is None or (t.dtype is dtype and t.is_contiguous()), f"{name}: a contiguous {dtype} tensor is wanted"
+        assert t is None or t.numel() >= n, f"{name}: at least {n} entries are wanted"
+        assert t is None or dev is None or t.get_device() == dev, f"{name}: all tensors have to be on the current CUDA device"
+
+
+def _layer_stream(stream, dev: int) -> Optional[int]:
+    """The stream of a mc_layer_* call whose tensors are on device dev."""
+    assert dev >= 0 and dev == torch._C._cuda_getDevice(), "all tensors have to be on the current CUDA device"
     # (the stream's handle itself: building a Stream object costs 1 us of a 10 us call)
     return (torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream) or None
 
@@ -351,16 +358,20 @@ class LayerCache:
         if self.status is None:
             self.status = torch.zeros(MC_STATUS_WORDS, dtype=torch.int32, device=self.k_pool.device)
 
-    def tensors(self):
-        return self.k_pool, self.v_pool, self.positions, self.weights, self.status
-
-    def c(self, n_pages: int, cfg: Optional[McConfig] = None) -> _LayerCache:
-        """cfg: the call's configuration (default: the cache's own), which the pools have to hold n_pages pages of."""
+    def c(self, n_pages: int, cfg: Optional[McConfig] = None, dev: Optional[int] = None) -> _LayerCache:
+        """cfg: the call's configuration (default: the cache's own), which the pools have to hold n_pages pages of; dev: the
+        device that the tensors have to be on."""
         cfg = cfg or self.cfg
+        k, v, pos, w, st = self.k_pool, self.v_pool, self.positions, self.weights, self.status
         dt, rows = cfg.torch_dtype, n_pages * cfg.n_kv_heads * cfg.page_size
-        return _LayerCache(_held("k_pool", self.k_pool, dt, 128 * rows), _held("v_pool", self.v_pool, dt, 128 * rows),
-                           _held("positions", self.positions, torch.int32, rows), _held("weights", self.weights, torch.float32, rows),
-                           _held("status", self.status, torch.int32, MC_STATUS_WORDS))
+        if not (k.dtype is dt and v.dtype is dt and k.numel() >= 128 * rows and v.numel() >= 128 * rows and k.is_contiguous()
+                and v.is_contiguous() and (dev is None or (k.get_device() == dev and v.get_device() == dev))
+                and (pos is None or _good(pos, torch.int32, rows, dev)) and (w is None or _good(w, torch.float32, rows, dev))
+                and _good(st, torch.int32, MC_STATUS_WORDS, dev)):
+            _refuse(dev, k_pool=(k, dt, 128 * rows), v_pool=(v, dt, 128 * rows), positions=(pos, torch.int32, rows),
+                    weights=(w, torch.float32, rows), status=(st, torch.int32, MC_STATUS_WORDS))
+        return _LayerCache(k.data_ptr(), v.data_ptr(), None if pos is None else pos.data_ptr(), None if w is None else w.data_ptr(),
+                           st.data_ptr())
 
 
 @dataclasses.dataclass
@@ -375,13 +386,14 @@ class ScoreOpts:
     prefix_len: Optional[torch.Tensor] = None
     q_pos: Optional[torch.Tensor] = None
 
-    def tensors(self):
-        return self.alibi_slopes, self.doc_start, self.prefix_len, self.q_pos
-
-    def c(self, cfg: McConfig, batch: int) -> _ScoreOpts:
-        return _ScoreOpts(_held("alibi_slopes", self.alibi_slopes, torch.float32, cfg.n_q_heads),
-                          _held("doc_start", self.doc_start, torch.int32, batch), _held("prefix_len", self.prefix_len, torch.int32, batch),
-                          _held("q_pos", self.q_pos, torch.int32, batch), self.sm_scale, self.softcap, self.window, 0)
+    def c(self, cfg: McConfig, batch: int, dev: Optional[int] = None) -> _ScoreOpts:
+        a, d, p, q = self.alibi_slopes, self.doc_start, self.prefix_len, self.q_pos
+        if not ((a is None or _good(a, torch.float32, cfg.n_q_heads, dev)) and (d is None or _good(d, torch.int32, batch, dev))
+                and (p is None or _good(p, torch.int32, batch, dev)) and (q is None or _good(q, torch.int32, batch, dev))):
+            _refuse(dev, alibi_slopes=(a, torch.float32, cfg.n_q_heads), doc_start=(d, torch.int32, batch),
+                    prefix_len=(p, torch.int32, batch), q_pos=(q, torch.int32, batch))
+        return _ScoreOpts(None if a is None else a.data_ptr(), None if d is None else d.data_ptr(), None if p is None else p.data_ptr(),
+                          None if q is None else q.data_ptr(), self.sm_scale, self.softcap, self.window, 0)
 
 
 @dataclasses.dataclass
@@ -392,8 +404,11 @@ class EvictOpts:
     n_recent: int = 0
     q_pos: Optional[torch.Tensor] = None
 
-    def c(self, batch: int) -> _EvictOpts:
-        return _EvictOpts(_held("q_pos", self.q_pos, torch.int32, batch), int(self.budget), int(self.n_sink), int(self.n_recent), 0)
+    def c(self, batch: int, dev: Optional[int] = None) -> _EvictOpts:
+        q = self.q_pos
+        if not _good(q, torch.int32, batch, dev):
+            _refuse(dev, q_pos=(q, torch.int32, batch))
+        return _EvictOpts(None if q is None else q.data_ptr(), int(self.budget), int(self.n_sink), int(self.n_recent), 0)
 
 
 class MiniCacheLib:
@@ -676,16 +691,22 @@ class MiniCacheLib:
         """q, out [batch][n_q_heads][128], k_new / v_new [batch][n_kv_heads][128] or None; flags: MC_LAYER_APPEND |
         MC_LAYER_ACCUMULATE; lse [batch][n_q_heads] float32 or None.  Every tensor of a mc_layer_* call has to be on the
         device that is current (AssertionError)."""
-        c, b = _cfg_c(cfg), batch.layer_c()
-        n, dt = b.batch, q.dtype
+        dev = q.get_device()
+        c, b, dt = _cfg_c(cfg), batch.layer_c(dev), cfg.torch_dtype
+        n = b.batch
         rows_q, rows_kv = n * cfg.n_q_heads * 128, n * cfg.n_kv_heads * 128
-        assert dt is cfg.torch_dtype, "q: the storage type is wanted"
-        for t, rows in ((q, rows_q), (out, rows_q), (k_new, rows_kv), (v_new, rows_kv)):
-            assert t is None or (t.dtype is dt and t.numel() == rows and t.is_contiguous()), \
-                "contiguous rows of 128 channels per sequence and head are wanted"
-        assert lse is None or (lse.dtype is torch.float32 and lse.numel() == n * cfg.n_q_heads and lse.is_contiguous()), "lse: float32 [batch][n_q_heads]"
-        l, o = layer.c(b.n_pages, cfg), opts.c(cfg, n)
-        at = _layer_stream(stream, (q, out, k_new, v_new, lse, workspace, batch.block_table, batch.seq_lens, *layer.tensors(), *opts.tensors()))
+        if not (q.dtype is dt and out.dtype is dt and q.numel() == rows_q and out.numel() == rows_q and q.is_contiguous()
+                and out.is_contiguous() and out.get_device() == dev and workspace.get_device() == dev):
+            _refuse(dev, q=(q, dt, rows_q), out=(out, dt, rows_q), workspace=(workspace, workspace.dtype, 0))
+            raise AssertionError("q and out: [batch][n_q_heads][128] are wanted")
+        for t in (k_new, v_new):
+            if t is not None and not (t.dtype is dt and t.numel() == rows_kv and t.is_contiguous() and t.get_device() == dev):
+                _refuse(dev, k_new=(k_new, dt, rows_kv), v_new=(v_new, dt, rows_kv))
+                raise AssertionError("k_new and v_new: [batch][n_kv_heads][128] are wanted")
+        if lse is not None and not (_good(lse, torch.float32, 0, dev) and lse.numel() == n * cfg.n_q_heads):
+            _refuse(dev, lse=(lse, torch.float32, n * cfg.n_q_heads))
+            raise AssertionError("lse: [batch][n_q_heads] is wanted")
+        l, o, at = layer.c(b.n_pages, cfg, dev), opts.c(cfg, n, dev), _layer_stream(stream, dev)
         code = self._lib.mc_layer_attn(c, b, l, o, q.data_ptr(), None if k_new is None else k_new.data_ptr(),
                                        None if v_new is None else v_new.data_ptr(), flags, out.data_ptr(),
                                        None if lse is None else lse.data_ptr(), workspace.data_ptr(), workspace.nbytes, at)
@@ -696,12 +717,13 @@ class MiniCacheLib:
                          stream=None):
         """q [batch][n_obs][n_q_heads][128]: the last n_obs queries of every sequence; flags: 0 (weights are written) or
         MC_LAYER_ACCUMULATE (added to)."""
-        c, b = _cfg_c(cfg), batch.layer_c()
-        shape = q.shape
+        dev, shape = q.get_device(), q.shape
+        c, b = _cfg_c(cfg), batch.layer_c(dev)
         assert len(shape) == 4 and shape[0] == b.batch and shape[2] == cfg.n_q_heads and shape[3] == 128, "q: [batch][n_obs][n_q_heads][128]"
-        assert q.dtype is cfg.torch_dtype and q.is_contiguous(), "q: contiguous rows of the storage type are wanted"
-        l, o = layer.c(b.n_pages, cfg), opts.c(cfg, b.batch)
-        at = _layer_stream(stream, (q, workspace, batch.block_table, batch.seq_lens, *layer.tensors(), *opts.tensors()))
+        if not (_good(q, cfg.torch_dtype, 0, dev) and workspace.get_device() == dev):
+            _refuse(dev, q=(q, cfg.torch_dtype, 0), workspace=(workspace, workspace.dtype, 0))
+            raise AssertionError("all tensors have to be on the current CUDA device")
+        l, o, at = layer.c(b.n_pages, cfg, dev), opts.c(cfg, b.batch, dev), _layer_stream(stream, dev)
         code = self._lib.mc_layer_observe(c, b, l, o, q.data_ptr(), shape[1], flags, workspace.data_ptr(), workspace.nbytes, at)
         if code:
             self._check(code)
@@ -709,10 +731,12 @@ class MiniCacheLib:
     def mc_layer_evict(self, cfg: McConfig, batch: Batch, layer: LayerCache, opts: EvictOpts, new_lens: torch.Tensor,
                        workspace: torch.Tensor, stream=None):
         """new_lens int32 [batch] receives min(seq_lens, budget); it must not share memory with batch.seq_lens or opts.q_pos."""
-        c, b = _cfg_c(cfg), batch.layer_c()
-        assert new_lens.dtype is torch.int32 and new_lens.numel() == b.batch and new_lens.is_contiguous(), "new_lens: int32 [batch]"
-        l, o = layer.c(b.n_pages, cfg), opts.c(b.batch)
-        at = _layer_stream(stream, (new_lens, workspace, batch.block_table, batch.seq_lens, *layer.tensors(), opts.q_pos))
+        dev = new_lens.get_device()
+        c, b = _cfg_c(cfg), batch.layer_c(dev)
+        if not (_good(new_lens, torch.int32, 0, dev) and new_lens.numel() == b.batch and workspace.get_device() == dev):
+            _refuse(dev, new_lens=(new_lens, torch.int32, b.batch), workspace=(workspace, workspace.dtype, 0))
+            raise AssertionError("new_lens: int32 [batch] is wanted")
+        l, o, at = layer.c(b.n_pages, cfg, dev), opts.c(b.batch, dev), _layer_stream(stream, dev)
         code = self._lib.mc_layer_evict(c, b, l, o, new_lens.data_ptr(), workspace.data_ptr(), workspace.nbytes, at)
         if code:
             self._check(code)
