@@ -580,8 +580,9 @@ mc_status mc_decode_attn_static(const mc_config* cfg, const mc_batch* batch, con
  * k_pool, v_pool  [n_pages][n_kv_heads][page_size][128] of cfg->dtype (the layer pools of mc_layer_kv)
  * positions       [n_pages][n_kv_heads][page_size] int32: position of every cached row, or NULL: a row's token index
  *                 is its position.  mc_layer_evict needs it (it fills holes with later rows, head by head, so that
- *                 rows end up in another order in every head).  256-byte aligned.
- * weights         [n_pages][n_kv_heads][page_size] fp32: accumulated attention weight of every cached row, or NULL
+ *                 rows end up in another order in every head).  16-byte aligned.
+ * weights         [n_pages][n_kv_heads][page_size] fp32: accumulated attention weight of every cached row, or NULL;
+ *                 16-byte aligned
  * status          [MC_STATUS_WORDS] int32, cleared by the caller; flags accumulate (MC_STATUS_FLAGS; the other words
  *                 are not used) */
 typedef struct mc_layer_cache {

@@ -286,3 +286,33 @@ def test_new_lengths_passed_straight_on(L, graph):
         got.append((torch.stack(outs), c.gathered("w", 0, budget), c.gathered("pos", 2, budget)))
         assert lib.mc_layer_read_status(c.layer, check=False)[1] == 0
     assert all(torch.equal(a, b) for a, b in zip(*got)) and torch.isfinite(got[0][0].float()).all()
+
+
+@pytest.mark.parametrize("shift", [4, 12, 16])
+def test_positions_and_weights_inside_one_allocation(L, shift):
+    """Positions and weights that begin 16, 48 and 64 bytes into their storage: the bits of those that begin at a pool's own."""
+    got = []
+    for off in (0, shift):
+        c = L.Cache([300, 77, 130], 1, 4, 16, "bf16", seed=31, marks=True, weights=True)
+        mc, lib = c.mc, c.mc.lib()
+        pos, w = (torch.zeros(c.d[k].numel() + off, dtype=c.d[k].dtype, device="cuda")[off:].view(c.d[k].shape) for k in ("pos", "w"))
+        pos.copy_(c.d["pos"])
+        w.copy_(c.d["w"])
+        layer = mc.LayerCache(c.cfg, c.d["k"], c.d["v"], pos, w)
+        q_pos = torch.tensor(c.q_next, dtype=torch.int32, device="cuda")
+        q, q_obs, kn, vn = c.queries(3, 4).cuda(), c.queries(3, 8, 4).cuda(), c.rows(3, 1).cuda(), c.rows(3, 1).cuda()
+        flags = mc.MC_LAYER_APPEND | mc.MC_LAYER_ACCUMULATE
+        ws = torch.zeros(max(lib.mc_layer_workspace_bytes(c.cfg, c.batch, op, arg)
+                             for op, arg in ((mc.MC_OP_LAYER_ATTN, flags), (mc.MC_OP_LAYER_OBSERVE, 8), (mc.MC_OP_LAYER_EVICT, 0))),
+                         dtype=torch.uint8, device="cuda")
+        out, new = torch.empty_like(q), torch.zeros_like(c.d_lens)
+        lib.mc_layer_observe(c.cfg, c.batch, layer, mc.ScoreOpts(SM, q_pos=q_pos - 1), q_obs, 0, ws)
+        lib.mc_layer_attn(c.cfg, c.batch, layer, mc.ScoreOpts(SM, q_pos=q_pos, window=90), q, kn, vn, flags, out, None, ws)
+        lib.mc_layer_evict(c.cfg, c.batch, layer, mc.EvictOpts(64, 2, 8, q_pos), new, ws)
+        torch.cuda.synchronize()
+        assert lib.mc_layer_read_status(layer, check=False)[1] == 0
+        held = [x.cpu()[c.table[b, :4].long()] for b in range(3) for x in (pos, w)]
+        got.append([out.cpu(), new.cpu()] + held + [c.gathered("k", b, 64) for b in range(3)])
+    for a, b in zip(*got):
+        assert torch.equal(a.float().nan_to_num(7.0), b.float().nan_to_num(7.0))
+    assert torch.isfinite(got[0][0].float()).all()

@@ -198,3 +198,11 @@ def test_binding_refuses_host_tensors_and_short_block_tables(lib):
             lib.mc_layer_observe(c, batch, layer, mc.ScoreOpts(0.1), q[:, None], 0, ws)
         with pytest.raises(AssertionError, match="CUDA device" if batch is ok else "block_table"):
             lib.mc_layer_evict(c, batch, layer, mc.EvictOpts(4), new, ws)
+
+
+def test_positions_and_weights_on_sixteen_byte_boundaries(lib):
+    """As the parts of one allocation are: past the alignment check (the workspace is refused next), not at eight bytes."""
+    for kw in (dict(pos=0x30010), dict(w=0x40040), dict(pos=0x300f0, w=0x40030)):
+        assert attn(lib, l=layer(**kw), n=16) == 5, kw
+    for kw in (dict(pos=0x30008), dict(w=0x40008)):
+        assert attn(lib, l=layer(**kw), n=16) == 4, kw
