@@ -281,7 +281,6 @@ template <int DT, int PASS, bool CAP>
 __global__ void __launch_bounds__(kObThreads, 1)
 layer_observe_kernel(const __grid_constant__ ObserveParams p, const __grid_constant__ CUtensorMap map_k,
                      const __grid_constant__ CUtensorMap map_q) {
-  grid_dep_launch();
   extern __shared__ unsigned char smem_raw[];
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   // barriers: K full / empty per stage, Q full / empty per buffer, accumulator full / empty per group
@@ -327,8 +326,6 @@ layer_observe_kernel(const __grid_constant__ ObserveParams p, const __grid_const
     *s_abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == 1) tmem_alloc(smem_u32(tmem_slot), tmem_cols);
-  tc_fence_before();
   __syncthreads();
   if (warp == 0) {  // exclusive prefix of the sequences' tiles (all kv heads)
     const int per = (p.g.batch + 31) / 32;
@@ -349,8 +346,6 @@ layer_observe_kernel(const __grid_constant__ ObserveParams p, const __grid_const
     if (lane == 0) pre_s[0] = 0;
   }
   __syncthreads();
-  tc_fence_after();
-  const uint32_t tmem_d = *tmem_slot;
   const long long U = pre_s[p.g.batch];
   const int T = (int)min((long long)p.n_ctas, max(U, 1LL));  // no live CTA's share is empty
   const int cta = blockIdx.x;
@@ -387,6 +382,14 @@ layer_observe_kernel(const __grid_constant__ ObserveParams p, const __grid_const
     page_n = load_window(win_tiles, head_n, has_n);
   }
   grid_dep_wait();
+  // Tensor memory is taken behind the wait -- held in front of it, it could be what a CTA of the grid ahead is waiting
+  // for -- and dependents may start once it is ours: one that took it first would wait for this grid.
+  if (warp == 1) tmem_alloc(smem_u32(tmem_slot), tmem_cols);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_d = *tmem_slot;
+  grid_dep_launch();
   if (bad) atomicOr(p.status, MC_FLAG_BAD_METADATA);
 
   if (PASS == 1 && p.zero) {  // tokens that no query sees keep no weight: all are cleared, pass 2 adds
@@ -764,7 +767,6 @@ layer_observe_short_kernel(const __grid_constant__ ObserveParams p, const __grid
     abort_s = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == 1) tmem_alloc(smem_u32(&tmem_slot), tmem_cols);
   int bad = 0;
   const ObSeq s = ob_seq(p, b, bad);
   const int t0 = rank * T * kObTile, n = s.n;
@@ -774,13 +776,37 @@ layer_observe_short_kernel(const __grid_constant__ ObserveParams p, const __grid
   const bool has = warp == 0 && lane < T * (kObTile >> shift) && t0 + (lane << shift) < n;
   const int copy_page = has ? table[(t0 >> shift) + lane] : 0;
   const int page = tid < T * kObTile && t0 + tid < n ? table[(t0 + tid) >> shift] : -1;
+  grid_dep_wait();
+  // Tensor memory is taken behind the wait -- held in front of it, it could be what a CTA of the grid ahead is waiting
+  // for -- while warp 0 issues the copies.
+  if (warp == 1) tmem_alloc(smem_u32(&tmem_slot), tmem_cols);
+  if (live && warp == 0) {
+    const int n_copy = __popc(__ballot_sync(0xffffffffu, has));
+    if (lane == 0) mbar_expect_tx(full, (uint32_t)(n_copy * 2 * ps * 128 + 2 * p.nt * p.rep * p.jt * p.nq * 128));
+    __syncwarp();
+    if (has) {
+      int pg = copy_page;
+      if (!page_ok(p.g, pg)) {  // never an address: page 0 is read in its place and the call flagged
+        atomicOr(p.status, MC_FLAG_BAD_METADATA);
+        pg = 0;
+      }
+      const int y = (pg * H + head) * ps;
+      const int j = (lane << shift) / kObTile;
+      const uint32_t to = sk + j * kObTileBytes + ((lane << shift) - j * kObTile) * 128;
+      tma_load_2d(to, &map_k, 0, y, full);
+      tma_load_2d(to + kObHalf, &map_k, 64, y, full);
+    }
+    if (lane < 2 * p.nt * p.rep) {
+      const int h = lane & 1, r = (lane >> 1) % p.rep, tt = (lane >> 1) / p.rep;
+      tma_load_3d(sq + h * q_half + (tt * kObTile + r * p.rp) * 128, &map_q, 64 * h, head * p.nq, b * p.n_obs + tt * p.jt, full);
+    }
+  }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem_d = tmem_slot;
   cl.barrier_arrive();
   grid_dep_launch();  // (not before the tensor memory is ours: a kernel behind that took it first would wait for this one)
-  grid_dep_wait();
   if (bad && rank == 0 && head == 0 && tid == 0) atomicOr(p.status, MC_FLAG_BAD_METADATA);
 
   // (one thread)
@@ -803,26 +829,6 @@ layer_observe_short_kernel(const __grid_constant__ ObserveParams p, const __grid
     umma_commit(done);
   };
   if (live && warp == 0) {
-    const int n_copy = __popc(__ballot_sync(0xffffffffu, has));
-    if (lane == 0) mbar_expect_tx(full, (uint32_t)(n_copy * 2 * ps * 128 + 2 * p.nt * p.rep * p.jt * p.nq * 128));
-    __syncwarp();
-    if (has) {
-      int pg = copy_page;
-      if (!page_ok(p.g, pg)) {  // never an address: page 0 is read in its place and the call flagged
-        atomicOr(p.status, MC_FLAG_BAD_METADATA);
-        pg = 0;
-      }
-      const int y = (pg * H + head) * ps;
-      const int j = (lane << shift) / kObTile;
-      const uint32_t to = sk + j * kObTileBytes + ((lane << shift) - j * kObTile) * 128;
-      tma_load_2d(to, &map_k, 0, y, full);
-      tma_load_2d(to + kObHalf, &map_k, 64, y, full);
-    }
-    if (lane < 2 * p.nt * p.rep) {
-      const int h = lane & 1, r = (lane >> 1) % p.rep, tt = (lane >> 1) / p.rep;
-      tma_load_3d(sq + h * q_half + (tt * kObTile + r * p.rp) * 128, &map_q, 64 * h, head * p.nq, b * p.n_obs + tt * p.jt, full);
-    }
-    __syncwarp();
     if (lane == 0 && mbar_wait_lean(full, 0, s_abort, p.status)) {
       tc_fence_after();
 #pragma unroll
