@@ -97,7 +97,7 @@ __device__ __forceinline__ float score_of(const ScoreRule& r, float dot) {
 }
 
 // Four scores of a warp's lanes.  With a cap: x P(x^2) two at a time while every |x| of the warp is at most 1 (scores up
-// to the cap itself before it), else the exact form.
+// to the cap itself before it), else the exact form.  The two differ in their last bits: what does not count comes as 0.
 __device__ __forceinline__ void scores_of(const ScoreRule& r, float (&s)[4]) {
   if (!(r.cap_log2 > 0.f)) {
 #pragma unroll

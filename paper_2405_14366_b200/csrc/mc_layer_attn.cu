@@ -403,8 +403,7 @@ layer_attn_split_kernel(const __grid_constant__ LayerAttnParams p, const __grid_
       float sc[4];
 #pragma unroll
       for (int k = 0; k < 4; ++k) sc[k] = (d[0][k] + d[1][k]) + (d[2][k] + d[3][k]);
-      scores_of(p.rule, sc);
-      // ---- distance bias and masks (tokens t0 + row and + 8)
+      // ---- masks (tokens t0 + row and + 8), the scores' form, the distance bias
       uint32_t hidden = 0;  // bit r: token t0 + r is not seen (the same in every lane)
       {
         int p0 = t0 + row, p8 = p0 + 8;
@@ -425,6 +424,12 @@ layer_attn_split_kernel(const __grid_constant__ LayerAttnParams p, const __grid_
             v8 = p8 < sq.a || (p8 >= sq.lo && p8 < sq.hi);
           }
         }
+        // (a row that is not seen, stale or poisoned, has no say in which form of the cap the others take)
+        if (!whole && p.rule.cap_log2 > 0.f) {
+          if (!v0) sc[0] = sc[1] = 0.f;
+          if (!v8) sc[2] = sc[3] = 0.f;
+        }
+        scores_of(p.rule, sc);
         if (p.rule.slopes) {
           const float e0 = (float)(sq.view.q_pos - p0), e8 = (float)(sq.view.q_pos - p8);
           sc[0] = fmaf(-sl0, e0, sc[0]);

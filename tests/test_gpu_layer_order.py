@@ -62,3 +62,52 @@ def test_observe_behind_a_prefill_merge(L, lens, Hq, J, graph):
         assert lib.mc_layer_read_status(c.layer, check=False)[1] == 0
         got.append([c.d["w"].clone(), p.pair.e_k.clone().view(torch.int16)])
     assert all(torch.equal(a, b) for a, b in zip(*got)) and float(got[0][0].sum()) > 0
+
+
+def unseen_filled(L, lens, H, Hq, ps, dtype, fill, visible, seed=11, max_len=None):
+    """A cache whose rows outside visible(b) (a truth value per token) all hold `fill`: hidden, behind the sequence, of nobody."""
+    c = L.Cache(lens, H, Hq, ps, dtype, seed=seed, weights=True, poison=False, max_len=max_len)
+    keep = torch.zeros(c.n_pages, ps, dtype=torch.bool)
+    for b, n in enumerate(lens):
+        t = torch.arange(n)
+        keep[c.table[b, t // ps].long(), t % ps] = visible(b)
+    for k in ("k", "v"):
+        c.d[k].copy_(torch.where(keep[:, None, :, None], getattr(c, k), torch.full((), fill).to(c.dt)))
+    return c
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("window,prefix,doc", [(0, 0, 0), (20, 3, 0), (0, 0, 9)])
+@pytest.mark.parametrize("lens,ps", [([32, 48, 7, 160], 16), ([64, 128, 33, 1], 64), ([500, 2000, 176], 32)])
+def test_attention_under_a_cap_does_not_see_what_it_must_not(L, lens, ps, window, prefix, doc, dtype):
+    """Which form of the cap a visible score takes may not follow from rows that do not count, nor from what another call left
+    in shared memory: the same bits whatever they are.  (A new row that opens a slice of 16 tokens stands among stale rows.)"""
+    H, Hq, B = 2, 8, len(lens)
+    got = []
+    for fill in (0.0, 6.0e4, float("nan"), float("inf"), -6.0e4):
+        c = unseen_filled(L, lens, H, Hq, ps, dtype, fill, lambda b: L.seen(torch.arange(lens[b]), lens[b], window, doc, prefix))
+        mc, lib = c.mc, c.mc.lib()
+        flags = mc.MC_LAYER_APPEND | mc.MC_LAYER_ACCUMULATE
+        ten = lambda x: torch.full((B,), x, dtype=torch.int32, device="cuda") if x else None  # noqa: E731
+        ws = c.workspace(mc.MC_OP_LAYER_ATTN, flags)
+        q, kn, vn = c.queries(B, Hq).cuda(), c.rows(B, H).cuda(), c.rows(B, H).cuda()
+        out, lse = torch.zeros_like(q), torch.zeros(B, Hq, device="cuda")
+
+        def before(value):  # every SM's stages full of `value`
+            d = L.Cache([300] * 64, H, Hq, 16, dtype, poison=False)
+            for k in ("k", "v"):
+                d.d[k].fill_(value)
+            x = torch.full((64, Hq, 128), 1.0, dtype=d.dt, device="cuda")
+            lib.mc_layer_attn(d.cfg, d.batch, d.layer, mc.ScoreOpts(SM, softcap=50.0), x, None, None, 0, torch.zeros_like(x), None,
+                              d.workspace(mc.MC_OP_LAYER_ATTN))
+        before(0.0 if fill != fill else fill)
+        torch.cuda.synchronize()
+        lib.mc_layer_attn(c.cfg, c.batch, c.layer, mc.ScoreOpts(SM, softcap=50.0, window=window, prefix_len=ten(prefix), doc_start=ten(doc)),
+                          q, kn, vn, flags, out, lse, ws)
+        torch.cuda.synchronize()
+        assert lib.mc_layer_read_status(c.layer, check=False)[1] == 0
+        w = [c.gathered("w", b, n + 1) for b, n in enumerate(lens)]
+        got.append([out.view(torch.int16).cpu(), lse.cpu()] + w)
+    assert not torch.isnan(got[0][1]).any()  # (-inf: a document that begins behind a short sequence's query)
+    for other in got[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(got[0], other))
