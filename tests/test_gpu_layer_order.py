@@ -111,3 +111,43 @@ def test_attention_under_a_cap_does_not_see_what_it_must_not(L, lens, ps, window
     assert not torch.isnan(got[0][1]).any()  # (-inf: a document that begins behind a short sequence's query)
     for other in got[1:]:
         assert all(torch.equal(a, b) for a, b in zip(got[0], other))
+
+
+@pytest.mark.parametrize("dtype,marks", [("f16", False), ("bf16", False), ("bf16", True)])
+@pytest.mark.parametrize("window,prefix,doc", [(0, 0, 0), (60, 3, 0), (0, 0, 90)])
+@pytest.mark.parametrize("lens,J", [([77, 512, 300], 5), ([1000, 130, 17], 17), ([1, 700, 257], 40), ([4200, 77, 200], 5), ([2300, 300, 129], 40),
+                                    ([4301, 1, 255], 13)])
+def test_weights_under_a_cap_do_not_see_what_they_must_not(L, lens, J, window, prefix, doc, marks, dtype):
+    """The same for a prompt's weights: tokens behind a sequence (their pages are copied or not), hidden ones, and the rows between
+    a group's queries and the tile's 32, 64 or 128 (nothing fills them).  Prompts in one launch and in two, one and two row tiles."""
+    H, Hq, B, ps = 2, 8, len(lens), 16
+    got = []
+    for fill in (0.0, 6.0e4, float("nan"), float("inf"), -6.0e4):
+        spots = (lambda b: torch.ones(lens[b], dtype=torch.bool)) if marks else \
+            (lambda b: torch.stack([L.seen(torch.arange(lens[b]), lens[b] - J + j, window, doc, prefix) for j in range(J)]).any(0))
+        c = unseen_filled(L, lens, H, Hq, ps, dtype, fill, spots)
+        mc, lib = c.mc, c.mc.lib()
+        layer = c.layer
+        if marks:  # positions as the tokens' own: nothing is left out, every tile is looked at token by token
+            pos = torch.full((c.n_pages, H, ps), -5, dtype=torch.int32)
+            for b, n in enumerate(lens):
+                t = torch.arange(n)
+                pos[c.table[b, t // ps].long(), :, t % ps] = t.int()[:, None].expand(n, H)
+            layer = mc.LayerCache(c.cfg, c.d["k"], c.d["v"], pos.cuda(), c.d["w"], status=c.layer.status)
+        ten = lambda x: torch.full((B,), x, dtype=torch.int32, device="cuda") if x else None  # noqa: E731
+        ws = c.workspace(mc.MC_OP_LAYER_OBSERVE, J)
+        q = c.queries(B, J, Hq).cuda()
+        for n, m in ((c.max_len, 64), (600, 32)):  # tiles, queries and tensor memory full of `fill`
+            d = L.Cache([n] * 8, H, Hq, ps, dtype, poison=False, weights=True)
+            x = 0.0 if fill != fill else fill
+            d.d["k"].fill_(x)
+            lib.mc_layer_observe(d.cfg, d.batch, d.layer, mc.ScoreOpts(SM, softcap=50.0), torch.full((8, m, Hq, 128), x, dtype=d.dt, device="cuda"),
+                                 0, d.workspace(mc.MC_OP_LAYER_OBSERVE, m))
+        torch.cuda.synchronize()
+        lib.mc_layer_observe(c.cfg, c.batch, layer, mc.ScoreOpts(SM, softcap=50.0, window=window, prefix_len=ten(prefix), doc_start=ten(doc)), q, 0, ws)
+        torch.cuda.synchronize()
+        assert lib.mc_layer_read_status(layer, check=False)[1] == 0
+        got.append([c.gathered("w", b, n) for b, n in enumerate(lens)])
+    assert all(torch.isfinite(w).all() for w in got[0]) and float(sum(w.sum() for w in got[0])) > 0
+    for other in got[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(got[0], other))
