@@ -336,9 +336,20 @@ static mc_status encode_map(CUtensorMap* map, int dtype, const void* base, int r
   EncodeTiledFn fn = encode_tiled_fn();
   if (fn == nullptr) return MC_ERR_UNSUPPORTED;
   const cuuint32_t estr[3] = {1, 1, 1};
-  const CUresult r = fn(map, dtype == MC_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank,
-                        const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                        CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  const auto encode = [&]() {
+    return fn(map, dtype == MC_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank,
+              const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  };
+  CUresult r = encode();
+  if (r != CUDA_SUCCESS) {
+    // (a call of the driver: it wants a current context, and a host thread has none before a call of the runtime that
+    // needs one binds the device's)
+    int dev = 0;
+    MC_CUDA_CHECK(cudaGetDevice(&dev));
+    MC_CUDA_CHECK(cudaSetDevice(dev));
+    r = encode();
+  }
   if (r != CUDA_SUCCESS) {
     set_cuda_error(cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
     return MC_ERR_CUDA;

@@ -151,3 +151,54 @@ def test_weights_under_a_cap_do_not_see_what_they_must_not(L, lens, J, window, p
     assert all(torch.isfinite(w).all() for w in got[0]) and float(sum(w.sum() for w in got[0])) > 0
     for other in got[1:]:
         assert all(torch.equal(a, b) for a, b in zip(got[0], other))
+
+
+
+@pytest.mark.parametrize("op", ["attn", "observe", "observe long", "evict", "prefill"])
+def test_the_first_call_of_a_host_thread(L, op):
+    """A thread that has made no CUDA call of its own yet: the same results as from the thread that made the tensors."""
+    import threading
+    c = L.Cache([4200 if op == "observe long" else 100, 30], 2, 8, 16, "bf16", marks=op == "evict", weights=True)
+    mc, lib = c.mc, c.mc.lib()
+    if op == "attn":
+        q = c.queries(2, 8).cuda()
+        got, ws = torch.zeros_like(q), c.workspace(mc.MC_OP_LAYER_ATTN)
+        call = lambda s: lib.mc_layer_attn(c.cfg, c.batch, c.layer, mc.ScoreOpts(SM), q, None, None, 0, got, None, ws, stream=s)  # noqa: E731
+    elif op == "evict":
+        got, ws = torch.zeros_like(c.d_lens), c.workspace(mc.MC_OP_LAYER_EVICT)
+        call = lambda s: lib.mc_layer_evict(c.cfg, c.batch, c.layer, mc.EvictOpts(50), got, ws, stream=s)  # noqa: E731
+    elif op == "prefill":
+        import mc_harness
+        wl = CONFIGS["c1"].scaled("pf", n_kv_heads=2, n_q_heads=2, dtype="bf16", batch=1, seq_len=128, index=68)
+        case = {k: v.cuda() for k, v in gen.make_projection_case(wl, 0, 128, 128).items()}
+        zeros = torch.zeros_like(case["k_lm1"]).cpu()
+        p = mc_harness.Problem(wl, seq_lens=np.asarray([128], np.int32),
+                               tensors={"k_lm1": case["k_lm1"].cpu(), "v_lm1": case["v_lm1"].cpu(), "k_l": zeros, "v_l": zeros.clone()})
+        got, ws = p.pair.e_k.view(torch.int16), p.workspace(0)
+        call = lambda s: lib.mc_prefill_merge_pair(p.cfg, p.batch(), case["x"], case["w_k"], case["w_v"],  # noqa: E731
+                                                   *[p.pools[k] for k in ("k_lm1", "v_lm1", "k_l", "v_l")], p.pair, 0.9, True, ws, stream=s)
+    else:
+        q, ws, got = c.queries(2, 8, 8).cuda(), c.workspace(mc.MC_OP_LAYER_OBSERVE, 8), c.d["w"]
+        call = lambda s: lib.mc_layer_observe(c.cfg, c.batch, c.layer, mc.ScoreOpts(SM), q, 0, ws, stream=s)  # noqa: E731
+    stream, start, failed = torch.cuda.Stream(), got.clone(), []
+
+    def work():
+        try:
+            call(stream)
+        except Exception as e:  # noqa: BLE001
+            failed.append(e)
+    torch.cuda.synchronize()
+    t = threading.Thread(target=work)
+    t.start()
+    t.join()
+    assert not failed, failed
+    torch.cuda.synchronize()
+    there = got.clone()
+    got.copy_(start)
+    if op == "evict":  # (both find all rows in place)
+        assert there.tolist() == [50, 30]
+        return
+    torch.cuda.synchronize()
+    call(stream)
+    torch.cuda.synchronize()
+    assert torch.equal(there, got) and not torch.equal(there, start)
