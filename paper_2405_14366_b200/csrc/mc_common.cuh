@@ -46,6 +46,13 @@ inline cudaError_t launch_pdl(void (*kernel)(KArgs...), dim3 grid, dim3 block, s
   cfg.numAttrs = 1;
   return cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
 }
+// Lets launches of `kernel` ask for up to `most` bytes of dynamic shared memory.  The limit belongs to the kernel, not to
+// the call: `most` has to be the largest size that any call can need, or one thread's call would lower the limit between
+// another thread's setting and launch.
+template <typename Kernel>
+inline cudaError_t allow_smem(Kernel* kernel, size_t most) {
+  return cudaFuncSetAttribute(reinterpret_cast<const void*>(kernel), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most);
+}
 #if defined(__CUDACC__)
 __device__ __forceinline__ void grid_dep_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void grid_dep_launch() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }

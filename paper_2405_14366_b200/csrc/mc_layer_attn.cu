@@ -787,6 +787,13 @@ static LayerAttnPlan layer_attn_plan(const mc_config* cfg, const mc_batch* bt, i
   pl.lse_bytes = (flags & MC_LAYER_ACCUMULATE) ? align_up((size_t)bt->batch * cfg->n_q_heads * 4, 256) : 0;
   return pl;
 }
+// Shared memory of a CTA: stages, positions, barriers and the batch; where its warps join their results.
+static constexpr size_t attn_smem_used(int batch) {
+  return ((size_t)kLaWarps * kLaStages * (kLaStageBytes + kLaSlice * 4 + 8) + (size_t)(batch + 2) * (4 + sizeof(Seq)) + 15) / 16 * 16;
+}
+static constexpr size_t attn_smem_join(int nq) { return (size_t)kLaWarps * nq * (kHeadDim + 2) * 4; }
+static_assert(1024 + attn_smem_used(kMaxLayerBatch) + attn_smem_join(8) >= 80 * 1024, "the largest size of a launch");
+
 size_t layer_attn_workspace_bytes(const mc_config* cfg, const mc_batch* bt, int flags) {
   const LayerAttnPlan pl = layer_attn_plan(cfg, bt, flags, kLaMaxCtas / kLaCtasPerSm);
   return pl.o_bytes + pl.ml_bytes + pl.score_bytes + pl.lse_bytes;
@@ -834,11 +841,10 @@ mc_status launch_layer_attn(const mc_config* cfg, const mc_batch* bt, const Geom
   ap.n_teams = direct ? bt->batch : pl.n_teams;
   // (asked for so much that two CTAs fill an SM: with room for a third, an early start behind another kernel packs some
   // SMs with three and leaves others with one -- 83 -> 86 us on 8 x 4096)
-  const size_t used = align_up((size_t)kLaWarps * kLaStages * (kLaStageBytes + kLaSlice * 4 + 8) + (size_t)(bt->batch + 2) * (4 + sizeof(Seq)), 16);
-  ap.direct = direct ? (int)used : 0;
-  const size_t smem = std::max<size_t>(80 * 1024, 1024 + used + (direct ? (size_t)kLaWarps * ap.nq * (kHeadDim + 2) * 4 : 0));
+  ap.direct = direct ? (int)attn_smem_used(bt->batch) : 0;
+  const size_t smem = std::max<size_t>(80 * 1024, 1024 + attn_smem_used(bt->batch) + (direct ? attn_smem_join(ap.nq) : 0));
   auto* split = cfg->dtype == MC_F16 ? layer_attn_split_kernel<MC_F16> : layer_attn_split_kernel<MC_BF16>;
-  MC_CUDA_CHECK(cudaFuncSetAttribute(split, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+  MC_CUDA_CHECK(allow_smem(split, 1024 + attn_smem_used(kMaxLayerBatch) + attn_smem_join(8)));
   MC_CUDA_CHECK(launch_pdl(split, dim3(ap.n_teams * pl.team_size), dim3(kLaThreads), smem, stream, ap, map_k, map_v));
   if (!direct) {
     // warps per output row: about three parts each

@@ -388,6 +388,8 @@ size_t layer_evict_workspace_bytes(const mc_config* cfg, const mc_batch* bt) {
   return align_up((size_t)bt->batch * cfg->n_kv_heads * 2 * evict_list_stride(bt) * 4, 256);
 }
 
+static constexpr size_t evict_smem(int keys) { return (size_t)(4 * kEvBins + keys + keys / 32 + 1) * 4; }
+
 mc_status launch_layer_evict(const mc_config* cfg, const mc_batch* bt, const Geom& g, const mc_layer_cache* layer,
                              const mc_evict_opts* opts, int32_t* new_lens, void* workspace, cudaStream_t stream) {
   if (bt->batch == 0) return MC_OK;
@@ -415,8 +417,8 @@ mc_status launch_layer_evict(const mc_config* cfg, const mc_batch* bt, const Geo
     cluster *= 2;
   const int per = (bt->max_seq_len + cluster - 1) / cluster;
   ep.smem_keys = std::min((per + 31) / 32 * 32, kEvSmemKeys);
-  const size_t smem = (size_t)(4 * kEvBins + ep.smem_keys + ep.smem_keys / 32 + 1) * 4;
-  MC_CUDA_CHECK(cudaFuncSetAttribute(layer_evict_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+  const size_t smem = evict_smem(ep.smem_keys);
+  MC_CUDA_CHECK(allow_smem(layer_evict_kernel, evict_smem(kEvSmemKeys)));
   cudaLaunchConfig_t cfgl = {};
   cfgl.gridDim = dim3((unsigned)(bt->batch * cfg->n_kv_heads * cluster));
   cfgl.blockDim = dim3(kEvThreads);

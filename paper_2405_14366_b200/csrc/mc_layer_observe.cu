@@ -1000,6 +1000,14 @@ static int short_tiles(int tiles, long long segs, int nt, int n_sm) {
   return 0;
 }
 
+// Shared memory of a CTA of the two launches, and of the one.
+static constexpr size_t observe_smem(int batch) {
+  return 1024 + kObSmem + (2 * kObMaxStages + 4 + 2 * kObGroups) * 8 + 16 + kObGroups * kObTile * (2 * 8 + 8) + (size_t)(batch + 1) * 4 +
+         (size_t)batch * sizeof(ObSeq);
+}
+static constexpr size_t short_smem(int tiles, int nt) { return 1024 + (size_t)(tiles + nt) * kObTileBytes + kOsArrays; }
+static_assert(short_smem(1, 2) >= 120 * 1024, "the largest size of a launch");
+
 mc_status launch_layer_observe(const mc_config* cfg, const mc_batch* bt, const Geom& g, const mc_layer_cache* layer,
                                const mc_score_opts* opts, const void* q, int n_obs, int flags, void* workspace, cudaStream_t stream) {
   if (bt->batch == 0) return MC_OK;
@@ -1057,8 +1065,8 @@ mc_status launch_layer_observe(const mc_config* cfg, const mc_batch* bt, const G
          {layer_observe_short_kernel<MC_BF16, true, 1>, layer_observe_short_kernel<MC_BF16, true, 2>, layer_observe_short_kernel<MC_BF16, true, 4>}}};
     const Short kern = shorts[cfg->dtype == MC_F16 ? 0 : 1][opts->softcap > 0.f ? 1 : 0][per >> 1];
     // (more than half an SM's shared memory: two CTAs on one SM might wait for each other's tensor memory)
-    const size_t need = std::max<size_t>(1024 + (size_t)(per + op.nt) * kObTileBytes + kOsArrays, 120 * 1024);
-    MC_CUDA_CHECK(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)need));
+    const size_t need = std::max<size_t>(short_smem(per, op.nt), 120 * 1024);
+    MC_CUDA_CHECK(allow_smem(kern, short_smem(per, per == kOsMaxTiles ? 1 : 2)));
     cudaLaunchConfig_t lc = {};
     lc.gridDim = dim3((unsigned)(bt->batch * cfg->n_kv_heads * cluster));
     lc.blockDim = dim3(kOsThreads);
@@ -1077,8 +1085,7 @@ mc_status launch_layer_observe(const mc_config* cfg, const mc_batch* bt, const G
     MC_CUDA_CHECK(cudaGetLastError());
     return MC_OK;
   }
-  const size_t smem = 1024 + kObSmem + (2 * kObMaxStages + 4 + 2 * kObGroups) * 8 + 16 + kObGroups * kObTile * (2 * 8 + 8) + (size_t)(bt->batch + 1) * 4 +
-                      (size_t)bt->batch * sizeof(ObSeq);
+  const size_t smem = observe_smem(bt->batch);
   using Kernel = void (*)(const ObserveParams, const CUtensorMap, const CUtensorMap);
   static const Kernel kernels[2][2][2] = {
       {{layer_observe_kernel<MC_F16, 1, false>, layer_observe_kernel<MC_F16, 1, true>},
@@ -1087,7 +1094,7 @@ mc_status launch_layer_observe(const mc_config* cfg, const mc_batch* bt, const G
        {layer_observe_kernel<MC_BF16, 2, false>, layer_observe_kernel<MC_BF16, 2, true>}}};
   for (int pass = 1; pass <= 2; ++pass) {
     const Kernel kern = kernels[cfg->dtype == MC_F16 ? 0 : 1][pass - 1][opts->softcap > 0.f ? 1 : 0];
-    MC_CUDA_CHECK(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    MC_CUDA_CHECK(allow_smem(kern, observe_smem(kMaxLayerBatch)));
     MC_CUDA_CHECK(launch_pdl(kern, dim3(op.n_ctas), dim3(kObThreads), smem, stream, op, map_k, map_q));
   }
   MC_CUDA_CHECK(cudaGetLastError());

@@ -202,3 +202,66 @@ def test_the_first_call_of_a_host_thread(L, op):
     call(stream)
     torch.cuda.synchronize()
     assert torch.equal(there, got) and not torch.equal(there, start)
+
+
+@pytest.mark.parametrize("op", ["attn", "observe", "observe long", "evict"])
+def test_threads_with_calls_of_different_sizes(L, op):
+    """Host threads, a stream and a workspace each, whose calls need different amounts of shared memory: none is refused, and
+    each gets what it gets alone.  (The library's own entry points, so that the threads meet inside them.)"""
+    import sys
+    import threading
+    small, large = {"attn": ([40] * 2, [40] * 512), "observe": ([500], [500]), "observe long": ([4200], [9] * 511 + [4200]),
+                    "evict": ([60] * 8, [60] * 8)}[op]
+    sides = []
+    for i, lens in enumerate((small, large, small, large)):
+        c = L.Cache(lens, 1, 8, 16, "bf16", seed=i, marks=op == "evict", weights=True, max_len=30000 if op == "evict" and i % 2 else None)
+        mc, lib, s = c.mc, c.mc.lib(), torch.cuda.Stream()
+        raw, made = lib._lib, []
+
+        class Spy:  # the entry point and the arguments that the binding gives it
+            def __getattr__(self, name):
+                def call(*a):
+                    made.append((getattr(raw, name), a))
+                    return getattr(raw, name)(*a)
+                return call
+        if op == "attn":
+            q = c.queries(c.B, 8).cuda()
+            keep = [q, torch.zeros_like(q), c.workspace(mc.MC_OP_LAYER_ATTN)]
+            args = ("mc_layer_attn", c.cfg, c.batch, c.layer, mc.ScoreOpts(SM), q, None, None, 0, keep[1], None, keep[2])
+        elif op == "evict":
+            keep = [None, torch.zeros_like(c.d_lens), c.workspace(mc.MC_OP_LAYER_EVICT)]
+            args = ("mc_layer_evict", c.cfg, c.batch, c.layer, mc.EvictOpts(60), keep[1], keep[2])
+        else:
+            J = 20 if i % 2 else 4
+            keep = [c.queries(c.B, J, 8).cuda(), c.d["w"], c.workspace(mc.MC_OP_LAYER_OBSERVE, J)]
+            args = ("mc_layer_observe", c.cfg, c.batch, c.layer, mc.ScoreOpts(SM), keep[0], 0, keep[2])
+        torch.cuda.synchronize()
+        lib._lib = Spy()
+        try:
+            getattr(lib, args[0])(*args[1:], stream=s)
+        finally:
+            lib._lib = raw
+        torch.cuda.synchronize()
+        sides.append((made[-1], keep[1], keep[1].clone(), c, keep, args, s))
+    refused, start = [0] * len(sides), threading.Barrier(len(sides))
+    times = 20000 if op == "evict" else 2000
+
+    def work(k):
+        call, a = sides[k][0]
+        start.wait()
+        for _ in range(times):
+            refused[k] += 1 if call(*a) else 0
+    threads = [threading.Thread(target=work, args=(k,)) for k in range(len(sides))]
+    was = sys.getswitchinterval()
+    sys.setswitchinterval(1e-6)
+    try:
+        for t in threads:
+            t.start()
+        for t in threads:
+            t.join()
+    finally:
+        sys.setswitchinterval(was)
+    torch.cuda.synchronize()
+    assert refused == [0] * len(sides)
+    for _, got, alone, c, *_ in sides:
+        assert torch.equal(got, alone) and c.mc.lib().mc_layer_read_status(c.layer, check=False)[1] == 0
