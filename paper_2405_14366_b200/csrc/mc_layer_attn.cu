@@ -160,7 +160,6 @@ struct Slice {
 enum { kSlTokens = 1, kSlLoad = 2, kSlFirst = 4, kSlLast = 8, kSlBadSlot = 16 };
 static_assert(kMaxLayerBatch <= 512, "nine bits");
 
-template <int DT>
 __device__ __forceinline__ uint32_t transpose8(uint32_t v) {
   uint32_t r;
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
@@ -488,7 +487,7 @@ layer_attn_split_kernel(const __grid_constant__ LayerAttnParams p, const __grid_
         l0 += e0 + e2;
         l1 += e1 + e3;
         // P as the B operand: rounded once to the storage type (half a step of a number <= 1, as a V element carries)
-        const uint32_t pb0 = transpose8<DT>(Elem<DT>::pack(e0, e1)), pb1 = transpose8<DT>(Elem<DT>::pack(e2, e3));
+        const uint32_t pb0 = transpose8(Elem<DT>::pack(e0, e1)), pb1 = transpose8(Elem<DT>::pack(e2, e3));
         if (hidden) {  // rows that are not seen may hold anything, infinities and NaN too: 0 * x has to stay 0
           for (int k = lane; k < kLaSlice * 16; k += 32) {
             const int r = k >> 4, c = k & 15;

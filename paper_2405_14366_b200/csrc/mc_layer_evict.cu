@@ -86,7 +86,7 @@ __global__ void __launch_bounds__(kEvThreads, 2) layer_evict_kernel(const __grid
   __shared__ Two warp_s[kEvWarps];
   __shared__ uint64_t best_s[kEvWarps];
   __shared__ Two pub[kEvMaxCluster], pub_tie[kEvMaxCluster];  // written by the cluster: (holes, movers) and ties of every CTA
-  __shared__ int found[4];                            // digit, keys above it, keys equal (cluster), keys equal (this CTA)
+  __shared__ int found[3];                            // digit, keys above it, keys equal to it
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int H = p.g.n_kv_heads, ps = p.g.page_size, shift = p.g.page_shift;
   const int seg = blockIdx.x / C, b = seg / H, head = seg - b * H;
@@ -206,7 +206,7 @@ __global__ void __launch_bounds__(kEvThreads, 2) layer_evict_kernel(const __grid
     __syncthreads();
     // a thread takes four digits, the largest first
     const int quad = kEvThreads - 1 - tid;
-    uint4 mine = reinterpret_cast<const uint4*>(h)[quad];
+    const uint4 mine = reinterpret_cast<const uint4*>(h)[quad];
     if (C > 1) {
       reinterpret_cast<uint4*>(h)[quad] = make_uint4(0u, 0u, 0u, 0u);
       const uint32_t v[4] = {mine.x, mine.y, mine.z, mine.w};
@@ -218,7 +218,6 @@ __global__ void __launch_bounds__(kEvThreads, 2) layer_evict_kernel(const __grid
     }
     const uint4 all = C > 1 ? reinterpret_cast<const uint4*>(tot)[quad] : mine;
     const int c4[4] = {(int)all.w, (int)all.z, (int)all.y, (int)all.x};
-    const int m4[4] = {(int)mine.w, (int)mine.z, (int)mine.y, (int)mine.x};
     const int sum = c4[0] + c4[1] + c4[2] + c4[3];
     int incl = sum;
 #pragma unroll
@@ -235,7 +234,6 @@ __global__ void __launch_bounds__(kEvThreads, 2) layer_evict_kernel(const __grid
         found[0] = 4 * quad + 3 - k;
         found[1] = above;
         found[2] = c4[k];
-        found[3] = m4[k];
       }
       above += c4[k];
     }

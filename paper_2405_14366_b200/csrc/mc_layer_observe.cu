@@ -55,7 +55,7 @@ struct ObserveParams {
   float* weights;
   int32_t* status;
   float* part_ml;  // [(CTA + segment)][rows][slots][2]
-  int n_obs, nq, n_q_heads;
+  int n_obs, nq;
   int rows;      // n_obs * nq
   int nq_shift;  // nq = 1, 2, 4 or 8
   int nt;        // row tiles of 128: 1 or 2
@@ -134,7 +134,6 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map
 __device__ __forceinline__ void group_sync(int grp) { asm volatile("bar.sync %0, 128;" ::"r"(1 + grp) : "memory"); }
 __device__ __forceinline__ void pair_sync(int pair) { asm volatile("bar.sync %0, 256;" ::"r"(1 + kObGroups + pair) : "memory"); }
 
-__device__ __forceinline__ void tmem_load(uint32_t addr, uint32_t (&r)[32]) { tmem_ld32(addr, r); }
 __device__ __forceinline__ void tmem_load(uint32_t addr, uint32_t (&r)[16]) {
   tmem_ld16_async(addr, r);
   tmem_wait16(r);
@@ -1022,7 +1021,6 @@ mc_status launch_layer_observe(const mc_config* cfg, const mc_batch* bt, const G
   op.part_ml = (float*)workspace;
   op.n_obs = n_obs;
   op.nq = cfg->n_q_heads / cfg->n_kv_heads;
-  op.n_q_heads = cfg->n_q_heads;
   op.rows = n_obs * op.nq;
   op.nq_shift = op.nq == 1 ? 0 : op.nq == 2 ? 1 : op.nq == 4 ? 2 : 3;
   op.nt = op.rows > kObTile ? 2 : 1;
