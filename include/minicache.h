@@ -651,7 +651,7 @@ mc_status mc_layer_attn(const mc_config* cfg, const mc_batch* batch, const mc_la
  *            mc_score_opts); one at a negative position is ignored (a prompt shorter than n_obs)
  * weights of every cached row = (MC_LAYER_ACCUMULATE: +=) the sum, over the queries and over the query heads of its kv
  *            head, of the softmax probability; every token of every sequence is written.  Positions and q_pos below
- *            2^31 - 1.
+ *            2^31 - 1.  Products and sums are held in fp32; exponentials are good to 2 ulp and a cap's tanh to 5e-8.
  * n_obs * n_q_heads / n_kv_heads at most 256 (MC_ERR_SHAPE).  flags: 0 or MC_LAYER_ACCUMULATE.
  * workspace  mc_layer_workspace_bytes(MC_OP_LAYER_OBSERVE, n_obs) bytes, 256-byte aligned */
 mc_status mc_layer_observe(const mc_config* cfg, const mc_batch* batch, const mc_layer_cache* layer, const mc_score_opts* opts,

@@ -50,7 +50,8 @@ static inline ScoreRule make_score_rule(const mc_score_opts* o) {
 
 #if defined(__CUDACC__)
 // tanh to about 2 ulp.  |x| < 1.4: Lambert's continued fraction x / (1 + x^2 / (3 + x^2 / (5 + ...))) cut behind the
-// 11, as one quotient (truncation below 1.7e-8 relative); larger: 1 - 2 / (1 + e^2x).  The hardware's tanh
+// 11, as one quotient (truncation below 1.7e-8 relative); larger: 1 - 2 / (1 + e^2x).  (__fdividef: 2 ulp, for denominators
+// below 2^126; beyond, where e^2x is, it gives 0 and tanh is 1.)  The hardware's tanh
 // instruction is good to 2^-11 only, which a cap of 50 would turn into an error of 0.02 in the exponent.
 __device__ __forceinline__ float tanh_score(float x) {
   const float y = fabsf(x);

@@ -16,7 +16,8 @@
 // Two stages of 8 KB per warp, 128 KB per SM: a third stage was SLOWER (7b batch 83 -> 88 us, 16 x 8192 grouped 87 ->
 // 93): more requests outstanding than the memory serves well.
 // Short sequences are not split: a CTA takes one whole and joins its warps' results itself (launch_layer_attn).
-// Measured: 83 us on 8 x 4096 tokens of 32 heads (6.45 TB/s: a copy's rate), 86 us on 16 x 8192 of 8 kv heads under a cap.
+// Measured, from a CUDA graph: 83 us on 8 x 4096 tokens of 32 heads (6.45 TB/s: a copy's rate), 87 us on 16 x 8192 of 8 kv
+// heads under a cap.
 // Where a slice's rows come from is worked out a lane per slice, 32 slices at a time and one window ahead: a
 // dependent load takes microseconds while the copies saturate the memory system.
 #include <algorithm>

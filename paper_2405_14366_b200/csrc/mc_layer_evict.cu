@@ -8,10 +8,13 @@
 // of its share of the tokens in shared memory, the budget-th largest key is found digit by digit (11 + 11 + 10 bits:
 // a histogram per CTA, its non-empty bins added to every CTA's total through distributed shared memory), then holes and
 // movers are listed in index order (a warp per run of tokens, counts scanned over the cluster) and the cluster's warps
-// copy the rows.  The steady state of a bounded cache, one token too many, needs no digits: the smallest key goes.
+// copy the rows.  One token too many, the steady state of a bounded cache, needs no digits where a segment has one CTA: the
+// smallest key goes (256 segments of 1025 tokens 4.2 us, of 4097 6.8).  Clusters, which few segments of more than 1024
+// tokens get, take the general way also then (128 segments of 1025 tokens 13.6 us, 8 of 4097 11.9).
 // Bytes: 8 per token for the keys, 2 x 512 per moved row; short caches are bound by the chain of dependent loads and
-// barriers.  Measured: 58 us on 8 x 32 segments of 4096 tokens down to 1000 (202 MB of rows at 5.6 TB/s in 36 us, the
-// selection before it 12 us), 49 us on 4 x 8 of 32768 down to 4096 (115 MB in 20 us).
+// barriers.  Measured, from a CUDA graph and with a copy of 2 to 4 us that puts the marks back: 55 us on 8 x 32 segments of
+// 4096 tokens down to 1000 (202 MB of rows at 5.6 TB/s in 36 us, the selection before it 12 us), 45 us on 4 x 8 of 32768
+// down to 4096 (115 MB in 20 us).
 #include <cooperative_groups.h>
 
 #include <algorithm>
@@ -100,7 +103,7 @@ __global__ void __launch_bounds__(kEvThreads, 2) layer_evict_kernel(const __grid
     was = atomicExch(p.new_lens + b, min(n, p.budget));
   }
   // The new length is in L2 before this grid ends, since the kernel behind may read it before its wait: an exchange has
-  // happened when what was there before is back, and this waits for that.  (5.9 us on 8 x 32 segments of 1025 tokens; a
+  // happened when what was there before is back, and this waits for that.  (8 x 32 segments of 1025 tokens, marks put back: 5.9 us; a
   // store, and a fence here, 6.0; the fence right behind the store 6.4.)
   auto settle = [&]() {
     if (was == 0x7fffffff) __nanosleep(0);

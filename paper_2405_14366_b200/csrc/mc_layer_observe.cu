@@ -19,10 +19,14 @@
 // out of tensor memory, each from a buffer of 128 columns of its own: up to 128 rows they take the tiles in turn, beyond
 // that two of them share a tile, one per 128 rows.  Two threads issue tcgen05.mma, each for two groups: with one, a
 // group that was late kept the others waiting for their next product.  Bounds: the keys' bytes, twice, and the 2 R
-// exponentials per token (16 a clock and SM), with the cap's polynomial on the FMA pipe next to them.  Measured: 165 us on
-// 16 x 8192 tokens, 8 kv heads under 32, 32 queries, a cap (128 rows; 268 MB of keys: 3.3 TB/s over the two passes, 208
-// TFLOP/s); 195 us on 4 x 32749, 64 queries (256 rows; 352 TFLOP/s), of which the exponentials alone are 126.  Every wait is
-// bounded; tensor memory is released on every path.
+// exponentials per token (16 a clock and SM), with the cap's polynomial on the FMA pipe next to them.  Measured, from a CUDA
+// graph: 168 us on 16 x 8192 tokens, 8 kv heads under 32, 32 queries, a cap (128 rows; 268 MB of keys: 3.2 TB/s over the two
+// passes, 205 TFLOP/s); 195 us on 4 x 32749, 64 queries (256 rows; 352 TFLOP/s), of which the exponentials alone are 126.
+// (Hundreds of passes back to back meet the power cap: 173 us at 1.84 GHz, 211 at 1.77, against 1.965.)
+// Exactness: products and sums in binary32; exponentials to 2 ulp with results below 2^-126 flushed; the cap's tanh to 5e-8
+// relative, its constants rounded once into the polynomial's coefficients.  Against 64 bits the weights are off by 1.7 times
+// what elementary binary32 operations are.
+// Every wait is bounded; tensor memory is taken behind the wait for the grid ahead and released on every path.
 #include <cooperative_groups.h>
 #include <math.h>
 
@@ -166,9 +170,10 @@ __device__ __forceinline__ void factors(const ObserveParams& p, uint32_t (&raw)[
   for (int k = 0; k < kObChunk; k += 2) big = max3_abs(big, __uint_as_float(raw[k]), __uint_as_float(raw[k + 1]));
   // Which form an accumulator takes follows from its own magnitude, as the forms differ in their last bits and most warps
   // hold accumulators that do not count (hidden, stale); the vote only spares the warp the forms that none of its
-  // accumulators takes.  (A NaN is dropped by the maximum and stays one in every form.  A form for the whole warp with what
-  // does not count masked ahead of the vote: 157 -> 187 us on 16 x 8192 tokens and 8 kv heads under 32 with 32 queries, from
-  // the registers that the masks took; this: 157 -> 155, and up to 13 % more where most scores lie beyond the cap.)
+  // accumulators takes.  (A NaN is dropped by the maximum and stays one in every form.  One form for the whole warp, with
+  // what does not count masked ahead of the vote, took 187 us on 16 x 8192 tokens, 8 kv heads under 32 and 32 queries, from
+  // the registers that the masks need, and 157 with the vote alone; this takes 155, 168 instead of 164 where scores reach
+  // half the cap, and up to 13 % more where most of them lie beyond it.)
   if (__all_sync(0xffffffffu, big <= p.tiny_max)) {
 #pragma unroll
     for (int k = 0; k < kObChunk / 2; ++k) {
