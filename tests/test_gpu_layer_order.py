@@ -265,3 +265,65 @@ def test_threads_with_calls_of_different_sizes(L, op):
     assert refused == [0] * len(sides)
     for _, got, alone, c, *_ in sides:
         assert torch.equal(got, alone) and c.mc.lib().mc_layer_read_status(c.layer, check=False)[1] == 0
+
+
+def drawn(seed):
+    import random
+    r = random.Random(seed)
+    nq, H = r.choice([1, 2, 4, 8]), r.choice([1, 2, 3])
+    return dict(H=H, Hq=H * nq, nq=nq, ps=r.choice([16, 32, 64]), dtype=r.choice(["f16", "bf16"]), marks=r.random() < 0.5,
+                lens=[r.choice([0, 1, 15, 16, 17, 63, 64, 130, 700, 1500]) for _ in range(r.randint(1, 5))] + [r.choice([33, 600, 4500])],
+                cap=r.choice([0.0, 0.5, 5.0, 50.0]), alibi=r.random() < 0.4, window=r.choice([0, 0, 1, 40, 900]), prefix=r.choice([0, 0, 5]),
+                doc=r.choice([0, 0, 30]), J=r.randint(1, 200 // nq if nq > 1 else 64), append=r.random() < 0.5, sm=r.choice([SM, -SM, 0.5]))
+
+
+@pytest.mark.parametrize("seed", range(40))
+def test_no_bit_follows_from_what_is_not_seen(L, seed):
+    """Drawn shapes and options: the rows that no query of a head sees, those behind the sequences and nobody's pages change, and
+    so does what the call before left behind; out, lse and weights do not."""
+    o = drawn(seed)
+    lens, H, Hq, ps, B, J = o["lens"], o["H"], o["Hq"], o["ps"], len(o["lens"]), o["J"]
+    got = []
+    for fill in (0.0, 6.0e4, float("nan"), -float("inf")):
+        c = L.Cache(lens, H, Hq, ps, o["dtype"], seed=seed, marks=o["marks"], weights=True, poison=False)
+        mc, lib = c.mc, c.mc.lib()
+        last = [x - 1 for x in c.q_next] if o["marks"] else [n - 1 for n in lens]
+        keeps = []
+        for queries in (1, J):  # the step's query stands at last + 1 if its row is new; the observed ones end at last
+            keep = torch.zeros(c.n_pages, H, ps, dtype=torch.bool)
+            for b, n in enumerate(lens):
+                t, p = torch.arange(n), c.dense_pos[b]
+                at = [last[b] + (1 if o["append"] else 0)] if queries == 1 else [last[b] - j for j in range(J) if last[b] - j >= 0]
+                ok = torch.zeros(n, H, dtype=torch.bool)
+                for x in at:
+                    ok |= L.seen(p, x, o["window"], o["doc"], o["prefix"])
+                keep[c.table[b, t // ps].long(), :, t % ps] = ok
+            keeps.append(keep)
+        ten = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+        some = lambda x: ten([x] * B) if x else None  # noqa: E731
+        slopes = torch.exp2(-8.0 * torch.arange(1, Hq + 1) / Hq).cuda() if o["alibi"] else None
+        opts = lambda q_pos: mc.ScoreOpts(o["sm"], softcap=o["cap"], alibi_slopes=slopes, window=o["window"], prefix_len=some(o["prefix"]),  # noqa: E731
+                                          doc_start=some(o["doc"]), q_pos=ten(q_pos) if o["marks"] else None)
+        q, qo, kn, vn = c.queries(B, Hq).cuda(), c.queries(B, J, Hq).cuda(), c.rows(B, H).cuda(), c.rows(B, H).cuda()
+        flags = mc.MC_LAYER_ACCUMULATE | (mc.MC_LAYER_APPEND if o["append"] else 0)
+        out, lse = torch.zeros_like(q), torch.zeros(B, Hq, device="cuda")
+        stale = L.Cache([max(lens)] * 4, H, Hq, ps, o["dtype"], poison=False, weights=True)
+        stale.d["k"].fill_(0.0 if fill != fill else fill)
+        results = []
+        for i in (1, 0):
+            for k in ("k", "v"):
+                c.d[k].copy_(torch.where(keeps[i][..., None], getattr(c, k), torch.full((), fill).to(c.dt)))
+            lib.mc_layer_observe(stale.cfg, stale.batch, stale.layer, mc.ScoreOpts(o["sm"], softcap=o["cap"]), c.queries(4, J, Hq).cuda() * 30, 0,
+                                 stale.workspace(mc.MC_OP_LAYER_OBSERVE, J))
+            if i:
+                lib.mc_layer_observe(c.cfg, c.batch, c.layer, opts(last), qo, 0, c.workspace(mc.MC_OP_LAYER_OBSERVE, J))
+            else:
+                lib.mc_layer_attn(c.cfg, c.batch, c.layer, opts([x + (1 if o["append"] else 0) for x in last]), q, kn if o["append"] else None,
+                                  vn if o["append"] else None, flags, out, lse, c.workspace(mc.MC_OP_LAYER_ATTN, flags))
+            torch.cuda.synchronize()
+            results += [c.gathered("w", b, n) for b, n in enumerate(lens)]
+        assert lib.mc_layer_read_status(c.layer, check=False)[1] == 0
+        got.append(results + [out.cpu().view(torch.int16), lse.cpu()])
+    assert not any(torch.isnan(x.float()).any() for x in got[0])
+    for other in got[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(got[0], other))
