@@ -64,6 +64,35 @@ def test_observe_behind_a_prefill_merge(L, lens, Hq, J, graph):
     assert all(torch.equal(a, b) for a, b in zip(*got)) and float(got[0][0].sum()) > 0
 
 
+@pytest.mark.parametrize("lens,Hq,J", [([512, 300], 8, 40), ([700, 1], 2, 128), ([4200, 77], 8, 20)])
+def test_observe_next_to_a_prefill_merge(L, lens, Hq, J):
+    """The same two operators at the same time, on streams of their own: each gets what it gets alone.  (A CTA that holds tensor
+    memory never waits for one that may not have it: the merge's wait for nobody, a cluster's wait for CTAs that wait for those.)"""
+    import mc_harness
+    wl = CONFIGS["c1"].scaled("pf", n_kv_heads=8, n_q_heads=8, dtype="bf16", batch=4, seq_len=512, index=68)
+    case = {k: v.cuda() for k, v in gen.make_projection_case(wl, 0, 1024, 512).items()}
+    zeros = torch.zeros_like(case["k_lm1"]).cpu()
+    p = mc_harness.Problem(wl, seq_lens=np.asarray([512, 512, 400, 512], np.int32),
+                           tensors={"k_lm1": case["k_lm1"].cpu(), "v_lm1": case["v_lm1"].cpu(), "k_l": zeros, "v_l": zeros.clone()})
+    ws_p, pools = p.workspace(0), [p.pools[k] for k in ("k_lm1", "v_lm1", "k_l", "v_l")]
+    c = L.Cache(lens, 2, Hq, 16, "bf16", seed=3, weights=True)
+    mc, lib = c.mc, c.mc.lib()
+    q, ws = c.queries(len(lens), J, Hq).cuda(), c.workspace(mc.MC_OP_LAYER_OBSERVE, J)
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    got = []
+    for times in (1, 100):
+        torch.cuda.synchronize()
+        for _ in range(times):
+            lib.mc_prefill_merge_pair(p.cfg, p.batch(), case["x"], case["w_k"], case["w_v"], *pools, p.pair, 0.9, False, ws_p, stream=streams[0])
+            if times == 1:
+                torch.cuda.synchronize()
+            lib.mc_layer_observe(c.cfg, c.batch, c.layer, mc.ScoreOpts(SM), q, 0, ws, stream=streams[1])
+        torch.cuda.synchronize()
+        assert lib.mc_layer_read_status(c.layer, check=False)[1] == 0
+        got.append([c.d["w"].clone(), p.pair.e_k.clone().view(torch.int16)])
+    assert all(torch.equal(a, b) for a, b in zip(*got)) and float(got[0][0].sum()) > 0
+
+
 def unseen_filled(L, lens, H, Hq, ps, dtype, fill, visible, seed=11, max_len=None):
     """A cache whose rows outside visible(b) (a truth value per token) all hold `fill`: hidden, behind the sequence, of nobody."""
     c = L.Cache(lens, H, Hq, ps, dtype, seed=seed, weights=True, poison=False, max_len=max_len)
