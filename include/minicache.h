@@ -684,6 +684,102 @@ mc_status mc_layer_evict(const mc_config* cfg, const mc_batch* batch, const mc_l
  * mc_read_status does. */
 mc_status mc_layer_read_status(const mc_layer_cache* layer, void* stream, int32_t* out_words);
 
+/* ---- One layer held in 4 bits -------------------------------------------------------------------------------
+ * The layers below S when the model's caches are 4-bit (mc_layer_q4): rows are written by mc_layer_q4_append and read
+ * back by mc_layer_q4_read, attended by mc_layer_q4_attn, over all pages or over those that mc_layer_q4_select names.
+ * (The paper has no counterpart: Sec. 5 puts MiniCache on top of a 4-bit cache and leaves that cache to the engine.)
+ * - cfg->page_size is 32, one key group; cfg->cache_bits is not looked at.  The conventions and limits of "One
+ *   uncompressed layer" hold (its own mc_batch, order of writing calls, batch at most 512), with units of 32 tokens:
+ *   batch * n_kv_heads * (max_seq_len / 32 + 2) below 2^31.
+ * - Only complete pages are in the pools: the tokens [32 floor(n / 32), n) of a sequence of n are 16-bit rows of res_k
+ *   and res_v.  The block table needs an entry for a page once the page is complete.  Complete pages are in the format of
+ *   mc_layer_q4: what mc_layer_q4_append wrote is what mc_merge_pair_q4 reads (for sequences of whole pages). */
+
+/* k_codes, k_meta, v_codes, v_meta  the pools of mc_layer_q4, [n_pages] pages.  value = code * scale + zero; scales are
+ *                                   positive and at most 16000 (mc_layer_q4_append writes none above 8736)
+ * res_k, res_v  [batch][n_kv_heads][32][128] of cfg->dtype: the rows of the begun page, token t at slot t % 32; slots
+ *               behind the sequence's last token may hold anything
+ * status        [MC_STATUS_WORDS] int32, cleared by the caller; flags accumulate.  All but status 256-byte aligned. */
+typedef struct mc_layer_q4_cache {
+  void* k_codes;
+  void* k_meta;
+  void* v_codes;
+  void* v_meta;
+  void* res_k;
+  void* res_v;
+  int32_t* status;
+} mc_layer_q4_cache;
+
+enum { MC_OP_LAYER_Q4_ATTN = 5, MC_OP_LAYER_Q4_SELECT = 6 }; /* mc_layer_workspace_bytes; arg: the call's flags, 0 */
+
+/* Appends rows behind the seq_lens[b] cached tokens of every sequence: a prompt, a chunk of one, single tokens.
+ * k, v         row r of kv head h at element r * k_stride + h * 128 (v alike), cfg->dtype: the rows of a projection, packed
+ *              or not.  Strides at least n_kv_heads * 128 and multiples of 8; bases 16-byte aligned; no part of the cache.
+ * row_offsets  device [batch + 1]: sequence b gets the rows [row_offsets[b], row_offsets[b + 1]).  If one lies
+ *              outside [0, n_rows] or below the one before it, that is flagged (MC_FLAG_BAD_METADATA) and nothing is done.
+ * n_rows       rows in k and v, below 2^30
+ * Pages that fill are quantised: zero = min and scale = (max - min) / 15 of a group, each rounded once to binary16 (scale
+ * 1 where that is 0), code = clamp(rint((x - zero) / scale), 0, 15) with the rounded ones, in arithmetic that gives the
+ * integers of the exact quotient.  What a page takes in is limited to +-65504 (bfloat16: +-65280, its
+ * largest below that), a NaN counts as 0.  The other rows go to res_k, res_v unchanged; slots that receive none keep what they held.  A page whose slot lies past max_pages_per_seq or whose id is
+ * out of range is flagged and not written.  seq_lens is not modified: batch->max_seq_len bounds the lengths before the call. */
+mc_status mc_layer_q4_append(const mc_config* cfg, const mc_batch* batch, const mc_layer_q4_cache* layer, const void* k,
+                             const void* v, int64_t k_stride, int64_t v_stride, const int32_t* row_offsets, int32_t n_rows,
+                             void* stream);
+
+/* Reads tokens back as 16-bit rows: token begin[b] + i of sequence b goes to row row_offsets[b] + i of k and v (laid out
+ * as in mc_layer_q4_append) for i < row_offsets[b + 1] - row_offsets[b].  begin: device [batch] or NULL (0).  A token behind
+ * seq_lens[b] leaves its row as it was; a negative begin, bad offsets and bad pages are flagged, their rows left alone.
+ * Values are code * scale + zero rounded once to binary16, or formed in binary32 and rounded to bfloat16, limited to the
+ * type's largest finite number; rows of the begun page are copied. */
+mc_status mc_layer_q4_read(const mc_config* cfg, const mc_batch* batch, const mc_layer_q4_cache* layer, const int32_t* begin, void* k,
+                           void* v, int64_t k_stride, int64_t v_stride, const int32_t* row_offsets, int32_t n_rows, void* stream);
+
+/* Which pages mc_layer_q4_select keeps.
+ * budget    pages per (sequence, kv head), at least 1, at least n_sink + n_recent
+ * n_sink    the first n_sink pages of a sequence stay;  n_recent: the last n_recent complete ones stay */
+typedef struct mc_page_selection {
+  int32_t budget;
+  int32_t n_sink;
+  int32_t n_recent;
+  int32_t reserved;
+} mc_page_selection;
+
+/* Names per (sequence, kv head) the complete pages worth attending: the guarded ones, then those with the largest bound of
+ * the group's scores, sum over the kv head's query heads of sum_c max(q_c lo_c, q_c hi_c), where lo = zero and hi = zero +
+ * 15 scale are what channel c of a key of that page can hold at least and at most.  The keys' group parameters are all it
+ * reads of the cache, a tenth.  Sums are held in 64 bits, so the choice does not depend on their order; ties go to the
+ * lower page, a NaN ranks below every number.  Only pages with a token that the query sees are named (opts' masks; the query's
+ * position is opts->q_pos, NULL: seq_lens[b], the step's new token).  opts->alibi_slopes must be NULL and sm_scale positive
+ * (MC_ERR_UNSUPPORTED): the order of the bounds is then that of the scores.
+ * q          [batch][n_q_heads][128]
+ * pages      [batch][n_kv_heads][budget] int32: page slots of the sequence (block-table columns), ascending; entries behind
+ *            the count are left as they were
+ * counts     [batch] int32: min(budget, pages with a visible token), the same for every kv head
+ * workspace  mc_layer_workspace_bytes(MC_OP_LAYER_Q4_SELECT, 0) bytes, 256-byte aligned.  max_seq_len at most 2^20. */
+mc_status mc_layer_q4_select(const mc_config* cfg, const mc_batch* batch, const mc_layer_q4_cache* layer, const mc_score_opts* opts,
+                             const mc_page_selection* keep, const void* q, int32_t* pages, int32_t* counts, void* workspace,
+                             size_t workspace_bytes, void* stream);
+
+/* Single-query attention of every sequence over one 4-bit layer: the complete pages, the rows of the begun page and the
+ * step's new row.  Scores, masks, q, k_new, v_new, out and lse as in mc_layer_attn (a token's index is its position).
+ * pages, counts, pages_stride  NULL, NULL, 0: every complete page that the query sees.  Else only pages[b][h][0 .. counts[b]),
+ *              pages_stride entries per (sequence, kv head), as mc_layer_q4_select writes them: page slots in ascending
+ *              order; an entry that is not above the one before it or names no complete page is flagged and skipped.  The
+ *              begun page's rows and the new row are always attended (as far as the masks let them).
+ * flags        MC_LAYER_APPEND: the new row is also written behind the cached tokens, as mc_layer_q4_append does it (the page
+ *              it completes is quantised).  seq_lens is not modified.
+ * workspace    mc_layer_workspace_bytes(MC_OP_LAYER_Q4_ATTN, flags) bytes, 256-byte aligned
+ * The products of a query with a group's scales are kept to 22 bits, scores, maxima and sums in fp32; probabilities, and
+ * their products with the values' scales, are rounded to 11 bits before they meet the codes. */
+mc_status mc_layer_q4_attn(const mc_config* cfg, const mc_batch* batch, const mc_layer_q4_cache* layer, const mc_score_opts* opts,
+                           const int32_t* pages, const int32_t* counts, int32_t pages_stride, const void* q, const void* k_new,
+                           const void* v_new, int32_t flags, void* out, float* lse, void* workspace, size_t workspace_bytes,
+                           void* stream);
+
+/* mc_layer_read_status for a 4-bit layer. */
+mc_status mc_layer_q4_read_status(const mc_layer_q4_cache* layer, void* stream, int32_t* out_words);
+
 /* Self-test of the error path of the bounded waits (the paper has no counterpart): enqueues a
  * one-warp kernel that waits, with the same bounded wait the streaming kernels use and a limit of
  * `poll_limit` polls, on a barrier that nothing completes.  The wait gives up, sets

@@ -10,6 +10,8 @@ from .binding import (  # noqa: F401
     LayerCache,
     ScoreOpts,
     EvictOpts,
+    LayerQ4Cache,
+    PageSelection,
     lib,
     MC_LAYER_LM1,
     MC_LAYER_L,
@@ -22,5 +24,7 @@ from .binding import (  # noqa: F401
     MC_OP_LAYER_ATTN,
     MC_OP_LAYER_OBSERVE,
     MC_OP_LAYER_EVICT,
+    MC_OP_LAYER_Q4_ATTN,
+    MC_OP_LAYER_Q4_SELECT,
     McError,
 )

@@ -17,6 +17,7 @@ MC_RETAIN_DISTINCT, MC_RETAIN_LITERAL, MC_RETAIN_TOPK = 0, 1, 2
 MC_LAYER_LM1, MC_LAYER_L, MC_LAYER_BOTH = 0, 1, 2
 MC_OP_MERGE, MC_OP_DECODE_ATTN = 0, 1
 MC_OP_LAYER_ATTN, MC_OP_LAYER_OBSERVE, MC_OP_LAYER_EVICT = 2, 3, 4
+MC_OP_LAYER_Q4_ATTN, MC_OP_LAYER_Q4_SELECT = 5, 6
 MC_LAYER_APPEND, MC_LAYER_ACCUMULATE = 1, 2
 MC_STATUS_WORDS = 4
 MC_STATUS_FLAGS, MC_STATUS_RETAINED_TOTAL, MC_STATUS_NEAR_THRESHOLD = 0, 1, 2
@@ -82,6 +83,15 @@ class _EvictOpts(C.Structure):
     _fields_ = [("q_pos", C.c_void_p), ("budget", C.c_int32), ("n_sink", C.c_int32), ("n_recent", C.c_int32), ("reserved", C.c_int32)]
 
 
+class _LayerQ4Cache(C.Structure):
+    _fields_ = [("k_codes", C.c_void_p), ("k_meta", C.c_void_p), ("v_codes", C.c_void_p), ("v_meta", C.c_void_p),
+                ("res_k", C.c_void_p), ("res_v", C.c_void_p), ("status", C.c_void_p)]
+
+
+class _PageSelection(C.Structure):
+    _fields_ = [("budget", C.c_int32), ("n_sink", C.c_int32), ("n_recent", C.c_int32), ("reserved", C.c_int32)]
+
+
 class _PairSizes(C.Structure):
     _fields_ = [("tile_bytes", C.c_size_t), ("e_bytes", C.c_size_t), ("dist_bytes", C.c_size_t),
                 ("ret_count_bytes", C.c_size_t), ("ret_offset_bytes", C.c_size_t), ("ret_index_bytes", C.c_size_t),
@@ -99,7 +109,8 @@ class _Stats(C.Structure):
 EXPORTS = ("mc_decode_drain_host", "mc_decode_stage_host", "mc_decode_attn_append", "mc_prefill_merge_pair", "mc_admit_sequences", "mc_build_flags", "mc_merge_pairs", "mc_pair_bytes", "mc_get_stats", "mc_version", "mc_status_str", "mc_last_cuda_error", "mc_workspace_bytes", "mc_merge_pair",
            "mc_append_pair", "mc_restore", "mc_decode_attn", "mc_read_status", "mc_merge_pair_host",
            "mc_decode_attn_host", "mc_decode_io_bytes", "mc_decode_attn_static", "mc_merge_pair_q4", "mc_selftest_wait_timeout",
-           "mc_layer_workspace_bytes", "mc_layer_attn", "mc_layer_observe", "mc_layer_evict", "mc_layer_read_status")
+           "mc_layer_workspace_bytes", "mc_layer_attn", "mc_layer_observe", "mc_layer_evict", "mc_layer_read_status",
+           "mc_layer_q4_append", "mc_layer_q4_read", "mc_layer_q4_select", "mc_layer_q4_attn", "mc_layer_q4_read_status")
 
 
 def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
@@ -411,6 +422,68 @@ class EvictOpts:
         return _EvictOpts(None if q is None else q.data_ptr(), int(self.budget), int(self.n_sink), int(self.n_recent), 0)
 
 
+@dataclasses.dataclass
+class LayerQ4Cache:
+    """One layer held in 4 bits (caller-owned tensors, see mc_layer_q4_cache): k_codes / v_codes uint8
+    [n_pages][n_kv_heads][32][64], k_meta [n_pages][n_kv_heads][128][2] / v_meta [n_pages][n_kv_heads][32][4][2] float16
+    (scale, zero), res_k / res_v [batch][n_kv_heads][32][128] in the storage type, status int32 [MC_STATUS_WORDS] (zeros;
+    made here if not given)."""
+    cfg: McConfig
+    k_codes: torch.Tensor
+    k_meta: torch.Tensor
+    v_codes: torch.Tensor
+    v_meta: torch.Tensor
+    res_k: torch.Tensor
+    res_v: torch.Tensor
+    status: Optional[torch.Tensor] = None
+
+    def __post_init__(self):
+        if self.status is None:
+            self.status = torch.zeros(MC_STATUS_WORDS, dtype=torch.int32, device=self.k_codes.device)
+
+    @classmethod
+    def empty(cls, cfg: McConfig, batch: int, n_pages: int, device="cuda") -> "LayerQ4Cache":
+        """A cache of n_pages pages for `batch` sequences, its contents undefined."""
+        h = cfg.n_kv_heads
+        mk = lambda shape, dt: torch.empty(shape, dtype=dt, device=device)  # noqa: E731
+        return cls(cfg, mk((n_pages, h, 32, 64), torch.uint8), mk((n_pages, h, 128, 2), torch.float16), mk((n_pages, h, 32, 64), torch.uint8),
+                   mk((n_pages, h, 32, 4, 2), torch.float16), mk((batch, h, 32, 128), cfg.torch_dtype), mk((batch, h, 32, 128), cfg.torch_dtype))
+
+    def c(self, batch: int, n_pages: int, cfg: Optional[McConfig] = None, dev: Optional[int] = None) -> _LayerQ4Cache:
+        """cfg: the call's configuration (default: the cache's own), of which the pools have to hold n_pages pages and the
+        begun pages `batch` sequences; dev: the device that the tensors have to be on."""
+        cfg = cfg or self.cfg
+        dt, tiles, begun = cfg.torch_dtype, n_pages * cfg.n_kv_heads, batch * cfg.n_kv_heads * 4096
+        kc, km, vc, vm, rk, rv, st = self.k_codes, self.k_meta, self.v_codes, self.v_meta, self.res_k, self.res_v, self.status
+        if not (_good(kc, torch.uint8, 2048 * tiles, dev) and _good(km, torch.float16, 256 * tiles, dev)
+                and _good(vc, torch.uint8, 2048 * tiles, dev) and _good(vm, torch.float16, 256 * tiles, dev)
+                and _good(rk, dt, begun, dev) and _good(rv, dt, begun, dev) and _good(st, torch.int32, MC_STATUS_WORDS, dev)):
+            _refuse(dev, k_codes=(kc, torch.uint8, 2048 * tiles), k_meta=(km, torch.float16, 256 * tiles),
+                    v_codes=(vc, torch.uint8, 2048 * tiles), v_meta=(vm, torch.float16, 256 * tiles), res_k=(rk, dt, begun),
+                    res_v=(rv, dt, begun), status=(st, torch.int32, MC_STATUS_WORDS))
+        return _LayerQ4Cache(kc.data_ptr(), km.data_ptr(), vc.data_ptr(), vm.data_ptr(), rk.data_ptr(), rv.data_ptr(), st.data_ptr())
+
+
+@dataclasses.dataclass
+class PageSelection:
+    """Which pages mc_layer_q4_select keeps (see mc_page_selection)."""
+    budget: int
+    n_sink: int = 0
+    n_recent: int = 0
+
+    def c(self) -> _PageSelection:
+        return _PageSelection(int(self.budget), int(self.n_sink), int(self.n_recent), 0)
+
+
+def _row_stride(name: str, t: torch.Tensor, cfg: "McConfig", rows: int, dev: int) -> int:
+    """Elements between two rows of [rows][n_kv_heads][128], whose heads have to be next to each other."""
+    sh, st = t.shape, t.stride()
+    if not (t.dtype is cfg.torch_dtype and len(sh) == 3 and sh[0] == rows and sh[1] == cfg.n_kv_heads and sh[2] == 128 and st[2] == 1
+            and (st[1] == 128 or sh[1] == 1) and t.get_device() == dev):
+        raise AssertionError(f"{name}: [rows][n_kv_heads][128] of {cfg.torch_dtype} with adjacent heads on device {dev} is wanted")
+    return st[0] if rows > 1 else max(st[0], cfg.n_kv_heads * 128)
+
+
 class MiniCacheLib:
     """Loads libminicache.so and exposes its entry points under their C names."""
 
@@ -471,6 +544,14 @@ class MiniCacheLib:
         L.mc_layer_evict.argtypes = [P(_Config), P(_Batch), P(_LayerCache), P(_EvictOpts), V, V, C.c_size_t, V]
         L.mc_layer_read_status.argtypes = [P(_LayerCache), V, P(C.c_int32)]
         for f in ("mc_layer_workspace_bytes", "mc_layer_attn", "mc_layer_observe", "mc_layer_evict", "mc_layer_read_status"):
+            getattr(L, f).restype = C.c_int32
+        head = [P(_Config), P(_Batch), P(_LayerQ4Cache)]
+        L.mc_layer_q4_append.argtypes = head + [V, V, C.c_int64, C.c_int64, V, C.c_int32, V]
+        L.mc_layer_q4_read.argtypes = head + [V, V, V, C.c_int64, C.c_int64, V, C.c_int32, V]
+        L.mc_layer_q4_select.argtypes = head + [P(_ScoreOpts), P(_PageSelection), V, V, V, V, C.c_size_t, V]
+        L.mc_layer_q4_attn.argtypes = head + [P(_ScoreOpts), V, V, C.c_int32, V, V, V, C.c_int32, V, V, V, C.c_size_t, V]
+        L.mc_layer_q4_read_status.argtypes = [P(_LayerQ4Cache), V, P(C.c_int32)]
+        for f in ("mc_layer_q4_append", "mc_layer_q4_read", "mc_layer_q4_select", "mc_layer_q4_attn", "mc_layer_q4_read_status"):
             getattr(L, f).restype = C.c_int32
         L.mc_selftest_wait_timeout.argtypes = [P(_PairCache), C.c_int32, V]
         L.mc_selftest_wait_timeout.restype = C.c_int32
@@ -680,7 +761,8 @@ class MiniCacheLib:
 
     # -- one uncompressed layer -------------------------------------------------------------------
     def mc_layer_workspace_bytes(self, cfg: McConfig, batch: Batch, op: int, arg: int = 0) -> int:
-        """arg: the call's flags (MC_OP_LAYER_ATTN), the number of observed queries (MC_OP_LAYER_OBSERVE), 0 (MC_OP_LAYER_EVICT)."""
+        """arg: the call's flags (MC_OP_LAYER_ATTN, MC_OP_LAYER_Q4_ATTN), the number of observed queries (MC_OP_LAYER_OBSERVE),
+        0 (MC_OP_LAYER_EVICT, MC_OP_LAYER_Q4_SELECT)."""
         out = C.c_size_t(0)
         c, b = cfg.c(), batch.c()
         self._check(self._lib.mc_layer_workspace_bytes(C.byref(c), C.byref(b), int(op), int(arg), C.byref(out)))
@@ -745,6 +827,95 @@ class MiniCacheLib:
         words = (C.c_int32 * MC_STATUS_WORDS)()
         l = layer.c(0)
         code = self._lib.mc_layer_read_status(C.byref(l), _stream(stream), words)
+        if check:
+            self._check(code)
+        return list(words), code
+
+    # -- one layer held in 4 bits -----------------------------------------------------------------
+    def _q4_rows(self, cfg, batch, layer, k, v, row_offsets, stream):
+        """What mc_layer_q4_append and mc_layer_q4_read have in common: k, v [rows][n_kv_heads][128], row_offsets int32 [batch + 1]."""
+        dev, rows = k.get_device(), k.size(0)
+        b = batch.layer_c(dev)
+        ks, vs = _row_stride("k", k, cfg, rows, dev), _row_stride("v", v, cfg, rows, dev)
+        if not _good(row_offsets, torch.int32, b.batch + 1, dev):
+            _refuse(dev, row_offsets=(row_offsets, torch.int32, b.batch + 1))
+        return _cfg_c(cfg), b, layer.c(b.batch, b.n_pages, cfg, dev), ks, vs, rows, _layer_stream(stream, dev)
+
+    def mc_layer_q4_append(self, cfg: McConfig, batch: Batch, layer: LayerQ4Cache, k, v, row_offsets: torch.Tensor, stream=None):
+        """k, v [rows][n_kv_heads][128], parts of a wider row allowed; sequence b gets rows row_offsets[b] .. row_offsets[b + 1]."""
+        c, b, l, ks, vs, rows, at = self._q4_rows(cfg, batch, layer, k, v, row_offsets, stream)
+        code = self._lib.mc_layer_q4_append(c, b, l, k.data_ptr(), v.data_ptr(), ks, vs, row_offsets.data_ptr(), rows, at)
+        if code:
+            self._check(code)
+
+    def mc_layer_q4_read(self, cfg: McConfig, batch: Batch, layer: LayerQ4Cache, begin: Optional[torch.Tensor], k, v,
+                         row_offsets: torch.Tensor, stream=None):
+        """Writes tokens begin[b] + i (begin int32 [batch] or None) to rows row_offsets[b] + i of k and v [rows][n_kv_heads][128]."""
+        c, b, l, ks, vs, rows, at = self._q4_rows(cfg, batch, layer, k, v, row_offsets, stream)
+        if begin is not None and not _good(begin, torch.int32, b.batch, k.get_device()):
+            _refuse(k.get_device(), begin=(begin, torch.int32, b.batch))
+        code = self._lib.mc_layer_q4_read(c, b, l, None if begin is None else begin.data_ptr(), k.data_ptr(), v.data_ptr(), ks, vs,
+                                          row_offsets.data_ptr(), rows, at)
+        if code:
+            self._check(code)
+
+    def mc_layer_q4_select(self, cfg: McConfig, batch: Batch, layer: LayerQ4Cache, opts: ScoreOpts, keep: PageSelection, q, pages,
+                           counts, workspace: torch.Tensor, stream=None):
+        """pages int32 [batch][n_kv_heads][budget], counts int32 [batch] receive the selection."""
+        dev = q.get_device()
+        c, b = _cfg_c(cfg), batch.layer_c(dev)
+        n, rows_q, dt = b.batch, b.batch * cfg.n_q_heads * 128, cfg.torch_dtype
+        if not (_good(q, dt, 0, dev) and q.numel() == rows_q and _good(pages, torch.int32, 0, dev)
+                and pages.numel() == n * cfg.n_kv_heads * keep.budget and _good(counts, torch.int32, 0, dev) and counts.numel() == n
+                and workspace.get_device() == dev):
+            _refuse(dev, q=(q, dt, rows_q), pages=(pages, torch.int32, n * cfg.n_kv_heads * keep.budget), counts=(counts, torch.int32, n),
+                    workspace=(workspace, workspace.dtype, 0))
+            raise AssertionError("q [batch][n_q_heads][128], pages [batch][n_kv_heads][budget] and counts [batch] are wanted")
+        l, o, at = layer.c(n, b.n_pages, cfg, dev), opts.c(cfg, n, dev), _layer_stream(stream, dev)
+        code = self._lib.mc_layer_q4_select(c, b, l, o, keep.c(), q.data_ptr(), pages.data_ptr(), counts.data_ptr(),
+                                            workspace.data_ptr(), workspace.nbytes, at)
+        if code:
+            self._check(code)
+
+    def mc_layer_q4_attn(self, cfg: McConfig, batch: Batch, layer: LayerQ4Cache, opts: ScoreOpts, pages, counts, q, k_new, v_new,
+                         flags: int, out, lse, workspace: torch.Tensor, stream=None):
+        """As mc_layer_attn; pages int32 [batch][n_kv_heads][any], counts int32 [batch]: the pages to attend, or None, None."""
+        dev = q.get_device()
+        c, b, dt = _cfg_c(cfg), batch.layer_c(dev), cfg.torch_dtype
+        n = b.batch
+        rows_q, rows_kv = n * cfg.n_q_heads * 128, n * cfg.n_kv_heads * 128
+        if not (q.dtype is dt and out.dtype is dt and q.numel() == rows_q and out.numel() == rows_q and q.is_contiguous()
+                and out.is_contiguous() and out.get_device() == dev and workspace.get_device() == dev):
+            _refuse(dev, q=(q, dt, rows_q), out=(out, dt, rows_q), workspace=(workspace, workspace.dtype, 0))
+            raise AssertionError("q and out: [batch][n_q_heads][128] are wanted")
+        for t in (k_new, v_new):
+            if t is not None and not (t.dtype is dt and t.numel() == rows_kv and t.is_contiguous() and t.get_device() == dev):
+                _refuse(dev, k_new=(k_new, dt, rows_kv), v_new=(v_new, dt, rows_kv))
+                raise AssertionError("k_new and v_new: [batch][n_kv_heads][128] are wanted")
+        if lse is not None and not (_good(lse, torch.float32, 0, dev) and lse.numel() == n * cfg.n_q_heads):
+            _refuse(dev, lse=(lse, torch.float32, n * cfg.n_q_heads))
+            raise AssertionError("lse: [batch][n_q_heads] is wanted")
+        stride = 0
+        if pages is not None:
+            if not (_good(pages, torch.int32, 0, dev) and pages.dim() == 3 and pages.size(0) == n and pages.size(1) == cfg.n_kv_heads):
+                _refuse(dev, pages=(pages, torch.int32, 0))
+                raise AssertionError("pages: [batch][n_kv_heads][any] is wanted")
+            if not (counts is not None and _good(counts, torch.int32, n, dev)):
+                assert counts is not None, "counts are wanted with pages"
+                _refuse(dev, counts=(counts, torch.int32, n))
+            stride = pages.size(2)
+        l, o, at = layer.c(n, b.n_pages, cfg, dev), opts.c(cfg, n, dev), _layer_stream(stream, dev)
+        code = self._lib.mc_layer_q4_attn(c, b, l, o, None if pages is None else pages.data_ptr(),
+                                          None if counts is None else counts.data_ptr(), stride, q.data_ptr(),
+                                          None if k_new is None else k_new.data_ptr(), None if v_new is None else v_new.data_ptr(), flags,
+                                          out.data_ptr(), None if lse is None else lse.data_ptr(), workspace.data_ptr(), workspace.nbytes, at)
+        if code:
+            self._check(code)
+
+    def mc_layer_q4_read_status(self, layer: LayerQ4Cache, stream=None, check: bool = True):
+        words = (C.c_int32 * MC_STATUS_WORDS)()
+        l = layer.c(0, 0)
+        code = self._lib.mc_layer_q4_read_status(C.byref(l), _stream(stream), words)
         if check:
             self._check(code)
         return list(words), code

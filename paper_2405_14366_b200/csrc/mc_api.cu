@@ -12,6 +12,8 @@
 #include "mc_items.cuh"
 #include "mc_kernels.h"
 #include "mc_layer.h"
+#include "mc_layer_q4.cuh"
+#include "mc_layer_q4.h"
 #include "mc_append.cuh"
 #include "mc_q4.cuh"
 
@@ -705,6 +707,10 @@ mc_status mc_decode_drain_host(const mc_config* cfg, const mc_batch* batch, int3
 static bool too_long(const mc_config* cfg, const mc_batch* batch) {
   return batch->max_seq_len > (1 << 30) || (int64_t)batch->batch * cfg->n_kv_heads * (batch->max_seq_len / 64 + 2) > 0x7fffffffLL;
 }
+// The same for the pages of a layer held in 4 bits.
+static bool too_many_pages(const mc_config* cfg, const mc_batch* batch) {
+  return batch->max_seq_len > (1 << 30) || (int64_t)batch->batch * cfg->n_kv_heads * (batch->max_seq_len / kLqPage + 2) > 0x7fffffffLL;
+}
 // What every mc_layer_* call checks about its configuration, batch and cache.
 static mc_status check_layer(const mc_config* cfg, const mc_batch* batch, const mc_layer_cache* layer) {
   mc_status st = check_config(cfg);
@@ -737,7 +743,17 @@ mc_status mc_layer_workspace_bytes(const mc_config* cfg, const mc_batch* batch, 
   if (batch == nullptr || bytes == nullptr) return MC_ERR_INVALID_ARG;
   if (batch->batch < 0 || batch->max_seq_len < 0) return MC_ERR_INVALID_ARG;
   if (batch->batch > kMaxLayerBatch || too_long(cfg, batch)) return MC_ERR_SHAPE;
+  if ((op == MC_OP_LAYER_Q4_ATTN || op == MC_OP_LAYER_Q4_SELECT) && (cfg->page_size != kLqPage || too_many_pages(cfg, batch))) return MC_ERR_SHAPE;
   switch (op) {
+    case MC_OP_LAYER_Q4_ATTN:
+      if (arg & ~MC_LAYER_APPEND) return MC_ERR_INVALID_ARG;
+      *bytes = layer_q4_attn_workspace_bytes(cfg, batch, arg) + 256;
+      return MC_OK;
+    case MC_OP_LAYER_Q4_SELECT:
+      if (arg != 0) return MC_ERR_INVALID_ARG;
+      if (batch->max_seq_len > kQ4MaxSelectLen) return MC_ERR_SHAPE;
+      *bytes = layer_q4_select_workspace_bytes(cfg, batch) + 256;
+      return MC_OK;
     case MC_OP_LAYER_ATTN:
       if (arg & ~(MC_LAYER_APPEND | MC_LAYER_ACCUMULATE)) return MC_ERR_INVALID_ARG;
       *bytes = layer_attn_workspace_bytes(cfg, batch, arg) + 256;
@@ -814,6 +830,107 @@ mc_status mc_layer_read_status(const mc_layer_cache* layer, void* stream, int32_
                                 (cudaStream_t)stream));
   MC_CUDA_CHECK(cudaStreamSynchronize((cudaStream_t)stream));
   return out_words[MC_STATUS_FLAGS] != 0 ? MC_ERR_DEVICE_STATUS : MC_OK;
+}
+
+// ---- one layer held in 4 bits ------------------------------------------------------------------------
+static mc_status check_layer_q4(const mc_config* cfg, const mc_batch* batch, const mc_layer_q4_cache* layer) {
+  mc_status st = check_config(cfg);
+  if (st != MC_OK) return st;
+  if (cfg->page_size != kLqPage) return MC_ERR_SHAPE;
+  st = check_batch(cfg, batch);
+  if (st != MC_OK) return st;
+  if (batch->batch > kMaxLayerBatch || too_many_pages(cfg, batch)) return MC_ERR_SHAPE;
+  if (batch->batch > 0 && batch->n_pages == 0) return MC_ERR_INVALID_ARG;  // (a bad page id reads page 0: there has to be one)
+  if (!layer || !layer->k_codes || !layer->k_meta || !layer->v_codes || !layer->v_meta || !layer->res_k || !layer->res_v || !layer->status)
+    return MC_ERR_INVALID_ARG;
+  for (const void* x : {(const void*)layer->k_codes, (const void*)layer->k_meta, (const void*)layer->v_codes, (const void*)layer->v_meta,
+                        (const void*)layer->res_k, (const void*)layer->res_v})
+    if (!aligned256(x)) return MC_ERR_ALIGN;
+  return ((uintptr_t)layer->status & 3u) ? MC_ERR_ALIGN : MC_OK;
+}
+
+// The rows of mc_layer_q4_append and mc_layer_q4_read.
+static mc_status check_rows(const mc_config* cfg, const void* k, const void* v, int64_t k_stride, int64_t v_stride,
+                            const int32_t* row_offsets, int32_t n_rows) {
+  if (n_rows < 0 || n_rows >= (1 << 30) || !row_offsets || (n_rows > 0 && (!k || !v))) return MC_ERR_INVALID_ARG;
+  const int64_t width = (int64_t)cfg->n_kv_heads * kHeadDim;
+  if (k_stride < width || v_stride < width || k_stride > (INT64_C(1) << 31) || v_stride > (INT64_C(1) << 31)) return MC_ERR_SHAPE;
+  if ((((uintptr_t)k | (uintptr_t)v) & 15u) || ((k_stride | v_stride) & 7) || ((uintptr_t)row_offsets & 3u)) return MC_ERR_ALIGN;
+  return MC_OK;
+}
+
+mc_status mc_layer_q4_append(const mc_config* cfg, const mc_batch* batch, const mc_layer_q4_cache* layer, const void* k,
+                             const void* v, int64_t k_stride, int64_t v_stride, const int32_t* row_offsets, int32_t n_rows,
+                             void* stream) {
+  ApiRange range_("mc_layer_q4_append");
+  mc_status st = check_layer_q4(cfg, batch, layer);
+  if (st != MC_OK) return st;
+  st = check_rows(cfg, k, v, k_stride, v_stride, row_offsets, n_rows);
+  if (st != MC_OK || n_rows == 0 || batch->batch == 0) return st;
+  const Q4RowArgs rows = {nullptr, row_offsets, n_rows, k_stride, v_stride};
+  return launch_layer_q4_append(cfg, batch, make_geom(cfg, batch), layer, k, v, rows, (cudaStream_t)stream);
+}
+
+mc_status mc_layer_q4_read(const mc_config* cfg, const mc_batch* batch, const mc_layer_q4_cache* layer, const int32_t* begin, void* k,
+                           void* v, int64_t k_stride, int64_t v_stride, const int32_t* row_offsets, int32_t n_rows, void* stream) {
+  ApiRange range_("mc_layer_q4_read");
+  mc_status st = check_layer_q4(cfg, batch, layer);
+  if (st != MC_OK) return st;
+  st = check_rows(cfg, k, v, k_stride, v_stride, row_offsets, n_rows);
+  if (st != MC_OK) return st;
+  if ((uintptr_t)begin & 3u) return MC_ERR_ALIGN;
+  if (n_rows == 0 || batch->batch == 0) return MC_OK;
+  const Q4RowArgs rows = {begin, row_offsets, n_rows, k_stride, v_stride};
+  return launch_layer_q4_read(cfg, batch, make_geom(cfg, batch), layer, k, v, rows, (cudaStream_t)stream);
+}
+
+mc_status mc_layer_q4_select(const mc_config* cfg, const mc_batch* batch, const mc_layer_q4_cache* layer, const mc_score_opts* opts,
+                             const mc_page_selection* keep, const void* q, int32_t* pages, int32_t* counts, void* workspace,
+                             size_t workspace_bytes, void* stream) {
+  ApiRange range_("mc_layer_q4_select");
+  mc_status st = check_layer_q4(cfg, batch, layer);
+  if (st != MC_OK) return st;
+  st = check_score_opts(opts);
+  if (st != MC_OK) return st;
+  if (opts->alibi_slopes != nullptr || !(opts->sm_scale > 0.f)) return MC_ERR_UNSUPPORTED;
+  if (batch->max_seq_len > kQ4MaxSelectLen) return MC_ERR_SHAPE;
+  if (!keep || !q || !pages || !counts) return MC_ERR_INVALID_ARG;
+  if (keep->budget < 1 || keep->n_sink < 0 || keep->n_recent < 0 || (int64_t)keep->n_sink + keep->n_recent > keep->budget)
+    return MC_ERR_INVALID_ARG;
+  if (((uintptr_t)q & 15u) || (((uintptr_t)pages | (uintptr_t)counts) & 3u)) return MC_ERR_ALIGN;
+  // every CTA reads its sequence's length and position, one of them writes the count
+  for (const int32_t* in : {batch->seq_lens, opts->q_pos, opts->doc_start, opts->prefix_len})
+    if (in != nullptr && counts < in + batch->batch && in < counts + batch->batch) return MC_ERR_INVALID_ARG;
+  if (workspace == nullptr || !aligned256(workspace)) return workspace ? MC_ERR_ALIGN : MC_ERR_INVALID_ARG;
+  if (workspace_bytes < layer_q4_select_workspace_bytes(cfg, batch)) return MC_ERR_CAPACITY;
+  return launch_layer_q4_select(cfg, batch, make_geom(cfg, batch), layer, opts, keep, q, pages, counts, workspace, (cudaStream_t)stream);
+}
+
+mc_status mc_layer_q4_attn(const mc_config* cfg, const mc_batch* batch, const mc_layer_q4_cache* layer, const mc_score_opts* opts,
+                           const int32_t* pages, const int32_t* counts, int32_t pages_stride, const void* q, const void* k_new,
+                           const void* v_new, int32_t flags, void* out, float* lse, void* workspace, size_t workspace_bytes,
+                           void* stream) {
+  ApiRange range_("mc_layer_q4_attn");
+  mc_status st = check_layer_q4(cfg, batch, layer);
+  if (st != MC_OK) return st;
+  st = check_score_opts(opts);
+  if (st != MC_OK) return st;
+  if (!q || !out || (k_new == nullptr) != (v_new == nullptr)) return MC_ERR_INVALID_ARG;
+  if ((pages == nullptr) != (counts == nullptr) || (pages == nullptr ? pages_stride != 0 : pages_stride < 1)) return MC_ERR_INVALID_ARG;
+  if (flags & ~MC_LAYER_APPEND) return MC_ERR_INVALID_ARG;
+  if ((flags & MC_LAYER_APPEND) && !k_new) return MC_ERR_INVALID_ARG;
+  if (((uintptr_t)q | (uintptr_t)out | (uintptr_t)k_new | (uintptr_t)v_new) & 15u) return MC_ERR_ALIGN;
+  if (((uintptr_t)lse | (uintptr_t)pages | (uintptr_t)counts) & 3u) return MC_ERR_ALIGN;
+  if (workspace == nullptr || !aligned256(workspace)) return workspace ? MC_ERR_ALIGN : MC_ERR_INVALID_ARG;
+  if (workspace_bytes < layer_q4_attn_workspace_bytes(cfg, batch, flags)) return MC_ERR_CAPACITY;
+  return launch_layer_q4_attn(cfg, batch, make_geom(cfg, batch), layer, opts, pages, counts, pages_stride, q, k_new, v_new, flags, out, lse,
+                              workspace, (cudaStream_t)stream);
+}
+
+mc_status mc_layer_q4_read_status(const mc_layer_q4_cache* layer, void* stream, int32_t* out_words) {
+  if (layer == nullptr) return MC_ERR_INVALID_ARG;
+  const mc_layer_cache words = {nullptr, nullptr, nullptr, nullptr, layer->status};
+  return mc_layer_read_status(&words, stream, out_words);
 }
 
 mc_status mc_selftest_wait_timeout(const mc_pair_cache* pair, int32_t poll_limit, void* stream) {

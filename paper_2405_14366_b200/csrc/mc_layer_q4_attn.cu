@@ -1,0 +1,908 @@
+// Single-query decode attention over one layer held in 4 bits (keys per channel over a page of 32 tokens, values per token
+// over 32 channels), the layers below MiniCache's start layer when the model's caches are 4-bit.
+//
+//   s_i   = sum_c (q_c scale_c) code_ic + sum_c q_c zero_c        (page by page: scale and zero belong to a page's channel)
+//   out_c = sum_i (p_i scale_ig) code_ic + sum_i p_i zero_ig      (g: the channel's group of 32)
+//
+// The group parameters move to the operand with few rows: a page's 4096 codes of K and of V meet the tensor cores as they
+// are, 128 products q scale and 128 products p scale are formed in their place.  A four-bit integer needs no conversion:
+// masked out of a word, the bits 0..3 of a half-word are the binary16 number code * 2^-24 and the bits 4..7 code * 2^-20
+// (subnormal numbers and the lowest binade share their unit), which the tensor cores multiply exactly; the powers of two
+// are taken out of the fp32 sums.  Five logic operations per eight codes are all that is done to them.
+//   q scale (22 bits) is carried as two binary16 numbers, its rounding and the rest, in neighbouring columns of the B operand
+// that one kv head's few query heads leave idle (eight query heads: two passes), so scores are as exact as fp32 sums make them.
+// p is kept below 2^e, p scale below 2^15, e chosen from the page's scales and lowered like a running maximum that rises.
+//
+// Work: the complete pages that are seen (or selected), split equally over teams of warps, a warp per kv head in each (neighbouring
+// warps stream neighbouring tiles of a page).  A warp is a pipeline of its own with a ring of stages of one tile (5 KB: codes and
+// parameters of K and V), two copied with the tensor map's swizzle so that ldmatrix and 16-byte loads meet no bank conflicts.
+// One more warp per CTA attends the 16-bit rows of the begun pages and the step's new rows, and appends them.  Partial results
+// are joined by a second kernel.
+#include <algorithm>
+
+#include "mc_kernels.h"
+#include "mc_layer.h"
+#include "mc_layer_q4.cuh"
+#include "mc_layer_q4.h"
+#include "mc_mma.cuh"
+#include "mc_pipe.cuh"
+#include "mc_tc.cuh"
+
+namespace mc {
+
+constexpr int kLqWarps = 7;  // that stream pages
+constexpr int kLqThreads = (kLqWarps + 1) * 32;
+constexpr int kLqCtasPerSm = 2;
+constexpr int kLqStages = 3;
+constexpr int kLqStageBytes = 2 * (kLqCodeBytes + kLqMetaBytes);
+constexpr int kLqVCodes = kLqCodeBytes, kLqKMeta = 2 * kLqCodeBytes, kLqVMeta = kLqKMeta + kLqMetaBytes;  // within a stage
+static_assert(kLqStageBytes % 1024 == 0, "the swizzle patterns repeat within 1 KB");
+
+struct LayerQ4Params {
+  Geom g;
+  ScoreRule rule;
+  const unsigned char* k_codes;
+  const unsigned char* v_meta;
+  unsigned char* pool[4];  // k_codes, k_meta, v_codes, v_meta (append)
+  char* res_k;
+  char* res_v;
+  int32_t* status;
+  const char* q;
+  const char* k_new;
+  const char* v_new;
+  const int32_t* sel;     // selected pages or null
+  const int32_t* counts;
+  int sel_stride;
+  float* part_o;   // [team + sequence][n_q_heads][128], then [sequence][n_q_heads][128] of the 16-bit rows
+  float* part_ml;  // [...][2]
+  int res_part;    // first row of the latter
+  int nq, n_q_heads;
+  int members, n_teams;  // warps of a team, teams
+  int flags;
+  unsigned short* out;
+  float* lse;
+};
+
+// What every CTA keeps of a sequence.
+struct Q4Seq {
+  int n, q_pos, a, lo, hi, ua, ub0;
+};
+__device__ __forceinline__ int q4_units(const LayerQ4Params& p, int b, PageView& v, int& bad) {
+  const int raw = __ldcg(p.g.seq_lens + b);
+  bad |= (raw < 0 || raw > p.g.max_seq_len) ? 1 : 0;
+  const int n = min(max(raw, 0), p.g.max_seq_len), n_tot = n + (p.k_new != nullptr ? 1 : 0);
+  v = page_view(p.rule, b, n, n_tot, n_tot - 1);
+  if (p.sel == nullptr) return v.u;
+  const int c = __ldcg(p.counts + b);
+  bad |= (c < 0 || c > p.sel_stride || c > n / kLqPage) ? 1 : 0;
+  return min(max(c, 0), min(p.sel_stride, n / kLqPage));
+}
+__device__ __forceinline__ int q4_live_teams(const LayerQ4Params& p, int units) { return min(p.n_teams, max(units, 1)); }
+
+// One tile as a lane of the window knows it.
+struct Tile {
+  int meta;  // flags | sequence << 5 | kv head << 14
+  int t0;    // first token
+  int page;  // raw page id
+};
+enum { kTlLoad = 1, kTlFirst = 2, kTlLast = 4, kTlBad = 8 };
+
+__device__ __forceinline__ uint32_t transpose_8x8(uint32_t v) {
+  uint32_t r;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+  return r;
+}
+__device__ __forceinline__ uint4 lds16(uint32_t a) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
+  return v;
+}
+__device__ __forceinline__ uint32_t lds4(uint32_t a) {
+  uint32_t v;
+  asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
+  return v;
+}
+__device__ __forceinline__ uint32_t h2_mul(uint32_t a, uint32_t b) {
+  const __half2 r = __hmul2(*reinterpret_cast<__half2*>(&a), *reinterpret_cast<__half2*>(&b));
+  return *reinterpret_cast<const uint32_t*>(&r);
+}
+// a b - c
+__device__ __forceinline__ uint32_t h2_fms(uint32_t a, uint32_t b, uint32_t c) {
+  const __half2 r = __hfma2(*reinterpret_cast<__half2*>(&a), *reinterpret_cast<__half2*>(&b), __hneg2(*reinterpret_cast<__half2*>(&c)));
+  return *reinterpret_cast<const uint32_t*>(&r);
+}
+__device__ __forceinline__ uint32_t h2_max(uint32_t a, uint32_t b) {
+  const __half2 r = __hmax2(*reinterpret_cast<__half2*>(&a), *reinterpret_cast<__half2*>(&b));
+  return *reinterpret_cast<const uint32_t*>(&r);
+}
+__device__ __forceinline__ uint32_t lows(uint32_t a, uint32_t b) { return __byte_perm(a, b, 0x5410); }
+__device__ __forceinline__ uint32_t highs(uint32_t a, uint32_t b) { return __byte_perm(a, b, 0x7632); }
+
+// The 16-bit rows of one (sequence, kv head), by a warp: the begun page's and the step's new one, up to 32 tokens, straight
+// from global memory.  The k axis of the first product is the channels in the order in which a lane's 16-byte loads bring
+// them; in the second a lane's rows and channels are the ones the codes' kernel uses, so that outputs leave alike.
+template <int DT>
+__device__ __noinline__ void q4_begun_page(const LayerQ4Params& p, int b, int head) {
+  const int lane = threadIdx.x & 31, row = lane >> 2, t4 = lane & 3, colp = 2 * t4;
+  const int nq = p.nq, H = p.g.n_kv_heads;
+  int bad = 0;
+  PageView v;
+  q4_units(p, b, v, bad);
+  const int n = v.n, base = n / kLqPage * kLqPage, n_tot = n + (p.k_new != nullptr ? 1 : 0);
+  const size_t at = ((size_t)b * H + head) * kLqResBytes, new_at = ((size_t)b * H + head) * kRowBytes;
+  const size_t prow = (size_t)p.res_part + (size_t)b * p.n_q_heads + head * nq;
+  uint32_t seen = 0;  // bit r: token base + r is attended
+  {
+    const int t = base + lane;
+    seen = __ballot_sync(0xffffffffu, t < n_tot && v.sees(t));
+  }
+  float acc[8][4];
+#pragma unroll
+  for (int j = 0; j < 8; ++j)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) acc[j][k] = 0.f;
+  float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;
+  if (seen != 0) {
+    auto row_ptr = [&](bool keys, int r) {
+      return base + r == n ? (keys ? p.k_new : p.v_new) + new_at : (keys ? p.res_k : p.res_v) + at + (size_t)r * kRowBytes;
+    };
+    uint4 qf[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      qf[j] = make_uint4(0u, 0u, 0u, 0u);
+      if (row < nq) qf[j] = *reinterpret_cast<const uint4*>(p.q + ((size_t)b * p.n_q_heads + head * nq + row) * kRowBytes + 64 * t4 + 16 * j);
+    }
+    float sc[2][4];
+    uint2 vr[2][4][4];  // [16 tokens][token 2 t4, + 1, + 8, + 9][channel group]
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const bool any = ((seen >> (16 * h)) & 0xffffu) != 0;
+      uint4 ka[2][4];
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int r = 16 * h + 8 * e + row;
+        const char* src = row_ptr(true, r) + 64 * t4;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          ka[e][j] = make_uint4(0u, 0u, 0u, 0u);
+          if (any && ((seen >> r) & 1u)) ka[e][j] = *reinterpret_cast<const uint4*>(src + 16 * j);
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int r = 16 * h + (e >> 1) * 8 + colp + (e & 1);
+        const char* src = row_ptr(false, r) + 8 * row;
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          vr[h][e][g] = make_uint2(0u, 0u);
+          if (any && ((seen >> r) & 1u)) vr[h][e][g] = *reinterpret_cast<const uint2*>(src + 64 * g);
+        }
+      }
+      float d[2][4] = {};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        mma_rows<DT>(d[0], ka[0][j].x, ka[1][j].x, ka[0][j].y, ka[1][j].y, qf[j].x, qf[j].y);
+        mma_rows<DT>(d[1], ka[0][j].z, ka[1][j].z, ka[0][j].w, ka[1][j].w, qf[j].z, qf[j].w);
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) sc[h][k] = d[0][k] + d[1][k];
+      const int p0 = base + 16 * h + row, p8 = p0 + 8;
+      const bool v0 = (seen >> (16 * h + row)) & 1u, v8 = (seen >> (16 * h + row + 8)) & 1u;
+      scores_of(p.rule, sc[h]);  // (what is not seen came as zeros)
+      if (p.rule.slopes) {
+        const float e0 = (float)(v.q_pos - p0), e8 = (float)(v.q_pos - p8);
+        const float sl0 = colp < nq ? p.rule.slopes[head * nq + colp] * kLog2e : 0.f;
+        const float sl1 = colp + 1 < nq ? p.rule.slopes[head * nq + colp + 1] * kLog2e : 0.f;
+        sc[h][0] = fmaf(-sl0, e0, sc[h][0]);
+        sc[h][1] = fmaf(-sl1, e0, sc[h][1]);
+        sc[h][2] = fmaf(-sl0, e8, sc[h][2]);
+        sc[h][3] = fmaf(-sl1, e8, sc[h][3]);
+      }
+      if (!v0) sc[h][0] = sc[h][1] = -INFINITY;
+      if (!v8) sc[h][2] = sc[h][3] = -INFINITY;
+      m0 = fmaxf(m0, fmaxf(sc[h][0], sc[h][2]));
+      m1 = fmaxf(m1, fmaxf(sc[h][1], sc[h][3]));
+    }
+#pragma unroll
+    for (int o = 4; o < 32; o <<= 1) {
+      m0 = fmaxf(m0, __shfl_xor_sync(0xffffffffu, m0, o));
+      m1 = fmaxf(m1, __shfl_xor_sync(0xffffffffu, m1, o));
+    }
+    const float b0 = m0 == -INFINITY ? 0.f : m0, b1 = m1 == -INFINITY ? 0.f : m1;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const float e0 = ex2(sc[h][0] - b0), e1 = ex2(sc[h][1] - b1), e2 = ex2(sc[h][2] - b0), e3 = ex2(sc[h][3] - b1);
+      l0 += e0 + e2;
+      l1 += e1 + e3;
+      const uint32_t pb0 = transpose_8x8(Elem<DT>::pack(e0, e1)), pb1 = transpose_8x8(Elem<DT>::pack(e2, e3));
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        mma_rows<DT>(acc[2 * g], lows(vr[h][0][g].x, vr[h][1][g].x), highs(vr[h][0][g].x, vr[h][1][g].x), lows(vr[h][2][g].x, vr[h][3][g].x),
+                     highs(vr[h][2][g].x, vr[h][3][g].x), pb0, pb1);
+        mma_rows<DT>(acc[2 * g + 1], lows(vr[h][0][g].y, vr[h][1][g].y), highs(vr[h][0][g].y, vr[h][1][g].y),
+                     lows(vr[h][2][g].y, vr[h][3][g].y), highs(vr[h][2][g].y, vr[h][3][g].y), pb0, pb1);
+      }
+    }
+#pragma unroll
+    for (int o = 4; o < 32; o <<= 1) {
+      l0 += __shfl_xor_sync(0xffffffffu, l0, o);
+      l1 += __shfl_xor_sync(0xffffffffu, l1, o);
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    const int r = colp + e;
+    if (r >= nq) continue;
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+      *reinterpret_cast<float4*>(p.part_o + (prow + r) * kHeadDim + 32 * g + 4 * row) =
+          make_float4(acc[2 * g][e], acc[2 * g][2 + e], acc[2 * g + 1][e], acc[2 * g + 1][2 + e]);
+    if (row == 0) *reinterpret_cast<float2*>(p.part_ml + 2 * (prow + r)) = make_float2(e ? m1 : m0, e ? l1 : l0);
+  }
+  if (p.flags & MC_LAYER_APPEND) {
+    const int slot = n & (kLqPage - 1);
+    const uint2 kr = *reinterpret_cast<const uint2*>(p.k_new + new_at + 8 * lane), vw = *reinterpret_cast<const uint2*>(p.v_new + new_at + 8 * lane);
+    if (slot == kLqPage - 1) {  // the row completes a page
+      const int page = checked_page(p.g, b, n / kLqPage, p.status);
+#pragma unroll 1
+      for (int tensor = 0; tensor < 2; ++tensor) {
+        if (page < 0) break;
+        const char* src = (tensor == 0 ? p.res_k : p.res_v) + at + 8 * lane;
+        uint2 r[kLqPage];
+#pragma unroll
+        for (int t = 0; t < kLqPage - 1; ++t) r[t] = *reinterpret_cast<const uint2*>(src + t * kRowBytes);
+        r[kLqPage - 1] = tensor == 0 ? kr : vw;
+        const size_t tile = (size_t)page * H + head;
+        lq_quantise<DT>(tensor == 0, r, p.pool[2 * tensor] + tile * kLqCodeBytes, p.pool[2 * tensor + 1] + tile * kLqMetaBytes);
+      }
+    }
+    *reinterpret_cast<uint2*>(p.res_k + at + slot * kRowBytes + 8 * lane) = kr;
+    *reinterpret_cast<uint2*>(p.res_v + at + slot * kRowBytes + 8 * lane) = vw;
+  }
+}
+
+// WIDE: eight query heads per kv head, a column of B each; else up to four, two columns each.
+template <int DT, bool WIDE>
+__global__ void __launch_bounds__(kLqThreads, kLqCtasPerSm)
+layer_q4_split_kernel(const __grid_constant__ LayerQ4Params p, const __grid_constant__ CUtensorMap map_km,
+                      const __grid_constant__ CUtensorMap map_vc) {
+  grid_dep_launch();
+  extern __shared__ unsigned char smem_raw[];
+  unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + kLqWarps * kLqStages * kLqStageBytes);
+  Q4Seq* seq_s = reinterpret_cast<Q4Seq*>(bars + kLqWarps * kLqStages);
+  int* pre_s = reinterpret_cast<int*>(seq_s + p.g.batch);
+  volatile int* s_abort = pre_s + p.g.batch + 1;
+
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int row = lane >> 2, t4 = lane & 3;
+  const int H = p.g.n_kv_heads, nq = p.nq;
+
+  if (tid == 32) {
+    prefetch_map(&map_km);
+    prefetch_map(&map_vc);
+  }
+  if (tid == 0) {
+    for (int s = 0; s < kLqWarps * kLqStages; ++s) mbar_init(smem_u32(bars + s), 1);
+    *s_abort = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  // (lengths, block table and score options are the caller's: read before the wait; a selection is what the kernel ahead wrote)
+  if (p.sel != nullptr) grid_dep_wait();
+  int bad = 0;
+  for (int b = tid; b < p.g.batch; b += kLqThreads) {
+    PageView v;
+    pre_s[b + 1] = q4_units(p, b, v, bad);
+    seq_s[b] = Q4Seq{v.n, v.q_pos, v.a, v.lo, v.hi, v.ua, v.ub0};
+  }
+  scan_counts(pre_s, p.g.batch);
+
+  if (warp == kLqWarps) {
+    grid_dep_wait();
+    if (bad && blockIdx.x == 0) atomicOr(p.status, MC_FLAG_BAD_METADATA);
+    for (int i = blockIdx.x; i < p.g.batch * H; i += gridDim.x) q4_begun_page<DT>(p, i / H, i % H);
+    return;
+  }
+
+  const int n_units = pre_s[p.g.batch];
+  const int teams = q4_live_teams(p, n_units);
+  const int gw = blockIdx.x * kLqWarps + warp;
+  const int team = gw / p.members, member = gw - team * p.members;
+  int x_begin = 0, x_end = 0;
+  if (team < teams) {
+    x_begin = (int)((long long)n_units * team / teams);
+    x_end = (int)((long long)n_units * (team + 1) / teams);
+  }
+  const int nx = x_end - x_begin;
+  const int n_heads = (H - member + p.members - 1) / p.members;
+  const int n_tiles = nx * n_heads;
+
+  auto load_tile = [&](int i) {  // tile i of this warp: head by head, page by page
+    Tile s;
+    s.meta = s.t0 = s.page = 0;
+    if (i >= n_tiles) return s;
+    const int hd = n_heads == 1 ? 0 : i / nx, rem = i - hd * nx;
+    const int head = member + hd * p.members;
+    const int x = x_begin + rem;
+    const int b = seq_of_item(pre_s, p.g.batch, x);
+    const int k = x - pre_s[b], n_k = pre_s[b + 1] - pre_s[b];
+    const Q4Seq& q = seq_s[b];
+    int fl = 0, slot;
+    if (p.sel == nullptr) {
+      slot = k < q.ua ? k : q.ub0 + k - q.ua;
+      fl |= kTlLoad;
+    } else {
+      const int32_t* list = p.sel + ((size_t)b * H + head) * p.sel_stride;
+      slot = __ldcg(list + k);
+      const int before = k > 0 ? __ldcg(list + k - 1) : -1;
+      if (slot > before && (unsigned)slot < (unsigned)(q.n / kLqPage)) {
+        const int t0 = slot * kLqPage;
+        if (t0 < q.a || (t0 + kLqPage > q.lo && t0 < q.hi)) fl |= kTlLoad;
+      } else {
+        fl |= kTlBad;
+        slot = 0;
+      }
+    }
+    s.t0 = slot * kLqPage;
+    if (fl & kTlLoad) {
+      if (slot < p.g.max_pages_per_seq) s.page = p.g.block_table[(size_t)b * p.g.max_pages_per_seq + slot];
+      else s.page = -1;
+    }
+    if (rem == 0 || k == 0) fl |= kTlFirst;
+    if (rem + 1 == nx || k + 1 == n_k) fl |= kTlLast;
+    s.meta = fl | b << 5 | head << 14;
+    return s;
+  };
+  // the pools' tile, -1 if nothing is to be copied; a page id outside the pools reads page 0 and is flagged
+  auto tile_of = [&](const Tile& s) {
+    if (s.meta & kTlBad) atomicOr(p.status, MC_FLAG_BAD_METADATA);
+    if (!(s.meta & kTlLoad)) return -1;
+    int page = s.page;
+    if (!page_ok(p.g, page)) {
+      atomicOr(p.status, MC_FLAG_BAD_METADATA);
+      page = 0;
+    }
+    return page * H + (s.meta >> 14);
+  };
+  Tile win = load_tile(lane), nxt = load_tile(32 + lane);
+  if (p.sel == nullptr) grid_dep_wait();
+  if (bad && blockIdx.x == 0) atomicOr(p.status, MC_FLAG_BAD_METADATA);  // (every thread has looked at other sequences)
+
+  const uint32_t bar0 = smem_u32(bars + warp * kLqStages);
+  const uint32_t st0 = smem_u32(smem) + warp * kLqStages * kLqStageBytes;
+  int win_tile = tile_of(win), nxt_tile = -1;
+  auto issue = [&](int i, int s) {  // tile i into stage s
+    if (i >= n_tiles) return;
+    const int y = __shfl_sync(0xffffffffu, i >= 32 && (i & 31) < kLqStages - 1 ? nxt_tile : win_tile, i & 31);
+    if (y < 0 || *s_abort) return;
+    if (lane == 0) {
+      const uint32_t bar = bar0 + 8 * s, dst = st0 + s * kLqStageBytes;
+      mbar_expect_tx(bar, (uint32_t)kLqStageBytes);
+      bulk_load(dst, p.k_codes + (size_t)y * kLqCodeBytes, kLqCodeBytes, bar);
+      tma_load_2d(dst + kLqKMeta, &map_km, 0, y * 4, bar);
+      tma_load_2d(dst + kLqVCodes, &map_vc, 0, y * kLqPage, bar);
+      bulk_load(dst + kLqVMeta, p.v_meta + (size_t)y * kLqMetaBytes, kLqMetaBytes, bar);
+    }
+  };
+  for (int i = 0; i < kLqStages - 1; ++i) issue(i, i);
+
+  // Query pairs (channels 8w + i, 8w + i + 4 of the lane's 32), as binary16 with the row's power of two taken out: the row's
+  // largest number becomes 2 to 4.
+  uint32_t qh[16];
+  float q_back = 0.f;  // of the lane's column(s): WIDE: column 2 t4 ...
+  float q_back1 = 0.f; // ... and 2 t4 + 1
+  auto load_q = [&](int b, int head) {
+    const int h = WIDE ? row : row >> 1;
+    uint4 w[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      w[j] = make_uint4(0u, 0u, 0u, 0u);
+      if (h < nq) w[j] = *reinterpret_cast<const uint4*>(p.q + ((size_t)b * p.n_q_heads + head * nq + h) * kRowBytes + 64 * t4 + 16 * j);
+    }
+    float big = 0.f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t x[4] = {w[j].x, w[j].y, w[j].z, w[j].w};
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float2 f = Elem<DT>::unpack(x[k]);
+        big = fmaxf(big, fmaxf(fabsf(f.x), fabsf(f.y)));
+      }
+    }
+    big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 1));
+    big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 2));
+    const int e = min(max(__float_as_int(big) >> 23, 2), 253);
+    const float f = __int_as_float((255 - e) << 23), back = __int_as_float((e - 1) << 23);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t x[4] = {w[j].x, w[j].y, w[j].z, w[j].w};
+      uint32_t h2[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float2 v = Elem<DT>::unpack(x[k]);
+        h2[k] = Elem<MC_F16>::pack(v.x * f, v.y * f);
+      }
+      qh[4 * j] = lows(h2[0], h2[2]);
+      qh[4 * j + 1] = highs(h2[0], h2[2]);
+      qh[4 * j + 2] = lows(h2[1], h2[3]);
+      qh[4 * j + 3] = highs(h2[1], h2[3]);
+    }
+    // the lane's result columns are 2 t4 and 2 t4 + 1: rows 8 t4 .. of the lanes that hold those query rows
+    q_back = __shfl_sync(0xffffffffu, back, 8 * t4);
+    if (WIDE) q_back1 = __shfl_sync(0xffffffffu, back, 8 * t4 + 4);
+  };
+  {
+    const int meta = __shfl_sync(0xffffffffu, win.meta, 0);
+    if (n_tiles > 0) load_q((meta >> 5) & 511, meta >> 14);
+  }
+  const uint32_t rest_mask = WIDE ? 0u : (row & 1) ? 0xffffffffu : 0u;  // this lane's column carries what the rounding left
+
+  float acc[8][4], zacc[4];
+  float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;  // of query head t4, or (WIDE) 2 t4 and 2 t4 + 1
+  float sl0 = 0.f, sl1 = 0.f;
+  int ve = 0;              // probabilities are kept times 2^ve
+  float scale_top = -1.f;  // the scale from which they no longer may be
+  Q4Seq sq = {};
+  uint32_t phase = 0;
+  int s = 0, s_next = kLqStages - 1;  // stage of this tile, and of the one to be copied
+
+  for (int i = 0; i < n_tiles; ++i) {
+    const int src = i & 31;
+    if (src == 0 && i > 0) {
+      win = nxt;
+      win_tile = nxt_tile;
+      nxt = load_tile((i & ~31) + 32 + lane);
+    }
+    if (src == 32 - kLqStages) nxt_tile = tile_of(nxt);
+    __syncwarp();  // (the stage of the tile before this one has been read)
+    issue(i + kLqStages - 1, s_next);
+    const int fl = __shfl_sync(0xffffffffu, win.meta, src);
+    const int b = (fl >> 5) & 511, head = fl >> 14;
+    const int t0 = __shfl_sync(0xffffffffu, win.t0, src);
+    if (fl & kTlFirst) {
+      m0 = m1 = -INFINITY;
+      l0 = l1 = 0.f;
+      scale_top = -1.f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) acc[j][k] = 0.f;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) zacc[k] = 0.f;
+      sq = seq_s[b];
+      const uint32_t later = __ballot_sync(0xffffffffu, (win.meta & kTlFirst) != 0) & ~((2u << src) - 1u);
+      if (later) {  // the next piece's queries go to L1 meanwhile
+        const int mn = __shfl_sync(0xffffffffu, win.meta, __ffs(later) - 1);
+        if (lane < 2 * nq)
+          asm volatile("prefetch.global.L1 [%0];" ::"l"(p.q + (((size_t)((mn >> 5) & 511) * p.n_q_heads + (mn >> 14) * nq) * kRowBytes) + lane * 128));
+      }
+      if (p.rule.slopes) {
+        const int h = WIDE ? 2 * t4 : t4;
+        sl0 = h < nq ? p.rule.slopes[head * nq + h] * kLog2e : 0.f;
+        if (WIDE) sl1 = p.rule.slopes[head * nq + h + 1] * kLog2e;
+      }
+    }
+    if (fl & kTlLoad) {
+      const uint32_t sb = st0 + s * kLqStageBytes;
+      mbar_wait(bar0 + 8 * s, (phase >> s) & 1, s_abort, p.status);  // (on a time-out the CTA only runs to its end)
+      phase ^= 1u << s;
+      // ---- scores of 32 tokens: two tiles of 16
+      float dl[2][4] = {}, dh[2][4] = {}, dz[4] = {};  // low and high nibbles' sums, the zeros' (alike in every row)
+      {
+        uint4 x[2][2];  // [tile][token row, row + 8]: 32 channels
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) x[j][e] = lds16(sb + (16 * j + 8 * e + row) * 64 + 16 * t4);
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          const uint4 ma = lds16(sb + kLqKMeta + 128 * t4 + (((2 * w) ^ t4) << 4));
+          const uint4 mb = lds16(sb + kLqKMeta + 128 * t4 + (((2 * w + 1) ^ t4) << 4));
+          const uint32_t s4[4] = {lows(ma.x, mb.x), lows(ma.y, mb.y), lows(ma.z, mb.z), lows(ma.w, mb.w)};
+          const uint32_t z4[4] = {highs(ma.x, mb.x), highs(ma.y, mb.y), highs(ma.z, mb.z), highs(ma.w, mb.w)};
+          uint32_t bq[4], br[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const uint32_t r = h2_mul(qh[4 * w + k], s4[k]);
+            if (WIDE) {
+              bq[k] = r;
+              br[k] = h2_fms(qh[4 * w + k], s4[k], r);
+            } else {
+              bq[k] = h2_fms(qh[4 * w + k], s4[k], r & rest_mask);
+            }
+          }
+          mma_rows<MC_F16>(dz, z4[0], z4[0], z4[1], z4[1], qh[4 * w], qh[4 * w + 1]);
+          mma_rows<MC_F16>(dz, z4[2], z4[2], z4[3], z4[3], qh[4 * w + 2], qh[4 * w + 3]);
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const uint32_t c0 = w == 0 ? x[j][0].x : w == 1 ? x[j][0].y : w == 2 ? x[j][0].z : x[j][0].w;
+            const uint32_t c8 = w == 0 ? x[j][1].x : w == 1 ? x[j][1].y : w == 2 ? x[j][1].z : x[j][1].w;
+            const uint32_t u0 = c0 >> 8, u8 = c8 >> 8;
+            const uint32_t a0 = c0 & 0x000f000fu, a1 = c8 & 0x000f000fu, a2 = u0 & 0x000f000fu, a3 = u8 & 0x000f000fu;
+            const uint32_t h0 = c0 & 0x00f000f0u, h1 = c8 & 0x00f000f0u, h2 = u0 & 0x00f000f0u, h3 = u8 & 0x00f000f0u;
+            mma_rows<MC_F16>(dl[j], a0, a1, a2, a3, bq[0], bq[2]);
+            mma_rows<MC_F16>(dh[j], h0, h1, h2, h3, bq[1], bq[3]);
+            if (WIDE) {
+              mma_rows<MC_F16>(dl[j], a0, a1, a2, a3, br[0], br[2]);
+              mma_rows<MC_F16>(dh[j], h0, h1, h2, h3, br[1], br[3]);
+            }
+          }
+        }
+      }
+      // tokens t0 + 16 j + row and + 8; not WIDE: sc[2 j + e] of query head t4; WIDE: sa of head 2 t4, sc of 2 t4 + 1
+      float sc[4], sa[4];
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          if (WIDE) {
+            sa[2 * j + e] = fmaf(dl[j][2 * e], 0x1p24f, fmaf(dh[j][2 * e], 0x1p20f, dz[0])) * q_back;
+            sc[2 * j + e] = fmaf(dl[j][2 * e + 1], 0x1p24f, fmaf(dh[j][2 * e + 1], 0x1p20f, dz[1])) * q_back1;
+          } else {
+            sc[2 * j + e] = fmaf(dl[j][2 * e] + dl[j][2 * e + 1], 0x1p24f, fmaf(dh[j][2 * e] + dh[j][2 * e + 1], 0x1p20f, dz[0])) * q_back;
+          }
+        }
+      // ---- masks, the scores' form, the distance bias
+      uint32_t hidden = 0;  // bit r: token t0 + r is not seen
+      const bool whole = t0 + kLqPage <= sq.a || (t0 >= sq.lo && t0 + kLqPage <= sq.hi);
+      bool ok[4] = {true, true, true, true};
+      if (!whole) {
+        const int t = t0 + lane;
+        hidden = ~__ballot_sync(0xffffffffu, t < sq.a || (t >= sq.lo && t < sq.hi));
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          ok[k] = !((hidden >> (8 * k + row)) & 1u);
+          if (!ok[k]) sc[k] = 0.f;  // (no say in which form of the cap the others take)
+          if (WIDE && !ok[k]) sa[k] = 0.f;
+        }
+      }
+      scores_of(p.rule, sc);
+      if (WIDE) scores_of(p.rule, sa);
+      if (p.rule.slopes) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const float dist = (float)(sq.q_pos - (t0 + 8 * k + row));
+          sc[k] = fmaf(WIDE ? -sl1 : -sl0, dist, sc[k]);
+          if (WIDE) sa[k] = fmaf(-sl0, dist, sa[k]);
+        }
+      }
+      if (!whole) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (!ok[k]) {
+            sc[k] = -INFINITY;
+            if (WIDE) sa[k] = -INFINITY;
+          }
+        // a row that is not seen has parameters that may be anything: 0 times them has to stay 0
+        if ((hidden >> lane) & 1u)
+          asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(sb + kLqVMeta + 16 * lane), "r"(0u) : "memory");
+        __syncwarp();
+      }
+      // ---- the values' scales: four tokens of the lane per 16, four groups
+      uint32_t sv[2][2][4];  // [16 tokens][tokens 2 t4 .. + 1, 2 t4 + 8 ..][group]
+      uint32_t top = 0;
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const uint32_t at = sb + kLqVMeta + 16 * (16 * j + 8 * e + 2 * t4);
+          const uint4 u = lds16(at), w = lds16(at + 16);
+          sv[j][e][0] = lows(u.x, w.x);
+          sv[j][e][1] = lows(u.y, w.y);
+          sv[j][e][2] = lows(u.z, w.z);
+          sv[j][e][3] = lows(u.w, w.w);
+#pragma unroll
+          for (int g = 0; g < 4; ++g) top = h2_max(top, sv[j][e][g]);
+        }
+      const float lane_top = fmaxf(half_lo(top), half_hi(top));
+      // ---- running maximum, and the power of two of the probabilities
+      float n1 = max3(fmaxf(sc[0], sc[1]), sc[2], sc[3]), n0 = WIDE ? max3(fmaxf(sa[0], sa[1]), sa[2], sa[3]) : -INFINITY;
+      if (__any_sync(0xffffffffu, n1 > m1 || (WIDE && n0 > m0) || lane_top >= scale_top)) {
+#pragma unroll
+        for (int o = 4; o < 32; o <<= 1) {
+          n1 = fmaxf(n1, __shfl_xor_sync(0xffffffffu, n1, o));
+          if (WIDE) n0 = fmaxf(n0, __shfl_xor_sync(0xffffffffu, n0, o));
+        }
+        n1 = fmaxf(n1, m1);
+        n0 = fmaxf(n0, m0);
+        int ve_new = ve;
+        float f_e = 1.f;
+        if (__any_sync(0xffffffffu, lane_top >= scale_top)) {
+          float t = fmaxf(lane_top, __shfl_xor_sync(0xffffffffu, lane_top, 1));
+          t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 2));
+          const int ex = (__float_as_int(t) >> 23) - 126;  // t < 2^ex
+          ve_new = min(max(8 - ex, -8), 15);  // largest scale times 2^ve below 2^8: seven bits of room above it
+          f_e = scale_top < 0.f ? 1.f : ex2((float)(ve_new - ve));
+          scale_top = ve_new <= -1 ? INFINITY : ex2((float)(15 - ve_new));
+          ve = ve_new;
+        }
+        const float f1 = (n1 == m1 ? 1.f : ex2(m1 - n1)) * f_e, f0 = (n0 == m0 ? 1.f : ex2(m0 - n0)) * f_e;
+        m1 = n1;
+        m0 = n0;
+        l1 *= f1;
+        l0 *= f0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          acc[j][0] *= WIDE ? f0 : f1;
+          acc[j][1] *= f1;
+          acc[j][2] *= WIDE ? f0 : f1;
+          acc[j][3] *= f1;
+        }
+        zacc[0] *= WIDE ? f0 : f1;
+        zacc[1] *= f1;
+        zacc[2] *= WIDE ? f0 : f1;
+        zacc[3] *= f1;
+      }
+      if (hidden != 0xffffffffu) {
+        const float b1 = m1 == -INFINITY ? 0.f : m1 - (float)ve, b0 = m0 == -INFINITY ? 0.f : m0 - (float)ve;
+        uint32_t pb[2][2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const float y = ex2(sc[2 * j + e] - b1), x = WIDE ? ex2(sa[2 * j + e] - b0) : 0.f;
+            l1 += y;
+            if (WIDE) l0 += x;
+            pb[j][e] = transpose_8x8(WIDE ? Elem<MC_F16>::pack(x, y) : Elem<MC_F16>::pack(y, 0.f));
+          }
+        // ---- D[channel][query row] += codes^T (p scale), zeros^T p
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const uint32_t zt = sb + kLqVMeta + 16 * (16 * j + 2 * t4) + 4 * (row & 3);  // rows of A: group row & 3
+          const uint32_t z0 = highs(lds4(zt), lds4(zt + 16)), z8 = highs(lds4(zt + 128), lds4(zt + 144));
+          mma_rows<MC_F16>(zacc, z0, z0, z8, z8, pb[j][0], pb[j][1]);
+          uint32_t r0[4], r8[4];
+          {
+            const int tr = 16 * j + (lane & 7), g = lane >> 3;
+            ldsm_x4_t(sb + kLqVCodes + tr * 64 + ((g ^ ((tr >> 1) & 3)) << 4), r0[0], r0[1], r0[2], r0[3]);
+            ldsm_x4_t(sb + kLqVCodes + (tr + 8) * 64 + ((g ^ ((tr >> 1) & 3)) << 4), r8[0], r8[1], r8[2], r8[3]);
+          }
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {
+            const uint32_t b0g = h2_mul(pb[j][0], sv[j][0][g]), b8g = h2_mul(pb[j][1], sv[j][1][g]);
+            const uint32_t u0 = r0[g] >> 8, u8 = r8[g] >> 8;
+            mma_rows<MC_F16>(acc[2 * g], r0[g] & 0x000f000fu, r0[g] & 0x00f000f0u, r8[g] & 0x000f000fu, r8[g] & 0x00f000f0u, b0g, b8g);
+            mma_rows<MC_F16>(acc[2 * g + 1], u0 & 0x000f000fu, u0 & 0x00f000f0u, u8 & 0x000f000fu, u8 & 0x00f000f0u, b0g, b8g);
+          }
+        }
+      }
+      if (!whole) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    if (fl & kTlLast) {
+      if (i + 1 < n_tiles) {
+        const int mn = __shfl_sync(0xffffffffu, src == 31 ? nxt.meta : win.meta, (i + 1) & 31);
+        load_q((mn >> 5) & 511, mn >> 14);
+      }
+#pragma unroll
+      for (int o = 4; o < 32; o <<= 1) {
+        l1 += __shfl_xor_sync(0xffffffffu, l1, o);
+        if (WIDE) l0 += __shfl_xor_sync(0xffffffffu, l0, o);
+      }
+      const size_t prow = (size_t)(team + b) * p.n_q_heads + head * nq;
+#pragma unroll
+      for (int e = 0; e < (WIDE ? 2 : 1); ++e) {
+        const int r = WIDE ? 2 * t4 + e : t4;
+        float z[4];
+#pragma unroll
+        for (int g = 0; g < 4; ++g) z[g] = __shfl_sync(0xffffffffu, zacc[e], 4 * g + t4);
+        if (r >= nq) continue;
+        const float m = WIDE && e == 0 ? m0 : m1, l = WIDE && e == 0 ? l0 : l1;
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+          *reinterpret_cast<float4*>(p.part_o + (prow + r) * kHeadDim + 32 * g + 4 * row) =
+              make_float4(fmaf(acc[2 * g][e], 0x1p24f, z[g]), fmaf(acc[2 * g][2 + e], 0x1p20f, z[g]),
+                          fmaf(acc[2 * g + 1][e], 0x1p24f, z[g]), fmaf(acc[2 * g + 1][2 + e], 0x1p20f, z[g]));
+        if (row == 0) *reinterpret_cast<float2*>(p.part_ml + 2 * (prow + r)) = make_float2(m - (float)ve, l);
+      }
+    }
+    s = s + 1 == kLqStages ? 0 : s + 1;
+    s_next = s_next + 1 == kLqStages ? 0 : s_next + 1;
+  }
+  if (*s_abort) {  // let copies in flight land before the CTA's memory is released
+    for (int k = 0; k < 2000; ++k) __nanosleep(1000);
+  }
+}
+
+// Joins a sequence's pieces (consecutive teams) and its 16-bit rows' part: out = sum_j 2^(m_j - M) o_j / sum_j 2^(m_j - M) l_j.
+// A block has R query heads, 8 / R warps each.
+constexpr int kLqCombThreads = 256;
+constexpr int kLqCombWarps = kLqCombThreads / 32;
+
+template <int DT, int R>
+__global__ void __launch_bounds__(kLqCombThreads) layer_q4_combine_kernel(const __grid_constant__ LayerQ4Params p) {
+  grid_dep_launch();
+  __shared__ int pre_s[kMaxLayerBatch + 1];
+  __shared__ float4 acc_s[kLqCombWarps][32];
+  __shared__ float l_s[kLqCombWarps], m_s[kLqCombWarps];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int b = blockIdx.y;
+  if (p.sel != nullptr) grid_dep_wait();
+  int bad = 0;
+  for (int i = tid; i < p.g.batch; i += kLqCombThreads) {
+    PageView v;
+    pre_s[i + 1] = q4_units(p, i, v, bad);
+  }
+  scan_counts(pre_s, p.g.batch);
+  const long long U = pre_s[p.g.batch];
+  const int T = q4_live_teams(p, (int)U);
+  const int x0 = pre_s[b], u = pre_s[b + 1] - x0;
+  // the team of unit x is the last c with floor(U c / T) <= x
+  const int c0 = u > 0 ? (int)(((long long)(x0 + 1) * T - 1) / U) : 0;
+  const int c1 = u > 0 ? (int)(((long long)(x0 + u) * T - 1) / U) : -1;
+  constexpr int GP = kLqCombWarps / R;  // warps per output row
+  const int grp = warp % GP;
+  const int hq = blockIdx.x * R + warp / GP;
+  const bool active = hq < p.n_q_heads;
+  if (p.sel == nullptr) grid_dep_wait();
+  float M = -INFINITY, L = 0.f;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (active) {
+    const int n_parts = c1 - c0 + 2;  // the last one: the 16-bit rows'
+    for (int c = grp; c < n_parts; c += 4 * GP) {  // four parts in flight
+      float2 ml[4];
+      float4 v[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        ml[k] = make_float2(-INFINITY, 0.f);
+        v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+        const int j = c + k * GP;
+        if (j < n_parts) {
+          const size_t prow = j + 1 < n_parts ? (size_t)(c0 + j + b) * p.n_q_heads + hq : (size_t)p.res_part + (size_t)b * p.n_q_heads + hq;
+          ml[k] = *reinterpret_cast<const float2*>(p.part_ml + 2 * prow);
+          v[k] = *reinterpret_cast<const float4*>(p.part_o + prow * kHeadDim + 4 * lane);
+        }
+      }
+      float M2 = M;
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (ml[k].y != 0.f) M2 = fmaxf(M2, ml[k].x);
+      const float f = L == 0.f ? 0.f : ex2(M - M2);
+      M = M2;
+      L *= f;
+      o.x *= f;
+      o.y *= f;
+      o.z *= f;
+      o.w *= f;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float w = ml[k].y == 0.f ? 0.f : ex2(ml[k].x - M);
+        L = fmaf(w, ml[k].y, L);
+        o.x = fmaf(w, v[k].x, o.x);
+        o.y = fmaf(w, v[k].y, o.y);
+        o.z = fmaf(w, v[k].z, o.z);
+        o.w = fmaf(w, v[k].w, o.w);
+      }
+    }
+  }
+  if (GP > 1) {
+    acc_s[warp][lane] = o;
+    if (lane == 0) {
+      l_s[warp] = L;
+      m_s[warp] = M;
+    }
+    __syncthreads();
+    if (grp != 0 || !active) return;
+    float Ma = M;
+    for (int g = 1; g < GP; ++g) Ma = fmaxf(Ma, m_s[warp + g]);
+    const float f = L == 0.f ? 0.f : ex2(M - Ma);
+    L *= f;
+    o.x *= f;
+    o.y *= f;
+    o.z *= f;
+    o.w *= f;
+    for (int g = 1; g < GP; ++g) {
+      const float lg = l_s[warp + g], fg = lg == 0.f ? 0.f : ex2(m_s[warp + g] - Ma);
+      const float4 t = acc_s[warp + g][lane];
+      L = fmaf(fg, lg, L);
+      o.x = fmaf(fg, t.x, o.x);
+      o.y = fmaf(fg, t.y, o.y);
+      o.z = fmaf(fg, t.z, o.z);
+      o.w = fmaf(fg, t.w, o.w);
+    }
+    M = Ma;
+  } else if (!active) {
+    return;
+  }
+  const float inv = L == 0.f ? 0.f : 1.f / L;  // (a query that sees nothing: zeros, log-sum-exp -inf)
+  const size_t orow = (size_t)b * p.n_q_heads + hq;
+  uint2 packed;
+  packed.x = Elem<DT>::pack(o.x * inv, o.y * inv);
+  packed.y = Elem<DT>::pack(o.z * inv, o.w * inv);
+  *reinterpret_cast<uint2*>(p.out + orow * kHeadDim + lane * 4) = packed;
+  if (lane == 0 && p.lse != nullptr) p.lse[orow] = L == 0.f ? -INFINITY : (M + log2f(L)) * kLn2;
+}
+
+// ---- host side ------------------------------------------------------------------------------------
+struct LayerQ4Plan {
+  int members, n_teams;
+  long long max_units;
+  size_t rows, o_bytes, ml_bytes;
+};
+// The workspace is sized for kLqMaxCtas CTAs, so that its size needs no device.
+constexpr int kLqMaxCtas = 512;
+static LayerQ4Plan layer_q4_plan(const mc_config* cfg, const mc_batch* bt, int ctas) {
+  LayerQ4Plan pl;
+  const int warps = std::min(ctas, kLqMaxCtas) * kLqWarps;
+  const int per_warp = (cfg->n_kv_heads + warps - 1) / warps;  // heads
+  pl.members = (cfg->n_kv_heads + per_warp - 1) / per_warp;
+  pl.max_units = std::max<long long>((long long)bt->batch * (bt->max_seq_len / kLqPage), 1);
+  pl.n_teams = (int)std::max<long long>(1, std::min<long long>(warps / pl.members, pl.max_units));
+  pl.rows = (size_t)(pl.n_teams + bt->batch) * cfg->n_q_heads + (size_t)bt->batch * cfg->n_q_heads;
+  pl.o_bytes = align_up(pl.rows * kHeadDim * 4, 256);
+  pl.ml_bytes = align_up(pl.rows * 2 * 4, 256);
+  return pl;
+}
+static constexpr size_t q4_smem_bytes(int batch) {
+  return 1024 + (size_t)kLqWarps * kLqStages * (kLqStageBytes + 8) + (size_t)(batch + 2) * (4 + sizeof(Q4Seq));
+}
+static_assert(q4_smem_bytes(kMaxLayerBatch) <= 227 * 1024, "a CTA's shared memory");
+
+size_t layer_q4_attn_workspace_bytes(const mc_config* cfg, const mc_batch* bt, int) {
+  const LayerQ4Plan pl = layer_q4_plan(cfg, bt, kLqMaxCtas);
+  return pl.o_bytes + pl.ml_bytes;
+}
+
+mc_status launch_layer_q4_attn(const mc_config* cfg, const mc_batch* bt, const Geom& g, const mc_layer_q4_cache* layer,
+                               const mc_score_opts* opts, const int32_t* pages, const int32_t* counts, int pages_stride, const void* q,
+                               const void* k_new, const void* v_new, int flags, void* out, float* lse, void* workspace,
+                               cudaStream_t stream) {
+  if (bt->batch == 0) return MC_OK;
+  int n_sm = 0;
+  if (mc_status st = sm_count(&n_sm)) return st;
+  const int ctas = std::min(n_sm * kLqCtasPerSm, kLqMaxCtas);
+  const LayerQ4Plan pl = layer_q4_plan(cfg, bt, ctas);
+  CUtensorMap map_km, map_vc;
+  const uint64_t tiles = (uint64_t)std::max<int64_t>(bt->n_pages, 1) * cfg->n_kv_heads;
+  if (mc_status st = make_map_rows(&map_km, layer->k_meta, tiles * 4, 128, 4)) return st;
+  if (mc_status st = make_map_rows(&map_vc, layer->v_codes, tiles * kLqPage, 64, kLqPage)) return st;
+  LayerQ4Params ap;
+  ap.g = g;
+  ap.rule = make_score_rule(opts);
+  ap.k_codes = (const unsigned char*)layer->k_codes;
+  ap.v_meta = (const unsigned char*)layer->v_meta;
+  ap.pool[0] = (unsigned char*)layer->k_codes;
+  ap.pool[1] = (unsigned char*)layer->k_meta;
+  ap.pool[2] = (unsigned char*)layer->v_codes;
+  ap.pool[3] = (unsigned char*)layer->v_meta;
+  ap.res_k = (char*)layer->res_k;
+  ap.res_v = (char*)layer->res_v;
+  ap.status = layer->status;
+  ap.q = (const char*)q;
+  ap.k_new = (const char*)k_new;
+  ap.v_new = (const char*)v_new;
+  ap.sel = pages;
+  ap.counts = counts;
+  ap.sel_stride = pages_stride;
+  ap.part_o = (float*)workspace;
+  ap.part_ml = (float*)((char*)workspace + pl.o_bytes);
+  ap.nq = cfg->n_q_heads / cfg->n_kv_heads;
+  ap.n_q_heads = cfg->n_q_heads;
+  ap.members = pl.members;
+  ap.n_teams = pl.n_teams;
+  ap.res_part = (pl.n_teams + bt->batch) * cfg->n_q_heads;
+  ap.flags = flags;
+  ap.out = (unsigned short*)out;
+  ap.lse = lse;
+  const bool wide = ap.nq == 8;
+  auto* split = cfg->dtype == MC_F16 ? (wide ? layer_q4_split_kernel<MC_F16, true> : layer_q4_split_kernel<MC_F16, false>)
+                                     : (wide ? layer_q4_split_kernel<MC_BF16, true> : layer_q4_split_kernel<MC_BF16, false>);
+  MC_CUDA_CHECK(allow_smem(split, q4_smem_bytes(kMaxLayerBatch)));
+  const int grid = std::max((pl.n_teams * pl.members + kLqWarps - 1) / kLqWarps, std::min(ctas, bt->batch * cfg->n_kv_heads));
+  MC_CUDA_CHECK(launch_pdl(split, dim3(grid), dim3(kLqThreads), q4_smem_bytes(bt->batch), stream, ap, map_km, map_vc));
+  // warps per output row: about three parts each
+  const long long parts = pl.n_teams / bt->batch + 2;
+  int per_block = kLqCombWarps;  // rows
+  while (per_block > 1 && parts > 3 * (kLqCombWarps / per_block)) per_block /= 2;
+  using Combine = void (*)(const LayerQ4Params);
+  static const Combine combines[2][4] = {
+      {layer_q4_combine_kernel<MC_F16, 1>, layer_q4_combine_kernel<MC_F16, 2>, layer_q4_combine_kernel<MC_F16, 4>,
+       layer_q4_combine_kernel<MC_F16, 8>},
+      {layer_q4_combine_kernel<MC_BF16, 1>, layer_q4_combine_kernel<MC_BF16, 2>, layer_q4_combine_kernel<MC_BF16, 4>,
+       layer_q4_combine_kernel<MC_BF16, 8>}};
+  const Combine combine = combines[cfg->dtype == MC_F16 ? 0 : 1][per_block == 1 ? 0 : per_block == 2 ? 1 : per_block == 4 ? 2 : 3];
+  MC_CUDA_CHECK(launch_pdl(combine, dim3((cfg->n_q_heads + per_block - 1) / per_block, bt->batch), dim3(kLqCombThreads), 0, stream, ap));
+  MC_CUDA_CHECK(cudaGetLastError());
+  return MC_OK;
+}
+
+}  // namespace mc

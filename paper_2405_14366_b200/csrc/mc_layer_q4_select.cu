@@ -1,0 +1,310 @@
+// Which pages of a 4-bit layer are worth attending: per (sequence, kv head) those with the largest bound
+//
+//   sum_h sum_c max(q_hc lo_c, q_hc hi_c) = Q.zero + 15 P.scale,   Q = sum_h q_h,  P = sum_h max(q_h, 0)
+//
+// over the kv head's query heads h (lo = zero, hi = zero + 15 scale, scale > 0: what channel c of a key of the page can hold).
+// The keys' group parameters are the bounds already: 512 of a page's 5120 bytes are read, nothing else of the cache.
+// Sums are held in 64 bits: the last page in and the first one out differ by less than binary32 resolves often enough
+// that the choice would hang on the order of a sum.  (256 products a page are 4 cycles of the SM's 64-bit units, their
+// operands' conversions 16; the page's bytes take 22 at the memory's rate.)
+// A cluster of CTAs per (sequence, kv head) forms the sums; their binary32 roundings, which keep the order, go to the first
+// CTA's shared memory, where a radix select finds the last one in.  Pages that round alike there are told apart by the
+// 64-bit sums, and equal ones by their index.
+#include <algorithm>
+
+#include "mc_kernels.h"
+#include "mc_layer.h"
+#include "mc_layer_q4.cuh"
+#include "mc_layer_q4.h"
+
+namespace mc {
+
+constexpr int kLsThreads = 256;
+constexpr int kLsWarps = kLsThreads / 32;
+constexpr int kLsMaxCluster = 8;
+constexpr int kLsBatch = 8;  // pages of a warp at a time
+constexpr int kLsBins = 2048;
+
+struct Q4SelectParams {
+  Geom g;
+  ScoreRule rule;
+  const unsigned char* k_meta;
+  int32_t* status;
+  const char* q;
+  int32_t* pages;
+  int32_t* counts;
+  unsigned long long* keys;  // [segment][key_stride]: the sums in an order that compares as integers
+  int key_stride;
+  int budget, n_sink, n_recent;
+  int nq, n_q_heads;
+  int cluster;
+};
+
+__device__ __forceinline__ uint32_t order32(float x) {
+  const uint32_t b = __float_as_uint(x);
+  return x != x ? 0u : (b & 0x80000000u) ? ~b : b | 0x80000000u;
+}
+__device__ __forceinline__ unsigned long long order64(double x) {
+  const unsigned long long b = (unsigned long long)__double_as_longlong(x);
+  return x != x ? 0ull : (b >> 63) ? ~b : b | (1ull << 63);
+}
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+__device__ __forceinline__ void store_first_cta(uint32_t* smem, uint32_t v) {
+  uint32_t a;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(a) : "r"((uint32_t)__cvta_generic_to_shared(smem)));
+  asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(a), "r"(v) : "memory");
+}
+
+template <int DT>
+__global__ void __launch_bounds__(kLsThreads) layer_q4_select_kernel(const __grid_constant__ Q4SelectParams p) {
+  grid_dep_launch();
+  extern __shared__ uint32_t keys_s[];  // [pages] of the first CTA
+  __shared__ uint32_t hist[kLsBins];
+  __shared__ uint32_t scan_s[kLsWarps], pick_s[3];
+  __shared__ int ins_s[kLsWarps], ties_s[kLsWarps];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int H = p.g.n_kv_heads;
+  const int rank = blockIdx.x % p.cluster, seg = blockIdx.x / p.cluster;
+  const int b = seg / H, head = seg - b * H;
+  cluster_arrive();  // (every CTA of the cluster runs before one writes to another)
+  grid_dep_wait();   // queries, parameters: what the kernels ahead have written
+  const int raw = __ldcg(p.g.seq_lens + b);
+  if ((raw < 0 || raw > p.g.max_seq_len) && tid == 0) atomicOr(p.status, MC_FLAG_BAD_METADATA);
+  const int n = min(max(raw, 0), p.g.max_seq_len), full = n / kLqPage;
+  const PageView v = page_view(p.rule, b, n, n + 1, n);
+  const int u = v.u, take = min(p.budget, u);
+  if (head == 0 && rank == 0 && tid == 0) p.counts[b] = take;
+  int32_t* list = p.pages + (size_t)seg * p.budget;
+  cluster_wait();
+  if (u <= p.budget) {  // (the whole cluster)
+    if (rank == 0)
+      for (int k = tid; k < u; k += kLsThreads) list[k] = v.page_of(k);
+    return;
+  }
+  unsigned long long* keys = p.keys + (size_t)seg * p.key_stride;
+  {
+    double Q[4] = {}, P[4] = {};
+    for (int h = 0; h < p.nq; ++h) {
+      const uint2 w = *reinterpret_cast<const uint2*>(p.q + ((size_t)b * p.n_q_heads + head * p.nq + h) * kRowBytes + 8 * lane);
+      const float2 x = Elem<DT>::unpack(w.x), y = Elem<DT>::unpack(w.y);
+      const float f[4] = {x.x, x.y, y.x, y.y};
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        Q[c] += (double)f[c];
+        P[c] += f[c] < 0.f ? 0.0 : (double)f[c];  // (a NaN stays one)
+      }
+    }
+#pragma unroll
+    for (int c = 0; c < 4; ++c) P[c] *= 15.0;
+    for (int k0 = (rank * kLsWarps + warp) * kLsBatch; k0 < u; k0 += p.cluster * kLsWarps * kLsBatch) {
+      int mine = 0;
+      if (lane < kLsBatch && k0 + lane < u) {
+        mine = checked_page(p.g, b, v.page_of(k0 + lane), p.status);
+        mine = mine < 0 ? 0 : mine;
+      }
+      uint4 m[kLsBatch];
+#pragma unroll
+      for (int j = 0; j < kLsBatch; ++j) {
+        const int page = __shfl_sync(0xffffffffu, mine, j);
+        m[j] = *reinterpret_cast<const uint4*>(p.k_meta + ((size_t)page * H + head) * kLqMetaBytes + 16 * lane);
+      }
+      double a[kLsBatch];
+#pragma unroll
+      for (int j = 0; j < kLsBatch; ++j) {
+        const uint32_t w[4] = {m[j].x, m[j].y, m[j].z, m[j].w};
+        double t = 0.0;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const float2 sz = Elem<MC_F16>::unpack(w[c]);
+          t = fma(Q[c], (double)sz.y, fma(P[c], (double)sz.x, t));
+        }
+        a[j] = t;
+      }
+      // eight sums over the warp, halving the pages a lane keeps: lane 4 j ends with page j
+#pragma unroll
+      for (int o = 16, c = 4; c > 0; o >>= 1, c >>= 1) {
+        const bool up = (lane & o) != 0;
+#pragma unroll
+        for (int j = 0; j < c; ++j) {
+          const double give = up ? a[j] : a[j + c], keep = up ? a[j + c] : a[j];
+          a[j] = keep + __shfl_xor_sync(0xffffffffu, give, o);
+        }
+      }
+      a[0] += __shfl_xor_sync(0xffffffffu, a[0], 2);
+      a[0] += __shfl_xor_sync(0xffffffffu, a[0], 1);
+      const int k = k0 + (lane >> 2);
+      if ((lane & 3) == 0 && k < u) {
+        const int slot = v.page_of(k);
+        const double x = a[0] + 0.0;  // (-0 counts as 0)
+        const bool guarded = slot < p.n_sink || slot >= full - p.n_recent;
+        keys[k] = guarded ? ~0ull : order64(x);
+        store_first_cta(keys_s + k, guarded ? 0xffffffffu : order32((float)x));
+      }
+    }
+  }
+  cluster_arrive();
+  cluster_wait();
+  if (rank != 0) return;
+
+  // ---- the last one in: digits of the 32-bit keys, then (of those that are alike in them) of the 64-bit ones
+  uint32_t p32 = 0, m32 = 0;
+  unsigned long long p64 = 0, m64 = 0;
+  int need = take;   // of those that match the digits so far
+  bool all = false;  // every one of them
+  auto matches = [&](int k) {
+    const uint32_t c = keys_s[k];
+    if ((c & m32) != p32) return false;
+    return m64 == 0 || (keys[k] & m64) == p64;
+  };
+  for (int pass = 0; pass < 9 && !all; ++pass) {
+    const bool wide = pass >= 3;
+    const int width = pass == 2 ? 10 : pass == 8 ? 9 : 11;
+    const int shift = pass == 0 ? 21 : pass == 1 ? 10 : pass == 2 ? 0 : pass == 8 ? 0 : 53 - 11 * (pass - 3);
+    for (int i = tid; i < kLsBins; i += kLsThreads) hist[i] = 0;
+    __syncthreads();
+    for (int k = tid; k < u; k += kLsThreads)
+      if (matches(k)) atomicAdd(&hist[(wide ? (uint32_t)(keys[k] >> shift) : keys_s[k] >> shift) & ((1u << width) - 1u)], 1u);
+    __syncthreads();
+    // the bin from the top in which the need-th lies: thread t has the bins 8 t .. 8 t + 7
+    constexpr int kOwn = kLsBins / kLsThreads;
+    uint32_t own[kOwn], sum = 0;
+#pragma unroll
+    for (int j = 0; j < kOwn; ++j) {
+      own[j] = hist[tid * kOwn + j];
+      sum += own[j];
+    }
+    uint32_t above = sum;  // bins of this thread and those behind it in the warp
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint32_t t = __shfl_down_sync(0xffffffffu, above, o);
+      if (lane + o < 32) above += t;
+    }
+    if (lane == 0) scan_s[warp] = above;
+    __syncthreads();
+    above -= sum;
+    for (int w = warp + 1; w < kLsWarps; ++w) above += scan_s[w];
+    if (above < (uint32_t)need && above + sum >= (uint32_t)need) {
+#pragma unroll
+      for (int j = kOwn - 1; j >= 0; --j) {
+        if (above < (uint32_t)need && above + own[j] >= (uint32_t)need) {
+          pick_s[0] = tid * kOwn + j;
+          pick_s[1] = need - above;
+          pick_s[2] = own[j];
+        }
+        above += own[j];
+      }
+    }
+    __syncthreads();
+    const unsigned long long digit = pick_s[0], mask = (1u << width) - 1u;
+    if (wide) {
+      p64 |= digit << shift;
+      m64 |= mask << shift;
+    } else {
+      p32 |= (uint32_t)digit << shift;
+      m32 |= (uint32_t)mask << shift;
+    }
+    need = pick_s[1];
+    all = pick_s[1] == pick_s[2];
+    __syncthreads();
+  }
+
+  // ---- the list, in ascending order: a warp has a run of pages
+  const int per = ((u + kLsWarps - 1) / kLsWarps + 31) / 32 * 32;
+  const int k0 = min(warp * per, u), k1 = min(k0 + per, u);
+  auto look = [&](int k, bool& in, bool& tie) {
+    in = tie = false;
+    if (k >= k1) return;
+    const uint32_t c = keys_s[k] & m32;
+    if (c != p32) {
+      in = c > p32;
+    } else if (m64 != 0) {
+      const unsigned long long d = keys[k] & m64;
+      in = d > p64;
+      tie = d == p64;
+    } else {
+      tie = true;
+    }
+  };
+  int ins = 0, ties = 0;
+  for (int k = k0; k < k1; k += 32) {
+    bool in, tie;
+    look(k + lane, in, tie);
+    ins += __popc(__ballot_sync(0xffffffffu, in));
+    ties += __popc(__ballot_sync(0xffffffffu, tie));
+  }
+  if (lane == 0) {
+    ins_s[warp] = ins;
+    ties_s[warp] = ties;
+  }
+  __syncthreads();
+  int in_before = 0, tie_before = 0;
+  for (int w = 0; w < warp; ++w) {
+    in_before += ins_s[w];
+    tie_before += ties_s[w];
+  }
+  const uint32_t below = (1u << lane) - 1u;
+  for (int k = k0; k < k1; k += 32) {
+    bool in, tie;
+    look(k + lane, in, tie);
+    const uint32_t bi = __ballot_sync(0xffffffffu, in), bt = __ballot_sync(0xffffffffu, tie);
+    const int t = tie_before + __popc(bt & below);  // ties ahead of this one: the first `need` are in
+    if (in || (tie && t < need)) list[in_before + __popc(bi & below) + min(t, need)] = v.page_of(k + lane);
+    in_before += __popc(bi);
+    tie_before += __popc(bt);
+  }
+}
+
+// ---- host side ------------------------------------------------------------------------------------
+size_t layer_q4_select_workspace_bytes(const mc_config* cfg, const mc_batch* bt) {
+  return align_up((size_t)bt->batch * cfg->n_kv_heads * (bt->max_seq_len / kLqPage) * 8, 256);
+}
+
+mc_status launch_layer_q4_select(const mc_config* cfg, const mc_batch* bt, const Geom& g, const mc_layer_q4_cache* layer,
+                                 const mc_score_opts* opts, const mc_page_selection* keep, const void* q, int32_t* pages, int32_t* counts,
+                                 void* workspace, cudaStream_t stream) {
+  if (bt->batch == 0) return MC_OK;
+  Q4SelectParams sp;
+  sp.g = g;
+  sp.rule = make_score_rule(opts);
+  sp.k_meta = (const unsigned char*)layer->k_meta;
+  sp.status = layer->status;
+  sp.q = (const char*)q;
+  sp.pages = pages;
+  sp.counts = counts;
+  sp.keys = (unsigned long long*)workspace;
+  sp.key_stride = bt->max_seq_len / kLqPage;
+  sp.budget = keep->budget;
+  sp.n_sink = keep->n_sink;
+  sp.n_recent = keep->n_recent;
+  sp.nq = cfg->n_q_heads / cfg->n_kv_heads;
+  sp.n_q_heads = cfg->n_q_heads;
+  int n_sm = 0;
+  if (mc_status st = sm_count(&n_sm)) return st;
+  // CTAs per (sequence, kv head): while all have an SM each and still a turn of pages for every warp
+  const long long segs = (long long)bt->batch * cfg->n_kv_heads;
+  int cluster = 1;
+  while (cluster < kLsMaxCluster && segs * cluster * 2 <= n_sm && sp.key_stride >= 2 * cluster * kLsWarps * kLsBatch) cluster *= 2;
+  sp.cluster = cluster;
+  auto* kernel = cfg->dtype == MC_F16 ? layer_q4_select_kernel<MC_F16> : layer_q4_select_kernel<MC_BF16>;
+  MC_CUDA_CHECK(allow_smem(kernel, (size_t)kQ4MaxSelectLen / kLqPage * 4));
+  cudaLaunchConfig_t lc = {};
+  lc.gridDim = dim3((unsigned)(segs * cluster));
+  lc.blockDim = dim3(kLsThreads);
+  lc.dynamicSmemBytes = (size_t)sp.key_stride * 4;
+  lc.stream = stream;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = cluster;
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = 1;
+  lc.attrs = attr;
+  lc.numAttrs = 2;
+  MC_CUDA_CHECK(cudaLaunchKernelEx(&lc, kernel, sp));
+  MC_CUDA_CHECK(cudaGetLastError());
+  return MC_OK;
+}
+
+}  // namespace mc

@@ -332,14 +332,14 @@ static EncodeTiledFn encode_tiled_fn() {
 }
 
 static mc_status encode_map(CUtensorMap* map, int dtype, const void* base, int rank, const cuuint64_t* dims, const cuuint64_t* strides,
-                            const cuuint32_t* box) {
+                            const cuuint32_t* box, CUtensorMapSwizzle swizzle = CU_TENSOR_MAP_SWIZZLE_128B) {
   EncodeTiledFn fn = encode_tiled_fn();
   if (fn == nullptr) return MC_ERR_UNSUPPORTED;
   const cuuint32_t estr[3] = {1, 1, 1};
   const auto encode = [&]() {
     return fn(map, dtype == MC_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank,
               const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+              swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   };
   CUresult r = encode();
   if (r != CUDA_SUCCESS) {
@@ -369,6 +369,13 @@ mc_status make_map3(CUtensorMap* map, int dtype, const void* base, uint64_t plan
   const cuuint64_t strides[2] = {cols * 2, rows * cols * 2};
   const cuuint32_t box[3] = {(cuuint32_t)kPfTileK, (cuuint32_t)box_rows, (cuuint32_t)box_planes};
   return encode_map(map, dtype, base, 3, dims, strides, box);
+}
+
+mc_status make_map_rows(CUtensorMap* map, const void* base, uint64_t rows, int row_bytes, int box_rows) {
+  const cuuint64_t dims[2] = {(cuuint64_t)row_bytes / 2, rows};
+  const cuuint64_t strides[1] = {(cuuint64_t)row_bytes};
+  const cuuint32_t box[2] = {(cuuint32_t)row_bytes / 2, (cuuint32_t)box_rows};
+  return encode_map(map, MC_F16, base, 2, dims, strides, box, row_bytes == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
 mc_status launch_prefill_merge(const mc_config* cfg, const mc_batch* bt, const Geom& g, const mc_projection* proj,
