@@ -16,8 +16,9 @@
 // Work: the complete pages that are seen (or selected), split equally over teams of warps, a warp per kv head in each (neighbouring
 // warps stream neighbouring tiles of a page).  A warp is a pipeline of its own with a ring of stages of one tile (5 KB: codes and
 // parameters of K and V), two copied with the tensor map's swizzle so that ldmatrix and 16-byte loads meet no bank conflicts.
-// One more warp per CTA attends the 16-bit rows of the begun pages and the step's new rows, and appends them.  Partial results
-// are joined by a second kernel.
+// A sequence's begun page and the step's new row, 16-bit rows, are one unit more, ahead of its pages: attended straight from
+// global memory while the first tiles are on their way, and the new row appended.  Partial results are joined by a second
+// kernel.
 #include <algorithm>
 
 #include "mc_kernels.h"
@@ -30,10 +31,10 @@
 
 namespace mc {
 
-constexpr int kLqWarps = 7;  // that stream pages
-constexpr int kLqThreads = (kLqWarps + 1) * 32;
-constexpr int kLqCtasPerSm = 2;
-constexpr int kLqStages = 3;
+constexpr int kLqWarps = 12;
+constexpr int kLqThreads = kLqWarps * 32;
+constexpr int kLqCtasPerSm = 1;
+constexpr int kLqStages = 2;
 constexpr int kLqStageBytes = 2 * (kLqCodeBytes + kLqMetaBytes);
 constexpr int kLqVCodes = kLqCodeBytes, kLqKMeta = 2 * kLqCodeBytes, kLqVMeta = kLqKMeta + kLqMetaBytes;  // within a stage
 static_assert(kLqStageBytes % 1024 == 0, "the swizzle patterns repeat within 1 KB");
@@ -63,29 +64,69 @@ struct LayerQ4Params {
   float* lse;
 };
 
-// What every CTA keeps of a sequence.
+// What every CTA keeps of a sequence: its length, the query's position, the tokens [0, a) and [lo, hi) that are seen.
 struct Q4Seq {
-  int n, q_pos, a, lo, hi, ua, ub0;
+  int n, q_pos, a, lo, hi;
 };
-__device__ __forceinline__ int q4_units(const LayerQ4Params& p, int b, PageView& v, int& bad) {
+__device__ __forceinline__ int q4_page_of(const Q4Seq& s, int k) {  // (as page_view counts them)
+  const int ua = (min(s.a, s.n / kLqPage * kLqPage) + kLqPage - 1) / kLqPage;
+  return k < ua ? k : max(s.lo / kLqPage, ua) + k - ua;
+}
+// Complete pages of sequence b that the call attends; `begun`: 1 if there are 16-bit rows too.
+__device__ __forceinline__ int q4_units(const LayerQ4Params& p, int b, PageView& v, int& begun, int& bad) {
   const int raw = __ldcg(p.g.seq_lens + b);
   bad |= (raw < 0 || raw > p.g.max_seq_len) ? 1 : 0;
   const int n = min(max(raw, 0), p.g.max_seq_len), n_tot = n + (p.k_new != nullptr ? 1 : 0);
   v = page_view(p.rule, b, n, n_tot, n_tot - 1);
+  begun = n_tot > n / kLqPage * kLqPage ? 1 : 0;
   if (p.sel == nullptr) return v.u;
   const int c = __ldcg(p.counts + b);
   bad |= (c < 0 || c > p.sel_stride || c > n / kLqPage) ? 1 : 0;
   return min(max(c, 0), min(p.sel_stride, n / kLqPage));
 }
+
+// The units of a call: all pages, sequence by sequence, then the begun pages, which count for kLqBegunUnits each (a begun
+// page is 16 KB and is not pipelined).
+constexpr int kLqBegunUnits = 3;
+struct Q4Prefix {
+  int* pages;  // [batch + 1] exclusive prefixes
+  int* begun;
+};
+__device__ __forceinline__ Q4Prefix q4_prefix_at(void* smem, int batch) {
+  Q4Prefix f;
+  f.pages = reinterpret_cast<int*>(smem);
+  f.begun = f.pages + batch + 1;
+  return f;
+}
+__device__ __forceinline__ void q4_scan(const Q4Prefix& f, int batch) {
+  scan_counts(f.pages, batch);
+  scan_counts(f.begun, batch);
+}
+__device__ __forceinline__ int q4_total(const Q4Prefix& f, int batch) { return f.pages[batch] + kLqBegunUnits * f.begun[batch]; }
 __device__ __forceinline__ int q4_live_teams(const LayerQ4Params& p, int units) { return min(p.n_teams, max(units, 1)); }
 
-// One tile as a lane of the window knows it.
-struct Tile {
-  int meta;  // flags | sequence << 5 | kv head << 14
-  int t0;    // first token
-  int page;  // raw page id
+// A warp's share: of the pages [x0, x1) and the begun pages [g0, g1) of the batch the kv heads member, member + members, ...
+struct Q4Share {
+  int team, member, n_heads;
+  int x0, x1, g0, g1;
 };
-enum { kTlLoad = 1, kTlFirst = 2, kTlLast = 4, kTlBad = 8 };
+__device__ __forceinline__ Q4Share q4_share(const LayerQ4Params& p, const Q4Prefix& f, int warp) {
+  Q4Share s;
+  s.team = warp / p.members;
+  s.member = warp - s.team * p.members;
+  s.n_heads = (p.g.n_kv_heads - s.member + p.members - 1) / p.members;
+  const int pages = f.pages[p.g.batch], units = q4_total(f, p.g.batch), teams = q4_live_teams(p, units);
+  int u0 = 0, u1 = 0;
+  if (s.team < teams) {
+    u0 = (int)((long long)units * s.team / teams);
+    u1 = (int)((long long)units * (s.team + 1) / teams);
+  }
+  s.x0 = min(u0, pages);
+  s.x1 = min(u1, pages);
+  s.g0 = (max(u0 - pages, 0) + kLqBegunUnits - 1) / kLqBegunUnits;  // (a begun page is its first unit's owner's)
+  s.g1 = (max(u1 - pages, 0) + kLqBegunUnits - 1) / kLqBegunUnits;
+  return s;
+}
 
 __device__ __forceinline__ uint32_t transpose_8x8(uint32_t v) {
   uint32_t r;
@@ -97,23 +138,40 @@ __device__ __forceinline__ uint4 lds16(uint32_t a) {
   asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
   return v;
 }
-__device__ __forceinline__ uint32_t lds4(uint32_t a) {
-  uint32_t v;
-  asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
-  return v;
-}
 __device__ __forceinline__ uint32_t h2_mul(uint32_t a, uint32_t b) {
   const __half2 r = __hmul2(*reinterpret_cast<__half2*>(&a), *reinterpret_cast<__half2*>(&b));
   return *reinterpret_cast<const uint32_t*>(&r);
 }
-// a b - c
-__device__ __forceinline__ uint32_t h2_fms(uint32_t a, uint32_t b, uint32_t c) {
-  const __half2 r = __hfma2(*reinterpret_cast<__half2*>(&a), *reinterpret_cast<__half2*>(&b), __hneg2(*reinterpret_cast<__half2*>(&c)));
+__device__ __forceinline__ uint32_t h2_fma(uint32_t a, uint32_t b, uint32_t c) {
+  const __half2 r = __hfma2(*reinterpret_cast<__half2*>(&a), *reinterpret_cast<__half2*>(&b), *reinterpret_cast<__half2*>(&c));
   return *reinterpret_cast<const uint32_t*>(&r);
 }
 __device__ __forceinline__ uint32_t h2_max(uint32_t a, uint32_t b) {
   const __half2 r = __hmax2(*reinterpret_cast<__half2*>(&a), *reinterpret_cast<__half2*>(&b));
   return *reinterpret_cast<const uint32_t*>(&r);
+}
+// D = A B (mma_rows without an addend: no registers to be cleared)
+__device__ __forceinline__ void mma_first(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
+}
+// c + (low or high half of a) (high half of b), in binary32: sm_100's mixed-precision FMA (a tensor-core row of zeros costs
+// eight of its cycles and the halves' rearrangement besides).
+__device__ __forceinline__ float fma_lo_hi(uint32_t a, uint32_t b, float c) {
+  float r;
+  asm("{\n\t.reg .b16 al, ah, bl, bh;\n\tmov.b32 {al, ah}, %1;\n\tmov.b32 {bl, bh}, %2;\n\tfma.rn.f32.f16 %0, al, bh, %3;\n\t}"
+      : "=f"(r)
+      : "r"(a), "r"(b), "f"(c));
+  return r;
+}
+__device__ __forceinline__ float fma_hi_hi(uint32_t a, uint32_t b, float c) {
+  float r;
+  asm("{\n\t.reg .b16 al, ah, bl, bh;\n\tmov.b32 {al, ah}, %1;\n\tmov.b32 {bl, bh}, %2;\n\tfma.rn.f32.f16 %0, ah, bh, %3;\n\t}"
+      : "=f"(r)
+      : "r"(a), "r"(b), "f"(c));
+  return r;
 }
 __device__ __forceinline__ uint32_t lows(uint32_t a, uint32_t b) { return __byte_perm(a, b, 0x5410); }
 __device__ __forceinline__ uint32_t highs(uint32_t a, uint32_t b) { return __byte_perm(a, b, 0x7632); }
@@ -125,9 +183,9 @@ template <int DT>
 __device__ __noinline__ void q4_begun_page(const LayerQ4Params& p, int b, int head) {
   const int lane = threadIdx.x & 31, row = lane >> 2, t4 = lane & 3, colp = 2 * t4;
   const int nq = p.nq, H = p.g.n_kv_heads;
-  int bad = 0;
+  int bad = 0, begun;
   PageView v;
-  q4_units(p, b, v, bad);
+  q4_units(p, b, v, begun, bad);
   const int n = v.n, base = n / kLqPage * kLqPage, n_tot = n + (p.k_new != nullptr ? 1 : 0);
   const size_t at = ((size_t)b * H + head) * kLqResBytes, new_at = ((size_t)b * H + head) * kRowBytes;
   const size_t prow = (size_t)p.res_part + (size_t)b * p.n_q_heads + head * nq;
@@ -271,8 +329,8 @@ layer_q4_split_kernel(const __grid_constant__ LayerQ4Params p, const __grid_cons
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + kLqWarps * kLqStages * kLqStageBytes);
   Q4Seq* seq_s = reinterpret_cast<Q4Seq*>(bars + kLqWarps * kLqStages);
-  int* pre_s = reinterpret_cast<int*>(seq_s + p.g.batch);
-  volatile int* s_abort = pre_s + p.g.batch + 1;
+  Q4Prefix pre = q4_prefix_at(seq_s + p.g.batch, p.g.batch);
+  volatile int* s_abort = pre.begun + p.g.batch + 1;
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int row = lane >> 2, t4 = lane & 3;
@@ -292,411 +350,415 @@ layer_q4_split_kernel(const __grid_constant__ LayerQ4Params p, const __grid_cons
   int bad = 0;
   for (int b = tid; b < p.g.batch; b += kLqThreads) {
     PageView v;
-    pre_s[b + 1] = q4_units(p, b, v, bad);
-    seq_s[b] = Q4Seq{v.n, v.q_pos, v.a, v.lo, v.hi, v.ua, v.ub0};
+    int begun;
+    pre.pages[b + 1] = q4_units(p, b, v, begun, bad);
+    pre.begun[b + 1] = begun;
+    seq_s[b] = Q4Seq{v.n, v.q_pos, v.a, v.lo, v.hi};
   }
-  scan_counts(pre_s, p.g.batch);
+  q4_scan(pre, p.g.batch);
 
-  if (warp == kLqWarps) {
-    grid_dep_wait();
-    if (bad && blockIdx.x == 0) atomicOr(p.status, MC_FLAG_BAD_METADATA);
-    for (int i = blockIdx.x; i < p.g.batch * H; i += gridDim.x) q4_begun_page<DT>(p, i / H, i % H);
-    return;
-  }
+  const Q4Share sh = q4_share(p, pre, blockIdx.x * kLqWarps + warp);
+  const int nx = sh.x1 - sh.x0;
+  const int n_tiles = nx * sh.n_heads;  // of this warp: head by head, page by page
 
-  const int n_units = pre_s[p.g.batch];
-  const int teams = q4_live_teams(p, n_units);
-  const int gw = blockIdx.x * kLqWarps + warp;
-  const int team = gw / p.members, member = gw - team * p.members;
-  int x_begin = 0, x_end = 0;
-  if (team < teams) {
-    x_begin = (int)((long long)n_units * team / teams);
-    x_end = (int)((long long)n_units * (team + 1) / teams);
-  }
-  const int nx = x_end - x_begin;
-  const int n_heads = (H - member + p.members - 1) / p.members;
-  const int n_tiles = nx * n_heads;
-
-  auto load_tile = [&](int i) {  // tile i of this warp: head by head, page by page
-    Tile s;
-    s.meta = s.t0 = s.page = 0;
-    if (i >= n_tiles) return s;
-    const int hd = n_heads == 1 ? 0 : i / nx, rem = i - hd * nx;
-    const int head = member + hd * p.members;
-    const int x = x_begin + rem;
-    const int b = seq_of_item(pre_s, p.g.batch, x);
-    const int k = x - pre_s[b], n_k = pre_s[b + 1] - pre_s[b];
-    const Q4Seq& q = seq_s[b];
-    int fl = 0, slot;
-    if (p.sel == nullptr) {
-      slot = k < q.ua ? k : q.ub0 + k - q.ua;
-      fl |= kTlLoad;
-    } else {
-      const int32_t* list = p.sel + ((size_t)b * H + head) * p.sel_stride;
-      slot = __ldcg(list + k);
-      const int before = k > 0 ? __ldcg(list + k - 1) : -1;
-      if (slot > before && (unsigned)slot < (unsigned)(q.n / kLqPage)) {
-        const int t0 = slot * kLqPage;
-        if (t0 < q.a || (t0 + kLqPage > q.lo && t0 < q.hi)) fl |= kTlLoad;
-      } else {
-        fl |= kTlBad;
-        slot = 0;
-      }
-    }
-    s.t0 = slot * kLqPage;
-    if (fl & kTlLoad) {
-      if (slot < p.g.max_pages_per_seq) s.page = p.g.block_table[(size_t)b * p.g.max_pages_per_seq + slot];
-      else s.page = -1;
-    }
-    if (rem == 0 || k == 0) fl |= kTlFirst;
-    if (rem + 1 == nx || k + 1 == n_k) fl |= kTlLast;
-    s.meta = fl | b << 5 | head << 14;
-    return s;
+  struct Tile {
+    int page;  // raw page id
+    int meta;  // kv head, or -1 where nothing is to be looked up
   };
-  // the pools' tile, -1 if nothing is to be copied; a page id outside the pools reads page 0 and is flagged
-  auto tile_of = [&](const Tile& s) {
-    if (s.meta & kTlBad) atomicOr(p.status, MC_FLAG_BAD_METADATA);
-    if (!(s.meta & kTlLoad)) return -1;
-    int page = s.page;
+  auto load_tile = [&](int i) {
+    Tile t;
+    t.page = 0;
+    t.meta = -1;
+    if (i >= n_tiles) return t;
+    const int hd = sh.n_heads == 1 ? 0 : i / nx, x = sh.x0 + i - hd * nx;
+    const int b = seq_of_item(pre.pages, p.g.batch, x), k = x - pre.pages[b];
+    t.meta = sh.member + hd * p.members;
+    int slot;
+    if (p.sel == nullptr) {
+      slot = q4_page_of(seq_s[b], k);
+    } else {
+      slot = __ldcg(p.sel + ((size_t)b * H + t.meta) * p.sel_stride + k);
+      if ((unsigned)slot >= (unsigned)(seq_s[b].n / kLqPage)) slot = -1;  // (flagged when its turn comes)
+    }
+    if (slot >= 0) t.page = slot < p.g.max_pages_per_seq ? p.g.block_table[(size_t)b * p.g.max_pages_per_seq + slot] : -1;
+    return t;
+  };
+  // the pools' tile; a page id outside the pools reads page 0 and is flagged
+  auto tile_of = [&](const Tile& t) {
+    if (t.meta < 0) return 0;
+    int page = t.page;
     if (!page_ok(p.g, page)) {
       atomicOr(p.status, MC_FLAG_BAD_METADATA);
       page = 0;
     }
-    return page * H + (s.meta >> 14);
+    return page * H + t.meta;
   };
-  Tile win = load_tile(lane), nxt = load_tile(32 + lane);
+  Tile first = load_tile(lane), ahead = load_tile(32 + lane);
   if (p.sel == nullptr) grid_dep_wait();
   if (bad && blockIdx.x == 0) atomicOr(p.status, MC_FLAG_BAD_METADATA);  // (every thread has looked at other sequences)
 
   const uint32_t bar0 = smem_u32(bars + warp * kLqStages);
   const uint32_t st0 = smem_u32(smem) + warp * kLqStages * kLqStageBytes;
-  int win_tile = tile_of(win), nxt_tile = -1;
-  auto issue = [&](int i, int s) {  // tile i into stage s
-    if (i >= n_tiles) return;
-    const int y = __shfl_sync(0xffffffffu, i >= 32 && (i & 31) < kLqStages - 1 ? nxt_tile : win_tile, i & 31);
-    if (y < 0 || *s_abort) return;
+  // Copies run kLqStages - 1 tiles ahead: tile j into stage j % kLqStages.  `tiles`: a lane per tile, 32 of them.
+  int tiles = tile_of(first);
+  int j = 0;
+  auto issue = [&](uint32_t st_j, uint32_t bar_j) {
+    if (j >= n_tiles) return;
+    if ((j & 31) == 0 && j > 0) {
+      tiles = tile_of(ahead);
+      ahead = load_tile(j + 32 + lane);
+    }
+    const int y = __shfl_sync(0xffffffffu, tiles, j & 31);
     if (lane == 0) {
-      const uint32_t bar = bar0 + 8 * s, dst = st0 + s * kLqStageBytes;
-      mbar_expect_tx(bar, (uint32_t)kLqStageBytes);
-      bulk_load(dst, p.k_codes + (size_t)y * kLqCodeBytes, kLqCodeBytes, bar);
-      tma_load_2d(dst + kLqKMeta, &map_km, 0, y * 4, bar);
-      tma_load_2d(dst + kLqVCodes, &map_vc, 0, y * kLqPage, bar);
-      bulk_load(dst + kLqVMeta, p.v_meta + (size_t)y * kLqMetaBytes, kLqMetaBytes, bar);
+      mbar_expect_tx(bar_j, (uint32_t)kLqStageBytes);
+      bulk_load(st_j, p.k_codes + (size_t)y * kLqCodeBytes, kLqCodeBytes, bar_j);
+      tma_load_2d(st_j + kLqKMeta, &map_km, 0, y * 4, bar_j);
+      tma_load_2d(st_j + kLqVCodes, &map_vc, 0, y * kLqPage, bar_j);
+      bulk_load(st_j + kLqVMeta, p.v_meta + (size_t)y * kLqMetaBytes, kLqMetaBytes, bar_j);
     }
+    ++j;
   };
-  for (int i = 0; i < kLqStages - 1; ++i) issue(i, i);
-
-  // Query pairs (channels 8w + i, 8w + i + 4 of the lane's 32), as binary16 with the row's power of two taken out: the row's
-  // largest number becomes 2 to 4.
-  uint32_t qh[16];
-  float q_back = 0.f;  // of the lane's column(s): WIDE: column 2 t4 ...
-  float q_back1 = 0.f; // ... and 2 t4 + 1
-  auto load_q = [&](int b, int head) {
-    const int h = WIDE ? row : row >> 1;
-    uint4 w[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      w[j] = make_uint4(0u, 0u, 0u, 0u);
-      if (h < nq) w[j] = *reinterpret_cast<const uint4*>(p.q + ((size_t)b * p.n_q_heads + head * nq + h) * kRowBytes + 64 * t4 + 16 * j);
-    }
-    float big = 0.f;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const uint32_t x[4] = {w[j].x, w[j].y, w[j].z, w[j].w};
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const float2 f = Elem<DT>::unpack(x[k]);
-        big = fmaxf(big, fmaxf(fabsf(f.x), fabsf(f.y)));
-      }
-    }
-    big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 1));
-    big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 2));
-    const int e = min(max(__float_as_int(big) >> 23, 2), 253);
-    const float f = __int_as_float((255 - e) << 23), back = __int_as_float((e - 1) << 23);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const uint32_t x[4] = {w[j].x, w[j].y, w[j].z, w[j].w};
-      uint32_t h2[4];
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const float2 v = Elem<DT>::unpack(x[k]);
-        h2[k] = Elem<MC_F16>::pack(v.x * f, v.y * f);
-      }
-      qh[4 * j] = lows(h2[0], h2[2]);
-      qh[4 * j + 1] = highs(h2[0], h2[2]);
-      qh[4 * j + 2] = lows(h2[1], h2[3]);
-      qh[4 * j + 3] = highs(h2[1], h2[3]);
-    }
-    // the lane's result columns are 2 t4 and 2 t4 + 1: rows 8 t4 .. of the lanes that hold those query rows
-    q_back = __shfl_sync(0xffffffffu, back, 8 * t4);
-    if (WIDE) q_back1 = __shfl_sync(0xffffffffu, back, 8 * t4 + 4);
-  };
-  {
-    const int meta = __shfl_sync(0xffffffffu, win.meta, 0);
-    if (n_tiles > 0) load_q((meta >> 5) & 511, meta >> 14);
+  for (int i = 0; i < kLqStages - 1; ++i) issue(st0 + i * kLqStageBytes, bar0 + 8 * i);
+  for (int k = sh.g0; k < sh.g1; ++k) {  // the begun pages of the warp's share
+    const int b = seq_of_item(pre.begun, p.g.batch, k);
+    for (int hd = 0; hd < sh.n_heads; ++hd) q4_begun_page<DT>(p, b, sh.member + hd * p.members);
   }
-  const uint32_t rest_mask = WIDE ? 0u : (row & 1) ? 0xffffffffu : 0u;  // this lane's column carries what the rounding left
 
-  float acc[8][4], zacc[4];
-  float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;  // of query head t4, or (WIDE) 2 t4 and 2 t4 + 1
-  float sl0 = 0.f, sl1 = 0.f;
-  int ve = 0;              // probabilities are kept times 2^ve
-  float scale_top = -1.f;  // the scale from which they no longer may be
-  Q4Seq sq = {};
-  uint32_t phase = 0;
-  int s = 0, s_next = kLqStages - 1;  // stage of this tile, and of the one to be copied
+  uint32_t st_i = st0, bar_i = bar0, parity = 0;
+  uint32_t st_free = st0 + (kLqStages - 1) * kLqStageBytes, bar_free = bar0 + 8 * (kLqStages - 1);  // the stage read last
+  uint32_t km_off[4];  // where the lane's 16-byte chunks of the keys' parameters are: chunk c ^ t4 of row t4
+#pragma unroll
+  for (int c = 0; c < 4; ++c) km_off[c] = kLqKMeta + 128 * t4 + ((c ^ t4) << 4);
+  const uint32_t k_off = row * 64 + 16 * t4;
+  const uint32_t vc_off = kLqVCodes + (lane & 7) * 64 + (((lane >> 3) ^ ((lane >> 1) & 3)) << 4);
+  const uint32_t vm_off = kLqVMeta + 32 * t4;
 
-  for (int i = 0; i < n_tiles; ++i) {
-    const int src = i & 31;
-    if (src == 0 && i > 0) {
-      win = nxt;
-      win_tile = nxt_tile;
-      nxt = load_tile((i & ~31) + 32 + lane);
-    }
-    if (src == 32 - kLqStages) nxt_tile = tile_of(nxt);
-    __syncwarp();  // (the stage of the tile before this one has been read)
-    issue(i + kLqStages - 1, s_next);
-    const int fl = __shfl_sync(0xffffffffu, win.meta, src);
-    const int b = (fl >> 5) & 511, head = fl >> 14;
-    const int t0 = __shfl_sync(0xffffffffu, win.t0, src);
-    if (fl & kTlFirst) {
-      m0 = m1 = -INFINITY;
-      l0 = l1 = 0.f;
-      scale_top = -1.f;
+  for (int hd = 0; hd < sh.n_heads; ++hd) {
+    const int head = sh.member + hd * p.members;
+    for (int x = sh.x0; x < sh.x1;) {
+      // ---- a piece: pages of one (sequence, kv head)
+      const int b = seq_of_item(pre.pages, p.g.batch, x);
+      const int k0 = x - pre.pages[b], k1 = min(sh.x1, pre.pages[b + 1]) - pre.pages[b];
+      x += k1 - k0;
+      const Q4Seq sq = seq_s[b];
+      const int32_t* list = p.sel ? p.sel + ((size_t)b * H + head) * p.sel_stride : nullptr;
+      const int ua = (min(sq.a, sq.n / kLqPage * kLqPage) + kLqPage - 1) / kLqPage, ub0 = max(sq.lo / kLqPage, ua);  // (as page_view has them)
+      int slot_next = list ? __ldcg(list + k0) : k0 < ua ? k0 : ub0 + k0 - ua;
+      int slot_last = list && k0 > 0 ? __ldcg(list + k0 - 1) : -1;
+
+      // Query pairs (channels 8w + i, 8w + i + 4 of the lane's 32), as binary16 with the row's power of two taken out: the
+      // row's largest number becomes 2 to 4.  q_back, of the lane's result column(s): what puts it back, and (without a
+      // cap) the scores' scale.
+      uint32_t qh[16];
+      float q_back, q_back1 = 0.f;
+      {
+        const int h = WIDE ? row : row >> 1;
+        uint4 w[4];
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
+        for (int c = 0; c < 4; ++c) {
+          w[c] = make_uint4(0u, 0u, 0u, 0u);
+          if (h < nq) w[c] = *reinterpret_cast<const uint4*>(p.q + ((size_t)b * p.n_q_heads + head * nq + h) * kRowBytes + 64 * t4 + 16 * c);
+        }
+        float big = 0.f;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) acc[j][k] = 0.f;
+        for (int c = 0; c < 4; ++c) {
+          const uint32_t y[4] = {w[c].x, w[c].y, w[c].z, w[c].w};
 #pragma unroll
-      for (int k = 0; k < 4; ++k) zacc[k] = 0.f;
-      sq = seq_s[b];
-      const uint32_t later = __ballot_sync(0xffffffffu, (win.meta & kTlFirst) != 0) & ~((2u << src) - 1u);
-      if (later) {  // the next piece's queries go to L1 meanwhile
-        const int mn = __shfl_sync(0xffffffffu, win.meta, __ffs(later) - 1);
-        if (lane < 2 * nq)
-          asm volatile("prefetch.global.L1 [%0];" ::"l"(p.q + (((size_t)((mn >> 5) & 511) * p.n_q_heads + (mn >> 14) * nq) * kRowBytes) + lane * 128));
+          for (int k = 0; k < 4; ++k) {
+            const float2 f = Elem<DT>::unpack(y[k]);
+            big = fmaxf(big, fmaxf(fabsf(f.x), fabsf(f.y)));
+          }
+        }
+        big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 1));
+        big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 2));
+        const int e = min(max(__float_as_int(big) >> 23, 2), 253);
+        const float f = __int_as_float((255 - e) << 23);
+        const float back = __int_as_float((e - 1) << 23) * (p.rule.cap_log2 > 0.f ? 1.f : p.rule.scale_log2);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const uint32_t y[4] = {w[c].x, w[c].y, w[c].z, w[c].w};
+          uint32_t h2[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const float2 v = Elem<DT>::unpack(y[k]);
+            h2[k] = Elem<MC_F16>::pack(v.x * f, v.y * f);
+          }
+          qh[4 * c] = lows(h2[0], h2[2]);
+          qh[4 * c + 1] = highs(h2[0], h2[2]);
+          qh[4 * c + 2] = lows(h2[1], h2[3]);
+          qh[4 * c + 3] = highs(h2[1], h2[3]);
+        }
+        // the lane's result columns are 2 t4 and 2 t4 + 1: rows 2 t4 and 2 t4 + 1 hold their queries
+        q_back = __shfl_sync(0xffffffffu, back, 8 * t4);
+        if (WIDE) q_back1 = __shfl_sync(0xffffffffu, back, 8 * t4 + 4);
       }
+      float sl0 = 0.f, sl1 = 0.f;
       if (p.rule.slopes) {
         const int h = WIDE ? 2 * t4 : t4;
         sl0 = h < nq ? p.rule.slopes[head * nq + h] * kLog2e : 0.f;
         if (WIDE) sl1 = p.rule.slopes[head * nq + h + 1] * kLog2e;
       }
-    }
-    if (fl & kTlLoad) {
-      const uint32_t sb = st0 + s * kLqStageBytes;
-      mbar_wait(bar0 + 8 * s, (phase >> s) & 1, s_abort, p.status);  // (on a time-out the CTA only runs to its end)
-      phase ^= 1u << s;
-      // ---- scores of 32 tokens: two tiles of 16
-      float dl[2][4] = {}, dh[2][4] = {}, dz[4] = {};  // low and high nibbles' sums, the zeros' (alike in every row)
-      {
-        uint4 x[2][2];  // [tile][token row, row + 8]: 32 channels
+      uint32_t qn[16];  // -q where the rounding is wanted, else 0 (a register each: a mask per product and page costs more)
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
+      for (int c = 0; c < 16; ++c) qn[c] = WIDE || (row & 1) ? qh[c] ^ 0x80008000u : 0u;
+      const bool unusual = p.rule.cap_log2 > 0.f || p.rule.slopes != nullptr;
+      float acc[8][4], zacc[4];
 #pragma unroll
-          for (int e = 0; e < 2; ++e) x[j][e] = lds16(sb + (16 * j + 8 * e + row) * 64 + 16 * t4);
+      for (int c = 0; c < 8; ++c)
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          const uint4 ma = lds16(sb + kLqKMeta + 128 * t4 + (((2 * w) ^ t4) << 4));
-          const uint4 mb = lds16(sb + kLqKMeta + 128 * t4 + (((2 * w + 1) ^ t4) << 4));
-          const uint32_t s4[4] = {lows(ma.x, mb.x), lows(ma.y, mb.y), lows(ma.z, mb.z), lows(ma.w, mb.w)};
-          const uint32_t z4[4] = {highs(ma.x, mb.x), highs(ma.y, mb.y), highs(ma.z, mb.z), highs(ma.w, mb.w)};
-          uint32_t bq[4], br[4];
+        for (int k = 0; k < 4; ++k) acc[c][k] = 0.f;
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const uint32_t r = h2_mul(qh[4 * w + k], s4[k]);
-            if (WIDE) {
-              bq[k] = r;
-              br[k] = h2_fms(qh[4 * w + k], s4[k], r);
-            } else {
-              bq[k] = h2_fms(qh[4 * w + k], s4[k], r & rest_mask);
+      for (int k = 0; k < 4; ++k) zacc[k] = 0.f;
+      float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;  // of query head t4, or (WIDE) 2 t4 and 2 t4 + 1
+      float ve = 0.f;          // probabilities are kept times 2^ve
+      uint32_t scale_top = 0;  // the scale (binary16, as an integer) from which they no longer may be
+
+      for (int k = k0; k < k1; ++k) {
+        __syncwarp();  // (the stage of the tile before this one has been read)
+        issue(st_free, bar_free);
+        int slot = slot_next;
+        if (list == nullptr) {
+          slot_next = k + 1 == ua ? ub0 : slot + 1;
+        } else {
+          if (k + 1 < k1) slot_next = __ldcg(list + k + 1);
+          const bool wrong = slot <= slot_last || slot < 0 || slot >= sq.n / kLqPage;
+          slot_last = slot;
+          if (wrong) {  // not above the one before it, or no complete page: nothing of it is seen
+            if (lane == 0) atomicOr(p.status, MC_FLAG_BAD_METADATA);
+            slot = -1;
+          }
+        }
+        const int t0 = slot * kLqPage;
+        const uint32_t sb = st_i;
+        mbar_wait_lean(bar_i, parity, s_abort, p.status);  // (on a time-out the CTA only runs to its end)
+        st_free = st_i;
+        bar_free = bar_i;
+        st_i += kLqStageBytes;
+        bar_i += 8;
+        if (st_i == st0 + kLqStages * kLqStageBytes) {
+          st_i = st0;
+          bar_i = bar0;
+          parity ^= 1u;
+        }
+        // ---- scores of 32 tokens: two tiles of 16
+        float dl[2][4], dh[2][4];  // low and high nibbles' sums
+        float dz[4] = {};                    // the zeros' sum of this lane's column and channels
+        {
+          uint4 c4[2][2];  // [tile][token row, row + 8]: 32 channels
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) c4[h][e] = lds16(sb + k_off + (16 * h + 8 * e) * 64);
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            const uint4 ma = lds16(sb + km_off[2 * (w & 1)] + 64 * (w >> 1)), mb = lds16(sb + km_off[2 * (w & 1) + 1] + 64 * (w >> 1));
+            const uint32_t s4[4] = {lows(ma.x, mb.x), lows(ma.y, mb.y), lows(ma.z, mb.z), lows(ma.w, mb.w)};
+            const uint32_t za[4] = {ma.x, ma.y, ma.z, ma.w}, zb[4] = {mb.x, mb.y, mb.z, mb.w};
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+              dz[c] = fma_lo_hi(qh[4 * w + c], za[c], dz[c]);
+              dz[c] = fma_hi_hi(qh[4 * w + c], zb[c], dz[c]);
+            }
+            uint32_t bq[4], br[4];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+              const uint32_t r = h2_mul(qn[4 * w + c], s4[c]);
+              if (WIDE) {
+                bq[c] = r ^ 0x80008000u;
+                br[c] = h2_fma(qh[4 * w + c], s4[c], r);
+              } else {
+                bq[c] = h2_fma(qh[4 * w + c], s4[c], r);  // the product, or it less its rounding
+              }
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const uint32_t c0 = w == 0 ? c4[h][0].x : w == 1 ? c4[h][0].y : w == 2 ? c4[h][0].z : c4[h][0].w;
+              const uint32_t c8 = w == 0 ? c4[h][1].x : w == 1 ? c4[h][1].y : w == 2 ? c4[h][1].z : c4[h][1].w;
+              const uint32_t u0 = c0 >> 8, u8 = c8 >> 8;
+              const uint32_t a0 = c0 & 0x000f000fu, a1 = c8 & 0x000f000fu, a2 = u0 & 0x000f000fu, a3 = u8 & 0x000f000fu;
+              const uint32_t h0 = c0 & 0x00f000f0u, h1 = c8 & 0x00f000f0u, h2 = u0 & 0x00f000f0u, h3 = u8 & 0x00f000f0u;
+              if (w == 0) {
+                mma_first(dl[h], a0, a1, a2, a3, bq[0], bq[2]);
+                mma_first(dh[h], h0, h1, h2, h3, bq[1], bq[3]);
+              } else {
+                mma_rows<MC_F16>(dl[h], a0, a1, a2, a3, bq[0], bq[2]);
+                mma_rows<MC_F16>(dh[h], h0, h1, h2, h3, bq[1], bq[3]);
+              }
+              if (WIDE) {
+                mma_rows<MC_F16>(dl[h], a0, a1, a2, a3, br[0], br[2]);
+                mma_rows<MC_F16>(dh[h], h0, h1, h2, h3, br[1], br[3]);
+              }
             }
           }
-          mma_rows<MC_F16>(dz, z4[0], z4[0], z4[1], z4[1], qh[4 * w], qh[4 * w + 1]);
-          mma_rows<MC_F16>(dz, z4[2], z4[2], z4[3], z4[3], qh[4 * w + 2], qh[4 * w + 3]);
-#pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            const uint32_t c0 = w == 0 ? x[j][0].x : w == 1 ? x[j][0].y : w == 2 ? x[j][0].z : x[j][0].w;
-            const uint32_t c8 = w == 0 ? x[j][1].x : w == 1 ? x[j][1].y : w == 2 ? x[j][1].z : x[j][1].w;
-            const uint32_t u0 = c0 >> 8, u8 = c8 >> 8;
-            const uint32_t a0 = c0 & 0x000f000fu, a1 = c8 & 0x000f000fu, a2 = u0 & 0x000f000fu, a3 = u8 & 0x000f000fu;
-            const uint32_t h0 = c0 & 0x00f000f0u, h1 = c8 & 0x00f000f0u, h2 = u0 & 0x00f000f0u, h3 = u8 & 0x00f000f0u;
-            mma_rows<MC_F16>(dl[j], a0, a1, a2, a3, bq[0], bq[2]);
-            mma_rows<MC_F16>(dh[j], h0, h1, h2, h3, bq[1], bq[3]);
-            if (WIDE) {
-              mma_rows<MC_F16>(dl[j], a0, a1, a2, a3, br[0], br[2]);
-              mma_rows<MC_F16>(dh[j], h0, h1, h2, h3, br[1], br[3]);
-            }
-          }
         }
-      }
-      // tokens t0 + 16 j + row and + 8; not WIDE: sc[2 j + e] of query head t4; WIDE: sa of head 2 t4, sc of 2 t4 + 1
-      float sc[4], sa[4];
+        // the zeros' sum over the lanes that share the column, then to the lanes that hold the column's results
+        float z0 = (dz[0] + dz[1]) + (dz[2] + dz[3]), z1 = 0.f;
+        z0 += __shfl_xor_sync(0xffffffffu, z0, 1);
+        z0 += __shfl_xor_sync(0xffffffffu, z0, 2);
+        if (WIDE) z1 = __shfl_sync(0xffffffffu, z0, 8 * t4 + 4);
+        z0 = __shfl_sync(0xffffffffu, z0, 8 * t4);
+        // tokens t0 + 16 h + row and + 8; not WIDE: sc[2 h + e] of query head t4; WIDE: sa of head 2 t4, sc of 2 t4 + 1
+        float sc[4], sa[4];
 #pragma unroll
-      for (int j = 0; j < 2; ++j)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          if (WIDE) {
-            sa[2 * j + e] = fmaf(dl[j][2 * e], 0x1p24f, fmaf(dh[j][2 * e], 0x1p20f, dz[0])) * q_back;
-            sc[2 * j + e] = fmaf(dl[j][2 * e + 1], 0x1p24f, fmaf(dh[j][2 * e + 1], 0x1p20f, dz[1])) * q_back1;
-          } else {
-            sc[2 * j + e] = fmaf(dl[j][2 * e] + dl[j][2 * e + 1], 0x1p24f, fmaf(dh[j][2 * e] + dh[j][2 * e + 1], 0x1p20f, dz[0])) * q_back;
-          }
-        }
-      // ---- masks, the scores' form, the distance bias
-      uint32_t hidden = 0;  // bit r: token t0 + r is not seen
-      const bool whole = t0 + kLqPage <= sq.a || (t0 >= sq.lo && t0 + kLqPage <= sq.hi);
-      bool ok[4] = {true, true, true, true};
-      if (!whole) {
-        const int t = t0 + lane;
-        hidden = ~__ballot_sync(0xffffffffu, t < sq.a || (t >= sq.lo && t < sq.hi));
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          ok[k] = !((hidden >> (8 * k + row)) & 1u);
-          if (!ok[k]) sc[k] = 0.f;  // (no say in which form of the cap the others take)
-          if (WIDE && !ok[k]) sa[k] = 0.f;
-        }
-      }
-      scores_of(p.rule, sc);
-      if (WIDE) scores_of(p.rule, sa);
-      if (p.rule.slopes) {
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const float dist = (float)(sq.q_pos - (t0 + 8 * k + row));
-          sc[k] = fmaf(WIDE ? -sl1 : -sl0, dist, sc[k]);
-          if (WIDE) sa[k] = fmaf(-sl0, dist, sa[k]);
-        }
-      }
-      if (!whole) {
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-          if (!ok[k]) {
-            sc[k] = -INFINITY;
-            if (WIDE) sa[k] = -INFINITY;
-          }
-        // a row that is not seen has parameters that may be anything: 0 times them has to stay 0
-        if ((hidden >> lane) & 1u)
-          asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(sb + kLqVMeta + 16 * lane), "r"(0u) : "memory");
-        __syncwarp();
-      }
-      // ---- the values' scales: four tokens of the lane per 16, four groups
-      uint32_t sv[2][2][4];  // [16 tokens][tokens 2 t4 .. + 1, 2 t4 + 8 ..][group]
-      uint32_t top = 0;
-#pragma unroll
-      for (int j = 0; j < 2; ++j)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const uint32_t at = sb + kLqVMeta + 16 * (16 * j + 8 * e + 2 * t4);
-          const uint4 u = lds16(at), w = lds16(at + 16);
-          sv[j][e][0] = lows(u.x, w.x);
-          sv[j][e][1] = lows(u.y, w.y);
-          sv[j][e][2] = lows(u.z, w.z);
-          sv[j][e][3] = lows(u.w, w.w);
-#pragma unroll
-          for (int g = 0; g < 4; ++g) top = h2_max(top, sv[j][e][g]);
-        }
-      const float lane_top = fmaxf(half_lo(top), half_hi(top));
-      // ---- running maximum, and the power of two of the probabilities
-      float n1 = max3(fmaxf(sc[0], sc[1]), sc[2], sc[3]), n0 = WIDE ? max3(fmaxf(sa[0], sa[1]), sa[2], sa[3]) : -INFINITY;
-      if (__any_sync(0xffffffffu, n1 > m1 || (WIDE && n0 > m0) || lane_top >= scale_top)) {
-#pragma unroll
-        for (int o = 4; o < 32; o <<= 1) {
-          n1 = fmaxf(n1, __shfl_xor_sync(0xffffffffu, n1, o));
-          if (WIDE) n0 = fmaxf(n0, __shfl_xor_sync(0xffffffffu, n0, o));
-        }
-        n1 = fmaxf(n1, m1);
-        n0 = fmaxf(n0, m0);
-        int ve_new = ve;
-        float f_e = 1.f;
-        if (__any_sync(0xffffffffu, lane_top >= scale_top)) {
-          float t = fmaxf(lane_top, __shfl_xor_sync(0xffffffffu, lane_top, 1));
-          t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 2));
-          const int ex = (__float_as_int(t) >> 23) - 126;  // t < 2^ex
-          ve_new = min(max(8 - ex, -8), 15);  // largest scale times 2^ve below 2^8: seven bits of room above it
-          f_e = scale_top < 0.f ? 1.f : ex2((float)(ve_new - ve));
-          scale_top = ve_new <= -1 ? INFINITY : ex2((float)(15 - ve_new));
-          ve = ve_new;
-        }
-        const float f1 = (n1 == m1 ? 1.f : ex2(m1 - n1)) * f_e, f0 = (n0 == m0 ? 1.f : ex2(m0 - n0)) * f_e;
-        m1 = n1;
-        m0 = n0;
-        l1 *= f1;
-        l0 *= f0;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          acc[j][0] *= WIDE ? f0 : f1;
-          acc[j][1] *= f1;
-          acc[j][2] *= WIDE ? f0 : f1;
-          acc[j][3] *= f1;
-        }
-        zacc[0] *= WIDE ? f0 : f1;
-        zacc[1] *= f1;
-        zacc[2] *= WIDE ? f0 : f1;
-        zacc[3] *= f1;
-      }
-      if (hidden != 0xffffffffu) {
-        const float b1 = m1 == -INFINITY ? 0.f : m1 - (float)ve, b0 = m0 == -INFINITY ? 0.f : m0 - (float)ve;
-        uint32_t pb[2][2];
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            const float y = ex2(sc[2 * j + e] - b1), x = WIDE ? ex2(sa[2 * j + e] - b0) : 0.f;
-            l1 += y;
-            if (WIDE) l0 += x;
-            pb[j][e] = transpose_8x8(WIDE ? Elem<MC_F16>::pack(x, y) : Elem<MC_F16>::pack(y, 0.f));
+            if (WIDE) {
+              sa[2 * h + e] = fmaf(dl[h][2 * e], 0x1p24f, fmaf(dh[h][2 * e], 0x1p20f, z0)) * q_back;
+              sc[2 * h + e] = fmaf(dl[h][2 * e + 1], 0x1p24f, fmaf(dh[h][2 * e + 1], 0x1p20f, z1)) * q_back1;
+            } else {
+              sc[2 * h + e] = fmaf(dl[h][2 * e] + dl[h][2 * e + 1], 0x1p24f, fmaf(dh[h][2 * e] + dh[h][2 * e + 1], 0x1p20f, z0)) * q_back;
+            }
           }
-        // ---- D[channel][query row] += codes^T (p scale), zeros^T p
+        // ---- masks, the scores' form, the distance bias
+        uint32_t hidden = 0;  // bit r: token t0 + r is not seen
+        const bool whole = (t0 + kLqPage <= sq.a || (t0 >= sq.lo && t0 + kLqPage <= sq.hi)) && slot >= 0;
+        if (!whole || unusual) {
+          if (!whole) {
+            const int t = t0 + lane;
+            hidden = ~__ballot_sync(0xffffffffu, slot >= 0 && (t < sq.a || (t >= sq.lo && t < sq.hi)));
+            if (p.rule.cap_log2 > 0.f) {  // (no say in which form of the cap the others take)
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const uint32_t zt = sb + kLqVMeta + 16 * (16 * j + 2 * t4) + 4 * (row & 3);  // rows of A: group row & 3
-          const uint32_t z0 = highs(lds4(zt), lds4(zt + 16)), z8 = highs(lds4(zt + 128), lds4(zt + 144));
-          mma_rows<MC_F16>(zacc, z0, z0, z8, z8, pb[j][0], pb[j][1]);
-          uint32_t r0[4], r8[4];
-          {
-            const int tr = 16 * j + (lane & 7), g = lane >> 3;
-            ldsm_x4_t(sb + kLqVCodes + tr * 64 + ((g ^ ((tr >> 1) & 3)) << 4), r0[0], r0[1], r0[2], r0[3]);
-            ldsm_x4_t(sb + kLqVCodes + (tr + 8) * 64 + ((g ^ ((tr >> 1) & 3)) << 4), r8[0], r8[1], r8[2], r8[3]);
+              for (int c = 0; c < 4; ++c)
+                if ((hidden >> (8 * c + row)) & 1u) sc[c] = sa[c] = 0.f;
+            }
           }
+          if (p.rule.cap_log2 > 0.f) {
+            scores_of(p.rule, sc);
+            if (WIDE) scores_of(p.rule, sa);
+          }
+          if (p.rule.slopes) {
 #pragma unroll
-          for (int g = 0; g < 4; ++g) {
-            const uint32_t b0g = h2_mul(pb[j][0], sv[j][0][g]), b8g = h2_mul(pb[j][1], sv[j][1][g]);
-            const uint32_t u0 = r0[g] >> 8, u8 = r8[g] >> 8;
-            mma_rows<MC_F16>(acc[2 * g], r0[g] & 0x000f000fu, r0[g] & 0x00f000f0u, r8[g] & 0x000f000fu, r8[g] & 0x00f000f0u, b0g, b8g);
-            mma_rows<MC_F16>(acc[2 * g + 1], u0 & 0x000f000fu, u0 & 0x00f000f0u, u8 & 0x000f000fu, u8 & 0x00f000f0u, b0g, b8g);
+            for (int c = 0; c < 4; ++c) {
+              const float dist = (float)(sq.q_pos - (t0 + 8 * c + row));
+              sc[c] = fmaf(WIDE ? -sl1 : -sl0, dist, sc[c]);
+              if (WIDE) sa[c] = fmaf(-sl0, dist, sa[c]);
+            }
+          }
+          if (!whole) {
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+              if ((hidden >> (8 * c + row)) & 1u) {
+                sc[c] = -INFINITY;
+                if (WIDE) sa[c] = -INFINITY;
+              }
+            // a row that is not seen has parameters that may be anything: 0 times them has to stay 0
+            if ((hidden >> lane) & 1u)
+              asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(sb + kLqVMeta + 16 * lane), "r"(0u) : "memory");
+            __syncwarp();
           }
         }
+        // ---- the values' scales: four tokens of the lane per 16, four groups; their zeros (odd rows of a transposed read)
+        uint32_t sv[2][2][4];  // [16 tokens][tokens 2 t4 .. + 1, 2 t4 + 8 ..][group]
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const uint4 u = lds16(sb + vm_off + 16 * (16 * h + 8 * e)), w = lds16(sb + vm_off + 16 * (16 * h + 8 * e) + 16);
+            sv[h][e][0] = lows(u.x, w.x);
+            sv[h][e][1] = lows(u.y, w.y);
+            sv[h][e][2] = lows(u.z, w.z);
+            sv[h][e][3] = lows(u.w, w.w);
+          }
+        uint32_t zt[4];
+        ldsm_x4_t(sb + kLqVMeta + 16 * lane, zt[0], zt[1], zt[2], zt[3]);
+        uint32_t lane_top;  // the largest scale of token `lane`
+        {
+          const uint4 u = lds16(sb + kLqVMeta + 16 * lane);
+          lane_top = h2_max(h2_max(u.x, u.y), h2_max(u.z, u.w)) & 0x7fffu;
+        }
+        // ---- running maximum, and the power of two of the probabilities
+        float n1 = max3(fmaxf(sc[0], sc[1]), sc[2], sc[3]), n0 = WIDE ? max3(fmaxf(sa[0], sa[1]), sa[2], sa[3]) : -INFINITY;
+        if (__any_sync(0xffffffffu, n1 > m1 || (WIDE && n0 > m0) || lane_top >= scale_top)) {
+#pragma unroll
+          for (int o = 4; o < 32; o <<= 1) {
+            n1 = fmaxf(n1, __shfl_xor_sync(0xffffffffu, n1, o));
+            if (WIDE) n0 = fmaxf(n0, __shfl_xor_sync(0xffffffffu, n0, o));
+          }
+          n1 = fmaxf(n1, m1);
+          n0 = fmaxf(n0, m0);
+          float f_e = 1.f;
+          if (__any_sync(0xffffffffu, lane_top >= scale_top)) {
+            const uint32_t t = __reduce_max_sync(0xffffffffu, lane_top);
+            const int ex = (int)(t >> 10) - 14;                      // the largest scale is below 2^ex
+            const int e = min(max(8 - ex, -8), 15);                  // times 2^e it is below 2^8: seven bits of room above it
+            f_e = scale_top == 0 ? 1.f : ex2((float)e - ve);
+            scale_top = e < 0 ? 0x8000u : (uint32_t)(30 - e) << 10;  // 2^(15 - e); below e = 0 no scale is too large
+            ve = (float)e;
+          }
+          const float f1 = (n1 == m1 ? 1.f : ex2(m1 - n1)) * f_e, f0 = (n0 == m0 ? 1.f : ex2(m0 - n0)) * f_e;
+          m1 = n1;
+          m0 = n0;
+          l1 *= f1;
+          l0 *= f0;
+#pragma unroll
+          for (int c = 0; c < 8; ++c) {
+            acc[c][0] *= WIDE ? f0 : f1;
+            acc[c][2] *= WIDE ? f0 : f1;
+            if (WIDE) {
+              acc[c][1] *= f1;
+              acc[c][3] *= f1;
+            }
+          }
+          zacc[0] *= WIDE ? f0 : f1;
+          if (WIDE) zacc[1] *= f1;
+        }
+        if (hidden != 0xffffffffu) {
+          const float b1 = m1 == -INFINITY ? 0.f : m1 - ve, b0 = m0 == -INFINITY ? 0.f : m0 - ve;
+          uint32_t pb[2][2];
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const float y = ex2(sc[2 * h + e] - b1), x2 = WIDE ? ex2(sa[2 * h + e] - b0) : 0.f;
+              l1 += y;
+              if (WIDE) l0 += x2;
+              pb[h][e] = transpose_8x8(WIDE ? Elem<MC_F16>::pack(x2, y) : Elem<MC_F16>::pack(y, 0.f));
+            }
+          // ---- D[channel][query row] += codes^T (p scale), zeros^T p
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            mma_rows<MC_F16>(zacc, zt[2 * h], zt[2 * h], zt[2 * h + 1], zt[2 * h + 1], pb[h][0], pb[h][1]);
+            uint32_t r0[4], r8[4];
+            ldsm_x4_t(sb + vc_off + 16 * h * 64, r0[0], r0[1], r0[2], r0[3]);
+            ldsm_x4_t(sb + vc_off + (16 * h + 8) * 64, r8[0], r8[1], r8[2], r8[3]);
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+              const uint32_t b0g = h2_mul(pb[h][0], sv[h][0][g]), b8g = h2_mul(pb[h][1], sv[h][1][g]);
+              // rows 0..7 of A: a byte, low nibble + 16 high nibble, rows 8..15: 16 high nibble; the difference is taken at the end
+              const uint32_t y0 = r0[g] & 0x00ff00ffu, y8 = r8[g] & 0x00ff00ffu;
+              const uint32_t w0 = __byte_perm(r0[g], 0, 0x4341), w8 = __byte_perm(r8[g], 0, 0x4341);
+              mma_rows<MC_F16>(acc[2 * g], y0, r0[g] & 0x00f000f0u, y8, r8[g] & 0x00f000f0u, b0g, b8g);
+              mma_rows<MC_F16>(acc[2 * g + 1], w0, w0 & 0x00f000f0u, w8, w8 & 0x00f000f0u, b0g, b8g);
+            }
+          }
+        }
+        if (!whole) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       }
-      if (!whole) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-    }
-    if (fl & kTlLast) {
-      if (i + 1 < n_tiles) {
-        const int mn = __shfl_sync(0xffffffffu, src == 31 ? nxt.meta : win.meta, (i + 1) & 31);
-        load_q((mn >> 5) & 511, mn >> 14);
-      }
+
+      // ---- the piece's result
 #pragma unroll
       for (int o = 4; o < 32; o <<= 1) {
         l1 += __shfl_xor_sync(0xffffffffu, l1, o);
         if (WIDE) l0 += __shfl_xor_sync(0xffffffffu, l0, o);
       }
-      const size_t prow = (size_t)(team + b) * p.n_q_heads + head * nq;
+      const size_t prow = (size_t)(sh.team + b) * p.n_q_heads + head * nq;
 #pragma unroll
       for (int e = 0; e < (WIDE ? 2 : 1); ++e) {
         const int r = WIDE ? 2 * t4 + e : t4;
         float z[4];
 #pragma unroll
-        for (int g = 0; g < 4; ++g) z[g] = __shfl_sync(0xffffffffu, zacc[e], 4 * g + t4);
+        for (int g = 0; g < 4; ++g) z[g] = __shfl_sync(0xffffffffu, zacc[e], 4 * (2 * g + 1) + t4);
         if (r >= nq) continue;
         const float m = WIDE && e == 0 ? m0 : m1, l = WIDE && e == 0 ? l0 : l1;
 #pragma unroll
         for (int g = 0; g < 4; ++g)
           *reinterpret_cast<float4*>(p.part_o + (prow + r) * kHeadDim + 32 * g + 4 * row) =
-              make_float4(fmaf(acc[2 * g][e], 0x1p24f, z[g]), fmaf(acc[2 * g][2 + e], 0x1p20f, z[g]),
-                          fmaf(acc[2 * g + 1][e], 0x1p24f, z[g]), fmaf(acc[2 * g + 1][2 + e], 0x1p20f, z[g]));
-        if (row == 0) *reinterpret_cast<float2*>(p.part_ml + 2 * (prow + r)) = make_float2(m - (float)ve, l);
+              make_float4(fmaf(acc[2 * g][e] - acc[2 * g][2 + e], 0x1p24f, z[g]), fmaf(acc[2 * g][2 + e], 0x1p20f, z[g]),
+                          fmaf(acc[2 * g + 1][e] - acc[2 * g + 1][2 + e], 0x1p24f, z[g]), fmaf(acc[2 * g + 1][2 + e], 0x1p20f, z[g]));
+        if (row == 0) *reinterpret_cast<float2*>(p.part_ml + 2 * (prow + r)) = make_float2(m - ve, l);
       }
     }
-    s = s + 1 == kLqStages ? 0 : s + 1;
-    s_next = s_next + 1 == kLqStages ? 0 : s_next + 1;
   }
   if (*s_abort) {  // let copies in flight land before the CTA's memory is released
     for (int k = 0; k < 2000; ++k) __nanosleep(1000);
@@ -711,21 +773,24 @@ constexpr int kLqCombWarps = kLqCombThreads / 32;
 template <int DT, int R>
 __global__ void __launch_bounds__(kLqCombThreads) layer_q4_combine_kernel(const __grid_constant__ LayerQ4Params p) {
   grid_dep_launch();
-  __shared__ int pre_s[kMaxLayerBatch + 1];
+  __shared__ int pre_s[2 * (kMaxLayerBatch + 1)];
   __shared__ float4 acc_s[kLqCombWarps][32];
   __shared__ float l_s[kLqCombWarps], m_s[kLqCombWarps];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int b = blockIdx.y;
   if (p.sel != nullptr) grid_dep_wait();
+  const Q4Prefix pre = q4_prefix_at(pre_s, p.g.batch);
   int bad = 0;
   for (int i = tid; i < p.g.batch; i += kLqCombThreads) {
     PageView v;
-    pre_s[i + 1] = q4_units(p, i, v, bad);
+    int begun;
+    pre.pages[i + 1] = q4_units(p, i, v, begun, bad);
+    pre.begun[i + 1] = begun;
   }
-  scan_counts(pre_s, p.g.batch);
-  const long long U = pre_s[p.g.batch];
+  q4_scan(pre, p.g.batch);
+  const long long U = q4_total(pre, p.g.batch);
   const int T = q4_live_teams(p, (int)U);
-  const int x0 = pre_s[b], u = pre_s[b + 1] - x0;
+  const int x0 = pre.pages[b], u = pre.pages[b + 1] - x0, begun = pre.begun[b + 1] - pre.begun[b];
   // the team of unit x is the last c with floor(U c / T) <= x
   const int c0 = u > 0 ? (int)(((long long)(x0 + 1) * T - 1) / U) : 0;
   const int c1 = u > 0 ? (int)(((long long)(x0 + u) * T - 1) / U) : -1;
@@ -737,7 +802,7 @@ __global__ void __launch_bounds__(kLqCombThreads) layer_q4_combine_kernel(const 
   float M = -INFINITY, L = 0.f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
   if (active) {
-    const int n_parts = c1 - c0 + 2;  // the last one: the 16-bit rows'
+    const int n_pages = c1 - c0 + 1, n_parts = n_pages + begun;
     for (int c = grp; c < n_parts; c += 4 * GP) {  // four parts in flight
       float2 ml[4];
       float4 v[4];
@@ -747,7 +812,7 @@ __global__ void __launch_bounds__(kLqCombThreads) layer_q4_combine_kernel(const 
         v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
         const int j = c + k * GP;
         if (j < n_parts) {
-          const size_t prow = j + 1 < n_parts ? (size_t)(c0 + j + b) * p.n_q_heads + hq : (size_t)p.res_part + (size_t)b * p.n_q_heads + hq;
+          const size_t prow = j < n_pages ? (size_t)(c0 + j + b) * p.n_q_heads + hq : (size_t)p.res_part + (size_t)b * p.n_q_heads + hq;
           ml[k] = *reinterpret_cast<const float2*>(p.part_ml + 2 * prow);
           v[k] = *reinterpret_cast<const float4*>(p.part_o + prow * kHeadDim + 4 * lane);
         }
@@ -825,7 +890,7 @@ static LayerQ4Plan layer_q4_plan(const mc_config* cfg, const mc_batch* bt, int c
   const int warps = std::min(ctas, kLqMaxCtas) * kLqWarps;
   const int per_warp = (cfg->n_kv_heads + warps - 1) / warps;  // heads
   pl.members = (cfg->n_kv_heads + per_warp - 1) / per_warp;
-  pl.max_units = std::max<long long>((long long)bt->batch * (bt->max_seq_len / kLqPage), 1);
+  pl.max_units = (long long)bt->batch * (bt->max_seq_len / kLqPage + kLqBegunUnits);
   pl.n_teams = (int)std::max<long long>(1, std::min<long long>(warps / pl.members, pl.max_units));
   pl.rows = (size_t)(pl.n_teams + bt->batch) * cfg->n_q_heads + (size_t)bt->batch * cfg->n_q_heads;
   pl.o_bytes = align_up(pl.rows * kHeadDim * 4, 256);
@@ -833,7 +898,7 @@ static LayerQ4Plan layer_q4_plan(const mc_config* cfg, const mc_batch* bt, int c
   return pl;
 }
 static constexpr size_t q4_smem_bytes(int batch) {
-  return 1024 + (size_t)kLqWarps * kLqStages * (kLqStageBytes + 8) + (size_t)(batch + 2) * (4 + sizeof(Q4Seq));
+  return 1024 + (size_t)kLqWarps * kLqStages * (kLqStageBytes + 8) + (size_t)(batch + 2) * (8 + sizeof(Q4Seq));
 }
 static_assert(q4_smem_bytes(kMaxLayerBatch) <= 227 * 1024, "a CTA's shared memory");
 
@@ -887,7 +952,7 @@ mc_status launch_layer_q4_attn(const mc_config* cfg, const mc_batch* bt, const G
   auto* split = cfg->dtype == MC_F16 ? (wide ? layer_q4_split_kernel<MC_F16, true> : layer_q4_split_kernel<MC_F16, false>)
                                      : (wide ? layer_q4_split_kernel<MC_BF16, true> : layer_q4_split_kernel<MC_BF16, false>);
   MC_CUDA_CHECK(allow_smem(split, q4_smem_bytes(kMaxLayerBatch)));
-  const int grid = std::max((pl.n_teams * pl.members + kLqWarps - 1) / kLqWarps, std::min(ctas, bt->batch * cfg->n_kv_heads));
+  const int grid = (pl.n_teams * pl.members + kLqWarps - 1) / kLqWarps;
   MC_CUDA_CHECK(launch_pdl(split, dim3(grid), dim3(kLqThreads), q4_smem_bytes(bt->batch), stream, ap, map_km, map_vc));
   // warps per output row: about three parts each
   const long long parts = pl.n_teams / bt->batch + 2;
