@@ -99,7 +99,7 @@ __device__ __forceinline__ int lq_code(float x, float z, float s, float inv_s) {
 }
 // (scale, zero) of a group from its extremes, in one word as the pools hold it: scale = half((hi - lo) / 15).
 __device__ __forceinline__ uint32_t lq_group(float lo, float hi) {
-  const float d = hi - lo;
+  const float d = fabsf(hi - lo);  // (-0 where the largest came as -0)
   uint32_t s = __half_as_ushort(__float2half_rd(d * (1.0f / 15.0f)));  // the number below (or one too low, next to a number)
   const float a = __half2float(__ushort_as_half((unsigned short)s)), b = __half2float(__ushort_as_half((unsigned short)(s + 1)));
   const float rest = fmaf(-7.5f, a + b, d) + diff_error(hi, lo, d);  // against 15 times the middle
@@ -110,14 +110,19 @@ __device__ __forceinline__ uint32_t lq_group(float lo, float hi) {
 }
 __device__ __forceinline__ float half_lo(uint32_t w) { return __half2float(__ushort_as_half((unsigned short)(w & 0xffffu))); }
 __device__ __forceinline__ float half_hi(uint32_t w) { return __half2float(__ushort_as_half((unsigned short)(w >> 16))); }
-__device__ __forceinline__ float min_nan(float a, float b) {
-  float r;
-  asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+// Element by element of a pair of 16-bit numbers, a NaN if either is one.
+template <int DT>
+__device__ __forceinline__ uint32_t min2_nan(uint32_t a, uint32_t b) {
+  uint32_t r;
+  if (DT == MC_F16) asm("min.NaN.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  else asm("min.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
   return r;
 }
-__device__ __forceinline__ float max_nan(float a, float b) {
-  float r;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+template <int DT>
+__device__ __forceinline__ uint32_t max2_nan(uint32_t a, uint32_t b) {
+  uint32_t r;
+  if (DT == MC_F16) asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  else asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
   return r;
 }
 // What a page takes in: what binary16 can hold (the largest bfloat16 below 65504 is 65280), a NaN as 0.
@@ -127,123 +132,174 @@ __device__ __forceinline__ float lq_tame(float x) {
   return x != x ? 0.f : fminf(fmaxf(x, -most), most);
 }
 template <int DT>
-__device__ __forceinline__ void lq_tame_words(uint2 (&r)[kLqPage]) {
-#pragma unroll
-  for (int t = 0; t < kLqPage; ++t) {
-    asm volatile("" : "+r"(r[t].x), "+r"(r[t].y));  // (row by row: see `four` below)
-    const float2 a = Elem<DT>::unpack(r[t].x), b = Elem<DT>::unpack(r[t].y);
-    r[t].x = Elem<DT>::pack(lq_tame<DT>(a.x), lq_tame<DT>(a.y));
-    r[t].y = Elem<DT>::pack(lq_tame<DT>(b.x), lq_tame<DT>(b.y));
-  }
+__device__ __forceinline__ uint2 lq_tame(const uint2& r) {
+  const float2 a = Elem<DT>::unpack(r.x), b = Elem<DT>::unpack(r.y);
+  return make_uint2(Elem<DT>::pack(lq_tame<DT>(a.x), lq_tame<DT>(a.y)), Elem<DT>::pack(lq_tame<DT>(b.x), lq_tame<DT>(b.y)));
 }
-
-// (in program order: a row's codes leave before the next row's are worked out)
-__device__ __forceinline__ void st_code(unsigned short* p, uint32_t c) {
-  asm volatile("st.global.u16 [%0], %1;" ::"l"(p), "h"((unsigned short)c) : "memory");
-}
-
-// One (page, kv head) of K or V by a warp: lane l holds channels 4l .. 4l + 3 of the page's 32 rows.
-// K: a group is one of the lane's channels, so nothing is exchanged.  V: a group is a row's part in eight lanes; eight
-// rows' extremes are joined at a time, halving the rows a lane keeps at every step (7 exchanges instead of 24), so that lane
-// j of the eight ends with row j's group, forms its parameters once and hands them round.
+// Two numbers of a word less z: for binary16 one mixed-precision FMA each.
 template <int DT>
-__device__ __forceinline__ void lq_quantise(bool keys, uint2 (&r)[kLqPage], unsigned char* codes, unsigned char* meta) {
+__device__ __forceinline__ float2 minus(uint32_t w, float zx, float zy) {
+  if (DT == MC_F16) {
+    float2 r;
+    asm("{\n\t.reg .b16 lo, hi, one;\n\tmov.b32 {lo, hi}, %2;\n\tmov.b16 one, 0x3C00;\n\t"
+        "fma.rn.f32.f16 %0, lo, one, %3;\n\tfma.rn.f32.f16 %1, hi, one, %4;\n\t}"
+        : "=f"(r.x), "=f"(r.y)
+        : "r"(w), "f"(-zx), "f"(-zy));
+    return r;
+  }
+  const float2 v = Elem<DT>::unpack(w);
+  return make_float2(v.x - zx, v.y - zy);
+}
+__device__ __forceinline__ float rcp_approx(float x) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+// Four codes, channel 4l + j at bits 4j, of differences d with scales' reciprocals inv, for quotients between 0 and 15.01; `tie`: one
+// of them is next to a tie (they are at most 15 * 3 * 2^-24 off).
+__device__ __forceinline__ uint32_t lq_codes(const float (&d)[4], const float (&inv)[4], bool& tie) {
+  float r[4], e[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    r[j] = fmaf(d[j], inv[j], 12582912.0f) - 12582912.0f;  // 1.5 * 2^23: the nearest integer
+    e[j] = fmaf(d[j], inv[j], -r[j]);
+  }
+  tie = max3_abs(fmaxf(fabsf(e[0]), fabsf(e[1])), e[2], e[3]) > 0.49999f;
+  return (uint32_t)__float_as_int(fmaf(fmaf(r[3], 16.f, r[2]), 256.f, fmaf(r[1], 16.f, r[0])) + 12582912.0f) & 0xffffu;
+}
+template <int DT>
+__device__ __forceinline__ uint32_t lq_codes_exact(const uint2& r, const float (&z)[4], const float (&s)[4]) {
+  const float2 a = Elem<DT>::unpack(r.x), b = Elem<DT>::unpack(r.y);
+  const float x[4] = {a.x, a.y, b.x, b.y};
+  uint32_t c = 0;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) c |= (uint32_t)lq_code(x[j], z[j], s[j], 1.0f / s[j]) << (4 * j);
+  return c;
+}
+// A group whose quotients may leave [0, 15.01]: a scale that is subnormal (coarse), a zero that is not the minimum itself.
+__device__ __forceinline__ bool lq_odd(uint32_t group, float lo) { return (group & 0x7fffu) < 0x0400u || half_hi(group) != lo; }
+
+// One (page, kv head) of K or V by a warp: lane l has channels 4l .. 4l + 3 of the page's 32 rows, load(t) gives those of row t.
+// False (nothing stored that counts): something in it is not a number that binary16 holds, and it has to be done again with WILD.
+// Loops that are not unrolled over registers: 16 KB of straight code per tensor made the instruction cache the limit (8 x 4096
+// prompts of 32 heads 606 us).
+// K: a group is one of the lane's channels, so nothing is exchanged.
+template <int DT, bool WILD, typename Load>
+__device__ __forceinline__ bool lq_quantise_keys(Load load, unsigned char* codes, unsigned char* meta) {
   const int lane = threadIdx.x & 31;
-  const float inf = __int_as_float(0x7f800000);
-  // (the words pass through an empty statement every time: the compiler would keep all 128 numbers of the first pass, in
-  // local memory, for the second)
-  auto four = [&](int t, float (&x)[4]) {
-    asm volatile("" : "+r"(r[t].x), "+r"(r[t].y));
-    const float2 a = Elem<DT>::unpack(r[t].x), b = Elem<DT>::unpack(r[t].y);
-    x[0] = a.x;
-    x[1] = a.y;
-    x[2] = b.x;
-    x[3] = b.y;
-  };
-  float lo[4], hi[4];
-#pragma unroll 1
-  for (int again = 0; again < 2; ++again) {
-    if (again) lq_tame_words<DT>(r);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      lo[j] = inf;
-      hi[j] = -inf;
-    }
-#pragma unroll
-    for (int t = 0; t < kLqPage; ++t) {
-      float x[4];
-      four(t, x);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        lo[j] = min_nan(lo[j], x[j]);
-        hi[j] = max_nan(hi[j], x[j]);
-      }
-    }
+  auto get = [&](int t) { return WILD ? lq_tame<DT>(load(t)) : load(t); };
+  uint2 lo2 = get(0), hi2 = lo2;
+#pragma unroll 8
+  for (int t = 1; t < kLqPage; ++t) {
+    const uint2 r = get(t);
+    lo2.x = min2_nan<DT>(lo2.x, r.x);
+    lo2.y = min2_nan<DT>(lo2.y, r.y);
+    hi2.x = max2_nan<DT>(hi2.x, r.x);
+    hi2.y = max2_nan<DT>(hi2.y, r.y);
+  }
+  const float2 la = Elem<DT>::unpack(lo2.x), lb = Elem<DT>::unpack(lo2.y), ha = Elem<DT>::unpack(hi2.x), hb = Elem<DT>::unpack(hi2.y);
+  const float lo[4] = {la.x, la.y, lb.x, lb.y}, hi[4] = {ha.x, ha.y, hb.x, hb.y};
+  if (!WILD) {
     bool tame = true;
 #pragma unroll
     for (int j = 0; j < 4; ++j) tame = tame && lo[j] >= -65504.f && hi[j] <= 65504.f;  // (false for a NaN)
-    if (__all_sync(0xffffffffu, tame)) break;
+    if (!__all_sync(0xffffffffu, tame)) return false;
   }
+  uint32_t w[4];
+  float z[4], s[4], inv[4];
+  bool odd = false;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    w[j] = lq_group(lo[j], hi[j]);
+    s[j] = half_lo(w[j]);
+    z[j] = half_hi(w[j]);
+    inv[j] = rcp_approx(s[j]);
+    odd = odd || lq_odd(w[j], lo[j]);
+  }
+  *reinterpret_cast<uint4*>(meta + 16 * lane) = make_uint4(w[0], w[1], w[2], w[3]);
   unsigned short* out = reinterpret_cast<unsigned short*>(codes) + lane;
+  uint32_t again = 0;  // rows with a quotient next to a tie
+#pragma unroll 4
+  for (int t = 0; t < kLqPage; ++t) {
+    const uint2 r = get(t);
+    const float2 a = minus<DT>(r.x, z[0], z[1]), b = minus<DT>(r.y, z[2], z[3]);
+    const float d[4] = {a.x, a.y, b.x, b.y};
+    bool tie;
+    out[32 * t] = (unsigned short)lq_codes(d, inv, tie);
+    if (tie) again |= 1u << t;
+  }
+  again = __any_sync(0xffffffffu, odd) ? 0xffffffffu : __reduce_or_sync(0xffffffffu, again);
+#pragma unroll 1
+  while (again != 0) {
+    const int t = __ffs(again) - 1;
+    again &= again - 1;
+    out[32 * t] = (unsigned short)lq_codes_exact<DT>(get(t), z, s);
+  }
+  return true;
+}
+// V: a group is a row's part in eight lanes.  Eight rows' extremes (the least and the negative of the largest, a pair) are joined
+// at a time, halving the rows a lane keeps at every step (7 exchanges instead of 24); lane j of the eight ends with row j's
+// group, forms its parameters once and hands them round.
+template <int DT, bool WILD, typename Load>
+__device__ __forceinline__ bool lq_quantise_values(Load load, unsigned char* codes, unsigned char* meta) {
+  const int lane = threadIdx.x & 31, j8 = lane & 7;
+  auto get = [&](int t) { return WILD ? lq_tame<DT>(load(t)) : load(t); };
+  unsigned short* out = reinterpret_cast<unsigned short*>(codes) + lane;
+#pragma unroll 1
+  for (int t0 = 0; t0 < kLqPage; t0 += 8) {
+    uint2 r[8];
+    uint32_t v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      r[i] = get(t0 + i);
+      const uint32_t mn = min2_nan<DT>(r[i].x, r[i].y), mx = max2_nan<DT>(r[i].x, r[i].y) ^ 0x80008000u;
+      v[i] = min2_nan<DT>(__byte_perm(mn, mx, 0x5410), __byte_perm(mn, mx, 0x7632));
+    }
+#pragma unroll
+    for (int o = 4, m = 4; o > 0; o >>= 1, m >>= 1) {  // m rows stay: those whose bit o is the lane's
+      const bool up = (lane & o) != 0;
+#pragma unroll
+      for (int i = 0; i < m; ++i) {
+        const uint32_t give = up ? v[i] : v[i + m], keep = up ? v[i + m] : v[i];
+        v[i] = min2_nan<DT>(keep, __shfl_xor_sync(0xffffffffu, give, o));
+      }
+    }
+    const float2 mm = Elem<DT>::unpack(v[0]);
+    const float lo = mm.x, hi = -mm.y;
+    if (!WILD && !__all_sync(0xffffffffu, lo >= -65504.f && hi <= 65504.f)) return false;
+    const uint32_t own = lq_group(lo, hi);
+    const float own_inv = rcp_approx(half_lo(own));
+    *reinterpret_cast<uint32_t*>(meta + 16 * (t0 + j8) + 4 * (lane >> 3)) = own;
+    uint32_t again = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t w = __shfl_sync(0xffffffffu, own, (lane & 24) + i);
+      const float f = __shfl_sync(0xffffffffu, own_inv, (lane & 24) + i), z = half_hi(w);
+      const float2 a = minus<DT>(r[i].x, z, z), b = minus<DT>(r[i].y, z, z);
+      const float d[4] = {a.x, a.y, b.x, b.y}, inv[4] = {f, f, f, f};
+      bool tie;
+      out[32 * (t0 + i)] = (unsigned short)lq_codes(d, inv, tie);
+      if (tie) again |= 1u << i;
+    }
+    again = __any_sync(0xffffffffu, lq_odd(own, lo)) ? 0xffu : __reduce_or_sync(0xffffffffu, again);
+#pragma unroll 1
+    while (again != 0) {
+      const int i = __ffs(again) - 1;
+      again &= again - 1;
+      const uint32_t w = __shfl_sync(0xffffffffu, own, (lane & 24) + i);
+      const float s = half_lo(w), z = half_hi(w);
+      const float s4[4] = {s, s, s, s}, z4[4] = {z, z, z, z};
+      out[32 * (t0 + i)] = (unsigned short)lq_codes_exact<DT>(get(t0 + i), z4, s4);
+    }
+  }
+  return true;
+}
+template <int DT, typename Load>
+__device__ __forceinline__ void lq_quantise(bool keys, Load load, unsigned char* codes, unsigned char* meta) {
   if (keys) {
-    uint32_t w[4];
-    float z[4], s[4], inv[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      w[j] = lq_group(lo[j], hi[j]);
-      s[j] = half_lo(w[j]);
-      z[j] = half_hi(w[j]);
-      inv[j] = 1.0f / s[j];
-    }
-    *reinterpret_cast<uint4*>(meta + 16 * lane) = make_uint4(w[0], w[1], w[2], w[3]);
-#pragma unroll
-    for (int t = 0; t < kLqPage; ++t) {
-      float x[4];
-      four(t, x);
-      uint32_t c = 0;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) c |= (uint32_t)lq_code(x[j], z[j], s[j], inv[j]) << (4 * j);
-      st_code(out + 32 * t, c);
-    }
+    if (!lq_quantise_keys<DT, false>(load, codes, meta)) lq_quantise_keys<DT, true>(load, codes, meta);
   } else {
-    const int j8 = lane & 7;
-#pragma unroll
-    for (int t0 = 0; t0 < kLqPage; t0 += 8) {
-      float a[8], b[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        float x[4];
-        four(t0 + i, x);
-        a[i] = fminf(fminf(x[0], x[1]), fminf(x[2], x[3]));
-        b[i] = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
-      }
-#pragma unroll
-      for (int o = 4, m = 4; o > 0; o >>= 1, m >>= 1) {  // m rows stay: those whose bit o is the lane's
-        const bool up = (lane & o) != 0;
-#pragma unroll
-        for (int i = 0; i < m; ++i) {
-          const float ga = up ? a[i] : a[i + m], gb = up ? b[i] : b[i + m];
-          const float ka = up ? a[i + m] : a[i], kb = up ? b[i + m] : b[i];
-          a[i] = fminf(ka, __shfl_xor_sync(0xffffffffu, ga, o));
-          b[i] = fmaxf(kb, __shfl_xor_sync(0xffffffffu, gb, o));
-        }
-      }
-      const uint32_t own = lq_group(a[0], b[0]);
-      const float own_inv = 1.0f / half_lo(own);
-      *reinterpret_cast<uint32_t*>(meta + 16 * (t0 + j8) + 4 * (lane >> 3)) = own;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const uint32_t w = __shfl_sync(0xffffffffu, own, (lane & 24) + i);
-        const float inv = __shfl_sync(0xffffffffu, own_inv, (lane & 24) + i);
-        const float s = half_lo(w), z = half_hi(w);
-        float x[4];
-        four(t0 + i, x);
-        uint32_t c = 0;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) c |= (uint32_t)lq_code(x[j], z, s, inv) << (4 * j);
-        st_code(out + 32 * (t0 + i), c);
-      }
-    }
+    if (!lq_quantise_values<DT, false>(load, codes, meta)) lq_quantise_values<DT, true>(load, codes, meta);
   }
 }
 #endif

@@ -299,23 +299,18 @@ __device__ __noinline__ void q4_begun_page(const LayerQ4Params& p, int b, int he
   }
   if (p.flags & MC_LAYER_APPEND) {
     const int slot = n & (kLqPage - 1);
-    const uint2 kr = *reinterpret_cast<const uint2*>(p.k_new + new_at + 8 * lane), vw = *reinterpret_cast<const uint2*>(p.v_new + new_at + 8 * lane);
-    if (slot == kLqPage - 1) {  // the row completes a page
+    *reinterpret_cast<uint2*>(p.res_k + at + slot * kRowBytes + 8 * lane) = *reinterpret_cast<const uint2*>(p.k_new + new_at + 8 * lane);
+    *reinterpret_cast<uint2*>(p.res_v + at + slot * kRowBytes + 8 * lane) = *reinterpret_cast<const uint2*>(p.v_new + new_at + 8 * lane);
+    if (slot == kLqPage - 1) {  // the row completes a page (a thread reads the columns of it that it has just written)
       const int page = checked_page(p.g, b, n / kLqPage, p.status);
 #pragma unroll 1
-      for (int tensor = 0; tensor < 2; ++tensor) {
-        if (page < 0) break;
+      for (int tensor = 0; tensor < 2 && page >= 0; ++tensor) {
         const char* src = (tensor == 0 ? p.res_k : p.res_v) + at + 8 * lane;
-        uint2 r[kLqPage];
-#pragma unroll
-        for (int t = 0; t < kLqPage - 1; ++t) r[t] = *reinterpret_cast<const uint2*>(src + t * kRowBytes);
-        r[kLqPage - 1] = tensor == 0 ? kr : vw;
         const size_t tile = (size_t)page * H + head;
-        lq_quantise<DT>(tensor == 0, r, p.pool[2 * tensor] + tile * kLqCodeBytes, p.pool[2 * tensor + 1] + tile * kLqMetaBytes);
+        lq_quantise<DT>(tensor == 0, [&](int t) { return *reinterpret_cast<const uint2*>(src + t * kRowBytes); },
+                        p.pool[2 * tensor] + tile * kLqCodeBytes, p.pool[2 * tensor + 1] + tile * kLqMetaBytes);
       }
     }
-    *reinterpret_cast<uint2*>(p.res_k + at + slot * kRowBytes + 8 * lane) = kr;
-    *reinterpret_cast<uint2*>(p.res_v + at + slot * kRowBytes + 8 * lane) = vw;
   }
 }
 

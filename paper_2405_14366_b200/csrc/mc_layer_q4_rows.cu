@@ -61,19 +61,18 @@ struct AppendItem {
   int n, first, count;  // cached tokens, the sequence's rows
 };
 
-// (in program order: the compiler would have all 32 addresses of a page in registers ahead of its loads)
-__device__ __forceinline__ uint2 ld_row8(const char* p) {
-  uint2 v;
-  asm volatile("ld.global.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p) : "memory");
-  return v;
-}
-
 // An item is a page that the call completes, or -- where it completes none -- the rows of the begun page.  The first
-// item of a sequence also leaves the rows behind its last complete page in the begun page's place, after it has read what
-// was there: a thread reads and writes the same columns of it, so that needs no barrier.
+// item of a sequence also leaves the rows behind its last complete page in the begun page's place, after the warp has read
+// what was there.  A warp keeps the page that it works on in shared memory and the next one, on its way, in registers.
+struct AppendWork {
+  int b, head, tensor, slot;
+  bool page, first;  // a page to quantise; the sequence's first item
+};
+
 template <int DT>
 __global__ void __launch_bounds__(kLrThreads, 2) layer_q4_append_kernel(const __grid_constant__ Q4RowParams p) {
   grid_dep_launch();
+  extern __shared__ __align__(16) unsigned char tile_smem[];  // [warps][8 KB]
   __shared__ int pre_s[kMaxLayerBatch + 1];
   __shared__ AppendItem seq_s[kMaxLayerBatch];
   const int tid = threadIdx.x, lane = tid & 31, H = p.g.n_kv_heads;
@@ -89,39 +88,72 @@ __global__ void __launch_bounds__(kLrThreads, 2) layer_q4_append_kernel(const __
   if (all_rows_bad(p, pre_s, bad, bad_rows)) return;
   const long long items = (long long)pre_s[p.g.batch] * 2 * H;
   const long long step = (long long)gridDim.x * kLrWarps;
-  for (long long i = (long long)blockIdx.x * kLrWarps + (tid >> 5); i < items; i += step) {
+  unsigned char* tile = tile_smem + (tid >> 5) * kLqResBytes;
+  const int ch = lane & 15, half = lane >> 4;  // loading: half a warp has a row, a lane 16 bytes of it
+
+  auto work_at = [&](long long i) {
+    AppendWork w;
     const int pg = (int)(i / (2 * H)), rem = (int)(i - (long long)pg * 2 * H);
-    const int tensor = rem / H, head = rem - tensor * H;
-    const int b = seq_of_item(pre_s, p.g.batch, pg);
-    const AppendItem s = seq_s[b];
-    const int slot = s.n / kLqPage + pg - pre_s[b];
-    const int done = (s.n + s.count) / kLqPage;  // complete pages afterwards
-    const bool head_item = pg == pre_s[b];
-    char* res = p.res[tensor] + ((long long)b * H + head) * kLqResBytes + 8 * lane;
-    const char* rows = p.rows[tensor] + (long long)head * kRowBytes + 8 * lane;
-    const long long pitch = p.stride[tensor] * 2;
-    auto row_at = [&](int t) -> const char* {  // token t of the sequence: already in the begun page, or new
-      return t < s.n ? res + (long long)(t & (kLqPage - 1)) * kRowBytes : rows + (long long)(s.first + t - s.n) * pitch;
-    };
-    if (slot < done) {
-      uint2 r[kLqPage];
+    w.tensor = rem / H;
+    w.head = rem - w.tensor * H;
+    w.b = seq_of_item(pre_s, p.g.batch, pg);
+    const AppendItem s = seq_s[w.b];
+    w.slot = s.n / kLqPage + pg - pre_s[w.b];
+    w.page = w.slot < (s.n + s.count) / kLqPage;
+    w.first = pg == pre_s[w.b];
+    return w;
+  };
+  auto row_at = [&](const AppendWork& w, const AppendItem& s, int t) -> const char* {  // token t: already in the begun page, or new
+    return t < s.n ? p.res[w.tensor] + (((long long)w.b * H + w.head) * kLqPage + (t & (kLqPage - 1))) * kRowBytes
+                   : p.rows[w.tensor] + (long long)w.head * kRowBytes + (long long)(s.first + t - s.n) * p.stride[w.tensor] * 2;
+  };
+  uint4 v[kLqPage / 2];
+  auto fetch = [&](const AppendWork& w) {
+    if (!w.page) return;
+    const AppendItem s = seq_s[w.b];
+    const int t0 = w.slot * kLqPage + half;
+    if (t0 - half >= s.n) {  // all rows new: one address, a stride
+      const char* src = row_at(w, s, t0) + 16 * ch;
+      const long long two = p.stride[w.tensor] * 4;
 #pragma unroll
-      for (int t = 0; t < kLqPage; ++t) r[t] = ld_row8(row_at(slot * kLqPage + t));
-      const long long tile = tile_of(p, b, slot, head);
-      if (tile >= 0) lq_quantise<DT>(tensor == 0, r, p.codes[tensor] + tile * kLqCodeBytes, p.meta[tensor] + tile * kLqMetaBytes);
+      for (int k = 0; k < kLqPage / 2; ++k, src += two) v[k] = *reinterpret_cast<const uint4*>(src);
+    } else {
+#pragma unroll
+      for (int k = 0; k < kLqPage / 2; ++k) v[k] = *reinterpret_cast<const uint4*>(row_at(w, s, t0 + 2 * k) + 16 * ch);
     }
-    if (head_item) {
-      const int t0 = max(done * kLqPage, s.n), t1 = s.n + s.count;
-      for (int t = t0; t < t1; t += 8) {
-        uint2 r[8];
+  };
+
+  long long i = (long long)blockIdx.x * kLrWarps + (tid >> 5);
+  AppendWork w;
+  if (i < items) {
+    w = work_at(i);
+    fetch(w);
+  }
+  for (; i < items; i += step) {
+    const AppendWork cur = w;
+    if (cur.page) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
-          if (t + k < t1) r[k] = ld_row8(row_at(t + k));
-#pragma unroll
-        for (int k = 0; k < 8; ++k)
-          if (t + k < t1) *reinterpret_cast<uint2*>(res + (long long)((t + k) & (kLqPage - 1)) * kRowBytes) = r[k];
-      }
+      for (int k = 0; k < kLqPage / 2; ++k) *reinterpret_cast<uint4*>(tile + (2 * k + half) * kRowBytes + 16 * ch) = v[k];
     }
+    __syncwarp();
+    if (i + step < items) {
+      w = work_at(i + step);
+      fetch(w);
+    }
+    if (cur.page) {
+      const long long at = tile_of(p, cur.b, cur.slot, cur.head);
+      if (at >= 0)
+        lq_quantise<DT>(cur.tensor == 0, [&](int t) { return *reinterpret_cast<const uint2*>(tile + t * kRowBytes + 8 * lane); },
+                        p.codes[cur.tensor] + at * kLqCodeBytes, p.meta[cur.tensor] + at * kLqMetaBytes);
+    }
+    if (cur.first) {
+      const AppendItem s = seq_s[cur.b];
+      const int t1 = s.n + s.count;
+      char* res = p.res[cur.tensor] + ((long long)cur.b * H + cur.head) * kLqResBytes + 16 * ch;
+      for (int t = max(t1 / kLqPage * kLqPage, s.n) + half; t < t1; t += 2)
+        *reinterpret_cast<uint4*>(res + (t & (kLqPage - 1)) * kRowBytes) = *reinterpret_cast<const uint4*>(row_at(cur, s, t) + 16 * ch);
+    }
+    __syncwarp();  // (the tile has been read)
   }
 }
 
@@ -256,8 +288,9 @@ mc_status launch_layer_q4_append(const mc_config* cfg, const mc_batch* bt, const
   int n_sm = 0;
   if (mc_status st = sm_count(&n_sm)) return st;
   auto* kernel = cfg->dtype == MC_F16 ? layer_q4_append_kernel<MC_F16> : layer_q4_append_kernel<MC_BF16>;
-  MC_CUDA_CHECK(launch_pdl(kernel, dim3(row_ctas(bt, rows.n_rows, 2 * cfg->n_kv_heads, 2 * n_sm)), dim3(kLrThreads), 0, stream,
-                           row_params(g, layer, const_cast<void*>(k), const_cast<void*>(v), rows)));
+  MC_CUDA_CHECK(allow_smem(kernel, kLrWarps * kLqResBytes));
+  MC_CUDA_CHECK(launch_pdl(kernel, dim3(row_ctas(bt, rows.n_rows, 2 * cfg->n_kv_heads, 2 * n_sm)), dim3(kLrThreads), kLrWarps * kLqResBytes,
+                           stream, row_params(g, layer, const_cast<void*>(k), const_cast<void*>(v), rows)));
   return MC_OK;
 }
 
