@@ -132,131 +132,160 @@ __device__ __forceinline__ float lq_tame(float x) {
   return x != x ? 0.f : fminf(fmaxf(x, -most), most);
 }
 template <int DT>
-__device__ __forceinline__ uint2 lq_tame(const uint2& r) {
-  const float2 a = Elem<DT>::unpack(r.x), b = Elem<DT>::unpack(r.y);
-  return make_uint2(Elem<DT>::pack(lq_tame<DT>(a.x), lq_tame<DT>(a.y)), Elem<DT>::pack(lq_tame<DT>(b.x), lq_tame<DT>(b.y)));
-}
-// Two numbers of a word less z: for binary16 one mixed-precision FMA each.
-template <int DT>
-__device__ __forceinline__ float2 minus(uint32_t w, float zx, float zy) {
-  if (DT == MC_F16) {
-    float2 r;
-    asm("{\n\t.reg .b16 lo, hi, one;\n\tmov.b32 {lo, hi}, %2;\n\tmov.b16 one, 0x3C00;\n\t"
-        "fma.rn.f32.f16 %0, lo, one, %3;\n\tfma.rn.f32.f16 %1, hi, one, %4;\n\t}"
-        : "=f"(r.x), "=f"(r.y)
-        : "r"(w), "f"(-zx), "f"(-zy));
-    return r;
-  }
-  const float2 v = Elem<DT>::unpack(w);
-  return make_float2(v.x - zx, v.y - zy);
+__device__ __forceinline__ uint32_t lq_tame2(uint32_t w) {
+  const float2 a = Elem<DT>::unpack(w);
+  return Elem<DT>::pack(lq_tame<DT>(a.x), lq_tame<DT>(a.y));
 }
 __device__ __forceinline__ float rcp_approx(float x) {
   float r;
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
 }
-// Four codes, channel 4l + j at bits 4j, of differences d with scales' reciprocals inv, for quotients between 0 and 15.01; `tie`: one
-// of them is next to a tie (they are at most 15 * 3 * 2^-24 off).
-__device__ __forceinline__ uint32_t lq_codes(const float (&d)[4], const float (&inv)[4], bool& tie) {
-  float r[4], e[4];
+// Two numbers of a word less z (nz = -z, two numbers): for binary16 one mixed-precision FMA each.
+template <int DT>
+__device__ __forceinline__ uint64_t plus2(uint32_t w, uint64_t nz) {
+  float zx, zy;
+  unpack2(nz, zx, zy);
+  if (DT == MC_F16) {
+    float x, y;
+    asm("{\n\t.reg .b16 lo, hi, one;\n\tmov.b32 {lo, hi}, %2;\n\tmov.b16 one, 0x3C00;\n\t"
+        "fma.rn.f32.f16 %0, lo, one, %3;\n\tfma.rn.f32.f16 %1, hi, one, %4;\n\t}"
+        : "=f"(x), "=f"(y)
+        : "r"(w), "f"(zx), "f"(zy));
+    return pack2(x, y);
+  }
+  const float2 v = Elem<DT>::unpack(w);
+  return add2(pack2(v.x, v.y), nz);
+}
+// The codes of eight channels of a row, channel j at bits 4j, for quotients between 0 and 15.01; `tie`: one of them is next to a
+// tie (they are at most 15 * 3 * 2^-24 off).  nz, inv: -zero and 1 / scale of channel pairs.  Two channels per instruction.
+template <int DT>
+__device__ __forceinline__ uint32_t lq_codes(const uint4& r, const uint64_t (&nz)[4], const uint64_t (&inv)[4], bool& tie) {
+  const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+  const uint64_t magic = pack2(12582912.0f, 12582912.0f), back = pack2(-12582912.0f, -12582912.0f);  // 1.5 * 2^23: the nearest integer
+  const uint64_t minus1 = pack2(-1.f, -1.f);
+  float c[8], worst = 0.f;
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    r[j] = fmaf(d[j], inv[j], 12582912.0f) - 12582912.0f;  // 1.5 * 2^23: the nearest integer
-    e[j] = fmaf(d[j], inv[j], -r[j]);
+    const uint64_t d = plus2<DT>(w[j], nz[j]);
+    const uint64_t n = add2(fma2(d, inv[j], magic), back);
+    float ex, ey;
+    unpack2(fma2(d, inv[j], mul2(n, minus1)), ex, ey);
+    worst = max3_abs(worst, ex, ey);
+    unpack2(n, c[2 * j], c[2 * j + 1]);
   }
-  tie = max3_abs(fmaxf(fabsf(e[0]), fabsf(e[1])), e[2], e[3]) > 0.49999f;
-  return (uint32_t)__float_as_int(fmaf(fmaf(r[3], 16.f, r[2]), 256.f, fmaf(r[1], 16.f, r[0])) + 12582912.0f) & 0xffffu;
+  tie = worst > 0.49999f;
+  const float lo = fmaf(fmaf(c[3], 16.f, c[2]), 256.f, fmaf(c[1], 16.f, c[0])) + 12582912.0f;
+  const float hi = fmaf(fmaf(c[7], 16.f, c[6]), 256.f, fmaf(c[5], 16.f, c[4])) + 12582912.0f;
+  return __byte_perm(__float_as_uint(lo), __float_as_uint(hi), 0x5410);
 }
-template <int DT>
-__device__ __forceinline__ uint32_t lq_codes_exact(const uint2& r, const float (&z)[4], const float (&s)[4]) {
-  const float2 a = Elem<DT>::unpack(r.x), b = Elem<DT>::unpack(r.y);
-  const float x[4] = {a.x, a.y, b.x, b.y};
+// The same, every code for itself and right whatever the quotient is; group(j): (scale, zero) of channel j.
+template <int DT, typename Group>
+__device__ __forceinline__ uint32_t lq_codes_exact(const uint4& r, Group group) {
+  const uint32_t w[4] = {r.x, r.y, r.z, r.w};
   uint32_t c = 0;
 #pragma unroll
-  for (int j = 0; j < 4; ++j) c |= (uint32_t)lq_code(x[j], z[j], s[j], 1.0f / s[j]) << (4 * j);
+  for (int j = 0; j < 8; ++j) {
+    const float2 x = Elem<DT>::unpack(w[j >> 1]);
+    const uint32_t g = group(j);
+    const float s = half_lo(g);
+    c |= (uint32_t)lq_code(j & 1 ? x.y : x.x, half_hi(g), s, rcp_approx(s)) << (4 * j);
+  }
   return c;
 }
 // A group whose quotients may leave [0, 15.01]: a scale that is subnormal (coarse), a zero that is not the minimum itself.
 __device__ __forceinline__ bool lq_odd(uint32_t group, float lo) { return (group & 0x7fffu) < 0x0400u || half_hi(group) != lo; }
 
-// One (page, kv head) of K or V by a warp: lane l has channels 4l .. 4l + 3 of the page's 32 rows, load(t) gives those of row t.
-// False (nothing stored that counts): something in it is not a number that binary16 holds, and it has to be done again with WILD.
-// Loops that are not unrolled over registers: 16 KB of straight code per tensor made the instruction cache the limit (8 x 4096
-// prompts of 32 heads 606 us).
-// K: a group is one of the lane's channels, so nothing is exchanged.
+// One (page, kv head) of K or V by a warp: half a warp has a row, lane l channels 8 (l & 15) .. + 7 of the rows 2k + (l >> 4);
+// load(t) gives those of row t.  False (nothing stored that counts): something in it is not a number that binary16 holds, and it
+// has to be done again with WILD.  The rows come from memory, not from registers: with a page in registers the code was 16 KB of
+// straight lines per tensor and the instruction cache the limit (8 x 4096 prompts of 32 heads 606 us).
+// K: a group is one of the lane's channels; the two half-warps join their extremes.
 template <int DT, bool WILD, typename Load>
 __device__ __forceinline__ bool lq_quantise_keys(Load load, unsigned char* codes, unsigned char* meta) {
-  const int lane = threadIdx.x & 31;
-  auto get = [&](int t) { return WILD ? lq_tame<DT>(load(t)) : load(t); };
-  uint2 lo2 = get(0), hi2 = lo2;
-#pragma unroll 8
-  for (int t = 1; t < kLqPage; ++t) {
-    const uint2 r = get(t);
-    lo2.x = min2_nan<DT>(lo2.x, r.x);
-    lo2.y = min2_nan<DT>(lo2.y, r.y);
-    hi2.x = max2_nan<DT>(hi2.x, r.x);
-    hi2.y = max2_nan<DT>(hi2.y, r.y);
+  const int lane = threadIdx.x & 31, half = lane >> 4, ch = lane & 15;
+  auto get = [&](int k) {
+    uint4 r = load(2 * k + half);
+    if (WILD) r = make_uint4(lq_tame2<DT>(r.x), lq_tame2<DT>(r.y), lq_tame2<DT>(r.z), lq_tame2<DT>(r.w));
+    return r;
+  };
+  uint32_t lo2[4], hi2[4];
+  {
+    const uint4 r = get(0);
+    lo2[0] = hi2[0] = r.x;
+    lo2[1] = hi2[1] = r.y;
+    lo2[2] = hi2[2] = r.z;
+    lo2[3] = hi2[3] = r.w;
   }
-  const float2 la = Elem<DT>::unpack(lo2.x), lb = Elem<DT>::unpack(lo2.y), ha = Elem<DT>::unpack(hi2.x), hb = Elem<DT>::unpack(hi2.y);
-  const float lo[4] = {la.x, la.y, lb.x, lb.y}, hi[4] = {ha.x, ha.y, hb.x, hb.y};
-  if (!WILD) {
-    bool tame = true;
+#pragma unroll 5
+  for (int k = 1; k < kLqPage / 2; ++k) {
+    const uint4 r = get(k);
+    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
 #pragma unroll
-    for (int j = 0; j < 4; ++j) tame = tame && lo[j] >= -65504.f && hi[j] <= 65504.f;  // (false for a NaN)
-    if (!__all_sync(0xffffffffu, tame)) return false;
+    for (int j = 0; j < 4; ++j) {
+      lo2[j] = min2_nan<DT>(lo2[j], w[j]);
+      hi2[j] = max2_nan<DT>(hi2[j], w[j]);
+    }
   }
-  uint32_t w[4];
-  float z[4], s[4], inv[4];
-  bool odd = false;
+  bool tame = true, odd = false;
+  uint32_t group[8];
+  uint64_t nz[4], inv[4];
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    w[j] = lq_group(lo[j], hi[j]);
-    s[j] = half_lo(w[j]);
-    z[j] = half_hi(w[j]);
-    inv[j] = rcp_approx(s[j]);
-    odd = odd || lq_odd(w[j], lo[j]);
+    const float2 lo = Elem<DT>::unpack(min2_nan<DT>(lo2[j], __shfl_xor_sync(0xffffffffu, lo2[j], 16)));
+    const float2 hi = Elem<DT>::unpack(max2_nan<DT>(hi2[j], __shfl_xor_sync(0xffffffffu, hi2[j], 16)));
+    tame = tame && lo.x >= -65504.f && lo.y >= -65504.f && hi.x <= 65504.f && hi.y <= 65504.f;  // (false for a NaN)
+    group[2 * j] = lq_group(lo.x, hi.x);
+    group[2 * j + 1] = lq_group(lo.y, hi.y);
+    odd = odd || lq_odd(group[2 * j], lo.x) || lq_odd(group[2 * j + 1], lo.y);
+    nz[j] = pack2(-half_hi(group[2 * j]), -half_hi(group[2 * j + 1]));
+    inv[j] = pack2(rcp_approx(half_lo(group[2 * j])), rcp_approx(half_lo(group[2 * j + 1])));
   }
-  *reinterpret_cast<uint4*>(meta + 16 * lane) = make_uint4(w[0], w[1], w[2], w[3]);
-  unsigned short* out = reinterpret_cast<unsigned short*>(codes) + lane;
-  uint32_t again = 0;  // rows with a quotient next to a tie
+  if (!WILD && !__all_sync(0xffffffffu, tame)) return false;
+  *reinterpret_cast<uint4*>(meta + 32 * ch + 16 * half) =
+      half ? make_uint4(group[4], group[5], group[6], group[7]) : make_uint4(group[0], group[1], group[2], group[3]);
+  uint32_t* out = reinterpret_cast<uint32_t*>(codes) + lane;
+  uint32_t again = 0;  // row pairs with a quotient next to a tie
 #pragma unroll 4
-  for (int t = 0; t < kLqPage; ++t) {
-    const uint2 r = get(t);
-    const float2 a = minus<DT>(r.x, z[0], z[1]), b = minus<DT>(r.y, z[2], z[3]);
-    const float d[4] = {a.x, a.y, b.x, b.y};
+  for (int k = 0; k < kLqPage / 2; ++k) {
     bool tie;
-    out[32 * t] = (unsigned short)lq_codes(d, inv, tie);
-    if (tie) again |= 1u << t;
+    out[32 * k] = lq_codes<DT>(get(k), nz, inv, tie);
+    if (tie) again |= 1u << k;
   }
-  again = __any_sync(0xffffffffu, odd) ? 0xffffffffu : __reduce_or_sync(0xffffffffu, again);
+  again = __any_sync(0xffffffffu, odd) ? 0xffffu : __reduce_or_sync(0xffffffffu, again);
 #pragma unroll 1
   while (again != 0) {
-    const int t = __ffs(again) - 1;
+    const int k = __ffs(again) - 1;
     again &= again - 1;
-    out[32 * t] = (unsigned short)lq_codes_exact<DT>(get(t), z, s);
+    out[32 * k] = lq_codes_exact<DT>(get(k), [&](int j) { return group[j]; });
   }
   return true;
 }
-// V: a group is a row's part in eight lanes.  Eight rows' extremes (the least and the negative of the largest, a pair) are joined
-// at a time, halving the rows a lane keeps at every step (7 exchanges instead of 24); lane j of the eight ends with row j's
+// V: a group is a row's part in four lanes.  The extremes of a lane's four rows (the least and the negative of the largest, a pair)
+// are joined at a time, halving the rows that a lane keeps (3 exchanges instead of 8); lane j of the four ends with row j's
 // group, forms its parameters once and hands them round.
 template <int DT, bool WILD, typename Load>
 __device__ __forceinline__ bool lq_quantise_values(Load load, unsigned char* codes, unsigned char* meta) {
-  const int lane = threadIdx.x & 31, j8 = lane & 7;
-  auto get = [&](int t) { return WILD ? lq_tame<DT>(load(t)) : load(t); };
-  unsigned short* out = reinterpret_cast<unsigned short*>(codes) + lane;
+  const int lane = threadIdx.x & 31, half = lane >> 4, ch = lane & 15;
+  auto get = [&](int k) {
+    uint4 r = load(2 * k + half);
+    if (WILD) r = make_uint4(lq_tame2<DT>(r.x), lq_tame2<DT>(r.y), lq_tame2<DT>(r.z), lq_tame2<DT>(r.w));
+    return r;
+  };
+  uint32_t* out = reinterpret_cast<uint32_t*>(codes) + lane;
 #pragma unroll 1
-  for (int t0 = 0; t0 < kLqPage; t0 += 8) {
-    uint2 r[8];
-    uint32_t v[8];
+  for (int k0 = 0; k0 < kLqPage / 2; k0 += 4) {
+    uint4 r[4];
+    uint32_t v[4];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      r[i] = get(t0 + i);
-      const uint32_t mn = min2_nan<DT>(r[i].x, r[i].y), mx = max2_nan<DT>(r[i].x, r[i].y) ^ 0x80008000u;
+    for (int i = 0; i < 4; ++i) {
+      r[i] = get(k0 + i);
+      const uint32_t mn = min2_nan<DT>(min2_nan<DT>(r[i].x, r[i].y), min2_nan<DT>(r[i].z, r[i].w));
+      const uint32_t mx = max2_nan<DT>(max2_nan<DT>(r[i].x, r[i].y), max2_nan<DT>(r[i].z, r[i].w)) ^ 0x80008000u;
       v[i] = min2_nan<DT>(__byte_perm(mn, mx, 0x5410), __byte_perm(mn, mx, 0x7632));
     }
 #pragma unroll
-    for (int o = 4, m = 4; o > 0; o >>= 1, m >>= 1) {  // m rows stay: those whose bit o is the lane's
+    for (int o = 2, m = 2; o > 0; o >>= 1, m >>= 1) {  // m rows stay: those whose bit o is the lane's
       const bool up = (lane & o) != 0;
 #pragma unroll
       for (int i = 0; i < m; ++i) {
@@ -269,27 +298,24 @@ __device__ __forceinline__ bool lq_quantise_values(Load load, unsigned char* cod
     if (!WILD && !__all_sync(0xffffffffu, lo >= -65504.f && hi <= 65504.f)) return false;
     const uint32_t own = lq_group(lo, hi);
     const float own_inv = rcp_approx(half_lo(own));
-    *reinterpret_cast<uint32_t*>(meta + 16 * (t0 + j8) + 4 * (lane >> 3)) = own;
+    *reinterpret_cast<uint32_t*>(meta + 16 * (2 * (k0 + (lane & 3)) + half) + 4 * (ch >> 2)) = own;
     uint32_t again = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const uint32_t w = __shfl_sync(0xffffffffu, own, (lane & 24) + i);
-      const float f = __shfl_sync(0xffffffffu, own_inv, (lane & 24) + i), z = half_hi(w);
-      const float2 a = minus<DT>(r[i].x, z, z), b = minus<DT>(r[i].y, z, z);
-      const float d[4] = {a.x, a.y, b.x, b.y}, inv[4] = {f, f, f, f};
+    for (int i = 0; i < 4; ++i) {
+      const float z = -half_hi(__shfl_sync(0xffffffffu, own, (lane & 28) + i)), f = __shfl_sync(0xffffffffu, own_inv, (lane & 28) + i);
+      const uint64_t z2 = pack2(z, z), f2 = pack2(f, f);
+      const uint64_t nz[4] = {z2, z2, z2, z2}, inv[4] = {f2, f2, f2, f2};
       bool tie;
-      out[32 * (t0 + i)] = (unsigned short)lq_codes(d, inv, tie);
+      out[32 * (k0 + i)] = lq_codes<DT>(r[i], nz, inv, tie);
       if (tie) again |= 1u << i;
     }
-    again = __any_sync(0xffffffffu, lq_odd(own, lo)) ? 0xffu : __reduce_or_sync(0xffffffffu, again);
+    again = __any_sync(0xffffffffu, lq_odd(own, lo)) ? 0xfu : __reduce_or_sync(0xffffffffu, again);
 #pragma unroll 1
     while (again != 0) {
       const int i = __ffs(again) - 1;
       again &= again - 1;
-      const uint32_t w = __shfl_sync(0xffffffffu, own, (lane & 24) + i);
-      const float s = half_lo(w), z = half_hi(w);
-      const float s4[4] = {s, s, s, s}, z4[4] = {z, z, z, z};
-      out[32 * (t0 + i)] = (unsigned short)lq_codes_exact<DT>(get(t0 + i), z4, s4);
+      const uint32_t w = __shfl_sync(0xffffffffu, own, (lane & 28) + i);
+      out[32 * (k0 + i)] = lq_codes_exact<DT>(get(k0 + i), [&](int) { return w; });
     }
   }
   return true;

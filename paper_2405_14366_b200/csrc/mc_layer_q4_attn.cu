@@ -299,15 +299,17 @@ __device__ __noinline__ void q4_begun_page(const LayerQ4Params& p, int b, int he
   }
   if (p.flags & MC_LAYER_APPEND) {
     const int slot = n & (kLqPage - 1);
-    *reinterpret_cast<uint2*>(p.res_k + at + slot * kRowBytes + 8 * lane) = *reinterpret_cast<const uint2*>(p.k_new + new_at + 8 * lane);
-    *reinterpret_cast<uint2*>(p.res_v + at + slot * kRowBytes + 8 * lane) = *reinterpret_cast<const uint2*>(p.v_new + new_at + 8 * lane);
-    if (slot == kLqPage - 1) {  // the row completes a page (a thread reads the columns of it that it has just written)
+    const int ch = lane & 15;  // lanes 0 .. 15: the new K row's chunks, 16 .. 31: the V row's
+    *reinterpret_cast<uint4*>((lane < 16 ? p.res_k : p.res_v) + at + slot * kRowBytes + 16 * ch) =
+        *reinterpret_cast<const uint4*>((lane < 16 ? p.k_new : p.v_new) + new_at + 16 * ch);
+    if (slot == kLqPage - 1) {  // the row completes a page
+      __syncwarp();             // (which other lanes of the warp have just written)
       const int page = checked_page(p.g, b, n / kLqPage, p.status);
 #pragma unroll 1
       for (int tensor = 0; tensor < 2 && page >= 0; ++tensor) {
-        const char* src = (tensor == 0 ? p.res_k : p.res_v) + at + 8 * lane;
+        const char* src = (tensor == 0 ? p.res_k : p.res_v) + at + 16 * ch;
         const size_t tile = (size_t)page * H + head;
-        lq_quantise<DT>(tensor == 0, [&](int t) { return *reinterpret_cast<const uint2*>(src + t * kRowBytes); },
+        lq_quantise<DT>(tensor == 0, [&](int t) { return *reinterpret_cast<const uint4*>(src + t * kRowBytes); },
                         p.pool[2 * tensor] + tile * kLqCodeBytes, p.pool[2 * tensor + 1] + tile * kLqMetaBytes);
       }
     }

@@ -143,7 +143,7 @@ __global__ void __launch_bounds__(kLrThreads, 2) layer_q4_append_kernel(const __
     if (cur.page) {
       const long long at = tile_of(p, cur.b, cur.slot, cur.head);
       if (at >= 0)
-        lq_quantise<DT>(cur.tensor == 0, [&](int t) { return *reinterpret_cast<const uint2*>(tile + t * kRowBytes + 8 * lane); },
+        lq_quantise<DT>(cur.tensor == 0, [&](int t) { return *reinterpret_cast<const uint4*>(tile + t * kRowBytes + 16 * ch); },
                         p.codes[cur.tensor] + at * kLqCodeBytes, p.meta[cur.tensor] + at * kLqMetaBytes);
     }
     if (cur.first) {

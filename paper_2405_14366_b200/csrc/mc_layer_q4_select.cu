@@ -19,7 +19,7 @@
 
 namespace mc {
 
-constexpr int kLsThreads = 256;
+constexpr int kLsThreads = 512;
 constexpr int kLsWarps = kLsThreads / 32;
 constexpr int kLsMaxCluster = 8;
 constexpr int kLsBatch = 8;  // pages of a warp at a time
@@ -51,7 +51,7 @@ __device__ __forceinline__ unsigned long long order64(double x) {
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 __device__ __forceinline__ void store_first_cta(uint32_t* smem, uint32_t v) {
-  uint32_t a;
+  uint32_t a;  // (its address in the first CTA)
   asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(a) : "r"((uint32_t)__cvta_generic_to_shared(smem)));
   asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(a), "r"(v) : "memory");
 }
@@ -97,22 +97,39 @@ __global__ void __launch_bounds__(kLsThreads) layer_q4_select_kernel(const __gri
     }
 #pragma unroll
     for (int c = 0; c < 4; ++c) P[c] *= 15.0;
-    for (int k0 = (rank * kLsWarps + warp) * kLsBatch; k0 < u; k0 += p.cluster * kLsWarps * kLsBatch) {
-      int mine = 0;
-      if (lane < kLsBatch && k0 + lane < u) {
-        mine = checked_page(p.g, b, v.page_of(k0 + lane), p.status);
-        mine = mine < 0 ? 0 : mine;
-      }
-      uint4 m[kLsBatch];
+    // The warp's pages: batches of eight, every (cluster * warps)-th.  A lane knows the page of one of the next 32 (four batches);
+    // the next batch's parameters are on their way while one is worked on.
+    const int step = p.cluster * kLsWarps * kLsBatch, first = (rank * kLsWarps + warp) * kLsBatch;
+    auto pages_from = [&](int k) {  // lane: page (lane & 7) of the batch k + (lane >> 3) step
+      const int at = k + (lane >> 3) * step + (lane & 7);
+      if (at >= u) return 0;
+      const int page = checked_page(p.g, b, v.page_of(at), p.status);
+      return page < 0 ? 0 : page;
+    };
+    int ids = pages_from(first), ids_next = pages_from(first + 4 * step), turn = 0;
+    uint4 m[kLsBatch];
+    auto fetch = [&](int t) {
 #pragma unroll
       for (int j = 0; j < kLsBatch; ++j) {
-        const int page = __shfl_sync(0xffffffffu, mine, j);
+        const int page = __shfl_sync(0xffffffffu, ids, 8 * t + j);
         m[j] = *reinterpret_cast<const uint4*>(p.k_meta + ((size_t)page * H + head) * kLqMetaBytes + 16 * lane);
       }
+    };
+    if (first < u) fetch(0);
+    for (int k0 = first; k0 < u; k0 += step) {
+      uint4 cur[kLsBatch];
+#pragma unroll
+      for (int j = 0; j < kLsBatch; ++j) cur[j] = m[j];
+      if (++turn == 4) {
+        turn = 0;
+        ids = ids_next;
+        ids_next = pages_from(k0 + 5 * step);
+      }
+      if (k0 + step < u) fetch(turn);
       double a[kLsBatch];
 #pragma unroll
       for (int j = 0; j < kLsBatch; ++j) {
-        const uint32_t w[4] = {m[j].x, m[j].y, m[j].z, m[j].w};
+        const uint32_t w[4] = {cur[j].x, cur[j].y, cur[j].z, cur[j].w};
         double t = 0.0;
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
@@ -147,6 +164,38 @@ __global__ void __launch_bounds__(kLsThreads) layer_q4_select_kernel(const __gri
   cluster_wait();
   if (rank != 0) return;
 
+  // ---- few pages, a thread each: its rank is the number of larger keys (512 comparisons are less than a pass over the digits)
+  if (u <= kLsThreads) {
+    bool in = false;
+    if (tid < u) {
+      const uint32_t c = keys_s[tid];
+      int above = 0, alike = 0;
+      const int u4 = u / 4 * 4;
+#pragma unroll 4
+      for (int k = 0; k < u4; k += 4) {
+        const uint4 o = *reinterpret_cast<const uint4*>(keys_s + k);
+        above += (o.x > c ? 1 : 0) + (o.y > c ? 1 : 0) + (o.z > c ? 1 : 0) + (o.w > c ? 1 : 0);
+        alike += (o.x == c ? 1 : 0) + (o.y == c ? 1 : 0) + (o.z == c ? 1 : 0) + (o.w == c ? 1 : 0);
+      }
+      for (int k = u4; k < u; ++k) {
+        above += keys_s[k] > c ? 1 : 0;
+        alike += keys_s[k] == c ? 1 : 0;
+      }
+      if (alike > 1 && above < take && above + alike > take) {  // some of those that are alike in 32 bits
+        const unsigned long long d = keys[tid];
+        for (int k = 0; k < u; ++k)
+          if (keys_s[k] == c && k != tid) above += keys[k] > d || (keys[k] == d && k < tid) ? 1 : 0;
+      }
+      in = above < take;
+    }
+    const uint32_t bi = __ballot_sync(0xffffffffu, in);
+    if (lane == 0) ins_s[warp] = __popc(bi);
+    __syncthreads();
+    int before = __popc(bi & ((1u << lane) - 1u));
+    for (int w = 0; w < warp; ++w) before += ins_s[w];
+    if (in) list[before] = v.page_of(tid);
+    return;
+  }
   // ---- the last one in: digits of the 32-bit keys, then (of those that are alike in them) of the 64-bit ones
   uint32_t p32 = 0, m32 = 0;
   unsigned long long p64 = 0, m64 = 0;
@@ -166,7 +215,7 @@ __global__ void __launch_bounds__(kLsThreads) layer_q4_select_kernel(const __gri
     for (int k = tid; k < u; k += kLsThreads)
       if (matches(k)) atomicAdd(&hist[(wide ? (uint32_t)(keys[k] >> shift) : keys_s[k] >> shift) & ((1u << width) - 1u)], 1u);
     __syncthreads();
-    // the bin from the top in which the need-th lies: thread t has the bins 8 t .. 8 t + 7
+    // the bin from the top in which the need-th lies: thread t has four of them
     constexpr int kOwn = kLsBins / kLsThreads;
     uint32_t own[kOwn], sum = 0;
 #pragma unroll
