@@ -162,21 +162,20 @@ __device__ __forceinline__ uint64_t plus2(uint32_t w, uint64_t nz) {
 template <int DT>
 __device__ __forceinline__ uint32_t lq_codes(const uint4& r, const uint64_t (&nz)[4], const uint64_t (&inv)[4], bool& tie) {
   const uint32_t w[4] = {r.x, r.y, r.z, r.w};
-  const uint64_t magic = pack2(12582912.0f, 12582912.0f), back = pack2(-12582912.0f, -12582912.0f);  // 1.5 * 2^23: the nearest integer
-  const uint64_t minus1 = pack2(-1.f, -1.f);
-  float c[8], worst = 0.f;
+  const uint64_t magic = pack2(12582912.0f, 12582912.0f), minus1 = pack2(-1.f, -1.f);  // 1.5 * 2^23: the nearest integer
+  float c[8], worst = 0.f;  // c: codes' negatives
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     const uint64_t d = plus2<DT>(w[j], nz[j]);
-    const uint64_t n = add2(fma2(d, inv[j], magic), back);
+    const uint64_t n = fma2(fma2(d, inv[j], magic), minus1, magic);
     float ex, ey;
-    unpack2(fma2(d, inv[j], mul2(n, minus1)), ex, ey);
+    unpack2(fma2(d, inv[j], n), ex, ey);
     worst = max3_abs(worst, ex, ey);
     unpack2(n, c[2 * j], c[2 * j + 1]);
   }
   tie = worst > 0.49999f;
-  const float lo = fmaf(fmaf(c[3], 16.f, c[2]), 256.f, fmaf(c[1], 16.f, c[0])) + 12582912.0f;
-  const float hi = fmaf(fmaf(c[7], 16.f, c[6]), 256.f, fmaf(c[5], 16.f, c[4])) + 12582912.0f;
+  const float lo = 12582912.0f - fmaf(fmaf(c[3], 16.f, c[2]), 256.f, fmaf(c[1], 16.f, c[0]));
+  const float hi = 12582912.0f - fmaf(fmaf(c[7], 16.f, c[6]), 256.f, fmaf(c[5], 16.f, c[4]));
   return __byte_perm(__float_as_uint(lo), __float_as_uint(hi), 0x5410);
 }
 // The same, every code for itself and right whatever the quotient is; group(j): (scale, zero) of channel j.
@@ -228,22 +227,32 @@ __device__ __forceinline__ bool lq_quantise_keys(Load load, unsigned char* codes
     }
   }
   bool tame = true, odd = false;
-  uint32_t group[8];
+  uint32_t own[4], group[8];  // a half-warp forms the parameters of four of a lane's channels, the other half those of the others
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    // (the other half's extremes of the channels that are this lane's to do, for this half's of the others)
+    const uint32_t gl = half ? lo2[j] : lo2[j + 2], gh = half ? hi2[j] : hi2[j + 2], kl = half ? lo2[j + 2] : lo2[j], kh = half ? hi2[j + 2] : hi2[j];
+    const float2 lo = Elem<DT>::unpack(min2_nan<DT>(kl, __shfl_xor_sync(0xffffffffu, gl, 16)));
+    const float2 hi = Elem<DT>::unpack(max2_nan<DT>(kh, __shfl_xor_sync(0xffffffffu, gh, 16)));
+    tame = tame && lo.x >= -65504.f && lo.y >= -65504.f && hi.x <= 65504.f && hi.y <= 65504.f;  // (false for a NaN)
+    own[2 * j] = lq_group(lo.x, hi.x);
+    own[2 * j + 1] = lq_group(lo.y, hi.y);
+    odd = odd || lq_odd(own[2 * j], lo.x) || lq_odd(own[2 * j + 1], lo.y);
+  }
+  if (!WILD && !__all_sync(0xffffffffu, tame)) return false;
+  *reinterpret_cast<uint4*>(meta + 32 * ch + 16 * half) = make_uint4(own[0], own[1], own[2], own[3]);
   uint64_t nz[4], inv[4];
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    const float2 lo = Elem<DT>::unpack(min2_nan<DT>(lo2[j], __shfl_xor_sync(0xffffffffu, lo2[j], 16)));
-    const float2 hi = Elem<DT>::unpack(max2_nan<DT>(hi2[j], __shfl_xor_sync(0xffffffffu, hi2[j], 16)));
-    tame = tame && lo.x >= -65504.f && lo.y >= -65504.f && hi.x <= 65504.f && hi.y <= 65504.f;  // (false for a NaN)
-    group[2 * j] = lq_group(lo.x, hi.x);
-    group[2 * j + 1] = lq_group(lo.y, hi.y);
-    odd = odd || lq_odd(group[2 * j], lo.x) || lq_odd(group[2 * j + 1], lo.y);
+    const uint32_t other = __shfl_xor_sync(0xffffffffu, own[j], 16);
+    group[j] = half ? other : own[j];
+    group[j + 4] = half ? own[j] : other;
+  }
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
     nz[j] = pack2(-half_hi(group[2 * j]), -half_hi(group[2 * j + 1]));
     inv[j] = pack2(rcp_approx(half_lo(group[2 * j])), rcp_approx(half_lo(group[2 * j + 1])));
   }
-  if (!WILD && !__all_sync(0xffffffffu, tame)) return false;
-  *reinterpret_cast<uint4*>(meta + 32 * ch + 16 * half) =
-      half ? make_uint4(group[4], group[5], group[6], group[7]) : make_uint4(group[0], group[1], group[2], group[3]);
   uint32_t* out = reinterpret_cast<uint32_t*>(codes) + lane;
   uint32_t again = 0;  // row pairs with a quotient next to a tie
 #pragma unroll 4

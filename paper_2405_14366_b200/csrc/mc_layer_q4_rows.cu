@@ -86,22 +86,32 @@ __global__ void __launch_bounds__(kLrThreads, 2) layer_q4_append_kernel(const __
     pre_s[b + 1] = s.count == 0 ? 0 : max((s.n + s.count) / kLqPage - s.n / kLqPage, 1);
   }
   if (all_rows_bad(p, pre_s, bad, bad_rows)) return;
-  const long long items = (long long)pre_s[p.g.batch] * 2 * H;
-  const long long step = (long long)gridDim.x * kLrWarps;
   unsigned char* tile = tile_smem + (tid >> 5) * kLqResBytes;
   const int ch = lane & 15, half = lane >> 4;  // loading: half a warp has a row, a lane 16 bytes of it
-
-  auto work_at = [&](long long i) {
-    AppendWork w;
-    const int pg = (int)(i / (2 * H)), rem = (int)(i - (long long)pg * 2 * H);
-    w.tensor = rem / H;
-    w.head = rem - w.tensor * H;
-    w.b = seq_of_item(pre_s, p.g.batch, pg);
-    const AppendItem s = seq_s[w.b];
-    w.slot = s.n / kLqPage + pg - pre_s[w.b];
+  // A warp has columns (K or V, kv head) that do not change, and every `step`-th page: as many pages as there are warps for all
+  // columns at a time (or, with more columns than warps, one, and several columns).
+  const int pages = pre_s[p.g.batch], columns = 2 * H, warps = gridDim.x * kLrWarps, gw = blockIdx.x * kLrWarps + (tid >> 5);
+  const int step = max(warps / columns, 1), pg0 = warps >= columns ? gw / columns : 0;
+  int column = warps >= columns ? gw % columns : gw, pg = pg0, b_at = 0;
+  if (pg0 >= step) column = columns;  // (a warp left over)
+  AppendWork w;
+  auto next = [&]() {  // the warp's next item into w; false behind the last one
+    while (column < columns && pg >= pages) {
+      column += warps >= columns ? columns : warps;
+      pg = pg0;
+      b_at = 0;
+    }
+    if (column >= columns) return false;
+    while (pg >= pre_s[b_at + 1]) ++b_at;
+    const AppendItem s = seq_s[b_at];
+    w.b = b_at;
+    w.tensor = column >= H ? 1 : 0;
+    w.head = column - w.tensor * H;
+    w.slot = s.n / kLqPage + pg - pre_s[b_at];
     w.page = w.slot < (s.n + s.count) / kLqPage;
-    w.first = pg == pre_s[w.b];
-    return w;
+    w.first = pg == pre_s[b_at];
+    pg += step;
+    return true;
   };
   auto row_at = [&](const AppendWork& w, const AppendItem& s, int t) -> const char* {  // token t: already in the begun page, or new
     return t < s.n ? p.res[w.tensor] + (((long long)w.b * H + w.head) * kLqPage + (t & (kLqPage - 1))) * kRowBytes
@@ -123,23 +133,17 @@ __global__ void __launch_bounds__(kLrThreads, 2) layer_q4_append_kernel(const __
     }
   };
 
-  long long i = (long long)blockIdx.x * kLrWarps + (tid >> 5);
-  AppendWork w;
-  if (i < items) {
-    w = work_at(i);
-    fetch(w);
-  }
-  for (; i < items; i += step) {
+  bool more = next();
+  if (more) fetch(w);
+  while (more) {
     const AppendWork cur = w;
     if (cur.page) {
 #pragma unroll
       for (int k = 0; k < kLqPage / 2; ++k) *reinterpret_cast<uint4*>(tile + (2 * k + half) * kRowBytes + 16 * ch) = v[k];
     }
     __syncwarp();
-    if (i + step < items) {
-      w = work_at(i + step);
-      fetch(w);
-    }
+    more = next();
+    if (more) fetch(w);
     if (cur.page) {
       const long long at = tile_of(p, cur.b, cur.slot, cur.head);
       if (at >= 0)
