@@ -42,28 +42,29 @@ __device__ __forceinline__ PageView page_view(const ScoreRule& rule, int b, int 
   return s;
 }
 
-// Exclusive prefix of [0, batch) counts in shared memory, pre[b + 1] = the count of sequence b on entry; pre[batch] = the
-// total.  Every thread of the CTA calls it.
+// Exclusive prefix of counts in shared memory by a warp: pre[b + 1] = the count of sequence b on entry; pre[batch] = the total.
+__device__ __forceinline__ void scan_warp(int* pre, int batch) {
+  const int lane = threadIdx.x & 31, per = (batch + 31) / 32;
+  const int b0 = min(lane * per, batch), b1 = min(b0 + per, batch);
+  int sum = 0;
+  for (int b = b0; b < b1; ++b) sum += pre[b + 1];
+  int incl = sum;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int v = __shfl_up_sync(0xffffffffu, incl, o);
+    if (lane >= o) incl += v;
+  }
+  int acc = incl - sum;
+  for (int b = b0; b < b1; ++b) {
+    acc += pre[b + 1];
+    pre[b + 1] = acc;
+  }
+  if (lane == 0) pre[0] = 0;
+}
+// The same for a CTA: every thread calls it.
 __device__ __forceinline__ void scan_counts(int* pre, int batch) {
   __syncthreads();
-  if (threadIdx.x < 32) {
-    const int lane = threadIdx.x, per = (batch + 31) / 32;
-    const int b0 = min(lane * per, batch), b1 = min(b0 + per, batch);
-    int sum = 0;
-    for (int b = b0; b < b1; ++b) sum += pre[b + 1];
-    int incl = sum;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int v = __shfl_up_sync(0xffffffffu, incl, o);
-      if (lane >= o) incl += v;
-    }
-    int acc = incl - sum;
-    for (int b = b0; b < b1; ++b) {
-      acc += pre[b + 1];
-      pre[b + 1] = acc;
-    }
-    if (lane == 0) pre[0] = 0;
-  }
+  if (threadIdx.x < 32) scan_warp(pre, batch);
   __syncthreads();
 }
 __device__ __forceinline__ int seq_of_item(const int* pre, int batch, int x) {

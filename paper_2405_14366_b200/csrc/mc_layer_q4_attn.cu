@@ -31,9 +31,9 @@
 
 namespace mc {
 
-constexpr int kLqWarps = 12;
+constexpr int kLqWarps = 6;
 constexpr int kLqThreads = kLqWarps * 32;
-constexpr int kLqCtasPerSm = 1;
+constexpr int kLqCtasPerSm = 2;
 constexpr int kLqStages = 2;
 constexpr int kLqStageBytes = 2 * (kLqCodeBytes + kLqMetaBytes);
 constexpr int kLqVCodes = kLqCodeBytes, kLqKMeta = 2 * kLqCodeBytes, kLqVMeta = kLqKMeta + kLqMetaBytes;  // within a stage
@@ -57,6 +57,7 @@ struct LayerQ4Params {
   float* part_o;   // [team + sequence][n_q_heads][128], then [sequence][n_q_heads][128] of the 16-bit rows
   float* part_ml;  // [...][2]
   int res_part;    // first row of the latter
+  int4* pieces;    // [batch]: first team, number of teams that have pages of a sequence, whether it has 16-bit rows
   int nq, n_q_heads;
   int members, n_teams;  // warps of a team, teams
   int flags;
@@ -99,8 +100,9 @@ __device__ __forceinline__ Q4Prefix q4_prefix_at(void* smem, int batch) {
   return f;
 }
 __device__ __forceinline__ void q4_scan(const Q4Prefix& f, int batch) {
-  scan_counts(f.pages, batch);
-  scan_counts(f.begun, batch);
+  __syncthreads();
+  if (threadIdx.x < 64) scan_warp(threadIdx.x < 32 ? f.pages : f.begun, batch);
+  __syncthreads();
 }
 __device__ __forceinline__ int q4_total(const Q4Prefix& f, int batch) { return f.pages[batch] + kLqBegunUnits * f.begun[batch]; }
 __device__ __forceinline__ int q4_live_teams(const LayerQ4Params& p, int units) { return min(p.n_teams, max(units, 1)); }
@@ -390,14 +392,26 @@ layer_q4_split_kernel(const __grid_constant__ LayerQ4Params p, const __grid_cons
     }
     return page * H + t.meta;
   };
-  Tile first = load_tile(lane), ahead = load_tile(32 + lane);
+  const Tile first = load_tile(lane);
   if (p.sel == nullptr) grid_dep_wait();
   if (bad && blockIdx.x == 0) atomicOr(p.status, MC_FLAG_BAD_METADATA);  // (every thread has looked at other sequences)
+  if (blockIdx.x == gridDim.x - 1) {  // for the kernel behind
+    const long long units = q4_total(pre, p.g.batch);
+    const int teams = q4_live_teams(p, (int)units);
+    for (int b = tid; b < p.g.batch; b += kLqThreads) {
+      const int u0 = pre.pages[b], u = pre.pages[b + 1] - u0;
+      // the team of unit x is the last c with floor(units c / teams) <= x
+      const int c0 = u > 0 ? (int)(((long long)(u0 + 1) * teams - 1) / units) : 0;
+      const int c1 = u > 0 ? (int)(((long long)(u0 + u) * teams - 1) / units) : -1;
+      p.pieces[b] = make_int4(c0, c1 - c0 + 1, pre.begun[b + 1] - pre.begun[b], 0);
+    }
+  }
 
   const uint32_t bar0 = smem_u32(bars + warp * kLqStages);
   const uint32_t st0 = smem_u32(smem) + warp * kLqStages * kLqStageBytes;
   // Copies run kLqStages - 1 tiles ahead: tile j into stage j % kLqStages.  `tiles`: a lane per tile, 32 of them.
   int tiles = tile_of(first);
+  Tile ahead;
   int j = 0;
   auto issue = [&](uint32_t st_j, uint32_t bar_j) {
     if (j >= n_tiles) return;
@@ -416,6 +430,7 @@ layer_q4_split_kernel(const __grid_constant__ LayerQ4Params p, const __grid_cons
     ++j;
   };
   for (int i = 0; i < kLqStages - 1; ++i) issue(st0 + i * kLqStageBytes, bar0 + 8 * i);
+  ahead = load_tile(32 + lane);
   for (int k = sh.g0; k < sh.g1; ++k) {  // the begun pages of the warp's share
     const int b = seq_of_item(pre.begun, p.g.batch, k);
     for (int hd = 0; hd < sh.n_heads; ++hd) q4_begun_page<DT>(p, b, sh.member + hd * p.members);
@@ -770,36 +785,21 @@ constexpr int kLqCombWarps = kLqCombThreads / 32;
 template <int DT, int R>
 __global__ void __launch_bounds__(kLqCombThreads) layer_q4_combine_kernel(const __grid_constant__ LayerQ4Params p) {
   grid_dep_launch();
-  __shared__ int pre_s[2 * (kMaxLayerBatch + 1)];
   __shared__ float4 acc_s[kLqCombWarps][32];
   __shared__ float l_s[kLqCombWarps], m_s[kLqCombWarps];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int b = blockIdx.y;
-  if (p.sel != nullptr) grid_dep_wait();
-  const Q4Prefix pre = q4_prefix_at(pre_s, p.g.batch);
-  int bad = 0;
-  for (int i = tid; i < p.g.batch; i += kLqCombThreads) {
-    PageView v;
-    int begun;
-    pre.pages[i + 1] = q4_units(p, i, v, begun, bad);
-    pre.begun[i + 1] = begun;
-  }
-  q4_scan(pre, p.g.batch);
-  const long long U = q4_total(pre, p.g.batch);
-  const int T = q4_live_teams(p, (int)U);
-  const int x0 = pre.pages[b], u = pre.pages[b + 1] - x0, begun = pre.begun[b + 1] - pre.begun[b];
-  // the team of unit x is the last c with floor(U c / T) <= x
-  const int c0 = u > 0 ? (int)(((long long)(x0 + 1) * T - 1) / U) : 0;
-  const int c1 = u > 0 ? (int)(((long long)(x0 + u) * T - 1) / U) : -1;
   constexpr int GP = kLqCombWarps / R;  // warps per output row
   const int grp = warp % GP;
   const int hq = blockIdx.x * R + warp / GP;
   const bool active = hq < p.n_q_heads;
-  if (p.sel == nullptr) grid_dep_wait();
+  grid_dep_wait();
+  const int4 pc = __ldcg(p.pieces + b);
+  const int c0 = pc.x, n_pages = pc.y, begun = pc.z;
   float M = -INFINITY, L = 0.f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
   if (active) {
-    const int n_pages = c1 - c0 + 1, n_parts = n_pages + begun;
+    const int n_parts = n_pages + begun;
     for (int c = grp; c < n_parts; c += 4 * GP) {  // four parts in flight
       float2 ml[4];
       float4 v[4];
@@ -878,7 +878,7 @@ __global__ void __launch_bounds__(kLqCombThreads) layer_q4_combine_kernel(const 
 struct LayerQ4Plan {
   int members, n_teams;
   long long max_units;
-  size_t rows, o_bytes, ml_bytes;
+  size_t rows, o_bytes, ml_bytes, piece_bytes;
 };
 // The workspace is sized for kLqMaxCtas CTAs, so that its size needs no device.
 constexpr int kLqMaxCtas = 512;
@@ -892,6 +892,7 @@ static LayerQ4Plan layer_q4_plan(const mc_config* cfg, const mc_batch* bt, int c
   pl.rows = (size_t)(pl.n_teams + bt->batch) * cfg->n_q_heads + (size_t)bt->batch * cfg->n_q_heads;
   pl.o_bytes = align_up(pl.rows * kHeadDim * 4, 256);
   pl.ml_bytes = align_up(pl.rows * 2 * 4, 256);
+  pl.piece_bytes = align_up((size_t)bt->batch * sizeof(int4), 256);
   return pl;
 }
 static constexpr size_t q4_smem_bytes(int batch) {
@@ -901,7 +902,7 @@ static_assert(q4_smem_bytes(kMaxLayerBatch) <= 227 * 1024, "a CTA's shared memor
 
 size_t layer_q4_attn_workspace_bytes(const mc_config* cfg, const mc_batch* bt, int) {
   const LayerQ4Plan pl = layer_q4_plan(cfg, bt, kLqMaxCtas);
-  return pl.o_bytes + pl.ml_bytes;
+  return pl.o_bytes + pl.ml_bytes + pl.piece_bytes;
 }
 
 mc_status launch_layer_q4_attn(const mc_config* cfg, const mc_batch* bt, const Geom& g, const mc_layer_q4_cache* layer,
@@ -937,6 +938,7 @@ mc_status launch_layer_q4_attn(const mc_config* cfg, const mc_batch* bt, const G
   ap.sel_stride = pages_stride;
   ap.part_o = (float*)workspace;
   ap.part_ml = (float*)((char*)workspace + pl.o_bytes);
+  ap.pieces = (int4*)((char*)workspace + pl.o_bytes + pl.ml_bytes);
   ap.nq = cfg->n_q_heads / cfg->n_kv_heads;
   ap.n_q_heads = cfg->n_q_heads;
   ap.members = pl.members;
