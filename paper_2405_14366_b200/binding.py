@@ -172,7 +172,8 @@ class Batch:
         """c() for the mc_layer_* calls: a row of the block table for every sequence, both tensors on device dev."""
         bt, sl = self.block_table, self.seq_lens
         n, pages = sl.numel(), bt.size(1) if bt.dim() == 2 else -1
-        if not (pages >= 0 and bt.size(0) >= n and _good(bt, torch.int32, 0, dev) and _good(sl, torch.int32, 0, dev)):
+        if not (pages >= 0 and bt.size(0) >= n and bt.dtype is torch.int32 and sl.dtype is torch.int32 and bt.is_contiguous()
+                and sl.is_contiguous() and (dev is None or (bt.get_device() == dev and sl.get_device() == dev))):
             _refuse(dev, block_table=(bt, torch.int32, 0), seq_lens=(sl, torch.int32, 0))
             raise AssertionError("block_table [batch][max_pages_per_seq] and seq_lens [batch] are wanted")
         return _Batch(bt.data_ptr(), sl.data_ptr(), n, pages, int(self.max_seq_len), 0, int(self.n_pages))
@@ -455,9 +456,14 @@ class LayerQ4Cache:
         cfg = cfg or self.cfg
         dt, tiles, begun = cfg.torch_dtype, n_pages * cfg.n_kv_heads, batch * cfg.n_kv_heads * 4096
         kc, km, vc, vm, rk, rv, st = self.k_codes, self.k_meta, self.v_codes, self.v_meta, self.res_k, self.res_v, self.status
-        if not (_good(kc, torch.uint8, 2048 * tiles, dev) and _good(km, torch.float16, 256 * tiles, dev)
-                and _good(vc, torch.uint8, 2048 * tiles, dev) and _good(vm, torch.float16, 256 * tiles, dev)
-                and _good(rk, dt, begun, dev) and _good(rv, dt, begun, dev) and _good(st, torch.int32, MC_STATUS_WORDS, dev)):
+        if not (kc.dtype is torch.uint8 and vc.dtype is torch.uint8 and km.dtype is torch.float16 and vm.dtype is torch.float16
+                and rk.dtype is dt and rv.dtype is dt and st.dtype is torch.int32
+                and kc.numel() >= 2048 * tiles and vc.numel() >= 2048 * tiles and km.numel() >= 256 * tiles and vm.numel() >= 256 * tiles
+                and rk.numel() >= begun and rv.numel() >= begun and st.numel() >= MC_STATUS_WORDS
+                and kc.is_contiguous() and vc.is_contiguous() and km.is_contiguous() and vm.is_contiguous() and rk.is_contiguous()
+                and rv.is_contiguous() and st.is_contiguous()
+                and (dev is None or (kc.get_device() == dev and vc.get_device() == dev and km.get_device() == dev and vm.get_device() == dev
+                                     and rk.get_device() == dev and rv.get_device() == dev and st.get_device() == dev))):
             _refuse(dev, k_codes=(kc, torch.uint8, 2048 * tiles), k_meta=(km, torch.float16, 256 * tiles),
                     v_codes=(vc, torch.uint8, 2048 * tiles), v_meta=(vm, torch.float16, 256 * tiles), res_k=(rk, dt, begun),
                     res_v=(rv, dt, begun), status=(st, torch.int32, MC_STATUS_WORDS))

@@ -73,17 +73,19 @@ __device__ __forceinline__ int q4_page_of(const Q4Seq& s, int k) {  // (as page_
   const int ua = (min(s.a, s.n / kLqPage * kLqPage) + kLqPage - 1) / kLqPage;
   return k < ua ? k : max(s.lo / kLqPage, ua) + k - ua;
 }
-// Complete pages of sequence b that the call attends; `begun`: 1 if there are 16-bit rows too.
-__device__ __forceinline__ int q4_units(const LayerQ4Params& p, int b, PageView& v, int& begun, int& bad) {
+// A sequence as the call sees it; `begun`: 1 if there are 16-bit rows (the begun page's, the step's new one).
+__device__ __forceinline__ PageView q4_view(const LayerQ4Params& p, int b, int& begun, int& bad) {
   const int raw = __ldcg(p.g.seq_lens + b);
   bad |= (raw < 0 || raw > p.g.max_seq_len) ? 1 : 0;
   const int n = min(max(raw, 0), p.g.max_seq_len), n_tot = n + (p.k_new != nullptr ? 1 : 0);
-  v = page_view(p.rule, b, n, n_tot, n_tot - 1);
   begun = n_tot > n / kLqPage * kLqPage ? 1 : 0;
-  if (p.sel == nullptr) return v.u;
-  const int c = __ldcg(p.counts + b);
-  bad |= (c < 0 || c > p.sel_stride || c > n / kLqPage) ? 1 : 0;
-  return min(max(c, 0), min(p.sel_stride, n / kLqPage));
+  return page_view(p.rule, b, n, n_tot, n_tot - 1);
+}
+// Pages of sequence b, of n tokens, in the selection.
+__device__ __forceinline__ int q4_selected(const LayerQ4Params& p, int b, int n, int& bad) {
+  const int c = __ldcg(p.counts + b), most = min(p.sel_stride, n / kLqPage);
+  bad |= (c < 0 || c > most) ? 1 : 0;
+  return min(max(c, 0), most);
 }
 
 // The units of a call: all pages, sequence by sequence, then the begun pages, which count for kLqBegunUnits each (a begun
@@ -186,8 +188,7 @@ __device__ __noinline__ void q4_begun_page(const LayerQ4Params& p, int b, int he
   const int lane = threadIdx.x & 31, row = lane >> 2, t4 = lane & 3, colp = 2 * t4;
   const int nq = p.nq, H = p.g.n_kv_heads;
   int bad = 0, begun;
-  PageView v;
-  q4_units(p, b, v, begun, bad);
+  const PageView v = q4_view(p, b, begun, bad);
   const int n = v.n, base = n / kLqPage * kLqPage, n_tot = n + (p.k_new != nullptr ? 1 : 0);
   const size_t at = ((size_t)b * H + head) * kLqResBytes, new_at = ((size_t)b * H + head) * kRowBytes;
   const size_t prow = (size_t)p.res_part + (size_t)b * p.n_q_heads + head * nq;
@@ -345,14 +346,19 @@ layer_q4_split_kernel(const __grid_constant__ LayerQ4Params p, const __grid_cons
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   // (lengths, block table and score options are the caller's: read before the wait; a selection is what the kernel ahead wrote)
-  if (p.sel != nullptr) grid_dep_wait();
+  if (tid * 32 < p.g.batch * p.g.max_pages_per_seq)  // the block table, or its first lines, on its way to L2 meanwhile
+    asm volatile("prefetch.global.L2 [%0];" ::"l"(p.g.block_table + tid * 32));
   int bad = 0;
   for (int b = tid; b < p.g.batch; b += kLqThreads) {
-    PageView v;
     int begun;
-    pre.pages[b + 1] = q4_units(p, b, v, begun, bad);
+    const PageView v = q4_view(p, b, begun, bad);
+    pre.pages[b + 1] = v.u;
     pre.begun[b + 1] = begun;
     seq_s[b] = Q4Seq{v.n, v.q_pos, v.a, v.lo, v.hi};
+  }
+  if (p.sel != nullptr) {
+    grid_dep_wait();
+    for (int b = tid; b < p.g.batch; b += kLqThreads) pre.pages[b + 1] = q4_selected(p, b, seq_s[b].n, bad);
   }
   q4_scan(pre, p.g.batch);
 
