@@ -696,7 +696,7 @@ mc_status mc_layer_read_status(const mc_layer_cache* layer, void* stream, int32_
  *   mc_layer_q4: what mc_layer_q4_append wrote is what mc_merge_pair_q4 reads (for sequences of whole pages). */
 
 /* k_codes, k_meta, v_codes, v_meta  the pools of mc_layer_q4, [n_pages] pages.  value = code * scale + zero; scales are
- *                                   positive and at most 16000 (mc_layer_q4_append writes none above 8736)
+ *                                   positive and at most 16000 (mc_layer_q4_append writes none above 8736), zeros finite
  * res_k, res_v  [batch][n_kv_heads][32][128] of cfg->dtype: the rows of the begun page, token t at slot t % 32; slots
  *               behind the sequence's last token may hold anything
  * status        [MC_STATUS_WORDS] int32, cleared by the caller; flags accumulate.  All but status 256-byte aligned. */
@@ -756,7 +756,7 @@ typedef struct mc_page_selection {
  * pages      [batch][n_kv_heads][budget] int32: page slots of the sequence (block-table columns), ascending; entries behind
  *            the count are left as they were
  * counts     [batch] int32: min(budget, pages with a visible token), the same for every kv head
- * workspace  mc_layer_workspace_bytes(MC_OP_LAYER_Q4_SELECT, 0) bytes, 256-byte aligned.  max_seq_len at most 2^20. */
+ * workspace  mc_layer_workspace_bytes(MC_OP_LAYER_Q4_SELECT, 0) bytes, 256-byte aligned.  max_seq_len at most 2^19. */
 mc_status mc_layer_q4_select(const mc_config* cfg, const mc_batch* batch, const mc_layer_q4_cache* layer, const mc_score_opts* opts,
                              const mc_page_selection* keep, const void* q, int32_t* pages, int32_t* counts, void* workspace,
                              size_t workspace_bytes, void* stream);

@@ -4,7 +4,7 @@
 
 namespace mc {
 
-constexpr int kQ4MaxSelectLen = 1 << 20;  // longest sequence mc_layer_q4_select takes: a key per page in shared memory
+constexpr int kQ4MaxSelectLen = 1 << 19;  // longest sequence mc_layer_q4_select takes: a key per page in shared memory
 
 // Rows of the append and read calls, in the caller's arrays.
 struct Q4RowArgs {

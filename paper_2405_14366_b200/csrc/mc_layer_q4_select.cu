@@ -5,8 +5,9 @@
 // over the kv head's query heads h (lo = zero, hi = zero + 15 scale, scale > 0: what channel c of a key of the page can hold).
 // The keys' group parameters are the bounds already: 512 of a page's 5120 bytes are read, nothing else of the cache.
 // Sums are held in 64 bits: the last page in and the first one out differ by less than binary32 resolves often enough
-// that the choice would hang on the order of a sum.  (256 products a page are 4 cycles of the SM's 64-bit units, their
-// operands' conversions 16; the page's bytes take 22 at the memory's rate.)
+// that the choice would hang on the order of a sum.  (256 products a page are 4 cycles of the SM's 64-bit units; the page's bytes
+// take 22 at the memory's rate.  Conversions, at 16 an SM and cycle, took as long as all the rest: the operands are put
+// together from their bits, see tiny_zero.)
 // A cluster of CTAs per (sequence, kv head) forms the sums; their binary32 roundings, which keep the order, go to the first
 // CTA's shared memory, where a radix select finds the last one in.  Pages that round alike there are told apart by the
 // 64-bit sums, and equal ones by their index.
@@ -22,7 +23,9 @@ namespace mc {
 constexpr int kLsThreads = 512;
 constexpr int kLsWarps = kLsThreads / 32;
 constexpr int kLsMaxCluster = 8;
-constexpr int kLsBatch = 8;  // pages of a warp at a time
+constexpr int kLsBatch = 4;   // pages of a warp at a time
+constexpr int kLsStages = 4;  // batches of a warp in shared memory: one worked on, three on their way
+constexpr int kLsRing = kLsWarps * kLsStages * kLsBatch * kLqMetaBytes;
 constexpr int kLsBins = 2048;
 
 struct Q4SelectParams {
@@ -48,6 +51,11 @@ __device__ __forceinline__ unsigned long long order64(double x) {
   const unsigned long long b = (unsigned long long)__double_as_longlong(x);
   return x != x ? 0ull : (b >> 63) ? ~b : b | (1ull << 63);
 }
+// 2^-1008 times the binary16 number in the high (low, positive) half of w, finite, as a double: its exponent and mantissa in
+// their places, its exponent not rebased -- a subnormal number too, as both formats count those in the unit of their lowest
+// binade.
+__device__ __forceinline__ double tiny_zero(uint32_t w) { return __hiloint2double((int)((w & 0x80000000u) | ((w >> 6) & 0x01fffc00u)), 0); }
+__device__ __forceinline__ double tiny_scale(uint32_t w) { return __hiloint2double((int)((w << 10) & 0x01fffc00u), 0); }
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 __device__ __forceinline__ void store_first_cta(uint32_t* smem, uint32_t v) {
@@ -57,9 +65,10 @@ __device__ __forceinline__ void store_first_cta(uint32_t* smem, uint32_t v) {
 }
 
 template <int DT>
-__global__ void __launch_bounds__(kLsThreads) layer_q4_select_kernel(const __grid_constant__ Q4SelectParams p) {
+__global__ void __launch_bounds__(kLsThreads, 1) layer_q4_select_kernel(const __grid_constant__ Q4SelectParams p) {
   grid_dep_launch();
-  extern __shared__ uint32_t keys_s[];  // [pages] of the first CTA
+  extern __shared__ __align__(16) unsigned char select_smem[];
+  uint32_t* keys_s = reinterpret_cast<uint32_t*>(select_smem + kLsRing);  // [pages] of the first CTA
   __shared__ uint32_t hist[kLsBins];
   __shared__ uint32_t scan_s[kLsWarps], pick_s[3];
   __shared__ int ins_s[kLsWarps], ties_s[kLsWarps];
@@ -96,51 +105,64 @@ __global__ void __launch_bounds__(kLsThreads) layer_q4_select_kernel(const __gri
       }
     }
 #pragma unroll
-    for (int c = 0; c < 4; ++c) P[c] *= 15.0;
-    // The warp's pages: batches of eight, every (cluster * warps)-th.  A lane knows the page of one of the next 32 (four batches);
-    // the next batch's parameters are on their way while one is worked on.
+    for (int c = 0; c < 4; ++c) {
+      P[c] *= 15.0 * 0x1p504;  // (what the tiny numbers lack is put back in two steps: 2^1008 times a query overflows)
+      Q[c] *= 0x1p504;
+    }
+    // The warp's pages: batches of four, every (cluster * warps)-th.  A lane knows the page of one of the next 32 (eight batches);
+    // three batches' parameters are on their way while one is worked on, each lane's 16 bytes of a page to where it reads them.
     const int step = p.cluster * kLsWarps * kLsBatch, first = (rank * kLsWarps + warp) * kLsBatch;
-    auto pages_from = [&](int k) {  // lane: page (lane & 7) of the batch k + (lane >> 3) step
-      const int at = k + (lane >> 3) * step + (lane & 7);
+    auto pages_from = [&](int k) {  // lane: page (lane & 3) of the batch k + (lane >> 2) step
+      const int at = k + (lane >> 2) * step + (lane & 3);
       if (at >= u) return 0;
       const int page = checked_page(p.g, b, v.page_of(at), p.status);
       return page < 0 ? 0 : page;
     };
-    int ids = pages_from(first), ids_next = pages_from(first + 4 * step), turn = 0;
-    uint4 m[kLsBatch];
-    auto fetch = [&](int t) {
+    int ids = pages_from(first), ids_next = pages_from(first + 8 * step), turn = 0, k_ahead = first, slot = 0;
+    const unsigned char* meta = p.k_meta + (size_t)head * kLqMetaBytes + 16 * lane;
+    unsigned char* ring = select_smem + warp * (kLsStages * kLsBatch * kLqMetaBytes) + 16 * lane;
+    const uint32_t ring_s = (uint32_t)__cvta_generic_to_shared(ring);
+    int slot_ahead = 0;
+    auto issue = [&]() {
+      if (k_ahead < u) {
 #pragma unroll
-      for (int j = 0; j < kLsBatch; ++j) {
-        const int page = __shfl_sync(0xffffffffu, ids, 8 * t + j);
-        m[j] = *reinterpret_cast<const uint4*>(p.k_meta + ((size_t)page * H + head) * kLqMetaBytes + 16 * lane);
+        for (int j = 0; j < kLsBatch; ++j) {
+          const int page = __shfl_sync(0xffffffffu, ids, 4 * turn + j);
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(ring_s + (slot_ahead * kLsBatch + j) * kLqMetaBytes),
+                       "l"(meta + (size_t)page * H * kLqMetaBytes)
+                       : "memory");
+        }
+        if (++turn == 8) {
+          turn = 0;
+          ids = ids_next;
+          ids_next = pages_from(k_ahead + 9 * step);
+        }
       }
+      asm volatile("cp.async.commit_group;" ::: "memory");
+      k_ahead += step;
+      slot_ahead = (slot_ahead + 1) % kLsStages;
     };
-    if (first < u) fetch(0);
+#pragma unroll
+    for (int i = 0; i < kLsStages - 1; ++i) issue();
     for (int k0 = first; k0 < u; k0 += step) {
+      asm volatile("cp.async.wait_group %0;" ::"n"(kLsStages - 2) : "memory");
       uint4 cur[kLsBatch];
 #pragma unroll
-      for (int j = 0; j < kLsBatch; ++j) cur[j] = m[j];
-      if (++turn == 4) {
-        turn = 0;
-        ids = ids_next;
-        ids_next = pages_from(k0 + 5 * step);
-      }
-      if (k0 + step < u) fetch(turn);
+      for (int j = 0; j < kLsBatch; ++j) cur[j] = *reinterpret_cast<const uint4*>(ring + (slot * kLsBatch + j) * kLqMetaBytes);
+      slot = (slot + 1) % kLsStages;
+      issue();  // (into the batch read before this one)
       double a[kLsBatch];
 #pragma unroll
       for (int j = 0; j < kLsBatch; ++j) {
         const uint32_t w[4] = {cur[j].x, cur[j].y, cur[j].z, cur[j].w};
         double t = 0.0;
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          const float2 sz = Elem<MC_F16>::unpack(w[c]);
-          t = fma(Q[c], (double)sz.y, fma(P[c], (double)sz.x, t));
-        }
+        for (int c = 0; c < 4; ++c) t = fma(P[c], tiny_scale(w[c]), fma(Q[c], tiny_zero(w[c]), t));
         a[j] = t;
       }
-      // eight sums over the warp, halving the pages a lane keeps: lane 4 j ends with page j
+      // four sums over the warp, halving the pages a lane keeps: lane 8 j ends with page j
 #pragma unroll
-      for (int o = 16, c = 4; c > 0; o >>= 1, c >>= 1) {
+      for (int o = 16, c = 2; c > 0; o >>= 1, c >>= 1) {
         const bool up = (lane & o) != 0;
 #pragma unroll
         for (int j = 0; j < c; ++j) {
@@ -148,12 +170,12 @@ __global__ void __launch_bounds__(kLsThreads) layer_q4_select_kernel(const __gri
           a[j] = keep + __shfl_xor_sync(0xffffffffu, give, o);
         }
       }
-      a[0] += __shfl_xor_sync(0xffffffffu, a[0], 2);
-      a[0] += __shfl_xor_sync(0xffffffffu, a[0], 1);
-      const int k = k0 + (lane >> 2);
-      if ((lane & 3) == 0 && k < u) {
+#pragma unroll
+      for (int o = 4; o > 0; o >>= 1) a[0] += __shfl_xor_sync(0xffffffffu, a[0], o);
+      const int k = k0 + (lane >> 3);
+      if ((lane & 7) == 0 && k < u) {
         const int slot = v.page_of(k);
-        const double x = a[0] + 0.0;  // (-0 counts as 0)
+        const double x = a[0] * 0x1p504 + 0.0;  // (-0 counts as 0)
         const bool guarded = slot < p.n_sink || slot >= full - p.n_recent;
         keys[k] = guarded ? ~0ull : order64(x);
         store_first_cta(keys_s + k, guarded ? 0xffffffffu : order32((float)x));
@@ -336,11 +358,11 @@ mc_status launch_layer_q4_select(const mc_config* cfg, const mc_batch* bt, const
   while (cluster < kLsMaxCluster && segs * cluster * 2 <= n_sm && sp.key_stride >= 2 * cluster * kLsWarps * kLsBatch) cluster *= 2;
   sp.cluster = cluster;
   auto* kernel = cfg->dtype == MC_F16 ? layer_q4_select_kernel<MC_F16> : layer_q4_select_kernel<MC_BF16>;
-  MC_CUDA_CHECK(allow_smem(kernel, (size_t)kQ4MaxSelectLen / kLqPage * 4));
+  MC_CUDA_CHECK(allow_smem(kernel, kLsRing + (size_t)kQ4MaxSelectLen / kLqPage * 4));
   cudaLaunchConfig_t lc = {};
   lc.gridDim = dim3((unsigned)(segs * cluster));
   lc.blockDim = dim3(kLsThreads);
-  lc.dynamicSmemBytes = (size_t)sp.key_stride * 4;
+  lc.dynamicSmemBytes = kLsRing + (size_t)sp.key_stride * 4;
   lc.stream = stream;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;

@@ -92,7 +92,7 @@ def test_select_refusals(L):
     assert call(q=0x100008) == 4 and call(pages=0x200002) == 4 and call(counts=0x300001) == 4
     assert call(counts=0x2000) == 1 and call(counts=0x2004) == 1 and call(o=opts(q_pos=0x300004)) == 1  # over what it reads
     assert call(ws=0) == 1 and call(ws=0x500080) == 4 and call(n=16) == 5
-    assert call(b=batch(max_len=2 ** 20 + 1, mpps=2 ** 16)) == 2
+    assert call(b=batch(max_len=2 ** 19 + 1, mpps=2 ** 16)) == 2
     assert call(b=batch(batch=0, bt=0, sl=0)) == 0
     c, b, l, o = cfg(), batch(), layer(), opts()
     assert L.mc_layer_q4_select(C.byref(c), C.byref(b), C.byref(l), None, C.byref(B._PageSelection(4, 0, 0, 0)), 16, 16, 0x300000, 0x500000, 1 << 30, None) == 1
@@ -126,7 +126,7 @@ def test_workspace_refusals(L):
         assert call(op) == 0 and out.value % 256 == 0 and out.value > 0
         assert call(op, 2) == 1 and call(op, c=cfg(page_size=16, cache_bits=0)) == 2
         assert call(op, b=batch(batch=513)) == 2 and call(op, b=batch(max_len=2 ** 30 + 1)) == 2 and call(op, b=batch(batch=512, max_len=2 ** 25)) == 2
-    assert call(5, 1) == 0 and call(6, 1) == 1 and call(6, b=batch(max_len=2 ** 20 + 1)) == 2 and call(7) == 1
+    assert call(5, 1) == 0 and call(6, 1) == 1 and call(6, b=batch(max_len=2 ** 19 + 1)) == 2 and call(7) == 1
 
 
 def test_binding_refuses_other_tensors():
