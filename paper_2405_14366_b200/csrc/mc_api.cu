@@ -138,7 +138,7 @@ using namespace mc;
 
 extern "C" {
 
-int32_t mc_version(void) { return 240; }
+int32_t mc_version(void) { return 250; }
 
 int32_t mc_build_flags(void) {
 #if defined(MC_BOUNDS) && MC_BOUNDS

@@ -346,7 +346,7 @@ layer_q4_split_kernel(const __grid_constant__ LayerQ4Params p, const __grid_cons
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   // (lengths, block table and score options are the caller's: read before the wait; a selection is what the kernel ahead wrote)
-  if (tid * 32 < p.g.batch * p.g.max_pages_per_seq)  // the block table, or its first lines, on its way to L2 meanwhile
+  if (tid * 32 < (long long)p.g.batch * p.g.max_pages_per_seq)  // the block table, or its first lines, on its way to L2 meanwhile
     asm volatile("prefetch.global.L2 [%0];" ::"l"(p.g.block_table + tid * 32));
   int bad = 0;
   for (int b = tid; b < p.g.batch; b += kLqThreads) {
@@ -465,8 +465,7 @@ layer_q4_split_kernel(const __grid_constant__ LayerQ4Params p, const __grid_cons
       int slot_last = list && k0 > 0 ? __ldcg(list + k0 - 1) : -1;
 
       // Query pairs (channels 8w + i, 8w + i + 4 of the lane's 32), as binary16 with the row's power of two taken out: the
-      // row's largest number becomes 2 to 4.  q_back, of the lane's result column(s): what puts it back, and (without a
-      // cap) the scores' scale.
+      // row's largest number becomes 2 to 4.  q_back, of the lane's result column(s), puts it back.
       uint32_t qh[16];
       float q_back, q_back1 = 0.f;
       {
@@ -491,7 +490,7 @@ layer_q4_split_kernel(const __grid_constant__ LayerQ4Params p, const __grid_cons
         big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 2));
         const int e = min(max(__float_as_int(big) >> 23, 2), 253);
         const float f = __int_as_float((255 - e) << 23);
-        const float back = __int_as_float((e - 1) << 23) * (p.rule.cap_log2 > 0.f ? 1.f : p.rule.scale_log2);
+        const float back = __int_as_float((e - 1) << 23);
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
           const uint32_t y[4] = {w[c].x, w[c].y, w[c].z, w[c].w};
@@ -629,6 +628,13 @@ layer_q4_split_kernel(const __grid_constant__ LayerQ4Params p, const __grid_cons
             }
           }
         // ---- masks, the scores' form, the distance bias
+        if (!(p.rule.cap_log2 > 0.f)) {  // (behind q_back: their product may be no number where the score is one)
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            sc[c] *= p.rule.scale_log2;
+            if (WIDE) sa[c] *= p.rule.scale_log2;
+          }
+        }
         uint32_t hidden = 0;  // bit r: token t0 + r is not seen
         const bool whole = (t0 + kLqPage <= sq.a || (t0 >= sq.lo && t0 + kLqPage <= sq.hi)) && slot >= 0;
         if (!whole || unusual) {

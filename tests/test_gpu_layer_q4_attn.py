@@ -141,6 +141,21 @@ def test_queries_of_zeros_and_of_one_channel(Q, Hq):
     run(Q, c, q=q)
 
 
+@pytest.mark.parametrize("Hq", [2, 8, 16])
+def test_scales_of_scores_at_their_limits(Q, Hq):
+    c = Q.Cache([100, 32, 5], 2, Hq, "bf16", seed=9)
+    q = torch.zeros(3, Hq, 128, dtype=c.dt)
+    q[:, :, 3] = 100.0
+    q[1] = 0
+    out, lse, *_ = run(Q, c, q=q * 0, sm=2.0e38, new=False)  # all alike
+    assert (lse.cpu() - torch.tensor([100.0, 32.0, 5.0]).log()[:, None]).abs().max() < 1e-5
+    run(Q, c, q=q, sm=1e-38)
+    run(Q, c, q=q, sm=0.0)
+    run(Q, c, q=q, sm=-0.02)
+    run(Q, c, q=q * 1e-30, sm=1e30)
+    run(Q, c, q=q * 1e30, sm=1e-31, cap=20.0)
+
+
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
 @pytest.mark.parametrize("H,Hq", [(2, 2), (3, 12), (2, 16)])
 def test_append_step_by_step_through_page_ends(Q, dtype, H, Hq):
