@@ -227,6 +227,48 @@ def test_no_output_beyond_what_is_asked_for(Q):
     assert (out[0] == 0).all() and not (out[1:] == 5).any() and c.same_as_host() is None
 
 
+def test_the_readme_snippet(Q, repo_root):
+    """README's loop over a 4-bit layer, as it stands there: every step against the definition over what the cache should hold."""
+    import os
+    import re
+    with open(os.path.join(repo_root, "README.md")) as f:
+        (code,) = [b for b in re.findall(r"```python\n(.*?)```", f.read(), re.S) if "LayerQ4Cache.empty(" in b]
+    lens, H, Hq, n_steps = [2500, 70, 1], 2, 8, 40
+    c = Q.Cache([0] * 3, H, Hq, "f16", seed=3, room=max(lens) + n_steps, max_len=2560, empty=True)
+    mc, g = c.mc, c.g
+    rows = [[c.rows(n + n_steps, H) for n in lens] for _ in range(2)]
+    k, v = (torch.cat([x[:n] for x, n in zip(r, lens)]).cuda() for r in rows)
+    off = torch.tensor([0] + np.cumsum(lens).tolist(), dtype=torch.int32, device="cuda")
+    ends = [n + n_steps for n in lens]
+    steps = [(c.queries(3, Hq).cuda(), *(torch.stack([x[n + i] for x, n in zip(r, lens)]).cuda() for r in rows)) for i in range(n_steps)]
+    back = [torch.zeros(sum(ends), H, 128, dtype=c.dt, device="cuda") for _ in range(2)]
+    space = dict(mc=mc, torch=torch, lib=mc.lib(), cfg=c.cfg, batch_size=3, n_pages=c.n_pages, block_table=c.d["table"], max_seq_len=2560, k=k, v=v,
+                 offsets=off, sm_scale=SM, steps=steps, out=torch.zeros(3, Hq, 128, dtype=c.dt, device="cuda"), lse=torch.zeros(3, Hq, device="cuda"),
+                 k_back=back[0], v_back=back[1], row_offsets=torch.tensor([0] + np.cumsum(ends).tolist(), dtype=torch.int32, device="cuda"))
+    exec(compile(code, "README.md", "exec"), space)
+    torch.cuda.synchronize()
+    assert mc.lib().mc_layer_q4_read_status(space["layer"], check=False)[1] == 0 and space["seq_lens"].tolist() == ends
+    at = 0
+    for b, n in enumerate(lens):  # the host's cache one step before the end
+        c.put(b, *(r[b][:n + n_steps - 1] for r in rows))
+        c.lens[b] = n + n_steps - 1
+    q, kn, vn = (x.cpu() for x in steps[-1])
+    for b, n in enumerate(c.lens):
+        for h in range(H):
+            r = slice(4 * h, 4 * h + 4)
+            want = Q.select64(c, q[b, r], b, h, 64, 1, 2, n)
+            assert space["pages"][b, h, :len(want)].tolist() == want and int(space["counts"][b]) == len(want)
+            o, z, tol, ztol = Q.attn64(c, b, h, q[b, r], SM, k_new=kn[b, h], v_new=vn[b, h], pages=want)
+            assert ((space["out"][b, r].cpu().double() - o).abs() <= tol).all() and ((space["lse"][b, r].cpu().double() - z).abs() <= ztol).all()
+            kc, kz, vc, vz = c.values(b, h)
+            full = (n + 1) // 32 * 32 if (n + 1) % 32 == 0 else n // 32 * 32
+            keep = min(full, n // 32 * 32)
+            for got, want64 in ((back[0], kc + kz), (back[1], vc + vz)):
+                d = (got[at:at + keep, h].cpu().double() - want64[:keep]).abs()
+                assert (d <= want64[:keep].abs() * Q.H11 + 2.0 ** -25).all()
+        at += n + 1
+
+
 def test_pools_past_four_gigabytes(Q):
     """Pools of more than 2^32 bytes: the pages in use are the last ones."""
     import paper_2405_14366_b200 as mc
