@@ -690,7 +690,7 @@ mc_status mc_layer_read_status(const mc_layer_cache* layer, void* stream, int32_
  * (The paper has no counterpart: Sec. 5 puts MiniCache on top of a 4-bit cache and leaves that cache to the engine.)
  * - cfg->page_size is 32, one key group; cfg->cache_bits is not looked at.  The conventions and limits of "One
  *   uncompressed layer" hold (its own mc_batch, order of writing calls, batch at most 512), with units of 32 tokens:
- *   batch * n_kv_heads * (max_seq_len / 32 + 2) below 2^31.
+ *   batch * n_kv_heads * (max_seq_len / 32 + 4) below 2^31.
  * - Only complete pages are in the pools: the tokens [32 floor(n / 32), n) of a sequence of n are 16-bit rows of res_k
  *   and res_v.  The block table needs an entry for a page once the page is complete.  Complete pages are in the format of
  *   mc_layer_q4: what mc_layer_q4_append wrote is what mc_merge_pair_q4 reads (for sequences of whole pages). */

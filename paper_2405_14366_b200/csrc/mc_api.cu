@@ -709,7 +709,7 @@ static bool too_long(const mc_config* cfg, const mc_batch* batch) {
 }
 // The same for the pages of a layer held in 4 bits.
 static bool too_many_pages(const mc_config* cfg, const mc_batch* batch) {
-  return batch->max_seq_len > (1 << 30) || (int64_t)batch->batch * cfg->n_kv_heads * (batch->max_seq_len / kLqPage + 2) > 0x7fffffffLL;
+  return batch->max_seq_len > (1 << 30) || (int64_t)batch->batch * cfg->n_kv_heads * (batch->max_seq_len / kLqPage + 4) > 0x7fffffffLL;
 }
 // What every mc_layer_* call checks about its configuration, batch and cache.
 static mc_status check_layer(const mc_config* cfg, const mc_batch* batch, const mc_layer_cache* layer) {

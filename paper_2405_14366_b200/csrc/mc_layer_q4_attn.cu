@@ -88,9 +88,10 @@ __device__ __forceinline__ int q4_selected(const LayerQ4Params& p, int b, int n,
   return min(max(c, 0), most);
 }
 
-// The units of a call: all pages, sequence by sequence, then the begun pages, which count for kLqBegunUnits each (a begun
-// page is 16 KB and is not pipelined).
-constexpr int kLqBegunUnits = 3;
+// The units of a call: all pages, sequence by sequence, then the begun pages, which count for kLqBegunUnits each: one waits for the
+// memory behind the stream and is not pipelined, 3.5 us against a page's 1.5.  (8 x 4109 tokens of 32 heads / 16 x 64 selected pages of
+// 8: one unit 57 / 25 us, two 48 / 19, three 39.6 / 17.7, four 38.6 / 17.6, five 41 / 17.5; rows prefetched to L2 ahead: no gain.)
+constexpr int kLqBegunUnits = 4;
 struct Q4Prefix {
   int* pages;  // [batch + 1] exclusive prefixes
   int* begun;
@@ -184,18 +185,16 @@ __device__ __forceinline__ uint32_t highs(uint32_t a, uint32_t b) { return __byt
 // from global memory.  The k axis of the first product is the channels in the order in which a lane's 16-byte loads bring
 // them; in the second a lane's rows and channels are the ones the codes' kernel uses, so that outputs leave alike.
 template <int DT>
-__device__ __noinline__ void q4_begun_page(const LayerQ4Params& p, int b, int head) {
+__device__ __noinline__ void q4_begun_page(const LayerQ4Params& p, const Q4Seq v, int b, int head) {
   const int lane = threadIdx.x & 31, row = lane >> 2, t4 = lane & 3, colp = 2 * t4;
   const int nq = p.nq, H = p.g.n_kv_heads;
-  int bad = 0, begun;
-  const PageView v = q4_view(p, b, begun, bad);
   const int n = v.n, base = n / kLqPage * kLqPage, n_tot = n + (p.k_new != nullptr ? 1 : 0);
   const size_t at = ((size_t)b * H + head) * kLqResBytes, new_at = ((size_t)b * H + head) * kRowBytes;
   const size_t prow = (size_t)p.res_part + (size_t)b * p.n_q_heads + head * nq;
   uint32_t seen = 0;  // bit r: token base + r is attended
   {
     const int t = base + lane;
-    seen = __ballot_sync(0xffffffffu, t < n_tot && v.sees(t));
+    seen = __ballot_sync(0xffffffffu, t < n_tot && (t < v.a || (t >= v.lo && t < v.hi)));
   }
   float acc[8][4];
 #pragma unroll
@@ -439,7 +438,7 @@ layer_q4_split_kernel(const __grid_constant__ LayerQ4Params p, const __grid_cons
   ahead = load_tile(32 + lane);
   for (int k = sh.g0; k < sh.g1; ++k) {  // the begun pages of the warp's share
     const int b = seq_of_item(pre.begun, p.g.batch, k);
-    for (int hd = 0; hd < sh.n_heads; ++hd) q4_begun_page<DT>(p, b, sh.member + hd * p.members);
+    for (int hd = 0; hd < sh.n_heads; ++hd) q4_begun_page<DT>(p, seq_s[b], b, sh.member + hd * p.members);
   }
 
   uint32_t st_i = st0, bar_i = bar0, parity = 0;
