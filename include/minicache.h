@@ -720,9 +720,10 @@ enum { MC_OP_LAYER_Q4_ATTN = 5, MC_OP_LAYER_Q4_SELECT = 6 }; /* mc_layer_workspa
  * n_rows       rows in k and v, below 2^30
  * Pages that fill are quantised: zero = min and scale = (max - min) / 15 of a group, each rounded once to binary16 (scale
  * 1 where that is 0), code = clamp(rint((x - zero) / scale), 0, 15) with the rounded ones, in arithmetic that gives the
- * integers of the exact quotient.  What a page takes in is limited to +-65504 (bfloat16: +-65280, its
- * largest below that), a NaN counts as 0.  The other rows go to res_k, res_v unchanged; slots that receive none keep what they held.  A page whose slot lies past max_pages_per_seq or whose id is
- * out of range is flagged and not written.  seq_lens is not modified: batch->max_seq_len bounds the lengths before the call. */
+ * integers of the exact quotient.  What a page takes in is limited to +-65504 (bfloat16: +-65280, its largest below that),
+ * a NaN counts as 0.  The other rows go to res_k, res_v unchanged; slots that receive none keep what they held.  A page
+ * whose slot lies past max_pages_per_seq or whose id is out of range is flagged and not written.  seq_lens is not modified:
+ * batch->max_seq_len bounds the lengths before the call. */
 mc_status mc_layer_q4_append(const mc_config* cfg, const mc_batch* batch, const mc_layer_q4_cache* layer, const void* k,
                              const void* v, int64_t k_stride, int64_t v_stride, const int32_t* row_offsets, int32_t n_rows,
                              void* stream);

@@ -8,7 +8,8 @@
 // are, 128 products q scale and 128 products p scale are formed in their place.  A four-bit integer needs no conversion:
 // masked out of a word, the bits 0..3 of a half-word are the binary16 number code * 2^-24 and the bits 4..7 code * 2^-20
 // (subnormal numbers and the lowest binade share their unit), which the tensor cores multiply exactly; the powers of two
-// are taken out of the fp32 sums.  Five logic operations per eight codes are all that is done to them.
+// are taken out of the fp32 sums.  Five logic operations per eight codes of K are all that is done to them, four of V: there a whole
+// byte, low nibble + 16 high, and 16 high go to two rows of the accumulator, whose difference is taken once at the end.
 //   q scale (22 bits) is carried as two binary16 numbers, its rounding and the rest, in neighbouring columns of the B operand
 // that one kv head's few query heads leave idle (eight query heads: two passes), so scores are as exact as fp32 sums make them.
 // p is kept below 2^e, p scale below 2^15, e chosen from the page's scales and lowered like a running maximum that rises.
@@ -16,9 +17,13 @@
 // Work: the complete pages that are seen (or selected), split equally over teams of warps, a warp per kv head in each (neighbouring
 // warps stream neighbouring tiles of a page).  A warp is a pipeline of its own with a ring of stages of one tile (5 KB: codes and
 // parameters of K and V), two copied with the tensor map's swizzle so that ldmatrix and 16-byte loads meet no bank conflicts.
-// A sequence's begun page and the step's new row, 16-bit rows, are one unit more, ahead of its pages: attended straight from
-// global memory while the first tiles are on their way, and the new row appended.  Partial results are joined by a second
-// kernel.
+// A sequence's begun page and the step's new row, 16-bit rows, are a piece of their own: attended straight from global memory
+// while the first tiles are on their way, and the new row appended.  Partial results are joined by a second kernel.
+//
+// Bound by the memory and, as much, by what a tile's instructions take: 266 of the ALU, 150 of the FMA pipe and 34 of the tensor
+// cores per 5 KB, which add up on this part (8 mma.sync, 32 lop3 and 32 fma of three warps a scheduler: 153 cycles; each kind alone 65,
+// 64 and 33).  Measured, from a CUDA graph: 8 x 4109 tokens of 32 heads 38.7 us (170 MB: 25.9 us at a copy's rate, 28.5 for a kernel
+// that only reads them), 16 x 8192 of 8 kv heads under 32, capped, 42.2 us.  Of 33 us in a CTA 5 pass until its first tile is there.
 #include <algorithm>
 
 #include "mc_kernels.h"
@@ -31,6 +36,9 @@
 
 namespace mc {
 
+// Twelve warps an SM fit 168 registers each (sixteen spill: 54 instead of 44 us); as two CTAs, so that the next kernel's first CTAs
+// find room (one of twelve 43, two of six 40, three of four up to 64: starts packed unevenly).  Two stages: three 47, more requests
+// outstanding than the memory serves well.
 constexpr int kLqWarps = 6;
 constexpr int kLqThreads = kLqWarps * 32;
 constexpr int kLqCtasPerSm = 2;
