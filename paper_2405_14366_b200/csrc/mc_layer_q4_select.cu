@@ -11,8 +11,8 @@
 // A cluster of CTAs per (sequence, kv head) forms the sums; their binary32 roundings, which keep the order, go to the first
 // CTA's shared memory, where a radix select finds the last one in (512 pages and fewer: a count).  Pages that round alike
 // there are told apart by the 64-bit sums, and equal ones by their index.
-// Measured, from a CUDA graph: 22.4 us for 4 x 131060 tokens of 8 kv heads (67 MB: 10.3 us at a copy's rate; the sums and the launch
-// take 17.3, then one CTA of a cluster's four selects), 9.8 us for 16 x 8192, 6.9 us for one sequence of 8200 tokens and 32 heads.
+// Measured, from a CUDA graph: 19.2 us for 4 x 131060 tokens of 8 kv heads (67 MB: 10.3 us at a copy's rate; the sums and the launch
+// take 15.3, then one CTA of a cluster's four selects), 8.0 us for 16 x 8192, 5.6 us for one sequence of 8200 tokens and 32 heads.
 #include <algorithm>
 
 #include "mc_kernels.h"
@@ -68,14 +68,20 @@ __device__ __forceinline__ void store_first_cta(uint32_t* smem, uint32_t v) {
   asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(a), "r"(v) : "memory");
 }
 
+// The sum of the warps' numbers that `mine` asks for (of warp `lane`).
+__device__ __forceinline__ int sum_of(const int* warps, bool mine) {
+  const int lane = threadIdx.x & 31;
+  return __reduce_add_sync(0xffffffffu, mine && lane < kLsWarps ? warps[lane] : 0);
+}
+
 template <int DT>
 __global__ void __launch_bounds__(kLsThreads, 1) layer_q4_select_kernel(const __grid_constant__ Q4SelectParams p) {
   grid_dep_launch();
   extern __shared__ __align__(16) unsigned char select_smem[];
   uint32_t* keys_s = reinterpret_cast<uint32_t*>(select_smem + kLsRing);  // [pages] of the first CTA
   __shared__ uint32_t hist[kLsBins];
-  __shared__ uint32_t scan_s[kLsWarps], pick_s[3];
-  __shared__ int ins_s[kLsWarps], ties_s[kLsWarps];
+  __shared__ int scan_s[kLsWarps], ins_s[kLsWarps], ties_s[kLsWarps];
+  __shared__ uint32_t pick_s[2][3];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int H = p.g.n_kv_heads;
   const int rank = blockIdx.x % p.cluster, seg = blockIdx.x / p.cluster;
@@ -96,6 +102,7 @@ __global__ void __launch_bounds__(kLsThreads, 1) layer_q4_select_kernel(const __
     return;
   }
   unsigned long long* keys = p.keys + (size_t)seg * p.key_stride;
+  for (int i = tid; i < kLsBins; i += kLsThreads) hist[i] = 0;
   {
     double Q[4] = {}, P[4] = {};
     for (int h = 0; h < p.nq; ++h) {
@@ -113,33 +120,36 @@ __global__ void __launch_bounds__(kLsThreads, 1) layer_q4_select_kernel(const __
       P[c] *= 15.0 * 0x1p504;  // (what the tiny numbers lack is put back in two steps: 2^1008 times a query overflows)
       Q[c] *= 0x1p504;
     }
-    // The warp's pages: batches of four, every (cluster * warps)-th.  A lane knows the page of one of the next 32 (eight batches);
+    // The warp's pages: batches of four, every (cluster * warps)-th.  A lane knows the page of one of the next 32 (eight batches), and
+    // keeps the sum of one: what is done to a sum is done to 32 at a time (to each batch's four at once: 22.5 us for 20.2);
     // the next batch's parameters are on their way while one is worked on, each lane's 16 bytes of a page to where it reads them.
     const int step = p.cluster * kLsWarps * kLsBatch, first = (rank * kLsWarps + warp) * kLsBatch;
-    auto pages_from = [&](int k) {  // lane: page (lane & 3) of the batch k + (lane >> 2) step
-      const int at = k + (lane >> 2) * step + (lane & 3);
+    auto pages_from = [&](int k) {  // lane: page lane % batch of the batch k + lane / batch * step
+      const int at = k + lane / kLsBatch * step + lane % kLsBatch;
       if (at >= u) return 0;
       const int page = checked_page(p.g, b, v.page_of(at), p.status);
       return page < 0 ? 0 : page;
     };
-    int ids = pages_from(first), ids_next = pages_from(first + 8 * step), turn = 0, k_ahead = first, slot = 0;
+    constexpr int kTurns = 32 / kLsBatch;
+    int ids = pages_from(first), ids_next = pages_from(first + kTurns * step), turn = 0, k_ahead = first, slot = 0;
     const unsigned char* meta = p.k_meta + (size_t)head * kLqMetaBytes + 16 * lane;
     unsigned char* ring = select_smem + warp * (kLsStages * kLsBatch * kLqMetaBytes) + 16 * lane;
     const uint32_t ring_s = (uint32_t)__cvta_generic_to_shared(ring);
-    int slot_ahead = 0;
+    int slot_ahead = 0, done = 0;
+    double mine = 0.0;
     auto issue = [&]() {
       if (k_ahead < u) {
 #pragma unroll
         for (int j = 0; j < kLsBatch; ++j) {
-          const int page = __shfl_sync(0xffffffffu, ids, 4 * turn + j);
+          const int page = __shfl_sync(0xffffffffu, ids, kLsBatch * turn + j);
           asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(ring_s + (slot_ahead * kLsBatch + j) * kLqMetaBytes),
                        "l"(meta + (size_t)page * H * kLqMetaBytes)
                        : "memory");
         }
-        if (++turn == 8) {
+        if (++turn == kTurns) {
           turn = 0;
           ids = ids_next;
-          ids_next = pages_from(k_ahead + 9 * step);
+          ids_next = pages_from(k_ahead + (kTurns + 1) * step);
         }
       }
       asm volatile("cp.async.commit_group;" ::: "memory");
@@ -166,7 +176,7 @@ __global__ void __launch_bounds__(kLsThreads, 1) layer_q4_select_kernel(const __
       }
       // four sums over the warp, halving the pages a lane keeps: lane 8 j ends with page j
 #pragma unroll
-      for (int o = 16, c = 2; c > 0; o >>= 1, c >>= 1) {
+      for (int o = 16, c = kLsBatch / 2; c > 0; o >>= 1, c >>= 1) {
         const bool up = (lane & o) != 0;
 #pragma unroll
         for (int j = 0; j < c; ++j) {
@@ -175,14 +185,19 @@ __global__ void __launch_bounds__(kLsThreads, 1) layer_q4_select_kernel(const __
         }
       }
 #pragma unroll
-      for (int o = 4; o > 0; o >>= 1) a[0] += __shfl_xor_sync(0xffffffffu, a[0], o);
-      const int k = k0 + (lane >> 3);
-      if ((lane & 7) == 0 && k < u) {
-        const int slot = v.page_of(k);
-        const double x = a[0] * 0x1p504 + 0.0;  // (-0 counts as 0)
-        const bool guarded = slot < p.n_sink || slot >= full - p.n_recent;
-        keys[k] = guarded ? ~0ull : order64(x);
-        store_first_cta(keys_s + k, guarded ? 0xffffffffu : order32((float)x));
+      for (int o = kTurns / 2; o > 0; o >>= 1) a[0] += __shfl_xor_sync(0xffffffffu, a[0], o);
+      // (the lanes from kTurns j on have page j)
+      if (lane % kTurns == done) mine = a[0];
+      if (++done == kTurns || k0 + step >= u) {
+        const int k = k0 + (lane % kTurns - (done - 1)) * step + lane / kTurns;
+        if (lane % kTurns < done && k < u) {
+          const int page = v.page_of(k);
+          const double x = mine * 0x1p504 + 0.0;  // (-0 counts as 0)
+          const bool guarded = page < p.n_sink || page >= full - p.n_recent;
+          keys[k] = guarded ? ~0ull : order64(x);
+          store_first_cta(keys_s + k, guarded ? 0xffffffffu : order32((float)x));
+        }
+        done = 0;
       }
     }
   }
@@ -190,35 +205,35 @@ __global__ void __launch_bounds__(kLsThreads, 1) layer_q4_select_kernel(const __
   cluster_wait();
   if (rank != 0) return;
 
-  // ---- few pages, a thread each: its rank is the number of larger keys (512 comparisons are less than a pass over the digits)
+  // ---- few pages, a thread each: its rank is the number of larger keys (512 comparisons are less than a pass over the digits);
+  // those that are alike are told apart only where they are too many
   if (u <= kLsThreads) {
     bool in = false;
+    uint32_t c = 0;
+    int above = 0;
+    const int u4 = u / 4 * 4;
     if (tid < u) {
-      const uint32_t c = keys_s[tid];
-      int above = 0, alike = 0;
-      const int u4 = u / 4 * 4;
-#pragma unroll 4
+      c = keys_s[tid];
+#pragma unroll 16
       for (int k = 0; k < u4; k += 4) {
         const uint4 o = *reinterpret_cast<const uint4*>(keys_s + k);
         above += (o.x > c ? 1 : 0) + (o.y > c ? 1 : 0) + (o.z > c ? 1 : 0) + (o.w > c ? 1 : 0);
-        alike += (o.x == c ? 1 : 0) + (o.y == c ? 1 : 0) + (o.z == c ? 1 : 0) + (o.w == c ? 1 : 0);
       }
-      for (int k = u4; k < u; ++k) {
-        above += keys_s[k] > c ? 1 : 0;
-        alike += keys_s[k] == c ? 1 : 0;
-      }
-      if (alike > 1 && above < take && above + alike > take) {  // some of those that are alike in 32 bits
+      for (int k = u4; k < u; ++k) above += keys_s[k] > c ? 1 : 0;
+      in = above < take;
+    }
+    if (__syncthreads_count(in) > take) {  // some of those that are alike in 32 bits
+      if (in) {
         const unsigned long long d = keys[tid];
         for (int k = 0; k < u; ++k)
           if (keys_s[k] == c && k != tid) above += keys[k] > d || (keys[k] == d && k < tid) ? 1 : 0;
       }
-      in = above < take;
+      in = in && above < take;
     }
     const uint32_t bi = __ballot_sync(0xffffffffu, in);
     if (lane == 0) ins_s[warp] = __popc(bi);
     __syncthreads();
-    int before = __popc(bi & ((1u << lane) - 1u));
-    for (int w = 0; w < warp; ++w) before += ins_s[w];
+    const int before = __popc(bi & ((1u << lane) - 1u)) + sum_of(ins_s, lane < warp);
     if (in) list[before] = v.page_of(tid);
     return;
   }
@@ -227,19 +242,20 @@ __global__ void __launch_bounds__(kLsThreads, 1) layer_q4_select_kernel(const __
   unsigned long long p64 = 0, m64 = 0;
   int need = take;   // of those that match the digits so far
   bool all = false;  // every one of them
-  auto matches = [&](int k) {
-    const uint32_t c = keys_s[k];
-    if ((c & m32) != p32) return false;
-    return m64 == 0 || (keys[k] & m64) == p64;
-  };
   for (int pass = 0; pass < 9 && !all; ++pass) {
     const bool wide = pass >= 3;
     const int width = pass == 2 ? 10 : pass == 8 ? 9 : 11;
     const int shift = pass == 0 ? 21 : pass == 1 ? 10 : pass == 2 ? 0 : pass == 8 ? 0 : 53 - 11 * (pass - 3);
-    for (int i = tid; i < kLsBins; i += kLsThreads) hist[i] = 0;
-    __syncthreads();
-    for (int k = tid; k < u; k += kLsThreads)
-      if (matches(k)) atomicAdd(&hist[(wide ? (uint32_t)(keys[k] >> shift) : keys_s[k] >> shift) & ((1u << width) - 1u)], 1u);
+    for (int k = 4 * tid; k < u; k += 4 * kLsThreads) {
+      const uint4 c4 = *reinterpret_cast<const uint4*>(keys_s + k);
+      const uint32_t c[4] = {c4.x, c4.y, c4.z, c4.w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if (k + j >= u || (c[j] & m32) != p32) continue;
+        if (wide && m64 != 0 && (keys[k + j] & m64) != p64) continue;
+        atomicAdd(&hist[(wide ? (uint32_t)(keys[k + j] >> shift) : c[j] >> shift) & ((1u << width) - 1u)], 1u);
+      }
+    }
     __syncthreads();
     // the bin from the top in which the need-th lies: thread t has four of them
     constexpr int kOwn = kLsBins / kLsThreads;
@@ -247,6 +263,7 @@ __global__ void __launch_bounds__(kLsThreads, 1) layer_q4_select_kernel(const __
 #pragma unroll
     for (int j = 0; j < kOwn; ++j) {
       own[j] = hist[tid * kOwn + j];
+      hist[tid * kOwn + j] = 0;  // (for the next digit)
       sum += own[j];
     }
     uint32_t above = sum;  // bins of this thread and those behind it in the warp
@@ -255,23 +272,23 @@ __global__ void __launch_bounds__(kLsThreads, 1) layer_q4_select_kernel(const __
       const uint32_t t = __shfl_down_sync(0xffffffffu, above, o);
       if (lane + o < 32) above += t;
     }
-    if (lane == 0) scan_s[warp] = above;
+    if (lane == 0) scan_s[warp] = (int)above;
     __syncthreads();
-    above -= sum;
-    for (int w = warp + 1; w < kLsWarps; ++w) above += scan_s[w];
+    above += sum_of(scan_s, lane > warp) - sum;
     if (above < (uint32_t)need && above + sum >= (uint32_t)need) {
 #pragma unroll
       for (int j = kOwn - 1; j >= 0; --j) {
         if (above < (uint32_t)need && above + own[j] >= (uint32_t)need) {
-          pick_s[0] = tid * kOwn + j;
-          pick_s[1] = need - above;
-          pick_s[2] = own[j];
+          pick_s[pass & 1][0] = tid * kOwn + j;
+          pick_s[pass & 1][1] = need - above;
+          pick_s[pass & 1][2] = own[j];
         }
         above += own[j];
       }
     }
     __syncthreads();
-    const unsigned long long digit = pick_s[0], mask = (1u << width) - 1u;
+    const uint32_t* pick = pick_s[pass & 1];
+    const unsigned long long digit = pick[0], mask = (1u << width) - 1u;
     if (wide) {
       p64 |= digit << shift;
       m64 |= mask << shift;
@@ -279,54 +296,61 @@ __global__ void __launch_bounds__(kLsThreads, 1) layer_q4_select_kernel(const __
       p32 |= (uint32_t)digit << shift;
       m32 |= (uint32_t)mask << shift;
     }
-    need = pick_s[1];
-    all = pick_s[1] == pick_s[2];
-    __syncthreads();
+    need = pick[1];
+    all = pick[1] == pick[2];
   }
 
-  // ---- the list, in ascending order: a warp has a run of pages
+  // ---- the list, in ascending order: a warp has a run of pages, a lane at last 32 of it
+  static_assert(kQ4MaxSelectLen / kLqPage <= kLsThreads * 32, "a lane has a word of them");
   const int per = ((u + kLsWarps - 1) / kLsWarps + 31) / 32 * 32;
   const int k0 = min(warp * per, u), k1 = min(k0 + per, u);
-  auto look = [&](int k, bool& in, bool& tie) {
-    in = tie = false;
-    if (k >= k1) return;
-    const uint32_t c = keys_s[k] & m32;
-    if (c != p32) {
-      in = c > p32;
-    } else if (m64 != 0) {
-      const unsigned long long d = keys[k] & m64;
-      in = d > p64;
-      tie = d == p64;
-    } else {
-      tie = true;
+  uint32_t ins = 0, ties = 0;  // bit i: page k0 + 32 lane + i is above the border, or one of those on it
+#pragma unroll 4
+  for (int it = 0; it < per / 32; ++it) {
+    const int k = k0 + 32 * it + lane;
+    bool in = false, tie = false;
+    if (k < k1) {
+      const uint32_t c = keys_s[k] & m32;
+      if (c != p32) {
+        in = c > p32;
+      } else if (m64 != 0) {
+        const unsigned long long d = keys[k] & m64;
+        in = d > p64;
+        tie = d == p64;
+      } else {
+        tie = true;
+      }
     }
-  };
-  int ins = 0, ties = 0;
-  for (int k = k0; k < k1; k += 32) {
-    bool in, tie;
-    look(k + lane, in, tie);
-    ins += __popc(__ballot_sync(0xffffffffu, in));
-    ties += __popc(__ballot_sync(0xffffffffu, tie));
+    const uint32_t bi = __ballot_sync(0xffffffffu, in), bt = __ballot_sync(0xffffffffu, tie);
+    if (lane == it) {
+      ins = bi;
+      ties = bt;
+    }
   }
-  if (lane == 0) {
-    ins_s[warp] = ins;
-    ties_s[warp] = ties;
+  const int n_in = __popc(ins), n_tie = __popc(ties);
+  int in_before = n_in, tie_before = n_tie;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int x = __shfl_up_sync(0xffffffffu, in_before, o), y = __shfl_up_sync(0xffffffffu, tie_before, o);
+    if (lane >= o) {
+      in_before += x;
+      tie_before += y;
+    }
+  }
+  if (lane == 31) {
+    ins_s[warp] = in_before;
+    ties_s[warp] = tie_before;
   }
   __syncthreads();
-  int in_before = 0, tie_before = 0;
-  for (int w = 0; w < warp; ++w) {
-    in_before += ins_s[w];
-    tie_before += ties_s[w];
-  }
-  const uint32_t below = (1u << lane) - 1u;
-  for (int k = k0; k < k1; k += 32) {
-    bool in, tie;
-    look(k + lane, in, tie);
-    const uint32_t bi = __ballot_sync(0xffffffffu, in), bt = __ballot_sync(0xffffffffu, tie);
-    const int t = tie_before + __popc(bt & below);  // ties ahead of this one: the first `need` are in
-    if (in || (tie && t < need)) list[in_before + __popc(bi & below) + min(t, need)] = v.page_of(k + lane);
-    in_before += __popc(bi);
-    tie_before += __popc(bt);
+  in_before += sum_of(ins_s, lane < warp) - n_in;
+  tie_before += sum_of(ties_s, lane < warp) - n_tie;
+  for (uint32_t left = ins | ties; left != 0; left &= left - 1) {
+    const int i = __ffs(left) - 1;
+    const bool in = (ins >> i) & 1u;
+    if (in || tie_before < need)  // (the first `need` of the ties are in)
+      list[in_before + min(tie_before, need)] = v.page_of(k0 + 32 * lane + i);
+    in_before += in ? 1 : 0;
+    tie_before += in ? 0 : 1;
   }
 }
 
@@ -366,7 +390,7 @@ mc_status launch_layer_q4_select(const mc_config* cfg, const mc_batch* bt, const
   cudaLaunchConfig_t lc = {};
   lc.gridDim = dim3((unsigned)(segs * cluster));
   lc.blockDim = dim3(kLsThreads);
-  lc.dynamicSmemBytes = kLsRing + (size_t)sp.key_stride * 4;
+  lc.dynamicSmemBytes = kLsRing + align_up((size_t)sp.key_stride * 4, 16);
   lc.stream = stream;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;

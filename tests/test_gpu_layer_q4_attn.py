@@ -256,6 +256,23 @@ def test_select_long(Q, B, H, n):
         select(Q, c, c.queries(B, 4 * H), budget, 1, 2)
 
 
+def test_select_long_ties(Q):
+    """More pages than threads, with sums that are alike, or alike in 32 bits only, on the border of the choice."""
+    c = Q.Cache([38000, 25013], 2, 4, "f16", seed=6)
+    select(Q, c, torch.zeros(2, 4, 128, dtype=c.dt), 513)  # all alike: the lowest
+    for s in range(38000 // 32):
+        c.km[c.table[0, s]] = c.km[c.table[0, s % 7]]
+    for s in range(25013 // 32):
+        c.km[c.table[1, s]] = c.km[c.table[1, 0]]
+        c.km[c.table[1, s], :, 7, 1] = float(s % 5) * 2.0 ** -24
+    c.d["km"].copy_(c.km)
+    q = c.queries(2, 4)
+    for budget, sink, recent in ((1, 0, 0), (33, 0, 0), (100, 3, 5), (170, 0, 0), (700, 1, 1), (780, 0, 0), (1186, 0, 0)):
+        select(Q, c, q, budget, sink, recent)
+    q[1, :, 5] = float("nan")  # no sum is a number: the lowest
+    select(Q, c, q, 77)
+
+
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
 @pytest.mark.parametrize("H,Hq", [(2, 2), (2, 8), (2, 16), (5, 10)])
 def test_attention_over_selected_pages(Q, dtype, H, Hq):
