@@ -26,8 +26,8 @@ constexpr int kLsThreads = 512;
 constexpr int kLsWarps = kLsThreads / 32;
 constexpr int kLsMaxCluster = 8;
 constexpr int kLsBatch = 4;   // pages of a warp at a time
-// batches of a warp in shared memory: one worked on, one on its way (16 warps then have 32 KB on their way; with four: 10.8 us for
-// 9.8 at 16 x 8192 tokens, 23.2 for 22.4 at 4 x 131060)
+// batches of a warp in shared memory: one worked on, one on its way (16 warps then have 32 KB on their way; with three or four:
+// 9.8, 10.3 us for 9.4 at 16 x 8192 tokens, 20.8, 21.3 for 20.2 at 4 x 131060)
 constexpr int kLsStages = 2;
 constexpr int kLsRing = kLsWarps * kLsStages * kLsBatch * kLqMetaBytes;
 constexpr int kLsBins = 2048;
