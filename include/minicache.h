@@ -771,8 +771,10 @@ mc_status mc_layer_q4_select(const mc_config* cfg, const mc_batch* batch, const 
  * flags        MC_LAYER_APPEND: the new row is also written behind the cached tokens, as mc_layer_q4_append does it (the page
  *              it completes is quantised).  seq_lens is not modified.
  * workspace    mc_layer_workspace_bytes(MC_OP_LAYER_Q4_ATTN, flags) bytes, 256-byte aligned
- * The products of a query with a group's scales are kept to 22 bits, scores, maxima and sums in fp32; probabilities, and
- * their products with the values' scales, are rounded to 11 bits before they meet the codes. */
+ * The products of a query with a group's scales are kept to 22 bits, or to 2^-25 of the query's largest entry times the page's largest
+ * key scale where that is more (entries below 2^-24 of the largest have fewer bits); scores, maxima and sums in fp32.
+ * Probabilities, the largest taken as 1, and their products with the values' scales are rounded to 11 bits before they meet the
+ * codes, or to 2^-32 of the largest value scale (2^-40 where that is below 2^-8); those of 16-bit rows once to cfg->dtype. */
 mc_status mc_layer_q4_attn(const mc_config* cfg, const mc_batch* batch, const mc_layer_q4_cache* layer, const mc_score_opts* opts,
                            const int32_t* pages, const int32_t* counts, int32_t pages_stride, const void* q, const void* k_new,
                            const void* v_new, int32_t flags, void* out, float* lse, void* workspace, size_t workspace_bytes,

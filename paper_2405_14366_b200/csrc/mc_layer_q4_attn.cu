@@ -11,7 +11,8 @@
 // are taken out of the fp32 sums.  Five logic operations per eight codes of K are all that is done to them, four of V: there a whole
 // byte, low nibble + 16 high, and 16 high go to two rows of the accumulator, whose difference is taken once at the end.
 //   q scale (22 bits) is carried as two binary16 numbers, its rounding and the rest, in neighbouring columns of the B operand
-// that one kv head's few query heads leave idle (eight query heads: two passes), so scores are as exact as fp32 sums make them.
+// that one kv head's few query heads leave idle (eight query heads: two passes), with a power of two that follows the page's scales,
+// so scores are as exact as fp32 sums make them.
 // p is kept below 2^e, p scale below 2^15, e chosen from the page's scales and lowered like a running maximum that rises.
 //
 // Work: the complete pages that are seen (or selected), split equally over teams of warps, a warp per kv head in each (neighbouring
@@ -326,6 +327,29 @@ __device__ __noinline__ void q4_begun_page(const LayerQ4Params& p, const Q4Seq v
   }
 }
 
+// q scale as two binary16 numbers loses what is below 2^-25.  A query's largest entry is brought to [2^kLqQueryExp, 2^(kLqQueryExp + 1)),
+// and a page whose largest key scale is in [2^-kLqQueryExp, 2^(15 - kLqQueryExp)) is met as it is: products are below 2^16, and the
+// largest that the page allows is 1 or more, so that 2^-25 of that one is what any of its products may lose.  Other pages (keys that
+// spread over more than 480, or less than 0.015 in every channel) have a power of two taken out of their scales first.
+constexpr int kLqQueryExp = 10;
+constexpr uint32_t kLqLeastTop = (uint32_t)(15 - kLqQueryExp) << 10, kLqTops = (uint32_t)(30 - kLqQueryExp) << 10;  // (binary16, as integers)
+static_assert(kLqQueryExp < 15, "normal numbers");
+
+// Brings the largest of a page's key scales, `top` (binary16, as an integer), to [2^3, 2^4), where they lie; 2^24 over the factor.
+__device__ __noinline__ float q4_rescale_keys(uint32_t k_meta, uint32_t top) {
+  const int lane = threadIdx.x & 31;
+  const int by = min(max(3 + 127 - (__float_as_int(half_lo(top)) >> 23), -12), 27);  // (a subnormal scale is a normal binary32 number)
+  const float f = __int_as_float((127 + by) << 23);
+  const uint4 u = lds16(k_meta + 16 * lane);
+  uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+  for (int c = 0; c < 4; ++c) w[c] = (w[c] & 0xffff0000u) | (uint32_t)__half_as_ushort(__float2half_rn(half_lo(w[c]) * f));
+  asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(k_meta + 16 * lane), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // (ahead of the copy that follows into this place)
+  __syncwarp();
+  return __int_as_float((127 + 24 - by) << 23);
+}
+
 // WIDE: eight query heads per kv head, a column of B each; else up to four, two columns each.
 template <int DT, bool WIDE>
 __global__ void __launch_bounds__(kLqThreads, kLqCtasPerSm)
@@ -472,7 +496,7 @@ layer_q4_split_kernel(const __grid_constant__ LayerQ4Params p, const __grid_cons
       int slot_last = list && k0 > 0 ? __ldcg(list + k0 - 1) : -1;
 
       // Query pairs (channels 8w + i, 8w + i + 4 of the lane's 32), as binary16 with the row's power of two taken out: the
-      // row's largest number becomes 2 to 4.  q_back, of the lane's result column(s), puts it back.
+      // row's largest number becomes 2^10 to 2^11.  q_back, of the lane's result column(s), puts it back.
       uint32_t qh[16];
       float q_back, q_back1 = 0.f;
       {
@@ -495,9 +519,9 @@ layer_q4_split_kernel(const __grid_constant__ LayerQ4Params p, const __grid_cons
         }
         big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 1));
         big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 2));
-        const int e = min(max(__float_as_int(big) >> 23, 2), 253);
-        const float f = __int_as_float((255 - e) << 23);
-        const float back = __int_as_float((e - 1) << 23);
+        const int e = min(max(__float_as_int(big) >> 23, kLqQueryExp + 1), 253);
+        const float f = __int_as_float((254 + kLqQueryExp - e) << 23);
+        const float back = __int_as_float((e - kLqQueryExp) << 23);
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
           const uint32_t y[4] = {w[c].x, w[c].y, w[c].z, w[c].w};
@@ -566,13 +590,20 @@ layer_q4_split_kernel(const __grid_constant__ LayerQ4Params p, const __grid_cons
         }
         // ---- scores of 32 tokens: two tiles of 16
         float dl[2][4], dh[2][4];  // low and high nibbles' sums
-        float dz[4] = {};                    // the zeros' sum of this lane's column and channels
+        float low = 0x1p24f, high;  // what takes the powers of two of the nibbles, and of the keys' scales, out of them
+        float dz[4] = {};           // the zeros' sum of this lane's column and channels
         {
           uint4 c4[2][2];  // [tile][token row, row + 8]: 32 channels
 #pragma unroll
           for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int e = 0; e < 2; ++e) c4[h][e] = lds16(sb + k_off + (16 * h + 8 * e) * 64);
+          {  // (the latency of this, a load, a reduction and a branch, is 1.5 of 40 us; with it behind the products: 3 to 6 more)
+            const uint4 u = lds16(sb + kLqKMeta + 16 * lane);
+            const uint32_t top = __reduce_max_sync(0xffffffffu, h2_max(h2_max(u.x, u.y), h2_max(u.z, u.w)) & 0x7fffu);
+            if (top - kLqLeastTop >= kLqTops - kLqLeastTop) low = q4_rescale_keys(sb + kLqKMeta, top);
+          }
+          high = low * 0x1p-4f;
 #pragma unroll
           for (int w = 0; w < 4; ++w) {
             const uint4 ma = lds16(sb + km_off[2 * (w & 1)] + 64 * (w >> 1)), mb = lds16(sb + km_off[2 * (w & 1) + 1] + 64 * (w >> 1));
@@ -628,10 +659,10 @@ layer_q4_split_kernel(const __grid_constant__ LayerQ4Params p, const __grid_cons
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
             if (WIDE) {
-              sa[2 * h + e] = fmaf(dl[h][2 * e], 0x1p24f, fmaf(dh[h][2 * e], 0x1p20f, z0)) * q_back;
-              sc[2 * h + e] = fmaf(dl[h][2 * e + 1], 0x1p24f, fmaf(dh[h][2 * e + 1], 0x1p20f, z1)) * q_back1;
+              sa[2 * h + e] = fmaf(dl[h][2 * e], low, fmaf(dh[h][2 * e], high, z0)) * q_back;
+              sc[2 * h + e] = fmaf(dl[h][2 * e + 1], low, fmaf(dh[h][2 * e + 1], high, z1)) * q_back1;
             } else {
-              sc[2 * h + e] = fmaf(dl[h][2 * e] + dl[h][2 * e + 1], 0x1p24f, fmaf(dh[h][2 * e] + dh[h][2 * e + 1], 0x1p20f, z0)) * q_back;
+              sc[2 * h + e] = fmaf(dl[h][2 * e] + dl[h][2 * e + 1], low, fmaf(dh[h][2 * e] + dh[h][2 * e + 1], high, z0)) * q_back;
             }
           }
         // ---- masks, the scores' form, the distance bias
