@@ -722,8 +722,9 @@ enum { MC_OP_LAYER_Q4_ATTN = 5, MC_OP_LAYER_Q4_SELECT = 6 }; /* mc_layer_workspa
  * 1 where that is 0), code = clamp(rint((x - zero) / scale), 0, 15) with the rounded ones, in arithmetic that gives the
  * integers of the exact quotient.  What a page takes in is limited to +-65504 (bfloat16: +-65280, its largest below that),
  * a NaN counts as 0.  The other rows go to res_k, res_v unchanged; slots that receive none keep what they held.  A page
- * whose slot lies past max_pages_per_seq or whose id is out of range is flagged and not written.  seq_lens is not modified:
- * batch->max_seq_len bounds the lengths before the call. */
+ * whose slot lies past max_pages_per_seq or whose id is out of range is flagged and not written; a sequence whose length is out of
+ * [0, max_seq_len] is flagged and gets none of its rows.  seq_lens is not modified: batch->max_seq_len bounds the lengths before
+ * the call. */
 mc_status mc_layer_q4_append(const mc_config* cfg, const mc_batch* batch, const mc_layer_q4_cache* layer, const void* k,
                              const void* v, int64_t k_stride, int64_t v_stride, const int32_t* row_offsets, int32_t n_rows,
                              void* stream);
@@ -769,7 +770,7 @@ mc_status mc_layer_q4_select(const mc_config* cfg, const mc_batch* batch, const 
  *              order; an entry that is not above the one before it or names no complete page is flagged and skipped.  The
  *              begun page's rows and the new row are always attended (as far as the masks let them).
  * flags        MC_LAYER_APPEND: the new row is also written behind the cached tokens, as mc_layer_q4_append does it (the page
- *              it completes is quantised).  seq_lens is not modified.
+ *              it completes is quantised; nothing is written for a sequence whose length is out of range).  seq_lens is not modified.
  * workspace    mc_layer_workspace_bytes(MC_OP_LAYER_Q4_ATTN, flags) bytes, 256-byte aligned
  * The products of a query with a group's scales are kept to 22 bits, or to 2^-25 of the query's largest entry times the page's largest
  * key scale where that is more (entries below 2^-24 of the largest have fewer bits); scores, maxima and sums in fp32.

@@ -74,9 +74,11 @@ struct LayerQ4Params {
   float* lse;
 };
 
-// What every CTA keeps of a sequence: its length, the query's position, the tokens [0, a) and [lo, hi) that are seen.
+// What every CTA keeps of a sequence: its length (and whether that was in range: else nothing is appended, which would land on cached
+// rows), the query's position, the tokens [0, a) and [lo, hi) that are seen.
 struct Q4Seq {
   int n, q_pos, a, lo, hi;
+  bool append;
 };
 __device__ __forceinline__ int q4_page_of(const Q4Seq& s, int k) {  // (as page_view counts them)
   const int ua = (min(s.a, s.n / kLqPage * kLqPage) + kLqPage - 1) / kLqPage;
@@ -308,7 +310,7 @@ __device__ __noinline__ void q4_begun_page(const LayerQ4Params& p, const Q4Seq v
           make_float4(acc[2 * g][e], acc[2 * g][2 + e], acc[2 * g + 1][e], acc[2 * g + 1][2 + e]);
     if (row == 0) *reinterpret_cast<float2*>(p.part_ml + 2 * (prow + r)) = make_float2(e ? m1 : m0, e ? l1 : l0);
   }
-  if (p.flags & MC_LAYER_APPEND) {
+  if (v.append) {
     const int slot = n & (kLqPage - 1);
     const int ch = lane & 15;  // lanes 0 .. 15: the new K row's chunks, 16 .. 31: the V row's
     *reinterpret_cast<uint4*>((lane < 16 ? p.res_k : p.res_v) + at + slot * kRowBytes + 16 * ch) =
@@ -382,10 +384,12 @@ layer_q4_split_kernel(const __grid_constant__ LayerQ4Params p, const __grid_cons
   int bad = 0;
   for (int b = tid; b < p.g.batch; b += kLqThreads) {
     int begun;
-    const PageView v = q4_view(p, b, begun, bad);
+    int no_len = 0;
+    const PageView v = q4_view(p, b, begun, no_len);
+    bad |= no_len;
     pre.pages[b + 1] = v.u;
     pre.begun[b + 1] = begun;
-    seq_s[b] = Q4Seq{v.n, v.q_pos, v.a, v.lo, v.hi};
+    seq_s[b] = Q4Seq{v.n, v.q_pos, v.a, v.lo, v.hi, (p.flags & MC_LAYER_APPEND) != 0 && no_len == 0};
   }
   if (p.sel != nullptr) {
     grid_dep_wait();

@@ -81,8 +81,11 @@ __global__ void __launch_bounds__(kLrThreads, 2) layer_q4_append_kernel(const __
   grid_dep_wait();  // (the offsets and lengths may be what the kernel ahead has written)
   for (int b = tid; b < p.g.batch; b += kLrThreads) {
     AppendItem s;
-    s.n = len_of(p, b, bad);
+    int no_len = 0;
+    s.n = len_of(p, b, no_len);
     rows_of(p, b, s.first, s.count, bad_rows);
+    if (no_len) s.count = 0;  // (rows would land on cached ones)
+    bad |= no_len;
     seq_s[b] = s;
     pre_s[b + 1] = s.count == 0 ? 0 : max((s.n + s.count) / kLqPage - s.n / kLqPage, 1);
   }
