@@ -767,8 +767,9 @@ mc_status mc_layer_q4_select(const mc_config* cfg, const mc_batch* batch, const 
  * step's new row.  Scores, masks, q, k_new, v_new, out and lse as in mc_layer_attn (a token's index is its position).
  * pages, counts, pages_stride  NULL, NULL, 0: every complete page that the query sees.  Else only pages[b][h][0 .. counts[b]),
  *              pages_stride entries per (sequence, kv head), as mc_layer_q4_select writes them: page slots in ascending
- *              order; an entry that is not above the one before it or names no complete page is flagged and skipped.  The
- *              begun page's rows and the new row are always attended (as far as the masks let them).
+ *              order; an entry that names no complete page, or one that is not above every page named before it, is flagged and
+ *              skipped, so that no page counts twice.  The begun page's rows and the new row are always attended (as far as the
+ *              masks let them).
  * flags        MC_LAYER_APPEND: the new row is also written behind the cached tokens, as mc_layer_q4_append does it (the page
  *              it completes is quantised; nothing is written for a sequence whose length is out of range).  seq_lens is not modified.
  * workspace    mc_layer_workspace_bytes(MC_OP_LAYER_Q4_ATTN, flags) bytes, 256-byte aligned

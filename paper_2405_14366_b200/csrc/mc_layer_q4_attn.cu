@@ -497,7 +497,9 @@ layer_q4_split_kernel(const __grid_constant__ LayerQ4Params p, const __grid_cons
       const int32_t* list = p.sel ? p.sel + ((size_t)b * H + head) * p.sel_stride : nullptr;
       const int ua = (min(sq.a, sq.n / kLqPage * kLqPage) + kLqPage - 1) / kLqPage, ub0 = max(sq.lo / kLqPage, ua);  // (as page_view has them)
       int slot_next = list ? __ldcg(list + k0) : k0 < ua ? k0 : ub0 + k0 - ua;
-      int slot_last = list && k0 > 0 ? __ldcg(list + k0 - 1) : -1;
+      // the last page of the list that counted: the largest so far, which may lie in another warp's part (a lane's first entry comes
+      // with the queries)
+      int slot_last = list && lane < k0 ? __ldcg(list + lane) : -1;
 
       // Query pairs (channels 8w + i, 8w + i + 4 of the lane's 32), as binary16 with the row's power of two taken out: the
       // row's largest number becomes 2^10 to 2^11.  q_back, of the lane's result column(s), puts it back.
@@ -544,6 +546,15 @@ layer_q4_split_kernel(const __grid_constant__ LayerQ4Params p, const __grid_cons
         q_back = __shfl_sync(0xffffffffu, back, 8 * t4);
         if (WIDE) q_back1 = __shfl_sync(0xffffffffu, back, 8 * t4 + 4);
       }
+      if (list != nullptr) {
+        if (slot_last >= sq.n / kLqPage) slot_last = -1;
+#pragma unroll 8
+        for (int k = lane + 32; k < k0; k += 32) {
+          const int e = __ldcg(list + k);
+          if (e < sq.n / kLqPage) slot_last = max(slot_last, e);
+        }
+        slot_last = __reduce_max_sync(0xffffffffu, max(slot_last, -1));
+      }
       float sl0 = 0.f, sl1 = 0.f;
       if (p.rule.slopes) {
         const int h = WIDE ? 2 * t4 : t4;
@@ -574,10 +585,11 @@ layer_q4_split_kernel(const __grid_constant__ LayerQ4Params p, const __grid_cons
         } else {
           if (k + 1 < k1) slot_next = __ldcg(list + k + 1);
           const bool wrong = slot <= slot_last || slot < 0 || slot >= sq.n / kLqPage;
-          slot_last = slot;
-          if (wrong) {  // not above the one before it, or no complete page: nothing of it is seen
+          if (wrong) {  // not above every one that counted, or no complete page: nothing of it is seen
             if (lane == 0) atomicOr(p.status, MC_FLAG_BAD_METADATA);
             slot = -1;
+          } else {
+            slot_last = slot;
           }
         }
         const int t0 = slot * kLqPage;
