@@ -487,7 +487,7 @@ def _row_stride(name: str, t: torch.Tensor, cfg: "McConfig", rows: int, dev: int
     if not (t.dtype is cfg.torch_dtype and len(sh) == 3 and sh[0] == rows and sh[1] == cfg.n_kv_heads and sh[2] == 128 and st[2] == 1
             and (st[1] == 128 or sh[1] == 1) and t.get_device() == dev):
         raise AssertionError(f"{name}: [rows][n_kv_heads][128] of {cfg.torch_dtype} with adjacent heads on device {dev} is wanted")
-    return st[0] if rows > 1 else max(st[0], cfg.n_kv_heads * 128)
+    return st[0] if rows > 1 else cfg.n_kv_heads * 128  # (no element of one row depends on its stride)
 
 
 class MiniCacheLib:
