@@ -11,17 +11,22 @@ constexpr int kLqMetaBytes = 512;                  // (scale, zero): K [128], V 
 constexpr int kLqResBytes = kLqPage * kRowBytes;   // the begun page's rows of one (sequence, kv head)
 
 #if defined(__CUDACC__)
-// A sequence's complete pages as a query sees them: tokens [0, a) and [lo, hi), so the pages [0, ua) and those from ub0
-// on, u in all.
-struct PageView {
-  int n;             // cached tokens
+// A sequence as a query sees it: the tokens [0, a) and [lo, hi).
+struct TokenView {
+  int n;  // cached tokens
   int q_pos;
   int a, lo, hi;
-  int ua, ub0, u;
-  __device__ __forceinline__ int page_of(int k) const { return k < ua ? k : ub0 + k - ua; }
+  __device__ __forceinline__ int full() const { return n / kLqPage; }  // complete pages
   __device__ __forceinline__ bool sees(int t) const { return t < a || (t >= lo && t < hi); }
   __device__ __forceinline__ bool all_of(int t0) const { return t0 + kLqPage <= a || (t0 >= lo && t0 + kLqPage <= hi); }
-  __device__ __forceinline__ bool some_of(int t0) const { return t0 < a || (t0 + kLqPage > lo && t0 < hi); }
+  // the complete pages with a token that is seen: [0, head_pages) and those from tail_page on
+  __device__ __forceinline__ int head_pages() const { return (min(a, full() * kLqPage) + kLqPage - 1) / kLqPage; }
+  __device__ __forceinline__ int tail_page(int head) const { return max(lo / kLqPage, head); }
+};
+// The same with these pages, u in all: [0, ua) and those from ub0 on.
+struct PageView : TokenView {
+  int ua, ub0, u;
+  __device__ __forceinline__ int page_of(int k) const { return k < ua ? k : ub0 + k - ua; }
 };
 // n_tot: tokens that count for the masks, the step's new one included; default_pos: the query's position without q_pos.
 __device__ __forceinline__ PageView page_view(const ScoreRule& rule, int b, int n, int n_tot, int default_pos) {
@@ -33,10 +38,9 @@ __device__ __forceinline__ PageView page_view(const ScoreRule& rule, int b, int 
   s.a = max(min(end, v.prefix), 0);
   s.lo = max(v.lo_pos, s.a);
   s.hi = max(end, s.lo);
-  const int full = n / kLqPage * kLqPage;  // tokens in complete pages
-  const int a = min(s.a, full), hi = min(s.hi, full);
-  s.ua = (a + kLqPage - 1) / kLqPage;
-  s.ub0 = max(s.lo / kLqPage, s.ua);
+  s.ua = s.head_pages();
+  s.ub0 = s.tail_page(s.ua);
+  const int hi = min(s.hi, s.full() * kLqPage);
   const int ub1 = hi > s.lo ? (hi + kLqPage - 1) / kLqPage : 0;
   s.u = s.ua + max(ub1 - s.ub0, 0);
   return s;

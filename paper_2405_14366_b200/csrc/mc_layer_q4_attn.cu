@@ -74,16 +74,10 @@ struct LayerQ4Params {
   float* lse;
 };
 
-// What every CTA keeps of a sequence: its length (and whether that was in range: else nothing is appended, which would land on cached
-// rows), the query's position, the tokens [0, a) and [lo, hi) that are seen.
-struct Q4Seq {
-  int n, q_pos, a, lo, hi;
-  bool append;
+// What every CTA keeps of a sequence.
+struct Q4Seq : TokenView {
+  bool append;  // (not where its length was out of range: the new row would land on cached ones)
 };
-__device__ __forceinline__ int q4_page_of(const Q4Seq& s, int k) {  // (as page_view counts them)
-  const int ua = (min(s.a, s.n / kLqPage * kLqPage) + kLqPage - 1) / kLqPage;
-  return k < ua ? k : max(s.lo / kLqPage, ua) + k - ua;
-}
 // A sequence as the call sees it; `begun`: 1 if there are 16-bit rows (the begun page's, the step's new one).
 __device__ __forceinline__ PageView q4_view(const LayerQ4Params& p, int b, int& begun, int& bad) {
   const int raw = __ldcg(p.g.seq_lens + b);
@@ -205,7 +199,7 @@ __device__ __noinline__ void q4_begun_page(const LayerQ4Params& p, const Q4Seq v
   uint32_t seen = 0;  // bit r: token base + r is attended
   {
     const int t = base + lane;
-    seen = __ballot_sync(0xffffffffu, t < n_tot && (t < v.a || (t >= v.lo && t < v.hi)));
+    seen = __ballot_sync(0xffffffffu, t < n_tot && v.sees(t));
   }
   float acc[8][4];
 #pragma unroll
@@ -389,7 +383,10 @@ layer_q4_split_kernel(const __grid_constant__ LayerQ4Params p, const __grid_cons
     bad |= no_len;
     pre.pages[b + 1] = v.u;
     pre.begun[b + 1] = begun;
-    seq_s[b] = Q4Seq{v.n, v.q_pos, v.a, v.lo, v.hi, (p.flags & MC_LAYER_APPEND) != 0 && no_len == 0};
+    Q4Seq s;
+    static_cast<TokenView&>(s) = v;
+    s.append = (p.flags & MC_LAYER_APPEND) != 0 && no_len == 0;
+    seq_s[b] = s;
   }
   if (p.sel != nullptr) {
     grid_dep_wait();
@@ -415,10 +412,11 @@ layer_q4_split_kernel(const __grid_constant__ LayerQ4Params p, const __grid_cons
     t.meta = sh.member + hd * p.members;
     int slot;
     if (p.sel == nullptr) {
-      slot = q4_page_of(seq_s[b], k);
+      const int ua = seq_s[b].head_pages();
+      slot = k < ua ? k : seq_s[b].tail_page(ua) + k - ua;
     } else {
       slot = __ldcg(p.sel + ((size_t)b * H + t.meta) * p.sel_stride + k);
-      if ((unsigned)slot >= (unsigned)(seq_s[b].n / kLqPage)) slot = -1;  // (flagged when its turn comes)
+      if ((unsigned)slot >= (unsigned)seq_s[b].full()) slot = -1;  // (flagged when its turn comes)
     }
     if (slot >= 0) t.page = slot < p.g.max_pages_per_seq ? p.g.block_table[(size_t)b * p.g.max_pages_per_seq + slot] : -1;
     return t;
@@ -495,7 +493,7 @@ layer_q4_split_kernel(const __grid_constant__ LayerQ4Params p, const __grid_cons
       x += k1 - k0;
       const Q4Seq sq = seq_s[b];
       const int32_t* list = p.sel ? p.sel + ((size_t)b * H + head) * p.sel_stride : nullptr;
-      const int ua = (min(sq.a, sq.n / kLqPage * kLqPage) + kLqPage - 1) / kLqPage, ub0 = max(sq.lo / kLqPage, ua);  // (as page_view has them)
+      const int ua = sq.head_pages(), ub0 = sq.tail_page(ua);
       int slot_next = list ? __ldcg(list + k0) : k0 < ua ? k0 : ub0 + k0 - ua;
       // the last page of the list that counted: the largest so far, which may lie in another warp's part (a lane's first entry comes
       // with the queries)
@@ -547,11 +545,11 @@ layer_q4_split_kernel(const __grid_constant__ LayerQ4Params p, const __grid_cons
         if (WIDE) q_back1 = __shfl_sync(0xffffffffu, back, 8 * t4 + 4);
       }
       if (list != nullptr) {
-        if (slot_last >= sq.n / kLqPage) slot_last = -1;
+        if (slot_last >= sq.full()) slot_last = -1;
 #pragma unroll 8
         for (int k = lane + 32; k < k0; k += 32) {
           const int e = __ldcg(list + k);
-          if (e < sq.n / kLqPage) slot_last = max(slot_last, e);
+          if (e < sq.full()) slot_last = max(slot_last, e);
         }
         slot_last = __reduce_max_sync(0xffffffffu, max(slot_last, -1));
       }
@@ -584,7 +582,7 @@ layer_q4_split_kernel(const __grid_constant__ LayerQ4Params p, const __grid_cons
           slot_next = k + 1 == ua ? ub0 : slot + 1;
         } else {
           if (k + 1 < k1) slot_next = __ldcg(list + k + 1);
-          const bool wrong = slot <= slot_last || slot < 0 || slot >= sq.n / kLqPage;
+          const bool wrong = slot <= slot_last || slot < 0 || slot >= sq.full();
           if (wrong) {  // not above every one that counted, or no complete page: nothing of it is seen
             if (lane == 0) atomicOr(p.status, MC_FLAG_BAD_METADATA);
             slot = -1;
@@ -690,11 +688,11 @@ layer_q4_split_kernel(const __grid_constant__ LayerQ4Params p, const __grid_cons
           }
         }
         uint32_t hidden = 0;  // bit r: token t0 + r is not seen
-        const bool whole = (t0 + kLqPage <= sq.a || (t0 >= sq.lo && t0 + kLqPage <= sq.hi)) && slot >= 0;
+        const bool whole = sq.all_of(t0) && slot >= 0;
         if (!whole || unusual) {
           if (!whole) {
             const int t = t0 + lane;
-            hidden = ~__ballot_sync(0xffffffffu, slot >= 0 && (t < sq.a || (t >= sq.lo && t < sq.hi)));
+            hidden = ~__ballot_sync(0xffffffffu, slot >= 0 && sq.sees(t));
             if (p.rule.cap_log2 > 0.f) {  // (no say in which form of the cap the others take)
 #pragma unroll
               for (int c = 0; c < 4; ++c)
