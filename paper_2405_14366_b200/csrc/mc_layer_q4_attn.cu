@@ -21,10 +21,11 @@
 // A sequence's begun page and the step's new row, 16-bit rows, are a piece of their own: attended straight from global memory
 // while the first tiles are on their way, and the new row appended.  Partial results are joined by a second kernel.
 //
-// Bound by the memory and, as much, by what a tile's instructions take: 266 of the ALU, 150 of the FMA pipe and 34 of the tensor
-// cores per 5 KB, which add up on this part (8 mma.sync, 32 lop3 and 32 fma of three warps a scheduler: 153 cycles; each kind alone 65,
-// 64 and 33).  Measured, from a CUDA graph: 8 x 4109 tokens of 32 heads 38.7 us (170 MB: 25.9 us at a copy's rate, 28.5 for a kernel
-// that only reads them), 16 x 8192 of 8 kv heads under 32, capped, 42.2 us.  Of 33 us in a CTA 5 pass until its first tile is there.
+// Measured, from a CUDA graph: 8 x 4109 tokens of 32 heads 40.0 us (170 MB: 25.9 us at a copy's rate, 28.5 for a kernel that only reads
+// them), 16 x 8192 of 8 kv heads under 32, capped, 43.8 us, under 64 without a cap 48.3 us.  Bound by how the work is started, streamed
+// and joined more than by any unit: without arithmetic the 40.0 us are 33.0, without the combine kernel 36.8, without both 31.9 (copies
+// of the kernel that leave these out), and no pipe is full (issue 51 %, ALU 45 %, tensor cores 19 %, memory 47 %).  A step in which
+// every sequence's page fills: 74 us, as one warp quantises a page of K, then of V, from global memory.
 #include <algorithm>
 
 #include "mc_kernels.h"
@@ -612,7 +613,7 @@ layer_q4_split_kernel(const __grid_constant__ LayerQ4Params p, const __grid_cons
           for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int e = 0; e < 2; ++e) c4[h][e] = lds16(sb + k_off + (16 * h + 8 * e) * 64);
-          {  // (the latency of this, a load, a reduction and a branch, is 1.5 of 40 us; with it behind the products: 3 to 6 more)
+          {  // (the latency of this, a load, a reduction and a branch, is 1.5 of 40 us; behind the products it costs 3 to 6)
             const uint4 u = lds16(sb + kLqKMeta + 16 * lane);
             const uint32_t top = __reduce_max_sync(0xffffffffu, h2_max(h2_max(u.x, u.y), h2_max(u.z, u.w)) & 0x7fffu);
             if (top - kLqLeastTop >= kLqTops - kLqLeastTop) low = q4_rescale_keys(sb + kLqKMeta, top);

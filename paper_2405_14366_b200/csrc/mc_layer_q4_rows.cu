@@ -2,8 +2,10 @@
 //   layer_q4_append_kernel  rows behind the cached tokens: complete pages are quantised, the others stay 16-bit
 //   layer_q4_read_kernel    code * scale + zero of a range of tokens, as 16-bit rows
 // 512 bytes of 16-bit rows and 160 of codes and parameters per (token, kv head) are what they cannot do without: 107 us each for
-// 8 x 4096 tokens of 32 heads.  Reading takes 127 us; writing 153, bound by its 1500 instructions per page of K or V (65 % of the issue
-// slots).  A warp takes one (page, kv head) -- of K or V when it writes -- with all its loads in flight at once; neighbouring warps
+// 8 x 4096 tokens of 32 heads.  Reading takes 127 us; writing 153 (bfloat16 176: no mixed-precision subtraction), with no unit at its limit
+// (61 % of the issue slots, ALU 41 %, memory 52 %): 1500 instructions per page of K or V in 16 warps an SM, whose latencies show.
+// Keys with a channel whose scale is subnormal take the exact code for the whole page: 307 us if every page has one; values for four rows:
+// 233 us if every eighth row is next to zero.  A warp takes one (page, kv head) -- of K or V when it writes -- with all its loads in flight at once; neighbouring warps
 // take neighbouring heads, whose parts of a row are next to each other.
 #include <algorithm>
 
